@@ -1,4 +1,4 @@
-"""ctypes binding of the kb C ABI (include/kb.h): argument marshalling only.
+"""ctypes binding of the kb C ABI (include/kb.h, include/kb_ops.h): argument marshalling only.
 
 Every step of the path runs in the CUDA library; torch is used here for device
 memory and the current stream.  There is no CPU fallback: loading fails loudly
@@ -9,7 +9,7 @@ from __future__ import annotations
 import ctypes
 import os
 import sys
-from typing import Optional, Sequence
+from typing import NamedTuple, Optional, Sequence
 
 import numpy as np
 import torch
@@ -24,6 +24,8 @@ STATUS_NAMES = {
 }
 KB_F32, KB_F16, KB_BF16, KB_F8E4M3, KB_F8E5M2 = 0, 1, 2, 3, 4
 KB_SELECT_ERR_THEN_TIME, KB_SELECT_TIME = 0, 1
+KB_SCALE_ROWS, KB_SCALE_TILES = 0, 1
+KB_BLOCK = 128
 KB_TIMER_SCREEN_STREAM, KB_TIMER_WINS = 0, 1
 DTYPE_CODE = {torch.float32: KB_F32, torch.float16: KB_F16, torch.bfloat16: KB_BF16,
               torch.float8_e4m3fn: KB_F8E4M3, torch.float8_e5m2: KB_F8E5M2}
@@ -48,6 +50,7 @@ EXPORTS = [
     "kb_screen", "kb_screen_f64", "kb_screen_host", "kb_screen_static", "kb_screen_indexed", "kb_screen_multi", "kb_merge_ranges", "kb_adjudicate", "kb_adjudicate_ragged", "kb_select",
     "kb_select_by_score", "kb_tail_ratios", "kb_copeland", "kb_confirm",
     "kb_ctx_fail_next_allocs", "kb_ctx_selftest_wait", "kb_ctx_check_guards", "kb_static_scratch_read", "kb_ctx_set_filter", "kb_ctx_last_filter",
+    "kb_quantize_blocks", "kb_layernorm", "kb_layernorm_backward", "kb_matmul_blocks",
 ]
 
 
@@ -110,6 +113,10 @@ def load() -> ctypes.CDLL:
     L.kb_tail_ratios.argtypes = [vp, vp, u32, u32, vp, vp]
     L.kb_copeland.argtypes = [vp, vp, u32, u32, vp, vp, vp]
     L.kb_confirm.argtypes = [vp, vp, vp, vp, u32, f32, vp, vp, vp]
+    L.kb_quantize_blocks.argtypes = [vp, vp, u64, u64, u64, i32, i32, i32, vp, u64, i32, vp, vp]
+    L.kb_layernorm.argtypes = [vp, vp, u64, u64, u64, i32, vp, vp, i32, f32, vp, u64, vp, vp, vp, u64, i32, vp, vp]
+    L.kb_layernorm_backward.argtypes = [vp, vp, u64, vp, u64, u64, u64, i32, vp, i32, vp, vp, vp, u64, vp, vp, vp]
+    L.kb_matmul_blocks.argtypes = [vp, vp, u64, i32, vp, vp, u64, i32, vp, i32, u64, u64, u64, vp, u64, i32, vp]
     for name in EXPORTS:
         if name != "kb_last_error":
             getattr(L, name).restype = i32
@@ -584,6 +591,170 @@ def confirm(self, first: torch.Tensor, second: torch.Tensor, prev: torch.Tensor,
                            _stream_ptr(first.device))
     self._check(rc, "kb_confirm")
     return status, score
+
+
+# ---- model operators (include/kb_ops.h) ----------------------------------------------------
+
+class LayerNormResult(NamedTuple):
+    """What ``Context.layernorm`` returns; an output that was not asked for is None."""
+    y: Optional[torch.Tensor]
+    mean: Optional[torch.Tensor]
+    rstd: Optional[torch.Tensor]
+    q: Optional[torch.Tensor]
+    scale: Optional[torch.Tensor]
+
+
+def _rows(t: torch.Tensor, name: str, where: str, device) -> torch.Tensor:
+    """A tensor as a matrix [rows, columns] with adjacent columns, without copying: 2-D with any
+    row stride, or of any rank if its rows are evenly spaced."""
+    if t.device != device:
+        raise KbError(1, where, f"{name} must be on {device}")
+    if t.dim() != 2:
+        if t.dim() == 0 or not (t.is_contiguous() or t.numel() == 0):
+            raise KbError(1, where, f"{name} must be 2-D or contiguous")
+        t = t.view(t.numel() // t.shape[-1] if t.shape[-1] else 0, t.shape[-1])
+    rows, cols = t.shape
+    if (cols > 1 and t.stride(1) != 1) or (rows > 1 and t.stride(0) < cols):
+        raise KbError(1, where, f"the columns of {name} must be adjacent and its rows must not overlap")
+    return t
+
+
+def _ld(t: torch.Tensor) -> int:
+    """Row stride of a matrix; that of a single row is free (torch may report anything)."""
+    return max(t.stride(0), t.shape[1]) if t.shape[0] > 1 else (t.shape[1] + 15) // 16 * 16
+
+
+def _codes(rows: int, cols: int, dtype: torch.dtype, device) -> torch.Tensor:
+    """Room for 8-bit codes [rows, cols] whose rows start on 16-byte boundaries."""
+    if cols % 16 == 0:
+        return torch.empty((rows, cols), dtype=dtype, device=device)
+    return torch.empty((rows, (cols + 15) // 16 * 16), dtype=dtype, device=device)[:, :cols]
+
+
+def _vector(t: Optional[torch.Tensor], n: int, name: str, where: str, device, dtypes):
+    """(address, dtype) of an optional contiguous vector of n elements."""
+    if t is None:
+        return None, None
+    if t.numel() != n or not t.is_contiguous() or t.device != device or t.dtype not in dtypes:
+        raise KbError(1, where, f"{name} must be a contiguous tensor of {n} elements of "
+                                f"{' or '.join(str(d) for d in dtypes)} on {device}")
+    return t.data_ptr(), t.dtype
+
+
+@_ctx_method
+def quantize_blocks(self, x: torch.Tensor, dtype: torch.dtype = torch.float8_e4m3fn, *, tiles: bool = False,
+                    transpose: bool = False):
+    """kb_quantize_blocks: ``x`` [rows, cols] (or its transpose) as 8-bit codes with a binary32
+    scale per 1 x 128 block along the columns, or per 128 x 128 tile -> (q, scale).
+
+    q [R, C] has rows on 16-byte boundaries; scale is [ceil(C/128), R], with tiles
+    [ceil(C/128), ceil(R/128)].
+    """
+    x = _rows(x, "x", "kb_quantize_blocks", self.device)
+    rows, cols = x.shape
+    R, C = (cols, rows) if transpose else (rows, cols)
+    q = _codes(R, C, dtype, self.device)
+    scale = torch.empty((-(-C // KB_BLOCK), -(-R // KB_BLOCK) if tiles else R), dtype=torch.float32,
+                        device=self.device)
+    rc = load().kb_quantize_blocks(self._h, x.data_ptr(), rows, cols, _ld(x), DTYPE_CODE.get(x.dtype, -1),
+                                   int(bool(transpose)), KB_SCALE_TILES if tiles else KB_SCALE_ROWS,
+                                   q.data_ptr(), _ld(q), DTYPE_CODE.get(dtype, -1), scale.data_ptr(),
+                                   _stream_ptr(self.device))
+    self._check(rc, "kb_quantize_blocks")
+    return q, scale
+
+
+@_ctx_method
+def layernorm(self, x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None,
+              eps: float = 1e-5, *, want_y: bool = True, want_stats: bool = True,
+              quantize: Optional[torch.dtype] = None) -> LayerNormResult:
+    """kb_layernorm over the last dimension of ``x``.
+
+    ``quantize`` (an 8-bit float type) also, or with ``want_y`` false only, returns the result as
+    codes q and scales as ``quantize_blocks`` lays them out, ready for ``matmul_blocks``;
+    ``want_stats`` returns each row's mean and 1/sqrt(var + eps) for the backward pass.
+    """
+    where = "kb_layernorm"
+    x2 = _rows(x, "x", where, self.device)
+    rows, cols = x2.shape
+    kinds = (x.dtype, torch.float32)
+    w, wt = _vector(weight, cols, "weight", where, self.device, kinds)
+    b, bt = _vector(bias, cols, "bias", where, self.device, kinds)
+    if wt is not None and bt is not None and wt != bt:
+        raise KbError(1, where, "weight and bias must have the same type")
+    y = torch.empty(x.shape, dtype=x.dtype, device=self.device) if want_y else None
+    mean = rstd = q = scale = None
+    if want_stats:
+        mean, rstd = torch.empty((2, rows), dtype=torch.float32, device=self.device).unbind(0)
+    if quantize is not None:
+        q = _codes(rows, cols, quantize, self.device)
+        scale = torch.empty((-(-cols // KB_BLOCK), rows), dtype=torch.float32, device=self.device)
+    if rows == 0:
+        return LayerNormResult(y, mean, rstd, q, scale)
+    rc = load().kb_layernorm(self._h, x2.data_ptr(), rows, cols, _ld(x2), DTYPE_CODE.get(x.dtype, -1), w, b,
+                             DTYPE_CODE.get(wt or bt or x.dtype, -1), float(eps),
+                             y.data_ptr() if want_y else None, cols,
+                             mean.data_ptr() if want_stats else None, rstd.data_ptr() if want_stats else None,
+                             q.data_ptr() if q is not None else None, _ld(q) if q is not None else 0,
+                             DTYPE_CODE.get(quantize, -1) if q is not None else KB_F8E4M3,
+                             scale.data_ptr() if q is not None else None, _stream_ptr(self.device))
+    self._check(rc, where)
+    return LayerNormResult(y, mean, rstd, q, scale)
+
+
+@_ctx_method
+def layernorm_backward(self, dy: torch.Tensor, x: torch.Tensor, weight: Optional[torch.Tensor], mean: torch.Tensor,
+                       rstd: torch.Tensor, *, want_bias: bool = True):
+    """kb_layernorm_backward -> (dx, dweight, dbias), the parameters' gradients in the weight's
+    type (binary32 without a weight); dbias is None unless ``want_bias``."""
+    where = "kb_layernorm_backward"
+    dy2, x2 = _rows(dy, "dy", where, self.device), _rows(x, "x", where, self.device)
+    rows, cols = x2.shape
+    if dy2.shape != x2.shape or dy.dtype != x.dtype:
+        raise KbError(1, where, "dy must have the shape and type of x")
+    w, wt = _vector(weight, cols, "weight", where, self.device, (x.dtype, torch.float32))
+    m, _ = _vector(mean, rows, "mean", where, self.device, (torch.float32,))
+    r, _ = _vector(rstd, rows, "rstd", where, self.device, (torch.float32,))
+    dx = torch.empty(x.shape, dtype=x.dtype, device=self.device)
+    dweight = torch.empty(cols, dtype=wt or torch.float32, device=self.device)
+    dbias = torch.empty(cols, dtype=wt or torch.float32, device=self.device) if want_bias else None
+    rc = load().kb_layernorm_backward(self._h, dy2.data_ptr(), _ld(dy2), x2.data_ptr(), _ld(x2), rows, cols,
+                                      DTYPE_CODE.get(x.dtype, -1), w, DTYPE_CODE.get(wt or torch.float32, -1), m, r,
+                                      dx.data_ptr(), cols, dweight.data_ptr(),
+                                      dbias.data_ptr() if want_bias else None, _stream_ptr(self.device))
+    self._check(rc, where)
+    return dx, dweight, dbias
+
+
+@_ctx_method
+def matmul_blocks(self, a: torch.Tensor, a_scale: torch.Tensor, b: torch.Tensor, b_scale: torch.Tensor,
+                  out_dtype: torch.dtype = torch.bfloat16, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """kb_matmul_blocks: A B^T of two block-quantised matrices a [M, K] and b [N, K] (as
+    ``quantize_blocks`` or ``layernorm`` made them) -> [M, N] in ``out_dtype``.
+
+    a_scale is [ceil(K/128), M]; b_scale is [ceil(K/128), ceil(N/128)] (tiles) or
+    [ceil(K/128), N] (rows).  ``out``: where to write the result (a 2-D tensor with adjacent columns).
+    """
+    where = "kb_matmul_blocks"
+    a, b = _rows(a, "a", where, self.device), _rows(b, "b", where, self.device)
+    (M, K), (N, Kb) = a.shape, b.shape
+    kb = -(-K // KB_BLOCK)
+    if Kb != K:
+        raise KbError(1, where, f"a has {K} columns, b {Kb}")
+    tiles = b_scale.shape != (kb, N)
+    sa, _ = _vector(a_scale, kb * M, "a_scale", where, self.device, (torch.float32,))
+    sb, _ = _vector(b_scale, kb * (-(-N // KB_BLOCK) if tiles else N), "b_scale", where, self.device, (torch.float32,))
+    if a_scale.shape != (kb, M) or b_scale.dim() != 2 or b_scale.shape[0] != kb:
+        raise KbError(1, where, "scales are laid out [ceil(K/128), rows] or [ceil(K/128), ceil(rows/128)]")
+    if out is None:
+        out = torch.empty((M, N), dtype=out_dtype, device=self.device)
+    elif out.shape != (M, N) or _rows(out, "out", where, self.device) is not out:
+        raise KbError(1, where, f"out must be a matrix [{M}, {N}]")
+    rc = load().kb_matmul_blocks(self._h, a.data_ptr(), _ld(a), DTYPE_CODE.get(a.dtype, -1), sa, b.data_ptr(), _ld(b),
+                                 DTYPE_CODE.get(b.dtype, -1), sb, KB_SCALE_TILES if tiles else KB_SCALE_ROWS, M, N, K,
+                                 out.data_ptr(), _ld(out), DTYPE_CODE.get(out.dtype, -1), _stream_ptr(self.device))
+    self._check(rc, where)
+    return out
 
 
 def records_f64(screen_out: torch.Tensor) -> np.ndarray:

@@ -1,7 +1,8 @@
 """Build the CUDA library in-tree:  python -m paper_2608_02611_b200.build
 
-One translation unit (csrc/kb_host.cu) compiled by nvcc for sm_100a into
-paper_2608_02611_b200/libkb.so, a plain C-ABI shared library (include/kb.h).
+Two translation units (csrc/kb_host.cu: the gate, adjudication and selection; csrc/kb_ops.cu:
+the model operators) compiled by nvcc for sm_100a into paper_2608_02611_b200/libkb.so, a plain
+C-ABI shared library (include/kb.h, include/kb_ops.h).
 """
 from __future__ import annotations
 
@@ -12,13 +13,12 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libkb.so")
-SOURCES = ["kb_host.cu"]
-DEPS = ["kb_host.cu", "kb_common.cuh", "kb_screen.cuh", "kb_screen8.cuh", "kb_ring.cuh", "kb_screen64.cuh", "kb_adjudicate.cuh", "kb_select.cuh",
-        os.path.join("..", "..", "include", "kb.h"), os.path.join("..", "..", "include", "kb_hooks.h")]
+SOURCES = ["kb_host.cu", "kb_ops.cu"]
+INCLUDE = os.path.join(HERE, "..", "include")
 
 NVCC_FLAGS = [
     "-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
-    "-Xcompiler", "-fPIC", "-Xcompiler", "-Wno-format-truncation", "-shared", "-ldl",
+    "-Xcompiler", "-fPIC", "-Xcompiler", "-Wno-format-truncation", "-shared", "-ldl", "--threads=2",
 ]
 
 
@@ -26,7 +26,8 @@ def stale() -> bool:
     if not os.path.exists(LIB):
         return True
     t = os.path.getmtime(LIB)
-    return any(os.path.getmtime(os.path.join(CSRC, d)) > t for d in DEPS)
+    deps = [os.path.join(d, f) for d in (CSRC, INCLUDE) for f in os.listdir(d) if f.endswith((".cu", ".cuh", ".h"))]
+    return any(os.path.getmtime(f) > t for f in deps)
 
 
 def build(force: bool = False, verbose: bool = False) -> str:

@@ -1,0 +1,216 @@
+// What the model operators share: a warp's view of a row in groups of 256 elements, and the
+// quantisation of blocks of 128 to 8-bit floating point.
+//
+// A warp handles a row in groups of 256 consecutive elements, 8 per lane, i.e. two quantisation
+// blocks.  Rows that start on 16-byte boundaries and are a multiple of 8 long (VEC) give lane l
+// the elements 8l..8l+7, so that it loads and stores 16-byte vectors and 16 lanes hold a block.
+// All other rows give it the elements l, 32+l, ..., 224+l: every load and store of the warp is
+// still one contiguous piece, and elements j < 4 and j >= 4 of all lanes hold a block each.
+#pragma once
+
+#include <cuda_bf16.h>
+
+#include "kb_common.cuh"
+
+namespace kb {
+
+constexpr uint32_t kGroup = 256;
+
+template <bool VEC>
+__device__ __forceinline__ uint32_t group_col(uint32_t g, int lane, int j) {
+  return g * kGroup + (VEC ? lane * 8 + j : j * 32 + lane);
+}
+
+// ---- storage types ------------------------------------------------------------------------
+template <int DT>
+__device__ __forceinline__ float load_elem(const void* p, uint64_t i) {
+  return Elem<DT>::load(p, i);
+}
+template <int DT>
+__device__ __forceinline__ void store_elem(void* p, uint64_t i, float v) {
+  if constexpr (DT == KB_F32)
+    reinterpret_cast<float*>(p)[i] = v;
+  else if constexpr (DT == KB_BF16)
+    reinterpret_cast<__nv_bfloat16*>(p)[i] = __float2bfloat16_rn(v);
+  else
+    reinterpret_cast<__half*>(p)[i] = __float2half_rn(v);
+}
+template <int DT>
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {   // 16-bit types
+  if constexpr (DT == KB_BF16) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&h);
+  } else {
+    const __half2 h = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&h);
+  }
+}
+// 8 consecutive elements from / to a 16-byte aligned place
+template <int DT>
+__device__ __forceinline__ void load8(const void* p, uint64_t i, float (&v)[8]) {
+  if constexpr (DT == KB_F32) {
+    const uint4* q = reinterpret_cast<const uint4*>(reinterpret_cast<const float*>(p) + i);
+    const uint4 a = q[0], b = q[1];
+    Elem<DT>::decode(a, v);
+    Elem<DT>::decode(b, v + 4);
+  } else {
+    const uint4 a = *reinterpret_cast<const uint4*>(reinterpret_cast<const unsigned short*>(p) + i);
+    Elem<DT>::decode(a, v);
+  }
+}
+template <int DT>
+__device__ __forceinline__ void store8(void* p, uint64_t i, const float (&v)[8]) {
+  if constexpr (DT == KB_F32) {
+    float4* q = reinterpret_cast<float4*>(reinterpret_cast<float*>(p) + i);
+    q[0] = make_float4(v[0], v[1], v[2], v[3]);
+    q[1] = make_float4(v[4], v[5], v[6], v[7]);
+  } else {
+    *reinterpret_cast<uint4*>(reinterpret_cast<unsigned short*>(p) + i) =
+        make_uint4(pack2<DT>(v[0], v[1]), pack2<DT>(v[2], v[3]), pack2<DT>(v[4], v[5]), pack2<DT>(v[6], v[7]));
+  }
+}
+
+// A lane's 8 elements of group g of a row that starts at element `row0`; elements past the row's
+// end read as `fill`.
+template <int DT, bool VEC>
+__device__ __forceinline__ void load_group(const void* base, uint64_t row0, uint32_t g, int lane, uint32_t cols,
+                                           float (&v)[8], float fill = 0.0f) {
+  if constexpr (VEC) {
+    const uint32_t c = group_col<true>(g, lane, 0);
+    if (c < cols) {
+      load8<DT>(base, row0 + c, v);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = fill;
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const uint32_t c = group_col<false>(g, lane, j);
+      v[j] = c < cols ? load_elem<DT>(base, row0 + c) : fill;
+    }
+  }
+}
+template <int DT, bool VEC>
+__device__ __forceinline__ void store_group(void* base, uint64_t row0, uint32_t g, int lane, uint32_t cols,
+                                            const float (&v)[8]) {
+  if constexpr (VEC) {
+    const uint32_t c = group_col<true>(g, lane, 0);
+    if (c < cols) store8<DT>(base, row0 + c, v);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const uint32_t c = group_col<false>(g, lane, j);
+      if (c < cols) store_elem<DT>(base, row0 + c, v[j]);
+    }
+  }
+}
+// Parameters [cols] of the row's own type or of binary32 (f32), or none (value `none`).
+template <int DT, bool VEC>
+__device__ __forceinline__ void load_params(const void* base, bool f32, uint32_t g, int lane, uint32_t cols,
+                                            float none, float (&v)[8]) {
+  if (base == nullptr) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = none;
+  } else if (DT == KB_F32 || f32) {
+    load_group<KB_F32, VEC>(base, 0, g, lane, cols, v);
+  } else {
+    load_group<DT, VEC>(base, 0, g, lane, cols, v);
+  }
+}
+
+// ---- 8-bit quantisation ---------------------------------------------------------------------
+// The block's scale S = a / F and the factor F / a its elements are multiplied with, a >= 2^-100
+// (so that neither quotient leaves the normal range, whatever the block holds).
+struct BlockScale {
+  float scale, inv;
+};
+template <bool E5M2>
+__device__ __forceinline__ BlockScale block_scale(float amax) {
+  constexpr float top = E5M2 ? 57344.0f : 448.0f;
+  const float a = fmaxf(amax, 0x1p-100f);
+  return {__fdiv_rn(a, top), __fdiv_rn(top, a)};
+}
+constexpr unsigned int kInfBits = 0x7F800000u;
+__device__ __forceinline__ unsigned int abs_bits(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
+// Two values to two codes (lo in the low byte), saturating; NaN becomes NaN.
+template <bool E5M2>
+__device__ __forceinline__ uint32_t quant2(float lo, float hi) {
+  unsigned short r;
+  if (E5M2)
+    asm("cvt.rn.satfinite.e5m2x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+  else
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+template <bool E5M2>
+__device__ __forceinline__ uint2 quant8(const float (&v)[8], float inv) {
+  uint2 r;
+  r.x = quant2<E5M2>(__fmul_rn(v[0], inv), __fmul_rn(v[1], inv)) |
+        quant2<E5M2>(__fmul_rn(v[2], inv), __fmul_rn(v[3], inv)) << 16;
+  r.y = quant2<E5M2>(__fmul_rn(v[4], inv), __fmul_rn(v[5], inv)) |
+        quant2<E5M2>(__fmul_rn(v[6], inv), __fmul_rn(v[7], inv)) << 16;
+  return r;
+}
+// Largest magnitude as bits; magnitudes order like their bit patterns, Inf and NaN above all
+// finite ones, so one integer maximum also tells whether a block holds any.
+template <int J0, int J1>
+__device__ __forceinline__ unsigned int max_bits(const float (&v)[8]) {
+  unsigned int m = 0u;
+#pragma unroll
+  for (int j = J0; j < J1; ++j) m = max(m, abs_bits(v[j]));
+  return m;
+}
+// Non-finite values of a block that holds some become NaN; returns the largest finite magnitude.
+template <int J0, int J1>
+__device__ __forceinline__ unsigned int settle_nonfinite(float (&v)[8]) {
+  unsigned int m = 0u;
+#pragma unroll
+  for (int j = J0; j < J1; ++j) {
+    if (abs_bits(v[j]) >= kInfBits)
+      v[j] = __uint_as_float(0x7FFFFFFFu);
+    else
+      m = max(m, abs_bits(v[j]));
+  }
+  return m;
+}
+
+// Quantise a lane's part of group g of row `row`: codes to q, the blocks' scales to
+// scale[block][row].  All 32 lanes take part; elements past the row's end must be 0.
+template <bool E5M2, bool VEC>
+__device__ __forceinline__ void quant_group(float (&v)[8], uint32_t g, int lane, uint32_t cols, uint64_t row,
+                                            uint64_t rows, unsigned char* q, uint64_t ldq, float* scale) {
+  if constexpr (VEC) {
+    const uint32_t c = group_col<true>(g, lane, 0);
+    const unsigned int half = 0xFFFFu << (lane & 16);
+    unsigned int m = max_bits<0, 8>(v);
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(half, m, o));
+    if (m >= kInfBits) {   // the same for the block's 16 lanes
+      m = settle_nonfinite<0, 8>(v);
+#pragma unroll
+      for (int o = 8; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(half, m, o));
+    }
+    const BlockScale s = block_scale<E5M2>(__uint_as_float(m));
+    if (c < cols) {
+      *reinterpret_cast<uint2*>(q + row * ldq + c) = quant8<E5M2>(v, s.inv);
+      if ((lane & 15) == 0) scale[(uint64_t)(c >> 7) * rows + row] = s.scale;
+    }
+  } else {
+    unsigned int m0 = warp_max_u32(max_bits<0, 4>(v)), m1 = warp_max_u32(max_bits<4, 8>(v));
+    if (m0 >= kInfBits) m0 = warp_max_u32(settle_nonfinite<0, 4>(v));
+    if (m1 >= kInfBits) m1 = warp_max_u32(settle_nonfinite<4, 8>(v));
+    const BlockScale s0 = block_scale<E5M2>(__uint_as_float(m0)), s1 = block_scale<E5M2>(__uint_as_float(m1));
+    const uint2 r0 = quant8<E5M2>(v, s0.inv), r1 = quant8<E5M2>(v, s1.inv);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const uint32_t c = group_col<false>(g, lane, j);
+      const uint32_t w = j < 4 ? r0.x : r1.y;
+      if (c < cols) q[row * ldq + c] = (unsigned char)(w >> (8 * (j & 3)));
+    }
+    const uint32_t kb = g * 2 + lane;   // lanes 0 and 1: the group's two blocks
+    if (lane < 2 && kb * 128u < cols) scale[(uint64_t)kb * rows + row] = lane ? s1.scale : s0.scale;
+  }
+}
+
+}  // namespace kb

@@ -227,20 +227,6 @@ __device__ __forceinline__ bool mbar_wait_bounded(uint64_t* bar, uint32_t parity
     }
   }
 }
-// Self-test of the wait above (kb_ctx_selftest_wait): one warp waits on a barrier that nothing
-// completes.  No copy is in flight, so giving up leaves nothing behind; the kernel returns
-// normally with KB_ERR_DEVICE_TIMEOUT in the status word.
-__global__ void wait_selftest_kernel(unsigned int* status, unsigned long long limit_ns) {
-  __shared__ uint64_t bar;
-  __shared__ unsigned int abort_flag;
-  if (threadIdx.x == 0) {
-    mbar_init(&bar, 1);
-    abort_flag = 0u;
-    mbar_fence_init();
-  }
-  __syncwarp();
-  mbar_wait_bounded(&bar, 0u, &abort_flag, status, limit_ns);
-}
 
 __device__ __forceinline__ uint64_t l2_policy_evict_first() {
   uint64_t pol;

@@ -1,0 +1,249 @@
+// Product of two 8-bit matrices with a binary32 scale per block of 128 along K (contract in
+// include/kb_ops.h):
+//     D[m][n] = sum_kb SA[kb][m] * SB[kb][n or n/128] * sum_{k in kb} A[m][k] * B[n][k]
+//
+// The scales differ from one K block of 128 to the next, so the tensor cores cannot add across
+// blocks: each block's 128-deep product goes to an accumulator of its own in tensor memory, and
+// the epilogue warps multiply it with its scales and add it to running sums in registers while
+// the tensor cores are at the next blocks.  K blocks are also the unit of the copies: a stage of
+// the shared-memory ring is one block of both operands, 128 bytes per row in the 128-byte
+// swizzle, and takes 4 matrix instructions.
+//
+// Roles: warp 0 copies (tensor maps; rows and columns outside a matrix read as zero), warp 1
+// issues matrix instructions, four warps scale and add.  Every wait is bounded.
+#pragma once
+
+#include "kb_block8.cuh"
+#include "kb_tcgen05.cuh"
+
+namespace kb {
+
+struct MatmulParams {
+  const float* a_scale;      // [KB][M]
+  const float* b_scale;      // [KB][N] or [KB][ceil(N/128)]
+  void* d;
+  uint64_t ldd;
+  uint32_t M, N, KB;
+  uint32_t b_scale_ld;       // N or ceil(N/128)
+  uint32_t b_scale_shift;    // 0 or 7
+  uint32_t tiles_m;          // column tiles (of A's rows)
+  uint32_t splits;           // CTAs per tile along K (a cluster)
+  uint32_t idesc;
+  int out;                   // kb_dtype of D
+  unsigned int* status;
+};
+
+__device__ __forceinline__ void store_out(void* d, int out, uint64_t i, float v) {
+  if (out == KB_BF16)
+    store_elem<KB_BF16>(d, i, v);
+  else if (out == KB_F16)
+    store_elem<KB_F16>(d, i, v);
+  else
+    store_elem<KB_F32>(d, i, v);
+}
+
+// After a wait has run out: let the copies already issued land, for a second at most.
+__device__ __forceinline__ void drain_copies(uint64_t* full, uint32_t stages, uint64_t issued) {
+  const uint64_t back = issued < stages ? issued : stages;
+  for (uint64_t m = issued - back; m < issued; ++m) {
+    const unsigned long long t0 = global_ns();
+    while (!mbar_try_wait(&full[m % stages], (uint32_t)((m / stages) & 1ull)))
+      if (global_ns() - t0 > 1000000000ull) break;
+  }
+}
+
+// ---- few rows of A ---------------------------------------------------------------------------
+// The rows of B (weights) take the 128 lanes of the tile and BN rows of A its columns, so that a
+// single token wastes no lanes and the weights stream through once.  A cluster of `splits` CTAs
+// shares a tile's K blocks; the partial sums are added over distributed shared memory in rank
+// order.
+template <int BN>
+struct LaneTile {
+  static constexpr uint32_t kStageBytes = (128 + BN) * 128;
+  static constexpr uint32_t kStages = BN == 128 ? 6 : BN == 64 ? 8 : 10;
+  static constexpr uint32_t kAcc = BN == 128 ? 2 : 4;          // accumulators in tensor memory
+  static constexpr uint32_t kTmemCols = kAcc * BN;
+  static constexpr uint32_t kSmem = 1024 + kStages * kStageBytes;
+  static constexpr int kThreads = 192;
+};
+
+template <int BN>
+__global__ void __launch_bounds__(LaneTile<BN>::kThreads, 1)
+    matmul_lanes_kernel(const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_a,
+                        const MatmulParams p) {
+  using T = LaneTile<BN>;
+  extern __shared__ unsigned char dyn[];
+  __shared__ uint64_t full[T::kStages], empty[T::kStages], acc_full[T::kAcc], acc_empty[T::kAcc], drained;
+  __shared__ uint32_t tmem_base;
+  __shared__ unsigned int abort_word;
+  __shared__ __align__(16) float col_scale[4][2][BN];
+  volatile unsigned int* abort_flag = &abort_word;
+  unsigned char* stages = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(dyn) + 1023) & ~(uintptr_t)1023);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = p.splits > 1 ? cluster_rank() : 0;
+  const uint32_t tile = blockIdx.x / p.splits;
+  const uint32_t n0 = tile / p.tiles_m * 128, m0 = tile % p.tiles_m * BN;
+  const uint32_t kb0 = (uint32_t)((uint64_t)p.KB * rank / p.splits);
+  const uint32_t nkb = (uint32_t)((uint64_t)p.KB * (rank + 1) / p.splits) - kb0;
+
+  if (threadIdx.x == 0) {
+    for (uint32_t i = 0; i < T::kStages; ++i) {
+      mbar_init(&full[i], 1);
+      mbar_init(&empty[i], 1);
+    }
+    for (uint32_t i = 0; i < T::kAcc; ++i) {
+      mbar_init(&acc_full[i], 1);
+      mbar_init(&acc_empty[i], 4);
+    }
+    mbar_init(&drained, 1);
+    abort_word = 0u;
+    mbar_fence_init();
+  }
+  if (warp == 1) tmem_alloc<1>(&tmem_base, T::kTmemCols);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = tmem_base;
+
+  float acc[BN];
+  bool ok = true;
+  if (warp == 0) {
+    if (lane == 0) {
+      uint32_t st = 0, phase = 0, issued = 0;
+      for (uint32_t i = 0; i < nkb; ++i) {
+        if (!mbar_wait_bounded(&empty[st], phase ^ 1u, abort_flag, p.status)) {
+          drain_copies(full, T::kStages, issued);
+          break;
+        }
+        unsigned char* s = stages + st * T::kStageBytes;
+        mbar_arrive_expect_tx(&full[st], T::kStageBytes);
+        tma_load_2d(s, &map_b, (int)((kb0 + i) * 128), (int)n0, &full[st]);
+        tma_load_2d(s + 128 * 128, &map_a, (int)((kb0 + i) * 128), (int)m0, &full[st]);
+        ++issued;
+        if (++st == T::kStages) {
+          st = 0;
+          phase ^= 1u;
+        }
+      }
+    }
+    __syncwarp();
+  } else if (warp == 1) {
+    if (lane == 0) {
+      uint32_t st = 0, phase = 0;
+      for (uint32_t i = 0; i < nkb; ++i) {
+        const uint32_t a = i % T::kAcc, a_phase = (i / T::kAcc) & 1u;
+        if (!mbar_wait_bounded(&acc_empty[a], a_phase ^ 1u, abort_flag, p.status) ||
+            !mbar_wait_bounded(&full[st], phase, abort_flag, p.status)) {
+          mma_commit(&drained);   // what has been issued ends before tensor memory is freed
+          const unsigned long long t0 = global_ns();
+          while (!mbar_try_wait(&drained, 0))
+            if (global_ns() - t0 > 1000000000ull) break;
+          break;
+        }
+        tc_fence_after();
+        const uint32_t s = smem_u32(stages + st * T::kStageBytes);
+        const uint64_t lanes_desc = smem_desc_k128(s), cols_desc = smem_desc_k128(s + 128 * 128);
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          mma_f8<1>(tmem + a * BN, lanes_desc + 2 * k, cols_desc + 2 * k, p.idesc, k > 0);
+        mma_commit(&empty[st]);
+        mma_commit(&acc_full[a]);
+        if (++st == T::kStages) {
+          st = 0;
+          phase ^= 1u;
+        }
+      }
+    }
+    __syncwarp();
+  } else {
+    const int quarter = warp & 3;                       // the lanes of tensor memory this warp may read
+    const uint32_t n = n0 + quarter * 32 + lane;
+    const float* bs = p.b_scale + (n >> p.b_scale_shift);
+    const bool n_in = n < p.N;
+    float (*cs)[BN] = col_scale[quarter];
+    constexpr int kPer = (BN + 31) / 32;
+    float next_col[kPer], next_lane = 0.0f;
+    auto fetch = [&](uint32_t kb) {
+      if (n_in) next_lane = bs[(uint64_t)kb * p.b_scale_ld];
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        const uint32_t m = m0 + i * 32 + lane;
+        next_col[i] = (i * 32 + lane < BN && m < p.M) ? p.a_scale[(uint64_t)kb * p.M + m] : 0.0f;
+      }
+    };
+#pragma unroll
+    for (int j = 0; j < BN; ++j) acc[j] = 0.0f;
+    if (nkb) fetch(kb0);
+    for (uint32_t i = 0; i < nkb; ++i) {
+      const uint32_t a = i % T::kAcc, a_phase = (i / T::kAcc) & 1u;
+      float* c = cs[i & 1];
+#pragma unroll
+      for (int k = 0; k < kPer; ++k)
+        if (k * 32 + lane < BN) c[k * 32 + lane] = next_col[k];
+      const float ls = next_lane;
+      __syncwarp();
+      if (i + 1 < nkb) fetch(kb0 + i + 1);
+      if (!__all_sync(0xFFFFFFFFu, mbar_wait_bounded(&acc_full[a], a_phase, abort_flag, p.status))) {
+        ok = false;
+        break;
+      }
+      tc_fence_after();
+      const uint32_t addr = tmem + ((uint32_t)(quarter * 32) << 16) + a * BN;
+      constexpr int kStep = BN < 32 ? 16 : 32;
+#pragma unroll
+      for (int j0 = 0; j0 < BN; j0 += kStep) {
+        float v[kStep];
+        if constexpr (kStep == 16)
+          tmem_ld16(addr + j0, v);
+        else
+          tmem_ld32(addr + j0, v);
+        tmem_wait_ld();
+        if (j0 + kStep == BN) {   // all of this accumulator is in registers
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&acc_empty[a]);
+        }
+#pragma unroll
+        for (int j = 0; j < kStep; j += 4) {
+          const float4 f = *reinterpret_cast<const float4*>(c + j0 + j);
+          acc[j0 + j] = fmaf(v[j] * f.x, ls, acc[j0 + j]);
+          acc[j0 + j + 1] = fmaf(v[j + 1] * f.y, ls, acc[j0 + j + 1]);
+          acc[j0 + j + 2] = fmaf(v[j + 2] * f.z, ls, acc[j0 + j + 2]);
+          acc[j0 + j + 3] = fmaf(v[j + 3] * f.w, ls, acc[j0 + j + 3]);
+        }
+      }
+    }
+    if (p.splits == 1 && ok && n_in) {
+#pragma unroll
+      for (int j = 0; j < BN; ++j)
+        if (m0 + j < p.M) store_out(p.d, p.out, (uint64_t)(m0 + j) * p.ldd + n, acc[j]);
+    }
+    if (p.splits > 1) {
+      // all copies and matrix instructions of this CTA are done: the ring holds the partial sums
+      float* red = reinterpret_cast<float*>(stages) + quarter * 32 + lane;
+#pragma unroll
+      for (int j = 0; j < BN; ++j) red[j * 128] = ok ? acc[j] : 0.0f;
+    }
+  }
+  if (p.splits > 1) {
+    cluster_sync_all();
+    if (warp >= 2) {
+      const int row = (warp & 3) * 32 + lane;
+      const uint32_t n = n0 + row;
+      const uint32_t per = BN / p.splits;
+      const uint32_t base = smem_u32(stages) + row * 4;
+      for (uint32_t j = rank * per; j < (rank + 1) * per; ++j) {
+        float s = 0.0f;
+        for (uint32_t r = 0; r < p.splits; ++r) s += ld_cluster_f32(map_to_rank(base + j * 512, r));
+        if (n < p.N && m0 + j < p.M && ok) store_out(p.d, p.out, (uint64_t)(m0 + j) * p.ldd + n, s);
+      }
+    }
+    cluster_sync_all();   // no CTA leaves while another reads its shared memory
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (warp == 1) tmem_free<1>(tmem, T::kTmemCols);
+}
+
+}  // namespace kb

@@ -1,0 +1,430 @@
+// Host side of the model operators: argument checks, choice of kernel, launch.
+// Declarations and their contracts are in include/kb_ops.h.
+#include <algorithm>
+#include <cmath>
+
+#include "../../include/kb_ops.h"
+#include "kb_ctx.cuh"
+#include "kb_matmul.cuh"
+#include "kb_norm.cuh"
+#include "kb_quant.cuh"
+
+using namespace kb;
+
+namespace {
+
+inline bool is_float_type(int dt) { return dt == KB_F32 || dt == KB_F16 || dt == KB_BF16; }
+inline bool is_f8_type(int dt) { return dt == KB_F8E4M3 || dt == KB_F8E5M2; }
+inline bool aligned_to(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+// rows of a matrix start on 16-byte boundaries
+inline bool rows_aligned(const void* p, uint64_t ld, int bytes) { return aligned16(p) && (ld * bytes) % 16 == 0; }
+
+// A matrix argument: not null, element-aligned, leading dimension at least its columns.
+kb_status check_matrix(kb_ctx* ctx, const char* where, const char* name, const void* p, uint64_t cols, uint64_t ld,
+                       int bytes) {
+  if (!p) return fail(ctx, KB_ERR_INVALID_ARG, "%s: %s is NULL", where, name);
+  if (!aligned_to(p, bytes)) return fail(ctx, KB_ERR_ALIGNMENT, "%s: %s is not aligned to its element type", where, name);
+  if (ld < cols)
+    return fail(ctx, KB_ERR_INVALID_ARG, "%s: leading dimension %llu of %s is less than its %llu columns", where,
+                (unsigned long long)ld, name, (unsigned long long)cols);
+  return KB_OK;
+}
+kb_status check_vector(kb_ctx* ctx, const char* where, const char* name, const void* p, int bytes) {
+  if (!aligned_to(p, bytes)) return fail(ctx, KB_ERR_ALIGNMENT, "%s: %s is not aligned to its element type", where, name);
+  return KB_OK;
+}
+#define KB_TRY(call)                     \
+  do {                                   \
+    const kb_status rc_ = (call);        \
+    if (rc_ != KB_OK) return rc_;        \
+  } while (0)
+
+kb_status launched(kb_ctx* ctx) {
+  ++ctx->launches;
+  KB_CUDA(ctx, cudaGetLastError());
+  return KB_OK;
+}
+
+// ---- quantisation ------------------------------------------------------------------------------
+
+template <int DT, bool VEC, bool E5M2>
+kb_status launch_quant(kb_ctx* ctx, const QuantParams& p, bool transpose, bool tiles, cudaStream_t st) {
+  if (!transpose && !tiles) {
+    const uint64_t pieces = (p.groups + kQuantRowGroups - 1) / kQuantRowGroups;
+    const dim3 grid((unsigned int)((p.rows + 7) / 8), (unsigned int)std::min<uint64_t>(pieces, 65535));
+    quant_rows_kernel<DT, VEC, E5M2><<<grid, 256, 0, st>>>(p);
+    return launched(ctx);
+  }
+  const uint64_t n = (uint64_t)p.rtiles * p.ctiles;
+  if (n > 0x7FFFFFFFull) return fail(ctx, KB_ERR_UNSUPPORTED, "kb_quantize_blocks: more than 2^31 - 1 tiles");
+  const unsigned int grid = (unsigned int)n;
+  if (tiles && transpose)
+    quant_tile_kernel<DT, VEC, E5M2, true, true><<<grid, 256, 0, st>>>(p);
+  else if (tiles)
+    quant_tile_kernel<DT, VEC, E5M2, true, false><<<grid, 256, 0, st>>>(p);
+  else
+    quant_tile_kernel<DT, VEC, E5M2, false, true><<<grid, 256, 0, st>>>(p);
+  return launched(ctx);
+}
+template <int DT>
+kb_status launch_quant(kb_ctx* ctx, const QuantParams& p, bool vec, bool e5m2, bool transpose, bool tiles,
+                       cudaStream_t st) {
+  if (vec)
+    return e5m2 ? launch_quant<DT, true, true>(ctx, p, transpose, tiles, st)
+                : launch_quant<DT, true, false>(ctx, p, transpose, tiles, st);
+  return e5m2 ? launch_quant<DT, false, true>(ctx, p, transpose, tiles, st)
+              : launch_quant<DT, false, false>(ctx, p, transpose, tiles, st);
+}
+
+// ---- layer norm ----------------------------------------------------------------------------------
+
+template <int DT, bool VEC>
+kb_status launch_norm(kb_ctx* ctx, const NormParams& p, cudaStream_t st) {
+  const uint32_t g = p.groups;
+  const unsigned int rows = (unsigned int)p.rows;
+  if (g <= 4) {   // a warp per row
+    const unsigned int grid = (rows + 3) / 4;
+    if (g == 1)
+      norm_kernel<DT, 1, VEC, true><<<grid, 128, 0, st>>>(p);
+    else if (g == 2)
+      norm_kernel<DT, 2, VEC, true><<<grid, 128, 0, st>>>(p);
+    else
+      norm_kernel<DT, 4, VEC, true><<<grid, 128, 0, st>>>(p);
+  } else if (g <= 32 && p.rows <= (uint64_t)ctx->sm_count) {   // one CTA per SM at most: as many warps as there are groups
+    norm_kernel<DT, 1, VEC, false><<<rows, 32 * g, 0, st>>>(p);
+  } else if (g <= 32) {
+    norm_kernel<DT, 2, VEC, false><<<rows, 32 * ((g + 1) / 2), 0, st>>>(p);
+  } else if (g <= 64) {
+    norm_kernel<DT, 4, VEC, false><<<rows, 32 * ((g + 3) / 4), 0, st>>>(p);
+  } else {
+    norm_long_kernel<DT, VEC><<<rows, 512, 0, st>>>(p);
+  }
+  return launched(ctx);
+}
+
+template <int DT, int NCH, bool VEC, bool WARP>
+kb_status launch_norm_bwd(kb_ctx* ctx, NormBwdParams& p, unsigned int threads, uint32_t* nparts, cudaStream_t st) {
+  const uint64_t per = WARP ? threads / 32 : 1;
+  const size_t smem = WARP ? 2 * sizeof(float) * p.cols : 0;
+  int per_sm = 0;
+  KB_CUDA(ctx, cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, norm_bwd_kernel<DT, NCH, VEC, WARP>,
+                                                             (int)threads, smem));
+  const uint64_t most = (uint64_t)ctx->sm_count * std::max(per_sm, 1);
+  const unsigned int grid = (unsigned int)std::min<uint64_t>((p.rows + per - 1) / per, most);
+  *nparts = grid;
+  if (p.want_param) {
+    KB_TRY(ensure_buf(ctx, &ctx->ops_ws, &ctx->ops_ws_bytes, (size_t)grid * 2 * p.cols * sizeof(float),
+                      "partial parameter gradients"));
+    p.partial = reinterpret_cast<float*>(ctx->ops_ws);
+  }
+  norm_bwd_kernel<DT, NCH, VEC, WARP><<<grid, threads, smem, st>>>(p);
+  return launched(ctx);
+}
+
+template <int DT, bool VEC>
+kb_status launch_norm_bwd(kb_ctx* ctx, NormBwdParams& p, uint32_t* nparts, cudaStream_t st) {
+  const uint32_t g = p.groups;
+  if (g == 1) return launch_norm_bwd<DT, 1, VEC, true>(ctx, p, 128, nparts, st);
+  if (g == 2) return launch_norm_bwd<DT, 2, VEC, true>(ctx, p, 128, nparts, st);
+  if (g <= 4) return launch_norm_bwd<DT, 4, VEC, true>(ctx, p, 128, nparts, st);
+  if (g <= 16) return launch_norm_bwd<DT, 1, VEC, false>(ctx, p, 32 * g, nparts, st);
+  if (g <= 32) return launch_norm_bwd<DT, 2, VEC, false>(ctx, p, 32 * ((g + 1) / 2), nparts, st);
+  if (p.dx) {
+    norm_bwd_long_kernel<DT, VEC><<<(unsigned int)p.rows, 512, 0, st>>>(p);
+    KB_TRY(launched(ctx));
+  }
+  if (p.want_param) {
+    const uint32_t gx = (g + 7) / 8;
+    const uint64_t want = std::max<uint64_t>(1, 8ull * ctx->sm_count / gx);
+    const uint32_t slices = (uint32_t)std::min<uint64_t>(std::min<uint64_t>(want, (p.rows + 7) / 8), 65535);
+    KB_TRY(ensure_buf(ctx, &ctx->ops_ws, &ctx->ops_ws_bytes, (size_t)slices * 2 * p.cols * sizeof(float),
+                      "partial parameter gradients"));
+    p.partial = reinterpret_cast<float*>(ctx->ops_ws);
+    *nparts = slices;
+    norm_bwd_cols_kernel<DT, VEC><<<dim3(gx, slices), 256, 0, st>>>(p);
+    KB_TRY(launched(ctx));
+  }
+  return KB_OK;
+}
+
+// ---- product ---------------------------------------------------------------------------------------
+
+using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
+                                 const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
+                                 CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+template <int BN>
+kb_status lanes_attr(kb_ctx* ctx) {
+  KB_CUDA(ctx, cudaFuncSetAttribute(matmul_lanes_kernel<BN>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                    (int)LaneTile<BN>::kSmem));
+  return KB_OK;
+}
+
+kb_status prepare_matmul(kb_ctx* ctx) {
+  if (ctx->ops_ready) return KB_OK;
+  void* fn = nullptr;
+  cudaDriverEntryPointQueryResult found = cudaDriverEntryPointSymbolNotFound;
+  KB_CUDA(ctx, cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &found));
+  if (found != cudaDriverEntryPointSuccess || !fn)
+    return fail(ctx, KB_ERR_CUDA, "kb_matmul_blocks: the driver has no cuTensorMapEncodeTiled");
+  KB_TRY(lanes_attr<16>(ctx));
+  KB_TRY(lanes_attr<32>(ctx));
+  KB_TRY(lanes_attr<64>(ctx));
+  KB_TRY(lanes_attr<128>(ctx));
+  ctx->encode_tiled = fn;
+  ctx->ops_ready = true;
+  return KB_OK;
+}
+
+// Tensor map of an 8-bit matrix [rows][cols], boxes of 128 columns and `box_rows` rows in the
+// 128-byte swizzle; places outside the matrix read as zero.
+kb_status encode_map(kb_ctx* ctx, CUtensorMap* map, const void* p, uint64_t rows, uint64_t cols, uint64_t ld,
+                     uint32_t box_rows) {
+  const cuuint64_t dims[2] = {cols, rows}, strides[1] = {ld};
+  const cuuint32_t box[2] = {128, box_rows}, step[2] = {1, 1};
+  const CUresult rc = reinterpret_cast<EncodeTiled>(ctx->encode_tiled)(
+      map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(p), dims, strides, box, step,
+      CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+      CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (rc != CUDA_SUCCESS) return fail(ctx, KB_ERR_CUDA, "cuTensorMapEncodeTiled failed with %d", (int)rc);
+  return KB_OK;
+}
+
+template <int BN>
+kb_status launch_lanes(kb_ctx* ctx, MatmulParams& p, const void* a, uint64_t lda, bool a_e5m2, const void* b,
+                       uint64_t ldb, bool b_e5m2, uint64_t K, cudaStream_t st) {
+  CUtensorMap map_a, map_b;
+  KB_TRY(encode_map(ctx, &map_a, a, p.M, K, lda, BN));
+  KB_TRY(encode_map(ctx, &map_b, b, p.N, K, ldb, 128));
+  p.idesc = mma_idesc_f8(b_e5m2, a_e5m2, 128, BN);
+  p.tiles_m = (p.M + BN - 1) / BN;
+  const uint64_t tiles = (uint64_t)p.tiles_m * ((p.N + 127) / 128);
+  uint32_t splits = 1;
+  while (splits < 8 && tiles * splits * 2 <= (uint64_t)ctx->sm_count && p.KB >= 4 * splits) splits *= 2;
+  p.splits = splits;
+  if (tiles * splits > 0x7FFFFFFFull) return fail(ctx, KB_ERR_UNSUPPORTED, "kb_matmul_blocks: more than 2^31 - 1 tiles");
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned int)(tiles * splits));
+  cfg.blockDim = dim3(LaneTile<BN>::kThreads);
+  cfg.dynamicSmemBytes = LaneTile<BN>::kSmem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = splits;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  KB_CUDA(ctx, cudaLaunchKernelEx(&cfg, matmul_lanes_kernel<BN>, map_b, map_a, p));
+  return launched(ctx);
+}
+
+}  // namespace
+
+// ---------------------------------------------------------------------------
+// entry points
+// ---------------------------------------------------------------------------
+
+extern "C" kb_status kb_quantize_blocks(kb_ctx* ctx, const void* d_x, uint64_t rows, uint64_t cols, uint64_t ldx,
+                                        kb_dtype dtype, int transpose, kb_scale_mode mode, void* d_q, uint64_t ldq,
+                                        kb_dtype q_dtype, float* d_scale, void* stream) {
+  TraceRange trace("kb_quantize_blocks");
+  if (!ctx) return KB_ERR_INVALID_ARG;
+  const char* where = "kb_quantize_blocks";
+  if (!is_float_type(dtype)) return fail(ctx, KB_ERR_UNSUPPORTED, "%s: dtype %d is not fp32, fp16 or bf16", where, (int)dtype);
+  if (!is_f8_type(q_dtype)) return fail(ctx, KB_ERR_UNSUPPORTED, "%s: q_dtype %d is not an 8-bit float", where, (int)q_dtype);
+  if (mode != KB_SCALE_ROWS && mode != KB_SCALE_TILES) return fail(ctx, KB_ERR_UNSUPPORTED, "%s: unknown mode %d", where, (int)mode);
+  if (transpose != 0 && transpose != 1) return fail(ctx, KB_ERR_INVALID_ARG, "%s: transpose must be 0 or 1", where);
+  if (rows > KB_OPS_MAX_DIM || cols > KB_OPS_MAX_DIM) return fail(ctx, KB_ERR_INVALID_ARG, "%s: rows or columns beyond 2^30", where);
+  if (rows == 0 || cols == 0) return KB_OK;
+  const int e = elem_bytes(dtype);
+  KB_TRY(check_matrix(ctx, where, "d_x", d_x, cols, ldx, e));
+  KB_TRY(check_matrix(ctx, where, "d_q", d_q, transpose ? rows : cols, ldq, 1));
+  if (!d_scale) return fail(ctx, KB_ERR_INVALID_ARG, "%s: d_scale is NULL", where);
+  KB_TRY(check_vector(ctx, where, "d_scale", d_scale, 4));
+  DeviceGuard g(ctx->device);
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  QuantParams p;
+  p.x = d_x;
+  p.q = static_cast<unsigned char*>(d_q);
+  p.scale = d_scale;
+  p.rows = rows;
+  p.cols = cols;
+  p.ldx = ldx;
+  p.ldq = ldq;
+  p.groups = (uint32_t)((cols + kGroup - 1) / kGroup);
+  p.rtiles = (uint32_t)((rows + 127) / 128);
+  p.ctiles = (uint32_t)((cols + 127) / 128);
+  const bool vec = cols % 8 == 0 && rows_aligned(d_x, ldx, e) && (transpose || (ldq % 8 == 0 && aligned_to(d_q, 8)));
+  const bool e5m2 = q_dtype == KB_F8E5M2, tiles = mode == KB_SCALE_TILES;
+  if (dtype == KB_F32) return launch_quant<KB_F32>(ctx, p, vec, e5m2, transpose, tiles, st);
+  if (dtype == KB_F16) return launch_quant<KB_F16>(ctx, p, vec, e5m2, transpose, tiles, st);
+  return launch_quant<KB_BF16>(ctx, p, vec, e5m2, transpose, tiles, st);
+}
+
+extern "C" kb_status kb_layernorm(kb_ctx* ctx, const void* d_x, uint64_t rows, uint64_t cols, uint64_t ldx,
+                                  kb_dtype dtype, const void* d_weight, const void* d_bias, kb_dtype param_dtype,
+                                  float eps, void* d_y, uint64_t ldy, float* d_mean, float* d_rstd, void* d_q,
+                                  uint64_t ldq, kb_dtype q_dtype, float* d_scale, void* stream) {
+  TraceRange trace("kb_layernorm");
+  if (!ctx) return KB_ERR_INVALID_ARG;
+  const char* where = "kb_layernorm";
+  if (!is_float_type(dtype)) return fail(ctx, KB_ERR_UNSUPPORTED, "%s: dtype %d is not fp32, fp16 or bf16", where, (int)dtype);
+  if (param_dtype != dtype && param_dtype != KB_F32)
+    return fail(ctx, KB_ERR_UNSUPPORTED, "%s: parameters are of the row's type or binary32", where);
+  if (!(eps > 0.0f) || !std::isfinite(eps)) return fail(ctx, KB_ERR_INVALID_ARG, "%s: eps must be finite and > 0", where);
+  if (cols == 0 || rows > KB_OPS_MAX_DIM || cols > KB_OPS_MAX_DIM)
+    return fail(ctx, KB_ERR_INVALID_ARG, "%s: columns outside [1, 2^30] or rows beyond 2^30", where);
+  if (!d_y && !d_mean && !d_rstd && !d_q) return fail(ctx, KB_ERR_INVALID_ARG, "%s: no output", where);
+  if ((d_q == nullptr) != (d_scale == nullptr)) return fail(ctx, KB_ERR_INVALID_ARG, "%s: d_q and d_scale come together", where);
+  if (d_q && !is_f8_type(q_dtype)) return fail(ctx, KB_ERR_UNSUPPORTED, "%s: q_dtype %d is not an 8-bit float", where, (int)q_dtype);
+  if (rows == 0) return KB_OK;
+  const int e = elem_bytes(dtype), pe = elem_bytes(param_dtype);
+  KB_TRY(check_matrix(ctx, where, "d_x", d_x, cols, ldx, e));
+  if (d_y) KB_TRY(check_matrix(ctx, where, "d_y", d_y, cols, ldy, e));
+  if (d_q) KB_TRY(check_matrix(ctx, where, "d_q", d_q, cols, ldq, 1));
+  KB_TRY(check_vector(ctx, where, "d_weight", d_weight, pe));
+  KB_TRY(check_vector(ctx, where, "d_bias", d_bias, pe));
+  KB_TRY(check_vector(ctx, where, "d_mean", d_mean, 4));
+  KB_TRY(check_vector(ctx, where, "d_rstd", d_rstd, 4));
+  KB_TRY(check_vector(ctx, where, "d_scale", d_scale, 4));
+  DeviceGuard g(ctx->device);
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  NormParams p;
+  p.x = d_x;
+  p.weight = d_weight;
+  p.bias = d_bias;
+  p.y = d_y;
+  p.mean = d_mean;
+  p.rstd = d_rstd;
+  p.q = static_cast<unsigned char*>(d_q);
+  p.scale = d_scale;
+  p.rows = rows;
+  p.ldx = ldx;
+  p.ldy = ldy;
+  p.ldq = ldq;
+  p.cols = (uint32_t)cols;
+  p.groups = (uint32_t)((cols + kGroup - 1) / kGroup);
+  p.eps = eps;
+  p.param_f32 = param_dtype == KB_F32;
+  p.e5m2 = q_dtype == KB_F8E5M2;
+  const bool vec = cols % 8 == 0 && rows_aligned(d_x, ldx, e) && (!d_y || rows_aligned(d_y, ldy, e)) &&
+                   (!d_q || (ldq % 8 == 0 && aligned_to(d_q, 8))) && aligned16(d_weight) && aligned16(d_bias);
+  if (dtype == KB_F32) return vec ? launch_norm<KB_F32, true>(ctx, p, st) : launch_norm<KB_F32, false>(ctx, p, st);
+  if (dtype == KB_F16) return vec ? launch_norm<KB_F16, true>(ctx, p, st) : launch_norm<KB_F16, false>(ctx, p, st);
+  return vec ? launch_norm<KB_BF16, true>(ctx, p, st) : launch_norm<KB_BF16, false>(ctx, p, st);
+}
+
+extern "C" kb_status kb_layernorm_backward(kb_ctx* ctx, const void* d_dy, uint64_t lddy, const void* d_x,
+                                           uint64_t ldx, uint64_t rows, uint64_t cols, kb_dtype dtype,
+                                           const void* d_weight, kb_dtype param_dtype, const float* d_mean,
+                                           const float* d_rstd, void* d_dx, uint64_t lddx, void* d_dweight,
+                                           void* d_dbias, void* stream) {
+  TraceRange trace("kb_layernorm_backward");
+  if (!ctx) return KB_ERR_INVALID_ARG;
+  const char* where = "kb_layernorm_backward";
+  if (!is_float_type(dtype)) return fail(ctx, KB_ERR_UNSUPPORTED, "%s: dtype %d is not fp32, fp16 or bf16", where, (int)dtype);
+  if (param_dtype != dtype && param_dtype != KB_F32)
+    return fail(ctx, KB_ERR_UNSUPPORTED, "%s: parameters are of the row's type or binary32", where);
+  if (cols == 0 || rows > KB_OPS_MAX_DIM || cols > KB_OPS_MAX_DIM)
+    return fail(ctx, KB_ERR_INVALID_ARG, "%s: columns outside [1, 2^30] or rows beyond 2^30", where);
+  if (!d_dx && !d_dweight && !d_dbias) return fail(ctx, KB_ERR_INVALID_ARG, "%s: no output", where);
+  const int e = elem_bytes(dtype), pe = elem_bytes(param_dtype);
+  KB_TRY(check_vector(ctx, where, "d_weight", d_weight, pe));
+  KB_TRY(check_vector(ctx, where, "d_dweight", d_dweight, pe));
+  KB_TRY(check_vector(ctx, where, "d_dbias", d_dbias, pe));
+  DeviceGuard g(ctx->device);
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  if (rows == 0) {
+    if (d_dweight) KB_CUDA(ctx, cudaMemsetAsync(d_dweight, 0, cols * pe, st));
+    if (d_dbias) KB_CUDA(ctx, cudaMemsetAsync(d_dbias, 0, cols * pe, st));
+    return KB_OK;
+  }
+  KB_TRY(check_matrix(ctx, where, "d_dy", d_dy, cols, lddy, e));
+  KB_TRY(check_matrix(ctx, where, "d_x", d_x, cols, ldx, e));
+  if (d_dx) KB_TRY(check_matrix(ctx, where, "d_dx", d_dx, cols, lddx, e));
+  if (!d_mean || !d_rstd) return fail(ctx, KB_ERR_INVALID_ARG, "%s: d_mean or d_rstd is NULL", where);
+  KB_TRY(check_vector(ctx, where, "d_mean", d_mean, 4));
+  KB_TRY(check_vector(ctx, where, "d_rstd", d_rstd, 4));
+  NormBwdParams p;
+  p.dy = d_dy;
+  p.x = d_x;
+  p.weight = d_weight;
+  p.mean = d_mean;
+  p.rstd = d_rstd;
+  p.dx = d_dx;
+  p.partial = nullptr;
+  p.rows = rows;
+  p.lddy = lddy;
+  p.ldx = ldx;
+  p.lddx = lddx;
+  p.cols = (uint32_t)cols;
+  p.groups = (uint32_t)((cols + kGroup - 1) / kGroup);
+  p.param_f32 = param_dtype == KB_F32;
+  p.want_param = d_dweight || d_dbias;
+  const bool vec = cols % 8 == 0 && rows_aligned(d_dy, lddy, e) && rows_aligned(d_x, ldx, e) &&
+                   (!d_dx || rows_aligned(d_dx, lddx, e)) && aligned16(d_weight);
+  uint32_t nparts = 0;
+  if (dtype == KB_F32)
+    KB_TRY((vec ? launch_norm_bwd<KB_F32, true>(ctx, p, &nparts, st) : launch_norm_bwd<KB_F32, false>(ctx, p, &nparts, st)));
+  else if (dtype == KB_F16)
+    KB_TRY((vec ? launch_norm_bwd<KB_F16, true>(ctx, p, &nparts, st) : launch_norm_bwd<KB_F16, false>(ctx, p, &nparts, st)));
+  else
+    KB_TRY((vec ? launch_norm_bwd<KB_BF16, true>(ctx, p, &nparts, st) : launch_norm_bwd<KB_BF16, false>(ctx, p, &nparts, st)));
+  if (!p.want_param) return KB_OK;
+  const dim3 grid((unsigned int)((cols + 31) / 32), 2);
+  if (param_dtype == KB_F32)
+    norm_param_kernel<KB_F32><<<grid, 1024, 0, st>>>(p.partial, nparts, p.cols, d_dweight, d_dbias);
+  else if (param_dtype == KB_F16)
+    norm_param_kernel<KB_F16><<<grid, 1024, 0, st>>>(p.partial, nparts, p.cols, d_dweight, d_dbias);
+  else
+    norm_param_kernel<KB_BF16><<<grid, 1024, 0, st>>>(p.partial, nparts, p.cols, d_dweight, d_dbias);
+  return launched(ctx);
+}
+
+extern "C" kb_status kb_matmul_blocks(kb_ctx* ctx, const void* d_a, uint64_t lda, kb_dtype a_dtype,
+                                      const float* d_a_scale, const void* d_b, uint64_t ldb, kb_dtype b_dtype,
+                                      const float* d_b_scale, kb_scale_mode b_mode, uint64_t M, uint64_t N,
+                                      uint64_t K, void* d_d, uint64_t ldd, kb_dtype d_dtype, void* stream) {
+  TraceRange trace("kb_matmul_blocks");
+  if (!ctx) return KB_ERR_INVALID_ARG;
+  const char* where = "kb_matmul_blocks";
+  if (!is_f8_type(a_dtype) || !is_f8_type(b_dtype)) return fail(ctx, KB_ERR_UNSUPPORTED, "%s: operands are 8-bit floats", where);
+  if (!is_float_type(d_dtype)) return fail(ctx, KB_ERR_UNSUPPORTED, "%s: d_dtype %d is not fp32, fp16 or bf16", where, (int)d_dtype);
+  if (b_mode != KB_SCALE_ROWS && b_mode != KB_SCALE_TILES) return fail(ctx, KB_ERR_UNSUPPORTED, "%s: unknown b_mode %d", where, (int)b_mode);
+  if (M > KB_OPS_MAX_DIM || N > KB_OPS_MAX_DIM || K > KB_OPS_MAX_DIM)
+    return fail(ctx, KB_ERR_INVALID_ARG, "%s: a dimension beyond 2^30", where);
+  if (M == 0 || N == 0) return KB_OK;
+  const int e = elem_bytes(d_dtype);
+  KB_TRY(check_matrix(ctx, where, "d_d", d_d, N, ldd, e));
+  DeviceGuard g(ctx->device);
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  if (K == 0) {
+    KB_CUDA(ctx, cudaMemset2DAsync(d_d, ldd * e, 0, N * e, M, st));
+    return KB_OK;
+  }
+  KB_TRY(check_matrix(ctx, where, "d_a", d_a, K, lda, 1));
+  KB_TRY(check_matrix(ctx, where, "d_b", d_b, K, ldb, 1));
+  if (!rows_aligned(d_a, lda, 1) || !rows_aligned(d_b, ldb, 1))
+    return fail(ctx, KB_ERR_ALIGNMENT, "%s: operands need 16-byte aligned pointers and row strides", where);
+  if (!d_a_scale || !d_b_scale) return fail(ctx, KB_ERR_INVALID_ARG, "%s: d_a_scale or d_b_scale is NULL", where);
+  KB_TRY(check_vector(ctx, where, "d_a_scale", d_a_scale, 4));
+  KB_TRY(check_vector(ctx, where, "d_b_scale", d_b_scale, 4));
+  KB_TRY(prepare_matmul(ctx));
+  MatmulParams p;
+  p.a_scale = d_a_scale;
+  p.b_scale = d_b_scale;
+  p.d = d_d;
+  p.ldd = ldd;
+  p.M = (uint32_t)M;
+  p.N = (uint32_t)N;
+  p.KB = (uint32_t)((K + KB_BLOCK - 1) / KB_BLOCK);
+  p.b_scale_shift = b_mode == KB_SCALE_TILES ? 7 : 0;
+  p.b_scale_ld = b_mode == KB_SCALE_TILES ? (p.N + 127) / 128 : p.N;
+  p.out = (int)d_dtype;
+  p.status = ctx->d_status;
+  const bool ae = a_dtype == KB_F8E5M2, be = b_dtype == KB_F8E5M2;
+  if (M <= 16) return launch_lanes<16>(ctx, p, d_a, lda, ae, d_b, ldb, be, K, st);
+  if (M <= 32) return launch_lanes<32>(ctx, p, d_a, lda, ae, d_b, ldb, be, K, st);
+  if (M <= 64) return launch_lanes<64>(ctx, p, d_a, lda, ae, d_b, ldb, be, K, st);
+  return launch_lanes<128>(ctx, p, d_a, lda, ae, d_b, ldb, be, K, st);
+}
