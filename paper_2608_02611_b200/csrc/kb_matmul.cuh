@@ -30,6 +30,7 @@ struct MatmulParams {
   uint32_t splits;           // CTAs per tile along K (a cluster)
   uint32_t idesc;
   int out;                   // kb_dtype of D
+  bool vec_out;              // rows of D start on 16-byte boundaries
   unsigned int* status;
 };
 
@@ -244,6 +245,291 @@ __global__ void __launch_bounds__(LaneTile<BN>::kThreads, 1)
   __syncthreads();
   tc_fence_after();
   if (warp == 1) tmem_free<1>(tmem, T::kTmemCols);
+}
+
+// ---- many rows of A ------------------------------------------------------------------------
+// A pair of CTAs shares a tile of 256 rows of A and 256 rows of B: each holds its own 128 rows of
+// either operand, the pair's matrix instructions (issued by the first CTA) read both halves of B,
+// and each CTA's tensor memory gets 128 rows x 256 columns.  Per K block of 128 the pair's tensor
+// cores are busy for 512 cycles at the 8-bit rate, while 32 KB per CTA have to arrive and 32,768
+// accumulators per CTA have to be scaled and added: half of the SM's binary32 rate.  Two
+// accumulators fill tensor memory, so the scaling of one block runs under the products of the
+// next.  Persistent: a pair walks over tiles, and a tile's last scaling and its stores run under
+// the next tile's first products.
+struct PairTile {
+  static constexpr uint32_t kHalfBytes = 128 * 128;             // one operand's share of a CTA
+  static constexpr uint32_t kStageBytes = 2 * kHalfBytes;
+  static constexpr uint32_t kStages = 6;
+  static constexpr uint32_t kScaleSlots = 8;                    // K blocks whose scales are in shared memory
+  static constexpr uint32_t kTmemCols = 512;
+  static constexpr uint32_t kSmem = 1024 + kStages * kStageBytes;
+  static constexpr int kEpiWarps = 8;
+  // three warpgroups: one copies and issues, two scale and add.  168 registers per thread at
+  // launch are split 104 / 200 / 200: 128 running sums and what is in flight need the 200.
+  static constexpr int kThreads = 128 + 32 * kEpiWarps;
+  static constexpr int kRegsLaunch = 168, kRegsControl = 104, kRegsEpi = 200;
+  static_assert(kRegsControl + 2 * kRegsEpi <= 3 * kRegsLaunch, "register shares");
+  static constexpr uint32_t kGroupM = 8;                        // tiles of A that neighbouring pairs share
+};
+
+__device__ __forceinline__ unsigned long long pack_f32x2(float lo, float hi) {
+  unsigned long long r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ void unpack_f32x2(unsigned long long v, float& lo, float& hi) {
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v));
+}
+__device__ __forceinline__ unsigned long long fma_f32x2(unsigned long long a, unsigned long long b,
+                                                        unsigned long long c) {
+  unsigned long long d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  return d;
+}
+__device__ __forceinline__ unsigned long long mul_f32x2(unsigned long long a, unsigned long long b) {
+  unsigned long long d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+
+// Tile coordinates of item `t`: down kGroupM tiles of A, then along B, so that the pairs that run
+// together read few different rows of either.
+__device__ __forceinline__ void pair_tile(uint32_t t, uint32_t tiles_m, uint32_t tiles_n, uint32_t& tm, uint32_t& tn) {
+  const uint32_t per = PairTile::kGroupM * tiles_n;
+  const uint32_t g = t / per, r = t % per;
+  const uint32_t h = min(PairTile::kGroupM, tiles_m - g * PairTile::kGroupM);
+  tm = g * PairTile::kGroupM + r % h;
+  tn = r / h;
+}
+
+// 8 results of one row
+template <int DT>
+__device__ __forceinline__ void store_row8(void* d, uint64_t i, const float (&v)[8], uint32_t n, uint32_t N, bool vec) {
+  if (vec && n + 8 <= N) {
+    store8<DT>(d, i, v);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (n + j < N) store_elem<DT>(d, i + j, v[j]);
+  }
+}
+
+// BROWS: B has one scale per row (per column of the tile) instead of one per 128 rows.
+template <bool BROWS>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PairTile::kThreads, 1)
+    matmul_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+                       const MatmulParams p) {
+  using T = PairTile;
+  extern __shared__ unsigned char dyn[];
+  __shared__ uint64_t full[T::kStages], empty[T::kStages], acc_full[2], acc_empty[2], drained;
+  __shared__ uint64_t sc_full[T::kScaleSlots], sc_empty[T::kScaleSlots];
+  __shared__ uint32_t tmem_base;
+  __shared__ unsigned int abort_word;
+  __shared__ __align__(16) float row_scale[T::kScaleSlots][128];
+  __shared__ __align__(16) float col_scale[T::kScaleSlots][BROWS ? 256 : 2];
+  volatile unsigned int* abort_flag = &abort_word;
+  unsigned char* stages = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(dyn) + 1023) & ~(uintptr_t)1023);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = cluster_rank();
+  const uint32_t tiles_n = (p.N + 255) / 256, tiles = p.tiles_m * tiles_n;
+  const uint32_t first = blockIdx.x >> 1, step = gridDim.x >> 1;
+
+  if (threadIdx.x == 0) {
+    for (uint32_t i = 0; i < T::kStages; ++i) {
+      mbar_init(&full[i], 1);
+      mbar_init(&empty[i], 1);
+    }
+    for (uint32_t i = 0; i < 2; ++i) {
+      mbar_init(&acc_full[i], 1);
+      mbar_init(&acc_empty[i], 2 * T::kEpiWarps);
+    }
+    for (uint32_t i = 0; i < T::kScaleSlots; ++i) {
+      mbar_init(&sc_full[i], 32);
+      mbar_init(&sc_empty[i], T::kEpiWarps);
+    }
+    mbar_init(&drained, 1);
+    abort_word = 0u;
+    mbar_fence_init();
+  }
+  if (warp == 1) tmem_alloc<2>(&tmem_base, T::kTmemCols);
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync_all();   // both CTAs' barriers are ready and their tensor memory is allocated
+  tc_fence_after();
+  const uint32_t tmem = tmem_base;
+
+  if (warp < 4) regs_shrink<T::kRegsControl>();
+  if (warp == 0) {
+    if (lane == 0) {
+      uint32_t st = 0, phase = 0;
+      uint64_t issued = 0;
+      bool ok = true;
+      for (uint32_t t = first; t < tiles && ok; t += step) {
+        uint32_t tm, tn;
+        pair_tile(t, p.tiles_m, tiles_n, tm, tn);
+        const int ya = (int)(tm * 256 + rank * 128), yb = (int)(tn * 256 + rank * 128);
+        for (uint32_t kb = 0; kb < p.KB; ++kb) {
+          if (!mbar_wait_bounded(&empty[st], phase ^ 1u, abort_flag, p.status)) {
+            ok = false;
+            break;
+          }
+          unsigned char* s = stages + st * T::kStageBytes;
+          const uint32_t bar = map_to_rank(smem_u32(&full[st]), 0);
+          if (rank == 0) mbar_arrive_expect_tx(&full[st], 2 * T::kStageBytes);
+          tma_load_2d_pair(s, &map_a, (int)(kb * 128), ya, bar);
+          tma_load_2d_pair(s + T::kHalfBytes, &map_b, (int)(kb * 128), yb, bar);
+          ++issued;
+          if (++st == T::kStages) {
+            st = 0;
+            phase ^= 1u;
+          }
+        }
+      }
+      if (!ok) {
+        // let the copies in flight land: the first CTA's barriers count both CTAs' bytes, the
+        // second CTA cannot see them and waits far longer than a copy takes
+        if (rank == 0) drain_copies(full, T::kStages, issued);
+        const unsigned long long t0 = global_ns();
+        while (global_ns() - t0 < 20000000ull) {
+        }
+      }
+    }
+    __syncwarp();
+  } else if (warp == 1) {
+    if (lane == 0 && rank == 0) {
+      uint32_t st = 0, phase = 0, it = 0;
+      bool ok = true;
+      for (uint32_t t = first; t < tiles && ok; t += step) {
+        for (uint32_t kb = 0; kb < p.KB; ++kb, ++it) {
+          const uint32_t a = it & 1u, a_phase = (it >> 1) & 1u;
+          if (!mbar_wait_bounded(&full[st], phase, abort_flag, p.status) ||
+              !mbar_wait_bounded(&acc_empty[a], a_phase ^ 1u, abort_flag, p.status)) {
+            ok = false;
+            break;
+          }
+          tc_fence_after();
+          const uint32_t s = smem_u32(stages + st * T::kStageBytes);
+          const uint64_t a_desc = smem_desc_k128(s), b_desc = smem_desc_k128(s + T::kHalfBytes);
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            mma_f8<2>(tmem + a * 256, a_desc + 2 * k, b_desc + 2 * k, p.idesc, k > 0);
+          mma_commit_pair(&acc_full[a]);
+          mma_commit_pair(&empty[st]);
+          if (++st == T::kStages) {
+            st = 0;
+            phase ^= 1u;
+          }
+        }
+      }
+      if (!ok) {   // what has been issued ends before tensor memory is freed
+        mma_commit_pair(&drained);
+        const unsigned long long t0 = global_ns();
+        while (!mbar_try_wait(&drained, 0))
+          if (global_ns() - t0 > 1000000000ull) break;
+      }
+    }
+    __syncwarp();
+  } else if (warp == 2) {
+    // the scales of each K block, several blocks ahead of their use
+    uint32_t it = 0;
+    bool ok = true;
+    for (uint32_t t = first; t < tiles && ok; t += step) {
+      uint32_t tm, tn;
+      pair_tile(t, p.tiles_m, tiles_n, tm, tn);
+      const uint32_t m0 = tm * 256 + rank * 128, n0 = tn * 256;
+      for (uint32_t kb = 0; kb < p.KB; ++kb, ++it) {
+        const uint32_t slot = it % T::kScaleSlots, phase = (it / T::kScaleSlots) & 1u;
+        ok = __all_sync(0xFFFFFFFFu, mbar_wait_bounded(&sc_empty[slot], phase ^ 1u, abort_flag, p.status));
+        if (!ok) break;
+        const float* as = p.a_scale + (uint64_t)kb * p.M;
+        const float* bs = p.b_scale + (uint64_t)kb * p.b_scale_ld;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t m = m0 + i * 32 + lane;
+          cp_async_f32(&row_scale[slot][i * 32 + lane], m < p.M ? as + m : as, m < p.M);
+        }
+        if constexpr (BROWS) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const uint32_t n = n0 + i * 32 + lane;
+            cp_async_f32(&col_scale[slot][i * 32 + lane], n < p.N ? bs + n : bs, n < p.N);
+          }
+        } else if (lane < 2) {
+          const uint32_t n = n0 + lane * 128;
+          cp_async_f32(&col_scale[slot][lane], n < p.N ? bs + (n >> 7) : bs, n < p.N);
+        }
+        cp_async_arrive(&sc_full[slot]);
+      }
+    }
+    cp_async_wait_all();
+    __syncwarp();
+  } else if (warp >= 4) {
+    regs_grow<T::kRegsEpi>();
+    const int quarter = warp & 3, half = (warp - 4) >> 2;
+    const uint32_t taddr = tmem + ((uint32_t)(quarter * 32) << 16) + half * 128;
+    const uint32_t release0 = map_to_rank(smem_u32(&acc_empty[0]), 0);
+    uint32_t it = 0;
+    bool ok = true;
+    for (uint32_t t = first; t < tiles && ok; t += step) {
+      unsigned long long acc[64];
+#pragma unroll
+      for (int j = 0; j < 64; ++j) acc[j] = 0ull;
+      for (uint32_t kb = 0; kb < p.KB; ++kb, ++it) {
+        const uint32_t a = it & 1u, slot = it % T::kScaleSlots;
+        ok = __all_sync(0xFFFFFFFFu, mbar_wait_bounded(&sc_full[slot], (it / T::kScaleSlots) & 1u, abort_flag, p.status) &&
+                                         mbar_wait_bounded(&acc_full[a], (it >> 1) & 1u, abort_flag, p.status));
+        if (!ok) break;
+        tc_fence_after();
+        float s = row_scale[slot][quarter * 32 + lane];
+        if constexpr (!BROWS) s *= col_scale[slot][half];
+        const unsigned long long s2 = pack_f32x2(s, s);
+        const float* c = &col_scale[slot][BROWS ? half * 128 : 0];
+#pragma unroll
+        for (int j0 = 0; j0 < 128; j0 += 32) {
+          float v[32];
+          tmem_ld32(taddr + a * 256 + j0, v);
+          tmem_wait_ld();
+          if (j0 == 96) {   // all of this accumulator is in registers
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_cluster(release0 + a * 8);
+          }
+#pragma unroll
+          for (int j = 0; j < 32; j += 2) {
+            unsigned long long d = pack_f32x2(v[j], v[j + 1]);
+            if constexpr (BROWS) d = mul_f32x2(d, *reinterpret_cast<const unsigned long long*>(c + j0 + j));
+            acc[(j0 + j) / 2] = fma_f32x2(d, s2, acc[(j0 + j) / 2]);
+          }
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sc_empty[slot]);
+      }
+      uint32_t tm, tn;
+      pair_tile(t, p.tiles_m, tiles_n, tm, tn);
+      const uint32_t m = tm * 256 + rank * 128 + quarter * 32 + lane, n0 = tn * 256 + half * 128;
+      if (ok && m < p.M && n0 < p.N) {
+        const uint64_t row = (uint64_t)m * p.ldd;
+#pragma unroll
+        for (int j = 0; j < 128; j += 8) {
+          float v[8];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) unpack_f32x2(acc[j / 2 + i], v[2 * i], v[2 * i + 1]);
+          const uint32_t n = n0 + j;
+          if (n >= p.N) break;
+          if (p.out == KB_BF16)
+            store_row8<KB_BF16>(p.d, row + n, v, n, p.N, p.vec_out);
+          else if (p.out == KB_F16)
+            store_row8<KB_F16>(p.d, row + n, v, n, p.N, p.vec_out);
+          else
+            store_row8<KB_F32>(p.d, row + n, v, n, p.N, p.vec_out);
+        }
+      }
+    }
+  }
+  tc_fence_before();
+  cluster_sync_all();   // neither CTA leaves while the other's instructions use its memory
+  tc_fence_after();
+  if (warp == 1) tmem_free<2>(tmem, T::kTmemCols);
 }
 
 }  // namespace kb

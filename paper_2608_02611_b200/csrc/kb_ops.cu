@@ -171,6 +171,8 @@ kb_status prepare_matmul(kb_ctx* ctx) {
   KB_TRY(lanes_attr<32>(ctx));
   KB_TRY(lanes_attr<64>(ctx));
   KB_TRY(lanes_attr<128>(ctx));
+  KB_CUDA(ctx, cudaFuncSetAttribute(matmul_pair_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)PairTile::kSmem));
+  KB_CUDA(ctx, cudaFuncSetAttribute(matmul_pair_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)PairTile::kSmem));
   ctx->encode_tiled = fn;
   ctx->ops_ready = true;
   return KB_OK;
@@ -215,6 +217,24 @@ kb_status launch_lanes(kb_ctx* ctx, MatmulParams& p, const void* a, uint64_t lda
   cfg.attrs = attr;
   cfg.numAttrs = 1;
   KB_CUDA(ctx, cudaLaunchKernelEx(&cfg, matmul_lanes_kernel<BN>, map_b, map_a, p));
+  return launched(ctx);
+}
+
+kb_status launch_pair(kb_ctx* ctx, MatmulParams& p, const void* a, uint64_t lda, bool a_e5m2, const void* b,
+                      uint64_t ldb, bool b_e5m2, uint64_t K, cudaStream_t st) {
+  CUtensorMap map_a, map_b;
+  KB_TRY(encode_map(ctx, &map_a, a, p.M, K, lda, 128));
+  KB_TRY(encode_map(ctx, &map_b, b, p.N, K, ldb, 128));
+  p.idesc = mma_idesc_f8(a_e5m2, b_e5m2, 256, 256);
+  p.tiles_m = (p.M + 255) / 256;
+  p.splits = 1;
+  const uint64_t tiles = (uint64_t)p.tiles_m * ((p.N + 255) / 256);
+  if (tiles > 0x3FFFFFFFull) return fail(ctx, KB_ERR_UNSUPPORTED, "kb_matmul_blocks: more than 2^30 - 1 tiles");
+  const unsigned int pairs = (unsigned int)std::min<uint64_t>(tiles, (uint64_t)ctx->sm_count / 2);
+  if (p.b_scale_shift)
+    matmul_pair_kernel<false><<<2 * pairs, PairTile::kThreads, PairTile::kSmem, st>>>(map_a, map_b, p);
+  else
+    matmul_pair_kernel<true><<<2 * pairs, PairTile::kThreads, PairTile::kSmem, st>>>(map_a, map_b, p);
   return launched(ctx);
 }
 
@@ -422,9 +442,11 @@ extern "C" kb_status kb_matmul_blocks(kb_ctx* ctx, const void* d_a, uint64_t lda
   p.b_scale_ld = b_mode == KB_SCALE_TILES ? (p.N + 127) / 128 : p.N;
   p.out = (int)d_dtype;
   p.status = ctx->d_status;
+  p.vec_out = rows_aligned(d_d, ldd, e);
   const bool ae = a_dtype == KB_F8E5M2, be = b_dtype == KB_F8E5M2;
   if (M <= 16) return launch_lanes<16>(ctx, p, d_a, lda, ae, d_b, ldb, be, K, st);
   if (M <= 32) return launch_lanes<32>(ctx, p, d_a, lda, ae, d_b, ldb, be, K, st);
   if (M <= 64) return launch_lanes<64>(ctx, p, d_a, lda, ae, d_b, ldb, be, K, st);
+  if (M > 256) return launch_pair(ctx, p, d_a, lda, ae, d_b, ldb, be, K, st);
   return launch_lanes<128>(ctx, p, d_a, lda, ae, d_b, ldb, be, K, st);
 }
