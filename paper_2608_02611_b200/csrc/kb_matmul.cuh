@@ -321,7 +321,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PairTile::kThreads, 
                        const MatmulParams p) {
   using T = PairTile;
   extern __shared__ unsigned char dyn[];
-  __shared__ uint64_t full[T::kStages], empty[T::kStages], acc_full[2], acc_empty[2], drained;
+  __shared__ uint64_t full[T::kStages], done[T::kStages], acc_empty[2], drained[2];
   __shared__ uint64_t sc_full[T::kScaleSlots], sc_empty[T::kScaleSlots];
   __shared__ uint32_t tmem_base;
   __shared__ unsigned int abort_word;
@@ -337,17 +337,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PairTile::kThreads, 
   if (threadIdx.x == 0) {
     for (uint32_t i = 0; i < T::kStages; ++i) {
       mbar_init(&full[i], 1);
-      mbar_init(&empty[i], 1);
+      mbar_init(&done[i], 1);
     }
     for (uint32_t i = 0; i < 2; ++i) {
-      mbar_init(&acc_full[i], 1);
       mbar_init(&acc_empty[i], 2 * T::kEpiWarps);
+      mbar_init(&drained[i], 1);
     }
     for (uint32_t i = 0; i < T::kScaleSlots; ++i) {
       mbar_init(&sc_full[i], 32);
       mbar_init(&sc_empty[i], T::kEpiWarps);
     }
-    mbar_init(&drained, 1);
     abort_word = 0u;
     mbar_fence_init();
   }
@@ -369,7 +368,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PairTile::kThreads, 
         pair_tile(t, p.tiles_m, tiles_n, tm, tn);
         const int ya = (int)(tm * 256 + rank * 128), yb = (int)(tn * 256 + rank * 128);
         for (uint32_t kb = 0; kb < p.KB; ++kb) {
-          if (!mbar_wait_bounded(&empty[st], phase ^ 1u, abort_flag, p.status)) {
+          if (!mbar_wait_bounded(&done[st], phase ^ 1u, abort_flag, p.status)) {
             ok = false;
             break;
           }
@@ -395,37 +394,31 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PairTile::kThreads, 
       }
     }
     __syncwarp();
-  } else if (warp == 1) {
+  } else if (warp == 1 || warp == 3) {
+    // Matrix instructions: one thread takes the even K blocks and their accumulator, another the
+    // odd ones, so that what a thread spends on its waits hides under the other's products.
+    const uint32_t a = warp >> 1;
     if (lane == 0 && rank == 0) {
-      uint32_t st = 0, phase = 0, it = 0;
-      bool ok = true;
-      for (uint32_t t = first; t < tiles && ok; t += step) {
-        for (uint32_t kb = 0; kb < p.KB; ++kb, ++it) {
-          const uint32_t a = it & 1u, a_phase = (it >> 1) & 1u;
-          if (!mbar_wait_bounded(&full[st], phase, abort_flag, p.status) ||
-              !mbar_wait_bounded(&acc_empty[a], a_phase ^ 1u, abort_flag, p.status)) {
-            ok = false;
-            break;
-          }
-          tc_fence_after();
-          const uint32_t s = smem_u32(stages + st * T::kStageBytes);
-          const uint64_t a_desc = smem_desc_k128(s), b_desc = smem_desc_k128(s + T::kHalfBytes);
-#pragma unroll
-          for (int k = 0; k < 4; ++k)
-            mma_f8<2>(tmem + a * 256, a_desc + 2 * k, b_desc + 2 * k, p.idesc, k > 0);
-          mma_commit_pair(&acc_full[a]);
-          mma_commit_pair(&empty[st]);
-          if (++st == T::kStages) {
-            st = 0;
-            phase ^= 1u;
-          }
+      uint32_t it = 0;
+      const uint32_t nkb = tiles > first ? ((tiles - first + step - 1) / step) * p.KB : 0;
+      for (it = a; it < nkb; it += 2) {
+        const uint32_t st = it % T::kStages;
+        if (!mbar_wait_bounded(&full[st], (it / T::kStages) & 1u, abort_flag, p.status) ||
+            !mbar_wait_bounded(&acc_empty[a], ((it >> 1) & 1u) ^ 1u, abort_flag, p.status)) {
+          // what has been issued ends before tensor memory is freed
+          mma_commit_pair(&drained[a]);
+          const unsigned long long t0 = global_ns();
+          while (!mbar_try_wait(&drained[a], 0))
+            if (global_ns() - t0 > 1000000000ull) break;
+          break;
         }
-      }
-      if (!ok) {   // what has been issued ends before tensor memory is freed
-        mma_commit_pair(&drained);
-        const unsigned long long t0 = global_ns();
-        while (!mbar_try_wait(&drained, 0))
-          if (global_ns() - t0 > 1000000000ull) break;
+        tc_fence_after();
+        const uint32_t s = smem_u32(stages + st * T::kStageBytes);
+        const uint64_t a_desc = smem_desc_k128(s), b_desc = smem_desc_k128(s + T::kHalfBytes);
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          mma_f8<2>(tmem + a * 256, a_desc + 2 * k, b_desc + 2 * k, p.idesc, k > 0);
+        mma_commit_pair(&done[st]);   // frees the stage and hands over the accumulator
       }
     }
     __syncwarp();
@@ -477,26 +470,30 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PairTile::kThreads, 
       for (uint32_t kb = 0; kb < p.KB; ++kb, ++it) {
         const uint32_t a = it & 1u, slot = it % T::kScaleSlots;
         ok = __all_sync(0xFFFFFFFFu, mbar_wait_bounded(&sc_full[slot], (it / T::kScaleSlots) & 1u, abort_flag, p.status) &&
-                                         mbar_wait_bounded(&acc_full[a], (it >> 1) & 1u, abort_flag, p.status));
+                                         mbar_wait_bounded(&done[it % T::kStages], (it / T::kStages) & 1u, abort_flag, p.status));
         if (!ok) break;
         tc_fence_after();
         float s = row_scale[slot][quarter * 32 + lane];
         if constexpr (!BROWS) s *= col_scale[slot][half];
         const unsigned long long s2 = pack_f32x2(s, s);
         const float* c = &col_scale[slot][BROWS ? half * 128 : 0];
+        // 16 columns at a time, the next 16 on their way while these are scaled and added
+        float v[2][16];
+        tmem_ld16(taddr + a * 256, v[0]);
 #pragma unroll
-        for (int j0 = 0; j0 < 128; j0 += 32) {
-          float v[32];
-          tmem_ld32(taddr + a * 256 + j0, v);
+        for (int j0 = 0; j0 < 128; j0 += 16) {
           tmem_wait_ld();
-          if (j0 == 96) {   // all of this accumulator is in registers
+          if (j0 + 16 < 128) {
+            tmem_ld16(taddr + a * 256 + j0 + 16, v[(j0 / 16 + 1) & 1]);
+          } else {   // all of this accumulator is in registers
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive_cluster(release0 + a * 8);
           }
+          const float(&w)[16] = v[(j0 / 16) & 1];
 #pragma unroll
-          for (int j = 0; j < 32; j += 2) {
-            unsigned long long d = pack_f32x2(v[j], v[j + 1]);
+          for (int j = 0; j < 16; j += 2) {
+            unsigned long long d = pack_f32x2(w[j], w[j + 1]);
             if constexpr (BROWS) d = mul_f32x2(d, *reinterpret_cast<const unsigned long long*>(c + j0 + j));
             acc[(j0 + j) / 2] = fma_f32x2(d, s2, acc[(j0 + j) / 2]);
           }
