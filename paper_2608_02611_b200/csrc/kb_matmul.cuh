@@ -259,37 +259,31 @@ __global__ void __launch_bounds__(LaneTile<BN>::kThreads, 1)
 struct PairTile {
   static constexpr uint32_t kHalfBytes = 128 * 128;             // one operand's share of a CTA
   static constexpr uint32_t kStageBytes = 2 * kHalfBytes;
-  static constexpr uint32_t kStages = 6;
-  static constexpr uint32_t kScaleSlots = 8;                    // K blocks whose scales are in shared memory
+  static constexpr uint32_t kStages = 5;
+  static constexpr uint32_t kScaleStep = 4;                     // K blocks whose scales share a slot of shared memory
+  static constexpr uint32_t kScaleSlots = 3;
   static constexpr uint32_t kTmemCols = 512;
-  static constexpr uint32_t kSmem = 1024 + kStages * kStageBytes;
   static constexpr int kEpiWarps = 8;
   // three warpgroups: one copies and issues, two scale and add.  168 registers per thread at
   // launch are split 104 / 200 / 200: 128 running sums and what is in flight need the 200.
   static constexpr int kThreads = 128 + 32 * kEpiWarps;
   static constexpr int kRegsLaunch = 168, kRegsControl = 104, kRegsEpi = 200;
-  static_assert(kRegsControl + 2 * kRegsEpi <= 3 * kRegsLaunch, "register shares");
+  static_assert(128 * kRegsControl + (kThreads - 128) * kRegsEpi <= kThreads * kRegsLaunch, "register shares");
+  // results leave through shared memory, 64 bytes of 32 rows per warp at a time, so that every
+  // store of a warp covers whole 32-byte sectors; 80-byte rows keep the 16-byte accesses apart
+  static constexpr uint32_t kOutPitch = 80;
+  static constexpr uint32_t kOutBytes = 32 * kOutPitch;
+  static constexpr uint32_t kSmem = 1024 + kStages * kStageBytes + kEpiWarps * kOutBytes;
   static constexpr uint32_t kGroupM = 8;                        // tiles of A that neighbouring pairs share
 };
 
-__device__ __forceinline__ unsigned long long pack_f32x2(float lo, float hi) {
-  unsigned long long r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
-  return r;
-}
-__device__ __forceinline__ void unpack_f32x2(unsigned long long v, float& lo, float& hi) {
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v));
-}
-__device__ __forceinline__ unsigned long long fma_f32x2(unsigned long long a, unsigned long long b,
-                                                        unsigned long long c) {
-  unsigned long long d;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
-  return d;
-}
-__device__ __forceinline__ unsigned long long mul_f32x2(unsigned long long a, unsigned long long b) {
-  unsigned long long d;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-  return d;
+// c0 += v0 * s, c1 += v1 * s as one packed instruction
+__device__ __forceinline__ void fma_pair(float& c0, float& c1, float v0, float v1, float s) {
+  asm("{\n.reg .b64 c, v, s;\n"
+      "mov.b64 c, {%0, %1};\nmov.b64 v, {%2, %3};\nmov.b64 s, {%4, %4};\n"
+      "fma.rn.f32x2 c, v, s, c;\nmov.b64 {%0, %1}, c;\n}"
+      : "+f"(c0), "+f"(c1)
+      : "f"(v0), "f"(v1), "f"(s));
 }
 
 // Tile coordinates of item `t`: down kGroupM tiles of A, then along B, so that the pairs that run
@@ -302,15 +296,50 @@ __device__ __forceinline__ void pair_tile(uint32_t t, uint32_t tiles_m, uint32_t
   tn = r / h;
 }
 
-// 8 results of one row
+// A warp's 32 rows x 128 columns of results (lane = row) to D at row m0 and column n0.
 template <int DT>
-__device__ __forceinline__ void store_row8(void* d, uint64_t i, const float (&v)[8], uint32_t n, uint32_t N, bool vec) {
-  if (vec && n + 8 <= N) {
-    store8<DT>(d, i, v);
-  } else {
+__device__ __forceinline__ void store_warp_tile(const MatmulParams& p, unsigned char* buf, int lane, uint32_t m0,
+                                                uint32_t n0, const float (&acc)[128]) {
+  constexpr int kBytes = DT == KB_F32 ? 4 : 2;
+  constexpr int kCols = 64 / kBytes;        // columns per round: 64 bytes
+  constexpr int kUnit = 16 / kBytes;        // columns per 16 bytes
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (n + j < N) store_elem<DT>(d, i + j, v[j]);
+  for (int c = 0; c < 128; c += kCols) {
+    if (n0 + c >= p.N) break;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const float* v = acc + c + u * kUnit;
+      uint4 w;
+      if constexpr (DT == KB_F32)
+        w = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+      else
+        w = make_uint4(pack2<DT>(v[0], v[1]), pack2<DT>(v[2], v[3]), pack2<DT>(v[4], v[5]), pack2<DT>(v[6], v[7]));
+      *reinterpret_cast<uint4*>(buf + lane * PairTile::kOutPitch + u * 16) = w;
+    }
+    __syncwarp();
+    if (p.vec_out && n0 + c + kCols <= p.N) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t row = i * 8 + (lane >> 2), unit = lane & 3;
+        if (m0 + row < p.M)
+          *reinterpret_cast<uint4*>(static_cast<unsigned char*>(p.d) +
+                                    ((uint64_t)(m0 + row) * p.ldd + n0 + c + unit * kUnit) * kBytes) =
+              *reinterpret_cast<const uint4*>(buf + row * PairTile::kOutPitch + unit * 16);
+      }
+    } else {
+      for (int i = lane; i < 32 * kCols; i += 32) {
+        const uint32_t row = i / kCols, col = i % kCols;
+        if (m0 + row < p.M && n0 + c + col < p.N) {
+          const uint64_t at = (uint64_t)(m0 + row) * p.ldd + n0 + c + col;
+          const unsigned char* src = buf + row * PairTile::kOutPitch + col * kBytes;
+          if constexpr (DT == KB_F32)
+            static_cast<uint32_t*>(p.d)[at] = *reinterpret_cast<const uint32_t*>(src);
+          else
+            static_cast<unsigned short*>(p.d)[at] = *reinterpret_cast<const unsigned short*>(src);
+        }
+      }
+    }
+    __syncwarp();
   }
 }
 
@@ -325,8 +354,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PairTile::kThreads, 
   __shared__ uint64_t sc_full[T::kScaleSlots], sc_empty[T::kScaleSlots];
   __shared__ uint32_t tmem_base;
   __shared__ unsigned int abort_word;
-  __shared__ __align__(16) float row_scale[T::kScaleSlots][128];
-  __shared__ __align__(16) float col_scale[T::kScaleSlots][BROWS ? 256 : 2];
+  __shared__ __align__(16) float row_scale[T::kScaleSlots][128][T::kScaleStep];
+  __shared__ __align__(16) float col_scale[T::kScaleSlots][BROWS ? T::kScaleStep * 256 : 2 * T::kScaleStep];
   volatile unsigned int* abort_flag = &abort_word;
   unsigned char* stages = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(dyn) + 1023) & ~(uintptr_t)1023);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -423,103 +452,125 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PairTile::kThreads, 
     }
     __syncwarp();
   } else if (warp == 2) {
-    // the scales of each K block, several blocks ahead of their use
-    uint32_t it = 0;
+    // the scales of kScaleStep K blocks at a time, one or two steps ahead of their use
+    uint32_t slot = 0, phase = 0;
     bool ok = true;
     for (uint32_t t = first; t < tiles && ok; t += step) {
       uint32_t tm, tn;
       pair_tile(t, p.tiles_m, tiles_n, tm, tn);
       const uint32_t m0 = tm * 256 + rank * 128, n0 = tn * 256;
-      for (uint32_t kb = 0; kb < p.KB; ++kb, ++it) {
-        const uint32_t slot = it % T::kScaleSlots, phase = (it / T::kScaleSlots) & 1u;
+      for (uint32_t kb0 = 0; kb0 < p.KB; kb0 += T::kScaleStep) {
         ok = __all_sync(0xFFFFFFFFu, mbar_wait_bounded(&sc_empty[slot], phase ^ 1u, abort_flag, p.status));
         if (!ok) break;
-        const float* as = p.a_scale + (uint64_t)kb * p.M;
-        const float* bs = p.b_scale + (uint64_t)kb * p.b_scale_ld;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const uint32_t m = m0 + i * 32 + lane;
-          cp_async_f32(&row_scale[slot][i * 32 + lane], m < p.M ? as + m : as, m < p.M);
-        }
-        if constexpr (BROWS) {
+        for (uint32_t k = 0; k < T::kScaleStep; ++k) {
+          const bool k_in = kb0 + k < p.KB;
+          const float* as = p.a_scale + (uint64_t)(kb0 + k) * p.M;
+          const float* bs = p.b_scale + (uint64_t)(kb0 + k) * p.b_scale_ld;
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const uint32_t n = n0 + i * 32 + lane;
-            cp_async_f32(&col_scale[slot][i * 32 + lane], n < p.N ? bs + n : bs, n < p.N);
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t m = m0 + i * 32 + lane;
+            const bool in = k_in && m < p.M;
+            cp_async_f32(&row_scale[slot][i * 32 + lane][k], in ? as + m : p.a_scale, in);
           }
-        } else if (lane < 2) {
-          const uint32_t n = n0 + lane * 128;
-          cp_async_f32(&col_scale[slot][lane], n < p.N ? bs + (n >> 7) : bs, n < p.N);
+          if constexpr (BROWS) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const uint32_t n = n0 + i * 32 + lane;
+              const bool in = k_in && n < p.N;
+              cp_async_f32(&col_scale[slot][k * 256 + i * 32 + lane], in ? bs + n : p.b_scale, in);
+            }
+          } else if (lane < 2) {
+            const uint32_t n = n0 + lane * 128;
+            const bool in = k_in && n < p.N;
+            cp_async_f32(&col_scale[slot][lane * T::kScaleStep + k], in ? bs + (n >> 7) : p.b_scale, in);
+          }
         }
         cp_async_arrive(&sc_full[slot]);
+        if (++slot == T::kScaleSlots) {
+          slot = 0;
+          phase ^= 1u;
+        }
       }
     }
     cp_async_wait_all();
     __syncwarp();
   } else if (warp >= 4) {
     regs_grow<T::kRegsEpi>();
-    const int quarter = warp & 3, half = (warp - 4) >> 2;
-    const uint32_t taddr = tmem + ((uint32_t)(quarter * 32) << 16) + half * 128;
+    const int quarter = warp & 3, cols = ((warp - 4) >> 2) * 128;   // 32 rows and 128 columns of the tile
+    const uint32_t taddr = tmem + ((uint32_t)(quarter * 32) << 16) + cols;
+    unsigned char* out_buf = stages + T::kStages * T::kStageBytes + (warp - 4) * T::kOutBytes;
     const uint32_t release0 = map_to_rank(smem_u32(&acc_empty[0]), 0);
-    uint32_t it = 0;
+    uint32_t a = 0, st = 0, st_phase = 0, slot = 0, slot_phase = 0;
+    // After a wait has run out every later one returns at once, so the loops just run to their end;
+    // no lane leaves its warp, whose reads of tensor memory are collective.
     bool ok = true;
-    for (uint32_t t = first; t < tiles && ok; t += step) {
-      unsigned long long acc[64];
+    for (uint32_t t = first; t < tiles; t += step) {
+      float acc[128];
 #pragma unroll
-      for (int j = 0; j < 64; ++j) acc[j] = 0ull;
-      for (uint32_t kb = 0; kb < p.KB; ++kb, ++it) {
-        const uint32_t a = it & 1u, slot = it % T::kScaleSlots;
-        ok = __all_sync(0xFFFFFFFFu, mbar_wait_bounded(&sc_full[slot], (it / T::kScaleSlots) & 1u, abort_flag, p.status) &&
-                                         mbar_wait_bounded(&done[it % T::kStages], (it / T::kStages) & 1u, abort_flag, p.status));
-        if (!ok) break;
-        tc_fence_after();
-        float s = row_scale[slot][quarter * 32 + lane];
-        if constexpr (!BROWS) s *= col_scale[slot][half];
-        const unsigned long long s2 = pack_f32x2(s, s);
-        const float* c = &col_scale[slot][BROWS ? half * 128 : 0];
-        // 16 columns at a time, the next 16 on their way while these are scaled and added
-        float v[2][16];
-        tmem_ld16(taddr + a * 256, v[0]);
-#pragma unroll
-        for (int j0 = 0; j0 < 128; j0 += 16) {
-          tmem_wait_ld();
-          if (j0 + 16 < 128) {
-            tmem_ld16(taddr + a * 256 + j0 + 16, v[(j0 / 16 + 1) & 1]);
-          } else {   // all of this accumulator is in registers
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive_cluster(release0 + a * 8);
+      for (int j = 0; j < 128; ++j) acc[j] = 0.0f;
+      for (uint32_t kb0 = 0; kb0 < p.KB; kb0 += T::kScaleStep) {
+        ok &= mbar_wait_bounded(&sc_full[slot], slot_phase, abort_flag, p.status);
+        const float4 rs = *reinterpret_cast<const float4*>(row_scale[slot][quarter * 32 + lane]);
+        float s4[4] = {rs.x, rs.y, rs.z, rs.w};
+        if constexpr (!BROWS) {
+          const float4 cs = *reinterpret_cast<const float4*>(&col_scale[slot][(cols >> 7) * T::kScaleStep]);
+          s4[0] *= cs.x;
+          s4[1] *= cs.y;
+          s4[2] *= cs.z;
+          s4[3] *= cs.w;
+        }
+#pragma unroll 1
+        for (uint32_t k = 0; k < T::kScaleStep && kb0 + k < p.KB; ++k) {
+          ok &= mbar_wait_bounded(&done[st], st_phase, abort_flag, p.status);
+          __syncwarp();
+          tc_fence_after();
+          const float s = s4[0];
+          s4[0] = s4[1];
+          s4[1] = s4[2];
+          s4[2] = s4[3];
+          const float* c = &col_scale[slot][BROWS ? k * 256 + cols : 0];
+          if (++st == T::kStages) {
+            st = 0;
+            st_phase ^= 1u;
           }
-          const float(&w)[16] = v[(j0 / 16) & 1];
+          // 16 columns at a time, the next 16 on their way while these are scaled and added
+          float v[2][16];
+          tmem_ld16(taddr + a * 256, v[0]);
 #pragma unroll
-          for (int j = 0; j < 16; j += 2) {
-            unsigned long long d = pack_f32x2(w[j], w[j + 1]);
-            if constexpr (BROWS) d = mul_f32x2(d, *reinterpret_cast<const unsigned long long*>(c + j0 + j));
-            acc[(j0 + j) / 2] = fma_f32x2(d, s2, acc[(j0 + j) / 2]);
+          for (int j0 = 0; j0 < 128; j0 += 16) {
+            tmem_wait_ld();
+            if (j0 + 16 < 128) {
+              tmem_ld16(taddr + a * 256 + j0 + 16, v[(j0 / 16 + 1) & 1]);
+            } else {   // all of this accumulator is in registers
+              tc_fence_before();
+              mbar_arrive_cluster_if(release0 + a * 8, lane == 0);
+            }
+            const float(&w)[16] = v[(j0 / 16) & 1];
+#pragma unroll
+            for (int j = 0; j < 16; j += 2)
+              fma_pair(acc[j0 + j], acc[j0 + j + 1], BROWS ? w[j] * c[j0 + j] : w[j],
+                       BROWS ? w[j + 1] * c[j0 + j + 1] : w[j + 1], s);
           }
+          a ^= 1u;
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(&sc_empty[slot]);
+        if (++slot == T::kScaleSlots) {
+          slot = 0;
+          slot_phase ^= 1u;
+        }
       }
       uint32_t tm, tn;
       pair_tile(t, p.tiles_m, tiles_n, tm, tn);
-      const uint32_t m = tm * 256 + rank * 128 + quarter * 32 + lane, n0 = tn * 256 + half * 128;
-      if (ok && m < p.M && n0 < p.N) {
-        const uint64_t row = (uint64_t)m * p.ldd;
-#pragma unroll
-        for (int j = 0; j < 128; j += 8) {
-          float v[8];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) unpack_f32x2(acc[j / 2 + i], v[2 * i], v[2 * i + 1]);
-          const uint32_t n = n0 + j;
-          if (n >= p.N) break;
-          if (p.out == KB_BF16)
-            store_row8<KB_BF16>(p.d, row + n, v, n, p.N, p.vec_out);
-          else if (p.out == KB_F16)
-            store_row8<KB_F16>(p.d, row + n, v, n, p.N, p.vec_out);
-          else
-            store_row8<KB_F32>(p.d, row + n, v, n, p.N, p.vec_out);
-        }
+      if (__all_sync(0xFFFFFFFFu, ok)) {
+        const uint32_t m0 = tm * 256 + rank * 128 + quarter * 32, n0 = tn * 256 + cols;
+        if (p.out == KB_BF16)
+          store_warp_tile<KB_BF16>(p, out_buf, lane, m0, n0, acc);
+        else if (p.out == KB_F16)
+          store_warp_tile<KB_F16>(p, out_buf, lane, m0, n0, acc);
+        else
+          store_warp_tile<KB_F32>(p, out_buf, lane, m0, n0, acc);
       }
     }
   }

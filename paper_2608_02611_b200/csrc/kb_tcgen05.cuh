@@ -161,8 +161,12 @@ __device__ __forceinline__ float ld_cluster_f32(uint32_t addr) {
 // Arrival on a barrier of any CTA of the cluster.  No cluster-wide release (which would wait for
 // every earlier memory access of the thread): it hands over tensor memory, whose accesses the
 // tcgen05 fences order.
-__device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_bar) {
-  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
+// Predicated inside the statement: no branch for the warp to come together after.
+__device__ __forceinline__ void mbar_arrive_cluster_if(uint32_t cluster_bar, bool yes) {
+  asm volatile(
+      "{\n.reg .pred p;\nsetp.ne.u32 p, %1, 0;\n@p mbarrier.arrive.shared::cluster.b64 _, [%0];\n}" ::"r"(cluster_bar),
+      "r"(yes ? 1u : 0u)
+      : "memory");
 }
 
 // ---- small asynchronous copies -----------------------------------------------------------------
