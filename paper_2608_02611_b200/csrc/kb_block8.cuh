@@ -83,6 +83,9 @@ __device__ __forceinline__ void load_group(const void* base, uint64_t row0, uint
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[j] = fill;
     }
+  } else if ((g + 1) * kGroup <= cols) {   // a whole group: no test per element
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = load_elem<DT>(base, row0 + group_col<false>(g, lane, j));
   } else {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
@@ -91,12 +94,23 @@ __device__ __forceinline__ void load_group(const void* base, uint64_t row0, uint
     }
   }
 }
+// Sets a lane's elements past the row's end.
+template <bool VEC>
+__device__ __forceinline__ void fill_tail(uint32_t g, int lane, uint32_t cols, float value, float (&v)[8]) {
+  if ((g + 1) * kGroup <= cols) return;
+#pragma unroll
+  for (int j = 0; j < 8; ++j)
+    if (group_col<VEC>(g, lane, j) >= cols) v[j] = value;
+}
 template <int DT, bool VEC>
 __device__ __forceinline__ void store_group(void* base, uint64_t row0, uint32_t g, int lane, uint32_t cols,
                                             const float (&v)[8]) {
   if constexpr (VEC) {
     const uint32_t c = group_col<true>(g, lane, 0);
     if (c < cols) store8<DT>(base, row0 + c, v);
+  } else if ((g + 1) * kGroup <= cols) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) store_elem<DT>(base, row0 + group_col<false>(g, lane, j), v[j]);
   } else {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
@@ -131,8 +145,6 @@ __device__ __forceinline__ BlockScale block_scale(float amax) {
   const float a = fmaxf(amax, 0x1p-100f);
   return {__fdiv_rn(a, top), __fdiv_rn(top, a)};
 }
-constexpr unsigned int kInfBits = 0x7F800000u;
-__device__ __forceinline__ unsigned int abs_bits(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
 // Two values to two codes (lo in the low byte), saturating; NaN becomes NaN.
 template <bool E5M2>
 __device__ __forceinline__ uint32_t quant2(float lo, float hi) {
@@ -152,27 +164,29 @@ __device__ __forceinline__ uint2 quant8(const float (&v)[8], float inv) {
         quant2<E5M2>(__fmul_rn(v[6], inv), __fmul_rn(v[7], inv)) << 16;
   return r;
 }
-// Largest magnitude as bits; magnitudes order like their bit patterns, Inf and NaN above all
-// finite ones, so one integer maximum also tells whether a block holds any.
+// Largest magnitude, NaN left out (the maximum of a number and NaN is the number).
 template <int J0, int J1>
-__device__ __forceinline__ unsigned int max_bits(const float (&v)[8]) {
-  unsigned int m = 0u;
+__device__ __forceinline__ float max_abs(const float (&v)[8]) {
+  float m = 0.0f;
 #pragma unroll
-  for (int j = J0; j < J1; ++j) m = max(m, abs_bits(v[j]));
+  for (int j = J0; j < J1; ++j) m = fmaxf(m, fabsf(v[j]));
   return m;
 }
-// Non-finite values of a block that holds some become NaN; returns the largest finite magnitude.
+// For a block whose maximum is infinite: Inf becomes NaN; returns the largest finite magnitude.
 template <int J0, int J1>
-__device__ __forceinline__ unsigned int settle_nonfinite(float (&v)[8]) {
-  unsigned int m = 0u;
+__device__ __forceinline__ float settle_inf(float (&v)[8]) {
+  float m = 0.0f;
 #pragma unroll
   for (int j = J0; j < J1; ++j) {
-    if (abs_bits(v[j]) >= kInfBits)
-      v[j] = __uint_as_float(0x7FFFFFFFu);
-    else
-      m = max(m, abs_bits(v[j]));
+    if (isinf(v[j])) v[j] = __uint_as_float(0x7FFFFFFFu);
+    m = fmaxf(m, fabsf(v[j]));
   }
   return m;
+}
+__device__ __forceinline__ float warp_max(float v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, o));
+  return v;
 }
 
 // Quantise a lane's part of group g of row `row`: codes to q, the blocks' scales to
@@ -183,24 +197,24 @@ __device__ __forceinline__ void quant_group(float (&v)[8], uint32_t g, int lane,
   if constexpr (VEC) {
     const uint32_t c = group_col<true>(g, lane, 0);
     const unsigned int half = 0xFFFFu << (lane & 16);
-    unsigned int m = max_bits<0, 8>(v);
+    float m = max_abs<0, 8>(v);
 #pragma unroll
-    for (int o = 8; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(half, m, o));
-    if (m >= kInfBits) {   // the same for the block's 16 lanes
-      m = settle_nonfinite<0, 8>(v);
+    for (int o = 8; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(half, m, o));
+    if (isinf(m)) {   // the same for the block's 16 lanes
+      m = settle_inf<0, 8>(v);
 #pragma unroll
-      for (int o = 8; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(half, m, o));
+      for (int o = 8; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(half, m, o));
     }
-    const BlockScale s = block_scale<E5M2>(__uint_as_float(m));
+    const BlockScale s = block_scale<E5M2>(m);
     if (c < cols) {
       *reinterpret_cast<uint2*>(q + row * ldq + c) = quant8<E5M2>(v, s.inv);
       if ((lane & 15) == 0) scale[(uint64_t)(c >> 7) * rows + row] = s.scale;
     }
   } else {
-    unsigned int m0 = warp_max_u32(max_bits<0, 4>(v)), m1 = warp_max_u32(max_bits<4, 8>(v));
-    if (m0 >= kInfBits) m0 = warp_max_u32(settle_nonfinite<0, 4>(v));
-    if (m1 >= kInfBits) m1 = warp_max_u32(settle_nonfinite<4, 8>(v));
-    const BlockScale s0 = block_scale<E5M2>(__uint_as_float(m0)), s1 = block_scale<E5M2>(__uint_as_float(m1));
+    float m0 = warp_max(max_abs<0, 4>(v)), m1 = warp_max(max_abs<4, 8>(v));
+    if (isinf(m0)) m0 = warp_max(settle_inf<0, 4>(v));
+    if (isinf(m1)) m1 = warp_max(settle_inf<4, 8>(v));
+    const BlockScale s0 = block_scale<E5M2>(m0), s1 = block_scale<E5M2>(m1);
     const uint2 r0 = quant8<E5M2>(v, s0.inv), r1 = quant8<E5M2>(v, s1.inv);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {

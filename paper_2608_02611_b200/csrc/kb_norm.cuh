@@ -1,12 +1,18 @@
 // Layer norm, forward and backward (contracts in include/kb_ops.h).
 //
-// Forward: a row lives in the registers of one warp (short rows) or one CTA, 8 elements per lane
-// and group of 256 (kb_block8.cuh).  The mean and then the sum of squared distances from it are
-// reduced from the registers, so the row is read once and the variance does not suffer from the
-// cancellation of sum(x^2)/n - mean^2.  The same registers then give y and, where asked for, the
-// row's 8-bit blocks, so a consumer in 8 bits costs no second pass over y.
+// Forward: a row lives in the registers of one warp (up to 1024 columns) or one CTA, 8 elements
+// per lane and group of 256 (kb_block8.cuh).  The mean and then the sum of squared distances from
+// it are reduced from the registers, so the row is read once and the variance does not suffer from
+// the cancellation of sum(x^2)/n - mean^2.  The same registers then give y and, where asked for,
+// the row's 8-bit blocks, so a consumer in 8 bits costs no second pass over y.
 //
-// Bound: memory.  Each element is read and written once; the parameters stay in L1/L2.
+// Backward: the same, walking over rows; each lane keeps its columns' sums of dy * xh and dy in
+// registers over all its rows.  They leave once, as a partial row per CTA, and norm_param_kernel
+// adds the partial rows in order.  So x and dy are read once for all three gradients.
+//
+// Bound: memory; each element is read and written once.  A CTA that walks over many rows gets them
+// through a ring in shared memory filled by 1-D bulk copies, several rows ahead: the registers that
+// hold the sums and the parameters leave too few warps to cover the memory's latency otherwise.
 #pragma once
 
 #include "kb_block8.cuh"
@@ -24,8 +30,10 @@ struct NormParams {
   float* scale;
   uint64_t rows, ldx, ldy, ldq;
   uint32_t cols, groups;
+  uint32_t stages, slot_bytes;   // of the row ring
   float eps;
   bool param_f32, e5m2;
+  unsigned int* status;
 };
 
 struct NormBwdParams {
@@ -38,7 +46,9 @@ struct NormBwdParams {
   float* partial;            // [partial rows][2][cols]: dweight, dbias
   uint64_t rows, lddy, ldx, lddx;
   uint32_t cols, groups;
+  uint32_t stages, slot_bytes;   // of the row ring
   bool param_f32, want_param;
+  unsigned int* status;
 };
 
 __device__ __forceinline__ float warp_sum(float v) {
@@ -55,20 +65,15 @@ __device__ __forceinline__ float cta_sum(float v, float* red, int warp, int lane
   return warp_sum(lane < nwarps ? red[lane] : 0.0f);
 }
 
-// y and the row's other outputs from a lane's 8 elements of group g
+// y and the row's other outputs from a lane's 8 centred elements (x - mean) of group g
 template <int DT, bool VEC>
-__device__ __forceinline__ void norm_emit(const NormParams& p, uint64_t row, uint32_t g, int lane, float mean,
-                                          float rstd, float (&v)[8]) {
-  float w[8], b[8];
-  load_params<DT, VEC>(p.weight, p.param_f32, g, lane, p.cols, 1.0f, w);
-  load_params<DT, VEC>(p.bias, p.param_f32, g, lane, p.cols, 0.0f, b);
+__device__ __forceinline__ void norm_emit(const NormParams& p, uint64_t row, uint32_t g, int lane, float rstd,
+                                          const float (&w)[8], const float (&b)[8], float (&v)[8]) {
 #pragma unroll
-  for (int j = 0; j < 8; ++j) v[j] = fmaf((v[j] - mean) * rstd, w[j], b[j]);
+  for (int j = 0; j < 8; ++j) v[j] = fmaf(v[j] * rstd, w[j], b[j]);
   if (p.y) store_group<DT, VEC>(p.y, row * p.ldy, g, lane, p.cols, v);
   if (p.q) {
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (group_col<VEC>(g, lane, j) >= p.cols) v[j] = 0.0f;
+    fill_tail<VEC>(g, lane, p.cols, 0.0f, v);
     if (p.e5m2)
       quant_group<true, VEC>(v, g, lane, p.cols, row, p.rows, p.q, p.ldq, p.scale);
     else
@@ -76,40 +81,165 @@ __device__ __forceinline__ void norm_emit(const NormParams& p, uint64_t row, uin
   }
 }
 
-// One row per warp (WARP) or per CTA, NCH groups per warp in registers.
-template <int DT, int NCH, bool VEC, bool WARP>
-__global__ void __launch_bounds__(WARP ? 128 : NCH == 1 ? 1024 : 512) norm_kernel(const NormParams p) {
-  __shared__ float red[2][32];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, nwarps = blockDim.x >> 5;
-  const uint64_t row = WARP ? (uint64_t)blockIdx.x * nwarps + warp : blockIdx.x;
-  if (WARP && row >= p.rows) return;
+// Rows on their way from global memory: a ring of `stages` slots of `tensors` rows each.
+constexpr uint32_t kRowRingStages = 8;   // at most
+struct RowRing {
+  unsigned char* buf;
+  uint64_t* full;
+  volatile unsigned int* abort_flag;
+  unsigned int* status;
+  uint32_t stages, row_bytes, slot_bytes;
+
+  __device__ __forceinline__ void init() {   // one thread
+    for (uint32_t i = 0; i < stages; ++i) mbar_init(&full[i], 1);
+    *abort_flag = 0u;
+    mbar_fence_init();
+  }
+  // one thread: the rows at s0 (and s1) into slot `slot`
+  __device__ __forceinline__ void fetch(uint32_t slot, const void* s0, const void* s1) {
+    const uint64_t policy = l2_policy_evict_first();   // read once
+    mbar_arrive_expect_tx(&full[slot], s1 ? 2 * row_bytes : row_bytes);
+    bulk_g2s(buf + slot * slot_bytes, s0, row_bytes, &full[slot], policy);
+    if (s1) bulk_g2s(buf + slot * slot_bytes + slot_bytes / 2, s1, row_bytes, &full[slot], policy);
+  }
+  __device__ __forceinline__ bool wait(uint32_t slot, uint32_t phase) {
+    return mbar_wait_bounded(&full[slot], phase, abort_flag, status);
+  }
+  // after a wait has run out: let the copies in flight land before the CTA may leave
+  __device__ __forceinline__ void drain(uint64_t issued) {
+    const uint64_t back = issued < stages ? issued : stages;
+    for (uint64_t m = issued - back; m < issued; ++m) {
+      const unsigned long long t0 = global_ns();
+      while (!mbar_try_wait(&full[m % stages], (uint32_t)((m / stages) & 1ull)))
+        if (global_ns() - t0 > 1000000000ull) break;
+    }
+  }
+};
+template <int DT>
+__device__ __forceinline__ const unsigned char* row_ptr(const void* base, uint64_t row, uint64_t ld) {
+  return static_cast<const unsigned char*>(base) + row * ld * Elem<DT>::kBytes;
+}
+
+// A row per warp, NCH groups in registers.
+template <int DT, int NCH, bool VEC>
+__global__ void __launch_bounds__(128) norm_warp_kernel(const NormParams p) {
+  const int lane = threadIdx.x & 31;
+  const uint64_t row = (uint64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
+  if (row >= p.rows) return;
   float v[NCH][8];
-  float s = 0.0f;
 #pragma unroll
-  for (int i = 0; i < NCH; ++i)
-    load_group<DT, VEC>(p.x, row * p.ldx, WARP ? i : i * nwarps + warp, lane, p.cols, v[i]);
+  for (int i = 0; i < NCH; ++i) load_group<DT, VEC>(p.x, row * p.ldx, i, lane, p.cols, v[i]);
+  float s = 0.0f;
 #pragma unroll
   for (int i = 0; i < NCH; ++i)
 #pragma unroll
     for (int j = 0; j < 8; ++j) s += v[i][j];
   const float n = (float)p.cols;
-  const float mean = (WARP ? warp_sum(s) : cta_sum(s, red[0], warp, lane, nwarps)) / n;
+  const float mean = warp_sum(s) / n;
   float ss = 0.0f;
 #pragma unroll
-  for (int i = 0; i < NCH; ++i)
+  for (int i = 0; i < NCH; ++i) {
+    fill_tail<VEC>(i, lane, p.cols, mean, v[i]);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const float d = v[i][j] - mean;
-      if (group_col<VEC>(WARP ? i : i * nwarps + warp, lane, j) < p.cols) ss = fmaf(d, d, ss);
+      v[i][j] -= mean;
+      ss = fmaf(v[i][j], v[i][j], ss);
     }
-  const float var = (WARP ? warp_sum(ss) : cta_sum(ss, red[1], warp, lane, nwarps)) / n;
-  const float rstd = 1.0f / sqrtf(var + p.eps);
+  }
+  const float rstd = 1.0f / sqrtf(warp_sum(ss) / n + p.eps);
 #pragma unroll
-  for (int i = 0; i < NCH; ++i)
-    norm_emit<DT, VEC>(p, row, WARP ? i : i * nwarps + warp, lane, mean, rstd, v[i]);
-  if (lane == 0 && (WARP || warp == 0)) {
+  for (int i = 0; i < NCH; ++i) {
+    float w[8], b[8];
+    load_params<DT, VEC>(p.weight, p.param_f32, i, lane, p.cols, 1.0f, w);
+    load_params<DT, VEC>(p.bias, p.param_f32, i, lane, p.cols, 0.0f, b);
+    norm_emit<DT, VEC>(p, row, i, lane, rstd, w, b, v[i]);
+  }
+  if (lane == 0) {
     if (p.mean) p.mean[row] = mean;
     if (p.rstd) p.rstd[row] = rstd;
+  }
+}
+
+// Rows by CTA, NCH groups per warp in registers; a CTA walks over the rows with the grid's stride
+// and keeps its columns' parameters.  RING (VEC only): rows come through shared memory.
+template <int DT, int NCH, bool VEC, bool RING>
+__global__ void __launch_bounds__(NCH == 1 ? 1024 : 512) norm_cta_kernel(const NormParams p) {
+  __shared__ float red[2][2][32];
+  __shared__ uint64_t full[kRowRingStages];
+  __shared__ unsigned int abort_word;
+  extern __shared__ __align__(128) unsigned char dyn[];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, nwarps = blockDim.x >> 5;
+  RowRing ring{dyn, full, &abort_word, p.status, p.stages, p.cols * Elem<DT>::kBytes, p.slot_bytes};
+  uint64_t issued = 0;
+  if constexpr (RING) {
+    if (threadIdx.x == 0) {
+      ring.init();
+      for (uint64_t r = blockIdx.x; r < p.rows && issued < p.stages; r += gridDim.x, ++issued)
+        ring.fetch((uint32_t)issued, row_ptr<DT>(p.x, r, p.ldx), nullptr);
+    }
+    __syncthreads();
+  }
+  float w[NCH][8], b[NCH][8];
+#pragma unroll
+  for (int i = 0; i < NCH; ++i) {
+    load_params<DT, VEC>(p.weight, p.param_f32, i * nwarps + warp, lane, p.cols, 1.0f, w[i]);
+    load_params<DT, VEC>(p.bias, p.param_f32, i * nwarps + warp, lane, p.cols, 0.0f, b[i]);
+  }
+  const float n = (float)p.cols;
+  uint32_t slot = 0, phase = 0;
+  int turn = 0;
+  for (uint64_t row = blockIdx.x; row < p.rows; row += gridDim.x, turn ^= 1) {
+    float v[NCH][8];
+    if constexpr (RING) {
+      ring.wait(slot, phase);   // on failure the loop runs on, quickly, to keep the barriers together
+#pragma unroll
+      for (int i = 0; i < NCH; ++i)
+        load_group<DT, true>(dyn + slot * p.slot_bytes, 0, i * nwarps + warp, lane, p.cols, v[i]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < NCH; ++i)
+        load_group<DT, VEC>(p.x, row * p.ldx, i * nwarps + warp, lane, p.cols, v[i]);
+    }
+    float s = 0.0f;
+#pragma unroll
+    for (int i = 0; i < NCH; ++i)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) s += v[i][j];
+    const float mean = cta_sum(s, red[turn][0], warp, lane, nwarps) / n;
+    if constexpr (RING) {
+      // every thread has read the row: the slot takes the row that is `stages` ahead
+      const uint64_t ahead = row + (uint64_t)p.stages * gridDim.x;
+      if (threadIdx.x == 0 && ahead < p.rows) {
+        ring.fetch(slot, row_ptr<DT>(p.x, ahead, p.ldx), nullptr);
+        ++issued;
+      }
+      if (++slot == p.stages) {
+        slot = 0;
+        phase ^= 1u;
+      }
+    }
+    float ss = 0.0f;
+#pragma unroll
+    for (int i = 0; i < NCH; ++i) {
+      fill_tail<VEC>(i * nwarps + warp, lane, p.cols, mean, v[i]);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        v[i][j] -= mean;
+        ss = fmaf(v[i][j], v[i][j], ss);
+      }
+    }
+    const float rstd = 1.0f / sqrtf(cta_sum(ss, red[turn][1], warp, lane, nwarps) / n + p.eps);
+#pragma unroll
+    for (int i = 0; i < NCH; ++i)
+      if (NCH == 1 || i * nwarps + warp < p.groups)
+        norm_emit<DT, VEC>(p, row, i * nwarps + warp, lane, rstd, w[i], b[i], v[i]);
+    if (threadIdx.x == 0) {
+      if (p.mean) p.mean[row] = mean;
+      if (p.rstd) p.rstd[row] = rstd;
+    }
+  }
+  if constexpr (RING) {
+    if (threadIdx.x == 0 && abort_word) ring.drain(issued);
   }
 }
 
@@ -142,8 +272,13 @@ __global__ void __launch_bounds__(512) norm_long_kernel(const NormParams p) {
   const float rstd = 1.0f / sqrtf(var + p.eps);
   for (uint32_t g = warp; g < p.groups; g += nwarps) {
     float v[8];
+    float w[8], b[8];
     load_group<DT, VEC>(p.x, row * p.ldx, g, lane, p.cols, v);
-    norm_emit<DT, VEC>(p, row, g, lane, mean, rstd, v);
+    load_params<DT, VEC>(p.weight, p.param_f32, g, lane, p.cols, 1.0f, w);
+    load_params<DT, VEC>(p.bias, p.param_f32, g, lane, p.cols, 0.0f, b);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] -= mean;
+    norm_emit<DT, VEC>(p, row, g, lane, rstd, w, b, v);
   }
   if (threadIdx.x == 0) {
     if (p.mean) p.mean[row] = mean;
@@ -151,51 +286,68 @@ __global__ void __launch_bounds__(512) norm_long_kernel(const NormParams p) {
   }
 }
 
-// Backward, short and middle rows: a warp or a CTA walks over rows with a stride of the grid.
-// Each lane keeps its columns' sums of dy * xh and dy in registers over all its rows; they leave
-// once, as a partial row per CTA, and norm_param_kernel adds the partial rows in order.  So x and
-// dy are read once for all three gradients.
-template <int DT, int NCH, bool VEC, bool WARP>
-__global__ void __launch_bounds__(512) norm_bwd_kernel(const NormBwdParams p) {
+// Backward, rows by warp (WARP) or by CTA, walking over the rows with the grid's stride.  RING
+// (VEC and CTA only): the rows of x and dy come through shared memory.
+template <int DT, int NCH, bool VEC, bool WARP, bool RING>
+__global__ void __launch_bounds__(WARP ? 128 : 512) norm_bwd_kernel(const NormBwdParams p) {
   __shared__ float red[2][2][16];
-  extern __shared__ float sum_smem[];   // WARP: [2][cols]
+  __shared__ uint64_t full[kRowRingStages];
+  __shared__ unsigned int abort_word;
+  extern __shared__ __align__(128) unsigned char dyn[];   // WARP: [2][cols] sums; RING: the ring
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, nwarps = blockDim.x >> 5;
   const uint64_t first = WARP ? (uint64_t)blockIdx.x * nwarps + warp : blockIdx.x;
   const uint64_t step = WARP ? (uint64_t)gridDim.x * nwarps : gridDim.x;
+  RowRing ring{dyn, full, &abort_word, p.status, p.stages, p.cols * Elem<DT>::kBytes, p.slot_bytes};
+  uint64_t issued = 0;
+  if constexpr (RING) {
+    if (threadIdx.x == 0) {
+      ring.init();
+      for (uint64_t r = blockIdx.x; r < p.rows && issued < p.stages; r += gridDim.x, ++issued)
+        ring.fetch((uint32_t)issued, row_ptr<DT>(p.x, r, p.ldx), row_ptr<DT>(p.dy, r, p.lddy));
+    }
+    __syncthreads();
+  }
   const float rn = 1.0f / (float)p.cols;
-  float dw[NCH][8], db[NCH][8];
+  float w[NCH][8], dw[NCH][8], db[NCH][8];
 #pragma unroll
-  for (int i = 0; i < NCH; ++i)
+  for (int i = 0; i < NCH; ++i) {
+    load_params<DT, VEC>(p.weight, p.param_f32, WARP ? i : i * nwarps + warp, lane, p.cols, 1.0f, w[i]);
 #pragma unroll
     for (int j = 0; j < 8; ++j) dw[i][j] = db[i][j] = 0.0f;
+  }
+  uint32_t slot = 0, phase = 0;
   int turn = 0;
   for (uint64_t row = first; row < p.rows; row += step, turn ^= 1) {
-    float xh[NCH][8], gy[NCH][8];
-#pragma unroll
-    for (int i = 0; i < NCH; ++i) {
-      const uint32_t g = WARP ? i : i * nwarps + warp;
-      load_group<DT, VEC>(p.x, row * p.ldx, g, lane, p.cols, xh[i]);
-      load_group<DT, VEC>(p.dy, row * p.lddy, g, lane, p.cols, gy[i]);
-    }
+    float xh[NCH][8], g[NCH][8];
     const float mean = p.mean[row], rstd = p.rstd[row];
+    if constexpr (RING) {
+      ring.wait(slot, phase);   // on failure the loop runs on, quickly, to keep the barriers together
+#pragma unroll
+      for (int i = 0; i < NCH; ++i) {
+        load_group<DT, true>(dyn + slot * p.slot_bytes, 0, i * nwarps + warp, lane, p.cols, xh[i], mean);
+        load_group<DT, true>(dyn + slot * p.slot_bytes + p.slot_bytes / 2, 0, i * nwarps + warp, lane, p.cols, g[i]);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < NCH; ++i) {
+        load_group<DT, VEC>(p.x, row * p.ldx, WARP ? i : i * nwarps + warp, lane, p.cols, xh[i], mean);
+        load_group<DT, VEC>(p.dy, row * p.lddy, WARP ? i : i * nwarps + warp, lane, p.cols, g[i]);
+      }
+    }
+    // past the row's end dy is 0 and x is the mean, unless the mean is not finite: the sums of such
+    // a row are not finite either, and no column past the end is ever written
     float s1 = 0.0f, s2 = 0.0f;
 #pragma unroll
-    for (int i = 0; i < NCH; ++i) {
-      const uint32_t g = WARP ? i : i * nwarps + warp;
-      float w[8];
-      load_params<DT, VEC>(p.weight, p.param_f32, g, lane, p.cols, 1.0f, w);
+    for (int i = 0; i < NCH; ++i)
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         xh[i][j] = (xh[i][j] - mean) * rstd;
-        dw[i][j] = fmaf(gy[i][j], xh[i][j], dw[i][j]);
-        db[i][j] += gy[i][j];
-        gy[i][j] *= w[j];
-        if (group_col<VEC>(g, lane, j) < p.cols) {
-          s1 += gy[i][j];
-          s2 = fmaf(gy[i][j], xh[i][j], s2);
-        }
+        dw[i][j] = fmaf(g[i][j], xh[i][j], dw[i][j]);
+        db[i][j] += g[i][j];
+        g[i][j] *= w[i][j];
+        s1 += g[i][j];
+        s2 = fmaf(g[i][j], xh[i][j], s2);
       }
-    }
     s1 = warp_sum(s1);
     s2 = warp_sum(s2);
     if constexpr (!WARP) {
@@ -204,6 +356,18 @@ __global__ void __launch_bounds__(512) norm_bwd_kernel(const NormBwdParams p) {
         red[turn][1][warp] = s2;
       }
       __syncthreads();   // one barrier per row: the other half of `red` serves the next row
+      if constexpr (RING) {
+        // every thread has read the rows: the slot takes those that are `stages` ahead
+        const uint64_t ahead = row + (uint64_t)p.stages * gridDim.x;
+        if (threadIdx.x == 0 && ahead < p.rows) {
+          ring.fetch(slot, row_ptr<DT>(p.x, ahead, p.ldx), row_ptr<DT>(p.dy, ahead, p.lddy));
+          ++issued;
+        }
+        if (++slot == p.stages) {
+          slot = 0;
+          phase ^= 1u;
+        }
+      }
       s1 = warp_sum(lane < nwarps ? red[turn][0][lane] : 0.0f);
       s2 = warp_sum(lane < nwarps ? red[turn][1][lane] : 0.0f);
     }
@@ -214,41 +378,41 @@ __global__ void __launch_bounds__(512) norm_bwd_kernel(const NormBwdParams p) {
       for (int i = 0; i < NCH; ++i) {
         float d[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) d[j] = rstd * (gy[i][j] - s1 - xh[i][j] * s2);
+        for (int j = 0; j < 8; ++j) d[j] = rstd * (fmaf(-xh[i][j], s2, g[i][j]) - s1);
         store_group<DT, VEC>(p.dx, row * p.lddx, WARP ? i : i * nwarps + warp, lane, p.cols, d);
       }
     }
   }
+  if constexpr (RING) {
+    if (threadIdx.x == 0 && abort_word) ring.drain(issued);
+  }
   if (!p.want_param) return;
   float* out = p.partial + (uint64_t)blockIdx.x * 2 * p.cols;
   if constexpr (WARP) {
-    for (int w = 0; w < nwarps; ++w) {   // warps add in order
-      if (warp == w) {
+    float* sums = reinterpret_cast<float*>(dyn);
+    for (int k = 0; k < nwarps; ++k) {   // warps add in order
+      if (warp == k) {
 #pragma unroll
         for (int i = 0; i < NCH; ++i)
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
             const uint32_t c = group_col<VEC>(i, lane, j);
             if (c < p.cols) {
-              sum_smem[c] = w ? sum_smem[c] + dw[i][j] : dw[i][j];
-              sum_smem[p.cols + c] = w ? sum_smem[p.cols + c] + db[i][j] : db[i][j];
+              sums[c] = k ? sums[c] + dw[i][j] : dw[i][j];
+              sums[p.cols + c] = k ? sums[p.cols + c] + db[i][j] : db[i][j];
             }
           }
       }
       __syncthreads();
     }
-    for (uint32_t c = threadIdx.x; c < 2 * p.cols; c += blockDim.x) out[c] = sum_smem[c];
+    for (uint32_t c = threadIdx.x; c < 2 * p.cols; c += blockDim.x) out[c] = sums[c];
   } else {
+    // partial rows start on 16-byte boundaries where the columns of a VEC row do
 #pragma unroll
-    for (int i = 0; i < NCH; ++i)
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const uint32_t c = group_col<VEC>(i * nwarps + warp, lane, j);
-        if (c < p.cols) {
-          out[c] = dw[i][j];
-          out[p.cols + c] = db[i][j];
-        }
-      }
+    for (int i = 0; i < NCH; ++i) {
+      store_group<KB_F32, VEC>(out, 0, i * nwarps + warp, lane, p.cols, dw[i]);
+      store_group<KB_F32, VEC>(out, p.cols, i * nwarps + warp, lane, p.cols, db[i]);
+    }
   }
 }
 

@@ -78,47 +78,106 @@ kb_status launch_quant(kb_ctx* ctx, const QuantParams& p, bool vec, bool e5m2, b
 
 // ---- layer norm ----------------------------------------------------------------------------------
 
-template <int DT, bool VEC>
-kb_status launch_norm(kb_ctx* ctx, const NormParams& p, cudaStream_t st) {
-  const uint32_t g = p.groups;
-  const unsigned int rows = (unsigned int)p.rows;
-  if (g <= 4) {   // a warp per row
-    const unsigned int grid = (rows + 3) / 4;
-    if (g == 1)
-      norm_kernel<DT, 1, VEC, true><<<grid, 128, 0, st>>>(p);
-    else if (g == 2)
-      norm_kernel<DT, 2, VEC, true><<<grid, 128, 0, st>>>(p);
-    else
-      norm_kernel<DT, 4, VEC, true><<<grid, 128, 0, st>>>(p);
-  } else if (g <= 32 && p.rows <= (uint64_t)ctx->sm_count) {   // one CTA per SM at most: as many warps as there are groups
-    norm_kernel<DT, 1, VEC, false><<<rows, 32 * g, 0, st>>>(p);
-  } else if (g <= 32) {
-    norm_kernel<DT, 2, VEC, false><<<rows, 32 * ((g + 1) / 2), 0, st>>>(p);
-  } else if (g <= 64) {
-    norm_kernel<DT, 4, VEC, false><<<rows, 32 * ((g + 3) / 4), 0, st>>>(p);
-  } else {
-    norm_long_kernel<DT, VEC><<<rows, 512, 0, st>>>(p);
+// The row ring of a CTA that walks over rows of `bytes` each: as many slots as fit its share of an
+// SM's shared memory, 0 if fewer than two do (then the rows are read directly).
+uint32_t ring_stages(size_t bytes, int ctas_per_sm) {
+  const size_t share = (size_t)(220 * 1024) / ctas_per_sm - 1024;
+  return (uint32_t)std::min<size_t>(share / round_up(bytes, 128), kRowRingStages);
+}
+// CTAs of `threads` threads of a kernel that fit an SM by its registers (the count is fixed at
+// compile time, so it is asked for once), at most `most`.
+template <auto Kernel>
+int ctas_by_registers(unsigned int threads, int most) {
+  static const int regs = [] {
+    cudaFuncAttributes a = {};
+    return cudaFuncGetAttributes(&a, Kernel) == cudaSuccess ? a.numRegs : 255;
+  }();
+  const int per_warp = (regs + 7) / 8 * 8 * 32;
+  return std::max(1, std::min(most, 65536 / per_warp / (int)(threads / 32)));
+}
+template <class K>
+kb_status ring_limits(kb_ctx* ctx, K kernel, size_t smem) {
+  if (smem > 48 * 1024)
+    KB_CUDA(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+  return KB_OK;
+}
+
+template <int DT, int NCH, bool VEC>
+kb_status launch_norm_cta(kb_ctx* ctx, NormParams& p, cudaStream_t st) {
+  const unsigned int threads = 32 * ((p.groups + NCH - 1) / NCH);
+  if constexpr (VEC && NCH == 2) {
+    // from three rows a CTA on, the ring pays for its start
+    const int per_sm = ctas_by_registers<norm_cta_kernel<DT, NCH, true, true>>(threads, 4);
+    const uint64_t resident = (uint64_t)ctx->sm_count * per_sm;
+    const size_t bytes = (size_t)p.cols * elem_bytes((kb_dtype)DT);
+    const uint32_t stages = ring_stages(bytes, per_sm);
+    if (p.rows >= 3 * resident && stages >= 2) {
+      p.stages = stages;
+      p.slot_bytes = (uint32_t)round_up(bytes, 128);
+      const size_t smem = (size_t)stages * p.slot_bytes;
+      KB_TRY(ring_limits(ctx, norm_cta_kernel<DT, NCH, true, true>, smem));
+      norm_cta_kernel<DT, NCH, true, true><<<(unsigned int)resident, threads, smem, st>>>(p);
+      return launched(ctx);
+    }
   }
+  const int per_sm = ctas_by_registers<norm_cta_kernel<DT, NCH, VEC, false>>(threads, 16);
+  const unsigned int grid = (unsigned int)std::min<uint64_t>(p.rows, (uint64_t)ctx->sm_count * per_sm);
+  norm_cta_kernel<DT, NCH, VEC, false><<<grid, threads, 0, st>>>(p);
+  return launched(ctx);
+}
+
+template <int DT, bool VEC>
+kb_status launch_norm(kb_ctx* ctx, NormParams& p, cudaStream_t st) {
+  const uint32_t g = p.groups;
+  if (g <= 4) {   // a warp per row
+    const unsigned int grid = (unsigned int)((p.rows + 3) / 4);
+    if (g == 1)
+      norm_warp_kernel<DT, 1, VEC><<<grid, 128, 0, st>>>(p);
+    else if (g == 2)
+      norm_warp_kernel<DT, 2, VEC><<<grid, 128, 0, st>>>(p);
+    else
+      norm_warp_kernel<DT, 4, VEC><<<grid, 128, 0, st>>>(p);
+    return launched(ctx);
+  }
+  // one row per SM at most: as many warps as there are groups, for the shortest time of one row
+  if (g <= 32 && p.rows <= (uint64_t)ctx->sm_count) return launch_norm_cta<DT, 1, VEC>(ctx, p, st);
+  if (g <= 32) return launch_norm_cta<DT, 2, VEC>(ctx, p, st);
+  if (g <= 64) return launch_norm_cta<DT, 4, VEC>(ctx, p, st);
+  norm_long_kernel<DT, VEC><<<(unsigned int)p.rows, 512, 0, st>>>(p);
   return launched(ctx);
 }
 
 template <int DT, int NCH, bool VEC, bool WARP>
 kb_status launch_norm_bwd(kb_ctx* ctx, NormBwdParams& p, unsigned int threads, uint32_t* nparts, cudaStream_t st) {
   const uint64_t per = WARP ? threads / 32 : 1;
-  const size_t smem = WARP ? 2 * sizeof(float) * p.cols : 0;
-  int per_sm = 0;
-  KB_CUDA(ctx, cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, norm_bwd_kernel<DT, NCH, VEC, WARP>,
-                                                             (int)threads, smem));
-  const uint64_t most = (uint64_t)ctx->sm_count * std::max(per_sm, 1);
-  const unsigned int grid = (unsigned int)std::min<uint64_t>((p.rows + per - 1) / per, most);
-  *nparts = grid;
-  if (p.want_param) {
-    KB_TRY(ensure_buf(ctx, &ctx->ops_ws, &ctx->ops_ws_bytes, (size_t)grid * 2 * p.cols * sizeof(float),
-                      "partial parameter gradients"));
-    p.partial = reinterpret_cast<float*>(ctx->ops_ws);
+  auto launch = [&](auto kernel, uint64_t resident, size_t smem) {
+    const unsigned int grid = (unsigned int)std::min<uint64_t>((p.rows + per - 1) / per, resident);
+    *nparts = grid;
+    if (p.want_param) {
+      KB_TRY(ensure_buf(ctx, &ctx->ops_ws, &ctx->ops_ws_bytes, (size_t)grid * 2 * p.cols * sizeof(float),
+                        "partial parameter gradients"));
+      p.partial = reinterpret_cast<float*>(ctx->ops_ws);
+    }
+    kernel<<<grid, threads, smem, st>>>(p);
+    return launched(ctx);
+  };
+  if constexpr (VEC && !WARP) {
+    constexpr auto kernel = norm_bwd_kernel<DT, NCH, true, false, true>;
+    const int per_sm = ctas_by_registers<kernel>(threads, 4);
+    const uint64_t resident = (uint64_t)ctx->sm_count * per_sm;
+    const size_t bytes = (size_t)p.cols * elem_bytes((kb_dtype)DT);
+    const uint32_t stages = ring_stages(2 * round_up(bytes, 128), per_sm);
+    if (p.rows >= 2 * resident && stages >= 2) {
+      p.stages = stages;
+      p.slot_bytes = (uint32_t)(2 * round_up(bytes, 128));
+      const size_t smem = (size_t)stages * p.slot_bytes;
+      KB_TRY(ring_limits(ctx, kernel, smem));
+      return launch(kernel, resident, smem);
+    }
   }
-  norm_bwd_kernel<DT, NCH, VEC, WARP><<<grid, threads, smem, st>>>(p);
-  return launched(ctx);
+  constexpr auto kernel = norm_bwd_kernel<DT, NCH, VEC, WARP, false>;
+  return launch(kernel, (uint64_t)ctx->sm_count * ctas_by_registers<kernel>(threads, WARP ? 4 : 2),
+                WARP ? 2 * sizeof(float) * p.cols : 0);
 }
 
 template <int DT, bool VEC>
@@ -327,6 +386,8 @@ extern "C" kb_status kb_layernorm(kb_ctx* ctx, const void* d_x, uint64_t rows, u
   p.eps = eps;
   p.param_f32 = param_dtype == KB_F32;
   p.e5m2 = q_dtype == KB_F8E5M2;
+  p.stages = p.slot_bytes = 0;
+  p.status = ctx->d_status;
   const bool vec = cols % 8 == 0 && rows_aligned(d_x, ldx, e) && (!d_y || rows_aligned(d_y, ldy, e)) &&
                    (!d_q || (ldq % 8 == 0 && aligned_to(d_q, 8))) && aligned16(d_weight) && aligned16(d_bias);
   if (dtype == KB_F32) return vec ? launch_norm<KB_F32, true>(ctx, p, st) : launch_norm<KB_F32, false>(ctx, p, st);
@@ -381,6 +442,8 @@ extern "C" kb_status kb_layernorm_backward(kb_ctx* ctx, const void* d_dy, uint64
   p.groups = (uint32_t)((cols + kGroup - 1) / kGroup);
   p.param_f32 = param_dtype == KB_F32;
   p.want_param = d_dweight || d_dbias;
+  p.stages = p.slot_bytes = 0;
+  p.status = ctx->d_status;
   const bool vec = cols % 8 == 0 && rows_aligned(d_dy, lddy, e) && rows_aligned(d_x, ldx, e) &&
                    (!d_dx || rows_aligned(d_dx, lddx, e)) && aligned16(d_weight);
   uint32_t nparts = 0;

@@ -40,11 +40,47 @@ __global__ void __launch_bounds__(256) quant_rows_kernel(const QuantParams p) {
 }
 
 // One 128 x 128 tile per CTA of 256 threads.  TILES: one scale for the tile, else one per column
-// of x (only needed transposed: the block then runs along the rows of x).
+// of x (only needed transposed: the block then runs along the rows of x).  A thread keeps its 8 x 8
+// elements in their storage type (32 registers for 16-bit types), so that three CTAs fit on an SM
+// and 96 KB are on their way while one of them reduces.
 constexpr int kTransposePitch = 132;   // bytes; an odd number of words spreads a column's rows over the banks
+template <int DT>
+struct Held8 {   // 8 consecutive elements of one row
+  static constexpr int kWords = DT == KB_F32 ? 8 : 4;
+  uint32_t w[kWords];
+  __device__ __forceinline__ void load(const void* p, uint64_t i) {
+    const uint4* q = reinterpret_cast<const uint4*>(static_cast<const unsigned char*>(p) + i * Elem<DT>::kBytes);
+    *reinterpret_cast<uint4*>(w) = q[0];
+    if constexpr (DT == KB_F32) *reinterpret_cast<uint4*>(w + 4) = q[1];
+  }
+  __device__ __forceinline__ void zero() {
+#pragma unroll
+    for (int k = 0; k < kWords; ++k) w[k] = 0u;
+  }
+  __device__ __forceinline__ void set(int j, const void* p, uint64_t i) {   // element j; the others stay
+    if constexpr (DT == KB_F32)
+      w[j] = static_cast<const uint32_t*>(p)[i];
+    else
+      w[j >> 1] |= (uint32_t) static_cast<const unsigned short*>(p)[i] << (16 * (j & 1));
+  }
+  __device__ __forceinline__ float get(int j) const {
+    if constexpr (DT == KB_F32)
+      return __uint_as_float(w[j]);
+    else if constexpr (DT == KB_BF16)
+      return __uint_as_float((j & 1) ? w[j >> 1] & 0xFFFF0000u : w[j >> 1] << 16);
+    else
+      return __half2float(__ushort_as_half((unsigned short)(w[j >> 1] >> (16 * (j & 1)))));
+  }
+  __device__ __forceinline__ void all(float (&v)[8]) const {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = get(j);
+  }
+};
+__device__ __forceinline__ float inf_to_nan(float v) { return isinf(v) ? __uint_as_float(0x7FFFFFFFu) : v; }
+
 template <int DT, bool VEC, bool E5M2, bool TILES, bool TRANSPOSE>
-__global__ void __launch_bounds__(256) quant_tile_kernel(const QuantParams p) {
-  __shared__ unsigned int smax[TILES ? 8 : 8 * 128];
+__global__ void __launch_bounds__(256, DT == KB_F32 ? 2 : 3) quant_tile_kernel(const QuantParams p) {
+  __shared__ float smax[TILES ? 8 : 8 * 128];
   __shared__ __align__(16) unsigned char st[TRANSPOSE ? 128 * kTransposePitch : 16];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int cx = threadIdx.x & 15, ry = threadIdx.x >> 4;
@@ -52,42 +88,46 @@ __global__ void __launch_bounds__(256) quant_tile_kernel(const QuantParams p) {
   const uint64_t row0 = (uint64_t)rt * 128 + ry * 8, col0 = (uint64_t)ct * 128 + cx * 8;
   const int nrow = row0 < p.rows ? (int)min((uint64_t)8, p.rows - row0) : 0;
   const int ncol = col0 < p.cols ? (int)min((uint64_t)8, p.cols - col0) : 0;
-  float v[8][8];
+  Held8<DT> h[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    if (VEC) {
-      if (i < nrow && ncol == 8) {
-        load8<DT>(p.x, (row0 + i) * p.ldx + col0, v[i]);
-      } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[i][j] = 0.0f;
-      }
+    if (VEC && i < nrow && ncol == 8) {
+      h[i].load(p.x, (row0 + i) * p.ldx + col0);
     } else {
+      h[i].zero();
+      if (!VEC) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
-        v[i][j] = (i < nrow && j < ncol) ? load_elem<DT>(p.x, (row0 + i) * p.ldx + col0 + j) : 0.0f;
+        for (int j = 0; j < 8; ++j)
+          if (i < nrow && j < ncol) h[i].set(j, p.x, (row0 + i) * p.ldx + col0 + j);
+      }
     }
   }
-  float inv[8];   // per column of the thread; all equal for TILES
+  bool infinite = false;   // the block (TILES: the tile) holds an Inf
+  float inv[8];            // per column of the thread; all equal for TILES
   if constexpr (TILES) {
-    unsigned int m = 0u;
+    float m = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) m = max(m, max_bits<0, 8>(v[i]));
-    m = warp_max_u32(m);
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) m = fmaxf(m, fabsf(h[i].get(j)));
+    m = warp_max(m);
     if (lane == 0) smax[warp] = m;
     __syncthreads();
-    m = warp_max_u32(smax[lane & 7]);
-    if (m >= kInfBits) {   // the same for the whole CTA
-      unsigned int f = 0u;
+    m = warp_max(smax[lane & 7]);
+    infinite = isinf(m);
+    if (infinite) {   // the same for the whole CTA
+      float f = 0.0f;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) f = max(f, settle_nonfinite<0, 8>(v[i]));
-      f = warp_max_u32(f);
+      for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f = fmaxf(f, fabsf(inf_to_nan(h[i].get(j))));
+      f = warp_max(f);
       __syncthreads();
       if (lane == 0) smax[warp] = f;
       __syncthreads();
-      m = warp_max_u32(smax[lane & 7]);
+      m = warp_max(smax[lane & 7]);
     }
-    const BlockScale s = block_scale<E5M2>(__uint_as_float(m));
+    const BlockScale s = block_scale<E5M2>(m);
 #pragma unroll
     for (int j = 0; j < 8; ++j) inv[j] = s.inv;
     if (threadIdx.x == 0) {
@@ -97,32 +137,43 @@ __global__ void __launch_bounds__(256) quant_tile_kernel(const QuantParams p) {
         p.scale[(uint64_t)ct * p.rtiles + rt] = s.scale;
     }
   } else {
-    unsigned int m[8];
+    auto columns = [&](bool settle) {   // each column's maximum over the warp's 16 rows
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      m[j] = 0u;
+      for (int j = 0; j < 8; ++j) {
+        float m = 0.0f;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        // a finite maximum needs no second look here: the select costs less than a column's barrier
-        const unsigned int b = abs_bits(v[i][j]);
-        if (b >= kInfBits)
-          v[i][j] = __uint_as_float(0x7FFFFFFFu);
-        else
-          m[j] = max(m[j], b);
+        for (int i = 0; i < 8; ++i) {
+          const float v = h[i].get(j);
+          m = fmaxf(m, fabsf(settle ? inf_to_nan(v) : v));
+        }
+        m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, 16));
+        if (lane < 16) smax[warp * 128 + cx * 8 + j] = m;
       }
-      m[j] = max(m[j], __shfl_xor_sync(0xFFFFFFFFu, m[j], 16));
-    }
-    if (lane < 16) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) smax[warp * 128 + cx * 8 + j] = m[j];
-    }
+    };
+    columns(false);
     __syncthreads();
+    auto column = [&](int j) {
+      float t = 0.0f;
+#pragma unroll
+      for (int w = 0; w < 8; ++w) t = fmaxf(t, smax[w * 128 + cx * 8 + j]);
+      return t;
+    };
+    bool mine = false;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      unsigned int t = 0u;
+      inv[j] = column(j);
+      mine |= isinf(inv[j]);
+    }
+    infinite = __syncthreads_or(mine);
+    if (infinite) {
+      columns(true);
+      __syncthreads();
 #pragma unroll
-      for (int w = 0; w < 8; ++w) t = max(t, smax[w * 128 + cx * 8 + j]);
-      const BlockScale s = block_scale<E5M2>(__uint_as_float(t));
+      for (int j = 0; j < 8; ++j) inv[j] = column(j);
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const BlockScale s = block_scale<E5M2>(inv[j]);
       inv[j] = s.inv;
       if (ry == 0 && j < ncol) p.scale[(uint64_t)rt * p.cols + col0 + j] = s.scale;
     }
@@ -131,7 +182,13 @@ __global__ void __launch_bounds__(256) quant_tile_kernel(const QuantParams p) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       if (i >= nrow) break;
-      const uint2 r = quant8<E5M2>(v[i], inv[0]);
+      float v[8];
+      h[i].all(v);
+      if (infinite) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = inf_to_nan(v[j]);
+      }
+      const uint2 r = quant8<E5M2>(v, inv[0]);
       unsigned char* dst = p.q + (row0 + i) * p.ldq + col0;
       if (VEC) {
         if (ncol == 8) *reinterpret_cast<uint2*>(dst) = r;
@@ -144,7 +201,7 @@ __global__ void __launch_bounds__(256) quant_tile_kernel(const QuantParams p) {
     for (int j = 0; j < 8; ++j) {
       float c[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) c[i] = v[i][j];
+      for (int i = 0; i < 8; ++i) c[i] = infinite ? inf_to_nan(h[i].get(j)) : h[i].get(j);
       const uint2 r = quant8<E5M2>(c, inv[j]);
       uint32_t* dst = reinterpret_cast<uint32_t*>(st + (cx * 8 + j) * kTransposePitch + ry * 8);
       dst[0] = r.x;
