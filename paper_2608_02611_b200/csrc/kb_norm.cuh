@@ -1,18 +1,21 @@
 // Layer norm, forward and backward (contracts in include/kb_ops.h).
 //
-// Forward: a row lives in the registers of one warp (up to 1024 columns) or one CTA, 8 elements
-// per lane and group of 256 (kb_block8.cuh).  The mean and then the sum of squared distances from
-// it are reduced from the registers, so the row is read once and the variance does not suffer from
-// the cancellation of sum(x^2)/n - mean^2.  The same registers then give y and, where asked for,
-// the row's 8-bit blocks, so a consumer in 8 bits costs no second pass over y.
+// Forward: a row lives in the registers of as few warps as still fill the card (up to 4096 columns
+// per warp), 8 elements per lane and group of 256 (kb_block8.cuh).  The mean and then the sum of
+// squared distances from it are reduced from the registers, so the row is read once and the
+// variance does not suffer from the cancellation of sum(x^2)/n - mean^2.  The same registers then
+// give y and, where asked for, the row's 8-bit blocks, so a consumer in 8 bits costs no second pass
+// over y.  Few warps per row: what a row costs beyond its elements (two trees of shuffles, a
+// division, a root) is paid once per warp, warps that share no barrier drift apart and keep the
+// memory busy, and a warp has its whole share of the row on the way at once.
 //
-// Backward: the same, walking over rows; each lane keeps its columns' sums of dy * xh and dy in
-// registers over all its rows.  They leave once, as a partial row per CTA, and norm_param_kernel
-// adds the partial rows in order.  So x and dy are read once for all three gradients.
+// Backward: rows by warp or CTA, walking over rows; each lane keeps its columns' sums of dy * xh and
+// dy in registers over all its rows.  They leave once, as a partial row per CTA, and
+// norm_param_kernel adds the partial rows in order.  So x and dy are read once for all three
+// gradients.  The registers that hold the sums leave too few warps to cover the memory's latency,
+// so long walks get their rows through a ring in shared memory, several rows ahead.
 //
-// Bound: memory; each element is read and written once.  A CTA that walks over many rows gets them
-// through a ring in shared memory filled by 1-D bulk copies, several rows ahead: the registers that
-// hold the sums and the parameters leave too few warps to cover the memory's latency otherwise.
+// Bound: memory; each element is read and written once.
 #pragma once
 
 #include "kb_block8.cuh"
@@ -30,10 +33,8 @@ struct NormParams {
   float* scale;
   uint64_t rows, ldx, ldy, ldq;
   uint32_t cols, groups;
-  uint32_t stages, slot_bytes;   // of the row ring
   float eps;
   bool param_f32, e5m2;
-  unsigned int* status;
 };
 
 struct NormBwdParams {
@@ -81,165 +82,48 @@ __device__ __forceinline__ void norm_emit(const NormParams& p, uint64_t row, uin
   }
 }
 
-// Rows on their way from global memory: a ring of `stages` slots of `tensors` rows each.
-constexpr uint32_t kRowRingStages = 8;   // at most
-struct RowRing {
-  unsigned char* buf;
-  uint64_t* full;
-  volatile unsigned int* abort_flag;
-  unsigned int* status;
-  uint32_t stages, row_bytes, slot_bytes;
-
-  __device__ __forceinline__ void init() {   // one thread
-    for (uint32_t i = 0; i < stages; ++i) mbar_init(&full[i], 1);
-    *abort_flag = 0u;
-    mbar_fence_init();
-  }
-  // one thread: the rows at s0 (and s1) into slot `slot`
-  __device__ __forceinline__ void fetch(uint32_t slot, const void* s0, const void* s1) {
-    const uint64_t policy = l2_policy_evict_first();   // read once
-    mbar_arrive_expect_tx(&full[slot], s1 ? 2 * row_bytes : row_bytes);
-    bulk_g2s(buf + slot * slot_bytes, s0, row_bytes, &full[slot], policy);
-    if (s1) bulk_g2s(buf + slot * slot_bytes + slot_bytes / 2, s1, row_bytes, &full[slot], policy);
-  }
-  __device__ __forceinline__ bool wait(uint32_t slot, uint32_t phase) {
-    return mbar_wait_bounded(&full[slot], phase, abort_flag, status);
-  }
-  // after a wait has run out: let the copies in flight land before the CTA may leave
-  __device__ __forceinline__ void drain(uint64_t issued) {
-    const uint64_t back = issued < stages ? issued : stages;
-    for (uint64_t m = issued - back; m < issued; ++m) {
-      const unsigned long long t0 = global_ns();
-      while (!mbar_try_wait(&full[m % stages], (uint32_t)((m / stages) & 1ull)))
-        if (global_ns() - t0 > 1000000000ull) break;
-    }
-  }
-};
-template <int DT>
-__device__ __forceinline__ const unsigned char* row_ptr(const void* base, uint64_t row, uint64_t ld) {
-  return static_cast<const unsigned char*>(base) + row * ld * Elem<DT>::kBytes;
-}
-
-// A row per warp, NCH groups in registers.
-template <int DT, int NCH, bool VEC>
-__global__ void __launch_bounds__(128) norm_warp_kernel(const NormParams p) {
-  const int lane = threadIdx.x & 31;
-  const uint64_t row = (uint64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
-  if (row >= p.rows) return;
+// A row per warp (WARP) or per CTA, NCH groups per warp in registers.
+template <int DT, int NCH, bool VEC, bool WARP>
+__global__ void __launch_bounds__(WARP ? 128 : NCH == 1 ? 1024 : 256) norm_kernel(const NormParams p) {
+  __shared__ float red[2][32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, nwarps = blockDim.x >> 5;
+  const uint64_t row = WARP ? (uint64_t)blockIdx.x * 4 + warp : blockIdx.x;
+  if (WARP && row >= p.rows) return;
+  const uint32_t g0 = WARP ? 0 : warp, gstep = WARP ? 1 : nwarps;   // this warp's groups: g0, g0 + gstep, ...
   float v[NCH][8];
 #pragma unroll
-  for (int i = 0; i < NCH; ++i) load_group<DT, VEC>(p.x, row * p.ldx, i, lane, p.cols, v[i]);
+  for (int i = 0; i < NCH; ++i) load_group<DT, VEC>(p.x, row * p.ldx, g0 + i * gstep, lane, p.cols, v[i]);
   float s = 0.0f;
 #pragma unroll
   for (int i = 0; i < NCH; ++i)
 #pragma unroll
     for (int j = 0; j < 8; ++j) s += v[i][j];
   const float n = (float)p.cols;
-  const float mean = warp_sum(s) / n;
+  const float mean = (WARP ? warp_sum(s) : cta_sum(s, red[0], warp, lane, nwarps)) / n;
   float ss = 0.0f;
 #pragma unroll
   for (int i = 0; i < NCH; ++i) {
-    fill_tail<VEC>(i, lane, p.cols, mean, v[i]);
+    fill_tail<VEC>(g0 + i * gstep, lane, p.cols, mean, v[i]);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       v[i][j] -= mean;
       ss = fmaf(v[i][j], v[i][j], ss);
     }
   }
-  const float rstd = 1.0f / sqrtf(warp_sum(ss) / n + p.eps);
+  const float var = (WARP ? warp_sum(ss) : cta_sum(ss, red[1], warp, lane, nwarps)) / n;
+  const float rstd = 1.0f / sqrtf(var + p.eps);
 #pragma unroll
   for (int i = 0; i < NCH; ++i) {
+    const uint32_t g = g0 + i * gstep;
+    if (g >= p.groups) break;
     float w[8], b[8];
-    load_params<DT, VEC>(p.weight, p.param_f32, i, lane, p.cols, 1.0f, w);
-    load_params<DT, VEC>(p.bias, p.param_f32, i, lane, p.cols, 0.0f, b);
-    norm_emit<DT, VEC>(p, row, i, lane, rstd, w, b, v[i]);
+    load_params<DT, VEC>(p.weight, p.param_f32, g, lane, p.cols, 1.0f, w);
+    load_params<DT, VEC>(p.bias, p.param_f32, g, lane, p.cols, 0.0f, b);
+    norm_emit<DT, VEC>(p, row, g, lane, rstd, w, b, v[i]);
   }
-  if (lane == 0) {
+  if (lane == 0 && (WARP || warp == 0)) {
     if (p.mean) p.mean[row] = mean;
     if (p.rstd) p.rstd[row] = rstd;
-  }
-}
-
-// Rows by CTA, NCH groups per warp in registers; a CTA walks over the rows with the grid's stride
-// and keeps its columns' parameters.  RING (VEC only): rows come through shared memory.
-template <int DT, int NCH, bool VEC, bool RING>
-__global__ void __launch_bounds__(NCH == 1 ? 1024 : 512) norm_cta_kernel(const NormParams p) {
-  __shared__ float red[2][2][32];
-  __shared__ uint64_t full[kRowRingStages];
-  __shared__ unsigned int abort_word;
-  extern __shared__ __align__(128) unsigned char dyn[];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, nwarps = blockDim.x >> 5;
-  RowRing ring{dyn, full, &abort_word, p.status, p.stages, p.cols * Elem<DT>::kBytes, p.slot_bytes};
-  uint64_t issued = 0;
-  if constexpr (RING) {
-    if (threadIdx.x == 0) {
-      ring.init();
-      for (uint64_t r = blockIdx.x; r < p.rows && issued < p.stages; r += gridDim.x, ++issued)
-        ring.fetch((uint32_t)issued, row_ptr<DT>(p.x, r, p.ldx), nullptr);
-    }
-    __syncthreads();
-  }
-  float w[NCH][8], b[NCH][8];
-#pragma unroll
-  for (int i = 0; i < NCH; ++i) {
-    load_params<DT, VEC>(p.weight, p.param_f32, i * nwarps + warp, lane, p.cols, 1.0f, w[i]);
-    load_params<DT, VEC>(p.bias, p.param_f32, i * nwarps + warp, lane, p.cols, 0.0f, b[i]);
-  }
-  const float n = (float)p.cols;
-  uint32_t slot = 0, phase = 0;
-  int turn = 0;
-  for (uint64_t row = blockIdx.x; row < p.rows; row += gridDim.x, turn ^= 1) {
-    float v[NCH][8];
-    if constexpr (RING) {
-      ring.wait(slot, phase);   // on failure the loop runs on, quickly, to keep the barriers together
-#pragma unroll
-      for (int i = 0; i < NCH; ++i)
-        load_group<DT, true>(dyn + slot * p.slot_bytes, 0, i * nwarps + warp, lane, p.cols, v[i]);
-    } else {
-#pragma unroll
-      for (int i = 0; i < NCH; ++i)
-        load_group<DT, VEC>(p.x, row * p.ldx, i * nwarps + warp, lane, p.cols, v[i]);
-    }
-    float s = 0.0f;
-#pragma unroll
-    for (int i = 0; i < NCH; ++i)
-#pragma unroll
-      for (int j = 0; j < 8; ++j) s += v[i][j];
-    const float mean = cta_sum(s, red[turn][0], warp, lane, nwarps) / n;
-    if constexpr (RING) {
-      // every thread has read the row: the slot takes the row that is `stages` ahead
-      const uint64_t ahead = row + (uint64_t)p.stages * gridDim.x;
-      if (threadIdx.x == 0 && ahead < p.rows) {
-        ring.fetch(slot, row_ptr<DT>(p.x, ahead, p.ldx), nullptr);
-        ++issued;
-      }
-      if (++slot == p.stages) {
-        slot = 0;
-        phase ^= 1u;
-      }
-    }
-    float ss = 0.0f;
-#pragma unroll
-    for (int i = 0; i < NCH; ++i) {
-      fill_tail<VEC>(i * nwarps + warp, lane, p.cols, mean, v[i]);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        v[i][j] -= mean;
-        ss = fmaf(v[i][j], v[i][j], ss);
-      }
-    }
-    const float rstd = 1.0f / sqrtf(cta_sum(ss, red[turn][1], warp, lane, nwarps) / n + p.eps);
-#pragma unroll
-    for (int i = 0; i < NCH; ++i)
-      if (NCH == 1 || i * nwarps + warp < p.groups)
-        norm_emit<DT, VEC>(p, row, i * nwarps + warp, lane, rstd, w[i], b[i], v[i]);
-    if (threadIdx.x == 0) {
-      if (p.mean) p.mean[row] = mean;
-      if (p.rstd) p.rstd[row] = rstd;
-    }
-  }
-  if constexpr (RING) {
-    if (threadIdx.x == 0 && abort_word) ring.drain(issued);
   }
 }
 
@@ -286,6 +170,45 @@ __global__ void __launch_bounds__(512) norm_long_kernel(const NormParams p) {
   }
 }
 
+// Rows on their way from global memory: a ring of `stages` slots of `tensors` rows each.
+constexpr uint32_t kRowRingStages = 8;   // at most
+struct RowRing {
+  unsigned char* buf;
+  uint64_t* full;
+  volatile unsigned int* abort_flag;
+  unsigned int* status;
+  uint32_t stages, row_bytes, slot_bytes;
+
+  __device__ __forceinline__ void init() {   // one thread
+    for (uint32_t i = 0; i < stages; ++i) mbar_init(&full[i], 1);
+    *abort_flag = 0u;
+    mbar_fence_init();
+  }
+  // one thread: the rows at s0 (and s1) into slot `slot`
+  __device__ __forceinline__ void fetch(uint32_t slot, const void* s0, const void* s1) {
+    const uint64_t policy = l2_policy_evict_first();   // read once
+    mbar_arrive_expect_tx(&full[slot], s1 ? 2 * row_bytes : row_bytes);
+    bulk_g2s(buf + slot * slot_bytes, s0, row_bytes, &full[slot], policy);
+    if (s1) bulk_g2s(buf + slot * slot_bytes + slot_bytes / 2, s1, row_bytes, &full[slot], policy);
+  }
+  __device__ __forceinline__ bool wait(uint32_t slot, uint32_t phase) {
+    return mbar_wait_bounded(&full[slot], phase, abort_flag, status);
+  }
+  // after a wait has run out: let the copies in flight land before the CTA may leave
+  __device__ __forceinline__ void drain(uint64_t issued) {
+    const uint64_t back = issued < stages ? issued : stages;
+    for (uint64_t m = issued - back; m < issued; ++m) {
+      const unsigned long long t0 = global_ns();
+      while (!mbar_try_wait(&full[m % stages], (uint32_t)((m / stages) & 1ull)))
+        if (global_ns() - t0 > 1000000000ull) break;
+    }
+  }
+};
+template <int DT>
+__device__ __forceinline__ const unsigned char* row_ptr(const void* base, uint64_t row, uint64_t ld) {
+  return static_cast<const unsigned char*>(base) + row * ld * Elem<DT>::kBytes;
+}
+
 // Backward, rows by warp (WARP) or by CTA, walking over the rows with the grid's stride.  RING
 // (VEC and CTA only): the rows of x and dy come through shared memory.
 template <int DT, int NCH, bool VEC, bool WARP, bool RING>
@@ -317,9 +240,14 @@ __global__ void __launch_bounds__(WARP ? 128 : 512) norm_bwd_kernel(const NormBw
   }
   uint32_t slot = 0, phase = 0;
   int turn = 0;
+  float next_mean = first < p.rows ? p.mean[first] : 0.0f, next_rstd = first < p.rows ? p.rstd[first] : 0.0f;
   for (uint64_t row = first; row < p.rows; row += step, turn ^= 1) {
     float xh[NCH][8], g[NCH][8];
-    const float mean = p.mean[row], rstd = p.rstd[row];
+    const float mean = next_mean, rstd = next_rstd;
+    if (row + step < p.rows) {   // a row ahead: their latency would stand at the head of every row
+      next_mean = p.mean[row + step];
+      next_rstd = p.rstd[row + step];
+    }
     if constexpr (RING) {
       ring.wait(slot, phase);   // on failure the loop runs on, quickly, to keep the barriers together
 #pragma unroll

@@ -103,46 +103,27 @@ kb_status ring_limits(kb_ctx* ctx, K kernel, size_t smem) {
 }
 
 template <int DT, int NCH, bool VEC>
-kb_status launch_norm_cta(kb_ctx* ctx, NormParams& p, cudaStream_t st) {
-  const unsigned int threads = 32 * ((p.groups + NCH - 1) / NCH);
-  if constexpr (VEC && NCH == 2) {
-    // from three rows a CTA on, the ring pays for its start
-    const int per_sm = ctas_by_registers<norm_cta_kernel<DT, NCH, true, true>>(threads, 4);
-    const uint64_t resident = (uint64_t)ctx->sm_count * per_sm;
-    const size_t bytes = (size_t)p.cols * elem_bytes((kb_dtype)DT);
-    const uint32_t stages = ring_stages(bytes, per_sm);
-    if (p.rows >= 3 * resident && stages >= 2) {
-      p.stages = stages;
-      p.slot_bytes = (uint32_t)round_up(bytes, 128);
-      const size_t smem = (size_t)stages * p.slot_bytes;
-      KB_TRY(ring_limits(ctx, norm_cta_kernel<DT, NCH, true, true>, smem));
-      norm_cta_kernel<DT, NCH, true, true><<<(unsigned int)resident, threads, smem, st>>>(p);
-      return launched(ctx);
-    }
-  }
-  const int per_sm = ctas_by_registers<norm_cta_kernel<DT, NCH, VEC, false>>(threads, 16);
-  const unsigned int grid = (unsigned int)std::min<uint64_t>(p.rows, (uint64_t)ctx->sm_count * per_sm);
-  norm_cta_kernel<DT, NCH, VEC, false><<<grid, threads, 0, st>>>(p);
+kb_status launch_norm(kb_ctx* ctx, const NormParams& p, cudaStream_t st) {
+  const uint32_t warps = (p.groups + NCH - 1) / NCH;
+  if (warps == 1)
+    norm_kernel<DT, NCH, VEC, true><<<(unsigned int)((p.rows + 3) / 4), 128, 0, st>>>(p);
+  else
+    norm_kernel<DT, NCH, VEC, false><<<(unsigned int)p.rows, 32 * warps, 0, st>>>(p);
   return launched(ctx);
 }
 
 template <int DT, bool VEC>
-kb_status launch_norm(kb_ctx* ctx, NormParams& p, cudaStream_t st) {
-  const uint32_t g = p.groups;
-  if (g <= 4) {   // a warp per row
-    const unsigned int grid = (unsigned int)((p.rows + 3) / 4);
-    if (g == 1)
-      norm_warp_kernel<DT, 1, VEC><<<grid, 128, 0, st>>>(p);
-    else if (g == 2)
-      norm_warp_kernel<DT, 2, VEC><<<grid, 128, 0, st>>>(p);
-    else
-      norm_warp_kernel<DT, 4, VEC><<<grid, 128, 0, st>>>(p);
-    return launched(ctx);
-  }
-  // one row per SM at most: as many warps as there are groups, for the shortest time of one row
-  if (g <= 32 && p.rows <= (uint64_t)ctx->sm_count) return launch_norm_cta<DT, 1, VEC>(ctx, p, st);
-  if (g <= 32) return launch_norm_cta<DT, 2, VEC>(ctx, p, st);
-  if (g <= 64) return launch_norm_cta<DT, 4, VEC>(ctx, p, st);
+kb_status launch_norm(kb_ctx* ctx, const NormParams& p, cudaStream_t st) {
+  // as few warps per row as still give every SM 12 of them (16 groups a warp take about 170
+  // registers a thread: 12 warps fill an SM); with few rows, as many as the row has groups
+  const uint64_t fill = 12ull * ctx->sm_count;
+  auto enough = [&](uint32_t nch) { return p.rows * ((p.groups + nch - 1) / nch) >= fill; };
+  auto fits = [&](uint32_t nch, uint32_t most) { return (p.groups + nch - 1) / nch <= most; };
+  if (p.groups == 1 || (!enough(2) && fits(1, 32))) return launch_norm<DT, 1, VEC>(ctx, p, st);
+  if (p.groups == 2 || (!enough(4) && fits(2, 8))) return launch_norm<DT, 2, VEC>(ctx, p, st);
+  if (p.groups <= 4 || (!enough(8) && fits(4, 8))) return launch_norm<DT, 4, VEC>(ctx, p, st);
+  if (p.groups <= 8 || (!enough(16) && fits(8, 8))) return launch_norm<DT, 8, VEC>(ctx, p, st);
+  if (fits(16, 8)) return launch_norm<DT, 16, VEC>(ctx, p, st);
   norm_long_kernel<DT, VEC><<<(unsigned int)p.rows, 512, 0, st>>>(p);
   return launched(ctx);
 }
@@ -386,8 +367,6 @@ extern "C" kb_status kb_layernorm(kb_ctx* ctx, const void* d_x, uint64_t rows, u
   p.eps = eps;
   p.param_f32 = param_dtype == KB_F32;
   p.e5m2 = q_dtype == KB_F8E5M2;
-  p.stages = p.slot_bytes = 0;
-  p.status = ctx->d_status;
   const bool vec = cols % 8 == 0 && rows_aligned(d_x, ldx, e) && (!d_y || rows_aligned(d_y, ldy, e)) &&
                    (!d_q || (ldq % 8 == 0 && aligned_to(d_q, 8))) && aligned16(d_weight) && aligned16(d_bias);
   if (dtype == KB_F32) return vec ? launch_norm<KB_F32, true>(ctx, p, st) : launch_norm<KB_F32, false>(ctx, p, st);

@@ -43,7 +43,10 @@ __global__ void __launch_bounds__(256) quant_rows_kernel(const QuantParams p) {
 // of x (only needed transposed: the block then runs along the rows of x).  A thread keeps its 8 x 8
 // elements in their storage type (32 registers for 16-bit types), so that three CTAs fit on an SM
 // and 96 KB are on their way while one of them reduces.
-constexpr int kTransposePitch = 132;   // bytes; an odd number of words spreads a column's rows over the banks
+// The transposed tile in shared memory: rows of 128 codes; the 8-byte piece k of row r stands at
+// place k ^ (r / 8), so that neither the writes (16 rows apart by 8, one piece each) nor the reads
+// (one row at a time) meet in a bank.
+__device__ __forceinline__ int transposed_at(int r, int k) { return r * 128 + ((k ^ (r >> 3)) & 15) * 8; }
 template <int DT>
 struct Held8 {   // 8 consecutive elements of one row
   static constexpr int kWords = DT == KB_F32 ? 8 : 4;
@@ -80,8 +83,9 @@ __device__ __forceinline__ float inf_to_nan(float v) { return isinf(v) ? __uint_
 
 template <int DT, bool VEC, bool E5M2, bool TILES, bool TRANSPOSE>
 __global__ void __launch_bounds__(256, DT == KB_F32 ? 2 : 3) quant_tile_kernel(const QuantParams p) {
-  __shared__ float smax[TILES ? 8 : 8 * 128];
-  __shared__ __align__(16) unsigned char st[TRANSPOSE ? 128 * kTransposePitch : 16];
+  __shared__ __align__(16) float smax[TILES ? 8 : 8 * 128];
+  __shared__ __align__(16) float sinv[TILES ? 4 : 128];
+  __shared__ __align__(16) unsigned char st[TRANSPOSE ? 128 * 128 : 16];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int cx = threadIdx.x & 15, ry = threadIdx.x >> 4;
   const uint32_t rt = blockIdx.x / p.ctiles, ct = blockIdx.x % p.ctiles;
@@ -137,46 +141,55 @@ __global__ void __launch_bounds__(256, DT == KB_F32 ? 2 : 3) quant_tile_kernel(c
         p.scale[(uint64_t)ct * p.rtiles + rt] = s.scale;
     }
   } else {
-    auto columns = [&](bool settle) {   // each column's maximum over the warp's 16 rows
+    auto columns = [&](bool settle) {   // each column's maximum over the warp's 16 rows, to smax[warp][column]
+      float m[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        float m = 0.0f;
+        m[j] = 0.0f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           const float v = h[i].get(j);
-          m = fmaxf(m, fabsf(settle ? inf_to_nan(v) : v));
+          m[j] = fmaxf(m[j], fabsf(settle ? inf_to_nan(v) : v));
         }
-        m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, 16));
-        if (lane < 16) smax[warp * 128 + cx * 8 + j] = m;
+        m[j] = fmaxf(m[j], __shfl_xor_sync(0xFFFFFFFFu, m[j], 16));
       }
+      if (lane < 16) {
+        float4* dst = reinterpret_cast<float4*>(smax + warp * 128 + cx * 8);
+        dst[0] = make_float4(m[0], m[1], m[2], m[3]);
+        dst[1] = make_float4(m[4], m[5], m[6], m[7]);
+      }
+    };
+    // one thread per column: the tile's maximum, the scale to memory, the factor back to shared memory
+    auto column = [&]() {
+      float t = 0.0f;
+      if (threadIdx.x < 128) {
+#pragma unroll
+        for (int w = 0; w < 8; ++w) t = fmaxf(t, smax[w * 128 + threadIdx.x]);
+        const BlockScale s = block_scale<E5M2>(t);
+        sinv[threadIdx.x] = s.inv;
+        const uint64_t c = (uint64_t)ct * 128 + threadIdx.x;
+        if (c < p.cols) p.scale[(uint64_t)rt * p.cols + c] = s.scale;
+      }
+      return isinf(t);
     };
     columns(false);
     __syncthreads();
-    auto column = [&](int j) {
-      float t = 0.0f;
-#pragma unroll
-      for (int w = 0; w < 8; ++w) t = fmaxf(t, smax[w * 128 + cx * 8 + j]);
-      return t;
-    };
-    bool mine = false;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      inv[j] = column(j);
-      mine |= isinf(inv[j]);
-    }
-    infinite = __syncthreads_or(mine);
+    infinite = __syncthreads_or(column());
     if (infinite) {
       columns(true);
       __syncthreads();
-#pragma unroll
-      for (int j = 0; j < 8; ++j) inv[j] = column(j);
+      column();
+      __syncthreads();
     }
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const BlockScale s = block_scale<E5M2>(inv[j]);
-      inv[j] = s.inv;
-      if (ry == 0 && j < ncol) p.scale[(uint64_t)rt * p.cols + col0 + j] = s.scale;
-    }
+    const float4 f0 = *reinterpret_cast<const float4*>(sinv + cx * 8), f1 = *reinterpret_cast<const float4*>(sinv + cx * 8 + 4);
+    inv[0] = f0.x;
+    inv[1] = f0.y;
+    inv[2] = f0.z;
+    inv[3] = f0.w;
+    inv[4] = f1.x;
+    inv[5] = f1.y;
+    inv[6] = f1.z;
+    inv[7] = f1.w;
   }
   if constexpr (!TRANSPOSE) {
 #pragma unroll
@@ -203,9 +216,7 @@ __global__ void __launch_bounds__(256, DT == KB_F32 ? 2 : 3) quant_tile_kernel(c
 #pragma unroll
       for (int i = 0; i < 8; ++i) c[i] = infinite ? inf_to_nan(h[i].get(j)) : h[i].get(j);
       const uint2 r = quant8<E5M2>(c, inv[j]);
-      uint32_t* dst = reinterpret_cast<uint32_t*>(st + (cx * 8 + j) * kTransposePitch + ry * 8);
-      dst[0] = r.x;
-      dst[1] = r.y;
+      *reinterpret_cast<uint2*>(st + transposed_at(cx * 8 + j, ry)) = r;
     }
     __syncthreads();
     // a warp writes one transposed row (a column of x) at a time
@@ -216,9 +227,9 @@ __global__ void __launch_bounds__(256, DT == KB_F32 ? 2 : 3) quant_tile_kernel(c
       if (trow >= p.cols) break;
       unsigned char* dst = p.q + trow * p.ldq + tcol0;
       if ((p.ldq & 3) == 0 && left == 128 && (reinterpret_cast<uintptr_t>(p.q) & 3) == 0) {
-        reinterpret_cast<uint32_t*>(dst)[lane] = *reinterpret_cast<const uint32_t*>(st + c * kTransposePitch + lane * 4);
+        reinterpret_cast<uint32_t*>(dst)[lane] = *reinterpret_cast<const uint32_t*>(st + transposed_at(c, lane >> 1) + (lane & 1) * 4);
       } else {
-        for (int b = lane; b < left; b += 32) dst[b] = st[c * kTransposePitch + b];
+        for (int b = lane; b < left; b += 32) dst[b] = st[transposed_at(c, b >> 3) + (b & 7)];
       }
     }
   }
