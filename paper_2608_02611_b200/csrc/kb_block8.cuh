@@ -189,41 +189,86 @@ __device__ __forceinline__ float warp_max(float v) {
   return v;
 }
 
-// Quantise a lane's part of group g of row `row`: codes to q, the blocks' scales to
-// scale[block][row].  All 32 lanes take part; elements past the row's end must be 0.
-template <bool E5M2, bool VEC>
-__device__ __forceinline__ void quant_group(float (&v)[8], uint32_t g, int lane, uint32_t cols, uint64_t row,
-                                            uint64_t rows, unsigned char* q, uint64_t ldq, float* scale) {
+// The scale and the factor of a block whose maximum all lanes of `mask` hold: one lane of the 16 (or
+// 32) divides one way round and the others the other way, so the two quotients cost one division.
+template <bool E5M2>
+__device__ __forceinline__ BlockScale shared_block_scale(float amax, unsigned int mask, int first, int lane) {
+  constexpr float top = E5M2 ? 57344.0f : 448.0f;
+  const float a = fmaxf(amax, 0x1p-100f);
+  const bool is_first = lane == first;
+  const float r = __fdiv_rn(is_first ? a : top, is_first ? top : a);
+  return {r, __shfl_sync(mask, r, first + 1)};   // .scale holds in lane `first` only
+}
+
+// Quantise a lane's part of the groups g0, g0 + gstep, ... (NCH of them) of row `row`: codes to q,
+// the blocks' scales to scale[block][row].  All 32 lanes take part; elements past the row's end must
+// be 0.  The steps of all groups stand side by side, so that their shuffles and divisions overlap.
+template <bool E5M2, bool VEC, int NCH>
+__device__ __forceinline__ void quant_groups(float (&v)[NCH][8], uint32_t g0, uint32_t gstep, int lane, uint32_t cols,
+                                             uint64_t row, uint64_t rows, unsigned char* q, uint64_t ldq,
+                                             float* scale) {
   if constexpr (VEC) {
-    const uint32_t c = group_col<true>(g, lane, 0);
     const unsigned int half = 0xFFFFu << (lane & 16);
-    float m = max_abs<0, 8>(v);
+    float m[NCH];
+    bool any = false;
 #pragma unroll
-    for (int o = 8; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(half, m, o));
-    if (isinf(m)) {   // the same for the block's 16 lanes
-      m = settle_inf<0, 8>(v);
+    for (int i = 0; i < NCH; ++i) m[i] = max_abs<0, 8>(v[i]);
 #pragma unroll
-      for (int o = 8; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(half, m, o));
+    for (int o = 8; o > 0; o >>= 1)
+#pragma unroll
+      for (int i = 0; i < NCH; ++i) m[i] = fmaxf(m[i], __shfl_xor_sync(half, m[i], o));
+#pragma unroll
+    for (int i = 0; i < NCH; ++i) any |= isinf(m[i]);
+    if (any) {   // the same for the 16 lanes of a block
+#pragma unroll
+      for (int i = 0; i < NCH; ++i) {
+        m[i] = settle_inf<0, 8>(v[i]);
+#pragma unroll
+        for (int o = 8; o > 0; o >>= 1) m[i] = fmaxf(m[i], __shfl_xor_sync(half, m[i], o));
+      }
     }
-    const BlockScale s = block_scale<E5M2>(m);
-    if (c < cols) {
-      *reinterpret_cast<uint2*>(q + row * ldq + c) = quant8<E5M2>(v, s.inv);
-      if ((lane & 15) == 0) scale[(uint64_t)(c >> 7) * rows + row] = s.scale;
+    BlockScale s[NCH];
+#pragma unroll
+    for (int i = 0; i < NCH; ++i) s[i] = shared_block_scale<E5M2>(m[i], half, lane & 16, lane);
+#pragma unroll
+    for (int i = 0; i < NCH; ++i) {
+      const uint32_t c = group_col<true>(g0 + i * gstep, lane, 0);
+      if (c < cols) {
+        *reinterpret_cast<uint2*>(q + row * ldq + c) = quant8<E5M2>(v[i], s[i].inv);
+        if ((lane & 15) == 0) scale[(uint64_t)(c >> 7) * rows + row] = s[i].scale;
+      }
     }
   } else {
-    float m0 = warp_max(max_abs<0, 4>(v)), m1 = warp_max(max_abs<4, 8>(v));
-    if (isinf(m0)) m0 = warp_max(settle_inf<0, 4>(v));
-    if (isinf(m1)) m1 = warp_max(settle_inf<4, 8>(v));
-    const BlockScale s0 = block_scale<E5M2>(m0), s1 = block_scale<E5M2>(m1);
-    const uint2 r0 = quant8<E5M2>(v, s0.inv), r1 = quant8<E5M2>(v, s1.inv);
+    float m[NCH][2];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const uint32_t c = group_col<false>(g, lane, j);
-      const uint32_t w = j < 4 ? r0.x : r1.y;
-      if (c < cols) q[row * ldq + c] = (unsigned char)(w >> (8 * (j & 3)));
+    for (int i = 0; i < NCH; ++i) {
+      m[i][0] = max_abs<0, 4>(v[i]);
+      m[i][1] = max_abs<4, 8>(v[i]);
     }
-    const uint32_t kb = g * 2 + lane;   // lanes 0 and 1: the group's two blocks
-    if (lane < 2 && kb * 128u < cols) scale[(uint64_t)kb * rows + row] = lane ? s1.scale : s0.scale;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1)
+#pragma unroll
+      for (int i = 0; i < 2 * NCH; ++i)
+        m[i >> 1][i & 1] = fmaxf(m[i >> 1][i & 1], __shfl_xor_sync(0xFFFFFFFFu, m[i >> 1][i & 1], o));
+#pragma unroll
+    for (int i = 0; i < NCH; ++i) {
+      const uint32_t g = g0 + i * gstep;
+      if (isinf(m[i][0])) m[i][0] = warp_max(settle_inf<0, 4>(v[i]));   // the same for the warp
+      if (isinf(m[i][1])) m[i][1] = warp_max(settle_inf<4, 8>(v[i]));
+      // lanes 0..15 work out the first block's quotients, lanes 16..31 the second's
+      const unsigned int half = 0xFFFFu << (lane & 16);
+      const BlockScale s = shared_block_scale<E5M2>(lane < 16 ? m[i][0] : m[i][1], half, lane & 16, lane);
+      const float inv0 = __shfl_sync(0xFFFFFFFFu, s.inv, 0), inv1 = __shfl_sync(0xFFFFFFFFu, s.inv, 16);
+      const uint2 r0 = quant8<E5M2>(v[i], inv0), r1 = quant8<E5M2>(v[i], inv1);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const uint32_t c = group_col<false>(g, lane, j);
+        const uint32_t w = j < 4 ? r0.x : r1.y;
+        if (c < cols) q[row * ldq + c] = (unsigned char)(w >> (8 * (j & 3)));
+      }
+      const uint32_t kb = g * 2 + (lane >> 4);
+      if ((lane & 15) == 0 && kb * 128u < cols) scale[(uint64_t)kb * rows + row] = s.scale;
+    }
   }
 }
 

@@ -1,13 +1,10 @@
 // Layer norm, forward and backward (contracts in include/kb_ops.h).
 //
-// Forward: a row lives in the registers of as few warps as still fill the card (up to 4096 columns
-// per warp), 8 elements per lane and group of 256 (kb_block8.cuh).  The mean and then the sum of
-// squared distances from it are reduced from the registers, so the row is read once and the
-// variance does not suffer from the cancellation of sum(x^2)/n - mean^2.  The same registers then
-// give y and, where asked for, the row's 8-bit blocks, so a consumer in 8 bits costs no second pass
-// over y.  Few warps per row: what a row costs beyond its elements (two trees of shuffles, a
-// division, a root) is paid once per warp, warps that share no barrier drift apart and keep the
-// memory busy, and a warp has its whole share of the row on the way at once.
+// Forward: a row lives in the registers of one warp (up to 1024 columns) or one CTA, 8 elements
+// per lane and group of 256 (kb_block8.cuh).  The mean and then the sum of squared distances from
+// it are reduced from the registers, so the row is read once and the variance does not suffer from
+// the cancellation of sum(x^2)/n - mean^2.  The same registers then give y and, where asked for,
+// the row's 8-bit blocks, so a consumer in 8 bits costs no second pass over y.
 //
 // Backward: rows by warp or CTA, walking over rows; each lane keeps its columns' sums of dy * xh and
 // dy in registers over all its rows.  They leave once, as a partial row per CTA, and
@@ -34,7 +31,7 @@ struct NormParams {
   uint64_t rows, ldx, ldy, ldq;
   uint32_t cols, groups;
   float eps;
-  bool param_f32, e5m2;
+  bool param_f32;
 };
 
 struct NormBwdParams {
@@ -66,25 +63,34 @@ __device__ __forceinline__ float cta_sum(float v, float* red, int warp, int lane
   return warp_sum(lane < nwarps ? red[lane] : 0.0f);
 }
 
-// y and the row's other outputs from a lane's 8 centred elements (x - mean) of group g
-template <int DT, bool VEC>
-__device__ __forceinline__ void norm_emit(const NormParams& p, uint64_t row, uint32_t g, int lane, float rstd,
-                                          const float (&w)[8], const float (&b)[8], float (&v)[8]) {
+// y and the row's blocks from a lane's centred elements (x - mean) of NCH groups.  Q: 0 no blocks,
+// 1 e4m3, 2 e5m2.
+template <int DT, bool VEC, int NCH, int Q>
+__device__ __forceinline__ void norm_emit(const NormParams& p, uint64_t row, uint32_t g0, uint32_t gstep, int lane,
+                                          float rstd, float (&v)[NCH][8]) {
 #pragma unroll
-  for (int j = 0; j < 8; ++j) v[j] = fmaf(v[j] * rstd, w[j], b[j]);
-  if (p.y) store_group<DT, VEC>(p.y, row * p.ldy, g, lane, p.cols, v);
-  if (p.q) {
-    fill_tail<VEC>(g, lane, p.cols, 0.0f, v);
-    if (p.e5m2)
-      quant_group<true, VEC>(v, g, lane, p.cols, row, p.rows, p.q, p.ldq, p.scale);
-    else
-      quant_group<false, VEC>(v, g, lane, p.cols, row, p.rows, p.q, p.ldq, p.scale);
+  for (int i = 0; i < NCH; ++i) {
+    float w[8], b[8];
+    load_params<DT, VEC>(p.weight, p.param_f32, g0 + i * gstep, lane, p.cols, 1.0f, w);
+    load_params<DT, VEC>(p.bias, p.param_f32, g0 + i * gstep, lane, p.cols, 0.0f, b);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[i][j] = fmaf(v[i][j] * rstd, w[j], b[j]);
+  }
+  if (p.y) {
+#pragma unroll
+    for (int i = 0; i < NCH; ++i)
+      store_group<DT, VEC>(p.y, row * p.ldy, g0 + i * gstep, lane, p.cols, v[i]);
+  }
+  if constexpr (Q != 0) {
+#pragma unroll
+    for (int i = 0; i < NCH; ++i) fill_tail<VEC>(g0 + i * gstep, lane, p.cols, 0.0f, v[i]);
+    quant_groups<Q == 2, VEC, NCH>(v, g0, gstep, lane, p.cols, row, p.rows, p.q, p.ldq, p.scale);
   }
 }
 
 // A row per warp (WARP) or per CTA, NCH groups per warp in registers.
-template <int DT, int NCH, bool VEC, bool WARP>
-__global__ void __launch_bounds__(WARP ? 128 : NCH == 1 ? 1024 : 256) norm_kernel(const NormParams p) {
+template <int DT, int NCH, bool VEC, bool WARP, int Q>
+__global__ void __launch_bounds__(WARP ? 128 : NCH == 1 ? 1024 : 512) norm_kernel(const NormParams p) {
   __shared__ float red[2][32];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, nwarps = blockDim.x >> 5;
   const uint64_t row = WARP ? (uint64_t)blockIdx.x * 4 + warp : blockIdx.x;
@@ -112,15 +118,7 @@ __global__ void __launch_bounds__(WARP ? 128 : NCH == 1 ? 1024 : 256) norm_kerne
   }
   const float var = (WARP ? warp_sum(ss) : cta_sum(ss, red[1], warp, lane, nwarps)) / n;
   const float rstd = 1.0f / sqrtf(var + p.eps);
-#pragma unroll
-  for (int i = 0; i < NCH; ++i) {
-    const uint32_t g = g0 + i * gstep;
-    if (g >= p.groups) break;
-    float w[8], b[8];
-    load_params<DT, VEC>(p.weight, p.param_f32, g, lane, p.cols, 1.0f, w);
-    load_params<DT, VEC>(p.bias, p.param_f32, g, lane, p.cols, 0.0f, b);
-    norm_emit<DT, VEC>(p, row, g, lane, rstd, w, b, v[i]);
-  }
+  norm_emit<DT, VEC, NCH, Q>(p, row, g0, gstep, lane, rstd, v);
   if (lane == 0 && (WARP || warp == 0)) {
     if (p.mean) p.mean[row] = mean;
     if (p.rstd) p.rstd[row] = rstd;
@@ -128,7 +126,7 @@ __global__ void __launch_bounds__(WARP ? 128 : NCH == 1 ? 1024 : 256) norm_kerne
 }
 
 // Rows too long for the registers of a CTA: three passes, the second and third from L2.
-template <int DT, bool VEC>
+template <int DT, bool VEC, int Q>
 __global__ void __launch_bounds__(512) norm_long_kernel(const NormParams p) {
   __shared__ float red[2][32];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, nwarps = blockDim.x >> 5;
@@ -155,14 +153,11 @@ __global__ void __launch_bounds__(512) norm_long_kernel(const NormParams p) {
   const float var = cta_sum(ss, red[1], warp, lane, nwarps) / n;
   const float rstd = 1.0f / sqrtf(var + p.eps);
   for (uint32_t g = warp; g < p.groups; g += nwarps) {
-    float v[8];
-    float w[8], b[8];
-    load_group<DT, VEC>(p.x, row * p.ldx, g, lane, p.cols, v);
-    load_params<DT, VEC>(p.weight, p.param_f32, g, lane, p.cols, 1.0f, w);
-    load_params<DT, VEC>(p.bias, p.param_f32, g, lane, p.cols, 0.0f, b);
+    float v[1][8];
+    load_group<DT, VEC>(p.x, row * p.ldx, g, lane, p.cols, v[0]);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] -= mean;
-    norm_emit<DT, VEC>(p, row, g, lane, rstd, w, b, v);
+    for (int j = 0; j < 8; ++j) v[0][j] -= mean;
+    norm_emit<DT, VEC, 1, Q>(p, row, g, 1, lane, rstd, v);
   }
   if (threadIdx.x == 0) {
     if (p.mean) p.mean[row] = mean;

@@ -102,30 +102,32 @@ kb_status ring_limits(kb_ctx* ctx, K kernel, size_t smem) {
   return KB_OK;
 }
 
-template <int DT, int NCH, bool VEC>
+template <int DT, int NCH, bool VEC, int Q>
 kb_status launch_norm(kb_ctx* ctx, const NormParams& p, cudaStream_t st) {
   const uint32_t warps = (p.groups + NCH - 1) / NCH;
   if (warps == 1)
-    norm_kernel<DT, NCH, VEC, true><<<(unsigned int)((p.rows + 3) / 4), 128, 0, st>>>(p);
+    norm_kernel<DT, NCH, VEC, true, Q><<<(unsigned int)((p.rows + 3) / 4), 128, 0, st>>>(p);
   else
-    norm_kernel<DT, NCH, VEC, false><<<(unsigned int)p.rows, 32 * warps, 0, st>>>(p);
+    norm_kernel<DT, NCH, VEC, false, Q><<<(unsigned int)p.rows, 32 * warps, 0, st>>>(p);
   return launched(ctx);
 }
-
-template <int DT, bool VEC>
+template <int DT, bool VEC, int Q>
 kb_status launch_norm(kb_ctx* ctx, const NormParams& p, cudaStream_t st) {
-  // as few warps per row as still give every SM 12 of them (16 groups a warp take about 170
-  // registers a thread: 12 warps fill an SM); with few rows, as many as the row has groups
-  const uint64_t fill = 12ull * ctx->sm_count;
-  auto enough = [&](uint32_t nch) { return p.rows * ((p.groups + nch - 1) / nch) >= fill; };
-  auto fits = [&](uint32_t nch, uint32_t most) { return (p.groups + nch - 1) / nch <= most; };
-  if (p.groups == 1 || (!enough(2) && fits(1, 32))) return launch_norm<DT, 1, VEC>(ctx, p, st);
-  if (p.groups == 2 || (!enough(4) && fits(2, 8))) return launch_norm<DT, 2, VEC>(ctx, p, st);
-  if (p.groups <= 4 || (!enough(8) && fits(4, 8))) return launch_norm<DT, 4, VEC>(ctx, p, st);
-  if (p.groups <= 8 || (!enough(16) && fits(8, 8))) return launch_norm<DT, 8, VEC>(ctx, p, st);
-  if (fits(16, 8)) return launch_norm<DT, 16, VEC>(ctx, p, st);
-  norm_long_kernel<DT, VEC><<<(unsigned int)p.rows, 512, 0, st>>>(p);
+  // one row per SM at most: as many warps as the row has groups, for the shortest time of one row
+  if (p.groups == 1 || (p.groups <= 32 && p.rows <= (uint64_t)ctx->sm_count))
+    return launch_norm<DT, 1, VEC, Q>(ctx, p, st);
+  if (p.groups == 2) return launch_norm<DT, 2, VEC, Q>(ctx, p, st);
+  if (p.groups <= 64) return launch_norm<DT, 4, VEC, Q>(ctx, p, st);
+  norm_long_kernel<DT, VEC, Q><<<(unsigned int)p.rows, 512, 0, st>>>(p);
   return launched(ctx);
+}
+template <int DT>
+kb_status launch_norm(kb_ctx* ctx, const NormParams& p, bool vec, bool e5m2, cudaStream_t st) {
+  if (vec)
+    return !p.q ? launch_norm<DT, true, 0>(ctx, p, st)
+                : e5m2 ? launch_norm<DT, true, 2>(ctx, p, st) : launch_norm<DT, true, 1>(ctx, p, st);
+  return !p.q ? launch_norm<DT, false, 0>(ctx, p, st)
+              : e5m2 ? launch_norm<DT, false, 2>(ctx, p, st) : launch_norm<DT, false, 1>(ctx, p, st);
 }
 
 template <int DT, int NCH, bool VEC, bool WARP>
@@ -366,12 +368,12 @@ extern "C" kb_status kb_layernorm(kb_ctx* ctx, const void* d_x, uint64_t rows, u
   p.groups = (uint32_t)((cols + kGroup - 1) / kGroup);
   p.eps = eps;
   p.param_f32 = param_dtype == KB_F32;
-  p.e5m2 = q_dtype == KB_F8E5M2;
+  const bool e5m2 = q_dtype == KB_F8E5M2;
   const bool vec = cols % 8 == 0 && rows_aligned(d_x, ldx, e) && (!d_y || rows_aligned(d_y, ldy, e)) &&
                    (!d_q || (ldq % 8 == 0 && aligned_to(d_q, 8))) && aligned16(d_weight) && aligned16(d_bias);
-  if (dtype == KB_F32) return vec ? launch_norm<KB_F32, true>(ctx, p, st) : launch_norm<KB_F32, false>(ctx, p, st);
-  if (dtype == KB_F16) return vec ? launch_norm<KB_F16, true>(ctx, p, st) : launch_norm<KB_F16, false>(ctx, p, st);
-  return vec ? launch_norm<KB_BF16, true>(ctx, p, st) : launch_norm<KB_BF16, false>(ctx, p, st);
+  if (dtype == KB_F32) return launch_norm<KB_F32>(ctx, p, vec, e5m2, st);
+  if (dtype == KB_F16) return launch_norm<KB_F16>(ctx, p, vec, e5m2, st);
+  return launch_norm<KB_BF16>(ctx, p, vec, e5m2, st);
 }
 
 extern "C" kb_status kb_layernorm_backward(kb_ctx* ctx, const void* d_dy, uint64_t lddy, const void* d_x,

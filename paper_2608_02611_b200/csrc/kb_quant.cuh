@@ -32,10 +32,7 @@ __global__ void __launch_bounds__(256) quant_rows_kernel(const QuantParams p) {
 #pragma unroll
     for (int i = 0; i < kQuantRowGroups; ++i)
       load_group<DT, VEC>(p.x, row * p.ldx, g0 + i, lane, (uint32_t)p.cols, v[i]);
-#pragma unroll
-    for (int i = 0; i < kQuantRowGroups; ++i)
-      if (g0 + i < p.groups)
-        quant_group<E5M2, VEC>(v[i], g0 + i, lane, (uint32_t)p.cols, row, p.rows, p.q, p.ldq, p.scale);
+    quant_groups<E5M2, VEC, kQuantRowGroups>(v, g0, 1, lane, (uint32_t)p.cols, row, p.rows, p.q, p.ldq, p.scale);
   }
 }
 
