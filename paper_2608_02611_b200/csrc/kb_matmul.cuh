@@ -57,7 +57,10 @@ __device__ __forceinline__ void drain_copies(uint64_t* full, uint32_t stages, ui
 // The rows of B (weights) take the 128 lanes of the tile and BN rows of A its columns, so that a
 // single token wastes no lanes and the weights stream through once.  A cluster of `splits` CTAs
 // shares a tile's K blocks; the partial sums are added over distributed shared memory in rank
-// order.
+// order.  Bound by the weights' bytes: 16 KB of weights per K block and CTA, up to ten blocks on
+// their way.  The scales come through a ring of their own, several blocks ahead: fetched when they
+// are needed, their latency would stand in every block.
+constexpr uint32_t kScaleStep = 4;          // K blocks whose scales share a slot of shared memory
 template <int BN>
 struct LaneTile {
   static constexpr uint32_t kStageBytes = (128 + BN) * 128;
@@ -65,19 +68,33 @@ struct LaneTile {
   static constexpr uint32_t kAcc = BN == 128 ? 2 : 4;          // accumulators in tensor memory
   static constexpr uint32_t kTmemCols = kAcc * BN;
   static constexpr uint32_t kSmem = 1024 + kStages * kStageBytes;
-  static constexpr int kThreads = 192;
+  static constexpr uint32_t kScaleSlots = 4;
+  static constexpr int kThreads = 224;                         // copies, issue, four warps that add, scales
 };
 
-template <int BN>
+// c0 += v0 * s0, c1 += v1 * s1 as one packed instruction
+__device__ __forceinline__ void fma_pair(float& c0, float& c1, float v0, float v1, float s0, float s1) {
+  asm("{\n.reg .b64 c, v, s;\n"
+      "mov.b64 c, {%0, %1};\nmov.b64 v, {%2, %3};\nmov.b64 s, {%4, %5};\n"
+      "fma.rn.f32x2 c, v, s, c;\nmov.b64 {%0, %1}, c;\n}"
+      : "+f"(c0), "+f"(c1)
+      : "f"(v0), "f"(v1), "f"(s0), "f"(s1));
+}
+
+// BROWS: B has one scale per row (per lane of the tile) instead of one per 128 rows.
+template <int BN, bool BROWS>
 __global__ void __launch_bounds__(LaneTile<BN>::kThreads, 1)
     matmul_lanes_kernel(const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_a,
                         const MatmulParams p) {
   using T = LaneTile<BN>;
   extern __shared__ unsigned char dyn[];
   __shared__ uint64_t full[T::kStages], empty[T::kStages], acc_full[T::kAcc], acc_empty[T::kAcc], drained;
+  __shared__ uint64_t sc_full[T::kScaleSlots], sc_empty[T::kScaleSlots];
   __shared__ uint32_t tmem_base;
   __shared__ unsigned int abort_word;
-  __shared__ __align__(16) float col_scale[4][2][BN];
+  __shared__ float lane_scale[T::kScaleSlots][kScaleStep][BROWS ? 128 : 1];
+  __shared__ float col_scale[T::kScaleSlots][kScaleStep][BN];
+  __shared__ __align__(16) float both_scale[4][2][BN];   // per warp
   volatile unsigned int* abort_flag = &abort_word;
   unsigned char* stages = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(dyn) + 1023) & ~(uintptr_t)1023);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -95,6 +112,10 @@ __global__ void __launch_bounds__(LaneTile<BN>::kThreads, 1)
     for (uint32_t i = 0; i < T::kAcc; ++i) {
       mbar_init(&acc_full[i], 1);
       mbar_init(&acc_empty[i], 4);
+    }
+    for (uint32_t i = 0; i < T::kScaleSlots; ++i) {
+      mbar_init(&sc_full[i], 32);
+      mbar_init(&sc_empty[i], 4);
     }
     mbar_init(&drained, 1);
     abort_word = 0u;
@@ -156,61 +177,93 @@ __global__ void __launch_bounds__(LaneTile<BN>::kThreads, 1)
       }
     }
     __syncwarp();
+  } else if (warp == 6) {
+    uint32_t slot = 0, phase = 0;
+    for (uint32_t i = 0; i < nkb; i += kScaleStep) {
+      if (!__all_sync(0xFFFFFFFFu, mbar_wait_bounded(&sc_empty[slot], phase ^ 1u, abort_flag, p.status))) break;
+#pragma unroll
+      for (uint32_t k = 0; k < kScaleStep; ++k) {
+        const bool k_in = i + k < nkb;
+        const float* as = p.a_scale + (uint64_t)(kb0 + i + k) * p.M;
+        const float* bs = p.b_scale + (uint64_t)(kb0 + i + k) * p.b_scale_ld;
+#pragma unroll
+        for (int c = 0; c < BN; c += 32) {
+          const uint32_t m = m0 + c + lane;
+          const bool in = k_in && m < p.M;
+          if (c + lane < BN) cp_async_f32(&col_scale[slot][k][c + lane], in ? as + m : p.a_scale, in);
+        }
+        if constexpr (BROWS) {
+#pragma unroll
+          for (int c = 0; c < 128; c += 32) {
+            const bool in = k_in && n0 + c + lane < p.N;
+            cp_async_f32(&lane_scale[slot][k][c + lane], in ? bs + n0 + c + lane : p.b_scale, in);
+          }
+        } else if (lane == 0) {
+          cp_async_f32(&lane_scale[slot][k][0], k_in ? bs + (n0 >> 7) : p.b_scale, k_in);
+        }
+      }
+      cp_async_arrive(&sc_full[slot]);
+      if (++slot == T::kScaleSlots) {
+        slot = 0;
+        phase ^= 1u;
+      }
+    }
+    cp_async_wait_all();
+    __syncwarp();
   } else {
     const int quarter = warp & 3;                       // the lanes of tensor memory this warp may read
     const uint32_t n = n0 + quarter * 32 + lane;
-    const float* bs = p.b_scale + (n >> p.b_scale_shift);
     const bool n_in = n < p.N;
-    float (*cs)[BN] = col_scale[quarter];
-    constexpr int kPer = (BN + 31) / 32;
-    float next_col[kPer], next_lane = 0.0f;
-    auto fetch = [&](uint32_t kb) {
-      if (n_in) next_lane = bs[(uint64_t)kb * p.b_scale_ld];
-#pragma unroll
-      for (int i = 0; i < kPer; ++i) {
-        const uint32_t m = m0 + i * 32 + lane;
-        next_col[i] = (i * 32 + lane < BN && m < p.M) ? p.a_scale[(uint64_t)kb * p.M + m] : 0.0f;
-      }
-    };
+    uint32_t slot = 0, slot_phase = 0;
 #pragma unroll
     for (int j = 0; j < BN; ++j) acc[j] = 0.0f;
-    if (nkb) fetch(kb0);
+    // after a wait has run out every later one returns at once: the loop runs to its end, because
+    // reads of tensor memory are collective
     for (uint32_t i = 0; i < nkb; ++i) {
-      const uint32_t a = i % T::kAcc, a_phase = (i / T::kAcc) & 1u;
-      float* c = cs[i & 1];
+      const uint32_t a = i % T::kAcc, a_phase = (i / T::kAcc) & 1u, k = i % kScaleStep;
+      if (k == 0) ok &= mbar_wait_bounded(&sc_full[slot], slot_phase, abort_flag, p.status);
+      // this warp's factors per column; without BROWS the tile's scale is in them
+      float* c = both_scale[quarter][i & 1];
+      const float ls = lane_scale[slot][k][BROWS ? quarter * 32 + lane : 0];
 #pragma unroll
-      for (int k = 0; k < kPer; ++k)
-        if (k * 32 + lane < BN) c[k * 32 + lane] = next_col[k];
-      const float ls = next_lane;
-      __syncwarp();
-      if (i + 1 < nkb) fetch(kb0 + i + 1);
-      if (!__all_sync(0xFFFFFFFFu, mbar_wait_bounded(&acc_full[a], a_phase, abort_flag, p.status))) {
-        ok = false;
-        break;
+      for (int j = 0; j < BN; j += 32)
+        if (j + lane < BN) c[j + lane] = BROWS ? col_scale[slot][k][j + lane] : col_scale[slot][k][j + lane] * ls;
+      if (k == kScaleStep - 1 || i + 1 == nkb) {
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sc_empty[slot]);
+        if (++slot == T::kScaleSlots) {
+          slot = 0;
+          slot_phase ^= 1u;
+        }
       }
+      ok &= mbar_wait_bounded(&acc_full[a], a_phase, abort_flag, p.status);
+      __syncwarp();
       tc_fence_after();
       const uint32_t addr = tmem + ((uint32_t)(quarter * 32) << 16) + a * BN;
-      constexpr int kStep = BN < 32 ? 16 : 32;
+      constexpr int kCols = BN < 32 ? 16 : 32;
 #pragma unroll
-      for (int j0 = 0; j0 < BN; j0 += kStep) {
-        float v[kStep];
-        if constexpr (kStep == 16)
+      for (int j0 = 0; j0 < BN; j0 += kCols) {
+        float v[kCols];
+        if constexpr (kCols == 16)
           tmem_ld16(addr + j0, v);
         else
           tmem_ld32(addr + j0, v);
         tmem_wait_ld();
-        if (j0 + kStep == BN) {   // all of this accumulator is in registers
+        if (j0 + kCols == BN) {   // all of this accumulator is in registers
           tc_fence_before();
           __syncwarp();
           if (lane == 0) mbar_arrive(&acc_empty[a]);
         }
 #pragma unroll
-        for (int j = 0; j < kStep; j += 4) {
+        for (int j = 0; j < kCols; j += 4) {
           const float4 f = *reinterpret_cast<const float4*>(c + j0 + j);
-          acc[j0 + j] = fmaf(v[j] * f.x, ls, acc[j0 + j]);
-          acc[j0 + j + 1] = fmaf(v[j + 1] * f.y, ls, acc[j0 + j + 1]);
-          acc[j0 + j + 2] = fmaf(v[j + 2] * f.z, ls, acc[j0 + j + 2]);
-          acc[j0 + j + 3] = fmaf(v[j + 3] * f.w, ls, acc[j0 + j + 3]);
+          if constexpr (BROWS) {
+            fma_pair(acc[j0 + j], acc[j0 + j + 1], v[j] * f.x, v[j + 1] * f.y, ls, ls);
+            fma_pair(acc[j0 + j + 2], acc[j0 + j + 3], v[j + 2] * f.z, v[j + 3] * f.w, ls, ls);
+          } else {
+            fma_pair(acc[j0 + j], acc[j0 + j + 1], v[j], v[j + 1], f.x, f.y);
+            fma_pair(acc[j0 + j + 2], acc[j0 + j + 3], v[j + 2], v[j + 3], f.z, f.w);
+          }
         }
       }
     }
@@ -223,20 +276,20 @@ __global__ void __launch_bounds__(LaneTile<BN>::kThreads, 1)
       // all copies and matrix instructions of this CTA are done: the ring holds the partial sums
       float* red = reinterpret_cast<float*>(stages) + quarter * 32 + lane;
 #pragma unroll
-      for (int j = 0; j < BN; ++j) red[j * 128] = ok ? acc[j] : 0.0f;
+      for (int j = 0; j < BN; ++j) red[j * 128] = acc[j];
     }
   }
   if (p.splits > 1) {
     cluster_sync_all();
-    if (warp >= 2) {
+    if (warp >= 2 && warp < 6) {
       const int row = (warp & 3) * 32 + lane;
       const uint32_t n = n0 + row;
-      const uint32_t per = BN / p.splits;
       const uint32_t base = smem_u32(stages) + row * 4;
-      for (uint32_t j = rank * per; j < (rank + 1) * per; ++j) {
+      for (uint32_t j = BN * rank / p.splits; j < BN * (rank + 1) / p.splits; ++j) {
+        if (m0 + j >= p.M) break;
         float s = 0.0f;
         for (uint32_t r = 0; r < p.splits; ++r) s += ld_cluster_f32(map_to_rank(base + j * 512, r));
-        if (n < p.N && m0 + j < p.M && ok) store_out(p.d, p.out, (uint64_t)(m0 + j) * p.ldd + n, s);
+        if (n < p.N && ok) store_out(p.d, p.out, (uint64_t)(m0 + j) * p.ldd + n, s);
       }
     }
     cluster_sync_all();   // no CTA leaves while another reads its shared memory
@@ -260,7 +313,6 @@ struct PairTile {
   static constexpr uint32_t kHalfBytes = 128 * 128;             // one operand's share of a CTA
   static constexpr uint32_t kStageBytes = 2 * kHalfBytes;
   static constexpr uint32_t kStages = 5;
-  static constexpr uint32_t kScaleStep = 4;                     // K blocks whose scales share a slot of shared memory
   static constexpr uint32_t kScaleSlots = 3;
   static constexpr uint32_t kTmemCols = 512;
   static constexpr int kEpiWarps = 8;
@@ -276,15 +328,6 @@ struct PairTile {
   static constexpr uint32_t kSmem = 1024 + kStages * kStageBytes + kEpiWarps * kOutBytes;
   static constexpr uint32_t kGroupM = 8;                        // tiles of A that neighbouring pairs share
 };
-
-// c0 += v0 * s, c1 += v1 * s as one packed instruction
-__device__ __forceinline__ void fma_pair(float& c0, float& c1, float v0, float v1, float s) {
-  asm("{\n.reg .b64 c, v, s;\n"
-      "mov.b64 c, {%0, %1};\nmov.b64 v, {%2, %3};\nmov.b64 s, {%4, %4};\n"
-      "fma.rn.f32x2 c, v, s, c;\nmov.b64 {%0, %1}, c;\n}"
-      : "+f"(c0), "+f"(c1)
-      : "f"(v0), "f"(v1), "f"(s));
-}
 
 // Tile coordinates of item `t`: down kGroupM tiles of A, then along B, so that the pairs that run
 // together read few different rows of either.
@@ -354,8 +397,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PairTile::kThreads, 
   __shared__ uint64_t sc_full[T::kScaleSlots], sc_empty[T::kScaleSlots];
   __shared__ uint32_t tmem_base;
   __shared__ unsigned int abort_word;
-  __shared__ __align__(16) float row_scale[T::kScaleSlots][128][T::kScaleStep];
-  __shared__ __align__(16) float col_scale[T::kScaleSlots][BROWS ? T::kScaleStep * 256 : 2 * T::kScaleStep];
+  __shared__ __align__(16) float row_scale[T::kScaleSlots][128][kScaleStep];
+  __shared__ __align__(16) float col_scale[T::kScaleSlots][BROWS ? kScaleStep * 256 : 2 * kScaleStep];
   volatile unsigned int* abort_flag = &abort_word;
   unsigned char* stages = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(dyn) + 1023) & ~(uintptr_t)1023);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -459,11 +502,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PairTile::kThreads, 
       uint32_t tm, tn;
       pair_tile(t, p.tiles_m, tiles_n, tm, tn);
       const uint32_t m0 = tm * 256 + rank * 128, n0 = tn * 256;
-      for (uint32_t kb0 = 0; kb0 < p.KB; kb0 += T::kScaleStep) {
+      for (uint32_t kb0 = 0; kb0 < p.KB; kb0 += kScaleStep) {
         ok = __all_sync(0xFFFFFFFFu, mbar_wait_bounded(&sc_empty[slot], phase ^ 1u, abort_flag, p.status));
         if (!ok) break;
 #pragma unroll
-        for (uint32_t k = 0; k < T::kScaleStep; ++k) {
+        for (uint32_t k = 0; k < kScaleStep; ++k) {
           const bool k_in = kb0 + k < p.KB;
           const float* as = p.a_scale + (uint64_t)(kb0 + k) * p.M;
           const float* bs = p.b_scale + (uint64_t)(kb0 + k) * p.b_scale_ld;
@@ -483,7 +526,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PairTile::kThreads, 
           } else if (lane < 2) {
             const uint32_t n = n0 + lane * 128;
             const bool in = k_in && n < p.N;
-            cp_async_f32(&col_scale[slot][lane * T::kScaleStep + k], in ? bs + (n >> 7) : p.b_scale, in);
+            cp_async_f32(&col_scale[slot][lane * kScaleStep + k], in ? bs + (n >> 7) : p.b_scale, in);
           }
         }
         cp_async_arrive(&sc_full[slot]);
@@ -509,19 +552,19 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PairTile::kThreads, 
       float acc[128];
 #pragma unroll
       for (int j = 0; j < 128; ++j) acc[j] = 0.0f;
-      for (uint32_t kb0 = 0; kb0 < p.KB; kb0 += T::kScaleStep) {
+      for (uint32_t kb0 = 0; kb0 < p.KB; kb0 += kScaleStep) {
         ok &= mbar_wait_bounded(&sc_full[slot], slot_phase, abort_flag, p.status);
         const float4 rs = *reinterpret_cast<const float4*>(row_scale[slot][quarter * 32 + lane]);
         float s4[4] = {rs.x, rs.y, rs.z, rs.w};
         if constexpr (!BROWS) {
-          const float4 cs = *reinterpret_cast<const float4*>(&col_scale[slot][(cols >> 7) * T::kScaleStep]);
+          const float4 cs = *reinterpret_cast<const float4*>(&col_scale[slot][(cols >> 7) * kScaleStep]);
           s4[0] *= cs.x;
           s4[1] *= cs.y;
           s4[2] *= cs.z;
           s4[3] *= cs.w;
         }
 #pragma unroll 1
-        for (uint32_t k = 0; k < T::kScaleStep && kb0 + k < p.KB; ++k) {
+        for (uint32_t k = 0; k < kScaleStep && kb0 + k < p.KB; ++k) {
           ok &= mbar_wait_bounded(&done[st], st_phase, abort_flag, p.status);
           __syncwarp();
           tc_fence_after();
@@ -550,7 +593,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PairTile::kThreads, 
 #pragma unroll
             for (int j = 0; j < 16; j += 2)
               fma_pair(acc[j0 + j], acc[j0 + j + 1], BROWS ? w[j] * c[j0 + j] : w[j],
-                       BROWS ? w[j + 1] * c[j0 + j + 1] : w[j + 1], s);
+                       BROWS ? w[j + 1] * c[j0 + j + 1] : w[j + 1], s, s);
           }
           a ^= 1u;
         }

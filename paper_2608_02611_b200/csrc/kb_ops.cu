@@ -197,7 +197,9 @@ using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, 
 
 template <int BN>
 kb_status lanes_attr(kb_ctx* ctx) {
-  KB_CUDA(ctx, cudaFuncSetAttribute(matmul_lanes_kernel<BN>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+  KB_CUDA(ctx, cudaFuncSetAttribute(matmul_lanes_kernel<BN, false>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                    (int)LaneTile<BN>::kSmem));
+  KB_CUDA(ctx, cudaFuncSetAttribute(matmul_lanes_kernel<BN, true>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                     (int)LaneTile<BN>::kSmem));
   return KB_OK;
 }
@@ -243,8 +245,10 @@ kb_status launch_lanes(kb_ctx* ctx, MatmulParams& p, const void* a, uint64_t lda
   p.idesc = mma_idesc_f8(b_e5m2, a_e5m2, 128, BN);
   p.tiles_m = (p.M + BN - 1) / BN;
   const uint64_t tiles = (uint64_t)p.tiles_m * ((p.N + 127) / 128);
-  uint32_t splits = 1;
-  while (splits < 8 && tiles * splits * 2 <= (uint64_t)ctx->sm_count && p.KB >= 4 * splits) splits *= 2;
+  // as many CTAs per tile as the card has room for, at least two K blocks each, 8 at most (the
+  // portable cluster size)
+  const uint32_t room = (uint32_t)std::max<uint64_t>(1, (uint64_t)ctx->sm_count / tiles);
+  const uint32_t splits = std::max(1u, std::min({room, p.KB / 2, 8u}));
   p.splits = splits;
   if (tiles * splits > 0x7FFFFFFFull) return fail(ctx, KB_ERR_UNSUPPORTED, "kb_matmul_blocks: more than 2^31 - 1 tiles");
   cudaLaunchConfig_t cfg = {};
@@ -258,7 +262,10 @@ kb_status launch_lanes(kb_ctx* ctx, MatmulParams& p, const void* a, uint64_t lda
   attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  KB_CUDA(ctx, cudaLaunchKernelEx(&cfg, matmul_lanes_kernel<BN>, map_b, map_a, p));
+  if (p.b_scale_shift)
+    KB_CUDA(ctx, cudaLaunchKernelEx(&cfg, matmul_lanes_kernel<BN, false>, map_b, map_a, p));
+  else
+    KB_CUDA(ctx, cudaLaunchKernelEx(&cfg, matmul_lanes_kernel<BN, true>, map_b, map_a, p));
   return launched(ctx);
 }
 
