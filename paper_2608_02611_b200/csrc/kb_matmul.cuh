@@ -69,7 +69,9 @@ struct LaneTile {
   static constexpr uint32_t kTmemCols = kAcc * BN;
   static constexpr uint32_t kSmem = 1024 + kStages * kStageBytes;
   static constexpr uint32_t kScaleSlots = 4;
-  static constexpr int kThreads = 224;                         // copies, issue, four warps that add, scales
+  static constexpr int kEpiWarps = BN >= 64 ? 8 : 4;           // each adds 32 rows x kEpiCols columns
+  static constexpr int kEpiCols = BN / (kEpiWarps / 4);
+  static constexpr int kThreads = 32 * (4 + kEpiWarps);        // and four warps that copy, issue, fetch scales
 };
 
 // c0 += v0 * s0, c1 += v1 * s1 as one packed instruction
@@ -93,8 +95,7 @@ __global__ void __launch_bounds__(LaneTile<BN>::kThreads, 1)
   __shared__ uint32_t tmem_base;
   __shared__ unsigned int abort_word;
   __shared__ float lane_scale[T::kScaleSlots][kScaleStep][BROWS ? 128 : 1];
-  __shared__ float col_scale[T::kScaleSlots][kScaleStep][BN];
-  __shared__ __align__(16) float both_scale[4][2][BN];   // per warp
+  __shared__ __align__(16) float col_scale[T::kScaleSlots][kScaleStep][BN];
   volatile unsigned int* abort_flag = &abort_word;
   unsigned char* stages = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(dyn) + 1023) & ~(uintptr_t)1023);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -111,11 +112,11 @@ __global__ void __launch_bounds__(LaneTile<BN>::kThreads, 1)
     }
     for (uint32_t i = 0; i < T::kAcc; ++i) {
       mbar_init(&acc_full[i], 1);
-      mbar_init(&acc_empty[i], 4);
+      mbar_init(&acc_empty[i], T::kEpiWarps);
     }
     for (uint32_t i = 0; i < T::kScaleSlots; ++i) {
       mbar_init(&sc_full[i], 32);
-      mbar_init(&sc_empty[i], 4);
+      mbar_init(&sc_empty[i], T::kEpiWarps);
     }
     mbar_init(&drained, 1);
     abort_word = 0u;
@@ -127,7 +128,7 @@ __global__ void __launch_bounds__(LaneTile<BN>::kThreads, 1)
   tc_fence_after();
   const uint32_t tmem = tmem_base;
 
-  float acc[BN];
+  float acc[T::kEpiCols];
   bool ok = true;
   if (warp == 0) {
     if (lane == 0) {
@@ -150,34 +151,30 @@ __global__ void __launch_bounds__(LaneTile<BN>::kThreads, 1)
     }
     __syncwarp();
   } else if (warp == 1) {
-    if (lane == 0) {
-      uint32_t st = 0, phase = 0;
-      for (uint32_t i = 0; i < nkb; ++i) {
-        const uint32_t a = i % T::kAcc, a_phase = (i / T::kAcc) & 1u;
-        if (!mbar_wait_bounded(&acc_empty[a], a_phase ^ 1u, abort_flag, p.status) ||
-            !mbar_wait_bounded(&full[st], phase, abort_flag, p.status)) {
-          mma_commit(&drained);   // what has been issued ends before tensor memory is freed
-          const unsigned long long t0 = global_ns();
-          while (!mbar_try_wait(&drained, 0))
-            if (global_ns() - t0 > 1000000000ull) break;
-          break;
-        }
-        tc_fence_after();
-        const uint32_t s = smem_u32(stages + st * T::kStageBytes);
-        const uint64_t lanes_desc = smem_desc_k128(s), cols_desc = smem_desc_k128(s + 128 * 128);
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-          mma_f8<1>(tmem + a * BN, lanes_desc + 2 * k, cols_desc + 2 * k, p.idesc, k > 0);
-        mma_commit(&empty[st]);
-        mma_commit(&acc_full[a]);
-        if (++st == T::kStages) {
-          st = 0;
-          phase ^= 1u;
-        }
+    uint32_t st = 0, phase = 0;
+    for (uint32_t i = 0; i < nkb; ++i) {
+      const uint32_t a = i % T::kAcc, a_phase = (i / T::kAcc) & 1u;
+      const bool go = mbar_wait_bounded(&acc_empty[a], a_phase ^ 1u, abort_flag, p.status) &&
+                      mbar_wait_bounded(&full[st], phase, abort_flag, p.status);
+      if (!__all_sync(0xFFFFFFFFu, go)) {
+        mma_commit(&drained);   // what has been issued ends before tensor memory is freed
+        const unsigned long long t0 = global_ns();
+        while (!mbar_try_wait(&drained, 0))
+          if (global_ns() - t0 > 1000000000ull) break;
+        __syncwarp();
+        break;
+      }
+      tc_fence_after();
+      const uint32_t s = smem_u32(stages + st * T::kStageBytes);
+      mma_f8_block<1>(tmem + a * BN, smem_desc_k128(s), smem_desc_k128(s + 128 * 128), p.idesc);
+      mma_commit(&empty[st]);
+      mma_commit(&acc_full[a]);
+      if (++st == T::kStages) {
+        st = 0;
+        phase ^= 1u;
       }
     }
-    __syncwarp();
-  } else if (warp == 6) {
+  } else if (warp == 2) {
     uint32_t slot = 0, phase = 0;
     for (uint32_t i = 0; i < nkb; i += kScaleStep) {
       if (!__all_sync(0xFFFFFFFFu, mbar_wait_bounded(&sc_empty[slot], phase ^ 1u, abort_flag, p.status))) break;
@@ -210,82 +207,73 @@ __global__ void __launch_bounds__(LaneTile<BN>::kThreads, 1)
     }
     cp_async_wait_all();
     __syncwarp();
-  } else {
+  } else if (warp >= 4) {
     const int quarter = warp & 3;                       // the lanes of tensor memory this warp may read
+    const int col0 = ((warp - 4) >> 2) * T::kEpiCols;   // and its columns
     const uint32_t n = n0 + quarter * 32 + lane;
     const bool n_in = n < p.N;
+    const uint32_t taddr = tmem + ((uint32_t)(quarter * 32) << 16) + col0;
     uint32_t slot = 0, slot_phase = 0;
 #pragma unroll
-    for (int j = 0; j < BN; ++j) acc[j] = 0.0f;
+    for (int j = 0; j < T::kEpiCols; ++j) acc[j] = 0.0f;
     // after a wait has run out every later one returns at once: the loop runs to its end, because
     // reads of tensor memory are collective
     for (uint32_t i = 0; i < nkb; ++i) {
       const uint32_t a = i % T::kAcc, a_phase = (i / T::kAcc) & 1u, k = i % kScaleStep;
       if (k == 0) ok &= mbar_wait_bounded(&sc_full[slot], slot_phase, abort_flag, p.status);
-      // this warp's factors per column; without BROWS the tile's scale is in them
-      float* c = both_scale[quarter][i & 1];
       const float ls = lane_scale[slot][k][BROWS ? quarter * 32 + lane : 0];
+      const float* c = &col_scale[slot][k][col0];
+      ok &= mbar_wait_bounded(&acc_full[a], a_phase, abort_flag, p.status);
+      __syncwarp();
+      tc_fence_after();
+      constexpr int kCols = T::kEpiCols < 32 ? 16 : 32;
 #pragma unroll
-      for (int j = 0; j < BN; j += 32)
-        if (j + lane < BN) c[j + lane] = BROWS ? col_scale[slot][k][j + lane] : col_scale[slot][k][j + lane] * ls;
-      if (k == kScaleStep - 1 || i + 1 == nkb) {
+      for (int j0 = 0; j0 < T::kEpiCols; j0 += kCols) {
+        float v[kCols];
+        if constexpr (kCols == 16)
+          tmem_ld16(taddr + a * BN + j0, v);
+        else
+          tmem_ld32(taddr + a * BN + j0, v);
+        tmem_wait_ld();
+        if (j0 + kCols == T::kEpiCols) {   // all of this accumulator is in registers
+          tc_fence_before();
+          mbar_arrive_if(&acc_empty[a], lane == 0);
+        }
+#pragma unroll
+        for (int j = 0; j < kCols; j += 4) {
+          const float4 f = *reinterpret_cast<const float4*>(c + j0 + j);
+          fma_pair(acc[j0 + j], acc[j0 + j + 1], v[j] * ls, v[j + 1] * ls, f.x, f.y);
+          fma_pair(acc[j0 + j + 2], acc[j0 + j + 3], v[j + 2] * ls, v[j + 3] * ls, f.z, f.w);
+        }
+      }
+      if (k == kScaleStep - 1) {
         __syncwarp();
-        if (lane == 0) mbar_arrive(&sc_empty[slot]);
+        mbar_arrive_if(&sc_empty[slot], lane == 0);
         if (++slot == T::kScaleSlots) {
           slot = 0;
           slot_phase ^= 1u;
         }
       }
-      ok &= mbar_wait_bounded(&acc_full[a], a_phase, abort_flag, p.status);
-      __syncwarp();
-      tc_fence_after();
-      const uint32_t addr = tmem + ((uint32_t)(quarter * 32) << 16) + a * BN;
-      constexpr int kCols = BN < 32 ? 16 : 32;
-#pragma unroll
-      for (int j0 = 0; j0 < BN; j0 += kCols) {
-        float v[kCols];
-        if constexpr (kCols == 16)
-          tmem_ld16(addr + j0, v);
-        else
-          tmem_ld32(addr + j0, v);
-        tmem_wait_ld();
-        if (j0 + kCols == BN) {   // all of this accumulator is in registers
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(&acc_empty[a]);
-        }
-#pragma unroll
-        for (int j = 0; j < kCols; j += 4) {
-          const float4 f = *reinterpret_cast<const float4*>(c + j0 + j);
-          if constexpr (BROWS) {
-            fma_pair(acc[j0 + j], acc[j0 + j + 1], v[j] * f.x, v[j + 1] * f.y, ls, ls);
-            fma_pair(acc[j0 + j + 2], acc[j0 + j + 3], v[j + 2] * f.z, v[j + 3] * f.w, ls, ls);
-          } else {
-            fma_pair(acc[j0 + j], acc[j0 + j + 1], v[j], v[j + 1], f.x, f.y);
-            fma_pair(acc[j0 + j + 2], acc[j0 + j + 3], v[j + 2], v[j + 3], f.z, f.w);
-          }
-        }
-      }
     }
     if (p.splits == 1 && ok && n_in) {
 #pragma unroll
-      for (int j = 0; j < BN; ++j)
-        if (m0 + j < p.M) store_out(p.d, p.out, (uint64_t)(m0 + j) * p.ldd + n, acc[j]);
+      for (int j = 0; j < T::kEpiCols; ++j)
+        if (m0 + col0 + j < p.M) store_out(p.d, p.out, (uint64_t)(m0 + col0 + j) * p.ldd + n, acc[j]);
     }
     if (p.splits > 1) {
       // all copies and matrix instructions of this CTA are done: the ring holds the partial sums
-      float* red = reinterpret_cast<float*>(stages) + quarter * 32 + lane;
+      float* red = reinterpret_cast<float*>(stages) + col0 * 128 + quarter * 32 + lane;
 #pragma unroll
-      for (int j = 0; j < BN; ++j) red[j * 128] = acc[j];
+      for (int j = 0; j < T::kEpiCols; ++j) red[j * 128] = acc[j];
     }
   }
   if (p.splits > 1) {
     cluster_sync_all();
-    if (warp >= 2 && warp < 6) {
+    if (warp >= 4) {
       const int row = (warp & 3) * 32 + lane;
       const uint32_t n = n0 + row;
       const uint32_t base = smem_u32(stages) + row * 4;
-      for (uint32_t j = BN * rank / p.splits; j < BN * (rank + 1) / p.splits; ++j) {
+      for (uint32_t j = BN * rank / p.splits + ((warp - 4) >> 2); j < BN * (rank + 1) / p.splits; j += T::kEpiWarps / 4) {
         if (m0 + j >= p.M) break;
         float s = 0.0f;
         for (uint32_t r = 0; r < p.splits; ++r) s += ld_cluster_f32(map_to_rank(base + j * 512, r));
@@ -470,30 +458,33 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PairTile::kThreads, 
     // Matrix instructions: one thread takes the even K blocks and their accumulator, another the
     // odd ones, so that what a thread spends on its waits hides under the other's products.
     const uint32_t a = warp >> 1;
-    if (lane == 0 && rank == 0) {
-      uint32_t it = 0;
+    if (rank == 0) {
       const uint32_t nkb = tiles > first ? ((tiles - first + step - 1) / step) * p.KB : 0;
-      for (it = a; it < nkb; it += 2) {
-        const uint32_t st = it % T::kStages;
-        if (!mbar_wait_bounded(&full[st], (it / T::kStages) & 1u, abort_flag, p.status) ||
-            !mbar_wait_bounded(&acc_empty[a], ((it >> 1) & 1u) ^ 1u, abort_flag, p.status)) {
+      uint32_t st = a, phase = 0, acc_phase = 1;   // stage a, a + 2, ... of the ring
+      for (uint32_t it = a; it < nkb; it += 2) {
+        const bool go = mbar_wait_bounded(&full[st], phase, abort_flag, p.status) &&
+                        mbar_wait_bounded(&acc_empty[a], acc_phase, abort_flag, p.status);
+        if (!__all_sync(0xFFFFFFFFu, go)) {
           // what has been issued ends before tensor memory is freed
           mma_commit_pair(&drained[a]);
           const unsigned long long t0 = global_ns();
           while (!mbar_try_wait(&drained[a], 0))
             if (global_ns() - t0 > 1000000000ull) break;
+          __syncwarp();
           break;
         }
         tc_fence_after();
         const uint32_t s = smem_u32(stages + st * T::kStageBytes);
-        const uint64_t a_desc = smem_desc_k128(s), b_desc = smem_desc_k128(s + T::kHalfBytes);
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-          mma_f8<2>(tmem + a * 256, a_desc + 2 * k, b_desc + 2 * k, p.idesc, k > 0);
+        mma_f8_block<2>(tmem + a * 256, smem_desc_k128(s), smem_desc_k128(s + T::kHalfBytes), p.idesc);
         mma_commit_pair(&done[st]);   // frees the stage and hands over the accumulator
+        acc_phase ^= 1u;
+        st += 2;
+        if (st >= T::kStages) {
+          st -= T::kStages;
+          phase ^= 1u;
+        }
       }
     }
-    __syncwarp();
   } else if (warp == 2) {
     // the scales of kScaleStep K blocks at a time, one or two steps ahead of their use
     uint32_t slot = 0, phase = 0;

@@ -71,34 +71,60 @@ __device__ __forceinline__ uint64_t smem_desc_k128(uint32_t smem_addr) {
 __host__ __device__ constexpr uint32_t mma_idesc_f8(bool a_e5m2, bool b_e5m2, uint32_t M, uint32_t N) {
   return (1u << 4) | ((a_e5m2 ? 1u : 0u) << 7) | ((b_e5m2 ? 1u : 0u) << 10) | ((N >> 3) << 17) | ((M >> 4) << 24);
 }
-// D (+)= A B^T for one step of 32 along K; issued by one thread
+// D = A B^T over one K block of 128 bytes (four steps of 32).  The whole warp calls it with equal
+// arguments and one thread of it issues: operands that are the same for the warp stay in uniform
+// registers, where a single thread's would have to be moved there for every instruction (250 cycles
+// per block instead of 60).
 template <int CG>
-__device__ __forceinline__ void mma_f8(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc,
-                                       bool accumulate) {
-  const uint32_t acc = accumulate ? 1u : 0u;
+__device__ __forceinline__ void mma_f8_block(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc) {
   if constexpr (CG == 1)
     asm volatile(
-        "{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\n"
-        "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n}" ::"r"(d_tmem),
-        "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(acc)
+        "{\n.reg .pred one, more;\n.reg .b64 a, b;\n"
+        "elect.sync _|one, 0xFFFFFFFF;\n"
+        "setp.ne.b32 more, 0, 0;\n"
+        "@one tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, more;\n"
+        "setp.eq.b32 more, 0, 0;\n"
+        "add.s64 a, %1, 2;\nadd.s64 b, %2, 2;\n"
+        "@one tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], a, b, %3, more;\n"
+        "setp.eq.b32 more, 0, 0;\n"
+        "add.s64 a, %1, 4;\nadd.s64 b, %2, 4;\n"
+        "@one tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], a, b, %3, more;\n"
+        "setp.eq.b32 more, 0, 0;\n"
+        "add.s64 a, %1, 6;\nadd.s64 b, %2, 6;\n"
+        "@one tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], a, b, %3, more;\n"
+        "}" ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc)
         : "memory");
   else
     asm volatile(
-        "{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\n"
-        "tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n}" ::"r"(d_tmem),
-        "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(acc)
+        "{\n.reg .pred one, more;\n.reg .b64 a, b;\n"
+        "elect.sync _|one, 0xFFFFFFFF;\n"
+        "setp.ne.b32 more, 0, 0;\n"
+        "@one tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, more;\n"
+        "setp.eq.b32 more, 0, 0;\n"
+        "add.s64 a, %1, 2;\nadd.s64 b, %2, 2;\n"
+        "@one tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], a, b, %3, more;\n"
+        "setp.eq.b32 more, 0, 0;\n"
+        "add.s64 a, %1, 4;\nadd.s64 b, %2, 4;\n"
+        "@one tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], a, b, %3, more;\n"
+        "setp.eq.b32 more, 0, 0;\n"
+        "add.s64 a, %1, 6;\nadd.s64 b, %2, 6;\n"
+        "@one tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], a, b, %3, more;\n"
+        "}" ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc)
         : "memory");
 }
-// The barrier gets one arrival when all matrix instructions this thread has issued are done.
+// The barrier gets one arrival when all matrix instructions of this warp's issuing thread are done
+// (whole warp; the same thread is elected every time).
 __device__ __forceinline__ void mma_commit(uint64_t* bar) {
-  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar))
-               : "memory");
+  asm volatile(
+      "{\n.reg .pred one;\nelect.sync _|one, 0xFFFFFFFF;\n"
+      "@one tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}" ::"r"(smem_u32(bar))
+      : "memory");
 }
-
 // The same for a pair of CTAs: one arrival on the barrier at this place in both of them.
 __device__ __forceinline__ void mma_commit_pair(uint64_t* bar) {
   asm volatile(
-      "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(
+      "{\n.reg .pred one;\nelect.sync _|one, 0xFFFFFFFF;\n"
+      "@one tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;\n}" ::"r"(
           smem_u32(bar)),
       "h"((unsigned short)3)
       : "memory");
@@ -167,6 +193,13 @@ __device__ __forceinline__ void mbar_arrive_cluster_if(uint32_t cluster_bar, boo
       "{\n.reg .pred p;\nsetp.ne.u32 p, %1, 0;\n@p mbarrier.arrive.shared::cluster.b64 _, [%0];\n}" ::"r"(cluster_bar),
       "r"(yes ? 1u : 0u)
       : "memory");
+}
+
+// The same on a barrier of this CTA
+__device__ __forceinline__ void mbar_arrive_if(uint64_t* bar, bool yes) {
+  asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %1, 0;\n@p mbarrier.arrive.shared::cta.b64 _, [%0];\n}" ::"r"(smem_u32(bar)),
+               "r"(yes ? 1u : 0u)
+               : "memory");
 }
 
 // ---- small asynchronous copies -----------------------------------------------------------------
