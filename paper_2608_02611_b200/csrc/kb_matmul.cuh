@@ -64,10 +64,12 @@ constexpr uint32_t kScaleStep = 4;          // K blocks whose scales share a slo
 template <int BN>
 struct LaneTile {
   static constexpr uint32_t kStageBytes = (128 + BN) * 128;
-  static constexpr uint32_t kStages = BN == 128 ? 6 : BN == 64 ? 8 : 10;
+  static constexpr uint32_t kStages = BN == 128 ? 4 : BN == 64 ? 7 : 9;
   static constexpr uint32_t kAcc = BN == 128 ? 2 : 4;          // accumulators in tensor memory
   static constexpr uint32_t kTmemCols = kAcc * BN;
-  static constexpr uint32_t kSmem = 1024 + kStages * kStageBytes;
+  // the cluster's partial sums for this CTA's share of the columns, 8 CTAs at most
+  static constexpr uint32_t kSumBytes = (BN + 8) * 512;
+  static constexpr uint32_t kSmem = 1024 + kStages * kStageBytes + kSumBytes;
   static constexpr uint32_t kScaleSlots = 4;
   static constexpr int kEpiWarps = BN >= 64 ? 8 : 4;           // each adds 32 rows x kEpiCols columns
   static constexpr int kEpiCols = BN / (kEpiWarps / 4);
@@ -92,7 +94,7 @@ __global__ void __launch_bounds__(LaneTile<BN>::kThreads, 1)
   extern __shared__ unsigned char dyn[];
   __shared__ uint64_t full[T::kStages], empty[T::kStages], acc_full[T::kAcc], acc_empty[T::kAcc], drained;
   __shared__ uint64_t sc_full[T::kScaleSlots], sc_empty[T::kScaleSlots];
-  __shared__ uint32_t tmem_base;
+  __shared__ uint32_t tmem_base, first_col[9];
   __shared__ unsigned int abort_word;
   __shared__ float lane_scale[T::kScaleSlots][kScaleStep][BROWS ? 128 : 1];
   __shared__ __align__(16) float col_scale[T::kScaleSlots][kScaleStep][BN];
@@ -122,6 +124,9 @@ __global__ void __launch_bounds__(LaneTile<BN>::kThreads, 1)
     abort_word = 0u;
     mbar_fence_init();
   }
+  // CTA o of the cluster finishes the columns from first_col[o] on: those with floor(c * splits / BN) = o
+  if (warp == 2 && lane < 9) first_col[lane] = (BN * lane + p.splits - 1) / p.splits;
+  if (p.splits > 1) cluster_arrive();   // "this CTA runs": waited for before the first write to another's memory
   if (warp == 1) tmem_alloc<1>(&tmem_base, T::kTmemCols);
   tc_fence_before();
   __syncthreads();
@@ -131,25 +136,24 @@ __global__ void __launch_bounds__(LaneTile<BN>::kThreads, 1)
   float acc[T::kEpiCols];
   bool ok = true;
   if (warp == 0) {
-    if (lane == 0) {
-      uint32_t st = 0, phase = 0, issued = 0;
-      for (uint32_t i = 0; i < nkb; ++i) {
-        if (!mbar_wait_bounded(&empty[st], phase ^ 1u, abort_flag, p.status)) {
-          drain_copies(full, T::kStages, issued);
-          break;
-        }
-        unsigned char* s = stages + st * T::kStageBytes;
-        mbar_arrive_expect_tx(&full[st], T::kStageBytes);
-        tma_load_2d(s, &map_b, (int)((kb0 + i) * 128), (int)n0, &full[st]);
-        tma_load_2d(s + 128 * 128, &map_a, (int)((kb0 + i) * 128), (int)m0, &full[st]);
-        ++issued;
-        if (++st == T::kStages) {
-          st = 0;
-          phase ^= 1u;
-        }
+    uint32_t st = 0, phase = 0, issued = 0;
+    for (uint32_t i = 0; i < nkb; ++i) {
+      if (!__all_sync(0xFFFFFFFFu, mbar_wait_bounded(&empty[st], phase ^ 1u, abort_flag, p.status))) {
+        drain_copies(full, T::kStages, issued);
+        __syncwarp();
+        break;
+      }
+      const uint32_t s = smem_u32(stages + st * T::kStageBytes), bar = smem_u32(&full[st]);
+      const int x = (int)((kb0 + i) * 128);
+      expect_tx_elect(bar, T::kStageBytes);
+      tma_load_2d(s, &map_b, x, (int)n0, bar);
+      tma_load_2d(s + 128 * 128, &map_a, x, (int)m0, bar);
+      ++issued;
+      if (++st == T::kStages) {
+        st = 0;
+        phase ^= 1u;
       }
     }
-    __syncwarp();
   } else if (warp == 1) {
     uint32_t st = 0, phase = 0;
     for (uint32_t i = 0; i < nkb; ++i) {
@@ -260,27 +264,48 @@ __global__ void __launch_bounds__(LaneTile<BN>::kThreads, 1)
       for (int j = 0; j < T::kEpiCols; ++j)
         if (m0 + col0 + j < p.M) store_out(p.d, p.out, (uint64_t)(m0 + col0 + j) * p.ldd + n, acc[j]);
     }
-    if (p.splits > 1) {
-      // all copies and matrix instructions of this CTA are done: the ring holds the partial sums
-      float* red = reinterpret_cast<float*>(stages) + col0 * 128 + quarter * 32 + lane;
-#pragma unroll
-      for (int j = 0; j < T::kEpiCols; ++j) red[j * 128] = acc[j];
-    }
   }
   if (p.splits > 1) {
-    cluster_sync_all();
+    // The cluster adds its partial sums: each CTA owns a share of the tile's columns and gets every
+    // CTA's sums for them written into its shared memory, then adds them in rank order.
+    cluster_wait();
+    const uint32_t share = (BN + p.splits - 1) / p.splits;       // places per CTA and owner
+    const uint32_t row = (warp & 3) * 32 + lane;
+    unsigned char* sum_buf = stages + T::kStages * T::kStageBytes;
     if (warp >= 4) {
-      const int row = (warp & 3) * 32 + lane;
-      const uint32_t n = n0 + row;
-      const uint32_t base = smem_u32(stages) + row * 4;
-      for (uint32_t j = BN * rank / p.splits + ((warp - 4) >> 2); j < BN * (rank + 1) / p.splits; j += T::kEpiWarps / 4) {
-        if (m0 + j >= p.M) break;
-        float s = 0.0f;
-        for (uint32_t r = 0; r < p.splits; ++r) s += ld_cluster_f32(map_to_rank(base + j * 512, r));
-        if (n < p.N && ok) store_out(p.d, p.out, (uint64_t)(m0 + j) * p.ldd + n, s);
+      const uint32_t col0 = ((warp - 4) >> 2) * T::kEpiCols;
+      const uint32_t mine = smem_u32(sum_buf) + (rank * share * 128 + row) * 4;
+      uint32_t owner = col0 * p.splits / BN, next = first_col[owner + 1];
+      uint32_t at = map_to_rank(mine, owner) + (col0 - first_col[owner]) * 512;
+#pragma unroll
+      for (uint32_t j = 0; j < T::kEpiCols; ++j, at += 512) {
+        if (col0 + j == next) {
+          next = first_col[++owner + 1];
+          at = map_to_rank(mine, owner);
+        }
+        if (m0 + col0 + j < p.M) st_cluster_f32(at, acc[j]);
       }
     }
-    cluster_sync_all();   // no CTA leaves while another reads its shared memory
+    cluster_sync_all();
+    if (warp >= 4 && ok && n0 + row < p.N) {
+      const uint32_t first = first_col[rank];
+      const uint32_t last = min(first_col[rank + 1], p.M - m0);
+      const float* sums = reinterpret_cast<const float*>(sum_buf) + row;
+      for (uint32_t c = first + ((warp - 4) >> 2) * 4; c < last; c += T::kEpiWarps) {   // 4 columns at a time
+        float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (uint32_t r = 0; r < 8; ++r) {
+          if (r < p.splits) {
+#pragma unroll
+            for (uint32_t k = 0; k < 4; ++k)
+              if (c + k < last) v[k] += sums[(r * share + c + k - first) * 128];
+          }
+        }
+#pragma unroll
+        for (uint32_t k = 0; k < 4; ++k)
+          if (c + k < last) store_out(p.d, p.out, (uint64_t)(m0 + c + k) * p.ldd + n0 + row, v[k]);
+      }
+    }
   }
   tc_fence_before();
   __syncthreads();
@@ -419,41 +444,37 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PairTile::kThreads, 
 
   if (warp < 4) regs_shrink<T::kRegsControl>();
   if (warp == 0) {
-    if (lane == 0) {
-      uint32_t st = 0, phase = 0;
-      uint64_t issued = 0;
-      bool ok = true;
-      for (uint32_t t = first; t < tiles && ok; t += step) {
-        uint32_t tm, tn;
-        pair_tile(t, p.tiles_m, tiles_n, tm, tn);
-        const int ya = (int)(tm * 256 + rank * 128), yb = (int)(tn * 256 + rank * 128);
-        for (uint32_t kb = 0; kb < p.KB; ++kb) {
-          if (!mbar_wait_bounded(&done[st], phase ^ 1u, abort_flag, p.status)) {
-            ok = false;
-            break;
-          }
-          unsigned char* s = stages + st * T::kStageBytes;
-          const uint32_t bar = map_to_rank(smem_u32(&full[st]), 0);
-          if (rank == 0) mbar_arrive_expect_tx(&full[st], 2 * T::kStageBytes);
-          tma_load_2d_pair(s, &map_a, (int)(kb * 128), ya, bar);
-          tma_load_2d_pair(s + T::kHalfBytes, &map_b, (int)(kb * 128), yb, bar);
-          ++issued;
-          if (++st == T::kStages) {
-            st = 0;
-            phase ^= 1u;
-          }
-        }
-      }
-      if (!ok) {
-        // let the copies in flight land: the first CTA's barriers count both CTAs' bytes, the
-        // second CTA cannot see them and waits far longer than a copy takes
-        if (rank == 0) drain_copies(full, T::kStages, issued);
-        const unsigned long long t0 = global_ns();
-        while (global_ns() - t0 < 20000000ull) {
+    uint32_t st = 0, phase = 0;
+    uint64_t issued = 0;
+    bool go = true;
+    for (uint32_t t = first; t < tiles && go; t += step) {
+      uint32_t tm, tn;
+      pair_tile(t, p.tiles_m, tiles_n, tm, tn);
+      const int ya = (int)(tm * 256 + rank * 128), yb = (int)(tn * 256 + rank * 128);
+      for (uint32_t kb = 0; kb < p.KB; ++kb) {
+        go = __all_sync(0xFFFFFFFFu, mbar_wait_bounded(&done[st], phase ^ 1u, abort_flag, p.status));
+        if (!go) break;
+        const uint32_t s = smem_u32(stages + st * T::kStageBytes);
+        const uint32_t bar = map_to_rank(smem_u32(&full[st]), 0);
+        if (rank == 0) expect_tx_elect(smem_u32(&full[st]), 2 * T::kStageBytes);
+        tma_load_2d_pair(s, &map_a, (int)(kb * 128), ya, bar);
+        tma_load_2d_pair(s + T::kHalfBytes, &map_b, (int)(kb * 128), yb, bar);
+        ++issued;
+        if (++st == T::kStages) {
+          st = 0;
+          phase ^= 1u;
         }
       }
     }
-    __syncwarp();
+    if (!go) {
+      // let the copies in flight land: the first CTA's barriers count both CTAs' bytes, the
+      // second CTA cannot see them and waits far longer than a copy takes
+      if (rank == 0) drain_copies(full, T::kStages, issued);
+      const unsigned long long t0 = global_ns();
+      while (global_ns() - t0 < 20000000ull) {
+      }
+      __syncwarp();
+    }
   } else if (warp == 1 || warp == 3) {
     // Matrix instructions: one thread takes the even K blocks and their accumulator, another the
     // odd ones, so that what a thread spends on its waits hides under the other's products.

@@ -131,25 +131,33 @@ __device__ __forceinline__ void mma_commit_pair(uint64_t* bar) {
 }
 
 // ---- tensor-map copies -----------------------------------------------------------------------
+// Called by a whole warp with equal arguments, like the matrix instructions above; one thread issues.
 // 2-D box of a row-major matrix to this CTA's shared memory; x (bytes here) is a multiple of 16.
-__device__ __forceinline__ void tma_load_2d(void* dst_smem, const CUtensorMap* map, int x, int y, uint64_t* bar) {
+__device__ __forceinline__ void tma_load_2d(uint32_t dst_smem, const CUtensorMap* map, int x, int y, uint32_t bar) {
   asm volatile(
-      "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes "
-      "[%0], [%1, {%2, %3}], [%4];" ::"r"(smem_u32(dst_smem)),
-      "l"(map), "r"(x), "r"(y), "r"(smem_u32(bar))
+      "{\n.reg .pred one;\nelect.sync _|one, 0xFFFFFFFF;\n"
+      "@one cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes "
+      "[%0], [%1, {%2, %3}], [%4];\n}" ::"r"(dst_smem),
+      "l"(map), "r"(x), "r"(y), "r"(bar)
       : "memory");
 }
 // The same by a CTA of a pair; the bytes count on a barrier of either CTA (a cluster address).
-__device__ __forceinline__ void tma_load_2d_pair(void* dst_smem, const CUtensorMap* map, int x, int y,
+__device__ __forceinline__ void tma_load_2d_pair(uint32_t dst_smem, const CUtensorMap* map, int x, int y,
                                                  uint32_t cluster_bar) {
   asm volatile(
-      "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes "
-      "[%0], [%1, {%2, %3}], [%4];" ::"r"(smem_u32(dst_smem)),
+      "{\n.reg .pred one;\nelect.sync _|one, 0xFFFFFFFF;\n"
+      "@one cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes "
+      "[%0], [%1, {%2, %3}], [%4];\n}" ::"r"(dst_smem),
       "l"(map), "r"(x), "r"(y), "r"(cluster_bar)
       : "memory");
 }
-__device__ __forceinline__ void tma_prefetch_map(const CUtensorMap* map) {
-  asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
+// Announces bytes on a barrier of this CTA (whole warp, one arrival)
+__device__ __forceinline__ void expect_tx_elect(uint32_t bar, uint32_t bytes) {
+  asm volatile(
+      "{\n.reg .pred one;\nelect.sync _|one, 0xFFFFFFFF;\n"
+      "@one mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n}" ::"r"(bar),
+      "r"(bytes)
+      : "memory");
 }
 
 // ---- registers ---------------------------------------------------------------------------------
@@ -173,15 +181,19 @@ __device__ __forceinline__ uint32_t cluster_rank() {
 __device__ __forceinline__ void cluster_sync_all() {
   asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
+__device__ __forceinline__ void cluster_arrive() {
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void cluster_wait() {
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
 __device__ __forceinline__ uint32_t map_to_rank(uint32_t smem_addr, uint32_t rank) {
   uint32_t r;
   asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(smem_addr), "r"(rank));
   return r;
 }
-__device__ __forceinline__ float ld_cluster_f32(uint32_t addr) {
-  float v;
-  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
-  return v;
+__device__ __forceinline__ void st_cluster_f32(uint32_t addr, float v) {
+  asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory");
 }
 
 // Arrival on a barrier of any CTA of the cluster.  No cluster-wide release (which would wait for
