@@ -34,13 +34,24 @@ struct MatmulParams {
   unsigned int* status;
 };
 
-__device__ __forceinline__ void store_out(void* d, int out, uint64_t i, float v) {
-  if (out == KB_BF16)
-    store_elem<KB_BF16>(d, i, v);
-  else if (out == KB_F16)
-    store_elem<KB_F16>(d, i, v);
+// v[0..n) to column `col` of the rows row0, row0 + 1, ... of D, where they exist
+template <int DT, int N>
+__device__ __forceinline__ void store_down(const MatmulParams& p, uint32_t row0, uint32_t col, const float* v) {
+  constexpr int kBytes = DT == KB_F32 ? 4 : 2;
+  unsigned char* at = static_cast<unsigned char*>(p.d) + ((uint64_t)row0 * p.ldd + col) * kBytes;
+  const uint64_t step = p.ldd * kBytes;
+#pragma unroll
+  for (int j = 0; j < N; ++j, at += step)
+    if (row0 + j < p.M) store_elem<DT>(at, 0, v[j]);
+}
+template <int N>
+__device__ __forceinline__ void store_down(const MatmulParams& p, uint32_t row0, uint32_t col, const float* v) {
+  if (p.out == KB_BF16)
+    store_down<KB_BF16, N>(p, row0, col, v);
+  else if (p.out == KB_F16)
+    store_down<KB_F16, N>(p, row0, col, v);
   else
-    store_elem<KB_F32>(d, i, v);
+    store_down<KB_F32, N>(p, row0, col, v);
 }
 
 // After a wait has run out: let the copies already issued land, for a second at most.
@@ -64,11 +75,13 @@ constexpr uint32_t kScaleStep = 4;          // K blocks whose scales share a slo
 template <int BN>
 struct LaneTile {
   static constexpr uint32_t kStageBytes = (128 + BN) * 128;
-  static constexpr uint32_t kStages = BN == 128 ? 4 : BN == 64 ? 7 : 9;
+  static constexpr uint32_t kStages = BN == 128 ? 4 : BN == 64 ? 6 : 9;
   static constexpr uint32_t kAcc = BN == 128 ? 2 : 4;          // accumulators in tensor memory
   static constexpr uint32_t kTmemCols = kAcc * BN;
   // the cluster's partial sums for this CTA's share of the columns, 8 CTAs at most
-  static constexpr uint32_t kSumBytes = (BN + 8) * 512;
+  // (in groups of 4 columns: 16 bytes per row)
+  static constexpr uint32_t kGroups = BN / 4;
+  static constexpr uint32_t kSumBytes = (kGroups + 8) * 2048;
   static constexpr uint32_t kSmem = 1024 + kStages * kStageBytes + kSumBytes;
   static constexpr uint32_t kScaleSlots = 4;
   static constexpr int kEpiWarps = BN >= 64 ? 8 : 4;           // each adds 32 rows x kEpiCols columns
@@ -94,7 +107,7 @@ __global__ void __launch_bounds__(LaneTile<BN>::kThreads, 1)
   extern __shared__ unsigned char dyn[];
   __shared__ uint64_t full[T::kStages], empty[T::kStages], acc_full[T::kAcc], acc_empty[T::kAcc], drained;
   __shared__ uint64_t sc_full[T::kScaleSlots], sc_empty[T::kScaleSlots];
-  __shared__ uint32_t tmem_base, first_col[9];
+  __shared__ uint32_t tmem_base, first_group[9];
   __shared__ unsigned int abort_word;
   __shared__ float lane_scale[T::kScaleSlots][kScaleStep][BROWS ? 128 : 1];
   __shared__ __align__(16) float col_scale[T::kScaleSlots][kScaleStep][BN];
@@ -124,8 +137,9 @@ __global__ void __launch_bounds__(LaneTile<BN>::kThreads, 1)
     abort_word = 0u;
     mbar_fence_init();
   }
-  // CTA o of the cluster finishes the columns from first_col[o] on: those with floor(c * splits / BN) = o
-  if (warp == 2 && lane < 9) first_col[lane] = (BN * lane + p.splits - 1) / p.splits;
+  // CTA o of the cluster finishes the groups of columns from first_group[o] on: those with
+  // floor(g * splits / kGroups) = o
+  if (warp == 2 && lane < 9) first_group[lane] = (T::kGroups * lane + p.splits - 1) / p.splits;
   if (p.splits > 1) cluster_arrive();   // "this CTA runs": waited for before the first write to another's memory
   if (warp == 1) tmem_alloc<1>(&tmem_base, T::kTmemCols);
   tc_fence_before();
@@ -259,51 +273,46 @@ __global__ void __launch_bounds__(LaneTile<BN>::kThreads, 1)
         }
       }
     }
-    if (p.splits == 1 && ok && n_in) {
-#pragma unroll
-      for (int j = 0; j < T::kEpiCols; ++j)
-        if (m0 + col0 + j < p.M) store_out(p.d, p.out, (uint64_t)(m0 + col0 + j) * p.ldd + n, acc[j]);
-    }
+    if (p.splits == 1 && ok && n_in) store_down<T::kEpiCols>(p, m0 + col0, n, acc);
   }
   if (p.splits > 1) {
     // The cluster adds its partial sums: each CTA owns a share of the tile's columns and gets every
     // CTA's sums for them written into its shared memory, then adds them in rank order.
     cluster_wait();
-    const uint32_t share = (BN + p.splits - 1) / p.splits;       // places per CTA and owner
+    const uint32_t share = (T::kGroups + p.splits - 1) / p.splits;       // places per CTA and owner
     const uint32_t row = (warp & 3) * 32 + lane;
     unsigned char* sum_buf = stages + T::kStages * T::kStageBytes;
     if (warp >= 4) {
-      const uint32_t col0 = ((warp - 4) >> 2) * T::kEpiCols;
-      const uint32_t mine = smem_u32(sum_buf) + (rank * share * 128 + row) * 4;
-      uint32_t owner = col0 * p.splits / BN, next = first_col[owner + 1];
-      uint32_t at = map_to_rank(mine, owner) + (col0 - first_col[owner]) * 512;
+      const uint32_t g0 = ((warp - 4) >> 2) * (T::kEpiCols / 4);
+      const uint32_t mine = smem_u32(sum_buf) + (rank * share * 128 + row) * 16;
+      uint32_t owner = g0 * p.splits / T::kGroups, next = first_group[owner + 1];
+      uint32_t at = map_to_rank(mine, owner) + (g0 - first_group[owner]) * 2048;
 #pragma unroll
-      for (uint32_t j = 0; j < T::kEpiCols; ++j, at += 512) {
-        if (col0 + j == next) {
-          next = first_col[++owner + 1];
+      for (uint32_t g = 0; g < T::kEpiCols / 4; ++g, at += 2048) {
+        while (g0 + g == next) {   // more than once where an owner has no group
+          next = first_group[++owner + 1];
           at = map_to_rank(mine, owner);
         }
-        if (m0 + col0 + j < p.M) st_cluster_f32(at, acc[j]);
+        if (m0 + (g0 + g) * 4 < p.M) st_cluster_f32x4(at, acc[4 * g], acc[4 * g + 1], acc[4 * g + 2], acc[4 * g + 3]);
       }
     }
     cluster_sync_all();
     if (warp >= 4 && ok && n0 + row < p.N) {
-      const uint32_t first = first_col[rank];
-      const uint32_t last = min(first_col[rank + 1], p.M - m0);
-      const float* sums = reinterpret_cast<const float*>(sum_buf) + row;
-      for (uint32_t c = first + ((warp - 4) >> 2) * 4; c < last; c += T::kEpiWarps) {   // 4 columns at a time
+      const uint32_t first = first_group[rank], last = first_group[rank + 1];
+      const float4* sums = reinterpret_cast<const float4*>(sum_buf) + row;
+      for (uint32_t g = first + ((warp - 4) >> 2); g < last && m0 + 4 * g < p.M; g += T::kEpiWarps / 4) {
         float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (uint32_t r = 0; r < 8; ++r) {
           if (r < p.splits) {
-#pragma unroll
-            for (uint32_t k = 0; k < 4; ++k)
-              if (c + k < last) v[k] += sums[(r * share + c + k - first) * 128];
+            const float4 f = sums[(r * share + g - first) * 128];
+            v[0] += f.x;
+            v[1] += f.y;
+            v[2] += f.z;
+            v[3] += f.w;
           }
         }
-#pragma unroll
-        for (uint32_t k = 0; k < 4; ++k)
-          if (c + k < last) store_out(p.d, p.out, (uint64_t)(m0 + c + k) * p.ldd + n0 + row, v[k]);
+        store_down<4>(p, m0 + 4 * g, n0 + row, v);
       }
     }
   }

@@ -236,6 +236,24 @@ kb_status encode_map(kb_ctx* ctx, CUtensorMap* map, const void* p, uint64_t rows
   return KB_OK;
 }
 
+// CTAs per tile of matmul_lanes_kernel: as many as the card has room for, at least two K blocks
+// each, 8 at most (the portable cluster size).
+uint32_t lane_splits(const kb_ctx* ctx, uint64_t tiles, uint32_t KB) {
+  const uint32_t room = (uint32_t)std::max<uint64_t>(1, (uint64_t)ctx->sm_count / tiles);
+  return std::max(1u, std::min({room, KB / 2, 8u}));
+}
+// Which kernel takes more than 64 rows of A.  Measured per K block and CTA, long K: 0.43 us for a
+// 128 x 128 tile of matmul_lanes_kernel, 0.58 us for a 256 x 256 tile of a pair.  The pair does four
+// times the work in it but needs 74 tiles to fill the card and cannot share a tile's K blocks:
+// 256x8192x8192 27 us by lanes and 38 by pairs, 300x1000x2000 6.6 and 18, 512x8192x8192 55 and 38.
+bool lanes_are_faster(const kb_ctx* ctx, uint64_t M, uint64_t N, uint32_t KB) {
+  const uint64_t lane_tiles = ((M + 127) / 128) * ((N + 127) / 128), pair_tiles = ((M + 255) / 256) * ((N + 255) / 256);
+  const uint64_t sms = (uint64_t)ctx->sm_count, pairs = sms / 2, splits = lane_splits(ctx, lane_tiles, KB);
+  const double lanes = 0.43 * (double)((lane_tiles * splits + sms - 1) / sms) * (double)((KB + splits - 1) / splits);
+  const double by_pairs = 0.58 * (double)((pair_tiles + pairs - 1) / pairs) * (double)KB;
+  return lanes < by_pairs;
+}
+
 template <int BN>
 kb_status launch_lanes(kb_ctx* ctx, MatmulParams& p, const void* a, uint64_t lda, bool a_e5m2, const void* b,
                        uint64_t ldb, bool b_e5m2, uint64_t K, cudaStream_t st) {
@@ -245,10 +263,7 @@ kb_status launch_lanes(kb_ctx* ctx, MatmulParams& p, const void* a, uint64_t lda
   p.idesc = mma_idesc_f8(b_e5m2, a_e5m2, 128, BN);
   p.tiles_m = (p.M + BN - 1) / BN;
   const uint64_t tiles = (uint64_t)p.tiles_m * ((p.N + 127) / 128);
-  // as many CTAs per tile as the card has room for, at least two K blocks each, 8 at most (the
-  // portable cluster size)
-  const uint32_t room = (uint32_t)std::max<uint64_t>(1, (uint64_t)ctx->sm_count / tiles);
-  const uint32_t splits = std::max(1u, std::min({room, p.KB / 2, 8u}));
+  const uint32_t splits = lane_splits(ctx, tiles, p.KB);
   p.splits = splits;
   if (tiles * splits > 0x7FFFFFFFull) return fail(ctx, KB_ERR_UNSUPPORTED, "kb_matmul_blocks: more than 2^31 - 1 tiles");
   cudaLaunchConfig_t cfg = {};
@@ -498,6 +513,6 @@ extern "C" kb_status kb_matmul_blocks(kb_ctx* ctx, const void* d_a, uint64_t lda
   if (M <= 16) return launch_lanes<16>(ctx, p, d_a, lda, ae, d_b, ldb, be, K, st);
   if (M <= 32) return launch_lanes<32>(ctx, p, d_a, lda, ae, d_b, ldb, be, K, st);
   if (M <= 64) return launch_lanes<64>(ctx, p, d_a, lda, ae, d_b, ldb, be, K, st);
-  if (M > 256) return launch_pair(ctx, p, d_a, lda, ae, d_b, ldb, be, K, st);
+  if (!lanes_are_faster(ctx, M, N, p.KB)) return launch_pair(ctx, p, d_a, lda, ae, d_b, ldb, be, K, st);
   return launch_lanes<128>(ctx, p, d_a, lda, ae, d_b, ldb, be, K, st);
 }
