@@ -83,6 +83,7 @@ struct kb_ctx {
   unsigned char* ops_ws = nullptr;  // partial sums of the norm's parameter gradients
   size_t ops_ws_bytes = 0;
   void* encode_tiled = nullptr;     // the driver's tensor-map encoder, looked up at first use
+  int cluster_room[9] = {};         // clusters of n CTAs, one CTA per SM, that run at the same time
   bool ops_ready = false;           // shared-memory limits of the operators' kernels are raised
 };
 
