@@ -128,6 +128,15 @@ def _stream_ptr(device) -> int:
     return int(torch.cuda.current_stream(device).cuda_stream)
 
 
+# The current stream's handle without building a Stream object (2 us of the 5 us that a call for a
+# single token takes on the device).
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+def _stream_of(device) -> int:
+    return _raw_stream(device.index) if _raw_stream is not None else _stream_ptr(device)
+
+
 class Mask:
     """A fidelity mask over tiles of 2**log2_tile elements (owned by a Context)."""
 
@@ -613,15 +622,17 @@ def _rows(t: torch.Tensor, name: str, where: str, device) -> torch.Tensor:
         if t.dim() == 0 or not (t.is_contiguous() or t.numel() == 0):
             raise KbError(1, where, f"{name} must be 2-D or contiguous")
         t = t.view(t.numel() // t.shape[-1] if t.shape[-1] else 0, t.shape[-1])
-    rows, cols = t.shape
-    if (cols > 1 and t.stride(1) != 1) or (rows > 1 and t.stride(0) < cols):
-        raise KbError(1, where, f"the columns of {name} must be adjacent and its rows must not overlap")
+    if not t.is_contiguous():
+        rows, cols = t.shape
+        if (cols > 1 and t.stride(1) != 1) or (rows > 1 and t.stride(0) < cols):
+            raise KbError(1, where, f"the columns of {name} must be adjacent and its rows must not overlap")
     return t
 
 
 def _ld(t: torch.Tensor) -> int:
     """Row stride of a matrix; that of a single row is free (torch may report anything)."""
-    return max(t.stride(0), t.shape[1]) if t.shape[0] > 1 else (t.shape[1] + 15) // 16 * 16
+    rows, cols = t.shape
+    return max(t.stride(0), cols) if rows > 1 else (cols + 15) // 16 * 16
 
 
 def _codes(rows: int, cols: int, dtype: torch.dtype, device) -> torch.Tensor:
@@ -631,14 +642,12 @@ def _codes(rows: int, cols: int, dtype: torch.dtype, device) -> torch.Tensor:
     return torch.empty((rows, (cols + 15) // 16 * 16), dtype=dtype, device=device)[:, :cols]
 
 
-def _vector(t: Optional[torch.Tensor], n: int, name: str, where: str, device, dtypes):
-    """(address, dtype) of an optional contiguous vector of n elements."""
-    if t is None:
-        return None, None
-    if t.numel() != n or not t.is_contiguous() or t.device != device or t.dtype not in dtypes:
+def _vector(t: torch.Tensor, n: int, name: str, where: str, device, *dtypes) -> int:
+    """Address of a contiguous tensor of n elements."""
+    if t.numel() != n or t.dtype not in dtypes or t.device != device or not t.is_contiguous():
         raise KbError(1, where, f"{name} must be a contiguous tensor of {n} elements of "
                                 f"{' or '.join(str(d) for d in dtypes)} on {device}")
-    return t.data_ptr(), t.dtype
+    return t.data_ptr()
 
 
 @_ctx_method
@@ -659,7 +668,7 @@ def quantize_blocks(self, x: torch.Tensor, dtype: torch.dtype = torch.float8_e4m
     rc = load().kb_quantize_blocks(self._h, x.data_ptr(), rows, cols, _ld(x), DTYPE_CODE.get(x.dtype, -1),
                                    int(bool(transpose)), KB_SCALE_TILES if tiles else KB_SCALE_ROWS,
                                    q.data_ptr(), _ld(q), DTYPE_CODE.get(dtype, -1), scale.data_ptr(),
-                                   _stream_ptr(self.device))
+                                   _stream_of(self.device))
     self._check(rc, "kb_quantize_blocks")
     return q, scale
 
@@ -677,27 +686,29 @@ def layernorm(self, x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias
     where = "kb_layernorm"
     x2 = _rows(x, "x", where, self.device)
     rows, cols = x2.shape
-    kinds = (x.dtype, torch.float32)
-    w, wt = _vector(weight, cols, "weight", where, self.device, kinds)
-    b, bt = _vector(bias, cols, "bias", where, self.device, kinds)
-    if wt is not None and bt is not None and wt != bt:
+    dtype = x.dtype
+    w = _vector(weight, cols, "weight", where, self.device, dtype, torch.float32) if weight is not None else None
+    b = _vector(bias, cols, "bias", where, self.device, dtype, torch.float32) if bias is not None else None
+    params = weight.dtype if weight is not None else bias.dtype if bias is not None else dtype
+    if w is not None and b is not None and weight.dtype != bias.dtype:
         raise KbError(1, where, "weight and bias must have the same type")
-    y = torch.empty(x.shape, dtype=x.dtype, device=self.device) if want_y else None
+    y = torch.empty(x.shape, dtype=dtype, device=self.device) if want_y else None
     mean = rstd = q = scale = None
     if want_stats:
-        mean, rstd = torch.empty((2, rows), dtype=torch.float32, device=self.device).unbind(0)
+        mean = torch.empty(rows, dtype=torch.float32, device=self.device)
+        rstd = torch.empty(rows, dtype=torch.float32, device=self.device)
     if quantize is not None:
         q = _codes(rows, cols, quantize, self.device)
         scale = torch.empty((-(-cols // KB_BLOCK), rows), dtype=torch.float32, device=self.device)
     if rows == 0:
         return LayerNormResult(y, mean, rstd, q, scale)
-    rc = load().kb_layernorm(self._h, x2.data_ptr(), rows, cols, _ld(x2), DTYPE_CODE.get(x.dtype, -1), w, b,
-                             DTYPE_CODE.get(wt or bt or x.dtype, -1), float(eps),
+    rc = load().kb_layernorm(self._h, x2.data_ptr(), rows, cols, _ld(x2), DTYPE_CODE.get(dtype, -1), w, b,
+                             DTYPE_CODE.get(params, -1), float(eps),
                              y.data_ptr() if want_y else None, cols,
                              mean.data_ptr() if want_stats else None, rstd.data_ptr() if want_stats else None,
                              q.data_ptr() if q is not None else None, _ld(q) if q is not None else 0,
                              DTYPE_CODE.get(quantize, -1) if q is not None else KB_F8E4M3,
-                             scale.data_ptr() if q is not None else None, _stream_ptr(self.device))
+                             scale.data_ptr() if q is not None else None, _stream_of(self.device))
     self._check(rc, where)
     return LayerNormResult(y, mean, rstd, q, scale)
 
@@ -712,16 +723,17 @@ def layernorm_backward(self, dy: torch.Tensor, x: torch.Tensor, weight: Optional
     rows, cols = x2.shape
     if dy2.shape != x2.shape or dy.dtype != x.dtype:
         raise KbError(1, where, "dy must have the shape and type of x")
-    w, wt = _vector(weight, cols, "weight", where, self.device, (x.dtype, torch.float32))
-    m, _ = _vector(mean, rows, "mean", where, self.device, (torch.float32,))
-    r, _ = _vector(rstd, rows, "rstd", where, self.device, (torch.float32,))
+    w = _vector(weight, cols, "weight", where, self.device, x.dtype, torch.float32) if weight is not None else None
+    params = weight.dtype if weight is not None else torch.float32
+    m = _vector(mean, rows, "mean", where, self.device, torch.float32)
+    r = _vector(rstd, rows, "rstd", where, self.device, torch.float32)
     dx = torch.empty(x.shape, dtype=x.dtype, device=self.device)
-    dweight = torch.empty(cols, dtype=wt or torch.float32, device=self.device)
-    dbias = torch.empty(cols, dtype=wt or torch.float32, device=self.device) if want_bias else None
+    dweight = torch.empty(cols, dtype=params, device=self.device)
+    dbias = torch.empty(cols, dtype=params, device=self.device) if want_bias else None
     rc = load().kb_layernorm_backward(self._h, dy2.data_ptr(), _ld(dy2), x2.data_ptr(), _ld(x2), rows, cols,
-                                      DTYPE_CODE.get(x.dtype, -1), w, DTYPE_CODE.get(wt or torch.float32, -1), m, r,
+                                      DTYPE_CODE.get(x.dtype, -1), w, DTYPE_CODE.get(params, -1), m, r,
                                       dx.data_ptr(), cols, dweight.data_ptr(),
-                                      dbias.data_ptr() if want_bias else None, _stream_ptr(self.device))
+                                      dbias.data_ptr() if want_bias else None, _stream_of(self.device))
     self._check(rc, where)
     return dx, dweight, dbias
 
@@ -742,17 +754,17 @@ def matmul_blocks(self, a: torch.Tensor, a_scale: torch.Tensor, b: torch.Tensor,
     if Kb != K:
         raise KbError(1, where, f"a has {K} columns, b {Kb}")
     tiles = b_scale.shape != (kb, N)
-    sa, _ = _vector(a_scale, kb * M, "a_scale", where, self.device, (torch.float32,))
-    sb, _ = _vector(b_scale, kb * (-(-N // KB_BLOCK) if tiles else N), "b_scale", where, self.device, (torch.float32,))
-    if a_scale.shape != (kb, M) or b_scale.dim() != 2 or b_scale.shape[0] != kb:
+    if a_scale.shape != (kb, M) or (tiles and b_scale.shape != (kb, -(-N // KB_BLOCK))):
         raise KbError(1, where, "scales are laid out [ceil(K/128), rows] or [ceil(K/128), ceil(rows/128)]")
+    sa = _vector(a_scale, kb * M, "a_scale", where, self.device, torch.float32)
+    sb = _vector(b_scale, kb * (-(-N // KB_BLOCK) if tiles else N), "b_scale", where, self.device, torch.float32)
     if out is None:
         out = torch.empty((M, N), dtype=out_dtype, device=self.device)
     elif out.shape != (M, N) or _rows(out, "out", where, self.device) is not out:
         raise KbError(1, where, f"out must be a matrix [{M}, {N}]")
     rc = load().kb_matmul_blocks(self._h, a.data_ptr(), _ld(a), DTYPE_CODE.get(a.dtype, -1), sa, b.data_ptr(), _ld(b),
                                  DTYPE_CODE.get(b.dtype, -1), sb, KB_SCALE_TILES if tiles else KB_SCALE_ROWS, M, N, K,
-                                 out.data_ptr(), _ld(out), DTYPE_CODE.get(out.dtype, -1), _stream_ptr(self.device))
+                                 out.data_ptr(), _ld(out), DTYPE_CODE.get(out.dtype, -1), _stream_of(self.device))
     self._check(rc, where)
     return out
 
