@@ -133,6 +133,37 @@ __device__ __forceinline__ void load_params(const void* base, bool f32, uint32_t
   }
 }
 
+// ---- two binary32 values in one register pair: one instruction for two operations ------------------
+// (The norms are bound by the number of instructions beside memory.)
+using Pair = unsigned long long;
+__device__ __forceinline__ Pair pair(float lo, float hi) {
+  Pair r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ void unpair(Pair v, float& lo, float& hi) {
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v));
+}
+__device__ __forceinline__ float fold(Pair v) {
+  float lo, hi;
+  unpair(v, lo, hi);
+  return lo + hi;
+}
+__device__ __forceinline__ Pair add2(Pair a, Pair b) {
+  Pair r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ Pair mul2(Pair a, Pair b) {
+  Pair r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) {
+  Pair r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
 // ---- 8-bit quantisation ---------------------------------------------------------------------
 // The block's scale S = a / F and the factor F / a its elements are multiplied with, a >= 2^-100
 // (so that neither quotient leaves the normal range, whatever the block holds).

@@ -74,7 +74,10 @@ __device__ __forceinline__ void norm_emit(const NormParams& p, uint64_t row, uin
     load_params<DT, VEC>(p.weight, p.param_f32, g0 + i * gstep, lane, p.cols, 1.0f, w);
     load_params<DT, VEC>(p.bias, p.param_f32, g0 + i * gstep, lane, p.cols, 0.0f, b);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[i][j] = fmaf(v[i][j] * rstd, w[j], b[j]);
+    for (int j = 0; j < 8; j += 2) {
+      const Pair t = mul2(pair(v[i][j], v[i][j + 1]), pair(rstd, rstd));
+      unpair(fma2(t, pair(w[j], w[j + 1]), pair(b[j], b[j + 1])), v[i][j], v[i][j + 1]);
+    }
   }
   if (p.y) {
 #pragma unroll
@@ -90,7 +93,8 @@ __device__ __forceinline__ void norm_emit(const NormParams& p, uint64_t row, uin
 
 // A row per warp (WARP) or per CTA, NCH groups per warp in registers.
 template <int DT, int NCH, bool VEC, bool WARP, int Q>
-__global__ void __launch_bounds__(WARP ? 128 : NCH == 1 ? 1024 : 512) norm_kernel(const NormParams p) {
+__global__ void __launch_bounds__(WARP ? 128 : NCH == 1 ? 1024 : 512, WARP ? 8 : NCH == 1 ? 1 : 2)
+    norm_kernel(const NormParams p) {   // 64 registers: 32 warps share an SM
   __shared__ float red[2][32];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, nwarps = blockDim.x >> 5;
   const uint64_t row = WARP ? (uint64_t)blockIdx.x * 4 + warp : blockIdx.x;
@@ -99,23 +103,26 @@ __global__ void __launch_bounds__(WARP ? 128 : NCH == 1 ? 1024 : 512) norm_kerne
   float v[NCH][8];
 #pragma unroll
   for (int i = 0; i < NCH; ++i) load_group<DT, VEC>(p.x, row * p.ldx, g0 + i * gstep, lane, p.cols, v[i]);
-  float s = 0.0f;
+  Pair s2 = pair(0.0f, 0.0f);
 #pragma unroll
   for (int i = 0; i < NCH; ++i)
 #pragma unroll
-    for (int j = 0; j < 8; ++j) s += v[i][j];
+    for (int j = 0; j < 8; j += 2) s2 = add2(s2, pair(v[i][j], v[i][j + 1]));
+  const float s = fold(s2);
   const float n = (float)p.cols;
   const float mean = (WARP ? warp_sum(s) : cta_sum(s, red[0], warp, lane, nwarps)) / n;
-  float ss = 0.0f;
+  Pair ss2 = pair(0.0f, 0.0f);
 #pragma unroll
   for (int i = 0; i < NCH; ++i) {
     fill_tail<VEC>(g0 + i * gstep, lane, p.cols, mean, v[i]);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      v[i][j] -= mean;
-      ss = fmaf(v[i][j], v[i][j], ss);
+    for (int j = 0; j < 8; j += 2) {
+      const Pair d = add2(pair(v[i][j], v[i][j + 1]), pair(-mean, -mean));
+      ss2 = fma2(d, d, ss2);
+      unpair(d, v[i][j], v[i][j + 1]);
     }
   }
+  const float ss = fold(ss2);
   const float var = (WARP ? warp_sum(ss) : cta_sum(ss, red[1], warp, lane, nwarps)) / n;
   const float rstd = 1.0f / sqrtf(var + p.eps);
   norm_emit<DT, VEC, NCH, Q>(p, row, g0, gstep, lane, rstd, v);
@@ -207,8 +214,8 @@ __device__ __forceinline__ const unsigned char* row_ptr(const void* base, uint64
 // Backward, rows by warp (WARP) or by CTA, walking over the rows with the grid's stride.  RING
 // (VEC and CTA only): the rows of x and dy come through shared memory.
 template <int DT, int NCH, bool VEC, bool WARP, bool RING>
-__global__ void __launch_bounds__(WARP ? 128 : 512) norm_bwd_kernel(const NormBwdParams p) {
-  __shared__ float red[2][2][16];
+__global__ void __launch_bounds__(WARP ? 128 : NCH == 1 ? 768 : 512) norm_bwd_kernel(const NormBwdParams p) {
+  __shared__ float red[2][2][32];
   __shared__ uint64_t full[kRowRingStages];
   __shared__ unsigned int abort_word;
   extern __shared__ __align__(128) unsigned char dyn[];   // WARP: [2][cols] sums; RING: the ring
@@ -236,6 +243,13 @@ __global__ void __launch_bounds__(WARP ? 128 : 512) norm_bwd_kernel(const NormBw
   uint32_t slot = 0, phase = 0;
   int turn = 0;
   float next_mean = first < p.rows ? p.mean[first] : 0.0f, next_rstd = first < p.rows ? p.rstd[first] : 0.0f;
+  // without a ring, a CTA with one group per warp has the registers to read a row ahead
+  constexpr bool kAhead = !RING && !WARP && NCH == 1;
+  float xn[NCH][8], gn[NCH][8];
+  if (kAhead && first < p.rows) {
+    load_group<DT, VEC>(p.x, first * p.ldx, warp, lane, p.cols, xn[0]);
+    load_group<DT, VEC>(p.dy, first * p.lddy, warp, lane, p.cols, gn[0]);
+  }
   for (uint64_t row = first; row < p.rows; row += step, turn ^= 1) {
     float xh[NCH][8], g[NCH][8];
     const float mean = next_mean, rstd = next_rstd;
@@ -250,6 +264,17 @@ __global__ void __launch_bounds__(WARP ? 128 : 512) norm_bwd_kernel(const NormBw
         load_group<DT, true>(dyn + slot * p.slot_bytes, 0, i * nwarps + warp, lane, p.cols, xh[i], mean);
         load_group<DT, true>(dyn + slot * p.slot_bytes + p.slot_bytes / 2, 0, i * nwarps + warp, lane, p.cols, g[i]);
       }
+    } else if constexpr (kAhead) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        xh[0][j] = xn[0][j];
+        g[0][j] = gn[0][j];
+      }
+      fill_tail<VEC>(warp, lane, p.cols, mean, xh[0]);
+      if (row + step < p.rows) {
+        load_group<DT, VEC>(p.x, (row + step) * p.ldx, warp, lane, p.cols, xn[0]);
+        load_group<DT, VEC>(p.dy, (row + step) * p.lddy, warp, lane, p.cols, gn[0]);
+      }
     } else {
 #pragma unroll
       for (int i = 0; i < NCH; ++i) {
@@ -259,20 +284,22 @@ __global__ void __launch_bounds__(WARP ? 128 : 512) norm_bwd_kernel(const NormBw
     }
     // past the row's end dy is 0 and x is the mean, unless the mean is not finite: the sums of such
     // a row are not finite either, and no column past the end is ever written
-    float s1 = 0.0f, s2 = 0.0f;
+    Pair s1p = pair(0.0f, 0.0f), s2p = s1p;
 #pragma unroll
     for (int i = 0; i < NCH; ++i)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        xh[i][j] = (xh[i][j] - mean) * rstd;
-        dw[i][j] = fmaf(g[i][j], xh[i][j], dw[i][j]);
-        db[i][j] += g[i][j];
-        g[i][j] *= w[i][j];
-        s1 += g[i][j];
-        s2 = fmaf(g[i][j], xh[i][j], s2);
+      for (int j = 0; j < 8; j += 2) {
+        const Pair x = mul2(add2(pair(xh[i][j], xh[i][j + 1]), pair(-mean, -mean)), pair(rstd, rstd));
+        Pair gy = pair(g[i][j], g[i][j + 1]);
+        unpair(fma2(gy, x, pair(dw[i][j], dw[i][j + 1])), dw[i][j], dw[i][j + 1]);
+        unpair(add2(gy, pair(db[i][j], db[i][j + 1])), db[i][j], db[i][j + 1]);
+        gy = mul2(gy, pair(w[i][j], w[i][j + 1]));
+        s1p = add2(s1p, gy);
+        s2p = fma2(gy, x, s2p);
+        unpair(x, xh[i][j], xh[i][j + 1]);
+        unpair(gy, g[i][j], g[i][j + 1]);
       }
-    s1 = warp_sum(s1);
-    s2 = warp_sum(s2);
+    float s1 = warp_sum(fold(s1p)), s2 = warp_sum(fold(s2p));
     if constexpr (!WARP) {
       if (lane == 0) {
         red[turn][0][warp] = s1;
@@ -301,7 +328,10 @@ __global__ void __launch_bounds__(WARP ? 128 : 512) norm_bwd_kernel(const NormBw
       for (int i = 0; i < NCH; ++i) {
         float d[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) d[j] = rstd * (fmaf(-xh[i][j], s2, g[i][j]) - s1);
+        for (int j = 0; j < 8; j += 2) {
+          const Pair t = fma2(pair(xh[i][j], xh[i][j + 1]), pair(-s2, -s2), pair(g[i][j], g[i][j + 1]));
+          unpair(mul2(add2(t, pair(-s1, -s1)), pair(rstd, rstd)), d[j], d[j + 1]);
+        }
         store_group<DT, VEC>(p.dx, row * p.lddx, WARP ? i : i * nwarps + warp, lane, p.cols, d);
       }
     }
@@ -403,26 +433,36 @@ __global__ void __launch_bounds__(256) norm_bwd_cols_kernel(const NormBwdParams 
   }
 }
 
-// Sums of the partial rows per column, in a fixed order: 32 columns per CTA, each warp takes the
-// partial rows w, w + 32, ..., then the warps' sums are added in order.  blockIdx.y: dweight, dbias.
+// Sums of the partial rows per column, in a fixed order: 32 columns per CTA, each of 16 warps takes
+// the partial rows w, w + 16, ... with eight loads on their way, then the warps' sums are added in
+// order.  blockIdx.y: dweight, dbias.
+constexpr int kParamWarps = 16;
 template <int PT>
-__global__ void __launch_bounds__(1024) norm_param_kernel(const float* partial, uint32_t nparts, uint32_t cols,
-                                                          void* dweight, void* dbias) {
-  __shared__ float part[32][33];
+__global__ void __launch_bounds__(32 * kParamWarps) norm_param_kernel(const float* partial, uint32_t nparts,
+                                                                      uint32_t cols, void* dweight, void* dbias) {
+  __shared__ float part[kParamWarps][33];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const uint32_t c = blockIdx.x * 32 + lane;
-  const float* src = partial + (uint64_t)blockIdx.y * cols;
+  const float* src = partial + (uint64_t)blockIdx.y * cols + c;
   void* out = blockIdx.y ? dbias : dweight;
   if (out == nullptr) return;
   float s = 0.0f;
-  if (c < cols)
-    for (uint32_t i = warp; i < nparts; i += 32) s += src[(uint64_t)i * 2 * cols + c];
+  for (uint32_t i0 = warp; i0 < nparts; i0 += 8 * kParamWarps) {
+    float v[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const uint32_t i = i0 + k * kParamWarps;
+      v[k] = i < nparts && c < cols ? src[(uint64_t)i * 2 * cols] : 0.0f;
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) s += v[k];
+  }
   part[warp][lane] = s;
   __syncthreads();
   if (warp == 0 && c < cols) {
     float t = 0.0f;
 #pragma unroll
-    for (int w = 0; w < 32; ++w) t += part[w][lane];
+    for (int w = 0; w < kParamWarps; ++w) t += part[w][lane];
     store_elem<PT>(out, c, t);
   }
 }

@@ -97,7 +97,7 @@ int ctas_by_registers(unsigned int threads, int most) {
 }
 template <class K>
 kb_status ring_limits(kb_ctx* ctx, K kernel, size_t smem) {
-  if (smem > 48 * 1024)
+  if (smem > 40 * 1024)   // static and dynamic shared memory together: 48 KB without asking
     KB_CUDA(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
   return KB_OK;
 }
@@ -169,7 +169,10 @@ kb_status launch_norm_bwd(kb_ctx* ctx, NormBwdParams& p, uint32_t* nparts, cudaS
   if (g == 1) return launch_norm_bwd<DT, 1, VEC, true>(ctx, p, 128, nparts, st);
   if (g == 2) return launch_norm_bwd<DT, 2, VEC, true>(ctx, p, 128, nparts, st);
   if (g <= 4) return launch_norm_bwd<DT, 4, VEC, true>(ctx, p, 128, nparts, st);
-  if (g <= 16) return launch_norm_bwd<DT, 1, VEC, false>(ctx, p, 32 * g, nparts, st);
+  // one group per warp up to 16 warps; up to 24 where the rows are too few for the ring or cannot
+  // take it (777 x 5003 fp16: 19 us with two groups per warp, 14 with one and a row ahead)
+  const bool few = !VEC || p.rows < 2ull * ctx->sm_count;
+  if (g <= 16 || (g <= 24 && few)) return launch_norm_bwd<DT, 1, VEC, false>(ctx, p, 32 * g, nparts, st);
   if (g <= 32) return launch_norm_bwd<DT, 2, VEC, false>(ctx, p, 32 * ((g + 1) / 2), nparts, st);
   if (p.dx) {
     norm_bwd_long_kernel<DT, VEC><<<(unsigned int)p.rows, 512, 0, st>>>(p);
@@ -473,11 +476,11 @@ extern "C" kb_status kb_layernorm_backward(kb_ctx* ctx, const void* d_dy, uint64
   if (!p.want_param) return KB_OK;
   const dim3 grid((unsigned int)((cols + 31) / 32), 2);
   if (param_dtype == KB_F32)
-    norm_param_kernel<KB_F32><<<grid, 1024, 0, st>>>(p.partial, nparts, p.cols, d_dweight, d_dbias);
+    norm_param_kernel<KB_F32><<<grid, 32 * kParamWarps, 0, st>>>(p.partial, nparts, p.cols, d_dweight, d_dbias);
   else if (param_dtype == KB_F16)
-    norm_param_kernel<KB_F16><<<grid, 1024, 0, st>>>(p.partial, nparts, p.cols, d_dweight, d_dbias);
+    norm_param_kernel<KB_F16><<<grid, 32 * kParamWarps, 0, st>>>(p.partial, nparts, p.cols, d_dweight, d_dbias);
   else
-    norm_param_kernel<KB_BF16><<<grid, 1024, 0, st>>>(p.partial, nparts, p.cols, d_dweight, d_dbias);
+    norm_param_kernel<KB_BF16><<<grid, 32 * kParamWarps, 0, st>>>(p.partial, nparts, p.cols, d_dweight, d_dbias);
   return launched(ctx);
 }
 

@@ -211,6 +211,40 @@ def test_layernorm_against_64_bits(ctx, rows, cols, dtype):
         _within(r.y, y, bound * (1 + HALF_ULP[dtype]) + HALF_ULP[dtype] * y.abs() + TINY[dtype])
 
 
+@pytest.mark.parametrize("rows,cols,dtype", [(5000, 1032, torch.bfloat16), (4001, 4096, torch.bfloat16),
+                                             (3700, 2056, torch.float16), (1800, 8192, torch.float32),
+                                             (1500, 16384, torch.bfloat16)])
+def test_layernorm_and_backward_of_many_rows(ctx, rows, cols, dtype):
+    """Rows enough for the walks that read ahead, in matrices whose rows lie apart."""
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(rows)
+    held = torch.full((rows, cols + 8), float("nan"), device=DEV).to(dtype)
+    x = held[:, :cols]
+    x.copy_(torch.randn(rows, cols, generator=gen, device=DEV) + 2.0 * torch.randn(rows, 1, generator=gen, device=DEV))
+    w, b = (1.0 + 0.2 * torch.randn(cols, generator=gen, device=DEV)).to(dtype), torch.randn(cols, generator=gen, device=DEV).to(dtype)
+    r = ctx.layernorm(x, w, b, quantize=torch.float8_e4m3fn)
+    y, mean, rstd, xh = _norm64(x, w, b, 1e-5)
+    k = _chain(cols)
+    mean_err = (k + 2) * U * x.double().abs().mean(1) * rstd
+    rstd_err = (k + 8) * U + mean_err.square()
+    _within(r.rstd, rstd, rstd_err * rstd)
+    bound = w.double().abs() * (mean_err[:, None] + xh.abs() * (rstd_err[:, None] + 4 * U)) + 2 * U * (y.abs() + b.double().abs())
+    _within(r.y, y, bound * (1 + HALF_ULP[dtype]) + HALF_ULP[dtype] * y.abs() + TINY[dtype])
+    pad = -cols % 128
+    amax = torch.nn.functional.pad(y, (0, pad)).abs().view(rows, -1, 128).amax(2).t()
+    _within(r.scale, amax / 448.0, 2.0 ** -14 * amax / 448.0)
+    s = r.scale.double().t().repeat_interleave(128, 1)[:, :cols]
+    _within(r.q.double() * s, y, (2.0 ** -4 * y.abs() + 2.0 ** -10 * s) * 1.001 + 1e-4)
+    dy = (0.1 * torch.randn(rows, cols, generator=gen, device=DEV)).to(dtype)
+    dx, dw, db = ctx.layernorm_backward(dy, x, w, r.mean, r.rstd)
+    want_dx, want_dw, want_db, xh, g = _bwd64(dy, x, w, r.mean, r.rstd)
+    bound = r.rstd.double()[:, None] * ((k + 8) * U * (g.abs().mean(1, keepdim=True) + xh.abs() * (g * xh).abs().mean(1, keepdim=True)) + 8 * U * g.abs())
+    _within(dx, want_dx, 1.01 * bound + HALF_ULP[dtype] * want_dx.abs() + TINY[dtype])
+    rk = 128 + rows
+    _within(dw, want_dw, 1.01 * rk * U * (dy.double() * xh).abs().sum(0) + HALF_ULP[dtype] * want_dw.abs() + TINY[dtype])
+    _within(db, want_db, 1.01 * rk * U * dy.double().abs().sum(0) + HALF_ULP[dtype] * want_db.abs() + TINY[dtype])
+
+
 @pytest.mark.parametrize("gap,offset", [(8, 0), (1, 0), (0, 1), (5, 3)])
 def test_layernorm_of_strided_and_unaligned_rows(ctx, gap, offset):
     for dtype in FLOATS:
