@@ -13,7 +13,7 @@
  * and host thread at a time.  Every output is a pure function of the inputs (sums have a fixed
  * order).  In addition:
  *   - Matrices are row-major.  A leading dimension (ld...) counts elements and is at least the
- *     number of columns; the gap between rows is neither read nor written.
+ *     number of columns; the gap between rows is not written and what it holds does not matter.
  *   - Zero rows are allowed: nothing is written, except that sums over no row are zero.
  *   - Inputs and outputs of one call do not overlap.
  *   - Pointers need their element type's alignment; 16-byte aligned pointers and rows are

@@ -70,6 +70,59 @@ __device__ __forceinline__ void store8(void* p, uint64_t i, const float (&v)[8])
   }
 }
 
+// The n (1..8) elements from element i on, of a matrix that holds `span` elements from `base` (its gaps
+// between rows included), as raw words with zeros after the n; E bytes per element, any alignment.
+// Where a granule reaches past the matrix's ends the elements are read one by one.
+template <int E>
+__device__ __forceinline__ void load_shifted(const void* base, uint64_t span, uint64_t i, int n, uint32_t (&w)[2 * E]) {
+  constexpr int kGranules = E / 2 + 1;         // 16-byte granules that 8 elements can lie in
+  const uintptr_t first = reinterpret_cast<uintptr_t>(base), at = first + i * E, from = at & ~(uintptr_t)15;
+  if (from >= first && from + 16 * kGranules <= first + span * E) {
+    uint32_t u[4 * kGranules];
+#pragma unroll
+    for (int k = 0; k < kGranules; ++k) {
+      const uint4 t = *reinterpret_cast<const uint4*>(from + 16 * k);
+      u[4 * k] = t.x;
+      u[4 * k + 1] = t.y;
+      u[4 * k + 2] = t.z;
+      u[4 * k + 3] = t.w;
+    }
+    const uint32_t off = (uint32_t)(at & 15);
+    constexpr int kWords = 2 * E + (E == 2 ? 1 : 0);   // words that still matter after the word shifts
+#pragma unroll
+    for (int k = 0; k < kWords + 1; ++k) u[k] = (off & 8) && k + 2 < 4 * kGranules ? u[k + 2] : u[k];
+#pragma unroll
+    for (int k = 0; k < kWords; ++k) u[k] = (off & 4) ? u[k + 1] : u[k];
+#pragma unroll
+    for (int k = 0; k < 2 * E; ++k) {
+      if constexpr (E == 2)
+        w[k] = (off & 2) ? __funnelshift_r(u[k], u[k + 1], 16) : u[k];
+      else
+        w[k] = u[k];
+    }
+    if (n < 8) {
+#pragma unroll
+      for (int k = 0; k < 2 * E; ++k) {
+        if constexpr (E == 2)
+          w[k] = 2 * k + 1 < n ? w[k] : 2 * k < n ? w[k] & 0xFFFFu : 0u;
+        else
+          w[k] = k < n ? w[k] : 0u;
+      }
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < 2 * E; ++k) w[k] = 0u;
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (j < n) {
+        if constexpr (E == 2)
+          w[j >> 1] |= (uint32_t) static_cast<const unsigned short*>(base)[i + j] << (16 * (j & 1));
+        else
+          w[j] = static_cast<const uint32_t*>(base)[i + j];
+      }
+  }
+}
+
 // A lane's 8 elements of group g of a row that starts at element `row0`; elements past the row's
 // end read as `fill`.
 template <int DT, bool VEC>
@@ -233,11 +286,12 @@ __device__ __forceinline__ BlockScale shared_block_scale(float amax, unsigned in
 
 // Quantise a lane's part of the groups g0, g0 + gstep, ... (NCH of them) of row `row`: codes to q,
 // the blocks' scales to scale[block][row].  All 32 lanes take part; elements past the row's end must
-// be 0.  The steps of all groups stand side by side, so that their shuffles and divisions overlap.
+// be 0.  `whole`: no lane's 8 elements end past the row's end.  The steps of all groups stand side by
+// side, so that their shuffles and divisions overlap.
 template <bool E5M2, bool VEC, int NCH>
 __device__ __forceinline__ void quant_groups(float (&v)[NCH][8], uint32_t g0, uint32_t gstep, int lane, uint32_t cols,
                                              uint64_t row, uint64_t rows, unsigned char* q, uint64_t ldq,
-                                             float* scale) {
+                                             float* scale, bool whole = true) {
   if constexpr (VEC) {
     const unsigned int half = 0xFFFFu << (lane & 16);
     float m[NCH];
@@ -265,7 +319,15 @@ __device__ __forceinline__ void quant_groups(float (&v)[NCH][8], uint32_t g0, ui
     for (int i = 0; i < NCH; ++i) {
       const uint32_t c = group_col<true>(g0 + i * gstep, lane, 0);
       if (c < cols) {
-        *reinterpret_cast<uint2*>(q + row * ldq + c) = quant8<E5M2>(v[i], s[i].inv);
+        const uint2 r = quant8<E5M2>(v[i], s[i].inv);
+        unsigned char* dst = q + row * ldq + c;
+        if (whole || c + 8 <= cols) {
+          *reinterpret_cast<uint2*>(dst) = r;
+        } else {
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            if (c + j < cols) dst[j] = (unsigned char)((j < 4 ? r.x : r.y) >> (8 * (j & 3)));
+        }
         if ((lane & 15) == 0) scale[(uint64_t)(c >> 7) * rows + row] = s[i].scale;
       }
     }

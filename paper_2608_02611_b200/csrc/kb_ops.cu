@@ -52,7 +52,10 @@ kb_status launch_quant(kb_ctx* ctx, const QuantParams& p, bool transpose, bool t
   if (!transpose && !tiles) {
     const uint64_t pieces = (p.groups + kQuantRowGroups - 1) / kQuantRowGroups;
     const dim3 grid((unsigned int)((p.rows + 7) / 8), (unsigned int)std::min<uint64_t>(pieces, 65535));
-    quant_rows_kernel<DT, VEC, E5M2><<<grid, 256, 0, st>>>(p);
+    if (!VEC && p.q_vec)
+      quant_rows_kernel<DT, VEC, !VEC, E5M2><<<grid, 256, 0, st>>>(p);
+    else
+      quant_rows_kernel<DT, VEC, false, E5M2><<<grid, 256, 0, st>>>(p);
     return launched(ctx);
   }
   const uint64_t n = (uint64_t)p.rtiles * p.ctiles;
@@ -355,7 +358,9 @@ extern "C" kb_status kb_quantize_blocks(kb_ctx* ctx, const void* d_x, uint64_t r
   p.groups = (uint32_t)((cols + kGroup - 1) / kGroup);
   p.rtiles = (uint32_t)((rows + 127) / 128);
   p.ctiles = (uint32_t)((cols + 127) / 128);
-  const bool vec = cols % 8 == 0 && rows_aligned(d_x, ldx, e) && (transpose || (ldq % 8 == 0 && aligned_to(d_q, 8)));
+  p.span = (rows - 1) * ldx + cols;
+  p.q_vec = ldq % 8 == 0 && aligned_to(d_q, 8);
+  const bool vec = cols % 8 == 0 && rows_aligned(d_x, ldx, e) && (transpose || p.q_vec);
   const bool e5m2 = q_dtype == KB_F8E5M2, tiles = mode == KB_SCALE_TILES;
   if (dtype == KB_F32) return launch_quant<KB_F32>(ctx, p, vec, e5m2, transpose, tiles, st);
   if (dtype == KB_F16) return launch_quant<KB_F16>(ctx, p, vec, e5m2, transpose, tiles, st);

@@ -16,37 +16,15 @@ struct QuantParams {
   unsigned char* q;
   float* scale;
   uint64_t rows, cols, ldx, ldq;    // of x
+  uint64_t span;                    // elements of x from its first to its last, gaps included
+  bool q_vec;                       // rows of q start on 8-byte boundaries
   uint32_t groups;                  // groups of 256 columns per row
   uint32_t rtiles, ctiles;          // tiles of 128 along the rows and columns of x
 };
 
-// 1 x 128 blocks along the rows of x: one warp per row and piece of NG groups.
-constexpr int kQuantRowGroups = 4;
-template <int DT, bool VEC, bool E5M2>
-__global__ void __launch_bounds__(256) quant_rows_kernel(const QuantParams p) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const uint64_t row = (uint64_t)blockIdx.x * 8 + warp;
-  if (row >= p.rows) return;
-  for (uint32_t g0 = blockIdx.y * kQuantRowGroups; g0 < p.groups; g0 += gridDim.y * kQuantRowGroups) {
-    float v[kQuantRowGroups][8];
-#pragma unroll
-    for (int i = 0; i < kQuantRowGroups; ++i)
-      load_group<DT, VEC>(p.x, row * p.ldx, g0 + i, lane, (uint32_t)p.cols, v[i]);
-    quant_groups<E5M2, VEC, kQuantRowGroups>(v, g0, 1, lane, (uint32_t)p.cols, row, p.rows, p.q, p.ldq, p.scale);
-  }
-}
-
-// One 128 x 128 tile per CTA of 256 threads.  TILES: one scale for the tile, else one per column
-// of x (only needed transposed: the block then runs along the rows of x).  A thread keeps its 8 x 8
-// elements in their storage type (32 registers for 16-bit types), so that three CTAs fit on an SM
-// and 96 KB are on their way while one of them reduces.
-// The transposed tile in shared memory: rows of 128 codes; the 8-byte piece k of row r stands at
-// place k ^ (r / 8), so that neither the writes (16 rows apart by 8, one piece each) nor the reads
-// (one row at a time) meet in a bank.
-__device__ __forceinline__ int transposed_at(int r, int k) { return r * 128 + ((k ^ (r >> 3)) & 15) * 8; }
 template <int DT>
 struct Held8 {   // 8 consecutive elements of one row
-  static constexpr int kWords = DT == KB_F32 ? 8 : 4;
+  static constexpr int kWords = 2 * Elem<DT>::kBytes;
   uint32_t w[kWords];
   __device__ __forceinline__ void load(const void* p, uint64_t i) {
     const uint4* q = reinterpret_cast<const uint4*>(static_cast<const unsigned char*>(p) + i * Elem<DT>::kBytes);
@@ -56,12 +34,6 @@ struct Held8 {   // 8 consecutive elements of one row
   __device__ __forceinline__ void zero() {
 #pragma unroll
     for (int k = 0; k < kWords; ++k) w[k] = 0u;
-  }
-  __device__ __forceinline__ void set(int j, const void* p, uint64_t i) {   // element j; the others stay
-    if constexpr (DT == KB_F32)
-      w[j] = static_cast<const uint32_t*>(p)[i];
-    else
-      w[j >> 1] |= (uint32_t) static_cast<const unsigned short*>(p)[i] << (16 * (j & 1));
   }
   __device__ __forceinline__ float get(int j) const {
     if constexpr (DT == KB_F32)
@@ -76,6 +48,46 @@ struct Held8 {   // 8 consecutive elements of one row
     for (int j = 0; j < 8; ++j) v[j] = get(j);
   }
 };
+
+// 1 x 128 blocks along the rows of x: one warp per row and piece of NG groups.
+constexpr int kQuantRowGroups = 4;
+// VEC: rows of x and q are aligned and a multiple of 8 long.  Otherwise, with aligned rows of q
+// (SHIFT), a lane still takes 8 consecutive elements and shifts the granules they lie in into place
+// (8191 x 8191 bf16: 72 us, element by element 89); rows of q at any address go element by element.
+template <int DT, bool VEC, bool SHIFT, bool E5M2>
+__global__ void __launch_bounds__(256) quant_rows_kernel(const QuantParams p) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const uint64_t row = (uint64_t)blockIdx.x * 8 + warp;
+  if (row >= p.rows) return;
+  for (uint32_t g0 = blockIdx.y * kQuantRowGroups; g0 < p.groups; g0 += gridDim.y * kQuantRowGroups) {
+    float v[kQuantRowGroups][8];
+#pragma unroll
+    for (int i = 0; i < kQuantRowGroups; ++i) {
+      if constexpr (SHIFT) {
+        const uint64_t c = (uint64_t)(g0 + i) * kGroup + lane * 8;
+        Held8<DT> h;
+        if (c < p.cols)
+          load_shifted<Elem<DT>::kBytes>(p.x, p.span, row * p.ldx + c, (int)min((uint64_t)8, p.cols - c), h.w);
+        else
+          h.zero();
+        h.all(v[i]);
+      } else {
+        load_group<DT, VEC>(p.x, row * p.ldx, g0 + i, lane, (uint32_t)p.cols, v[i]);
+      }
+    }
+    quant_groups<E5M2, VEC || SHIFT, kQuantRowGroups>(v, g0, 1, lane, (uint32_t)p.cols, row, p.rows, p.q, p.ldq,
+                                                      p.scale, !SHIFT);
+  }
+}
+
+// One 128 x 128 tile per CTA of 256 threads.  TILES: one scale for the tile, else one per column
+// of x (only needed transposed: the block then runs along the rows of x).  A thread keeps its 8 x 8
+// elements in their storage type (32 registers for 16-bit types), so that three CTAs fit on an SM
+// and 96 KB are on their way while one of them reduces.
+// The transposed tile in shared memory: rows of 128 codes; the 8-byte piece k of row r stands at
+// place k ^ (r / 8), so that neither the writes (16 rows apart by 8, one piece each) nor the reads
+// (one row at a time) meet in a bank.
+__device__ __forceinline__ int transposed_at(int r, int k) { return r * 128 + ((k ^ (r >> 3)) & 15) * 8; }
 __device__ __forceinline__ float inf_to_nan(float v) { return isinf(v) ? __uint_as_float(0x7FFFFFFFu) : v; }
 
 template <int DT, bool VEC, bool E5M2, bool TILES, bool TRANSPOSE>
@@ -92,16 +104,12 @@ __global__ void __launch_bounds__(256, DT == KB_F32 ? 2 : 3) quant_tile_kernel(c
   Held8<DT> h[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    if (VEC && i < nrow && ncol == 8) {
-      h[i].load(p.x, (row0 + i) * p.ldx + col0);
-    } else {
+    if (i >= nrow || ncol == 0)
       h[i].zero();
-      if (!VEC) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if (i < nrow && j < ncol) h[i].set(j, p.x, (row0 + i) * p.ldx + col0 + j);
-      }
-    }
+    else if constexpr (VEC)
+      h[i].load(p.x, (row0 + i) * p.ldx + col0);
+    else
+      load_shifted<Elem<DT>::kBytes>(p.x, p.span, (row0 + i) * p.ldx + col0, ncol, h[i].w);
   }
   bool infinite = false;   // the block (TILES: the tile) holds an Inf
   float inv[8];            // per column of the thread; all equal for TILES
@@ -200,8 +208,8 @@ __global__ void __launch_bounds__(256, DT == KB_F32 ? 2 : 3) quant_tile_kernel(c
       }
       const uint2 r = quant8<E5M2>(v, inv[0]);
       unsigned char* dst = p.q + (row0 + i) * p.ldq + col0;
-      if (VEC) {
-        if (ncol == 8) *reinterpret_cast<uint2*>(dst) = r;
+      if (ncol == 8 && (VEC || p.q_vec)) {
+        *reinterpret_cast<uint2*>(dst) = r;
       } else {
         for (int j = 0; j < ncol; ++j) dst[j] = (unsigned char)((j < 4 ? r.x : r.y) >> (8 * (j & 3)));
       }

@@ -124,6 +124,20 @@ def test_quantisation_of_strided_and_unaligned_rows(ctx, gap, offset, tiles, tra
         _same_codes(q, code, torch.float8_e4m3fn)
 
 
+@pytest.mark.parametrize("rows,cols", [(1, 5), (3, 131), (37, 1001), (129, 515)])
+@pytest.mark.parametrize("gap,offset", [(0, 0), (0, 1), (0, 3), (1, 5), (6, 7)])
+@pytest.mark.parametrize("tiles,transpose", [(False, False), (True, False), (False, True)])
+def test_quantisation_of_rows_at_every_alignment(ctx, rows, cols, gap, offset, tiles, transpose):
+    """The granules of 16 bytes that a row shares with its neighbours, and with what lies before and
+    behind the matrix, hold NaN."""
+    for dtype in FLOATS:
+        x = _quant_input(rows, cols, dtype, rows + cols)
+        q, scale = ctx.quantize_blocks(_strided(x, gap, offset), tiles=tiles, transpose=transpose)
+        code, want = _blocks32(x.t() if transpose else x, torch.float8_e4m3fn, tiles)
+        assert bool((scale.cpu() == want).all())
+        _same_codes(q, code, torch.float8_e4m3fn)
+
+
 @pytest.mark.parametrize("cols", [384, 300])
 @pytest.mark.parametrize("tiles,transpose", [(False, False), (False, True), (True, False), (True, True)])
 def test_quantisation_of_nonfinite_zero_and_extreme_blocks(ctx, cols, tiles, transpose):
