@@ -612,9 +612,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PairTile::kThreads, 
             }
             const float(&w)[16] = v[(j0 / 16) & 1];
 #pragma unroll
-            for (int j = 0; j < 16; j += 2)
-              fma_pair(acc[j0 + j], acc[j0 + j + 1], BROWS ? w[j] * c[j0 + j] : w[j],
-                       BROWS ? w[j + 1] * c[j0 + j + 1] : w[j + 1], s, s);
+            for (int j = 0; j < 16; j += 4) {
+              const float4 f = BROWS ? *reinterpret_cast<const float4*>(c + j0 + j) : make_float4(1.0f, 1.0f, 1.0f, 1.0f);
+              fma_pair(acc[j0 + j], acc[j0 + j + 1], BROWS ? w[j] * f.x : w[j], BROWS ? w[j + 1] * f.y : w[j + 1], s, s);
+              fma_pair(acc[j0 + j + 2], acc[j0 + j + 3], BROWS ? w[j + 2] * f.z : w[j + 2],
+                       BROWS ? w[j + 3] * f.w : w[j + 3], s, s);
+            }
           }
           a ^= 1u;
         }

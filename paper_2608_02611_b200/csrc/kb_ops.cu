@@ -149,7 +149,7 @@ kb_status launch_norm_bwd(kb_ctx* ctx, NormBwdParams& p, unsigned int threads, u
   };
   if constexpr (VEC && !WARP) {
     constexpr auto kernel = norm_bwd_kernel<DT, NCH, true, false, true>;
-    const int per_sm = ctas_by_registers<kernel>(threads, 4);
+    const int per_sm = ctas_by_registers<kernel>(threads, std::max(4, (int)(1024 / threads)));
     const uint64_t resident = (uint64_t)ctx->sm_count * per_sm;
     const size_t bytes = (size_t)p.cols * elem_bytes((kb_dtype)DT);
     const uint32_t stages = ring_stages(2 * round_up(bytes, 128), per_sm);
@@ -162,20 +162,20 @@ kb_status launch_norm_bwd(kb_ctx* ctx, NormBwdParams& p, unsigned int threads, u
     }
   }
   constexpr auto kernel = norm_bwd_kernel<DT, NCH, VEC, WARP, false>;
-  return launch(kernel, (uint64_t)ctx->sm_count * ctas_by_registers<kernel>(threads, WARP ? 4 : 2),
+  return launch(kernel, (uint64_t)ctx->sm_count * ctas_by_registers<kernel>(threads, WARP ? 4 : std::max(2, (int)(1024 / threads))),
                 WARP ? 2 * sizeof(float) * p.cols : 0);
 }
 
 template <int DT, bool VEC>
 kb_status launch_norm_bwd(kb_ctx* ctx, NormBwdParams& p, uint32_t* nparts, cudaStream_t st) {
   const uint32_t g = p.groups;
+  // a warp per row up to 512 columns (32768 x 512 bf16: 32 us, by CTAs 42; 32768 x 768: 51 and 48)
   if (g == 1) return launch_norm_bwd<DT, 1, VEC, true>(ctx, p, 128, nparts, st);
   if (g == 2) return launch_norm_bwd<DT, 2, VEC, true>(ctx, p, 128, nparts, st);
-  if (g <= 4) return launch_norm_bwd<DT, 4, VEC, true>(ctx, p, 128, nparts, st);
   // one group per warp up to 16 warps; up to 24 where the rows are too few for the ring or cannot
   // take it (777 x 5003 fp16: 19 us with two groups per warp, 14 with one and a row ahead)
   const bool few = !VEC || p.rows < 2ull * ctx->sm_count;
-  if (g <= 16 || (g <= 24 && few)) return launch_norm_bwd<DT, 1, VEC, false>(ctx, p, 32 * g, nparts, st);
+  if (few && g <= 24) return launch_norm_bwd<DT, 1, VEC, false>(ctx, p, 32 * g, nparts, st);
   if (g <= 32) return launch_norm_bwd<DT, 2, VEC, false>(ctx, p, 32 * ((g + 1) / 2), nparts, st);
   if (p.dx) {
     norm_bwd_long_kernel<DT, VEC><<<(unsigned int)p.rows, 512, 0, st>>>(p);
