@@ -1,4 +1,5 @@
-"""ctypes binding of the kb C ABI (include/kb.h, include/kb_ops.h): argument marshalling only.
+"""Binding of the kb C ABI (include/kb.h by ctypes, include/kb_ops.h by csrc/kb_torch.cpp):
+argument marshalling only.
 
 Every step of the path runs in the CUDA library; torch is used here for device
 memory and the current stream.  There is no CPU fallback: loading fails loudly
@@ -126,15 +127,6 @@ def load() -> ctypes.CDLL:
 
 def _stream_ptr(device) -> int:
     return int(torch.cuda.current_stream(device).cuda_stream)
-
-
-# The current stream's handle without building a Stream object (2 us of the 5 us that a call for a
-# single token takes on the device).
-_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-
-
-def _stream_of(device) -> int:
-    return _raw_stream(device.index) if _raw_stream is not None else _stream_ptr(device)
 
 
 class Mask:
@@ -613,41 +605,21 @@ class LayerNormResult(NamedTuple):
     scale: Optional[torch.Tensor]
 
 
-def _rows(t: torch.Tensor, name: str, where: str, device) -> torch.Tensor:
-    """A tensor as a matrix [rows, columns] with adjacent columns, without copying: 2-D with any
-    row stride, or of any rank if its rows are evenly spaced."""
-    if t.device != device:
-        raise KbError(1, where, f"{name} must be on {device}")
-    if t.dim() != 2:
-        if t.dim() == 0 or not (t.is_contiguous() or t.numel() == 0):
-            raise KbError(1, where, f"{name} must be 2-D or contiguous")
-        t = t.view(t.numel() // t.shape[-1] if t.shape[-1] else 0, t.shape[-1])
-    if not t.is_contiguous():
-        rows, cols = t.shape
-        if (cols > 1 and t.stride(1) != 1) or (rows > 1 and t.stride(0) < cols):
-            raise KbError(1, where, f"the columns of {name} must be adjacent and its rows must not overlap")
-    return t
+_native_module = None
 
 
-def _ld(t: torch.Tensor) -> int:
-    """Row stride of a matrix; that of a single row is free (torch may report anything)."""
-    rows, cols = t.shape
-    return max(t.stride(0), cols) if rows > 1 else (cols + 15) // 16 * 16
-
-
-def _codes(rows: int, cols: int, dtype: torch.dtype, device) -> torch.Tensor:
-    """Room for 8-bit codes [rows, cols] whose rows start on 16-byte boundaries."""
-    if cols % 16 == 0:
-        return torch.empty((rows, cols), dtype=dtype, device=device)
-    return torch.empty((rows, (cols + 15) // 16 * 16), dtype=dtype, device=device)[:, :cols]
-
-
-def _vector(t: torch.Tensor, n: int, name: str, where: str, device, *dtypes) -> int:
-    """Address of a contiguous tensor of n elements."""
-    if t.numel() != n or t.dtype not in dtypes or t.device != device or not t.is_contiguous():
-        raise KbError(1, where, f"{name} must be a contiguous tensor of {n} elements of "
-                                f"{' or '.join(str(d) for d in dtypes)} on {device}")
-    return t.data_ptr()
+def _native():
+    """The native half of the operators' calls (csrc/kb_torch.cpp), bound to the loaded library."""
+    global _native_module
+    if _native_module is None:
+        L = load()
+        if not os.path.exists(os.path.join(_HERE, "_kb_torch.so")):
+            raise ImportError("_kb_torch.so is missing: build it first (python -m paper_2608_02611_b200.build)")
+        from . import _kb_torch
+        _kb_torch.bind(KbError, *[ctypes.cast(getattr(L, name), ctypes.c_void_p).value for name in (
+            "kb_quantize_blocks", "kb_layernorm", "kb_layernorm_backward", "kb_matmul_blocks", "kb_last_error")])
+        _native_module = _kb_torch
+    return _native_module
 
 
 @_ctx_method
@@ -656,61 +628,27 @@ def quantize_blocks(self, x: torch.Tensor, dtype: torch.dtype = torch.float8_e4m
     """kb_quantize_blocks: ``x`` [rows, cols] (or its transpose) as 8-bit codes with a binary32
     scale per 1 x 128 block along the columns, or per 128 x 128 tile -> (q, scale).
 
-    q [R, C] has rows on 16-byte boundaries; scale is [ceil(C/128), R], with tiles
-    [ceil(C/128), ceil(R/128)].
+    ``x`` is 2-D with adjacent columns and any row stride, or contiguous of any rank (its last
+    dimension are the columns).  q [R, C] has rows on 16-byte boundaries; scale is
+    [ceil(C/128), R], with tiles [ceil(C/128), ceil(R/128)].
     """
-    x = _rows(x, "x", "kb_quantize_blocks", self.device)
-    rows, cols = x.shape
-    R, C = (cols, rows) if transpose else (rows, cols)
-    q = _codes(R, C, dtype, self.device)
-    scale = torch.empty((-(-C // KB_BLOCK), -(-R // KB_BLOCK) if tiles else R), dtype=torch.float32,
-                        device=self.device)
-    rc = load().kb_quantize_blocks(self._h, x.data_ptr(), rows, cols, _ld(x), DTYPE_CODE.get(x.dtype, -1),
-                                   int(bool(transpose)), KB_SCALE_TILES if tiles else KB_SCALE_ROWS,
-                                   q.data_ptr(), _ld(q), DTYPE_CODE.get(dtype, -1), scale.data_ptr(),
-                                   _stream_of(self.device))
-    self._check(rc, "kb_quantize_blocks")
-    return q, scale
+    return (_native_module or _native()).quantize_blocks(self._h, self.device.index, x, DTYPE_CODE.get(dtype, -1), tiles,
+                                                         transpose)
 
 
 @_ctx_method
 def layernorm(self, x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None,
               eps: float = 1e-5, *, want_y: bool = True, want_stats: bool = True,
               quantize: Optional[torch.dtype] = None) -> LayerNormResult:
-    """kb_layernorm over the last dimension of ``x``.
+    """kb_layernorm over the last dimension of ``x`` (shapes as for ``quantize_blocks``).
 
     ``quantize`` (an 8-bit float type) also, or with ``want_y`` false only, returns the result as
     codes q and scales as ``quantize_blocks`` lays them out, ready for ``matmul_blocks``;
     ``want_stats`` returns each row's mean and 1/sqrt(var + eps) for the backward pass.
     """
-    where = "kb_layernorm"
-    x2 = _rows(x, "x", where, self.device)
-    rows, cols = x2.shape
-    dtype = x.dtype
-    w = _vector(weight, cols, "weight", where, self.device, dtype, torch.float32) if weight is not None else None
-    b = _vector(bias, cols, "bias", where, self.device, dtype, torch.float32) if bias is not None else None
-    params = weight.dtype if weight is not None else bias.dtype if bias is not None else dtype
-    if w is not None and b is not None and weight.dtype != bias.dtype:
-        raise KbError(1, where, "weight and bias must have the same type")
-    y = torch.empty(x.shape, dtype=dtype, device=self.device) if want_y else None
-    mean = rstd = q = scale = None
-    if want_stats:
-        mean = torch.empty(rows, dtype=torch.float32, device=self.device)
-        rstd = torch.empty(rows, dtype=torch.float32, device=self.device)
-    if quantize is not None:
-        q = _codes(rows, cols, quantize, self.device)
-        scale = torch.empty((-(-cols // KB_BLOCK), rows), dtype=torch.float32, device=self.device)
-    if rows == 0:
-        return LayerNormResult(y, mean, rstd, q, scale)
-    rc = load().kb_layernorm(self._h, x2.data_ptr(), rows, cols, _ld(x2), DTYPE_CODE.get(dtype, -1), w, b,
-                             DTYPE_CODE.get(params, -1), float(eps),
-                             y.data_ptr() if want_y else None, cols,
-                             mean.data_ptr() if want_stats else None, rstd.data_ptr() if want_stats else None,
-                             q.data_ptr() if q is not None else None, _ld(q) if q is not None else 0,
-                             DTYPE_CODE.get(quantize, -1) if q is not None else KB_F8E4M3,
-                             scale.data_ptr() if q is not None else None, _stream_of(self.device))
-    self._check(rc, where)
-    return LayerNormResult(y, mean, rstd, q, scale)
+    code = None if quantize is None else DTYPE_CODE.get(quantize, -1)
+    return LayerNormResult(*(_native_module or _native()).layernorm(self._h, self.device.index, x, weight, bias, eps,
+                                                                    want_y, want_stats, code))
 
 
 @_ctx_method
@@ -718,24 +656,8 @@ def layernorm_backward(self, dy: torch.Tensor, x: torch.Tensor, weight: Optional
                        rstd: torch.Tensor, *, want_bias: bool = True):
     """kb_layernorm_backward -> (dx, dweight, dbias), the parameters' gradients in the weight's
     type (binary32 without a weight); dbias is None unless ``want_bias``."""
-    where = "kb_layernorm_backward"
-    dy2, x2 = _rows(dy, "dy", where, self.device), _rows(x, "x", where, self.device)
-    rows, cols = x2.shape
-    if dy2.shape != x2.shape or dy.dtype != x.dtype:
-        raise KbError(1, where, "dy must have the shape and type of x")
-    w = _vector(weight, cols, "weight", where, self.device, x.dtype, torch.float32) if weight is not None else None
-    params = weight.dtype if weight is not None else torch.float32
-    m = _vector(mean, rows, "mean", where, self.device, torch.float32)
-    r = _vector(rstd, rows, "rstd", where, self.device, torch.float32)
-    dx = torch.empty(x.shape, dtype=x.dtype, device=self.device)
-    dweight = torch.empty(cols, dtype=params, device=self.device)
-    dbias = torch.empty(cols, dtype=params, device=self.device) if want_bias else None
-    rc = load().kb_layernorm_backward(self._h, dy2.data_ptr(), _ld(dy2), x2.data_ptr(), _ld(x2), rows, cols,
-                                      DTYPE_CODE.get(x.dtype, -1), w, DTYPE_CODE.get(params, -1), m, r,
-                                      dx.data_ptr(), cols, dweight.data_ptr(),
-                                      dbias.data_ptr() if want_bias else None, _stream_of(self.device))
-    self._check(rc, where)
-    return dx, dweight, dbias
+    return (_native_module or _native()).layernorm_backward(self._h, self.device.index, dy, x, weight, mean, rstd,
+                                                            want_bias)
 
 
 @_ctx_method
@@ -745,28 +667,10 @@ def matmul_blocks(self, a: torch.Tensor, a_scale: torch.Tensor, b: torch.Tensor,
     ``quantize_blocks`` or ``layernorm`` made them) -> [M, N] in ``out_dtype``.
 
     a_scale is [ceil(K/128), M]; b_scale is [ceil(K/128), ceil(N/128)] (tiles) or
-    [ceil(K/128), N] (rows).  ``out``: where to write the result (a 2-D tensor with adjacent columns).
+    [ceil(K/128), N] (rows).  ``out``: where to write the result (a matrix with adjacent columns).
     """
-    where = "kb_matmul_blocks"
-    a, b = _rows(a, "a", where, self.device), _rows(b, "b", where, self.device)
-    (M, K), (N, Kb) = a.shape, b.shape
-    kb = -(-K // KB_BLOCK)
-    if Kb != K:
-        raise KbError(1, where, f"a has {K} columns, b {Kb}")
-    tiles = b_scale.shape != (kb, N)
-    if a_scale.shape != (kb, M) or (tiles and b_scale.shape != (kb, -(-N // KB_BLOCK))):
-        raise KbError(1, where, "scales are laid out [ceil(K/128), rows] or [ceil(K/128), ceil(rows/128)]")
-    sa = _vector(a_scale, kb * M, "a_scale", where, self.device, torch.float32)
-    sb = _vector(b_scale, kb * (-(-N // KB_BLOCK) if tiles else N), "b_scale", where, self.device, torch.float32)
-    if out is None:
-        out = torch.empty((M, N), dtype=out_dtype, device=self.device)
-    elif out.shape != (M, N) or _rows(out, "out", where, self.device) is not out:
-        raise KbError(1, where, f"out must be a matrix [{M}, {N}]")
-    rc = load().kb_matmul_blocks(self._h, a.data_ptr(), _ld(a), DTYPE_CODE.get(a.dtype, -1), sa, b.data_ptr(), _ld(b),
-                                 DTYPE_CODE.get(b.dtype, -1), sb, KB_SCALE_TILES if tiles else KB_SCALE_ROWS, M, N, K,
-                                 out.data_ptr(), _ld(out), DTYPE_CODE.get(out.dtype, -1), _stream_of(self.device))
-    self._check(rc, where)
-    return out
+    return (_native_module or _native()).matmul_blocks(self._h, self.device.index, a, a_scale, b, b_scale,
+                                                       DTYPE_CODE.get(out_dtype, -1), out)
 
 
 def records_f64(screen_out: torch.Tensor) -> np.ndarray:

@@ -2,7 +2,8 @@
 
 Two translation units (csrc/kb_host.cu: the gate, adjudication and selection; csrc/kb_ops.cu:
 the model operators) compiled by nvcc for sm_100a into paper_2608_02611_b200/libkb.so, a plain
-C-ABI shared library (include/kb.h, include/kb_ops.h).
+C-ABI shared library (include/kb.h, include/kb_ops.h); and csrc/kb_torch.cpp, compiled by g++ against
+torch's headers into paper_2608_02611_b200/_kb_torch.so, the native half of the operators' binding.
 """
 from __future__ import annotations
 
@@ -13,6 +14,8 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libkb.so")
+NATIVE = os.path.join(HERE, "_kb_torch.so")
+NATIVE_SOURCE = os.path.join(CSRC, "kb_torch.cpp")
 SOURCES = ["kb_host.cu", "kb_ops.cu"]
 INCLUDE = os.path.join(HERE, "..", "include")
 
@@ -22,12 +25,31 @@ NVCC_FLAGS = [
 ]
 
 
+def _newer(target: str, deps) -> bool:
+    return not os.path.exists(target) or any(os.path.getmtime(f) > os.path.getmtime(target) for f in deps)
+
+
+def _sources(*suffixes):
+    return [os.path.join(d, f) for d in (CSRC, INCLUDE) for f in os.listdir(d) if f.endswith(suffixes)]
+
+
 def stale() -> bool:
-    if not os.path.exists(LIB):
-        return True
-    t = os.path.getmtime(LIB)
-    deps = [os.path.join(d, f) for d in (CSRC, INCLUDE) for f in os.listdir(d) if f.endswith((".cu", ".cuh", ".h"))]
-    return any(os.path.getmtime(f) > t for f in deps)
+    return _newer(LIB, _sources(".cu", ".cuh", ".h"))
+
+
+def build_native(force: bool = False) -> str:
+    if force or _newer(NATIVE, _sources(".h") + [NATIVE_SOURCE]):
+        import sysconfig
+        import torch
+        from torch.utils import cpp_extension
+        inc = cpp_extension.include_paths() + [os.path.join(os.environ.get("CUDA_HOME", "/usr/local/cuda"), "include"),
+                                               sysconfig.get_paths()["include"]]
+        libs = cpp_extension.library_paths()
+        cmd = ["g++", "-O2", "-std=c++17", "-shared", "-fPIC", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}"]
+        cmd += [f"-I{d}" for d in inc] + ["-o", NATIVE, NATIVE_SOURCE] + [f"-L{d}" for d in libs]
+        cmd += ["-ltorch_python", "-ltorch", "-ltorch_cpu", "-ltorch_cuda", "-lc10", "-lc10_cuda"]
+        subprocess.run(cmd, check=True)
+    return NATIVE
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
@@ -36,6 +58,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
         cmd = [nvcc] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) + \
               ["-o", LIB] + [os.path.join(CSRC, s) for s in SOURCES]
         subprocess.run(cmd, check=True)
+    build_native(force)
     return LIB
 
 

@@ -339,9 +339,10 @@ struct PairTile {
   static constexpr uint32_t kTmemCols = 512;
   static constexpr int kEpiWarps = 8;
   // three warpgroups: one copies and issues, two scale and add.  168 registers per thread at
-  // launch are split 104 / 200 / 200: 128 running sums and what is in flight need the 200.
+  // launch are split 56 / 224 / 224: 128 running sums and 32 values on their way need that many
+  // before the compiler stops moving them about (8192^3: 548 us, with 104 / 200 / 200 570).
   static constexpr int kThreads = 128 + 32 * kEpiWarps;
-  static constexpr int kRegsLaunch = 168, kRegsControl = 104, kRegsEpi = 200;
+  static constexpr int kRegsLaunch = 168, kRegsControl = 56, kRegsEpi = 224;
   static_assert(128 * kRegsControl + (kThreads - 128) * kRegsEpi <= kThreads * kRegsLaunch, "register shares");
   // results leave through shared memory, 64 bytes of 32 rows per warp at a time, so that every
   // store of a warp covers whole 32-byte sectors; 80-byte rows keep the 16-byte accesses apart
@@ -598,25 +599,21 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PairTile::kThreads, 
             st = 0;
             st_phase ^= 1u;
           }
-          // 16 columns at a time, the next 16 on their way while these are scaled and added
-          float v[2][16];
-          tmem_ld16(taddr + a * 256, v[0]);
 #pragma unroll
-          for (int j0 = 0; j0 < 128; j0 += 16) {
+          for (int j0 = 0; j0 < 128; j0 += 32) {
+            float v[32];
+            tmem_ld32(taddr + a * 256 + j0, v);
             tmem_wait_ld();
-            if (j0 + 16 < 128) {
-              tmem_ld16(taddr + a * 256 + j0 + 16, v[(j0 / 16 + 1) & 1]);
-            } else {   // all of this accumulator is in registers
+            if (j0 == 96) {   // all of this accumulator is in registers
               tc_fence_before();
               mbar_arrive_cluster_if(release0 + a * 8, lane == 0);
             }
-            const float(&w)[16] = v[(j0 / 16) & 1];
 #pragma unroll
-            for (int j = 0; j < 16; j += 4) {
+            for (int j = 0; j < 32; j += 4) {
               const float4 f = BROWS ? *reinterpret_cast<const float4*>(c + j0 + j) : make_float4(1.0f, 1.0f, 1.0f, 1.0f);
-              fma_pair(acc[j0 + j], acc[j0 + j + 1], BROWS ? w[j] * f.x : w[j], BROWS ? w[j + 1] * f.y : w[j + 1], s, s);
-              fma_pair(acc[j0 + j + 2], acc[j0 + j + 3], BROWS ? w[j + 2] * f.z : w[j + 2],
-                       BROWS ? w[j + 3] * f.w : w[j + 3], s, s);
+              fma_pair(acc[j0 + j], acc[j0 + j + 1], BROWS ? v[j] * f.x : v[j], BROWS ? v[j + 1] * f.y : v[j + 1], s, s);
+              fma_pair(acc[j0 + j + 2], acc[j0 + j + 3], BROWS ? v[j + 2] * f.z : v[j + 2],
+                       BROWS ? v[j + 3] * f.w : v[j + 3], s, s);
             }
           }
           a ^= 1u;
