@@ -45,8 +45,9 @@ typedef enum {
  *     V[r][c] ~ Q[r][c] * S[c / 128][r]          KB_SCALE_ROWS,   S is [ceil(C/128)][R]
  *     V[r][c] ~ Q[r][c] * S[c / 128][r / 128]    KB_SCALE_TILES,  S is [ceil(C/128)][ceil(R/128)]
  * Per block, every operation rounded to binary32 once, F = 448 (KB_F8E4M3) or 57344 (KB_F8E5M2):
- *     a = max(2^-100, largest |V| that is finite);  S = a / F;  Q = round(min(max(V * (F / a), -F), F))
- * with round-to-nearest-even to the format.  NaN and +-Inf become the format's NaN and do not
+ *     a = max(2^-100, largest |V| that is finite);  S = a / F
+ *     Q = round((V * 0.875) / (a * (0.875 / F)))       = V * F / a, its quotient rounded once before
+ * with round-to-nearest-even to the format (0.875 / F is a power of two).  NaN and +-Inf become the format's NaN and do not
  * enter a.
  *
  *   d_x        DEVICE [rows][cols] of `dtype` (KB_F32, KB_F16 or KB_BF16), row stride ldx.

@@ -218,16 +218,24 @@ __device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) {
   return r;
 }
 // ---- 8-bit quantisation ---------------------------------------------------------------------
-// The block's scale S = a / F and the factor F / a its elements are multiplied with, a >= 2^-100
-// (so that neither quotient leaves the normal range, whatever the block holds).
-struct BlockScale {
-  float scale, inv;
+// A block with largest magnitude a >= 2^-100 has the scale S = a / F, and its codes are the quotients
+// v F / a rounded.  Inputs of 8 or 11 significant bits make quotients that lie exactly between two
+// codes, and a product with a rounded F / a would send some of them the wrong way; so the quotient is
+// rounded correctly, as (v * 0.875) / (a 2^-kShift) with F = 1.75 * 2^(kShift - 1): neither side leaves the
+// range of binary32.
+template <bool E5M2>
+struct Fp8 {
+  static constexpr float kTop = E5M2 ? 57344.0f : 448.0f;
+  static constexpr float kUnscale = E5M2 ? 0x1p-16f : 0x1p-9f;   // 2^-kShift
 };
+struct BlockScale {
+  float scale, den, inv;   // S, a 2^-kShift, 1 / den
+};
+constexpr float kLeastMax = 0x1p-100f;
 template <bool E5M2>
 __device__ __forceinline__ BlockScale block_scale(float amax) {
-  constexpr float top = E5M2 ? 57344.0f : 448.0f;
-  const float a = fmaxf(amax, 0x1p-100f);
-  return {__fdiv_rn(a, top), __fdiv_rn(top, a)};
+  const float a = fmaxf(amax, kLeastMax), den = a * Fp8<E5M2>::kUnscale;
+  return {__fdiv_rn(a, Fp8<E5M2>::kTop), den, __fdiv_rn(1.0f, den)};
 }
 // Two values to two codes (lo in the low byte), saturating; NaN becomes NaN.
 template <bool E5M2>
@@ -239,14 +247,28 @@ __device__ __forceinline__ uint32_t quant2(float lo, float hi) {
     asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
   return r;
 }
+// (v * 0.875) / den, rounded correctly from the rounded reciprocal (Markstein 1990: a quotient estimate
+// within an ulp, corrected once by its exact remainder)
+__device__ __forceinline__ void quotients(float& v0, float& v1, const Pair den, const Pair inv) {
+  const Pair num = mul2(pair(v0, v1), pair(0.875f, 0.875f));
+  const Pair t = mul2(num, inv);
+  const Pair rest = fma2(t, den, num);   // den comes negated
+  unpair(fma2(rest, inv, t), v0, v1);
+}
 template <bool E5M2>
-__device__ __forceinline__ uint2 quant8(const float (&v)[8], float inv) {
-  uint2 r;
-  r.x = quant2<E5M2>(__fmul_rn(v[0], inv), __fmul_rn(v[1], inv)) |
-        quant2<E5M2>(__fmul_rn(v[2], inv), __fmul_rn(v[3], inv)) << 16;
-  r.y = quant2<E5M2>(__fmul_rn(v[4], inv), __fmul_rn(v[5], inv)) |
-        quant2<E5M2>(__fmul_rn(v[6], inv), __fmul_rn(v[7], inv)) << 16;
-  return r;
+__device__ __forceinline__ uint2 quant8(const float (&v)[8], float den, float inv) {
+  const Pair d = pair(-den, -den), r = pair(inv, inv);
+  float t[8];
+#pragma unroll
+  for (int j = 0; j < 8; j += 2) {
+    t[j] = v[j];
+    t[j + 1] = v[j + 1];
+    quotients(t[j], t[j + 1], d, r);
+  }
+  uint2 q;
+  q.x = quant2<E5M2>(t[0], t[1]) | quant2<E5M2>(t[2], t[3]) << 16;
+  q.y = quant2<E5M2>(t[4], t[5]) | quant2<E5M2>(t[6], t[7]) << 16;
+  return q;
 }
 // Largest magnitude, NaN left out (the maximum of a number and NaN is the number).
 template <int J0, int J1>
@@ -273,15 +295,14 @@ __device__ __forceinline__ float warp_max(float v) {
   return v;
 }
 
-// The scale and the factor of a block whose maximum all lanes of `mask` hold: one lane of the 16 (or
-// 32) divides one way round and the others the other way, so the two quotients cost one division.
+// The quotients of a block whose maximum all lanes of `mask` hold: one lane divides for the scale and
+// the others for the reciprocal, so the two cost one division.
 template <bool E5M2>
 __device__ __forceinline__ BlockScale shared_block_scale(float amax, unsigned int mask, int first, int lane) {
-  constexpr float top = E5M2 ? 57344.0f : 448.0f;
-  const float a = fmaxf(amax, 0x1p-100f);
+  const float a = fmaxf(amax, kLeastMax), den = a * Fp8<E5M2>::kUnscale;
   const bool is_first = lane == first;
-  const float r = __fdiv_rn(is_first ? a : top, is_first ? top : a);
-  return {r, __shfl_sync(mask, r, first + 1)};   // .scale holds in lane `first` only
+  const float r = __fdiv_rn(is_first ? a : 1.0f, is_first ? Fp8<E5M2>::kTop : den);
+  return {r, den, __shfl_sync(mask, r, first + 1)};   // .scale holds in lane `first` only
 }
 
 // Quantise a lane's part of the groups g0, g0 + gstep, ... (NCH of them) of row `row`: codes to q,
@@ -319,7 +340,7 @@ __device__ __forceinline__ void quant_groups(float (&v)[NCH][8], uint32_t g0, ui
     for (int i = 0; i < NCH; ++i) {
       const uint32_t c = group_col<true>(g0 + i * gstep, lane, 0);
       if (c < cols) {
-        const uint2 r = quant8<E5M2>(v[i], s[i].inv);
+        const uint2 r = quant8<E5M2>(v[i], s[i].den, s[i].inv);
         unsigned char* dst = q + row * ldq + c;
         if (whole || c + 8 <= cols) {
           *reinterpret_cast<uint2*>(dst) = r;
@@ -352,7 +373,8 @@ __device__ __forceinline__ void quant_groups(float (&v)[NCH][8], uint32_t g0, ui
       const unsigned int half = 0xFFFFu << (lane & 16);
       const BlockScale s = shared_block_scale<E5M2>(lane < 16 ? m[i][0] : m[i][1], half, lane & 16, lane);
       const float inv0 = __shfl_sync(0xFFFFFFFFu, s.inv, 0), inv1 = __shfl_sync(0xFFFFFFFFu, s.inv, 16);
-      const uint2 r0 = quant8<E5M2>(v[i], inv0), r1 = quant8<E5M2>(v[i], inv1);
+      const float den0 = __shfl_sync(0xFFFFFFFFu, s.den, 0), den1 = __shfl_sync(0xFFFFFFFFu, s.den, 16);
+      const uint2 r0 = quant8<E5M2>(v[i], den0, inv0), r1 = quant8<E5M2>(v[i], den1, inv1);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         const uint32_t c = group_col<false>(g, lane, j);

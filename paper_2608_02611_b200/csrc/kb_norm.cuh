@@ -309,7 +309,7 @@ __global__ void __launch_bounds__(WARP ? 128 : NCH == 1 ? 768 : 512) norm_bwd_ke
       if constexpr (RING) {
         // every thread has read the rows: the slot takes those that are `stages` ahead
         const uint64_t ahead = row + (uint64_t)p.stages * gridDim.x;
-        if (threadIdx.x == 0 && ahead < p.rows) {
+        if (threadIdx.x == 0 && ahead < p.rows && !*ring.abort_flag) {
           ring.fetch(slot, row_ptr<DT>(p.x, ahead, p.ldx), row_ptr<DT>(p.dy, ahead, p.lddy));
           ++issued;
         }

@@ -270,15 +270,16 @@ uint32_t lane_splits(const kb_ctx* ctx, uint64_t tiles, uint32_t KB) {
   while (splits > 1 && tiles > (uint64_t)ctx->cluster_room[splits]) --splits;
   return splits;
 }
-// Which kernel takes more than 64 rows of A.  Measured per K block and CTA, long K: 0.43 us for a
-// 128 x 128 tile of matmul_lanes_kernel, 0.58 us for a 256 x 256 tile of a pair.  The pair does four
+// Which kernel takes more than 64 rows of A.  Measured per K block and CTA, long K: 0.47 us for a
+// 128 x 128 tile of matmul_lanes_kernel, 0.52 us for a 256 x 256 tile of a pair.  The pair does four
 // times the work in it but needs 74 tiles to fill the card and cannot share a tile's K blocks:
-// 256x8192x8192 27 us by lanes and 38 by pairs, 300x1000x2000 6.6 and 18, 512x8192x8192 55 and 38.
+// 300x1000x2000 8.5 us by lanes and 18 by pairs, 512x512x8192 12 and 34, 256x4096x4096 14 and 21;
+// 1024x2048x4096 19 and 21; 512x8192x8192 85 and 36.
 bool lanes_are_faster(const kb_ctx* ctx, uint64_t M, uint64_t N, uint32_t KB) {
   const uint64_t lane_tiles = ((M + 127) / 128) * ((N + 127) / 128), pair_tiles = ((M + 255) / 256) * ((N + 255) / 256);
   const uint64_t sms = (uint64_t)ctx->sm_count, pairs = sms / 2, splits = lane_splits(ctx, lane_tiles, KB);
-  const double lanes = 0.43 * (double)((lane_tiles * splits + sms - 1) / sms) * (double)((KB + splits - 1) / splits);
-  const double by_pairs = 0.58 * (double)((pair_tiles + pairs - 1) / pairs) * (double)KB;
+  const double lanes = 0.47 * (double)((lane_tiles * splits + sms - 1) / sms) * (double)((KB + splits - 1) / splits);
+  const double by_pairs = 0.52 * (double)((pair_tiles + pairs - 1) / pairs) * (double)KB;
   return lanes < by_pairs;
 }
 

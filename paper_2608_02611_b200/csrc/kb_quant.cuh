@@ -55,7 +55,7 @@ constexpr int kQuantRowGroups = 4;
 // (SHIFT), a lane still takes 8 consecutive elements and shifts the granules they lie in into place
 // (8191 x 8191 bf16: 72 us, element by element 89); rows of q at any address go element by element.
 template <int DT, bool VEC, bool SHIFT, bool E5M2>
-__global__ void __launch_bounds__(256) quant_rows_kernel(const QuantParams p) {
+__global__ void __launch_bounds__(256, 4) quant_rows_kernel(const QuantParams p) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const uint64_t row = (uint64_t)blockIdx.x * 8 + warp;
   if (row >= p.rows) return;
@@ -93,7 +93,7 @@ __device__ __forceinline__ float inf_to_nan(float v) { return isinf(v) ? __uint_
 template <int DT, bool VEC, bool E5M2, bool TILES, bool TRANSPOSE>
 __global__ void __launch_bounds__(256, DT == KB_F32 ? 2 : 3) quant_tile_kernel(const QuantParams p) {
   __shared__ __align__(16) float smax[TILES ? 8 : 8 * 128];
-  __shared__ __align__(16) float sinv[TILES ? 4 : 128];
+  __shared__ __align__(16) float sinv[TILES ? 4 : 128], sden[TILES ? 4 : 128];
   __shared__ __align__(16) unsigned char st[TRANSPOSE ? 128 * 128 : 16];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int cx = threadIdx.x & 15, ry = threadIdx.x >> 4;
@@ -112,7 +112,7 @@ __global__ void __launch_bounds__(256, DT == KB_F32 ? 2 : 3) quant_tile_kernel(c
       load_shifted<Elem<DT>::kBytes>(p.x, p.span, (row0 + i) * p.ldx + col0, ncol, h[i].w);
   }
   bool infinite = false;   // the block (TILES: the tile) holds an Inf
-  float inv[8];            // per column of the thread; all equal for TILES
+  __align__(16) float den[TILES ? 4 : 8], inv[TILES ? 4 : 8];   // per column of the thread, or of the tile
   if constexpr (TILES) {
     float m = 0.0f;
 #pragma unroll
@@ -137,8 +137,8 @@ __global__ void __launch_bounds__(256, DT == KB_F32 ? 2 : 3) quant_tile_kernel(c
       m = warp_max(smax[lane & 7]);
     }
     const BlockScale s = block_scale<E5M2>(m);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) inv[j] = s.inv;
+    den[0] = s.den;
+    inv[0] = s.inv;
     if (threadIdx.x == 0) {
       if (TRANSPOSE)
         p.scale[(uint64_t)rt * p.ctiles + ct] = s.scale;
@@ -164,7 +164,8 @@ __global__ void __launch_bounds__(256, DT == KB_F32 ? 2 : 3) quant_tile_kernel(c
         dst[1] = make_float4(m[4], m[5], m[6], m[7]);
       }
     };
-    // one thread per column: the tile's maximum, the scale to memory, the factor back to shared memory
+    // one thread per column: the tile's maximum, the scale to memory, the divisor and its
+    // reciprocal back to shared memory
     auto column = [&]() {
       float t = 0.0f;
       if (threadIdx.x < 128) {
@@ -172,6 +173,7 @@ __global__ void __launch_bounds__(256, DT == KB_F32 ? 2 : 3) quant_tile_kernel(c
         for (int w = 0; w < 8; ++w) t = fmaxf(t, smax[w * 128 + threadIdx.x]);
         const BlockScale s = block_scale<E5M2>(t);
         sinv[threadIdx.x] = s.inv;
+        sden[threadIdx.x] = s.den;
         const uint64_t c = (uint64_t)ct * 128 + threadIdx.x;
         if (c < p.cols) p.scale[(uint64_t)rt * p.cols + c] = s.scale;
       }
@@ -186,15 +188,11 @@ __global__ void __launch_bounds__(256, DT == KB_F32 ? 2 : 3) quant_tile_kernel(c
       column();
       __syncthreads();
     }
-    const float4 f0 = *reinterpret_cast<const float4*>(sinv + cx * 8), f1 = *reinterpret_cast<const float4*>(sinv + cx * 8 + 4);
-    inv[0] = f0.x;
-    inv[1] = f0.y;
-    inv[2] = f0.z;
-    inv[3] = f0.w;
-    inv[4] = f1.x;
-    inv[5] = f1.y;
-    inv[6] = f1.z;
-    inv[7] = f1.w;
+#pragma unroll
+    for (int j = 0; j < 8; j += 4) {
+      *reinterpret_cast<float4*>(inv + j) = *reinterpret_cast<const float4*>(sinv + cx * 8 + j);
+      *reinterpret_cast<float4*>(den + j) = *reinterpret_cast<const float4*>(sden + cx * 8 + j);
+    }
   }
   if constexpr (!TRANSPOSE) {
 #pragma unroll
@@ -206,7 +204,7 @@ __global__ void __launch_bounds__(256, DT == KB_F32 ? 2 : 3) quant_tile_kernel(c
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] = inf_to_nan(v[j]);
       }
-      const uint2 r = quant8<E5M2>(v, inv[0]);
+      const uint2 r = quant8<E5M2>(v, den[0], inv[0]);
       unsigned char* dst = p.q + (row0 + i) * p.ldq + col0;
       if (ncol == 8 && (VEC || p.q_vec)) {
         *reinterpret_cast<uint2*>(dst) = r;
@@ -220,7 +218,7 @@ __global__ void __launch_bounds__(256, DT == KB_F32 ? 2 : 3) quant_tile_kernel(c
       float c[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) c[i] = infinite ? inf_to_nan(h[i].get(j)) : h[i].get(j);
-      const uint2 r = quant8<E5M2>(c, inv[j]);
+      const uint2 r = quant8<E5M2>(c, den[TILES ? 0 : j], inv[TILES ? 0 : j]);
       *reinterpret_cast<uint2*>(st + transposed_at(cx * 8 + j, ry)) = r;
     }
     __syncthreads();

@@ -77,7 +77,8 @@ def _blocks32(v, fp8, tiles):
             fin = blk[blk.isfinite()].abs()
             a = torch.maximum(torch.tensor(2.0 ** -100), fin.max() if fin.numel() else torch.tensor(0.0))
             scale[b, r // step] = a / top
-            t = torch.minimum(torch.maximum(blk * (top / a), -top), top)
+            t = (blk * 0.875) / (a * (0.875 / FP8_MAX[fp8]))      # the last factor is a power of two
+            t = torch.minimum(torch.maximum(t, -top), top)
             t = torch.where(blk.isfinite(), t, torch.tensor(float("nan")))
             code[r:r + step, cols] = t.to(fp8).view(torch.uint8)
     return code, scale
@@ -111,6 +112,26 @@ def test_quantisation_bit_for_bit(ctx, rows, cols, tiles, transpose, fp8):
         code, want = _blocks32(x.t() if transpose else x, fp8, tiles)
         assert scale.shape == want.shape and bool((scale.cpu() == want).all())
         _same_codes(q, code, fp8)
+
+
+@pytest.mark.parametrize("tiles,transpose", [(False, False), (False, True), (True, False), (True, True)])
+@pytest.mark.parametrize("fp8", [torch.float8_e4m3fn, torch.float8_e5m2])
+def test_quotients_halfway_between_two_codes_go_to_the_even_one(ctx, tiles, transpose, fp8):
+    """16-bit inputs make quotients V F / a that lie exactly between two codes: against the definition
+    in 64 bits, code for code, with largest values of every bf16 significand."""
+    top = FP8_MAX[fp8]
+    sig = torch.arange(128, 256, dtype=torch.float64)
+    x = torch.zeros(128, 128, dtype=torch.float64)
+    x[:, :] = sig[None, :] * torch.exp2(-torch.arange(128)[:, None] % 9).double()
+    for amax in range(128, 256, 3):
+        v = torch.minimum(x, torch.tensor(float(amax)).double())
+        v[:, 0] = v[0, :] = amax
+        q, _ = ctx.quantize_blocks(v.to(torch.bfloat16).to(DEV), fp8, tiles=tiles, transpose=transpose)
+        t = (v.t() if transpose else v) * top / amax
+        bits, low = (3, -6) if fp8 == torch.float8_e4m3fn else (2, -14)
+        step = torch.exp2(torch.floor(torch.log2(t)).clamp_min(low) - bits)
+        want = torch.round(t / step) * step
+        assert bool((q.double().cpu() == want).all())
 
 
 @pytest.mark.parametrize("gap,offset", [(8, 0), (3, 0), (0, 1), (5, 3)])
