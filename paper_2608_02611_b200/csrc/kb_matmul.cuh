@@ -9,8 +9,9 @@
 // the shared-memory ring is one block of both operands, 128 bytes per row in the 128-byte
 // swizzle, and takes 4 matrix instructions.
 //
-// Roles: warp 0 copies (tensor maps; rows and columns outside a matrix read as zero), warp 1
-// issues matrix instructions, four warps scale and add.  Every wait is bounded.
+// Roles: warp 0 copies (tensor maps; rows and columns outside a matrix read as zero), warp 1 (and 3
+// in the pair kernel) issues matrix instructions, warp 2 fetches scales, warps from 4 on scale and
+// add.  Every wait on a barrier in shared memory is bounded.
 #pragma once
 
 #include "kb_block8.cuh"

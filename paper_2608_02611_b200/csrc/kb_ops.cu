@@ -173,7 +173,7 @@ kb_status launch_norm_bwd(kb_ctx* ctx, NormBwdParams& p, uint32_t* nparts, cudaS
   if (g == 1) return launch_norm_bwd<DT, 1, VEC, true>(ctx, p, 128, nparts, st);
   if (g == 2) return launch_norm_bwd<DT, 2, VEC, true>(ctx, p, 128, nparts, st);
   // one group per warp up to 16 warps; up to 24 where the rows are too few for the ring or cannot
-  // take it (777 x 5003 fp16: 19 us with two groups per warp, 14 with one and a row ahead)
+  // take it (777 x 5003 fp16: 19 us with two groups per warp, 17 with one and a row ahead)
   const bool few = !VEC || p.rows < 2ull * ctx->sm_count;
   if (few && g <= 24) return launch_norm_bwd<DT, 1, VEC, false>(ctx, p, 32 * g, nparts, st);
   if (g <= 32) return launch_norm_bwd<DT, 2, VEC, false>(ctx, p, 32 * ((g + 1) / 2), nparts, st);
