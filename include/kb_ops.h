@@ -46,9 +46,10 @@ typedef enum {
  *     V[r][c] ~ Q[r][c] * S[c / 128][r / 128]    KB_SCALE_TILES,  S is [ceil(C/128)][ceil(R/128)]
  * Per block, every operation rounded to binary32 once, F = 448 (KB_F8E4M3) or 57344 (KB_F8E5M2):
  *     a = max(2^-100, largest |V| that is finite);  S = a / F
- *     Q = round((V * 0.875) / (a * (0.875 / F)))       = V * F / a, its quotient rounded once before
- * with round-to-nearest-even to the format (0.875 / F is a power of two).  NaN and +-Inf become the format's NaN and do not
- * enter a.
+ *     Q = round((V * L * 0.875) / (a * L * (0.875 / F)))     = V * F / a, its quotient rounded once before
+ * with round-to-nearest-even to the format.  0.875 / F is a power of two; L = 2^40 for a < 2^-60 and 1
+ * elsewhere keeps the steps above binary32's smallest numbers.  NaN and +-Inf become the format's NaN and
+ * do not enter a.
  *
  *   d_x        DEVICE [rows][cols] of `dtype` (KB_F32, KB_F16 or KB_BF16), row stride ldx.
  *   transpose  0: V = x (R = rows, C = cols).  1: V = the transpose of x (R = cols, C = rows):

@@ -221,20 +221,25 @@ __device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) {
 // A block with largest magnitude a >= 2^-100 has the scale S = a / F, and its codes are the quotients
 // v F / a rounded.  Inputs of 8 or 11 significant bits make quotients that lie exactly between two
 // codes, and a product with a rounded F / a would send some of them the wrong way; so the quotient is
-// rounded correctly, as (v * 0.875) / (a 2^-kShift) with F = 1.75 * 2^(kShift - 1): neither side leaves the
-// range of binary32.
+// rounded correctly, as (v L * 0.875) / (a 2^-kShift L) with F = 1.75 * 2^(kShift - 1).  The remainder of that
+// division is a multiple of 2^-79 a L (quotients from 2^-17 on, half the smallest e5m2 step, and 23 bits
+// below each leading bit) and has to stay above binary32's smallest step, 2^-149.  So L = 2^40 for a
+// under kSmallMax, and 1 elsewhere.  Such blocks and those with an Inf are rare: one test per block finds
+// both, and only there the values are treated first.
 template <bool E5M2>
 struct Fp8 {
   static constexpr float kTop = E5M2 ? 57344.0f : 448.0f;
   static constexpr float kUnscale = E5M2 ? 0x1p-16f : 0x1p-9f;   // 2^-kShift
 };
 struct BlockScale {
-  float scale, den, inv;   // S, a 2^-kShift, 1 / den
+  float scale, den, inv;   // S, a 2^-kShift L, 1 / den
 };
-constexpr float kLeastMax = 0x1p-100f;
+constexpr float kLeastMax = 0x1p-100f, kSmallMax = 0x1p-60f;
+__device__ __forceinline__ float block_lift(float amax) { return amax < kSmallMax ? 0x1p40f : 1.0f; }   // L
+__device__ __forceinline__ bool block_is_rare(float amax) { return !(amax >= kSmallMax && amax <= 0x1.fffffep127f); }
 template <bool E5M2>
 __device__ __forceinline__ BlockScale block_scale(float amax) {
-  const float a = fmaxf(amax, kLeastMax), den = a * Fp8<E5M2>::kUnscale;
+  const float a = fmaxf(amax, kLeastMax), den = a * (Fp8<E5M2>::kUnscale * block_lift(a));
   return {__fdiv_rn(a, Fp8<E5M2>::kTop), den, __fdiv_rn(1.0f, den)};
 }
 // Two values to two codes (lo in the low byte), saturating; NaN becomes NaN.
@@ -247,8 +252,8 @@ __device__ __forceinline__ uint32_t quant2(float lo, float hi) {
     asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
   return r;
 }
-// (v * 0.875) / den, rounded correctly from the rounded reciprocal (Markstein 1990: a quotient estimate
-// within an ulp, corrected once by its exact remainder)
+// (v * 0.875) / den, v and den lifted where the block's maximum is small, rounded correctly from the rounded
+// reciprocal (Markstein 1990: a quotient estimate within an ulp, corrected once by its exact remainder)
 __device__ __forceinline__ void quotients(float& v0, float& v1, const Pair den, const Pair inv) {
   const Pair num = mul2(pair(v0, v1), pair(0.875f, 0.875f));
   const Pair t = mul2(num, inv);
@@ -278,7 +283,7 @@ __device__ __forceinline__ float max_abs(const float (&v)[8]) {
   for (int j = J0; j < J1; ++j) m = fmaxf(m, fabsf(v[j]));
   return m;
 }
-// For a block whose maximum is infinite: Inf becomes NaN; returns the largest finite magnitude.
+// For a block whose maximum may be infinite: Inf becomes NaN; returns the largest finite magnitude.
 template <int J0, int J1>
 __device__ __forceinline__ float settle_inf(float (&v)[8]) {
   float m = 0.0f;
@@ -288,6 +293,11 @@ __device__ __forceinline__ float settle_inf(float (&v)[8]) {
     m = fmaxf(m, fabsf(v[j]));
   }
   return m;
+}
+template <int J0, int J1>
+__device__ __forceinline__ void lift_values(float (&v)[8], float lift) {
+#pragma unroll
+  for (int j = J0; j < J1; ++j) v[j] *= lift;
 }
 __device__ __forceinline__ float warp_max(float v) {
 #pragma unroll
@@ -299,7 +309,7 @@ __device__ __forceinline__ float warp_max(float v) {
 // the others for the reciprocal, so the two cost one division.
 template <bool E5M2>
 __device__ __forceinline__ BlockScale shared_block_scale(float amax, unsigned int mask, int first, int lane) {
-  const float a = fmaxf(amax, kLeastMax), den = a * Fp8<E5M2>::kUnscale;
+  const float a = fmaxf(amax, kLeastMax), den = a * (Fp8<E5M2>::kUnscale * block_lift(a));
   const bool is_first = lane == first;
   const float r = __fdiv_rn(is_first ? a : 1.0f, is_first ? Fp8<E5M2>::kTop : den);
   return {r, den, __shfl_sync(mask, r, first + 1)};   // .scale holds in lane `first` only
@@ -324,13 +334,14 @@ __device__ __forceinline__ void quant_groups(float (&v)[NCH][8], uint32_t g0, ui
 #pragma unroll
       for (int i = 0; i < NCH; ++i) m[i] = fmaxf(m[i], __shfl_xor_sync(half, m[i], o));
 #pragma unroll
-    for (int i = 0; i < NCH; ++i) any |= isinf(m[i]);
+    for (int i = 0; i < NCH; ++i) any |= block_is_rare(m[i]);
     if (any) {   // the same for the 16 lanes of a block
 #pragma unroll
       for (int i = 0; i < NCH; ++i) {
         m[i] = settle_inf<0, 8>(v[i]);
 #pragma unroll
         for (int o = 8; o > 0; o >>= 1) m[i] = fmaxf(m[i], __shfl_xor_sync(half, m[i], o));
+        lift_values<0, 8>(v[i], block_lift(m[i]));
       }
     }
     BlockScale s[NCH];
@@ -367,8 +378,14 @@ __device__ __forceinline__ void quant_groups(float (&v)[NCH][8], uint32_t g0, ui
 #pragma unroll
     for (int i = 0; i < NCH; ++i) {
       const uint32_t g = g0 + i * gstep;
-      if (isinf(m[i][0])) m[i][0] = warp_max(settle_inf<0, 4>(v[i]));   // the same for the warp
-      if (isinf(m[i][1])) m[i][1] = warp_max(settle_inf<4, 8>(v[i]));
+      if (block_is_rare(m[i][0])) {   // the same for the warp
+        m[i][0] = warp_max(settle_inf<0, 4>(v[i]));
+        lift_values<0, 4>(v[i], block_lift(m[i][0]));
+      }
+      if (block_is_rare(m[i][1])) {
+        m[i][1] = warp_max(settle_inf<4, 8>(v[i]));
+        lift_values<4, 8>(v[i], block_lift(m[i][1]));
+      }
       // lanes 0..15 work out the first block's quotients, lanes 16..31 the second's
       const unsigned int half = 0xFFFFu << (lane & 16);
       const BlockScale s = shared_block_scale<E5M2>(lane < 16 ? m[i][0] : m[i][1], half, lane & 16, lane);

@@ -94,6 +94,8 @@ template <int DT, bool VEC, bool E5M2, bool TILES, bool TRANSPOSE>
 __global__ void __launch_bounds__(256, DT == KB_F32 ? 2 : 3) quant_tile_kernel(const QuantParams p) {
   __shared__ __align__(16) float smax[TILES ? 8 : 8 * 128];
   __shared__ __align__(16) float sinv[TILES ? 4 : 128], sden[TILES ? 4 : 128];
+  __shared__ float slift[TILES ? 1 : 128];
+  __shared__ int some_small;   // a column's maximum is (only written where TILES does not hold)
   __shared__ __align__(16) unsigned char st[TRANSPOSE ? 128 * 128 : 16];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int cx = threadIdx.x & 15, ry = threadIdx.x >> 4;
@@ -111,7 +113,7 @@ __global__ void __launch_bounds__(256, DT == KB_F32 ? 2 : 3) quant_tile_kernel(c
     else
       load_shifted<Elem<DT>::kBytes>(p.x, p.span, (row0 + i) * p.ldx + col0, ncol, h[i].w);
   }
-  bool infinite = false;   // the block (TILES: the tile) holds an Inf
+  bool rare = false;       // the tile holds an Inf, or a block of it has a small maximum
   __align__(16) float den[TILES ? 4 : 8], inv[TILES ? 4 : 8];   // per column of the thread, or of the tile
   if constexpr (TILES) {
     float m = 0.0f;
@@ -123,8 +125,8 @@ __global__ void __launch_bounds__(256, DT == KB_F32 ? 2 : 3) quant_tile_kernel(c
     if (lane == 0) smax[warp] = m;
     __syncthreads();
     m = warp_max(smax[lane & 7]);
-    infinite = isinf(m);
-    if (infinite) {   // the same for the whole CTA
+    rare = block_is_rare(m);
+    if (rare) {   // the same for the whole CTA
       float f = 0.0f;
 #pragma unroll
       for (int i = 0; i < 8; ++i)
@@ -135,6 +137,7 @@ __global__ void __launch_bounds__(256, DT == KB_F32 ? 2 : 3) quant_tile_kernel(c
       if (lane == 0) smax[warp] = f;
       __syncthreads();
       m = warp_max(smax[lane & 7]);
+      slift[0] = block_lift(m);   // by every thread: only needed, and read back, where `rare` holds
     }
     const BlockScale s = block_scale<E5M2>(m);
     den[0] = s.den;
@@ -174,20 +177,24 @@ __global__ void __launch_bounds__(256, DT == KB_F32 ? 2 : 3) quant_tile_kernel(c
         const BlockScale s = block_scale<E5M2>(t);
         sinv[threadIdx.x] = s.inv;
         sden[threadIdx.x] = s.den;
+        slift[threadIdx.x] = block_lift(t);
+        if (t < kSmallMax) some_small = 1;
         const uint64_t c = (uint64_t)ct * 128 + threadIdx.x;
         if (c < p.cols) p.scale[(uint64_t)rt * p.cols + c] = s.scale;
       }
       return isinf(t);
     };
+    if (threadIdx.x == 0) some_small = 0;
     columns(false);
     __syncthreads();
-    infinite = __syncthreads_or(column());
-    if (infinite) {
+    rare = __syncthreads_or(column());
+    if (rare) {
       columns(true);
       __syncthreads();
       column();
       __syncthreads();
     }
+    rare |= some_small != 0;
 #pragma unroll
     for (int j = 0; j < 8; j += 4) {
       *reinterpret_cast<float4*>(inv + j) = *reinterpret_cast<const float4*>(sinv + cx * 8 + j);
@@ -200,9 +207,10 @@ __global__ void __launch_bounds__(256, DT == KB_F32 ? 2 : 3) quant_tile_kernel(c
       if (i >= nrow) break;
       float v[8];
       h[i].all(v);
-      if (infinite) {
+      if (rare) {
+        const float lift = slift[0];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = inf_to_nan(v[j]);
+        for (int j = 0; j < 8; ++j) v[j] = inf_to_nan(v[j]) * lift;
       }
       const uint2 r = quant8<E5M2>(v, den[0], inv[0]);
       unsigned char* dst = p.q + (row0 + i) * p.ldq + col0;
@@ -217,7 +225,12 @@ __global__ void __launch_bounds__(256, DT == KB_F32 ? 2 : 3) quant_tile_kernel(c
     for (int j = 0; j < 8; ++j) {
       float c[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) c[i] = infinite ? inf_to_nan(h[i].get(j)) : h[i].get(j);
+      for (int i = 0; i < 8; ++i) c[i] = h[i].get(j);
+      if (rare) {
+        const float lift = slift[TILES ? 0 : cx * 8 + j];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) c[i] = inf_to_nan(c[i]) * lift;
+      }
       const uint2 r = quant8<E5M2>(c, den[TILES ? 0 : j], inv[TILES ? 0 : j]);
       *reinterpret_cast<uint2*>(st + transposed_at(cx * 8 + j, ry)) = r;
     }

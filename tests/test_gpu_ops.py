@@ -134,6 +134,43 @@ def test_quotients_halfway_between_two_codes_go_to_the_even_one(ctx, tiles, tran
         assert bool((q.double().cpu() == want).all())
 
 
+@pytest.mark.parametrize("tiles,transpose", [(False, False), (False, True), (True, False), (True, True)])
+@pytest.mark.parametrize("fp8", [torch.float8_e4m3fn, torch.float8_e5m2])
+def test_quotients_of_the_smallest_and_largest_blocks(ctx, tiles, transpose, fp8):
+    """The same with largest values of 2^-100 to 2^-90, around 2^-60 and at the top of the range, and quotients
+    down to half the smallest code: neither the division nor its remainder may lose bits to binary32's range."""
+    top = FP8_MAX[fp8]
+    bits, low, steps = (3, -6, 20) if fp8 == torch.float8_e4m3fn else (2, -14, 34)
+    sig = torch.arange(128, 256, dtype=torch.float64)
+    for e in [*range(-100, -89), -70, -61, -60, 100, 126, 127]:
+        x = sig[None, :] * torch.exp2(float(e - 7) - (torch.arange(128)[:, None] % steps).double())
+        for m in (*range(128, 256, 9), 167, 224, 231):
+            amax = m * 2.0 ** (e - 7)
+            v = torch.minimum(x, torch.tensor(amax).double())
+            v[:, 0] = v[0, :] = amax
+            v = v.to(torch.bfloat16)                        # the smallest lose bits to the type, before the call
+            q, scale = ctx.quantize_blocks(v.to(DEV), fp8, tiles=tiles, transpose=transpose)
+            assert bool((scale.cpu() == (torch.tensor(amax, dtype=torch.float32) / top)).all())
+            t = (v.t() if transpose else v).double() * top / amax
+            step = torch.exp2(torch.floor(torch.log2(t.clamp_min(2.0 ** -60))).clamp_min(low) - bits)
+            assert bool((q.double().cpu() == torch.round(t / step) * step).all()), (e, m)
+
+
+@pytest.mark.parametrize("exponent", [-100, -97, -80, -62, -59])
+@pytest.mark.parametrize("fp8", [torch.float8_e4m3fn, torch.float8_e5m2])
+def test_quantisation_of_tiny_binary32_blocks_bit_for_bit(ctx, exponent, fp8):
+    """Elements down to and below binary32's smallest normal value, in blocks of tiny largest values."""
+    gen = _gen(exponent + 200)
+    x = torch.rand(64, 256, generator=gen) * torch.exp2(-40.0 * torch.rand(64, 256, generator=gen)) * 2.0 ** exponent
+    x[:, ::2].neg_()
+    x[:, ::128] = 1.3 * 2.0 ** exponent
+    q, scale = ctx.quantize_blocks(x.to(DEV), fp8)
+    want = _blocks32(x, fp8, False)[1]
+    code = _blocks32(x * 2.0 ** 40 if exponent < -60 else x, fp8, False)[0]
+    assert bool((scale.cpu() == want).all())
+    _same_codes(q, code, fp8)
+
+
 @pytest.mark.parametrize("gap,offset", [(8, 0), (3, 0), (0, 1), (5, 3)])
 @pytest.mark.parametrize("tiles,transpose", [(False, False), (False, True), (True, False), (True, True)])
 def test_quantisation_of_strided_and_unaligned_rows(ctx, gap, offset, tiles, transpose):
