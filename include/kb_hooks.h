@@ -47,6 +47,11 @@ kb_status kb_ctx_set_filter(kb_ctx* ctx, int mode);
  * 3 by definition. */
 kb_status kb_ctx_last_filter(const kb_ctx* ctx, int* mode);
 
+/* The kernel of this context's last kb_matmul_blocks that launched one (HOST out): *rows = 16, 32, 64
+ * or 128, the rows of A per tile of the kernel for few rows, or 256 for the kernel of CTA pairs;
+ * *splits = CTAs that share a tile's K blocks.  Both 0 before the first. */
+kb_status kb_ctx_last_product(const kb_ctx* ctx, uint32_t* rows, uint32_t* splits);
+
 /* ---- instrumentation (used by the benchmark) ------------------------------ */
 
 typedef enum {

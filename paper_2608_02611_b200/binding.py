@@ -50,7 +50,7 @@ EXPORTS = [
     "kb_mask_create_strided", "kb_mask_create_bitmap", "kb_mask_count", "kb_mask_destroy",
     "kb_screen", "kb_screen_f64", "kb_screen_host", "kb_screen_static", "kb_screen_indexed", "kb_screen_multi", "kb_merge_ranges", "kb_adjudicate", "kb_adjudicate_ragged", "kb_select",
     "kb_select_by_score", "kb_tail_ratios", "kb_copeland", "kb_confirm",
-    "kb_ctx_fail_next_allocs", "kb_ctx_selftest_wait", "kb_ctx_check_guards", "kb_static_scratch_read", "kb_ctx_set_filter", "kb_ctx_last_filter",
+    "kb_ctx_fail_next_allocs", "kb_ctx_selftest_wait", "kb_ctx_check_guards", "kb_static_scratch_read", "kb_ctx_set_filter", "kb_ctx_last_filter", "kb_ctx_last_product",
     "kb_quantize_blocks", "kb_layernorm", "kb_layernorm_backward", "kb_matmul_blocks",
 ]
 
@@ -92,6 +92,7 @@ def load() -> ctypes.CDLL:
     L.kb_ctx_set_dependent_launch.argtypes = [vp, i32]
     L.kb_ctx_set_filter.argtypes = [vp, i32]
     L.kb_ctx_last_filter.argtypes = [vp, ctypes.POINTER(i32)]
+    L.kb_ctx_last_product.argtypes = [vp, ctypes.POINTER(u32), ctypes.POINTER(u32)]
     L.kb_ctx_fail_next_allocs.argtypes = [vp, u32, u32]
     L.kb_ctx_check_guards.argtypes = [vp, vp, ctypes.POINTER(u32), ctypes.POINTER(u32)]
     L.kb_static_scratch_read.argtypes = [vp, u32]
@@ -264,6 +265,14 @@ class Context:
         v = ctypes.c_int(0)
         self._check(load().kb_ctx_last_filter(self._h, ctypes.byref(v)), "kb_ctx_last_filter")
         return int(v.value)
+
+    @property
+    def last_product(self):
+        """(rows of A per tile, CTAs per tile) of the last product's launch: 16 to 128 rows for the kernel for
+        few rows, 256 for the kernel of CTA pairs."""
+        rows, splits = ctypes.c_uint32(0), ctypes.c_uint32(0)
+        self._check(load().kb_ctx_last_product(self._h, ctypes.byref(rows), ctypes.byref(splits)), "kb_ctx_last_product")
+        return int(rows.value), int(splits.value)
 
     def set_wins_algo(self, algo: int):
         """0 automatic, 1 direct comparison of all sample pairs, 2 binary search on sorted rows,

@@ -85,6 +85,7 @@ struct kb_ctx {
   void* encode_tiled = nullptr;     // the driver's tensor-map encoder, looked up at first use
   int cluster_room[9] = {};         // clusters of n CTAs, one CTA per SM, that run at the same time
   bool ops_ready = false;           // shared-memory limits of the operators' kernels are raised
+  uint32_t product_rows = 0, product_splits = 0;   // of the last product's launch: rows of A per tile, CTAs per tile
 };
 
 namespace kb {

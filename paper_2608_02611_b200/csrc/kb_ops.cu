@@ -3,6 +3,7 @@
 #include <algorithm>
 #include <cmath>
 
+#include "../../include/kb_hooks.h"
 #include "../../include/kb_ops.h"
 #include "kb_ctx.cuh"
 #include "kb_matmul.cuh"
@@ -302,6 +303,8 @@ kb_status launch_lanes(kb_ctx* ctx, MatmulParams& p, const void* a, uint64_t lda
     KB_CUDA(ctx, cudaLaunchKernelEx(&cfg, matmul_lanes_kernel<BN, false>, map_b, map_a, p));
   else
     KB_CUDA(ctx, cudaLaunchKernelEx(&cfg, matmul_lanes_kernel<BN, true>, map_b, map_a, p));
+  ctx->product_rows = BN;
+  ctx->product_splits = splits;
   return launched(ctx);
 }
 
@@ -320,6 +323,8 @@ kb_status launch_pair(kb_ctx* ctx, MatmulParams& p, const void* a, uint64_t lda,
     matmul_pair_kernel<false><<<2 * pairs, PairTile::kThreads, PairTile::kSmem, st>>>(map_a, map_b, p);
   else
     matmul_pair_kernel<true><<<2 * pairs, PairTile::kThreads, PairTile::kSmem, st>>>(map_a, map_b, p);
+  ctx->product_rows = 256;
+  ctx->product_splits = 1;
   return launched(ctx);
 }
 
@@ -328,6 +333,13 @@ kb_status launch_pair(kb_ctx* ctx, MatmulParams& p, const void* a, uint64_t lda,
 // ---------------------------------------------------------------------------
 // entry points
 // ---------------------------------------------------------------------------
+
+extern "C" kb_status kb_ctx_last_product(const kb_ctx* ctx, uint32_t* rows, uint32_t* splits) {
+  if (!ctx || !rows || !splits) return KB_ERR_INVALID_ARG;
+  *rows = ctx->product_rows;
+  *splits = ctx->product_splits;
+  return KB_OK;
+}
 
 extern "C" kb_status kb_quantize_blocks(kb_ctx* ctx, const void* d_x, uint64_t rows, uint64_t cols, uint64_t ldx,
                                         kb_dtype dtype, int transpose, kb_scale_mode mode, void* d_q, uint64_t ldq,
