@@ -30,6 +30,11 @@ struct MatmulParams {
   uint32_t tiles_m;          // column tiles (of A's rows)
   uint32_t splits;           // CTAs per tile along K (a cluster)
   uint32_t idesc;
+  const unsigned char* a;    // the codes themselves, for the rows that recompute_wide_rows takes
+  const unsigned char* b;
+  uint64_t lda, ldb;
+  uint32_t K;
+  bool a_e5m2, b_e5m2;
   int out;                   // kb_dtype of D
   bool vec_out;              // rows of D start on 16-byte boundaries
   unsigned int* status;
@@ -97,6 +102,26 @@ __device__ __forceinline__ void fma_pair(float& c0, float& c1, float v0, float v
       "fma.rn.f32x2 c, v, s, c;\nmov.b64 {%0, %1}, c;\n}"
       : "+f"(c0), "+f"(c1)
       : "f"(v0), "f"(v1), "f"(s0), "f"(s1));
+}
+
+// ---- scales at the ends of binary32's range ------------------------------------------------------
+// A block's sum is 0 or between 2^-32 and 2^39 in magnitude.  With a first scale in [2^-94, 2^88] its
+// product with that stays a normal number, and the second scale overflows or underflows only where the
+// result does.  Of a first scale outside ("wide"), a power of two goes over to the second: where that one
+// then leaves the range, the result does too.  Rows whose scale is not wide get 1 and add as ever.
+__device__ __forceinline__ bool scale_is_wide(float s) {   // 0, Inf and NaN are not
+  const float a = fabsf(s);
+  return (a > 0.0f && a < 0x1p-94f) || (a > 0x1p88f && a <= 0x1.fffffep127f);
+}
+__device__ __forceinline__ float take_over(float& first) {   // returns the second scale's factor
+  if (!scale_is_wide(first)) return 1.0f;
+  const bool up = fabsf(first) < 1.0f;
+  first *= up ? 0x1p40f : 0x1p-40f;
+  return up ? 0x1p-40f : 0x1p40f;
+}
+// Tile scales are multiplied with each other first, which takes a product that is a normal number.
+__device__ __forceinline__ bool product_is_wide(float s, float s1, float s2) {   // s = s1 * s2
+  return !(fabsf(s) >= 0x1p-126f && fabsf(s) <= 0x1.fffffep127f) && s1 != 0.0f && s2 != 0.0f && isfinite(s1) && isfinite(s2);
 }
 
 // BROWS: B has one scale per row (per lane of the tile) instead of one per 128 rows.
@@ -245,25 +270,34 @@ __global__ void __launch_bounds__(LaneTile<BN>::kThreads, 1)
       ok &= mbar_wait_bounded(&acc_full[a], a_phase, abort_flag, p.status);
       __syncwarp();
       tc_fence_after();
-      constexpr int kCols = T::kEpiCols < 32 ? 16 : 32;
+      auto add_block = [&](float first, auto over) {
+        constexpr int kCols = T::kEpiCols < 32 ? 16 : 32;
 #pragma unroll
-      for (int j0 = 0; j0 < T::kEpiCols; j0 += kCols) {
-        float v[kCols];
-        if constexpr (kCols == 16)
-          tmem_ld16(taddr + a * BN + j0, v);
-        else
-          tmem_ld32(taddr + a * BN + j0, v);
-        tmem_wait_ld();
-        if (j0 + kCols == T::kEpiCols) {   // all of this accumulator is in registers
-          tc_fence_before();
-          mbar_arrive_if(&acc_empty[a], lane == 0);
-        }
+        for (int j0 = 0; j0 < T::kEpiCols; j0 += kCols) {
+          float v[kCols];
+          if constexpr (kCols == 16)
+            tmem_ld16(taddr + a * BN + j0, v);
+          else
+            tmem_ld32(taddr + a * BN + j0, v);
+          tmem_wait_ld();
+          if (j0 + kCols == T::kEpiCols) {   // all of this accumulator is in registers
+            tc_fence_before();
+            mbar_arrive_if(&acc_empty[a], lane == 0);
+          }
 #pragma unroll
-        for (int j = 0; j < kCols; j += 4) {
-          const float4 f = *reinterpret_cast<const float4*>(c + j0 + j);
-          fma_pair(acc[j0 + j], acc[j0 + j + 1], v[j] * ls, v[j + 1] * ls, f.x, f.y);
-          fma_pair(acc[j0 + j + 2], acc[j0 + j + 3], v[j + 2] * ls, v[j + 3] * ls, f.z, f.w);
+          for (int j = 0; j < kCols; j += 4) {
+            const float4 f = over(*reinterpret_cast<const float4*>(c + j0 + j));
+            fma_pair(acc[j0 + j], acc[j0 + j + 1], v[j] * first, v[j + 1] * first, f.x, f.y);
+            fma_pair(acc[j0 + j + 2], acc[j0 + j + 3], v[j + 2] * first, v[j + 3] * first, f.z, f.w);
+          }
         }
+      };
+      if (!__any_sync(0xFFFFFFFFu, scale_is_wide(ls))) {   // the reads of tensor memory are the whole warp's
+        add_block(ls, [](float4 f) { return f; });
+      } else {
+        float first = ls;
+        const float t = take_over(first);
+        add_block(first, [t](float4 f) { return make_float4(f.x * t, f.y * t, f.z * t, f.w * t); });
       }
       if (k == kScaleStep - 1) {
         __syncwarp();
@@ -410,6 +444,68 @@ __device__ __forceinline__ void store_warp_tile(const MatmulParams& p, unsigned 
   }
 }
 
+// Tile scales: the rows, of 32 rows x 128 columns of D (one tile of B), for which some K block's product of
+// scales is no normal number, element by element in plain arithmetic.  Such scales come from values around
+// 2^-60, or 2^60, on both sides at once, so nothing of this stands in the loops of the kernel: a second
+// path there cost 11% of 8192^3, and four branches per K block 4%.  Rows whose codes are 0 wherever the
+// product underflows are left alone.
+template <bool E5M2>
+__device__ __forceinline__ void widen_codes(uint32_t w, float (&v)[4]) {
+  uint32_t lo, hi;
+  ElemF8<E5M2>::widen4(w, lo, hi);
+  const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&lo)), b = __half22float2(*reinterpret_cast<const __half2*>(&hi));
+  v[0] = a.x;
+  v[1] = a.y;
+  v[2] = b.x;
+  v[3] = b.y;
+}
+// four codes from column k on of a row (16-byte aligned, k a multiple of 4) of K columns, 0 past its end
+__device__ __forceinline__ uint32_t code_word(const unsigned char* row, uint32_t k, uint32_t K) {
+  if (k + 4 <= K) return *reinterpret_cast<const uint32_t*>(row + k);
+  uint32_t w = 0;
+  for (uint32_t j = 0; k + j < K; ++j) w |= (uint32_t)row[k + j] << (8 * j);
+  return w;
+}
+__device__ __forceinline__ void recompute_wide_rows(const MatmulParams& p, uint32_t m0, uint32_t n0, int lane) {
+  if (n0 >= p.N) return;
+  const float* bs = p.b_scale + (n0 >> 7);
+  const uint32_t row = m0 + lane;
+  bool need = false;
+  for (uint32_t kb = 0; row < p.M && kb < p.KB && !need; ++kb) {
+    const float r = p.a_scale[(uint64_t)kb * p.M + row], c = bs[(uint64_t)kb * p.b_scale_ld], s = r * c;
+    if (!product_is_wide(s, r, c)) continue;
+    need = fabsf(s) > 1.0f;
+    for (uint32_t k = 0; k < 128 && !need && kb * 128 + k < p.K; k += 4)
+      need = (code_word(p.a + row * p.lda, kb * 128 + k, p.K) & 0x7F7F7F7Fu) != 0;
+  }
+  for (uint32_t rows = __ballot_sync(0xFFFFFFFFu, need); rows; rows &= rows - 1) {
+    const uint32_t m = m0 + __ffs(rows) - 1;
+#pragma unroll 1
+    for (uint32_t n = n0 + lane; n < n0 + 128 && n < p.N; n += 32) {
+      float d = 0.0f;
+      for (uint32_t kb = 0; kb < p.KB; ++kb) {
+        float first = p.a_scale[(uint64_t)kb * p.M + m], second = bs[(uint64_t)kb * p.b_scale_ld], v = 0.0f;
+        for (uint32_t k = kb * 128; k < kb * 128 + 128 && k < p.K; k += 4) {
+          const uint32_t wa = code_word(p.a + m * p.lda, k, p.K), wb = code_word(p.b + n * p.ldb, k, p.K);
+          float x[4], y[4];
+          p.a_e5m2 ? widen_codes<true>(wa, x) : widen_codes<false>(wa, x);
+          p.b_e5m2 ? widen_codes<true>(wb, y) : widen_codes<false>(wb, y);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) v = fmaf(x[j], y[j], v);
+        }
+        if (product_is_wide(first * second, first, second)) {
+          second *= take_over(first);
+        } else {
+          second *= first;
+          first = 1.0f;
+        }
+        d = fmaf(v * first, second, d);
+      }
+      store_down<1>(p, m, n, &d);
+    }
+  }
+}
+
 // BROWS: B has one scale per row (per column of the tile) instead of one per 128 rows.
 template <bool BROWS>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PairTile::kThreads, 1)
@@ -419,8 +515,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PairTile::kThreads, 
   extern __shared__ unsigned char dyn[];
   __shared__ uint64_t full[T::kStages], done[T::kStages], acc_empty[2], drained[2];
   __shared__ uint64_t sc_full[T::kScaleSlots], sc_empty[T::kScaleSlots];
+  __shared__ uint64_t stored;
   __shared__ uint32_t tmem_base;
-  __shared__ unsigned int abort_word;
+  __shared__ unsigned int abort_word, redo_word;
   __shared__ __align__(16) float row_scale[T::kScaleSlots][128][kScaleStep];
   __shared__ __align__(16) float col_scale[T::kScaleSlots][BROWS ? kScaleStep * 256 : 2 * kScaleStep];
   volatile unsigned int* abort_flag = &abort_word;
@@ -443,7 +540,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PairTile::kThreads, 
       mbar_init(&sc_full[i], 32);
       mbar_init(&sc_empty[i], T::kEpiWarps);
     }
-    abort_word = 0u;
+    mbar_init(&stored, T::kEpiWarps);
+    abort_word = redo_word = 0u;
     mbar_fence_init();
   }
   if (warp == 1) tmem_alloc<2>(&tmem_base, T::kTmemCols);
@@ -561,6 +659,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PairTile::kThreads, 
     }
     cp_async_wait_all();
     __syncwarp();
+    if constexpr (!BROWS) {
+      // once everything is stored (nothing waits for this warp any more): the rows with scales that need it
+      ok = ok && __all_sync(0xFFFFFFFFu, mbar_wait_bounded(&stored, 0, abort_flag, p.status)) && !*abort_flag;
+      for (uint32_t t = first; t < tiles && ok && redo_word; t += step) {
+        uint32_t tm, tn;
+        pair_tile(t, p.tiles_m, tiles_n, tm, tn);
+        for (uint32_t part = 0; part < 8; ++part)
+          recompute_wide_rows(p, tm * 256 + rank * 128 + (part & 3) * 32, tn * 256 + (part >> 2) * 128, lane);
+      }
+    }
   } else if (warp >= 4) {
     regs_grow<T::kRegsEpi>();
     const int quarter = warp & 3, cols = ((warp - 4) >> 2) * 128;   // 32 rows and 128 columns of the tile
@@ -579,12 +687,21 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PairTile::kThreads, 
         ok &= mbar_wait_bounded(&sc_full[slot], slot_phase, abort_flag, p.status);
         const float4 rs = *reinterpret_cast<const float4*>(row_scale[slot][quarter * 32 + lane]);
         float s4[4] = {rs.x, rs.y, rs.z, rs.w};
-        if constexpr (!BROWS) {
+        bool wide = false;
+        if constexpr (BROWS) {
+#pragma unroll
+          for (int k = 0; k < 4; ++k) wide |= scale_is_wide(s4[k]);
+          wide = __any_sync(0xFFFFFFFFu, wide);   // one path for the warp, whose reads of tensor memory are collective
+        } else {
           const float4 cs = *reinterpret_cast<const float4*>(&col_scale[slot][(cols >> 7) * kScaleStep]);
-          s4[0] *= cs.x;
-          s4[1] *= cs.y;
-          s4[2] *= cs.z;
-          s4[3] *= cs.w;
+          const float c4[4] = {cs.x, cs.y, cs.z, cs.w};
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const float r = s4[k];
+            s4[k] *= c4[k];
+            wide |= product_is_wide(s4[k], r, c4[k]);
+          }
+          if (wide) redo_word = 1u;
         }
 #pragma unroll 1
         for (uint32_t k = 0; k < kScaleStep && kb0 + k < p.KB; ++k) {
@@ -600,22 +717,31 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PairTile::kThreads, 
             st = 0;
             st_phase ^= 1u;
           }
+          auto add_block = [&](float first, auto second) {   // acc += (v * first) * second, tile scales: v * first
 #pragma unroll
-          for (int j0 = 0; j0 < 128; j0 += 32) {
-            float v[32];
-            tmem_ld32(taddr + a * 256 + j0, v);
-            tmem_wait_ld();
-            if (j0 == 96) {   // all of this accumulator is in registers
-              tc_fence_before();
-              mbar_arrive_cluster_if(release0 + a * 8, lane == 0);
-            }
+            for (int j0 = 0; j0 < 128; j0 += 32) {
+              float v[32];
+              tmem_ld32(taddr + a * 256 + j0, v);
+              tmem_wait_ld();
+              if (j0 == 96) {   // all of this accumulator is in registers
+                tc_fence_before();
+                mbar_arrive_cluster_if(release0 + a * 8, lane == 0);
+              }
 #pragma unroll
-            for (int j = 0; j < 32; j += 4) {
-              const float4 f = BROWS ? *reinterpret_cast<const float4*>(c + j0 + j) : make_float4(1.0f, 1.0f, 1.0f, 1.0f);
-              fma_pair(acc[j0 + j], acc[j0 + j + 1], BROWS ? v[j] * f.x : v[j], BROWS ? v[j + 1] * f.y : v[j + 1], s, s);
-              fma_pair(acc[j0 + j + 2], acc[j0 + j + 3], BROWS ? v[j + 2] * f.z : v[j + 2],
-                       BROWS ? v[j + 3] * f.w : v[j + 3], s, s);
+              for (int j = 0; j < 32; j += 4) {
+                const float4 f = BROWS ? second(*reinterpret_cast<const float4*>(c + j0 + j)) : make_float4(first, first, first, first);
+                fma_pair(acc[j0 + j], acc[j0 + j + 1], BROWS ? v[j] * first : v[j], BROWS ? v[j + 1] * first : v[j + 1], f.x, f.y);
+                fma_pair(acc[j0 + j + 2], acc[j0 + j + 3], BROWS ? v[j + 2] * first : v[j + 2],
+                         BROWS ? v[j + 3] * first : v[j + 3], f.z, f.w);
+              }
             }
+          };
+          if (!BROWS || !wide) {
+            add_block(s, [](float4 f) { return f; });
+          } else {
+            float first = s;
+            const float t = take_over(first);
+            add_block(first, [t](float4 f) { return make_float4(f.x * t, f.y * t, f.z * t, f.w * t); });
           }
           a ^= 1u;
         }
@@ -637,6 +763,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PairTile::kThreads, 
         else
           store_warp_tile<KB_F32>(p, out_buf, lane, m0, n0, acc);
       }
+    }
+    if constexpr (!BROWS) {
+      __syncwarp();
+      mbar_arrive_if(&stored, lane == 0);
     }
   }
   tc_fence_before();

@@ -541,6 +541,13 @@ extern "C" kb_status kb_matmul_blocks(kb_ctx* ctx, const void* d_a, uint64_t lda
   p.KB = (uint32_t)((K + KB_BLOCK - 1) / KB_BLOCK);
   p.b_scale_shift = b_mode == KB_SCALE_TILES ? 7 : 0;
   p.b_scale_ld = b_mode == KB_SCALE_TILES ? (p.N + 127) / 128 : p.N;
+  p.a = static_cast<const unsigned char*>(d_a);
+  p.b = static_cast<const unsigned char*>(d_b);
+  p.lda = lda;
+  p.ldb = ldb;
+  p.K = (uint32_t)K;
+  p.a_e5m2 = a_dtype == KB_F8E5M2;
+  p.b_e5m2 = b_dtype == KB_F8E5M2;
   p.out = (int)d_dtype;
   p.status = ctx->d_status;
   p.vec_out = rows_aligned(d_d, ldd, e);

@@ -112,3 +112,46 @@ def test_product_of_few_rows_over_long_contractions(ctx, M, N, K, rows, splits, 
         assert -(-K // 128) // shared > 16
         _within(d, want, _product_bound(want, size, K, out))
         assert bool((ctx.matmul_blocks(a, sa, b, sb, out_dtype=out) == d).all())
+
+
+SCALES = [2.0 ** e for e in (65, -72, -100, 112, -109, 127, -126, 90)]
+
+
+@pytest.mark.parametrize("M,N,K,rows", [(5, 700, 500, 16), (20, 1100, 700, 32), (60, 900, 300, 64), (110, 1300, 500, 128),
+                                        (2305, 2111, 500, 256), (2500, 2401, 1300, 256)])
+@pytest.mark.parametrize("tiles", [True, False])
+def test_product_with_scales_at_the_ends_of_the_range(ctx, M, N, K, rows, tiles):
+    """Scales whose product, or whose product with a block's sum, leaves binary32 although the result does
+    not: against 64 bits wherever the sum of magnitudes stays under 2^127.  Beside the usual bound, each of the
+    kb additions and the products before it may lose 2^-150 to the smallest numbers."""
+    a, sa, b, sb = _case(M, N, K, tiles)
+    clean = ctx.matmul_blocks(a, sa, b, sb, out_dtype=torch.float32)
+    step = 128 if tiles else 1
+    touched_m, touched_n = torch.zeros(M, dtype=torch.bool, device=DEV), torch.zeros(N, dtype=torch.bool, device=DEV)
+    sa, sb = sa.clone(), sb.clone()
+    picks = sorted({min(M - 1, 1 + 37 * i) for i in range(2 * len(SCALES))})
+    for i, m in enumerate(picks):
+        sa[:, m] = SCALES[i % len(SCALES)]
+        if M > 100:
+            sa[i % sa.shape[0], m] = 0.01                  # one block of the row stays ordinary
+        touched_m[m] = True
+    a.view(torch.uint8)[picks[0]] = 0x80                   # codes of -0: sums of 0 under every scale
+    a.view(torch.uint8)[picks[-1]] = 0x7E                  # the largest codes
+    for i in range(len(SCALES)):
+        n = min(sb.shape[1] - 1, i if tiles else 1 + 53 * i)
+        sb[:, n] = SCALES[(3 * i + 1) % len(SCALES)]
+        touched_n[n * step:(n + 1) * step] = True
+    want, size = _product64(a, sa, b, sb, tiles)
+    kb = -(-K // 128)
+    for out in (torch.float32, torch.bfloat16):
+        d = ctx.matmul_blocks(a, sa, b, sb, out_dtype=out)
+        assert ctx.last_product[0] == rows
+        inside = size < 2.0 ** 127
+        assert bool(d[inside].isfinite().all())
+        bound = _product_bound(want, size, K, out) + (kb + 2) * 2.0 ** -149
+        _within(d[inside], want[inside], bound[inside])
+        assert bool((d[picks[0]] == 0.0).all())
+        if out == torch.float32:
+            same = ~touched_m[:, None] & ~touched_n[None, :]
+            assert bool((d[same] == clean[same]).all())
+        assert bool((ctx.matmul_blocks(a, sa, b, sb, out_dtype=out)[inside] == d[inside]).all())
