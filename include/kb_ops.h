@@ -89,13 +89,20 @@ kb_status kb_layernorm(kb_ctx* ctx, const void* d_x, uint64_t rows, uint64_t col
  *   d_mean, d_rstd   DEVICE binary32 [rows], what the forward pass wrote.
  *   d_dx             DEVICE [rows][cols] of `dtype`, row stride lddx; NULL: not written.
  *   d_dweight, d_dbias  DEVICE [cols] of `param_dtype`; NULL: not written.
- * At least one output is not NULL.  Partial sums over rows live in the context's workspace,
- * which grows on demand. */
+ * At least one output is not NULL.  Partial sums over rows live in the context's workspace, which
+ * grows on demand.  A call that is captured into a graph uses the workspace as it is: it is refused with
+ * KB_ERR_WORKSPACE if that would have to grow (kb_layernorm_backward_reserve, or such a call outside the
+ * capture, makes room first).  Later growth leaves what a graph uses in place; a graph must not run after
+ * the context is destroyed, nor at the same time as another call or graph on the context. */
 kb_status kb_layernorm_backward(kb_ctx* ctx, const void* d_dy, uint64_t lddy, const void* d_x,
                                 uint64_t ldx, uint64_t rows, uint64_t cols, kb_dtype dtype,
                                 const void* d_weight, kb_dtype param_dtype, const float* d_mean,
                                 const float* d_rstd, void* d_dx, uint64_t lddx, void* d_dweight,
                                 void* d_dbias, void* stream);
+
+/* Room for backward passes over at most `rows` rows of `cols` columns, whatever their types and strides.
+ * `stream` is only asked whether it is being captured (then the call is refused where it would allocate). */
+kb_status kb_layernorm_backward_reserve(kb_ctx* ctx, uint64_t rows, uint64_t cols, void* stream);
 
 /* ---- product of two block-quantised matrices ---------------------------------------------
  *

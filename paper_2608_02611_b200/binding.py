@@ -51,7 +51,7 @@ EXPORTS = [
     "kb_screen", "kb_screen_f64", "kb_screen_host", "kb_screen_static", "kb_screen_indexed", "kb_screen_multi", "kb_merge_ranges", "kb_adjudicate", "kb_adjudicate_ragged", "kb_select",
     "kb_select_by_score", "kb_tail_ratios", "kb_copeland", "kb_confirm",
     "kb_ctx_fail_next_allocs", "kb_ctx_selftest_wait", "kb_ctx_check_guards", "kb_static_scratch_read", "kb_ctx_set_filter", "kb_ctx_last_filter", "kb_ctx_last_product",
-    "kb_quantize_blocks", "kb_layernorm", "kb_layernorm_backward", "kb_matmul_blocks",
+    "kb_quantize_blocks", "kb_layernorm", "kb_layernorm_backward", "kb_layernorm_backward_reserve", "kb_matmul_blocks",
 ]
 
 
@@ -118,6 +118,7 @@ def load() -> ctypes.CDLL:
     L.kb_quantize_blocks.argtypes = [vp, vp, u64, u64, u64, i32, i32, i32, vp, u64, i32, vp, vp]
     L.kb_layernorm.argtypes = [vp, vp, u64, u64, u64, i32, vp, vp, i32, f32, vp, u64, vp, vp, vp, u64, i32, vp, vp]
     L.kb_layernorm_backward.argtypes = [vp, vp, u64, vp, u64, u64, u64, i32, vp, i32, vp, vp, vp, u64, vp, vp, vp]
+    L.kb_layernorm_backward_reserve.argtypes = [vp, u64, u64, vp]
     L.kb_matmul_blocks.argtypes = [vp, vp, u64, i32, vp, vp, u64, i32, vp, i32, u64, u64, u64, vp, u64, i32, vp]
     for name in EXPORTS:
         if name != "kb_last_error":
@@ -667,6 +668,14 @@ def layernorm_backward(self, dy: torch.Tensor, x: torch.Tensor, weight: Optional
     type (binary32 without a weight); dbias is None unless ``want_bias``."""
     return (_native_module or _native()).layernorm_backward(self._h, self.device.index, dy, x, weight, mean, rstd,
                                                             want_bias)
+
+
+@_ctx_method
+def reserve_layernorm_backward(self, rows: int, cols: int):
+    """kb_layernorm_backward_reserve: workspace for backward passes over at most ``rows`` rows of ``cols`` columns,
+    for calls that are then captured into a CUDA graph (a capture cannot allocate it)."""
+    self._check(load().kb_layernorm_backward_reserve(self._h, rows, cols, _stream_ptr(self.device)),
+                "kb_layernorm_backward_reserve")
 
 
 @_ctx_method

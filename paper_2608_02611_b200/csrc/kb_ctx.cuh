@@ -82,6 +82,8 @@ struct kb_ctx {
   // model operators (kb_ops.h)
   unsigned char* ops_ws = nullptr;  // partial sums of the norm's parameter gradients
   size_t ops_ws_bytes = 0;
+  bool ops_ws_captured = false;     // its address is in a captured launch: it is never freed before the context is
+  std::vector<unsigned char*> ops_ws_outgrown;
   void* encode_tiled = nullptr;     // the driver's tensor-map encoder, looked up at first use
   int cluster_room[9] = {};         // clusters of n CTAs, one CTA per SM, that run at the same time
   bool ops_ready = false;           // shared-memory limits of the operators' kernels are raised

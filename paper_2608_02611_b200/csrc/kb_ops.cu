@@ -134,6 +134,44 @@ kb_status launch_norm(kb_ctx* ctx, const NormParams& p, bool vec, bool e5m2, cud
               : e5m2 ? launch_norm<DT, false, 2>(ctx, p, st) : launch_norm<DT, false, 1>(ctx, p, st);
 }
 
+// The workspace of partial sums, with room for `need` bytes.  A launch that is being captured into a graph
+// keeps its address: from then on a buffer that is outgrown stays allocated until the context goes, and
+// growing (an allocation) is refused while the stream is captured.
+kb_status ensure_partials(kb_ctx* ctx, size_t need, cudaStream_t st) {
+  cudaStreamCaptureStatus status = cudaStreamCaptureStatusNone;
+  if (cudaStreamIsCapturing(st, &status) != cudaSuccess) {
+    cudaGetLastError();   // the default stream while another stream is captured
+    status = cudaStreamCaptureStatusActive;
+  }
+  const bool capturing = status != cudaStreamCaptureStatusNone;
+  if (need > ctx->ops_ws_bytes) {
+    if (capturing)
+      return fail(ctx, KB_ERR_WORKSPACE,
+                  "the workspace of partial parameter gradients would have to grow to %zu bytes while the stream is "
+                  "captured: call kb_layernorm_backward_reserve before the capture", need);
+    if (ctx->ops_ws_captured) {
+      try {
+        ctx->ops_ws_outgrown.reserve(ctx->ops_ws_outgrown.size() + 1);
+      } catch (...) {
+        return fail(ctx, KB_ERR_WORKSPACE, "no host memory to keep an outgrown workspace");
+      }
+      unsigned char* old = ctx->ops_ws;
+      ctx->ops_ws = nullptr;
+      const kb_status rc = ensure_buf(ctx, &ctx->ops_ws, &ctx->ops_ws_bytes, need, "partial parameter gradients");
+      if (rc != KB_OK) {
+        ctx->ops_ws = old;
+        return rc;
+      }
+      ctx->ops_ws_outgrown.push_back(old);
+      ctx->ops_ws_captured = false;
+    } else {
+      KB_TRY(ensure_buf(ctx, &ctx->ops_ws, &ctx->ops_ws_bytes, need, "partial parameter gradients"));
+    }
+  }
+  ctx->ops_ws_captured |= capturing;
+  return KB_OK;
+}
+
 template <int DT, int NCH, bool VEC, bool WARP>
 kb_status launch_norm_bwd(kb_ctx* ctx, NormBwdParams& p, unsigned int threads, uint32_t* nparts, cudaStream_t st) {
   const uint64_t per = WARP ? threads / 32 : 1;
@@ -141,8 +179,7 @@ kb_status launch_norm_bwd(kb_ctx* ctx, NormBwdParams& p, unsigned int threads, u
     const unsigned int grid = (unsigned int)std::min<uint64_t>((p.rows + per - 1) / per, resident);
     *nparts = grid;
     if (p.want_param) {
-      KB_TRY(ensure_buf(ctx, &ctx->ops_ws, &ctx->ops_ws_bytes, (size_t)grid * 2 * p.cols * sizeof(float),
-                        "partial parameter gradients"));
+      KB_TRY(ensure_partials(ctx, (size_t)grid * 2 * p.cols * sizeof(float), st));
       p.partial = reinterpret_cast<float*>(ctx->ops_ws);
     }
     kernel<<<grid, threads, smem, st>>>(p);
@@ -167,6 +204,19 @@ kb_status launch_norm_bwd(kb_ctx* ctx, NormBwdParams& p, unsigned int threads, u
                 WARP ? 2 * sizeof(float) * p.cols : 0);
 }
 
+// Rows too long for the registers: slices of the rows, a partial row each
+uint32_t norm_bwd_slices(const kb_ctx* ctx, uint64_t rows, uint32_t groups) {
+  const uint64_t want = std::max<uint64_t>(1, 8ull * ctx->sm_count / ((groups + 7) / 8));
+  return (uint32_t)std::min<uint64_t>(std::min<uint64_t>(want, (rows + 7) / 8), 65535);
+}
+// Partial rows of a backward pass over `rows` rows or fewer, at most: the grids below as if registers did not
+// limit the CTAs per SM
+uint64_t norm_bwd_most_partials(const kb_ctx* ctx, uint64_t rows, uint32_t groups) {
+  if (groups > 32) return norm_bwd_slices(ctx, rows, groups);
+  const uint32_t threads = 32 * ((groups + 1) / 2);   // two groups per warp: the most CTAs per SM
+  return std::min<uint64_t>(rows, (uint64_t)ctx->sm_count * (groups <= 2 ? 4 : std::max(4u, 1024 / threads)));
+}
+
 template <int DT, bool VEC>
 kb_status launch_norm_bwd(kb_ctx* ctx, NormBwdParams& p, uint32_t* nparts, cudaStream_t st) {
   const uint32_t g = p.groups;
@@ -178,17 +228,16 @@ kb_status launch_norm_bwd(kb_ctx* ctx, NormBwdParams& p, uint32_t* nparts, cudaS
   const bool few = !VEC || p.rows < 2ull * ctx->sm_count;
   if (few && g <= 24) return launch_norm_bwd<DT, 1, VEC, false>(ctx, p, 32 * g, nparts, st);
   if (g <= 32) return launch_norm_bwd<DT, 2, VEC, false>(ctx, p, 32 * ((g + 1) / 2), nparts, st);
+  const uint32_t gx = (g + 7) / 8, slices = norm_bwd_slices(ctx, p.rows, g);
+  if (p.want_param) {   // what can be refused comes before the first launch
+    KB_TRY(ensure_partials(ctx, (size_t)slices * 2 * p.cols * sizeof(float), st));
+    p.partial = reinterpret_cast<float*>(ctx->ops_ws);
+  }
   if (p.dx) {
     norm_bwd_long_kernel<DT, VEC><<<(unsigned int)p.rows, 512, 0, st>>>(p);
     KB_TRY(launched(ctx));
   }
   if (p.want_param) {
-    const uint32_t gx = (g + 7) / 8;
-    const uint64_t want = std::max<uint64_t>(1, 8ull * ctx->sm_count / gx);
-    const uint32_t slices = (uint32_t)std::min<uint64_t>(std::min<uint64_t>(want, (p.rows + 7) / 8), 65535);
-    KB_TRY(ensure_buf(ctx, &ctx->ops_ws, &ctx->ops_ws_bytes, (size_t)slices * 2 * p.cols * sizeof(float),
-                      "partial parameter gradients"));
-    p.partial = reinterpret_cast<float*>(ctx->ops_ws);
     *nparts = slices;
     norm_bwd_cols_kernel<DT, VEC><<<dim3(gx, slices), 256, 0, st>>>(p);
     KB_TRY(launched(ctx));
@@ -431,6 +480,16 @@ extern "C" kb_status kb_layernorm(kb_ctx* ctx, const void* d_x, uint64_t rows, u
   if (dtype == KB_F32) return launch_norm<KB_F32>(ctx, p, vec, e5m2, st);
   if (dtype == KB_F16) return launch_norm<KB_F16>(ctx, p, vec, e5m2, st);
   return launch_norm<KB_BF16>(ctx, p, vec, e5m2, st);
+}
+
+extern "C" kb_status kb_layernorm_backward_reserve(kb_ctx* ctx, uint64_t rows, uint64_t cols, void* stream) {
+  TraceRange trace("kb_layernorm_backward_reserve");
+  if (!ctx) return KB_ERR_INVALID_ARG;
+  if (cols == 0 || rows > KB_OPS_MAX_DIM || cols > KB_OPS_MAX_DIM)
+    return fail(ctx, KB_ERR_INVALID_ARG, "kb_layernorm_backward_reserve: columns outside [1, 2^30] or rows beyond 2^30");
+  DeviceGuard g(ctx->device);
+  const uint64_t parts = norm_bwd_most_partials(ctx, rows, (uint32_t)((cols + kGroup - 1) / kGroup));
+  return ensure_partials(ctx, (size_t)parts * 2 * cols * sizeof(float), reinterpret_cast<cudaStream_t>(stream));
 }
 
 extern "C" kb_status kb_layernorm_backward(kb_ctx* ctx, const void* d_dy, uint64_t lddy, const void* d_x,
