@@ -84,8 +84,9 @@ kb_status launch_quant(kb_ctx* ctx, const QuantParams& p, bool vec, bool e5m2, b
 
 // The row ring of a CTA that walks over rows of `bytes` each: as many slots as fit its share of an
 // SM's shared memory, 0 if fewer than two do (then the rows are read directly).
+constexpr size_t kRingBytes = 220 * 1024;   // of an SM's shared memory
 uint32_t ring_stages(size_t bytes, int ctas_per_sm) {
-  const size_t share = (size_t)(220 * 1024) / ctas_per_sm - 1024;
+  const size_t share = kRingBytes / ctas_per_sm - 1024;
   return (uint32_t)std::min<size_t>(share / round_up(bytes, 128), kRowRingStages);
 }
 // CTAs of `threads` threads of a kernel that fit an SM by its registers (the count is fixed at
@@ -99,10 +100,12 @@ int ctas_by_registers(unsigned int threads, int most) {
   const int per_warp = (regs + 7) / 8 * 8 * 32;
   return std::max(1, std::min(most, 65536 / per_warp / (int)(threads / 32)));
 }
+// The limit belongs to the kernel on the device, not to the context: it is raised to the same size by every
+// call, so that no other thread's call, with narrower rows on a context of its own, takes it back.
 template <class K>
 kb_status ring_limits(kb_ctx* ctx, K kernel, size_t smem) {
   if (smem > 40 * 1024)   // static and dynamic shared memory together: 48 KB without asking
-    KB_CUDA(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    KB_CUDA(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kRingBytes));
   return KB_OK;
 }
 
