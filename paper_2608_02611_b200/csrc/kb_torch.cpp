@@ -41,7 +41,14 @@ struct Call {
   kb_ctx* ctx;
   at::Device device;
   void* stream;
-  void check(kb_status rc) const {
+  // Runs an entry point without Python's lock (as ctypes would): a launch can wait for room in the stream's
+  // queue and a workspace can grow, and other threads go on meanwhile.  The tensors stay alive: the
+  // caller holds them.
+  template <class F>
+  void run(F entry) const {
+    PyThreadState* held = PyEval_SaveThread();
+    const kb_status rc = entry();
+    PyEval_RestoreThread(held);
     if (rc != KB_OK) refuse(where, g_lib.last_error(ctx), rc);
   }
   at::Tensor empty(at::IntArrayRef sizes, at::ScalarType type) const {
@@ -175,9 +182,13 @@ PyObject* quantize_blocks(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const int64_t R = transpose ? m.cols : m.rows, C = transpose ? m.rows : m.cols;
     const at::Tensor q = c.codes(R, C, type_of(code));
     const at::Tensor scale = c.empty({blocks(C), tiles ? blocks(R) : R}, at::kFloat);
-    c.check(g_lib.quantize_blocks(c.ctx, m.p, m.rows, m.cols, m.ld, (kb_dtype)code_of(x.scalar_type()), transpose,
-                               tiles ? KB_SCALE_TILES : KB_SCALE_ROWS, q.data_ptr(), (C + 15) / 16 * 16,
-                               (kb_dtype)code, scale.data_ptr<float>(), c.stream));
+    void* qp = q.data_ptr();
+    float* sp = scale.data_ptr<float>();
+    const kb_dtype type = (kb_dtype)code_of(x.scalar_type());
+    c.run([&] {
+      return g_lib.quantize_blocks(c.ctx, m.p, m.rows, m.cols, m.ld, type, transpose, tiles ? KB_SCALE_TILES : KB_SCALE_ROWS,
+                                   qp, (C + 15) / 16 * 16, (kb_dtype)code, sp, c.stream);
+    });
     return wrap_tuple({q, scale});
   });
 }
@@ -216,12 +227,15 @@ PyObject* layernorm(PyObject*, PyObject* const* a, Py_ssize_t n) {
       q = c.codes(m.rows, m.cols, type_of(code));
       scale = c.empty({blocks(m.cols), m.rows}, at::kFloat);
     }
-    if (m.rows > 0)   // the addresses of empty tensors are null
-      c.check(g_lib.layernorm(c.ctx, m.p, m.rows, m.cols, m.ld, (kb_dtype)code_of(type), w, b, (kb_dtype)code_of(params),
-                           (float)eps, want_y ? y.data_ptr() : nullptr, m.cols,
-                           want_stats ? mean.data_ptr<float>() : nullptr, want_stats ? rstd.data_ptr<float>() : nullptr,
-                           want_q ? q.data_ptr() : nullptr, (m.cols + 15) / 16 * 16, (kb_dtype)code,
-                           want_q ? scale.data_ptr<float>() : nullptr, c.stream));
+    if (m.rows > 0) {   // the addresses of empty tensors are null
+      void *yp = want_y ? y.data_ptr() : nullptr, *qp = want_q ? q.data_ptr() : nullptr;
+      float *mp = want_stats ? mean.data_ptr<float>() : nullptr, *rp = want_stats ? rstd.data_ptr<float>() : nullptr;
+      float* sp = want_q ? scale.data_ptr<float>() : nullptr;
+      c.run([&] {
+        return g_lib.layernorm(c.ctx, m.p, m.rows, m.cols, m.ld, (kb_dtype)code_of(type), w, b, (kb_dtype)code_of(params),
+                               (float)eps, yp, m.cols, mp, rp, qp, (m.cols + 15) / 16 * 16, (kb_dtype)code, sp, c.stream);
+      });
+    }
     return wrap_tuple({y, mean, rstd, q, scale});
   });
 }
@@ -248,10 +262,12 @@ PyObject* layernorm_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const at::Tensor dx = c.empty(x.sizes(), type), dweight = c.empty({m.cols}, params);
     at::Tensor dbias;
     if (want_bias) dbias = c.empty({m.cols}, params);
-    c.check(g_lib.layernorm_backward(c.ctx, mg.p, mg.ld, m.p, m.ld, m.rows, m.cols, (kb_dtype)code_of(type), w,
-                                  (kb_dtype)code_of(params), static_cast<float*>(mean), static_cast<float*>(rstd),
-                                  dx.data_ptr(), m.cols, dweight.data_ptr(), want_bias ? dbias.data_ptr() : nullptr,
-                                  c.stream));
+    void *dxp = dx.data_ptr(), *dwp = dweight.data_ptr(), *dbp = want_bias ? dbias.data_ptr() : nullptr;
+    c.run([&] {
+      return g_lib.layernorm_backward(c.ctx, mg.p, mg.ld, m.p, m.ld, m.rows, m.cols, (kb_dtype)code_of(type), w,
+                                      (kb_dtype)code_of(params), static_cast<float*>(mean), static_cast<float*>(rstd), dxp,
+                                      m.cols, dwp, dbp, c.stream);
+    });
     return wrap_tuple({dx, dweight, dbias});
   });
 }
@@ -282,10 +298,12 @@ PyObject* matmul_blocks(PyObject*, PyObject* const* a, Py_ssize_t n) {
         refuse(c.where, "out must be a matrix [" + std::to_string(M) + ", " + std::to_string(N) + "]");
     }
     const Rows md = rows_of(c, D, "out");
-    c.check(g_lib.matmul_blocks(c.ctx, ma.p, ma.ld, (kb_dtype)code_of(A.scalar_type()), static_cast<float*>(sa), mb.p,
-                             mb.ld, (kb_dtype)code_of(B.scalar_type()), static_cast<float*>(sb),
-                             tiles ? KB_SCALE_TILES : KB_SCALE_ROWS, M, N, K, md.p, md.ld,
-                             (kb_dtype)code_of(D.scalar_type()), c.stream));
+    const kb_dtype ta = (kb_dtype)code_of(A.scalar_type()), tb = (kb_dtype)code_of(B.scalar_type());
+    const kb_dtype td = (kb_dtype)code_of(D.scalar_type());
+    c.run([&] {
+      return g_lib.matmul_blocks(c.ctx, ma.p, ma.ld, ta, static_cast<float*>(sa), mb.p, mb.ld, tb, static_cast<float*>(sb),
+                                 tiles ? KB_SCALE_TILES : KB_SCALE_ROWS, M, N, K, md.p, md.ld, td, c.stream);
+    });
     return wrap(D);
   });
 }

@@ -47,3 +47,61 @@ def test_backward_passes_of_two_widths_in_two_threads():
     for t in threads:
         t.join()
     assert not refused, refused
+
+
+WAIT_C = """
+#include <time.h>
+/* Stands in for any entry point: waits up to 5 s for another thread to set the flag. */
+volatile int flag = 0;
+int wait_for_flag(void) {
+  for (int i = 0; i < 5000 && !flag; ++i) {
+    struct timespec t = {0, 1000000};
+    nanosleep(&t, 0);
+  }
+  return flag ? 0 : 5;
+}
+const char* no_error(const void* ctx) { return "the other thread did not run"; }
+"""
+
+
+def test_other_threads_run_while_an_operator_call_waits(tmp_path):
+    """A call whose entry point waits (here a stand-in on the host; no kernel runs) leaves Python's lock to the
+    other threads, one of which ends the wait."""
+    import ctypes
+    import subprocess
+    from paper_2608_02611_b200 import binding
+    src, lib = tmp_path / "wait.c", tmp_path / "wait.so"
+    src.write_text(WAIT_C)
+    subprocess.run(["gcc", "-shared", "-fPIC", "-o", str(lib), str(src)], check=True)
+    W = ctypes.CDLL(str(lib))
+    flag = ctypes.c_int.in_dll(W, "flag")
+    wait, text = (ctypes.cast(f, ctypes.c_void_p).value for f in (W.wait_for_flag, W.no_error))
+    ctx = binding.Context(0)
+    x = torch.randn(64, 256, device=DEV)
+    m, r = torch.zeros(64, device=DEV), torch.ones(64, device=DEV)
+    q, s = ctx.quantize_blocks(x)
+    calls = (lambda: ctx.quantize_blocks(x), lambda: ctx.layernorm(x), lambda: ctx.layernorm_backward(x, x, None, m, r),
+             lambda: ctx.matmul_blocks(q, s, q, s))
+    module = binding._native()
+    module.bind(binding.KbError, wait, wait, wait, wait, text)
+    try:
+        for call in calls:
+            flag.value = 0
+            started = threading.Event()
+
+            def release():
+                started.wait()
+                flag.value = 1
+
+            t = threading.Thread(target=release)
+            t.start()
+            started.set()
+            try:
+                call()                    # KbError if the flag was not set meanwhile
+            finally:
+                t.join()
+    finally:
+        binding._native_module = None     # the library's own entry points again
+        binding._native()
+    assert bool((ctx.quantize_blocks(x)[1] == s).all())
+    ctx.close()
