@@ -76,6 +76,18 @@ const at::Tensor& tensor(const Call& c, PyObject* o, const char* name) {
   return t;
 }
 
+// Python's truth value and whole numbers; what raises there raises here, before any launch
+bool truth(PyObject* o) {
+  const int t = PyObject_IsTrue(o);
+  if (t < 0) throw Refused{};
+  return t != 0;
+}
+long whole(PyObject* o) {
+  const long v = PyLong_AsLong(o);
+  if (v == -1 && PyErr_Occurred()) throw Refused{};
+  return v;
+}
+
 int code_of(at::ScalarType t) {
   switch (t) {
     case at::kFloat: return KB_F32;
@@ -176,8 +188,8 @@ PyObject* quantize_blocks(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 6, [&]() -> PyObject* {
     const Call c = open_call("kb_quantize_blocks", a[0], a[1]);
     const at::Tensor& x = tensor(c, a[2], "x");
-    const long code = PyLong_AsLong(a[3]);
-    const bool tiles = PyObject_IsTrue(a[4]), transpose = PyObject_IsTrue(a[5]);
+    const long code = whole(a[3]);
+    const bool tiles = truth(a[4]), transpose = truth(a[5]);
     const Rows m = rows_of(c, x, "x");
     const int64_t R = transpose ? m.cols : m.rows, C = transpose ? m.rows : m.cols;
     const at::Tensor q = c.codes(R, C, type_of(code));
@@ -214,9 +226,9 @@ PyObject* layernorm(PyObject*, PyObject* const* a, Py_ssize_t n) {
       params = t.scalar_type();
     }
     const double eps = PyFloat_AsDouble(a[5]);
-    const bool want_y = PyObject_IsTrue(a[6]), want_stats = PyObject_IsTrue(a[7]), want_q = a[8] != Py_None;
-    const long code = want_q ? PyLong_AsLong(a[8]) : KB_F8E4M3;
-    if (PyErr_Occurred()) throw Refused{};
+    if (eps == -1.0 && PyErr_Occurred()) throw Refused{};
+    const bool want_y = truth(a[6]), want_stats = truth(a[7]), want_q = a[8] != Py_None;
+    const long code = want_q ? whole(a[8]) : KB_F8E4M3;
     at::Tensor y, mean, rstd, q, scale;
     if (want_y) y = c.empty(x.sizes(), type);
     if (want_stats) {
@@ -258,7 +270,7 @@ PyObject* layernorm_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     }
     void* mean = vector_of(c, tensor(c, a[5], "mean"), m.rows, "mean", at::kFloat, at::kFloat);
     void* rstd = vector_of(c, tensor(c, a[6], "rstd"), m.rows, "rstd", at::kFloat, at::kFloat);
-    const bool want_bias = PyObject_IsTrue(a[7]);
+    const bool want_bias = truth(a[7]);
     const at::Tensor dx = c.empty(x.sizes(), type), dweight = c.empty({m.cols}, params);
     at::Tensor dbias;
     if (want_bias) dbias = c.empty({m.cols}, params);
@@ -289,9 +301,7 @@ PyObject* matmul_blocks(PyObject*, PyObject* const* a, Py_ssize_t n) {
     void* sb = vector_of(c, SB, SB.numel(), "b_scale", at::kFloat, at::kFloat);
     at::Tensor D;
     if (a[7] == Py_None) {
-      const long code = PyLong_AsLong(a[6]);
-      if (PyErr_Occurred()) throw Refused{};
-      D = c.empty({M, N}, type_of(code));
+      D = c.empty({M, N}, type_of(whole(a[6])));
     } else {
       D = tensor(c, a[7], "out");
       if (D.dim() != 2 || D.size(0) != M || D.size(1) != N)
