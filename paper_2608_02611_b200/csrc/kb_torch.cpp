@@ -239,15 +239,16 @@ PyObject* layernorm(PyObject*, PyObject* const* a, Py_ssize_t n) {
       q = c.codes(m.rows, m.cols, type_of(code));
       scale = c.empty({blocks(m.cols), m.rows}, at::kFloat);
     }
-    if (m.rows > 0) {   // the addresses of empty tensors are null
-      void *yp = want_y ? y.data_ptr() : nullptr, *qp = want_q ? q.data_ptr() : nullptr;
-      float *mp = want_stats ? mean.data_ptr<float>() : nullptr, *rp = want_stats ? rstd.data_ptr<float>() : nullptr;
-      float* sp = want_q ? scale.data_ptr<float>() : nullptr;
-      c.run([&] {
-        return g_lib.layernorm(c.ctx, m.p, m.rows, m.cols, m.ld, (kb_dtype)code_of(type), w, b, (kb_dtype)code_of(params),
-                               (float)eps, yp, m.cols, mp, rp, qp, (m.cols + 15) / 16 * 16, (kb_dtype)code, sp, c.stream);
-      });
-    }
+    // the addresses of empty tensors are null, which would mean "not wanted": with no row the call checks
+    // its arguments and writes nothing, so any address does
+    alignas(16) static float no_row[4];
+    auto out = [&](bool want, const at::Tensor& t) -> void* { return !want ? nullptr : m.rows ? t.data_ptr() : no_row; };
+    void *yp = out(want_y, y), *mp = out(want_stats, mean), *rp = out(want_stats, rstd), *qp = out(want_q, q), *sp = out(want_q, scale);
+    c.run([&] {
+      return g_lib.layernorm(c.ctx, m.p, m.rows, m.cols, m.ld, (kb_dtype)code_of(type), w, b, (kb_dtype)code_of(params),
+                             (float)eps, yp, m.cols, static_cast<float*>(mp), static_cast<float*>(rp), qp,
+                             (m.cols + 15) / 16 * 16, (kb_dtype)code, static_cast<float*>(sp), c.stream);
+    });
     return wrap_tuple({y, mean, rstd, q, scale});
   });
 }

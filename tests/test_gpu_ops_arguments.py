@@ -32,3 +32,19 @@ def test_an_argument_without_a_truth_value_raises_its_own_error(ctx):
     assert ctx.launch_count == before
     with pytest.raises(TypeError):
         ctx.layernorm(x, eps="small")
+
+
+def test_a_norm_over_no_row_refuses_what_a_norm_over_rows_refuses(ctx):
+    from paper_2608_02611_b200 import binding
+    z = torch.empty(0, 256, device=DEV)
+    w = torch.ones(256, device=DEV)
+    for call in (lambda: ctx.layernorm(z, w, eps=0.0), lambda: ctx.layernorm(z, w, eps=float("inf")),
+                 lambda: ctx.layernorm(z, w, quantize=torch.bfloat16), lambda: ctx.layernorm(z.int(), None),
+                 lambda: ctx.layernorm(z, w, want_y=False, want_stats=False), lambda: ctx.layernorm(z[:, :0], None)):
+        with pytest.raises(binding.KbError):
+            call()
+    r = ctx.layernorm(z, w, w, quantize=torch.float8_e5m2)
+    assert r.y.shape == (0, 256) and r.mean.shape == (0,) and r.rstd.shape == (0,)
+    assert r.q.shape == (0, 256) and r.q.dtype == torch.float8_e5m2 and r.scale.shape == (2, 0)
+    only = ctx.layernorm(z.view(3, 0, 256), w, want_y=False)
+    assert only.y is None and only.mean.shape == (0,)
