@@ -626,6 +626,10 @@ def _native():
         if not os.path.exists(os.path.join(_HERE, "_kb_torch.so")):
             raise ImportError("_kb_torch.so is missing: build it first (python -m paper_2608_02611_b200.build)")
         from . import _kb_torch
+        from .build import native_marker
+        if _kb_torch.built_for != native_marker():
+            raise ImportError(f"_kb_torch.so was built for {_kb_torch.built_for}, this is {native_marker()}: build it again "
+                              "(python -m paper_2608_02611_b200.build)")
         _kb_torch.bind(KbError, *[ctypes.cast(getattr(L, name), ctypes.c_void_p).value for name in (
             "kb_quantize_blocks", "kb_layernorm", "kb_layernorm_backward", "kb_matmul_blocks", "kb_last_error")])
         _native_module = _kb_torch

@@ -347,4 +347,8 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_kb_torch", nullptr, -1, methods, 
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__kb_torch() { return PyModule_Create(&module); }
+PyMODINIT_FUNC PyInit__kb_torch() {
+  PyObject* m = PyModule_Create(&module);
+  if (m && PyModule_AddStringConstant(m, "built_for", KB_BUILT_FOR) < 0) Py_CLEAR(m);
+  return m;
+}
