@@ -53,9 +53,10 @@ struct Held8 {   // 8 consecutive elements of one row
 constexpr int kQuantRowGroups = 4;
 // VEC: rows of x and q are aligned and a multiple of 8 long.  Otherwise, with aligned rows of q
 // (SHIFT), a lane still takes 8 consecutive elements and shifts the granules they lie in into place
-// (8191 x 8191 bf16: 73 us, element by element 89); rows of q at any address go element by element.
+// (8191 x 8191 bf16: 73 us, element by element 90; 2000 x 5003: 11.7 and 15.0); rows of q at any address go
+// element by element.  Four CTAs per SM: with three, and registers to spare, 8191 x 8191 takes 89 us.
 template <int DT, bool VEC, bool SHIFT, bool E5M2>
-__global__ void __launch_bounds__(256, SHIFT ? 3 : 4) quant_rows_kernel(const QuantParams p) {
+__global__ void __launch_bounds__(256, 4) quant_rows_kernel(const QuantParams p) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const uint64_t row = (uint64_t)blockIdx.x * 8 + warp;
   if (row >= p.rows) return;
