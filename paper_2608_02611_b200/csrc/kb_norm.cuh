@@ -212,7 +212,7 @@ __device__ __forceinline__ const unsigned char* row_ptr(const void* base, uint64
 }
 
 // Backward, rows by warp (WARP) or by CTA, walking over the rows with the grid's stride.  RING
-// (VEC and CTA only): the rows of x and dy come through shared memory.
+// (VEC, CTA and two groups per warp only): the rows of x and dy come through shared memory.
 template <int DT, int NCH, bool VEC, bool WARP, bool RING>
 __global__ void __launch_bounds__(WARP ? 128 : NCH == 1 ? 768 : 512) norm_bwd_kernel(const NormBwdParams p) {
   __shared__ float red[2][2][32];

@@ -188,7 +188,7 @@ kb_status launch_norm_bwd(kb_ctx* ctx, NormBwdParams& p, unsigned int threads, u
     kernel<<<grid, threads, smem, st>>>(p);
     return launched(ctx);
   };
-  if constexpr (VEC && !WARP) {
+  if constexpr (VEC && !WARP && NCH == 2) {   // with one group per warp the rows are too few for the ring
     constexpr auto kernel = norm_bwd_kernel<DT, NCH, true, false, true>;
     const int per_sm = ctas_by_registers<kernel>(threads, std::max(4, (int)(1024 / threads)));
     const uint64_t resident = (uint64_t)ctx->sm_count * per_sm;
@@ -226,8 +226,11 @@ kb_status launch_norm_bwd(kb_ctx* ctx, NormBwdParams& p, uint32_t* nparts, cudaS
   // a warp per row up to 512 columns (32768 x 512 bf16: 32 us, by CTAs 42; 32768 x 768: 51 and 48)
   if (g == 1) return launch_norm_bwd<DT, 1, VEC, true>(ctx, p, 128, nparts, st);
   if (g == 2) return launch_norm_bwd<DT, 2, VEC, true>(ctx, p, 128, nparts, st);
-  // one group per warp up to 16 warps; up to 24 where the rows are too few for the ring or cannot
-  // take it (777 x 5003 fp16: 19 us with two groups per warp, 17 with one and a row ahead)
+  // Two groups per warp, through the ring from twice the resident CTAs on (16000 x 4096 bf16: 73 us, with one
+  // group per warp 101); one group per warp with a row ahead, up to 24 warps, for fewer than two rows per SM
+  // and for rows that cannot take the ring (777 x 5003 fp16: 17 us, with two groups 19).  In between, up to
+  // the ring's first row, the two differ either way: 400 x 1024 bf16 8.2 us with two groups and 8.6 with
+  // one, 500 x 3000 9.7 and 10.0, 1000 x 2048 12.5 and 11.7, 2000 x 1024 17.0 and 14.1.
   const bool few = !VEC || p.rows < 2ull * ctx->sm_count;
   if (few && g <= 24) return launch_norm_bwd<DT, 1, VEC, false>(ctx, p, 32 * g, nparts, st);
   if (g <= 32) return launch_norm_bwd<DT, 2, VEC, false>(ctx, p, 32 * ((g + 1) / 2), nparts, st);
