@@ -112,9 +112,9 @@ kb_status ring_limits(kb_ctx* ctx, K kernel, size_t smem) {
 template <int DT, int NCH, bool VEC, int Q>
 kb_status launch_norm(kb_ctx* ctx, const NormParams& p, cudaStream_t st) {
   const uint32_t warps = (p.groups + NCH - 1) / NCH;
-  if (warps == 1)
+  if (NCH == 2 || warps == 1)   // two groups per lane are only chosen for rows of two groups
     norm_kernel<DT, NCH, VEC, true, Q><<<(unsigned int)((p.rows + 3) / 4), 128, 0, st>>>(p);
-  else
+  else if constexpr (NCH != 2)
     norm_kernel<DT, NCH, VEC, false, Q><<<(unsigned int)p.rows, 32 * warps, 0, st>>>(p);
   return launched(ctx);
 }
