@@ -17,7 +17,7 @@ namespace kb {
 constexpr uint32_t kGroup = 256;
 
 template <bool VEC>
-__device__ __forceinline__ uint32_t group_col(uint32_t g, int lane, int j) {
+__host__ __device__ __forceinline__ uint32_t group_col(uint32_t g, int lane, int j) {
   return g * kGroup + (VEC ? lane * 8 + j : j * 32 + lane);
 }
 

@@ -95,6 +95,14 @@ struct LaneTile {
   static constexpr int kThreads = 32 * (4 + kEpiWarps);        // and four warps that copy, issue, fetch scales
 };
 
+// A cluster of `splits` CTAs divides a tile's `groups` of columns: CTA o finishes those from cluster_first(o) up
+// to cluster_first(o + 1), none if they are equal, and holds cluster_share places for each CTA's part.
+__host__ __device__ constexpr uint32_t cluster_first(uint32_t groups, uint32_t splits, uint32_t o) {
+  return (groups * o + splits - 1) / splits;
+}
+__host__ __device__ constexpr uint32_t cluster_owner(uint32_t groups, uint32_t splits, uint32_t g) { return g * splits / groups; }
+__host__ __device__ constexpr uint32_t cluster_share(uint32_t groups, uint32_t splits) { return (groups + splits - 1) / splits; }
+
 // c0 += v0 * s0, c1 += v1 * s1 as one packed instruction
 __device__ __forceinline__ void fma_pair(float& c0, float& c1, float v0, float v1, float s0, float s1) {
   asm("{\n.reg .b64 c, v, s;\n"
@@ -163,9 +171,7 @@ __global__ void __launch_bounds__(LaneTile<BN>::kThreads, 1)
     abort_word = 0u;
     mbar_fence_init();
   }
-  // CTA o of the cluster finishes the groups of columns from first_group[o] on: those with
-  // floor(g * splits / kGroups) = o
-  if (warp == 2 && lane < 9) first_group[lane] = (T::kGroups * lane + p.splits - 1) / p.splits;
+  if (warp == 2 && lane < 9) first_group[lane] = cluster_first(T::kGroups, p.splits, lane);
   if (p.splits > 1) cluster_arrive();   // "this CTA runs": waited for before the first write to another's memory
   if (warp == 1) tmem_alloc<1>(&tmem_base, T::kTmemCols);
   tc_fence_before();
@@ -314,13 +320,13 @@ __global__ void __launch_bounds__(LaneTile<BN>::kThreads, 1)
     // The cluster adds its partial sums: each CTA owns a share of the tile's columns and gets every
     // CTA's sums for them written into its shared memory, then adds them in rank order.
     cluster_wait();
-    const uint32_t share = (T::kGroups + p.splits - 1) / p.splits;       // places per CTA and owner
+    const uint32_t share = cluster_share(T::kGroups, p.splits);          // places per CTA and owner
     const uint32_t row = (warp & 3) * 32 + lane;
     unsigned char* sum_buf = stages + T::kStages * T::kStageBytes;
     if (warp >= 4) {
       const uint32_t g0 = ((warp - 4) >> 2) * (T::kEpiCols / 4);
       const uint32_t mine = smem_u32(sum_buf) + (rank * share * 128 + row) * 16;
-      uint32_t owner = g0 * p.splits / T::kGroups, next = first_group[owner + 1];
+      uint32_t owner = cluster_owner(T::kGroups, p.splits, g0), next = first_group[owner + 1];
       uint32_t at = map_to_rank(mine, owner) + (g0 - first_group[owner]) * 2048;
 #pragma unroll
       for (uint32_t g = 0; g < T::kEpiCols / 4; ++g, at += 2048) {
@@ -389,7 +395,7 @@ struct PairTile {
 
 // Tile coordinates of item `t`: down kGroupM tiles of A, then along B, so that the pairs that run
 // together read few different rows of either.
-__device__ __forceinline__ void pair_tile(uint32_t t, uint32_t tiles_m, uint32_t tiles_n, uint32_t& tm, uint32_t& tn) {
+__host__ __device__ __forceinline__ void pair_tile(uint32_t t, uint32_t tiles_m, uint32_t tiles_n, uint32_t& tm, uint32_t& tn) {
   const uint32_t per = PairTile::kGroupM * tiles_n;
   const uint32_t g = t / per, r = t % per;
   const uint32_t h = min(PairTile::kGroupM, tiles_m - g * PairTile::kGroupM);

@@ -88,7 +88,7 @@ __global__ void __launch_bounds__(256, 4) quant_rows_kernel(const QuantParams p)
 // The transposed tile in shared memory: rows of 128 codes; the 8-byte piece k of row r stands at
 // place k ^ (r / 8), so that neither the writes (16 rows apart by 8, one piece each) nor the reads
 // (one row at a time) meet in a bank.
-__device__ __forceinline__ int transposed_at(int r, int k) { return r * 128 + ((k ^ (r >> 3)) & 15) * 8; }
+__host__ __device__ __forceinline__ int transposed_at(int r, int k) { return r * 128 + ((k ^ (r >> 3)) & 15) * 8; }
 __device__ __forceinline__ float inf_to_nan(float v) { return isinf(v) ? __uint_as_float(0x7FFFFFFFu) : v; }
 
 template <int DT, bool VEC, bool E5M2, bool TILES, bool TRANSPOSE>
