@@ -291,6 +291,15 @@ kb_status prepare_matmul(kb_ctx* ctx) {
   KB_TRY(lanes_attr<128>(ctx));
   KB_CUDA(ctx, cudaFuncSetAttribute(matmul_pair_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)PairTile::kSmem));
   KB_CUDA(ctx, cudaFuncSetAttribute(matmul_pair_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)PairTile::kSmem));
+  // the pair kernel's warps split the registers it was launched with; with fewer, as other compiler
+  // options would give it, they would wait for the rest for good
+  for (const void* kernel : {reinterpret_cast<const void*>(&matmul_pair_kernel<false>), reinterpret_cast<const void*>(&matmul_pair_kernel<true>)}) {
+    cudaFuncAttributes attr = {};
+    KB_CUDA(ctx, cudaFuncGetAttributes(&attr, kernel));
+    if (attr.numRegs < PairTile::kRegsLaunch)
+      return fail(ctx, KB_ERR_UNSUPPORTED, "kb_matmul_blocks: the library was compiled with %d registers for a kernel that splits %d",
+                  attr.numRegs, PairTile::kRegsLaunch);
+  }
   // every variant takes an SM of its own, so one of them stands for all
   for (uint32_t n = 1; n <= 8; ++n) {
     cudaLaunchConfig_t cfg = {};

@@ -43,3 +43,16 @@ def test_a_changed_index_is_noticed(tmp_path, header, have, want):
                     text = text.replace(have, want)
                 (dst / name).write_text(text)
     assert run(tmp_path, copy).returncode == 1
+
+
+def test_registers_of_the_kernel_of_cta_pairs(tmp_path):
+    """Its warps split 168 registers per thread, which is what the compiler has to launch it with; and its
+    sums leave none over: spills in its loop cost a fifth of its speed."""
+    from paper_2608_02611_b200 import build
+    flags = [f for f in build.NVCC_FLAGS if f not in ("-shared", "-ldl", "--threads=2")]
+    done = subprocess.run([os.environ.get("NVCC", "nvcc"), *flags, "-Xptxas", "-v", "-I", CSRC, "-c",
+                           os.path.join(ROOT, "tests", "c", "pair_kernel.cu"), "-o", str(tmp_path / "k.o")], capture_output=True, text=True)
+    assert done.returncode == 0, done.stderr
+    text = done.stdout + done.stderr
+    assert text.count("Used 168 registers") == 2, text
+    assert text.count("0 bytes spill stores, 0 bytes spill loads") == 2, text
