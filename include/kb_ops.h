@@ -3,10 +3,11 @@
  * (forward, backward), quantisation to 8-bit floating point in blocks of 128, and the matrix
  * product of two such operands.
  *
- * The paper's workloads are operators of models (Appendix "Benchmark Descriptions and Shapes":
- * a normalisation, linear layers, attention).  The calls of kb.h compare and rank candidates
- * for them; these calls make the reference outputs, the operands and the baseline kernels the
- * candidates are compared with, in the gate's own storage types.
+ * The paper searches kernels for operators of models (Appendix "Benchmark Descriptions and Shapes":
+ * RMSNorm, LinearReLUDiv, attention and others; none of those is here).  The calls of kb.h compare and
+ * rank candidates; these calls make, in the gate's own storage types, the operands and a baseline kernel
+ * for candidates of a linear layer in 8 bits.  They compute what they are asked for and nothing else:
+ * gradients come from the backward calls, not from a framework's bookkeeping.
  *
  * The conventions of kb.h hold: plain C99 types, caller-owned buffers, work enqueued on
  * `stream` without synchronising, argument errors before any launch, one context per stream

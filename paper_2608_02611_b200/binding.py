@@ -605,6 +605,8 @@ def confirm(self, first: torch.Tensor, second: torch.Tensor, prev: torch.Tensor,
 
 
 # ---- model operators (include/kb_ops.h) ----------------------------------------------------
+# None of these calls takes part in autograd: inputs may require gradients, outputs never do, and a training
+# step calls the backward operators itself (examples/eight_bit_layer.py).
 
 class LayerNormResult(NamedTuple):
     """What ``Context.layernorm`` returns; an output that was not asked for is None."""
@@ -658,7 +660,8 @@ def layernorm(self, x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias
 
     ``quantize`` (an 8-bit float type) also, or with ``want_y`` false only, returns the result as
     codes q and scales as ``quantize_blocks`` lays them out, ready for ``matmul_blocks``;
-    ``want_stats`` returns each row's mean and 1/sqrt(var + eps) for the backward pass.
+    ``want_stats`` returns each row's mean and 1/sqrt(var + eps) for the backward pass: the outputs carry
+    no gradient, even where an input requires one; ``layernorm_backward`` computes it.
     """
     code = None if quantize is None else DTYPE_CODE.get(quantize, -1)
     return LayerNormResult(*(_native_module or _native()).layernorm(self._h, self.device.index, x, weight, bias, eps,

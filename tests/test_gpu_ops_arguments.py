@@ -48,3 +48,15 @@ def test_a_norm_over_no_row_refuses_what_a_norm_over_rows_refuses(ctx):
     assert r.q.shape == (0, 256) and r.q.dtype == torch.float8_e5m2 and r.scale.shape == (2, 0)
     only = ctx.layernorm(z.view(3, 0, 256), w, want_y=False)
     assert only.y is None and only.mean.shape == (0,)
+
+
+def test_outputs_carry_no_gradient(ctx):
+    """As documented: the operators take no part in autograd, whatever their inputs require."""
+    x = torch.randn(8, 256, device=DEV, requires_grad=True)
+    w = torch.ones(256, device=DEV, requires_grad=True)
+    r = ctx.layernorm(x, w, quantize=torch.float8_e4m3fn)
+    q, s = ctx.quantize_blocks(x)
+    outs = [*r, q, s, ctx.matmul_blocks(q, s, q, s), *ctx.layernorm_backward(x, x, w, r.mean, r.rstd)]
+    assert not any(o.requires_grad for o in outs)
+    for call in (ctx.layernorm, ctx.layernorm_backward):
+        assert "gradient" in call.__doc__
