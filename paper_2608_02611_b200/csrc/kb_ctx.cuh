@@ -71,6 +71,10 @@ struct kb_ctx {
   // kb_ctx_check_guards counts the band bytes that no longer hold it (an out-of-bounds write).
   struct Guarded { unsigned char* raw; size_t bytes; };
   std::vector<Guarded> guarded;
+  // A launch that is captured into a graph keeps the addresses it was given: from the first such call on,
+  // workspaces that are outgrown stay allocated until the context goes.
+  bool captured = false;
+  std::vector<void*> outgrown;
   // instrumentation
   uint64_t launches = 0;
   bool timing = false;
@@ -82,8 +86,6 @@ struct kb_ctx {
   // model operators (kb_ops.h)
   unsigned char* ops_ws = nullptr;  // partial sums of the norm's parameter gradients
   size_t ops_ws_bytes = 0;
-  bool ops_ws_captured = false;     // its address is in a captured launch: it is never freed before the context is
-  std::vector<unsigned char*> ops_ws_outgrown;
   void* encode_tiled = nullptr;     // the driver's tensor-map encoder, looked up at first use
   int cluster_room[9] = {};         // clusters of n CTAs, one CTA per SM, that run at the same time
   bool ops_ready = false;           // shared-memory limits of the operators' kernels are raised
@@ -190,6 +192,40 @@ inline kb_status ensure_buf(kb_ctx* ctx, T** buf, size_t* have, size_t need, con
   *buf = static_cast<T*>(fresh);
   *have = need;
   return KB_OK;
+}
+
+// Whether launches on `st` go into a graph (asked about the default stream while another one is
+// captured, the runtime answers with an error: nothing may be allocated then either).
+inline bool is_capturing(cudaStream_t st) {
+  cudaStreamCaptureStatus status = cudaStreamCaptureStatusNone;
+  if (cudaStreamIsCapturing(st, &status) != cudaSuccess) {
+    cudaGetLastError();
+    return true;
+  }
+  return status != cudaStreamCaptureStatusNone;
+}
+// The same for a workspace that kernels on `st` are given the address of.  Growing is refused while the
+// stream is captured; what a graph may use is kept.  Callers set ctx->captured for calls that are captured.
+template <typename T>
+inline kb_status ensure_workspace(kb_ctx* ctx, T** buf, size_t* have, size_t need, cudaStream_t st, const char* what) {
+  if (need <= *have) return KB_OK;
+  if (is_capturing(st))
+    return fail(ctx, KB_ERR_WORKSPACE, "%s: %zu bytes cannot be allocated while a stream is captured; make such a call "
+                "(or reserve) before the capture", what, need);
+  if (!ctx->captured || !*buf) return ensure_buf(ctx, buf, have, need, what);
+  try {
+    ctx->outgrown.reserve(ctx->outgrown.size() + 1);
+  } catch (...) {   // nothing may be thrown across the C boundary
+    return fail(ctx, KB_ERR_WORKSPACE, "%s: no host memory to keep an outgrown buffer", what);
+  }
+  T* old = *buf;
+  *buf = nullptr;
+  const kb_status rc = ensure_buf(ctx, buf, have, need, what);
+  if (rc == KB_OK)
+    ctx->outgrown.push_back(old);
+  else
+    *buf = old;
+  return rc;
 }
 
 }  // namespace kb

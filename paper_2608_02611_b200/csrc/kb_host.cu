@@ -79,13 +79,13 @@ inline size_t ws_acc64_offset(uint32_t cap_K) {
   return 2 * ws_region(cap_K) + round_up((size_t)cap_K * sizeof(void*), 256);
 }
 inline unsigned int* counter_set(kb_ctx* ctx, int set) { return ctx->d_status + 8 + 8 * set; }
-kb_status ensure_ws(kb_ctx* ctx, uint32_t K) {
+kb_status ensure_ws(kb_ctx* ctx, uint32_t K, cudaStream_t st) {
   if (K <= ctx->ws_cap_K) return KB_OK;
   if (ctx->ws_fixed)
     return fail(ctx, KB_ERR_WORKSPACE, "the fixed scratch holds %u candidates, %u asked for", ctx->ws_cap_K, K);
   const uint32_t cap = K < 32768u ? 2u * K : 65535u;
   const kb_status rc =
-      ensure_buf(ctx, &ctx->ws, &ctx->ws_bytes, ws_acc64_offset(cap) + ws_region(cap), "device workspace");
+      ensure_workspace(ctx, &ctx->ws, &ctx->ws_bytes, ws_acc64_offset(cap) + ws_region(cap), st, "device workspace");
   if (rc != KB_OK) return rc;
   ctx->ws_cap_K = cap;
   ctx->ws_dirty = true;   // fresh memory
@@ -354,7 +354,7 @@ extern "C" kb_status kb_ctx_destroy(kb_ctx* ctx) {
   ctx_free(ctx, ctx->srt);
   ctx_free(ctx, ctx->small_ws);
   ctx_free(ctx, ctx->ops_ws);
-  for (unsigned char* p : ctx->ops_ws_outgrown) ctx_free(ctx, p);
+  for (void* p : ctx->outgrown) ctx_free(ctx, p);
   for (int i = 0; i < 2; ++i) {
     ctx_free(ctx, ctx->st_batch[i]);
     if (ctx->ev_copied[i]) cudaEventDestroy(ctx->ev_copied[i]);
@@ -735,7 +735,7 @@ kb_status screen_impl(kb_ctx* ctx, const void* d_ref, const void* const* h_cands
     KB_CUDA(ctx, cudaGetLastError());
     return KB_OK;
   }
-  kb_status rc = ensure_ws(ctx, K);
+  kb_status rc = ensure_ws(ctx, K, st);
   if (rc != KB_OK) return rc;
   const void** table = reinterpret_cast<const void**>(ctx->ws + ws_table_offset(ctx->ws_cap_K));
 
@@ -743,12 +743,8 @@ kb_status screen_impl(kb_ctx* ctx, const void* d_ref, const void* const* h_cands
   // kernel zeroes for the next call.  Whatever may have broken that is repaired with memsets.
   // A call that is being captured into a graph takes nothing on trust (the graph may be
   // replayed in any state) and leaves the workspace marked dirty for the calls after it.
-  cudaStreamCaptureStatus cap = cudaStreamCaptureStatusNone;
-  if (cudaStreamIsCapturing(st, &cap) != cudaSuccess) {
-    cudaGetLastError();
-    cap = cudaStreamCaptureStatusActive;
-  }
-  const bool capturing = cap != cudaStreamCaptureStatusNone;
+  const bool capturing = is_capturing(st);
+  ctx->captured |= capturing;
   if (capturing || ctx->ws_dirty) {
     KB_CUDA(ctx, cudaMemsetAsync(ctx->ws, 0, 2 * ws_region(ctx->ws_cap_K), st));
     KB_CUDA(ctx, cudaMemsetAsync(counter_set(ctx, 0), 0, 16 * sizeof(unsigned int), st));   // both sets, the sums
@@ -984,7 +980,8 @@ extern "C" kb_status kb_screen_f64(kb_ctx* ctx, const double* d_ref, const doubl
   }
   DeviceGuard g(ctx->device);
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-  kb_status rc = ensure_ws(ctx, K);
+  ctx->captured |= is_capturing(st);
+  kb_status rc = ensure_ws(ctx, K, st);
   if (rc != KB_OK) return rc;
   // its own accumulator region and counters, zeroed by its prep kernel: independent of the
   // binary32 gate's two sets
@@ -1342,7 +1339,8 @@ extern "C" kb_status kb_adjudicate(kb_ctx* ctx, const float* d_timings, uint32_t
     return fail(ctx, KB_ERR_UNSUPPORTED, "kb_adjudicate: the binary-search win count needs S <= 4096");
   if (ctx->wins_algo == 3 && d_wins && S > kMergeMaxS)
     return fail(ctx, KB_ERR_UNSUPPORTED, "kb_adjudicate: the merge win count needs S <= %u", kMergeMaxS);
-  if (rank && ensure_buf(ctx, &ctx->srt, &ctx->srt_bytes, (size_t)K * S * sizeof(float), "sorted timings") != KB_OK) {
+  if (rank) ctx->captured |= is_capturing(st);
+  if (rank && ensure_workspace(ctx, &ctx->srt, &ctx->srt_bytes, (size_t)K * S * sizeof(float), st, "sorted timings") != KB_OK) {
     if (ctx->wins_algo >= 2) return KB_ERR_WORKSPACE;
     rank = false;     // no room for the sorted copy: count by direct comparison
   }
@@ -1565,7 +1563,8 @@ extern "C" kb_status kb_adjudicate_ragged(kb_ctx* ctx, const float* d_timings,
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   float* srt = nullptr;
   if (d_wins) {
-    kb_status rc = ensure_buf(ctx, &ctx->srt, &ctx->srt_bytes, (size_t)total * sizeof(float), "sorted timings");
+    ctx->captured |= is_capturing(st);
+    kb_status rc = ensure_workspace(ctx, &ctx->srt, &ctx->srt_bytes, (size_t)total * sizeof(float), st, "sorted timings");
     if (rc != KB_OK) return rc;
     srt = ctx->srt;
   }

@@ -137,42 +137,10 @@ kb_status launch_norm(kb_ctx* ctx, const NormParams& p, bool vec, bool e5m2, cud
               : e5m2 ? launch_norm<DT, false, 2>(ctx, p, st) : launch_norm<DT, false, 1>(ctx, p, st);
 }
 
-// The workspace of partial sums, with room for `need` bytes.  A launch that is being captured into a graph
-// keeps its address: from then on a buffer that is outgrown stays allocated until the context goes, and
-// growing (an allocation) is refused while the stream is captured.
+// The workspace of partial sums, with room for `need` bytes
 kb_status ensure_partials(kb_ctx* ctx, size_t need, cudaStream_t st) {
-  cudaStreamCaptureStatus status = cudaStreamCaptureStatusNone;
-  if (cudaStreamIsCapturing(st, &status) != cudaSuccess) {
-    cudaGetLastError();   // the default stream while another stream is captured
-    status = cudaStreamCaptureStatusActive;
-  }
-  const bool capturing = status != cudaStreamCaptureStatusNone;
-  if (need > ctx->ops_ws_bytes) {
-    if (capturing)
-      return fail(ctx, KB_ERR_WORKSPACE,
-                  "the workspace of partial parameter gradients would have to grow to %zu bytes while the stream is "
-                  "captured: call kb_layernorm_backward_reserve before the capture", need);
-    if (ctx->ops_ws_captured) {
-      try {
-        ctx->ops_ws_outgrown.reserve(ctx->ops_ws_outgrown.size() + 1);
-      } catch (...) {
-        return fail(ctx, KB_ERR_WORKSPACE, "no host memory to keep an outgrown workspace");
-      }
-      unsigned char* old = ctx->ops_ws;
-      ctx->ops_ws = nullptr;
-      const kb_status rc = ensure_buf(ctx, &ctx->ops_ws, &ctx->ops_ws_bytes, need, "partial parameter gradients");
-      if (rc != KB_OK) {
-        ctx->ops_ws = old;
-        return rc;
-      }
-      ctx->ops_ws_outgrown.push_back(old);
-      ctx->ops_ws_captured = false;
-    } else {
-      KB_TRY(ensure_buf(ctx, &ctx->ops_ws, &ctx->ops_ws_bytes, need, "partial parameter gradients"));
-    }
-  }
-  ctx->ops_ws_captured |= capturing;
-  return KB_OK;
+  ctx->captured |= is_capturing(st);
+  return ensure_workspace(ctx, &ctx->ops_ws, &ctx->ops_ws_bytes, need, st, "partial parameter gradients");
 }
 
 template <int DT, int NCH, bool VEC, bool WARP>

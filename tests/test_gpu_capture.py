@@ -1,0 +1,79 @@
+"""Gate and adjudication captured into CUDA graphs and mixed with other calls on the same context."""
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+
+
+def _ctx():
+    from paper_2608_02611_b200 import binding
+    return binding, binding.Context(0)
+
+
+def _tensors(n, k, seed):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed)
+    ref = torch.randn(n, generator=g, device=DEV).to(torch.bfloat16)
+    cands = []
+    for i in range(k):
+        c = ref.clone()
+        c[i::97 + i] += 1.0                    # i-dependent numbers of mismatches
+        cands.append(c)
+    return ref, cands
+
+
+def _capture(call):
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = call()
+    return graph, out
+
+
+def test_replays_after_the_workspaces_have_been_outgrown():
+    """A captured gate call and a captured adjudication still give their records after calls with more
+    candidates and more timings have outgrown both workspaces."""
+    kb, ctx = _ctx()
+    ctx.set_small_path(False)
+    ref, cands = _tensors(1 << 16, 5, 1)
+    t = torch.rand(40, 200, device=DEV) + 1.0
+    want = kb.records(ctx.screen(ref, cands, 1e-2, 1e-2)).tobytes()
+    median, iqr, wins = [v.clone() for v in ctx.adjudicate(t)]
+    graph, (out, adj) = _capture(lambda: (ctx.screen(ref, cands, 1e-2, 1e-2), ctx.adjudicate(t)))
+    for K in (1500, 5000):
+        ctx.screen(ref, [cands[i % 5] for i in range(K)], 1e-2, 1e-2)
+        ctx.adjudicate(torch.rand(K // 10, 1000, device=DEV) + 1.0)
+        held = torch.full((32 << 20,), 7.0, device=DEV)
+        out.fill_(0xEE)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert kb.records(out).tobytes() == want
+        for got, same in zip(adj, (median, iqr, wins)):
+            assert bool((got == same).all())
+        assert bool((held == 7.0).all())
+        del held
+    assert ctx.poll() == 0 and ctx.check_guards()[1] == 0
+    del graph, out, adj
+    ctx.close()
+
+
+def test_growth_of_the_gates_workspace_inside_a_capture_is_refused():
+    kb, ctx = _ctx()
+    ctx.set_small_path(False)
+    ref, cands = _tensors(4096, 2, 3)
+    many = [cands[i % 2] for i in range(3000)]
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with pytest.raises(kb.KbError) as e:
+        with torch.cuda.graph(graph):
+            ctx.screen(ref, many, 1e-2, 1e-2)
+    assert e.value.status == 4
+    want = kb.records(ctx.screen(ref, many, 1e-2, 1e-2)).tobytes()
+    graph, out = _capture(lambda: ctx.screen(ref, many, 1e-2, 1e-2))
+    graph.replay()
+    torch.cuda.synchronize()
+    assert kb.records(out).tobytes() == want
+    del graph, out
+    ctx.close()
