@@ -742,12 +742,17 @@ kb_status screen_impl(kb_ctx* ctx, const void* d_ref, const void* const* h_cands
   // Two sets of accumulators and counters: this call's (zero on entry) and the one its lead
   // kernel zeroes for the next call.  Whatever may have broken that is repaired with memsets.
   // A call that is being captured into a graph takes nothing on trust (the graph may be
-  // replayed in any state) and leaves the workspace marked dirty for the calls after it.
+  // replayed in any state) and, as its last step, zeroes both sets again: direct calls after a replay
+  // rely on them as if it had not run.
   const bool capturing = is_capturing(st);
   ctx->captured |= capturing;
-  if (capturing || ctx->ws_dirty) {
+  auto zero_sets = [&]() {
     KB_CUDA(ctx, cudaMemsetAsync(ctx->ws, 0, 2 * ws_region(ctx->ws_cap_K), st));
     KB_CUDA(ctx, cudaMemsetAsync(counter_set(ctx, 0), 0, 16 * sizeof(unsigned int), st));   // both sets, the sums
+    return KB_OK;
+  };
+  if (capturing || ctx->ws_dirty) {
+    if ((rc = zero_sets()) != KB_OK) return rc;
     ctx->used_K[0] = ctx->used_K[1] = 0;
     ctx->steps_hist[0] = ctx->steps_hist[1] = 0.0f;
   }
@@ -767,7 +772,7 @@ kb_status screen_impl(kb_ctx* ctx, const void* d_ref, const void* const* h_cands
       ctx->ws_parity = set ^ 1;
       ctx->ws_dirty = false;
     }
-    return KB_OK;
+    return capturing ? zero_sets() : KB_OK;
   };
 
   // Candidate pointers: up to kPtrsPerLaunch travel in the lead kernel's own arguments (it puts

@@ -59,6 +59,35 @@ def test_replays_after_the_workspaces_have_been_outgrown():
     ctx.close()
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float8_e4m3fn, torch.float64])
+def test_calls_between_replays_give_their_own_records(dtype):
+    """Replays and direct calls in turn, with numbers of candidates that differ: neither leaves anything behind
+    in the accumulators for the other."""
+    kb, ctx = _ctx()
+    ctx.set_small_path(False)
+    ref, cands = _tensors(1 << 16, 12, 2)
+    ref, cands = ref.to(dtype), [c.to(dtype) for c in cands]
+    screen, records = (ctx.screen_f64, kb.records_f64) if dtype == torch.float64 else (ctx.screen, kb.records)
+    fresh = kb.Context(0)
+    fresh.set_small_path(False)
+    one = fresh.screen_f64 if dtype == torch.float64 else fresh.screen
+    few, many = [records(one(ref, c, 1e-2, 1e-2)).tobytes() for c in (cands[:3], cands)]
+    fresh.close()
+    screen(ref, cands, 1e-2, 1e-2)
+    graph, out = _capture(lambda: screen(ref, cands, 1e-2, 1e-2))
+    for order in ("mrf", "rmfr", "frfm", "rrm", "mfrmrrfmffrrfrmfm"):
+        for step in order:
+            if step == "r":
+                graph.replay()
+                torch.cuda.synchronize()
+            got = {"r": lambda: out, "f": lambda: screen(ref, cands[:3], 1e-2, 1e-2),
+                   "m": lambda: screen(ref, cands, 1e-2, 1e-2)}[step]()
+            assert records(got).tobytes() == (few if step == "f" else many), (order, step)
+    assert ctx.poll() == 0
+    del graph, out
+    ctx.close()
+
+
 def test_growth_of_the_gates_workspace_inside_a_capture_is_refused():
     kb, ctx = _ctx()
     ctx.set_small_path(False)
