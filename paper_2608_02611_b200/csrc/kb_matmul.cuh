@@ -10,8 +10,9 @@
 // swizzle, and takes 4 matrix instructions.
 //
 // Roles: warp 0 copies (tensor maps; rows and columns outside a matrix read as zero), warp 1 (and 3
-// in the pair kernel) issues matrix instructions, warp 2 fetches scales, warps from 4 on scale and
-// add.  Every wait on a barrier in shared memory is bounded.
+// in the pair kernel) issues matrix instructions, warp 2 fetches scales (and, in the pair kernel, sees to
+// the rows with extreme scales at the end), warps from 4 on scale and add.  Every wait on a barrier in
+// shared memory is bounded.
 #pragma once
 
 #include "kb_block8.cuh"
@@ -381,7 +382,8 @@ struct PairTile {
   static constexpr int kEpiWarps = 8;
   // three warpgroups: one copies and issues, two scale and add.  168 registers per thread at
   // launch are split 56 / 224 / 224: 128 running sums and 32 values on their way need that many
-  // before the compiler stops moving them about (8192^3: 548 us, with 104 / 200 / 200 570).
+  // before the compiler stops moving them about (8192^3, when the split was chosen: 548 us, with
+  // 104 / 200 / 200 570; 570 now, with scales safe at both ends of the range).
   static constexpr int kThreads = 128 + 32 * kEpiWarps;
   static constexpr int kRegsLaunch = 168, kRegsControl = 56, kRegsEpi = 224;
   static_assert(128 * kRegsControl + (kThreads - 128) * kRegsEpi <= kThreads * kRegsLaunch, "register shares");

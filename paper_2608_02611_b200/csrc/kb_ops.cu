@@ -307,7 +307,7 @@ uint32_t lane_splits(const kb_ctx* ctx, uint64_t tiles, uint32_t KB) {
 // 128 x 128 tile of matmul_lanes_kernel, 0.52 us for a 256 x 256 tile of a pair.  The pair does four
 // times the work in it but needs 74 tiles to fill the card and cannot share a tile's K blocks:
 // 300x1000x2000 8.5 us by lanes and 18 by pairs, 512x512x8192 12 and 34, 256x4096x4096 14 and 21;
-// 1024x2048x4096 19 and 21; 512x8192x8192 85 and 36.
+// 1024x2048x4096 19 and 21; 512x8192x8192 85 and 38.
 bool lanes_are_faster(const kb_ctx* ctx, uint64_t M, uint64_t N, uint32_t KB) {
   const uint64_t lane_tiles = ((M + 127) / 128) * ((N + 127) / 128), pair_tiles = ((M + 255) / 256) * ((N + 255) / 256);
   const uint64_t sms = (uint64_t)ctx->sm_count, pairs = sms / 2, splits = lane_splits(ctx, lane_tiles, KB);

@@ -59,17 +59,18 @@ def test_replays_after_the_workspaces_have_been_outgrown():
     ctx.close()
 
 
-@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float8_e4m3fn, torch.float64])
-def test_calls_between_replays_give_their_own_records(dtype):
+@pytest.mark.parametrize("dtype,small", [(torch.bfloat16, False), (torch.float8_e4m3fn, False), (torch.float64, False),
+                                         (torch.bfloat16, True)])
+def test_calls_between_replays_give_their_own_records(dtype, small):
     """Replays and direct calls in turn, with numbers of candidates that differ: neither leaves anything behind
     in the accumulators for the other."""
     kb, ctx = _ctx()
-    ctx.set_small_path(False)
+    ctx.set_small_path(small)
     ref, cands = _tensors(1 << 16, 12, 2)
     ref, cands = ref.to(dtype), [c.to(dtype) for c in cands]
     screen, records = (ctx.screen_f64, kb.records_f64) if dtype == torch.float64 else (ctx.screen, kb.records)
     fresh = kb.Context(0)
-    fresh.set_small_path(False)
+    fresh.set_small_path(small)
     one = fresh.screen_f64 if dtype == torch.float64 else fresh.screen
     few, many = [records(one(ref, c, 1e-2, 1e-2)).tobytes() for c in (cands[:3], cands)]
     fresh.close()
