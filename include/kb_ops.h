@@ -110,8 +110,8 @@ kb_status kb_layernorm_backward_reserve(kb_ctx* ctx, uint64_t rows, uint64_t col
  *     D[m][n] = sum over blocks kb of  SA[kb][m] * SB[kb][n or n/128] * sum_{k in kb} A[m][k] * B[n][k]
  * The inner sums run on the tensor cores in binary32; they are scaled and added in binary32, in
  * an order that the sizes alone fix, and D is rounded once.  Finite scales overflow or underflow only
- * where a block's part of D does, not in their own product (rows of a large product in which that product
- * leaves binary32 take plain arithmetic, far slower than the tensor cores).
+ * where a block's part of D does, not in their own product (rows of a large product with tile scales in which
+ * that product leaves binary32 are computed twice, the second time far slower).
  *
  *   d_a, d_b     DEVICE codes A [M][K] and B [N][K] (KB_F8E4M3 or KB_F8E5M2 each), row strides
  *                lda and ldb; pointers 16-byte aligned, strides multiples of 16.

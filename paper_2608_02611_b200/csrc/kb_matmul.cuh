@@ -453,63 +453,91 @@ __device__ __forceinline__ void store_warp_tile(const MatmulParams& p, unsigned 
 }
 
 // Tile scales: the rows, of 32 rows x 128 columns of D (one tile of B), for which some K block's product of
-// scales is no normal number, element by element in plain arithmetic.  Such scales come from values around
-// 2^-60, or 2^60, on both sides at once, so nothing of this stands in the loops of the kernel: a second
-// path there cost 11% of 8192^3, and four branches per K block 4%.  Rows whose codes are 0 wherever the
-// product underflows are left alone.
-template <bool E5M2>
-__device__ __forceinline__ void widen_codes(uint32_t w, float (&v)[4]) {
-  uint32_t lo, hi;
-  ElemF8<E5M2>::widen4(w, lo, hi);
-  const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&lo)), b = __half22float2(*reinterpret_cast<const __half2*>(&hi));
-  v[0] = a.x;
-  v[1] = a.y;
-  v[2] = b.x;
-  v[3] = b.y;
-}
-// four codes from column k on of a row (16-byte aligned, k a multiple of 4) of K columns, 0 past its end
-__device__ __forceinline__ uint32_t code_word(const unsigned char* row, uint32_t k, uint32_t K) {
-  if (k + 4 <= K) return *reinterpret_cast<const uint32_t*>(row + k);
-  uint32_t w = 0;
-  for (uint32_t j = 0; k + j < K; ++j) w |= (uint32_t)row[k + j] << (8 * j);
+// scales is no normal number, once more by one warp.  Such scales come from values around 2^-60, or 2^60, on
+// both sides at once, so nothing of this stands in the loops of the kernel: a second path there cost 11%
+// of 8192^3, and four branches per K block 4%.  Rows whose codes are 0 wherever the product underflows are
+// left alone.  Codes are exact in binary16, so the block sums come from warp-wide matrix instructions on
+// 16 rows x 8 columns (2048 x 2560 x 1024 with every row taken: 90 ms element by element, so 5.7).
+// Eight codes of a row from column k (a multiple of 8) on, 0 past its K columns
+__device__ __forceinline__ uint2 code_pair(const unsigned char* row, uint32_t k, uint32_t K) {
+  if (k + 8 <= K) return *reinterpret_cast<const uint2*>(row + k);   // rows start on 16-byte boundaries
+  uint2 w = make_uint2(0u, 0u);
+  for (uint32_t j = 0; k + j < K; ++j) (j < 4 ? w.x : w.y) |= (uint32_t)row[k + j] << (8 * (j & 3));
   return w;
+}
+__device__ __forceinline__ void widen_codes(uint32_t w, bool e5m2, uint32_t& lo, uint32_t& hi) {
+  if (e5m2)
+    ElemF8<true>::widen4(w, lo, hi);
+  else
+    ElemF8<false>::widen4(w, lo, hi);
 }
 __device__ __forceinline__ void recompute_wide_rows(const MatmulParams& p, uint32_t m0, uint32_t n0, int lane) {
   if (n0 >= p.N) return;
   const float* bs = p.b_scale + (n0 >> 7);
   const uint32_t row = m0 + lane;
+  const unsigned char* codes = p.a + row * p.lda;
   bool need = false;
   for (uint32_t kb = 0; row < p.M && kb < p.KB && !need; ++kb) {
     const float r = p.a_scale[(uint64_t)kb * p.M + row], c = bs[(uint64_t)kb * p.b_scale_ld], s = r * c;
     if (!product_is_wide(s, r, c)) continue;
     need = fabsf(s) > 1.0f;
-    for (uint32_t k = 0; k < 128 && !need && kb * 128 + k < p.K; k += 4)
-      need = (code_word(p.a + row * p.lda, kb * 128 + k, p.K) & 0x7F7F7F7Fu) != 0;
+    for (uint32_t k = kb * 128; k < kb * 128 + 128 && !need; k += 8) {
+      const uint2 w = code_pair(codes, k, p.K);
+      need = ((w.x | w.y) & 0x7F7F7F7Fu) != 0;
+    }
   }
-  for (uint32_t rows = __ballot_sync(0xFFFFFFFFu, need); rows; rows &= rows - 1) {
-    const uint32_t m = m0 + __ffs(rows) - 1;
+  const uint32_t rows = __ballot_sync(0xFFFFFFFFu, need);
 #pragma unroll 1
-    for (uint32_t n = n0 + lane; n < n0 + 128 && n < p.N; n += 32) {
-      float d = 0.0f;
+  for (uint32_t half = 0; half < 2; ++half) {
+    if (((rows >> (16 * half)) & 0xFFFFu) == 0) continue;
+    // this lane's rows of the fragments (rows and columns outside D repeat the last one and are not stored)
+    const uint32_t g = half * 16 + (lane >> 2), r0 = min(m0 + g, p.M - 1), r1 = min(m0 + g + 8, p.M - 1);
+    const unsigned char *a0 = p.a + r0 * p.lda, *a1 = p.a + r1 * p.lda;
+#pragma unroll 1
+    for (uint32_t nt = n0; nt < n0 + 128 && nt < p.N; nt += 8) {
+      const unsigned char* b = p.b + min(nt + (lane >> 2), p.N - 1) * p.ldb;
+      float d[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 1
       for (uint32_t kb = 0; kb < p.KB; ++kb) {
-        float first = p.a_scale[(uint64_t)kb * p.M + m], second = bs[(uint64_t)kb * p.b_scale_ld], v = 0.0f;
-        for (uint32_t k = kb * 128; k < kb * 128 + 128 && k < p.K; k += 4) {
-          const uint32_t wa = code_word(p.a + m * p.lda, k, p.K), wb = code_word(p.b + n * p.ldb, k, p.K);
-          float x[4], y[4];
-          p.a_e5m2 ? widen_codes<true>(wa, x) : widen_codes<false>(wa, x);
-          p.b_e5m2 ? widen_codes<true>(wb, y) : widen_codes<false>(wb, y);
+        float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 2
+        for (uint32_t h = 0; h < 4; ++h) {
+          // four lanes hold 32 columns, 8 each: the order of the contraction is the same for both operands
+          const uint32_t k = kb * 128 + h * 32 + (lane & 3) * 8;
+          const uint2 wa = code_pair(a0, k, p.K), wc = code_pair(a1, k, p.K), wb = code_pair(b, k, p.K);
 #pragma unroll
-          for (int j = 0; j < 4; ++j) v = fmaf(x[j], y[j], v);
+          for (int w = 0; w < 2; ++w) {
+            uint32_t x0, x1, y0, y1, z0, z1;
+            widen_codes(w ? wa.y : wa.x, p.a_e5m2, x0, x1);
+            widen_codes(w ? wc.y : wc.x, p.a_e5m2, y0, y1);
+            widen_codes(w ? wb.y : wb.x, p.b_e5m2, z0, z1);
+            asm volatile(
+                "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                : "+f"(v[0]), "+f"(v[1]), "+f"(v[2]), "+f"(v[3])
+                : "r"(x0), "r"(y0), "r"(x1), "r"(y1), "r"(z0), "r"(z1));
+          }
         }
-        if (product_is_wide(first * second, first, second)) {
-          second *= take_over(first);
-        } else {
-          second *= first;
-          first = 1.0f;
+        const float c = bs[(uint64_t)kb * p.b_scale_ld];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          float first = p.a_scale[(uint64_t)kb * p.M + (i ? r1 : r0)], second = c;
+          if (product_is_wide(first * c, first, c)) {
+            second *= take_over(first);
+          } else {
+            second *= first;
+            first = 1.0f;
+          }
+          d[2 * i] = fmaf(v[2 * i] * first, second, d[2 * i]);
+          d[2 * i + 1] = fmaf(v[2 * i + 1] * first, second, d[2 * i + 1]);
         }
-        d = fmaf(v * first, second, d);
       }
-      store_down<1>(p, m, n, &d);
+      const uint32_t col = nt + (lane & 3) * 2;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        if (((rows >> (g + 8 * i)) & 1u) == 0) continue;
+        if (col < p.N) store_down<1>(p, i ? r1 : r0, col, &d[2 * i]);
+        if (col + 1 < p.N) store_down<1>(p, i ? r1 : r0, col + 1, &d[2 * i + 1]);
+      }
     }
   }
 }

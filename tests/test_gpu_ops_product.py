@@ -155,3 +155,25 @@ def test_product_with_scales_at_the_ends_of_the_range(ctx, M, N, K, rows, tiles)
             same = ~touched_m[:, None] & ~touched_n[None, :]
             assert bool((d[same] == clean[same]).all())
         assert bool((ctx.matmul_blocks(a, sa, b, sb, out_dtype=out)[inside] == d[inside]).all())
+
+
+@pytest.mark.parametrize("ta", [E4M3, E5M2])
+@pytest.mark.parametrize("tb", [E4M3, E5M2])
+@pytest.mark.parametrize("M,N,K", [(2305, 2111, 500), (2200, 2400, 261)])
+@pytest.mark.parametrize("scale,code", [((2.0 ** -70, 2.0 ** -71), 64.0), ((2.0 ** 99, 2.0 ** 29), 2.0 ** -6)])
+def test_product_by_pairs_with_every_row_at_the_end_of_the_range(ctx, M, N, K, ta, tb, scale, code):
+    """Tile scales whose product underflows or overflows for every row and block, with codes that bring the
+    result back into the range: in every format, ragged in every direction, into rows at any alignment."""
+    kb = -(-K // 128)
+    a, b = _operand(M, K, ta, 1, code), _operand(N, K, tb, 2, code)
+    sa = torch.full((kb, M), scale[0], device=DEV)
+    sb = torch.full((kb, -(-N // 128)), scale[1], device=DEV)
+    want, size = _product64(a, sa, b, sb, True)
+    inside = size < 2.0 ** 127                             # elsewhere partial sums may overflow
+    assert float(inside.double().mean()) > 0.1
+    held = torch.full((M + 2, N + 3), -3.0, device=DEV)
+    d = ctx.matmul_blocks(a, sa, b, sb, out=held[1:-1, :N])
+    assert ctx.last_product == (256, 1)
+    bound = _product_bound(want, size, K, torch.float32) + (kb + 2) * 2.0 ** -149
+    _within(d[inside], want[inside], bound[inside])
+    assert bool((held[0] == -3.0).all()) and bool((held[-1] == -3.0).all()) and bool((held[:, N:] == -3.0).all())
