@@ -32,6 +32,12 @@
  *     been synchronised.  Host arrays passed in (h_cands) are consumed before
  *     the call returns.  One kb_ctx must not be used from two streams or two
  *     host threads at the same time.
+ *   - Graphs: calls may be captured into a CUDA graph.  Nothing is allocated inside
+ *     a capture: a call whose workspace would have to grow is refused with
+ *     KB_ERR_WORKSPACE (kb_adjudicate counts wins without one instead), so make
+ *     a call of that size before.  What a graph uses stays allocated until
+ *     kb_ctx_destroy; a graph runs neither after that nor at the same time as
+ *     another call or graph on the context.
  *   - Errors: a kb_status is returned; nothing aborts or throws.  Argument
  *     errors are detected before any launch and leave the outputs untouched.
  *     Conditions only the device can see (a non-finite timing, a bounded wait

@@ -107,3 +107,17 @@ def test_growth_of_the_gates_workspace_inside_a_capture_is_refused():
     assert kb.records(out).tobytes() == want
     del graph, out
     ctx.close()
+
+
+def test_first_adjudication_inside_a_capture_counts_without_a_workspace():
+    kb, ctx = _ctx()
+    t = torch.rand(40, 200, device=DEV) + 1.0
+    graph, adj = _capture(lambda: ctx.adjudicate(t))
+    graph.replay()
+    torch.cuda.synchronize()
+    held = [v.clone() for v in adj]
+    for got, want in zip(held, ctx.adjudicate(t)):
+        assert bool((got == want).all())
+    assert ctx.poll() == 0
+    del graph, adj
+    ctx.close()
