@@ -286,7 +286,7 @@ __global__ void __launch_bounds__(LaneTile<BN>::kThreads, 1)
             tmem_ld16(taddr + a * BN + j0, v);
           else
             tmem_ld32(taddr + a * BN + j0, v);
-          tmem_wait_ld();
+          tmem_wait_ld(v);
           if (j0 + kCols == T::kEpiCols) {   // all of this accumulator is in registers
             tc_fence_before();
             mbar_arrive_if(&acc_empty[a], lane == 0);
@@ -758,7 +758,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PairTile::kThreads, 
             for (int j0 = 0; j0 < 128; j0 += 32) {
               float v[32];
               tmem_ld32(taddr + a * 256 + j0, v);
-              tmem_wait_ld();
+              tmem_wait_ld(v);
               if (j0 == 96) {   // all of this accumulator is in registers
                 tc_fence_before();
                 mbar_arrive_cluster_if(release0 + a * 8, lane == 0);
