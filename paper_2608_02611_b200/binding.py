@@ -1,4 +1,4 @@
-"""Binding of the kb C ABI (include/kb.h by ctypes, include/kb_ops.h by csrc/kb_torch.cpp):
+"""Binding of the kb C ABI (include/kb.h by ctypes, include/kb_ops.h and kb_attention.h by csrc/kb_torch.cpp):
 argument marshalling only.
 
 Every step of the path runs in the CUDA library; torch is used here for device
@@ -52,7 +52,15 @@ EXPORTS = [
     "kb_select_by_score", "kb_tail_ratios", "kb_copeland", "kb_confirm",
     "kb_ctx_fail_next_allocs", "kb_ctx_selftest_wait", "kb_ctx_check_guards", "kb_static_scratch_read", "kb_ctx_set_filter", "kb_ctx_last_filter", "kb_ctx_last_product",
     "kb_quantize_blocks", "kb_layernorm", "kb_layernorm_backward", "kb_layernorm_backward_reserve", "kb_matmul_blocks",
+    "kb_qk_norm_rope", "kb_attention", "kb_attention_paged", "kb_attention_paged_reserve",
 ]
+
+
+class PagedCache(ctypes.Structure):
+    """kb_paged_cache"""
+    _fields_ = [("d_k", ctypes.c_void_p), ("d_v", ctypes.c_void_p),
+                *((name, ctypes.c_uint64) for name in ("k_page", "k_row", "k_head", "v_page", "v_row", "v_head", "pages")),
+                ("page_size", ctypes.c_uint32)]
 
 
 class KbError(RuntimeError):
@@ -120,6 +128,13 @@ def load() -> ctypes.CDLL:
     L.kb_layernorm_backward.argtypes = [vp, vp, u64, vp, u64, u64, u64, i32, vp, i32, vp, vp, vp, u64, vp, vp, vp]
     L.kb_layernorm_backward_reserve.argtypes = [vp, u64, u64, vp]
     L.kb_matmul_blocks.argtypes = [vp, vp, u64, i32, vp, vp, u64, i32, vp, i32, u64, u64, u64, vp, u64, i32, vp]
+    cache = ctypes.POINTER(PagedCache)
+    L.kb_qk_norm_rope.argtypes = [vp, vp, u64, u64, u32, vp, u64, u64, u32, u64, u32, i32, i32, vp, vp, i32, f32, vp, vp, u32, i32,
+                                  vp, u64, u64, vp, u64, u64, vp, u64, u64, cache, vp, vp]
+    L.kb_attention.argtypes = [vp, vp, u64, u64, u32, u64, vp, u64, u64, vp, u64, u64, u32, u64, u32, i32, vp, vp, u32, i32, f32, vp, u64, u64,
+                               vp, vp]
+    L.kb_attention_paged.argtypes = [vp, vp, u64, u64, u32, cache, u32, u32, i32, vp, u64, u32, vp, u32, f32, vp, u64, u64, vp, vp]
+    L.kb_attention_paged_reserve.argtypes = [vp, vp]
     for name in EXPORTS:
         if name != "kb_last_error":
             getattr(L, name).restype = i32
@@ -633,7 +648,8 @@ def _native():
             raise ImportError(f"_kb_torch.so was built for {_kb_torch.built_for}, this is {native_marker()}: build it again "
                               "(python -m paper_2608_02611_b200.build)")
         _kb_torch.bind(KbError, *[ctypes.cast(getattr(L, name), ctypes.c_void_p).value for name in (
-            "kb_quantize_blocks", "kb_layernorm", "kb_layernorm_backward", "kb_matmul_blocks", "kb_last_error")])
+            "kb_quantize_blocks", "kb_layernorm", "kb_layernorm_backward", "kb_matmul_blocks", "kb_last_error",
+            "kb_qk_norm_rope", "kb_attention", "kb_attention_paged")])
         _native_module = _kb_torch
     return _native_module
 
@@ -696,6 +712,73 @@ def matmul_blocks(self, a: torch.Tensor, a_scale: torch.Tensor, b: torch.Tensor,
     """
     return (_native_module or _native()).matmul_blocks(self._h, self.device.index, a, a_scale, b, b_scale,
                                                        DTYPE_CODE.get(out_dtype, -1), out)
+
+
+# ---- attention (include/kb_attention.h) ------------------------------------------------------
+# Forms of a serving path: no gradients.  Heads are [tokens, heads, dim] with adjacent elements and any other strides, so that
+# slices of one projection [tokens, (q heads + 2 kv heads) dim] need no copy.
+
+class AttentionResult(NamedTuple):
+    """What the attention calls return; lse is None unless it was asked for."""
+    out: torch.Tensor
+    lse: Optional[torch.Tensor]
+
+
+@_ctx_method
+def qk_norm_rope(self, q: torch.Tensor, k: torch.Tensor, positions: Optional[torch.Tensor] = None,
+                 inv_freq: Optional[torch.Tensor] = None, q_weight: Optional[torch.Tensor] = None,
+                 k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6, *, norm: bool = True, interleaved: bool = False,
+                 want_q: bool = True, want_k: bool = True, v: Optional[torch.Tensor] = None,
+                 k_cache: Optional[torch.Tensor] = None, v_cache: Optional[torch.Tensor] = None,
+                 slots: Optional[torch.Tensor] = None, out=(None, None)):
+    """kb_qk_norm_rope -> (q, k): each head of ``q`` [tokens, q heads, dim] and ``k`` [tokens, kv heads, dim] divided by
+    its root mean square (unless ``norm`` is false) and turned by its token's position.
+
+    ``positions`` int64 [tokens]; ``inv_freq`` float64 [pairs], radians per position, turns the first 2 * pairs elements:
+    halves against each other, or neighbours with ``interleaved``; None turns nothing.  With ``k_cache`` and ``v_cache``
+    [pages, page size, kv heads, dim] the turned keys and ``v`` also go to ``slots`` (int64 [tokens]: page * page size +
+    place on it; negative: not stored).  ``want_q``/``want_k`` false: that output is None and is not computed, or only
+    stored.  ``out``: tensors to write to, q and k themselves among them.
+    """
+    return (_native_module or _native()).qk_norm_rope(self._h, self.device.index, q, k, positions, inv_freq, q_weight, k_weight,
+                                                      eps, norm, interleaved, want_q, want_k, v, k_cache, v_cache, slots, *out)
+
+
+@_ctx_method
+def attention(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_offsets: Optional[torch.Tensor] = None,
+              k_offsets: Optional[torch.Tensor] = None, *, causal: bool = True, scale: Optional[float] = None,
+              want_lse: bool = False, out: Optional[torch.Tensor] = None) -> AttentionResult:
+    """kb_attention over packed prompts: ``q`` [tokens, q heads, dim], ``k`` and ``v`` [keys, kv heads, dim], fp16 or bf16.
+
+    Sequence s has the queries q_offsets[s] .. q_offsets[s + 1] (int32) and the keys between its ``k_offsets``
+    (``q_offsets`` unless given; one sequence of all tokens without either); its last query sees all of its
+    keys and each earlier one a key less, unless ``causal`` is false.  ``scale`` is 1 / sqrt(dim) unless given.
+    lse: float32 [tokens, q heads].  Queries that see nothing give zeros and -infinity; rows of the outputs
+    outside every sequence are not written.
+    """
+    return AttentionResult(*(_native_module or _native()).attention(self._h, self.device.index, q, k, v, q_offsets, k_offsets, causal,
+                                                                    scale, want_lse, out))
+
+
+@_ctx_method
+def attention_paged(self, q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, table: torch.Tensor,
+                    lengths: torch.Tensor, *, scale: Optional[float] = None, want_lse: bool = False,
+                    out: Optional[torch.Tensor] = None) -> AttentionResult:
+    """kb_attention_paged: one new token per sequence, ``q`` [sequences, q heads, dim] (fp16 or bf16), over the first
+    ``lengths`` (int32 [sequences]) keys on the pages that ``table`` (int32 [sequences, pages]) names in the caches
+    [pages, page size, kv heads, dim].
+
+    ``scale`` is 1 / sqrt(dim) unless given.  lse: float32 [sequences, q heads].  An empty sequence gives zeros and
+    -infinity; a length or page that is not there is left out and shows in ``poll``.
+    """
+    return AttentionResult(*(_native_module or _native()).attention_paged(self._h, self.device.index, q, k_cache, v_cache, table,
+                                                                          lengths, scale, want_lse, out))
+
+
+@_ctx_method
+def reserve_attention_paged(self):
+    """kb_attention_paged_reserve: the workspace, for calls that are then captured into a CUDA graph."""
+    self._check(load().kb_attention_paged_reserve(self._h, _stream_ptr(self.device)), "kb_attention_paged_reserve")
 
 
 def records_f64(screen_out: torch.Tensor) -> np.ndarray:

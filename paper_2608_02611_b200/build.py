@@ -1,8 +1,8 @@
 """Build the CUDA library in-tree:  python -m paper_2608_02611_b200.build
 
-Two translation units (csrc/kb_host.cu: the gate, adjudication and selection; csrc/kb_ops.cu:
-the model operators) compiled by nvcc for sm_100a into paper_2608_02611_b200/libkb.so, a plain
-C-ABI shared library (include/kb.h, include/kb_ops.h); and csrc/kb_torch.cpp, compiled by g++ against
+Three translation units (csrc/kb_host.cu: the gate, adjudication and selection; csrc/kb_ops.cu:
+the operators of a linear layer; csrc/kb_attention.cu: those of an attention block) compiled by nvcc for sm_100a into paper_2608_02611_b200/libkb.so, a plain
+C-ABI shared library (include/kb.h, include/kb_ops.h, include/kb_attention.h); and csrc/kb_torch.cpp, compiled by g++ against
 torch's headers into paper_2608_02611_b200/_kb_torch.so, the native half of the operators' binding.
 The gate, and the operators from C, need only the former.
 """
@@ -18,7 +18,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libkb.so")
 NATIVE = os.path.join(HERE, "_kb_torch.so")
 NATIVE_SOURCE = os.path.join(CSRC, "kb_torch.cpp")
-SOURCES = ["kb_host.cu", "kb_ops.cu"]
+SOURCES = ["kb_host.cu", "kb_ops.cu", "kb_attention.cu"]
 INCLUDE = os.path.join(HERE, "..", "include")
 
 NVCC_FLAGS = [

@@ -1,0 +1,443 @@
+// Host side of the attention operators: argument checks, choice of kernel, launch.
+// Declarations and their contracts are in include/kb_attention.h.
+#include <algorithm>
+#include <cmath>
+
+#include "../../include/kb_attention.h"
+#include "kb_ctx.cuh"
+#include "kb_paged.cuh"
+#include "kb_prompt.cuh"
+#include "kb_rope.cuh"
+
+using namespace kb;
+
+namespace {
+
+constexpr uint64_t kMaxStride = 1ull << 40;   // elements
+
+// Heads of a batch, [tokens][heads][dim]: not null, element-aligned, strides that an address can hold.
+struct Heads {
+  const char* name;
+  const void* p;
+  uint64_t row, head;
+};
+kb_status check_heads(kb_ctx* ctx, const char* where, const Heads& t, int bytes) {
+  if (!t.p) return fail(ctx, KB_ERR_INVALID_ARG, "%s: %s is NULL", where, t.name);
+  if (!aligned_to(t.p, bytes)) return fail(ctx, KB_ERR_ALIGNMENT, "%s: %s is not aligned to its element type", where, t.name);
+  if (t.row > kMaxStride || t.head > kMaxStride)
+    return fail(ctx, KB_ERR_INVALID_ARG, "%s: a stride of %s is beyond 2^40 elements", where, t.name);
+  return KB_OK;
+}
+// The same for an output, no two elements of which may be one
+kb_status check_out(kb_ctx* ctx, const char* where, const Heads& t, uint64_t tokens, uint64_t heads, uint64_t dim, int bytes) {
+  KB_TRY(check_heads(ctx, where, t, bytes));
+  const bool by_row = (tokens <= 1 || t.row >= (heads - 1) * t.head + dim) && (heads <= 1 || t.head >= dim);
+  const bool by_head = (heads <= 1 || t.head >= (tokens - 1) * t.row + dim) && (tokens <= 1 || t.row >= dim);
+  if (!by_row && !by_head) return fail(ctx, KB_ERR_INVALID_ARG, "%s: the strides of %s let its rows overlap", where, t.name);
+  return KB_OK;
+}
+// Rows start on 16-byte boundaries
+bool heads_aligned(const void* p, uint64_t row, uint64_t head, int bytes) {
+  return aligned16(p) && (row * bytes) % 16 == 0 && (head * bytes) % 16 == 0;
+}
+// Number of heads and dim, as every call has them
+kb_status check_sizes(kb_ctx* ctx, const char* where, uint32_t q_heads, uint32_t kv_heads, uint32_t dim, uint32_t most) {
+  if (dim == 0 || dim > most) return fail(ctx, KB_ERR_UNSUPPORTED, "%s: dim %u is not within 1 .. %u", where, dim, most);
+  if (q_heads == 0 || kv_heads == 0 || q_heads > 65536 || q_heads % kv_heads != 0)
+    return fail(ctx, KB_ERR_INVALID_ARG, "%s: %u query heads are not a multiple (up to 65536) of %u key heads", where, q_heads, kv_heads);
+  return KB_OK;
+}
+kb_status check_cache(kb_ctx* ctx, const char* where, const kb_paged_cache& c, int bytes) {
+  KB_TRY(check_heads(ctx, where, {"the cache's keys", c.d_k, c.k_row, c.k_head}, bytes));
+  KB_TRY(check_heads(ctx, where, {"the cache's values", c.d_v, c.v_row, c.v_head}, bytes));
+  if (c.k_page > kMaxStride || c.v_page > kMaxStride)
+    return fail(ctx, KB_ERR_INVALID_ARG, "%s: a stride of the cache's pages is beyond 2^40 elements", where);
+  if (c.page_size == 0 || c.pages > 0x7FFFFFFFull / c.page_size)
+    return fail(ctx, KB_ERR_INVALID_ARG, "%s: a cache of %llu pages of %u slots (1 .. 2^31 - 1 slots in all)", where,
+                (unsigned long long)c.pages, c.page_size);
+  return KB_OK;
+}
+
+// ---- norms and rotation ------------------------------------------------------------------------
+
+template <int DT, int L>
+kb_status launch_rope(kb_ctx* ctx, const RopeParams& p, bool vec, cudaStream_t st) {
+  // a token per CTA until they fill the card, then several, so that the weights and the start are paid for less often
+  const uint32_t per = p.tokens >= 16ull * ctx->sm_count ? kRopeTokens : 1;
+  const unsigned int grid = (unsigned int)((p.tokens + per - 1) / per);
+  if (vec)
+    qk_norm_rope_kernel<DT, L, true><<<grid, kRopeThreads, 0, st>>>(p, per);
+  else
+    qk_norm_rope_kernel<DT, L, false><<<grid, kRopeThreads, 0, st>>>(p, per);
+  return launched(ctx);
+}
+template <int DT>
+kb_status launch_rope(kb_ctx* ctx, const RopeParams& p, bool vec, cudaStream_t st) {
+  if (p.dim <= 64) return launch_rope<DT, 8>(ctx, p, vec, st);
+  if (p.dim <= 128) return launch_rope<DT, 16>(ctx, p, vec, st);
+  return launch_rope<DT, 32>(ctx, p, vec, st);
+}
+
+// ---- paged attention ---------------------------------------------------------------------------
+
+// CTAs per SM of the kernel, by its registers and shared memory (launch bounds), and the most of any variant
+constexpr uint32_t paged_per_sm(int nt) { return nt == 1 ? 2 : 1; }
+constexpr uint32_t kPagedMostHeads = 16, kPagedMostDim = 128;
+
+struct PagedSpace {
+  size_t part, rl, arrived, bytes;
+  explicit PagedSpace(const kb_ctx* ctx) {   // for the largest grid with the fewest heads, and the reverse: the same
+    const size_t slots = 2ull * ctx->sm_count * 2;
+    part = 0;
+    rl = slots * kPagedMostHeads * kPagedMostDim * sizeof(float);
+    arrived = rl + slots * kPagedMostHeads * 2 * sizeof(float);
+    bytes = arrived + slots * sizeof(unsigned int);
+  }
+};
+kb_status ensure_paged(kb_ctx* ctx, cudaStream_t st) {
+  ctx->captured |= is_capturing(st);
+  const PagedSpace space(ctx);
+  if (ctx->paged_ws_bytes >= space.bytes) return KB_OK;
+  KB_TRY(ensure_workspace(ctx, &ctx->paged_ws, &ctx->paged_ws_bytes, space.bytes, st, "parts of divided sequences"));
+  const cudaError_t e = cudaMemset(ctx->paged_ws + space.arrived, 0, space.bytes - space.arrived);
+  if (e != cudaSuccess || cudaStreamSynchronize(nullptr) != cudaSuccess) {
+    ctx_free(ctx, ctx->paged_ws);
+    ctx->paged_ws = nullptr;
+    ctx->paged_ws_bytes = 0;
+    return fail(ctx, KB_ERR_CUDA, "the workspace of paged attention could not be zeroed");
+  }
+  return KB_OK;
+}
+
+template <int DT, int DP, int NT, bool PAGE16>
+kb_status launch_paged(kb_ctx* ctx, PagedParams& p, uint64_t most_units, cudaStream_t st) {
+  constexpr auto kernel = attention_paged_kernel<DT, DP, NT, PAGE16>;
+  constexpr size_t smem = sizeof(float) * kPagedWarps * 8 * NT * DP;
+  static_assert(smem <= 64 * 1024, "shared memory");
+  if (smem > 40 * 1024)   // raised to one fixed size, whatever thread or context calls
+    KB_CUDA(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+  const uint64_t grid = std::min<uint64_t>(most_units, (uint64_t)ctx->sm_count * paged_per_sm(NT));
+  if (grid * 8 * NT * sizeof(float) > smem) return fail(ctx, KB_ERR_UNSUPPORTED, "kb_attention_paged: a card of more SMs than foreseen");
+  kernel<<<(unsigned int)grid, kPagedThreads, smem, st>>>(p);
+  return launched(ctx);
+}
+template <int DT>
+kb_status launch_paged(kb_ctx* ctx, PagedParams& p, uint64_t most_units, cudaStream_t st) {
+  const bool wide = p.dim > 64, two = p.group > 8, page16 = p.page_size % 16 == 0;
+  if (wide) {
+    if (two) return page16 ? launch_paged<DT, 128, 2, true>(ctx, p, most_units, st) : launch_paged<DT, 128, 2, false>(ctx, p, most_units, st);
+    return page16 ? launch_paged<DT, 128, 1, true>(ctx, p, most_units, st) : launch_paged<DT, 128, 1, false>(ctx, p, most_units, st);
+  }
+  if (two) return page16 ? launch_paged<DT, 64, 2, true>(ctx, p, most_units, st) : launch_paged<DT, 64, 2, false>(ctx, p, most_units, st);
+  return page16 ? launch_paged<DT, 64, 1, true>(ctx, p, most_units, st) : launch_paged<DT, 64, 1, false>(ctx, p, most_units, st);
+}
+
+// ---- attention over prompts ----------------------------------------------------------------------
+
+// Tensor map of heads [tokens][heads][dim], boxes of 64 elements of dim and 128 tokens of a head in the 128-byte
+// swizzle; places outside the tensor read as zero.
+kb_status encode_heads(kb_ctx* ctx, CUtensorMap* map, const Heads& t, uint64_t tokens, uint32_t heads, uint32_t dim, kb_dtype dtype) {
+  const cuuint64_t dims[3] = {dim, tokens, heads}, strides[2] = {t.row * 2, t.head * 2};
+  const cuuint32_t box[3] = {64, 128, 1}, step[3] = {1, 1, 1};
+  const CUresult rc = reinterpret_cast<EncodeTiled>(ctx->encode_tiled)(
+      map, dtype == KB_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(t.p), dims, strides,
+      box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+      CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (rc != CUDA_SUCCESS) return fail(ctx, KB_ERR_CUDA, "cuTensorMapEncodeTiled failed with %d for %s", (int)rc, t.name);
+  return KB_OK;
+}
+
+template <int DT, int DP>
+kb_status prepare_prompt(kb_ctx* ctx) {
+  constexpr auto kernel = attention_kernel<DT, DP>;
+  KB_CUDA(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)PromptTile<DP>::kSmem));
+  // the warpgroups split the registers that the kernel is launched with; with fewer they would wait for the rest for good
+  cudaFuncAttributes attr = {};
+  KB_CUDA(ctx, cudaFuncGetAttributes(&attr, kernel));
+  if (attr.numRegs < PromptTile<DP>::kRegsLaunch)
+    return fail(ctx, KB_ERR_UNSUPPORTED, "kb_attention: the library was compiled with %d registers for a kernel that splits %d",
+                attr.numRegs, PromptTile<DP>::kRegsLaunch);
+  return KB_OK;
+}
+kb_status prepare_prompt(kb_ctx* ctx) {
+  if (ctx->attention_ready) return KB_OK;
+  KB_TRY(find_encoder(ctx, "kb_attention"));
+  KB_TRY((prepare_prompt<KB_F16, 64>(ctx)));
+  KB_TRY((prepare_prompt<KB_F16, 128>(ctx)));
+  KB_TRY((prepare_prompt<KB_BF16, 64>(ctx)));
+  KB_TRY((prepare_prompt<KB_BF16, 128>(ctx)));
+  ctx->attention_ready = true;
+  return KB_OK;
+}
+template <int DT, int DP>
+kb_status launch_prompt(kb_ctx* ctx, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const PromptParams& p,
+                        unsigned int grid, cudaStream_t st) {
+  attention_kernel<DT, DP><<<grid, PromptTile<DP>::kThreads, PromptTile<DP>::kSmem, st>>>(q, k, v, p);
+  return launched(ctx);
+}
+
+}  // namespace
+
+// ---------------------------------------------------------------------------
+// entry points
+// ---------------------------------------------------------------------------
+
+extern "C" kb_status kb_qk_norm_rope(kb_ctx* ctx, const void* d_q, uint64_t q_row, uint64_t q_head, uint32_t q_heads,
+                                     const void* d_k, uint64_t k_row, uint64_t k_head, uint32_t kv_heads,
+                                     uint64_t tokens, uint32_t dim, kb_dtype dtype, int norm, const void* d_q_weight,
+                                     const void* d_k_weight, kb_dtype param_dtype, float eps,
+                                     const int64_t* d_positions, const double* d_inv_freq, uint32_t rotary_dim,
+                                     int interleaved, void* d_q_out, uint64_t q_out_row, uint64_t q_out_head,
+                                     void* d_k_out, uint64_t k_out_row, uint64_t k_out_head, const void* d_v,
+                                     uint64_t v_row, uint64_t v_head, const kb_paged_cache* cache,
+                                     const int64_t* d_slots, void* stream) {
+  TraceRange trace("kb_qk_norm_rope");
+  if (!ctx) return KB_ERR_INVALID_ARG;
+  const char* where = "kb_qk_norm_rope";
+  if (!is_float_type(dtype)) return fail(ctx, KB_ERR_UNSUPPORTED, "%s: dtype %d is not fp32, fp16 or bf16", where, (int)dtype);
+  if (param_dtype != dtype && param_dtype != KB_F32)
+    return fail(ctx, KB_ERR_UNSUPPORTED, "%s: weights are of the heads' type or binary32", where);
+  KB_TRY(check_sizes(ctx, where, q_heads, kv_heads, dim, KB_ROPE_MAX_DIM));
+  if ((norm != 0 && norm != 1) || (interleaved != 0 && interleaved != 1))
+    return fail(ctx, KB_ERR_INVALID_ARG, "%s: norm and interleaved must be 0 or 1", where);
+  if (norm && (!(eps > 0.0f) || !std::isfinite(eps))) return fail(ctx, KB_ERR_INVALID_ARG, "%s: eps must be finite and > 0", where);
+  if (!norm && (d_q_weight || d_k_weight)) return fail(ctx, KB_ERR_INVALID_ARG, "%s: weights without the norm", where);
+  if (rotary_dim > dim || rotary_dim % 2 != 0)
+    return fail(ctx, KB_ERR_INVALID_ARG, "%s: rotary_dim %u is odd or more than dim %u", where, rotary_dim, dim);
+  if (tokens > KB_OPS_MAX_DIM) return fail(ctx, KB_ERR_INVALID_ARG, "%s: more than 2^30 tokens", where);
+  if (!d_q_out && !d_k_out && !cache && tokens) return fail(ctx, KB_ERR_INVALID_ARG, "%s: no output", where);
+  if (tokens == 0) return KB_OK;
+  const int e = elem_bytes(dtype), pe = elem_bytes(param_dtype);
+  if (d_q_out) {
+    KB_TRY(check_heads(ctx, where, {"d_q", d_q, q_row, q_head}, e));
+    KB_TRY(check_out(ctx, where, {"d_q_out", d_q_out, q_out_row, q_out_head}, tokens, q_heads, dim, e));
+  }
+  if (d_k_out || cache) KB_TRY(check_heads(ctx, where, {"d_k", d_k, k_row, k_head}, e));
+  if (d_k_out) KB_TRY(check_out(ctx, where, {"d_k_out", d_k_out, k_out_row, k_out_head}, tokens, kv_heads, dim, e));
+  // in place means the very same rows: others would be written while they are still to be read
+  if (d_q_out && d_q_out == d_q && (q_out_row != q_row || q_out_head != q_head))
+    return fail(ctx, KB_ERR_INVALID_ARG, "%s: d_q_out is d_q with other strides", where);
+  if (d_k_out && d_k_out == d_k && (k_out_row != k_row || k_out_head != k_head))
+    return fail(ctx, KB_ERR_INVALID_ARG, "%s: d_k_out is d_k with other strides", where);
+  if (cache) {
+    KB_TRY(check_heads(ctx, where, {"d_v", d_v, v_row, v_head}, e));
+    KB_TRY(check_cache(ctx, where, *cache, e));
+    if (!d_slots) return fail(ctx, KB_ERR_INVALID_ARG, "%s: a cache without d_slots", where);
+    if (!aligned_to(d_slots, 8)) return fail(ctx, KB_ERR_ALIGNMENT, "%s: d_slots is not aligned to its element type", where);
+  }
+  if (!aligned_to(d_q_weight, pe) || !aligned_to(d_k_weight, pe))
+    return fail(ctx, KB_ERR_ALIGNMENT, "%s: a weight is not aligned to its element type", where);
+  if (rotary_dim && (!d_positions || !d_inv_freq)) return fail(ctx, KB_ERR_INVALID_ARG, "%s: d_positions or d_inv_freq is NULL", where);
+  if (!aligned_to(d_positions, 8) || !aligned_to(d_inv_freq, 8))
+    return fail(ctx, KB_ERR_ALIGNMENT, "%s: d_positions or d_inv_freq is not aligned to its element type", where);
+  DeviceGuard g(ctx->device);
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  RopeParams p = {};
+  p.q = d_q;
+  p.q_row = q_row;
+  p.q_head = q_head;
+  p.k = d_k;
+  p.k_row = k_row;
+  p.k_head = k_head;
+  p.v = d_v;
+  p.v_row = v_row;
+  p.v_head = v_head;
+  p.q_out = d_q_out;
+  p.qo_row = q_out_row;
+  p.qo_head = q_out_head;
+  p.k_out = d_k_out;
+  p.ko_row = k_out_row;
+  p.ko_head = k_out_head;
+  if (cache) {
+    p.k_cache = cache->d_k;
+    p.v_cache = cache->d_v;
+    p.kc_page = cache->k_page;
+    p.kc_row = cache->k_row;
+    p.kc_head = cache->k_head;
+    p.vc_page = cache->v_page;
+    p.vc_row = cache->v_row;
+    p.vc_head = cache->v_head;
+    p.slots_end = cache->pages * cache->page_size;
+    p.page_size = cache->page_size;
+    p.slots = reinterpret_cast<const long long*>(d_slots);
+  }
+  p.positions = reinterpret_cast<const long long*>(d_positions);
+  p.inv_freq = d_inv_freq;
+  p.q_weight = d_q_weight;
+  p.k_weight = d_k_weight;
+  p.param_f32 = param_dtype == KB_F32;
+  p.norm = norm;
+  p.interleaved = interleaved;
+  p.eps = eps;
+  p.tokens = tokens;
+  p.hq = q_heads;
+  p.hkv = kv_heads;
+  p.first_row = d_q_out ? 0 : q_heads;
+  p.rows = q_heads + (d_k_out || cache ? kv_heads : 0) + (cache ? kv_heads : 0);
+  p.dim = dim;
+  p.half = rotary_dim / 2;
+  p.status = ctx->d_status;
+  const bool vec = dim % 8 == 0 && (interleaved || p.half % 8 == 0) && (!d_q_out || (heads_aligned(d_q, q_row, q_head, e) && heads_aligned(d_q_out, q_out_row, q_out_head, e))) &&
+                   (!(d_k_out || cache) || heads_aligned(d_k, k_row, k_head, e)) && (!d_k_out || heads_aligned(d_k_out, k_out_row, k_out_head, e)) &&
+                   (!cache || (heads_aligned(d_v, v_row, v_head, e) && heads_aligned(cache->d_k, cache->k_row, cache->k_head, e) &&
+                               heads_aligned(cache->d_v, cache->v_row, cache->v_head, e) && (cache->k_page * e) % 16 == 0 && (cache->v_page * e) % 16 == 0));
+  if (dtype == KB_F32) return launch_rope<KB_F32>(ctx, p, vec, st);
+  if (dtype == KB_F16) return launch_rope<KB_F16>(ctx, p, vec, st);
+  return launch_rope<KB_BF16>(ctx, p, vec, st);
+}
+
+extern "C" kb_status kb_attention(kb_ctx* ctx, const void* d_q, uint64_t q_row, uint64_t q_head, uint32_t q_heads,
+                                  uint64_t q_tokens, const void* d_k, uint64_t k_row, uint64_t k_head, const void* d_v,
+                                  uint64_t v_row, uint64_t v_head, uint32_t kv_heads, uint64_t k_tokens, uint32_t dim,
+                                  kb_dtype dtype, const int32_t* d_q_offsets, const int32_t* d_k_offsets,
+                                  uint32_t sequences, int causal, float scale, void* d_out, uint64_t out_row,
+                                  uint64_t out_head, float* d_lse, void* stream) {
+  TraceRange trace("kb_attention");
+  if (!ctx) return KB_ERR_INVALID_ARG;
+  const char* where = "kb_attention";
+  if (dtype != KB_F16 && dtype != KB_BF16) return fail(ctx, KB_ERR_UNSUPPORTED, "%s: dtype %d is not fp16 or bf16", where, (int)dtype);
+  KB_TRY(check_sizes(ctx, where, q_heads, kv_heads, dim, KB_ATTENTION_MAX_DIM));
+  if (dim % 8 != 0) return fail(ctx, KB_ERR_UNSUPPORTED, "%s: dim %u is not a multiple of 8", where, dim);
+  if (causal != 0 && causal != 1) return fail(ctx, KB_ERR_INVALID_ARG, "%s: causal must be 0 or 1", where);
+  if (!(scale > 0.0f) || !std::isfinite(scale)) return fail(ctx, KB_ERR_INVALID_ARG, "%s: scale must be finite and > 0", where);
+  if (q_tokens > KB_OPS_MAX_DIM || k_tokens > KB_OPS_MAX_DIM || sequences > KB_OPS_MAX_DIM)
+    return fail(ctx, KB_ERR_INVALID_ARG, "%s: tokens or sequences beyond 2^30", where);
+  if ((d_q_offsets == nullptr) != (d_k_offsets == nullptr) || (!d_q_offsets && sequences != 1))
+    return fail(ctx, KB_ERR_INVALID_ARG, "%s: offsets of queries and keys come together, and without them there is one sequence", where);
+  if (q_tokens == 0 || sequences == 0) return KB_OK;
+  Heads q{"d_q", d_q, q_row, q_head}, k{"d_k", d_k, k_row, k_head}, v{"d_v", d_v, v_row, v_head};
+  KB_TRY(check_heads(ctx, where, q, 2));
+  KB_TRY(check_out(ctx, where, {"d_out", d_out, out_row, out_head}, q_tokens, q_heads, dim, 2));
+  if (k_tokens) {
+    KB_TRY(check_heads(ctx, where, k, 2));
+    KB_TRY(check_heads(ctx, where, v, 2));
+  } else {   // no key anywhere: the copies that are never made still want an address
+    k.p = v.p = d_q;
+    k.row = v.row = k.head = v.head = 8;
+  }
+  for (const Heads& t : {q, k, v}) {
+    if (!heads_aligned(t.p, t.row, t.head, 2)) return fail(ctx, KB_ERR_ALIGNMENT, "%s: %s needs 16-byte aligned pointers and strides", where, t.name);
+    if (t.row == 0 || t.head == 0 || t.row >= kMaxStride / 2 || t.head >= kMaxStride / 2)
+      return fail(ctx, KB_ERR_INVALID_ARG, "%s: a stride of %s is 0 or beyond 2^39 elements", where, t.name);
+  }
+  if (!aligned_to(d_q_offsets, 4) || !aligned_to(d_k_offsets, 4) || !aligned_to(d_lse, 4))
+    return fail(ctx, KB_ERR_ALIGNMENT, "%s: offsets or d_lse are not aligned to their element type", where);
+  DeviceGuard g(ctx->device);
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  KB_TRY(prepare_prompt(ctx));
+  CUtensorMap map_q, map_k, map_v;
+  KB_TRY(encode_heads(ctx, &map_q, q, q_tokens, q_heads, dim, dtype));
+  KB_TRY(encode_heads(ctx, &map_k, k, std::max<uint64_t>(k_tokens, 1), kv_heads, dim, dtype));
+  KB_TRY(encode_heads(ctx, &map_v, v, std::max<uint64_t>(k_tokens, 1), kv_heads, dim, dtype));
+  PromptParams p = {};
+  p.q_offsets = d_q_offsets;
+  p.k_offsets = d_k_offsets;
+  p.sequences = sequences;
+  p.q_tokens = (uint32_t)q_tokens;
+  p.k_tokens = (uint32_t)k_tokens;
+  p.hq = q_heads;
+  p.group = q_heads / kv_heads;
+  p.dim = dim;
+  p.pair = p.group % 2 == 0;
+  p.causal = causal;
+  p.vec_out = aligned16(d_out) && out_row % 8 == 0 && out_head % 8 == 0;
+  p.scale_log2 = (float)((double)scale * 1.4426950408889634);
+  p.q = q.p;
+  p.k = k.p;
+  p.v = v.p;
+  p.q_row = q_row;
+  p.q_head = q_head;
+  p.k_row = k_row;
+  p.k_head = k_head;
+  p.v_row = v_row;
+  p.v_head = v_head;
+  p.out = d_out;
+  p.o_row = out_row;
+  p.o_head = out_head;
+  p.lse = d_lse;
+  p.status = ctx->d_status;
+  // the lengths are the device's: room for every sequence's last, partial piece
+  const uint64_t rows = p.pair ? 128 : 256, pieces = d_q_offsets ? q_tokens / rows + sequences : (q_tokens + rows - 1) / rows;
+  const uint64_t grid = pieces * (p.pair ? q_heads / 2 : q_heads);
+  if (grid > 0x7FFFFFFFull) return fail(ctx, KB_ERR_UNSUPPORTED, "%s: more than 2^31 - 1 tiles", where);
+  const unsigned int n = (unsigned int)grid;
+  if (dim <= 64)
+    return dtype == KB_F16 ? launch_prompt<KB_F16, 64>(ctx, map_q, map_k, map_v, p, n, st) : launch_prompt<KB_BF16, 64>(ctx, map_q, map_k, map_v, p, n, st);
+  return dtype == KB_F16 ? launch_prompt<KB_F16, 128>(ctx, map_q, map_k, map_v, p, n, st) : launch_prompt<KB_BF16, 128>(ctx, map_q, map_k, map_v, p, n, st);
+}
+
+extern "C" kb_status kb_attention_paged_reserve(kb_ctx* ctx, void* stream) {
+  TraceRange trace("kb_attention_paged_reserve");
+  if (!ctx) return KB_ERR_INVALID_ARG;
+  DeviceGuard g(ctx->device);
+  return ensure_paged(ctx, reinterpret_cast<cudaStream_t>(stream));
+}
+
+extern "C" kb_status kb_attention_paged(kb_ctx* ctx, const void* d_q, uint64_t q_row, uint64_t q_head, uint32_t q_heads,
+                                        const kb_paged_cache* cache, uint32_t kv_heads, uint32_t dim, kb_dtype dtype,
+                                        const int32_t* d_table, uint64_t table_row, uint32_t max_pages,
+                                        const int32_t* d_lengths, uint32_t sequences, float scale, void* d_out,
+                                        uint64_t out_row, uint64_t out_head, float* d_lse, void* stream) {
+  TraceRange trace("kb_attention_paged");
+  if (!ctx) return KB_ERR_INVALID_ARG;
+  const char* where = "kb_attention_paged";
+  if (dtype != KB_F16 && dtype != KB_BF16) return fail(ctx, KB_ERR_UNSUPPORTED, "%s: dtype %d is not fp16 or bf16", where, (int)dtype);
+  KB_TRY(check_sizes(ctx, where, q_heads, kv_heads, dim, KB_ATTENTION_MAX_DIM));
+  if (dim % 8 != 0) return fail(ctx, KB_ERR_UNSUPPORTED, "%s: dim %u is not a multiple of 8", where, dim);
+  if (!(scale > 0.0f) || !std::isfinite(scale)) return fail(ctx, KB_ERR_INVALID_ARG, "%s: scale must be finite and > 0", where);
+  if (sequences > KB_OPS_MAX_DIM) return fail(ctx, KB_ERR_INVALID_ARG, "%s: more than 2^30 sequences", where);
+  if (!cache) return fail(ctx, KB_ERR_INVALID_ARG, "%s: cache is NULL", where);
+  if (sequences == 0) return KB_OK;
+  KB_TRY(check_heads(ctx, where, {"d_q", d_q, q_row, q_head}, 2));
+  KB_TRY(check_out(ctx, where, {"d_out", d_out, out_row, out_head}, sequences, q_heads, dim, 2));
+  KB_TRY(check_cache(ctx, where, *cache, 2));
+  if (!heads_aligned(d_q, q_row, q_head, 2) || !heads_aligned(cache->d_k, cache->k_row, cache->k_head, 2) || cache->k_page % 8 != 0 ||
+      !heads_aligned(cache->d_v, cache->v_row, cache->v_head, 2) || cache->v_page % 8 != 0)
+    return fail(ctx, KB_ERR_ALIGNMENT, "%s: queries and cache need 16-byte aligned pointers and strides", where);
+  if (!d_lengths || (!d_table && max_pages)) return fail(ctx, KB_ERR_INVALID_ARG, "%s: d_table or d_lengths is NULL", where);
+  if (!aligned_to(d_table, 4) || !aligned_to(d_lengths, 4) || !aligned_to(d_lse, 4))
+    return fail(ctx, KB_ERR_ALIGNMENT, "%s: d_table, d_lengths or d_lse is not aligned to its element type", where);
+  if (sequences > 1 && (table_row < max_pages || table_row > kMaxStride))
+    return fail(ctx, KB_ERR_INVALID_ARG, "%s: table_row %llu is less than max_pages %u, or beyond 2^40", where, (unsigned long long)table_row, max_pages);
+  if ((uint64_t)max_pages * cache->page_size > 0x7FFFFFFFull) return fail(ctx, KB_ERR_INVALID_ARG, "%s: max_pages * page_size is beyond 2^31 - 1", where);
+  DeviceGuard g(ctx->device);
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  KB_TRY(ensure_paged(ctx, st));
+  const PagedSpace space(ctx);
+  PagedParams p = {};
+  p.q = d_q;
+  p.q_row = q_row;
+  p.q_head = q_head;
+  p.k = cache->d_k;
+  p.v = cache->d_v;
+  p.k_page = cache->k_page;
+  p.k_row = cache->k_row;
+  p.k_head = cache->k_head;
+  p.v_page = cache->v_page;
+  p.v_row = cache->v_row;
+  p.v_head = cache->v_head;
+  p.pages = cache->pages;
+  p.page_size = cache->page_size;
+  p.max_pages = max_pages;
+  p.table = d_table;
+  p.table_row = table_row;
+  p.lengths = d_lengths;
+  p.sequences = sequences;
+  p.hkv = kv_heads;
+  p.group = q_heads / kv_heads;
+  p.chunks = p.group > 8 ? (p.group + 15) / 16 : 1;
+  p.dim = dim;
+  p.scale_log2 = (float)((double)scale * 1.4426950408889634);
+  p.out = d_out;
+  p.o_row = out_row;
+  p.o_head = out_head;
+  p.lse = d_lse;
+  p.q_heads = q_heads;
+  p.vec_out = aligned_to(d_out, 8) && out_row % 4 == 0 && out_head % 4 == 0;
+  p.part = reinterpret_cast<float*>(ctx->paged_ws + space.part);
+  p.part_rl = reinterpret_cast<float*>(ctx->paged_ws + space.rl);
+  p.arrived = reinterpret_cast<unsigned int*>(ctx->paged_ws + space.arrived);
+  p.status = ctx->d_status;
+  const uint64_t most = (uint64_t)paged_units(paged_length(0x7FFFFFFF, max_pages, cache->page_size)) * sequences * kv_heads * p.chunks;
+  return dtype == KB_F16 ? launch_paged<KB_F16>(ctx, p, most, st) : launch_paged<KB_BF16>(ctx, p, most, st);
+}

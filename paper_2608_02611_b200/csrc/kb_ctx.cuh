@@ -7,6 +7,7 @@
 #include <cstring>
 #include <vector>
 
+#include <cuda.h>
 #include <nvtx3/nvToolsExt.h>
 
 #include "kb_common.cuh"
@@ -89,6 +90,10 @@ struct kb_ctx {
   void* encode_tiled = nullptr;     // the driver's tensor-map encoder, looked up at first use
   int cluster_room[9] = {};         // clusters of n CTAs, one CTA per SM, that run at the same time
   bool ops_ready = false;           // shared-memory limits of the operators' kernels are raised
+  // paged attention (kb_attention.h)
+  unsigned char* paged_ws = nullptr;   // parts of divided sequences, and arrival counts that are zero between calls
+  size_t paged_ws_bytes = 0;
+  bool attention_ready = false;     // the attention kernels' limits are raised
   uint32_t product_rows = 0, product_splits = 0;   // of the last product's launch: rows of A per tile, CTAs per tile
 };
 
@@ -125,6 +130,8 @@ struct DeviceGuard {
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 inline size_t round_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 inline int elem_bytes(kb_dtype dt) { return dt == KB_F32 ? 4 : (dt == KB_F8E4M3 || dt == KB_F8E5M2) ? 1 : 2; }
+inline bool is_float_type(int dt) { return dt == KB_F32 || dt == KB_F16 || dt == KB_BF16; }
+inline bool aligned_to(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 inline bool known_dtype(int dt) { return dt >= KB_F32 && dt <= KB_F8E5M2; }
 
 // A named range around an entry point's host work, for a timeline tool that is attached
@@ -226,6 +233,33 @@ inline kb_status ensure_workspace(kb_ctx* ctx, T** buf, size_t* have, size_t nee
   else
     *buf = old;
   return rc;
+}
+
+#define KB_TRY(call)                     \
+  do {                                   \
+    const kb_status rc_ = (call);        \
+    if (rc_ != KB_OK) return rc_;        \
+  } while (0)
+
+// After a launch: counts it and reports what the runtime said.
+inline kb_status launched(kb_ctx* ctx) {
+  ++ctx->launches;
+  KB_CUDA(ctx, cudaGetLastError());
+  return KB_OK;
+}
+
+// The driver's encoder of tensor maps, looked up at first use.
+using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
+                                 const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
+                                 CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+inline kb_status find_encoder(kb_ctx* ctx, const char* where) {
+  if (ctx->encode_tiled) return KB_OK;
+  void* fn = nullptr;
+  cudaDriverEntryPointQueryResult found = cudaDriverEntryPointSymbolNotFound;
+  KB_CUDA(ctx, cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &found));
+  if (found != cudaDriverEntryPointSuccess || !fn) return fail(ctx, KB_ERR_CUDA, "%s: the driver has no cuTensorMapEncodeTiled", where);
+  ctx->encode_tiled = fn;
+  return KB_OK;
 }
 
 }  // namespace kb

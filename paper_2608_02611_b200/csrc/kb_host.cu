@@ -354,6 +354,7 @@ extern "C" kb_status kb_ctx_destroy(kb_ctx* ctx) {
   ctx_free(ctx, ctx->srt);
   ctx_free(ctx, ctx->small_ws);
   ctx_free(ctx, ctx->ops_ws);
+  ctx_free(ctx, ctx->paged_ws);
   for (void* p : ctx->outgrown) ctx_free(ctx, p);
   for (int i = 0; i < 2; ++i) {
     ctx_free(ctx, ctx->st_batch[i]);

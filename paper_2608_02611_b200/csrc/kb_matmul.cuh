@@ -61,16 +61,6 @@ __device__ __forceinline__ void store_down(const MatmulParams& p, uint32_t row0,
     store_down<KB_F32, N>(p, row0, col, v);
 }
 
-// After a wait has run out: let the copies already issued land, for a second at most.
-__device__ __forceinline__ void drain_copies(uint64_t* full, uint32_t stages, uint64_t issued) {
-  const uint64_t back = issued < stages ? issued : stages;
-  for (uint64_t m = issued - back; m < issued; ++m) {
-    const unsigned long long t0 = global_ns();
-    while (!mbar_try_wait(&full[m % stages], (uint32_t)((m / stages) & 1ull)))
-      if (global_ns() - t0 > 1000000000ull) break;
-  }
-}
-
 // ---- few rows of A ---------------------------------------------------------------------------
 // The rows of B (weights) take the 128 lanes of the tile and BN rows of A its columns, so that a
 // single token wastes no lanes and the weights stream through once.  A cluster of `splits` CTAs

@@ -14,9 +14,7 @@ using namespace kb;
 
 namespace {
 
-inline bool is_float_type(int dt) { return dt == KB_F32 || dt == KB_F16 || dt == KB_BF16; }
 inline bool is_f8_type(int dt) { return dt == KB_F8E4M3 || dt == KB_F8E5M2; }
-inline bool aligned_to(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 // rows of a matrix start on 16-byte boundaries
 inline bool rows_aligned(const void* p, uint64_t ld, int bytes) { return aligned16(p) && (ld * bytes) % 16 == 0; }
 
@@ -32,17 +30,6 @@ kb_status check_matrix(kb_ctx* ctx, const char* where, const char* name, const v
 }
 kb_status check_vector(kb_ctx* ctx, const char* where, const char* name, const void* p, int bytes) {
   if (!aligned_to(p, bytes)) return fail(ctx, KB_ERR_ALIGNMENT, "%s: %s is not aligned to its element type", where, name);
-  return KB_OK;
-}
-#define KB_TRY(call)                     \
-  do {                                   \
-    const kb_status rc_ = (call);        \
-    if (rc_ != KB_OK) return rc_;        \
-  } while (0)
-
-kb_status launched(kb_ctx* ctx) {
-  ++ctx->launches;
-  KB_CUDA(ctx, cudaGetLastError());
   return KB_OK;
 }
 
@@ -221,10 +208,6 @@ kb_status launch_norm_bwd(kb_ctx* ctx, NormBwdParams& p, uint32_t* nparts, cudaS
 
 // ---- product ---------------------------------------------------------------------------------------
 
-using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                 const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                                 CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
 template <int BN>
 void lanes_config(cudaLaunchConfig_t* cfg, cudaLaunchAttribute* attr, unsigned int grid, uint32_t splits, cudaStream_t st) {
   cfg->gridDim = dim3(grid);
@@ -248,11 +231,7 @@ kb_status lanes_attr(kb_ctx* ctx) {
 
 kb_status prepare_matmul(kb_ctx* ctx) {
   if (ctx->ops_ready) return KB_OK;
-  void* fn = nullptr;
-  cudaDriverEntryPointQueryResult found = cudaDriverEntryPointSymbolNotFound;
-  KB_CUDA(ctx, cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &found));
-  if (found != cudaDriverEntryPointSuccess || !fn)
-    return fail(ctx, KB_ERR_CUDA, "kb_matmul_blocks: the driver has no cuTensorMapEncodeTiled");
+  KB_TRY(find_encoder(ctx, "kb_matmul_blocks"));
   KB_TRY(lanes_attr<16>(ctx));
   KB_TRY(lanes_attr<32>(ctx));
   KB_TRY(lanes_attr<64>(ctx));
@@ -275,7 +254,6 @@ kb_status prepare_matmul(kb_ctx* ctx) {
     lanes_config<128>(&cfg, attr, n, n, nullptr);
     KB_CUDA(ctx, cudaOccupancyMaxActiveClusters(&ctx->cluster_room[n], matmul_lanes_kernel<128, false>, &cfg));
   }
-  ctx->encode_tiled = fn;
   ctx->ops_ready = true;
   return KB_OK;
 }

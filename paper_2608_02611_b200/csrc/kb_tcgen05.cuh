@@ -1,5 +1,5 @@
 // Wrappers around the tensor-core, tensor-memory, tensor-map copy and cluster instructions the
-// 8-bit product uses (PTX ISA, sm_100a).
+// 8-bit product and the attention over prompts use (PTX ISA, sm_100a).
 #pragma once
 
 #include <cuda.h>
@@ -72,6 +72,19 @@ __device__ __forceinline__ void tmem_wait_ld(float (&v)[32]) {
                  "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31]));
 }
 
+// 32 columns of this warp's 32 lanes from registers; tmem_wait_st before the values are handed over
+__device__ __forceinline__ void tmem_st32(uint32_t addr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+      "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(addr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+      "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]),
+      "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+      : "memory");
+}
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
 // ---- matrix instructions ---------------------------------------------------------------------
 // Descriptor of a K-major operand in shared memory, rows of 128 bytes in the 128-byte swizzle
 // (what a tensor-map copy with that swizzle writes): start address and the distance of 1024
@@ -127,6 +140,53 @@ __device__ __forceinline__ void mma_f8_block(uint32_t d_tmem, uint64_t a_desc, u
         "}" ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc)
         : "memory");
 }
+// 16-bit operands: descriptor of a 16-bit instruction (binary32 accumulator; `bf16` for both operands, else
+// binary16; A K-major; B K-major, or N-major with `b_n_major`).
+__host__ __device__ constexpr uint32_t mma_idesc_f16(bool bf16, bool b_n_major, uint32_t M, uint32_t N) {
+  return (1u << 4) | ((bf16 ? 1u : 0u) << 7) | ((bf16 ? 1u : 0u) << 10) | ((b_n_major ? 1u : 0u) << 16) | ((N >> 3) << 17) |
+         ((M >> 4) << 24);
+}
+// Descriptor of an N-major operand, rows (of K) of 64 elements = 128 bytes in the 128-byte swizzle: groups of 8 rows
+// 1024 bytes apart, the next 64 columns of N `next64` bytes further.
+__device__ __forceinline__ uint64_t smem_desc_n128(uint32_t smem_addr, uint32_t next64) {
+  return (uint64_t)((smem_addr & 0x3FFFFu) >> 4) | ((uint64_t)(next64 >> 4) << 16) | ((uint64_t)(1024u >> 4) << 32) | (1ull << 46) |
+         (2ull << 61);
+}
+// D (+)= A B^T, both K-major in shared memory, over 64 elements of K (four steps of 16; whole warp, as above).
+__device__ __forceinline__ void mma_f16_block(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, bool add) {
+  asm volatile(
+      "{\n.reg .pred one, more;\n.reg .b64 a, b;\n"
+      "elect.sync _|one, 0xFFFFFFFF;\n"
+      "setp.ne.u32 more, %4, 0;\n"
+      "@one tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, more;\n"
+      "setp.eq.b32 more, 0, 0;\n"
+      "add.s64 a, %1, 2;\nadd.s64 b, %2, 2;\n"
+      "@one tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, more;\n"
+      "add.s64 a, %1, 4;\nadd.s64 b, %2, 4;\n"
+      "@one tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, more;\n"
+      "add.s64 a, %1, 6;\nadd.s64 b, %2, 6;\n"
+      "@one tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, more;\n"
+      "}" ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(add ? 1u : 0u)
+      : "memory");
+}
+// D (+)= A B over 64 elements of K: A from tensor memory (two to a column), B N-major in shared memory (16 rows of K
+// are 2048 bytes).
+__device__ __forceinline__ void mma_f16_block_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, bool add) {
+  asm volatile(
+      "{\n.reg .pred one, more;\n.reg .b64 b;\n.reg .b32 a;\n"
+      "elect.sync _|one, 0xFFFFFFFF;\n"
+      "setp.ne.u32 more, %4, 0;\n"
+      "@one tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, more;\n"
+      "setp.eq.b32 more, 0, 0;\n"
+      "add.s32 a, %1, 8;\nadd.s64 b, %2, 128;\n"
+      "@one tcgen05.mma.cta_group::1.kind::f16 [%0], [a], b, %3, more;\n"
+      "add.s32 a, %1, 16;\nadd.s64 b, %2, 256;\n"
+      "@one tcgen05.mma.cta_group::1.kind::f16 [%0], [a], b, %3, more;\n"
+      "add.s32 a, %1, 24;\nadd.s64 b, %2, 384;\n"
+      "@one tcgen05.mma.cta_group::1.kind::f16 [%0], [a], b, %3, more;\n"
+      "}" ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(add ? 1u : 0u)
+      : "memory");
+}
 // The barrier gets one arrival when all matrix instructions of this warp's issuing thread are done
 // (whole warp; the same thread is elected every time).
 __device__ __forceinline__ void mma_commit(uint64_t* bar) {
@@ -156,6 +216,15 @@ __device__ __forceinline__ void tma_load_2d(uint32_t dst_smem, const CUtensorMap
       "l"(map), "r"(x), "r"(y), "r"(bar)
       : "memory");
 }
+// A box of a tensor of three axes; x counts elements and x * element size is a multiple of 16.
+__device__ __forceinline__ void tma_load_3d(uint32_t dst_smem, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
+  asm volatile(
+      "{\n.reg .pred one;\nelect.sync _|one, 0xFFFFFFFF;\n"
+      "@one cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes "
+      "[%0], [%1, {%2, %3, %4}], [%5];\n}" ::"r"(dst_smem),
+      "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
+      : "memory");
+}
 // The same by a CTA of a pair; the bytes count on a barrier of either CTA (a cluster address).
 __device__ __forceinline__ void tma_load_2d_pair(uint32_t dst_smem, const CUtensorMap* map, int x, int y,
                                                  uint32_t cluster_bar) {
@@ -173,6 +242,16 @@ __device__ __forceinline__ void expect_tx_elect(uint32_t bar, uint32_t bytes) {
       "@one mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n}" ::"r"(bar),
       "r"(bytes)
       : "memory");
+}
+
+// After a wait has run out: let the copies already issued land, for a second at most.
+__device__ __forceinline__ void drain_copies(uint64_t* full, uint32_t stages, uint64_t issued) {
+  const uint64_t back = issued < stages ? issued : stages;
+  for (uint64_t m = issued - back; m < issued; ++m) {
+    const unsigned long long t0 = global_ns();
+    while (!mbar_try_wait(&full[m % stages], (uint32_t)((m / stages) & 1ull)))
+      if (global_ns() - t0 > 1000000000ull) break;
+  }
 }
 
 // ---- registers ---------------------------------------------------------------------------------

@@ -1,14 +1,17 @@
 // The model operators' Python calls, natively: checks tensors, makes the outputs and calls the C
-// entry points (include/kb_ops.h).  Marshalling only, like binding.py, whose Context methods are
+// entry points (include/kb_ops.h, include/kb_attention.h).  Marshalling only, like binding.py, whose Context methods are
 // thin wrappers around these functions.  Through ctypes such a call spends 13 to 18 us in Python and
 // the kernels of a single token take 3 to 15 us; from here it spends about half of that.
 #include <Python.h>
+
+#include <cmath>
+#include <cstring>
 
 #include <ATen/ATen.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
-#include "../../include/kb_ops.h"
+#include "../../include/kb_attention.h"
 
 namespace {
 
@@ -20,6 +23,9 @@ struct {
   decltype(&::kb_layernorm_backward) layernorm_backward;
   decltype(&::kb_matmul_blocks) matmul_blocks;
   decltype(&::kb_last_error) last_error;
+  decltype(&::kb_qk_norm_rope) qk_norm_rope;
+  decltype(&::kb_attention) attention;
+  decltype(&::kb_attention_paged) attention_paged;
 } g_lib;
 
 struct Refused {};             // a Python exception is set
@@ -319,17 +325,242 @@ PyObject* matmul_blocks(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
-// (error class, addresses of the five entry points in the order above)
+// ---- attention (include/kb_attention.h) ----------------------------------------------------------
+
+// A tensor as heads [tokens][heads][dim] with adjacent elements, any other strides.  The stride of an axis of
+// one element is free (torch may report anything) and becomes one that suits the kernels.
+struct Heads {
+  int64_t tokens, heads, dim;
+  uint64_t row, head;
+  void* p;
+};
+uint64_t stride_of(const Call& c, const at::Tensor& t, int64_t axis, int64_t dim, const char* name) {
+  if (t.size(axis) <= 1) return (uint64_t)((dim + 7) / 8 * 8);
+  if (t.stride(axis) < 0) refuse(c.where, std::string(name) + " has a negative stride");
+  return (uint64_t)t.stride(axis);
+}
+Heads heads_of(const Call& c, const at::Tensor& t, const char* name) {
+  if (t.dim() != 3) refuse(c.where, std::string(name) + " must be [tokens, heads, dim]");
+  const int64_t dim = t.size(2);
+  if (dim > 1 && t.numel() && t.stride(2) != 1) refuse(c.where, std::string("the elements of the heads of ") + name + " must be adjacent");
+  Heads h{t.size(0), t.size(1), dim, 0, 0, t.data_ptr()};
+  h.head = stride_of(c, t, 1, dim, name);
+  h.row = t.size(0) <= 1 ? (uint64_t)std::max<int64_t>(1, t.size(1)) * std::max<uint64_t>(h.head, (uint64_t)((dim + 7) / 8 * 8)) : stride_of(c, t, 0, dim, name);
+  if (t.size(1) <= 1 && t.size(0) > 1) h.head = (uint64_t)((dim + 7) / 8 * 8);
+  return h;
+}
+void same_type(const Call& c, const at::Tensor& t, at::ScalarType type, const char* name) {
+  if (t.scalar_type() != type) refuse(c.where, std::string(name) + " must be of type " + c10::toString(type));
+}
+kb_paged_cache cache_of(const Call& c, const at::Tensor& k, const at::Tensor& v, int64_t heads, int64_t dim, at::ScalarType type) {
+  const char* names[2] = {"k_cache", "v_cache"};
+  const at::Tensor* both[2] = {&k, &v};
+  for (int i = 0; i < 2; ++i) {
+    const at::Tensor& t = *both[i];
+    if (t.dim() != 4 || t.size(2) != heads || t.size(3) != dim || (dim > 1 && t.numel() && t.stride(3) != 1))
+      refuse(c.where, std::string(names[i]) + " must be [pages, page size, " + std::to_string(heads) + ", " + std::to_string(dim) +
+                          "] with adjacent elements");
+    same_type(c, t, type, names[i]);
+  }
+  if (k.size(0) != v.size(0) || k.size(1) != v.size(1)) refuse(c.where, "k_cache and v_cache differ in pages or their size");
+  if (k.size(1) < 1 || k.size(1) > 0x7FFFFFFF) refuse(c.where, "pages of no slot, or of more than 2^31 - 1");
+  kb_paged_cache r;
+  r.d_k = k.data_ptr();
+  r.d_v = v.data_ptr();
+  r.k_page = stride_of(c, k, 0, dim, "k_cache");
+  r.k_row = stride_of(c, k, 1, dim, "k_cache");
+  r.k_head = stride_of(c, k, 2, dim, "k_cache");
+  r.v_page = stride_of(c, v, 0, dim, "v_cache");
+  r.v_row = stride_of(c, v, 1, dim, "v_cache");
+  r.v_head = stride_of(c, v, 2, dim, "v_cache");
+  r.pages = (uint64_t)k.size(0);
+  r.page_size = (uint32_t)k.size(1);
+  return r;
+}
+const at::Tensor& given(const Call& c, PyObject* o, const at::Tensor& like, int64_t heads, const char* name) {
+  const at::Tensor& t = tensor(c, o, name);
+  if (t.dim() != 3 || t.size(0) != like.size(0) || t.size(1) != heads || t.size(2) != like.size(2))
+    refuse(c.where, std::string(name) + " must be [" + std::to_string(like.size(0)) + ", " + std::to_string(heads) + ", " +
+                        std::to_string(like.size(2)) + "]");
+  same_type(c, t, like.scalar_type(), name);
+  return t;
+}
+uint32_t count32(const Call& c, int64_t n, const char* what) {
+  if (n > 0x7FFFFFFF) refuse(c.where, std::string(what) + " beyond 2^31 - 1");
+  return (uint32_t)n;
+}
+// the addresses of empty tensors are null, which would mean "not given": with nothing to do any address will do
+alignas(16) float g_nothing[4];
+template <class T>
+T* some(T* p) {
+  return p ? p : reinterpret_cast<T*>(g_nothing);
+}
+
+// (handle, device, q, k, positions, inv_freq, q_weight, k_weight, eps, norm, interleaved, want_q, want_k, v, k_cache, v_cache,
+//  slots, q_out, k_out) -> (q_out, k_out)
+PyObject* qk_norm_rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 19, [&]() -> PyObject* {
+    const Call c = open_call("kb_qk_norm_rope", a[0], a[1]);
+    const at::Tensor &q = tensor(c, a[2], "q"), &k = tensor(c, a[3], "k");
+    const Heads hq = heads_of(c, q, "q"), hk = heads_of(c, k, "k");
+    const at::ScalarType type = q.scalar_type();
+    if (hk.tokens != hq.tokens || hk.dim != hq.dim) refuse(c.where, "k must have the tokens and the dim of q");
+    same_type(c, k, type, "k");
+    const double eps = PyFloat_AsDouble(a[8]);
+    if (eps == -1.0 && PyErr_Occurred()) throw Refused{};
+    const bool norm = truth(a[9]), interleaved = truth(a[10]), want_q = truth(a[11]), want_k = truth(a[12]);
+    uint32_t rotary = 0;
+    const int64_t* positions = nullptr;
+    const double* inv_freq = nullptr;
+    if (a[5] != Py_None) {
+      const at::Tensor &f = tensor(c, a[5], "inv_freq"), &t = tensor(c, a[4], "positions");
+      inv_freq = static_cast<const double*>(vector_of(c, f, f.numel(), "inv_freq", at::kDouble, at::kDouble));
+      positions = static_cast<const int64_t*>(vector_of(c, t, hq.tokens, "positions", at::kLong, at::kLong));
+      if (f.numel() > KB_ROPE_MAX_DIM) refuse(c.where, "inv_freq has more elements than a head has pairs");
+      rotary = (uint32_t)(2 * f.numel());
+    }
+    at::ScalarType params = type;
+    void *wq = nullptr, *wk = nullptr;
+    if (a[6] != Py_None) {
+      const at::Tensor& t = tensor(c, a[6], "q_weight");
+      wq = vector_of(c, t, hq.dim, "q_weight", type, at::kFloat);
+      params = t.scalar_type();
+    }
+    if (a[7] != Py_None) {
+      const at::Tensor& t = tensor(c, a[7], "k_weight");
+      wk = vector_of(c, t, hq.dim, "k_weight", type, at::kFloat);
+      if (wq && t.scalar_type() != params) refuse(c.where, "q_weight and k_weight must have the same type");
+      params = t.scalar_type();
+    }
+    const bool cached = a[14] != Py_None || a[15] != Py_None;
+    kb_paged_cache cache = {};
+    Heads hv = {};
+    const int64_t* slots = nullptr;
+    if (cached) {
+      const at::Tensor& v = tensor(c, a[13], "v");
+      hv = heads_of(c, v, "v");
+      if (hv.tokens != hk.tokens || hv.heads != hk.heads || hv.dim != hk.dim) refuse(c.where, "v must have the shape of k");
+      same_type(c, v, type, "v");
+      cache = cache_of(c, tensor(c, a[14], "k_cache"), tensor(c, a[15], "v_cache"), hk.heads, hk.dim, type);
+      slots = static_cast<const int64_t*>(vector_of(c, tensor(c, a[16], "slots"), hq.tokens, "slots", at::kLong, at::kLong));
+    } else if (a[13] != Py_None || a[16] != Py_None) {
+      refuse(c.where, "v and slots belong to a cache");
+    }
+    at::Tensor qo, ko;
+    if (a[17] != Py_None)
+      qo = given(c, a[17], q, hq.heads, "q_out");
+    else if (want_q)
+      qo = c.empty({hq.tokens, hq.heads, hq.dim}, type);
+    if (a[18] != Py_None)
+      ko = given(c, a[18], k, hk.heads, "k_out");
+    else if (want_k)
+      ko = c.empty({hk.tokens, hk.heads, hk.dim}, type);
+    Heads oq = {}, ok = {};
+    if (qo.defined()) oq = heads_of(c, qo, "q_out");
+    if (ko.defined()) ok = heads_of(c, ko, "k_out");
+    c.run([&] {
+      return g_lib.qk_norm_rope(c.ctx, hq.p, hq.row, hq.head, (uint32_t)hq.heads, hk.p, hk.row, hk.head, (uint32_t)hk.heads,
+                                hq.tokens, (uint32_t)hq.dim, (kb_dtype)code_of(type), norm, wq, wk, (kb_dtype)code_of(params),
+                                (float)eps, positions, inv_freq, rotary, interleaved, oq.p, oq.row, oq.head, ok.p, ok.row,
+                                ok.head, hv.p, hv.row, hv.head, cached ? &cache : nullptr, slots, c.stream);
+    });
+    return wrap_tuple({qo, ko});
+  });
+}
+
+double scale_of(PyObject* o, int64_t dim) {
+  if (o == Py_None) return 1.0 / std::sqrt((double)std::max<int64_t>(1, dim));
+  const double v = PyFloat_AsDouble(o);
+  if (v == -1.0 && PyErr_Occurred()) throw Refused{};
+  return v;
+}
+
+// (handle, device, q, k, v, q_offsets or None, k_offsets or None, causal, scale or None, want_lse, out or None) -> (out, lse)
+PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 11, [&]() -> PyObject* {
+    const Call c = open_call("kb_attention", a[0], a[1]);
+    const at::Tensor &q = tensor(c, a[2], "q"), &k = tensor(c, a[3], "k"), &v = tensor(c, a[4], "v");
+    const Heads hq = heads_of(c, q, "q"), hk = heads_of(c, k, "k"), hv = heads_of(c, v, "v");
+    const at::ScalarType type = q.scalar_type();
+    same_type(c, k, type, "k");
+    same_type(c, v, type, "v");
+    if (hk.dim != hq.dim) refuse(c.where, "k must have the dim of q");
+    if (hv.tokens != hk.tokens || hv.heads != hk.heads || hv.dim != hk.dim) refuse(c.where, "v must have the shape of k");
+    int64_t sequences = 1;
+    const int32_t *qo = nullptr, *ko = nullptr;
+    if (a[5] != Py_None) {
+      const at::Tensor& t = tensor(c, a[5], "q_offsets");
+      sequences = t.numel() - 1;
+      if (sequences < 0) refuse(c.where, "q_offsets must have an element more than there are sequences");
+      qo = ko = static_cast<const int32_t*>(vector_of(c, t, t.numel(), "q_offsets", at::kInt, at::kInt));
+      if (a[6] != Py_None) ko = static_cast<const int32_t*>(vector_of(c, tensor(c, a[6], "k_offsets"), sequences + 1, "k_offsets", at::kInt, at::kInt));
+      else if (hk.tokens != hq.tokens) refuse(c.where, "without k_offsets k must have the tokens of q");
+    } else if (a[6] != Py_None) {
+      refuse(c.where, "k_offsets without q_offsets");
+    }
+    const bool causal = truth(a[7]), want_lse = truth(a[9]);
+    const double scale = scale_of(a[8], hq.dim);
+    const at::Tensor out = a[10] == Py_None ? c.empty({hq.tokens, hq.heads, hq.dim}, type) : given(c, a[10], q, hq.heads, "out");
+    const Heads ho = heads_of(c, out, "out");
+    at::Tensor lse;
+    if (want_lse) lse = c.empty({hq.tokens, hq.heads}, at::kFloat);
+    float* lp = want_lse ? lse.data_ptr<float>() : nullptr;
+    const uint32_t count = count32(c, sequences, "sequences");
+    c.run([&] {
+      return g_lib.attention(c.ctx, hq.p, hq.row, hq.head, (uint32_t)hq.heads, hq.tokens, hk.p, hk.row, hk.head, hv.p, hv.row,
+                             hv.head, (uint32_t)hk.heads, hk.tokens, (uint32_t)hq.dim, (kb_dtype)code_of(type), qo, ko, count,
+                             causal, (float)scale, ho.p, ho.row, ho.head, lp, c.stream);
+    });
+    return wrap_tuple({out, lse});
+  });
+}
+
+// (handle, device, q, k_cache, v_cache, table, lengths, scale or None, want_lse, out or None) -> (out, lse)
+PyObject* attention_paged(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 10, [&]() -> PyObject* {
+    const Call c = open_call("kb_attention_paged", a[0], a[1]);
+    const at::Tensor &q = tensor(c, a[2], "q"), &k = tensor(c, a[3], "k_cache"), &v = tensor(c, a[4], "v_cache");
+    const at::Tensor &table = tensor(c, a[5], "table"), &lengths = tensor(c, a[6], "lengths");
+    const Heads hq = heads_of(c, q, "q");
+    const at::ScalarType type = q.scalar_type();
+    if (k.dim() != 4) refuse(c.where, "k_cache must be [pages, page size, heads, dim]");
+    const int64_t hkv = k.size(2);
+    const kb_paged_cache cache = cache_of(c, k, v, hkv, hq.dim, type);
+    if (table.dim() != 2 || table.size(0) != hq.tokens || table.scalar_type() != at::kInt || (table.size(1) > 1 && table.numel() && table.stride(1) != 1))
+      refuse(c.where, "table must be an int32 matrix [" + std::to_string(hq.tokens) + ", pages] with adjacent columns");
+    const uint64_t table_row = hq.tokens > 1 ? (uint64_t)std::max<int64_t>(0, table.stride(0)) : (uint64_t)table.size(1);
+    const int32_t* lens = static_cast<const int32_t*>(vector_of(c, lengths, hq.tokens, "lengths", at::kInt, at::kInt));
+    const double scale = scale_of(a[7], hq.dim);
+    const bool want_lse = truth(a[8]);
+    const at::Tensor out = a[9] == Py_None ? c.empty({hq.tokens, hq.heads, hq.dim}, type) : given(c, a[9], q, hq.heads, "out");
+    const Heads ho = heads_of(c, out, "out");
+    at::Tensor lse;
+    if (want_lse) lse = c.empty({hq.tokens, hq.heads}, at::kFloat);
+    float* lp = want_lse ? lse.data_ptr<float>() : nullptr;
+    const uint32_t most = count32(c, table.size(1), "pages of a sequence"), sequences = count32(c, hq.tokens, "sequences");
+    const int32_t* tp = table.data_ptr<int32_t>();
+    kb_paged_cache held = cache;
+    if (held.pages == 0) held.d_k = some(held.d_k), held.d_v = some(held.d_v);
+    c.run([&] {
+      return g_lib.attention_paged(c.ctx, hq.p, hq.row, hq.head, (uint32_t)hq.heads, &held, (uint32_t)hkv, (uint32_t)hq.dim,
+                                   (kb_dtype)code_of(type), tp, table_row, most, lens, sequences, (float)scale, ho.p, ho.row,
+                                   ho.head, lp, c.stream);
+    });
+    return wrap_tuple({out, lse});
+  });
+}
+
+// (error class, addresses of the entry points in the order of g_lib)
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  return guarded(n, 6, [&]() -> PyObject* {
-    void* p[5];
-    for (int i = 0; i < 5; ++i) {
+  constexpr int kEntries = sizeof g_lib / sizeof(void*);
+  return guarded(n, 1 + kEntries, [&]() -> PyObject* {
+    void* p[kEntries];
+    for (int i = 0; i < kEntries; ++i) {
       p[i] = PyLong_AsVoidPtr(a[1 + i]);
       if (!p[i]) throw Refused{};
     }
-    g_lib = {reinterpret_cast<decltype(g_lib.quantize_blocks)>(p[0]), reinterpret_cast<decltype(g_lib.layernorm)>(p[1]),
-             reinterpret_cast<decltype(g_lib.layernorm_backward)>(p[2]),
-             reinterpret_cast<decltype(g_lib.matmul_blocks)>(p[3]), reinterpret_cast<decltype(g_lib.last_error)>(p[4])};
+    static_assert(sizeof p == sizeof g_lib, "one address per entry point");
+    std::memcpy(&g_lib, p, sizeof p);
     Py_INCREF(a[0]);
     Py_XSETREF(g_error, a[0]);
     Py_RETURN_NONE;
@@ -341,6 +572,9 @@ PyMethodDef methods[] = {KB_FAST(quantize_blocks),
                          KB_FAST(layernorm),
                          KB_FAST(layernorm_backward),
                          KB_FAST(matmul_blocks),
+                         KB_FAST(qk_norm_rope),
+                         KB_FAST(attention),
+                         KB_FAST(attention_paged),
                          KB_FAST(bind),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_kb_torch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
