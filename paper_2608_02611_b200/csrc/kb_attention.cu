@@ -2,6 +2,7 @@
 // Declarations and their contracts are in include/kb_attention.h.
 #include <algorithm>
 #include <cmath>
+#include <tuple>
 
 #include "../../include/kb_attention.h"
 #include "kb_ctx.cuh"
@@ -66,9 +67,9 @@ kb_status launch_rope(kb_ctx* ctx, const RopeParams& p, bool vec, cudaStream_t s
   const uint32_t per = p.tokens >= 16ull * ctx->sm_count ? kRopeTokens : 1;
   const unsigned int grid = (unsigned int)((p.tokens + per - 1) / per);
   if (vec)
-    qk_norm_rope_kernel<DT, L, true><<<grid, kRopeThreads, 0, st>>>(p, per);
+    qk_norm_rope_kernel<DT, L><<<grid, kRopeThreads, 0, st>>>(p, per);
   else
-    qk_norm_rope_kernel<DT, L, false><<<grid, kRopeThreads, 0, st>>>(p, per);
+    qk_norm_rope_plain_kernel<DT, L><<<grid, kRopeThreads, 0, st>>>(p, per);
   return launched(ctx);
 }
 template <int DT>
@@ -80,14 +81,12 @@ kb_status launch_rope(kb_ctx* ctx, const RopeParams& p, bool vec, cudaStream_t s
 
 // ---- paged attention ---------------------------------------------------------------------------
 
-// CTAs per SM of the kernel, by its registers and shared memory (launch bounds), and the most of any variant
-constexpr uint32_t paged_per_sm(int nt) { return nt == 1 ? 2 : 1; }
 constexpr uint32_t kPagedMostHeads = 16, kPagedMostDim = 128;
 
 struct PagedSpace {
   size_t part, rl, arrived, bytes;
-  explicit PagedSpace(const kb_ctx* ctx) {   // for the largest grid with the fewest heads, and the reverse: the same
-    const size_t slots = 2ull * ctx->sm_count * 2;
+  explicit PagedSpace(const kb_ctx* ctx) {
+    const size_t slots = 2ull * ctx->sm_count * kPagedWaves;   // two per CTA
     part = 0;
     rl = slots * kPagedMostHeads * kPagedMostDim * sizeof(float);
     arrived = rl + slots * kPagedMostHeads * 2 * sizeof(float);
@@ -109,27 +108,62 @@ kb_status ensure_paged(kb_ctx* ctx, cudaStream_t st) {
   return KB_OK;
 }
 
-template <int DT, int DP, int NT, bool PAGE16>
-kb_status launch_paged(kb_ctx* ctx, PagedParams& p, uint64_t most_units, cudaStream_t st) {
-  constexpr auto kernel = attention_paged_kernel<DT, DP, NT, PAGE16>;
-  constexpr size_t smem = sizeof(float) * kPagedWarps * 8 * NT * DP;
-  static_assert(smem <= 64 * 1024, "shared memory");
-  if (smem > 40 * 1024)   // raised to one fixed size, whatever thread or context calls
-    KB_CUDA(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-  const uint64_t grid = std::min<uint64_t>(most_units, (uint64_t)ctx->sm_count * paged_per_sm(NT));
-  if (grid * 8 * NT * sizeof(float) > smem) return fail(ctx, KB_ERR_UNSUPPORTED, "kb_attention_paged: a card of more SMs than foreseen");
-  kernel<<<(unsigned int)grid, kPagedThreads, smem, st>>>(p);
+// Pieces of the row of units, each of which takes a CTA per group of heads, one CTA per SM: as many as run at
+// the same time; or, where that would leave more than a tenth of the card idle (32 groups: 4 x 32 of 148 SMs), the
+// number that fills up to kPagedWaves waves best.
+uint32_t paged_pieces(uint64_t sms, uint64_t per_seq, uint64_t most_units) {
+  auto use = [&](uint64_t n) { return (double)(n * per_seq) / (double)((n * per_seq + sms - 1) / sms * sms); };
+  uint64_t best = std::max<uint64_t>(1, sms / per_seq);
+  if (use(best) < 0.9)
+    for (uint64_t n = best + 1; n * per_seq <= kPagedWaves * sms; ++n)
+      if (use(n) > use(best)) best = n;
+  return (uint32_t)std::min(best, most_units);   // no more than there are SMs
+}
+
+template <int DT, int DP, int NT>
+kb_status prepare_paged(kb_ctx* ctx) {   // one fixed size, whatever thread or context calls
+  KB_CUDA(ctx, cudaFuncSetAttribute(attention_paged_kernel<DT, DP, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                    (int)PagedTile<DP, NT>::smem(ctx->sm_count)));
+  return KB_OK;
+}
+kb_status prepare_paged(kb_ctx* ctx) {
+  if (ctx->paged_ready) return KB_OK;
+  KB_TRY(find_encoder(ctx, "kb_attention_paged"));
+  KB_TRY((prepare_paged<KB_F16, 64, 1>(ctx)));
+  KB_TRY((prepare_paged<KB_F16, 64, 2>(ctx)));
+  KB_TRY((prepare_paged<KB_F16, 128, 1>(ctx)));
+  KB_TRY((prepare_paged<KB_F16, 128, 2>(ctx)));
+  KB_TRY((prepare_paged<KB_BF16, 64, 1>(ctx)));
+  KB_TRY((prepare_paged<KB_BF16, 64, 2>(ctx)));
+  KB_TRY((prepare_paged<KB_BF16, 128, 1>(ctx)));
+  KB_TRY((prepare_paged<KB_BF16, 128, 2>(ctx)));
+  ctx->paged_ready = true;
+  return KB_OK;
+}
+// Tensor map of a cache [pages][page size][heads][dim], boxes of 64 elements of a head and `box` keys of a page
+kb_status encode_cache(kb_ctx* ctx, CUtensorMap* map, const void* d, uint64_t page, uint64_t row, uint64_t head, const kb_paged_cache& c,
+                       uint32_t heads, uint32_t dim, kb_dtype dtype, uint32_t box_rows) {
+  const uint64_t any = round_up(dim, 8);   // the stride of an axis of one element is free
+  const cuuint64_t dims[4] = {dim, heads, c.page_size, std::max<uint64_t>(c.pages, 1)};
+  const cuuint64_t strides[3] = {(heads > 1 ? head : any) * 2, (c.page_size > 1 ? row : any) * 2, (c.pages > 1 ? page : any) * 2};
+  const cuuint32_t box[4] = {64, 1, box_rows, 1}, step[4] = {1, 1, 1, 1};
+  const CUresult rc = reinterpret_cast<EncodeTiled>(ctx->encode_tiled)(
+      map, dtype == KB_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(d), dims, strides,
+      box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+      CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (rc != CUDA_SUCCESS) return fail(ctx, KB_ERR_CUDA, "cuTensorMapEncodeTiled failed with %d for a cache", (int)rc);
+  return KB_OK;
+}
+
+template <int DT, int DP, int NT>
+kb_status launch_paged(kb_ctx* ctx, const CUtensorMap& k, const CUtensorMap& v, const PagedParams& p, uint32_t pieces, cudaStream_t st) {
+  attention_paged_kernel<DT, DP, NT><<<dim3(p.hkv * p.chunks, pieces), kPagedThreads, PagedTile<DP, NT>::smem(pieces), st>>>(k, v, p);
   return launched(ctx);
 }
 template <int DT>
-kb_status launch_paged(kb_ctx* ctx, PagedParams& p, uint64_t most_units, cudaStream_t st) {
-  const bool wide = p.dim > 64, two = p.group > 8, page16 = p.page_size % 16 == 0;
-  if (wide) {
-    if (two) return page16 ? launch_paged<DT, 128, 2, true>(ctx, p, most_units, st) : launch_paged<DT, 128, 2, false>(ctx, p, most_units, st);
-    return page16 ? launch_paged<DT, 128, 1, true>(ctx, p, most_units, st) : launch_paged<DT, 128, 1, false>(ctx, p, most_units, st);
-  }
-  if (two) return page16 ? launch_paged<DT, 64, 2, true>(ctx, p, most_units, st) : launch_paged<DT, 64, 2, false>(ctx, p, most_units, st);
-  return page16 ? launch_paged<DT, 64, 1, true>(ctx, p, most_units, st) : launch_paged<DT, 64, 1, false>(ctx, p, most_units, st);
+kb_status launch_paged(kb_ctx* ctx, const CUtensorMap& k, const CUtensorMap& v, const PagedParams& p, uint32_t pieces, cudaStream_t st) {
+  if (p.dim > 64) return p.group > 8 ? launch_paged<DT, 128, 2>(ctx, k, v, p, pieces, st) : launch_paged<DT, 128, 1>(ctx, k, v, p, pieces, st);
+  return p.group > 8 ? launch_paged<DT, 64, 2>(ctx, k, v, p, pieces, st) : launch_paged<DT, 64, 1>(ctx, k, v, p, pieces, st);
 }
 
 // ---- attention over prompts ----------------------------------------------------------------------
@@ -272,12 +306,10 @@ extern "C" kb_status kb_qk_norm_rope(kb_ctx* ctx, const void* d_q, uint64_t q_ro
   p.tokens = tokens;
   p.hq = q_heads;
   p.hkv = kv_heads;
-  p.first_row = d_q_out ? 0 : q_heads;
-  p.rows = q_heads + (d_k_out || cache ? kv_heads : 0) + (cache ? kv_heads : 0);
   p.dim = dim;
   p.half = rotary_dim / 2;
   p.status = ctx->d_status;
-  const bool vec = dim % 8 == 0 && (interleaved || p.half % 8 == 0) && (!d_q_out || (heads_aligned(d_q, q_row, q_head, e) && heads_aligned(d_q_out, q_out_row, q_out_head, e))) &&
+  const bool vec = dim % 8 == 0 && (interleaved || p.half % 4 == 0) && (!d_q_out || (heads_aligned(d_q, q_row, q_head, e) && heads_aligned(d_q_out, q_out_row, q_out_head, e))) &&
                    (!(d_k_out || cache) || heads_aligned(d_k, k_row, k_head, e)) && (!d_k_out || heads_aligned(d_k_out, k_out_row, k_out_head, e)) &&
                    (!cache || (heads_aligned(d_v, v_row, v_head, e) && heads_aligned(cache->d_k, cache->k_row, cache->k_head, e) &&
                                heads_aligned(cache->d_v, cache->v_row, cache->v_head, e) && (cache->k_page * e) % 16 == 0 && (cache->v_page * e) % 16 == 0));
@@ -370,6 +402,7 @@ extern "C" kb_status kb_attention_paged_reserve(kb_ctx* ctx, void* stream) {
   TraceRange trace("kb_attention_paged_reserve");
   if (!ctx) return KB_ERR_INVALID_ARG;
   DeviceGuard g(ctx->device);
+  KB_TRY(prepare_paged(ctx));
   return ensure_paged(ctx, reinterpret_cast<cudaStream_t>(stream));
 }
 
@@ -394,6 +427,10 @@ extern "C" kb_status kb_attention_paged(kb_ctx* ctx, const void* d_q, uint64_t q
   if (!heads_aligned(d_q, q_row, q_head, 2) || !heads_aligned(cache->d_k, cache->k_row, cache->k_head, 2) || cache->k_page % 8 != 0 ||
       !heads_aligned(cache->d_v, cache->v_row, cache->v_head, 2) || cache->v_page % 8 != 0)
     return fail(ctx, KB_ERR_ALIGNMENT, "%s: queries and cache need 16-byte aligned pointers and strides", where);
+  for (const auto& [n, a, b] : {std::tuple<uint64_t, uint64_t, uint64_t>{kv_heads, cache->k_head, cache->v_head}, {cache->page_size, cache->k_row, cache->v_row},
+                                {cache->pages, cache->k_page, cache->v_page}})
+    if (n > 1 && (a == 0 || b == 0 || a >= kMaxStride / 2 || b >= kMaxStride / 2))
+      return fail(ctx, KB_ERR_INVALID_ARG, "%s: a stride of the cache is 0 or beyond 2^39 elements", where);
   if (!d_lengths || (!d_table && max_pages)) return fail(ctx, KB_ERR_INVALID_ARG, "%s: d_table or d_lengths is NULL", where);
   if (!aligned_to(d_table, 4) || !aligned_to(d_lengths, 4) || !aligned_to(d_lse, 4))
     return fail(ctx, KB_ERR_ALIGNMENT, "%s: d_table, d_lengths or d_lse is not aligned to its element type", where);
@@ -402,22 +439,17 @@ extern "C" kb_status kb_attention_paged(kb_ctx* ctx, const void* d_q, uint64_t q
   if ((uint64_t)max_pages * cache->page_size > 0x7FFFFFFFull) return fail(ctx, KB_ERR_INVALID_ARG, "%s: max_pages * page_size is beyond 2^31 - 1", where);
   DeviceGuard g(ctx->device);
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  KB_TRY(prepare_paged(ctx));
   KB_TRY(ensure_paged(ctx, st));
   const PagedSpace space(ctx);
   PagedParams p = {};
   p.q = d_q;
   p.q_row = q_row;
   p.q_head = q_head;
-  p.k = cache->d_k;
-  p.v = cache->d_v;
-  p.k_page = cache->k_page;
-  p.k_row = cache->k_row;
-  p.k_head = cache->k_head;
-  p.v_page = cache->v_page;
-  p.v_row = cache->v_row;
-  p.v_head = cache->v_head;
   p.pages = cache->pages;
   p.page_size = cache->page_size;
+  p.box = 16;
+  while (p.page_size % p.box) p.box /= 2;
   p.max_pages = max_pages;
   p.table = d_table;
   p.table_row = table_row;
@@ -438,6 +470,11 @@ extern "C" kb_status kb_attention_paged(kb_ctx* ctx, const void* d_q, uint64_t q
   p.part_rl = reinterpret_cast<float*>(ctx->paged_ws + space.rl);
   p.arrived = reinterpret_cast<unsigned int*>(ctx->paged_ws + space.arrived);
   p.status = ctx->d_status;
-  const uint64_t most = (uint64_t)paged_units(paged_length(0x7FFFFFFF, max_pages, cache->page_size)) * sequences * kv_heads * p.chunks;
-  return dtype == KB_F16 ? launch_paged<KB_F16>(ctx, p, most, st) : launch_paged<KB_BF16>(ctx, p, most, st);
+  const uint64_t most = (uint64_t)paged_units(paged_length(0x7FFFFFFF, max_pages, cache->page_size)) * sequences;
+  if (most > 0x7FFFFFFFull) return fail(ctx, KB_ERR_UNSUPPORTED, "%s: sequences * max_pages * page_size is beyond 2^38", where);
+  const uint32_t pieces = paged_pieces(ctx->sm_count, (uint64_t)kv_heads * p.chunks, most);
+  CUtensorMap map_k, map_v;
+  KB_TRY(encode_cache(ctx, &map_k, cache->d_k, cache->k_page, cache->k_row, cache->k_head, *cache, kv_heads, dim, dtype, p.box));
+  KB_TRY(encode_cache(ctx, &map_v, cache->d_v, cache->v_page, cache->v_row, cache->v_head, *cache, kv_heads, dim, dtype, p.box));
+  return dtype == KB_F16 ? launch_paged<KB_F16>(ctx, map_k, map_v, p, pieces, st) : launch_paged<KB_BF16>(ctx, map_k, map_v, p, pieces, st);
 }

@@ -93,7 +93,7 @@ struct kb_ctx {
   // paged attention (kb_attention.h)
   unsigned char* paged_ws = nullptr;   // parts of divided sequences, and arrival counts that are zero between calls
   size_t paged_ws_bytes = 0;
-  bool attention_ready = false;     // the attention kernels' limits are raised
+  bool attention_ready = false, paged_ready = false;   // the attention kernels' limits are raised
   uint32_t product_rows = 0, product_splits = 0;   // of the last product's launch: rows of A per tile, CTAs per tile
 };
 

@@ -1,22 +1,29 @@
 // Attention of one new token per sequence over a paged cache (contract in include/kb_attention.h).
 //
 // Bound by the cache's bytes: every key and value is read once for the query heads that share it, up to
-// 16 of them, and the rest has to stay out of the way.  Work is divided evenly whatever the lengths: an
-// item is a (sequence, group of heads), its units are steps of 128 keys, the units of all items form
-// one row that is cut into as many pieces as CTAs fit the card, and a CTA takes the items that its piece
-// touches one after the other.  An item that lies in one piece is finished there; otherwise each piece
-// leaves its part in the workspace, and the CTA that comes last adds the parts up in the order of the keys.
+// 16 of them, and the rest has to stay out of the way.  Work is divided evenly whatever the lengths: steps
+// of 128 keys are the units, those of all sequences form one row, and the row is cut into pieces, as many
+// as let the card run a CTA for each piece and group of heads at the same time.  A CTA takes the sequences that its
+// piece touches one after the other; CTAs of the same piece are neighbours, so that the groups'
+// heads, which lie side by side in the cache, are read at about the same time.  A sequence that lies in
+// one piece is finished there; otherwise each piece leaves its part in the workspace, and the CTA that comes
+// last adds the parts up in the order of the keys.
 //
-// A warp takes 16 keys of a step at a time, straight from global memory into the registers of
-// the warp-wide matrix instructions, with no staging in between.  What makes that possible: the order of a
-// contraction is free as long as both operands have the same.
-//   scores  S^T[16 keys][8 heads] = K Q^T: lane (g, t) = (lane / 4, lane % 4) holds the elements
-//     32 h + 8 t .. + 7 of keys g and g + 8, so that every load is 16 bytes and four lanes read 64 in a row;
-//     q is held in the same order.
-//   out  O^T[dim][8 heads] = V^T P^T: lane (g, t) holds the elements 64 c + 8 g .. + 7 of the keys 2t, 2t + 1,
-//     2t + 8, 2t + 9; two keys' elements are paired by byte permutes, and the rows of the product are
-//     whatever elements the lanes' loads brought.  P^T comes from S^T by transposing 8 x 8 matrices of
-//     16-bit numbers between lanes.
+// A warp takes 16 keys of a step at a time, which a ring of its own in shared memory gets by tensor-map copies
+// (boxes of 64 elements and up to 16 keys of a page in the 128-byte swizzle), kPagedStages tiles ahead and
+// on into the next sequence: 192 KB are on their way per SM at dim 128.  Straight from global memory into
+// registers, with 16 warps per SM, 128 x 4096 keys of 8 heads took 486 us.  From there they go into warp-wide
+// matrix instructions without any rearrangement, because the order of a contraction and of an operand's rows is
+// free as long as the other operand and the result's readers have the same:
+//   scores  S^T[16 keys][8 heads] = K Q^T: lane (g, t) = (lane / 4, lane % 4) reads the elements 32 h + 8 t .. + 7
+//     of keys kappa(g) and kappa(g) + 8, 16 bytes each, as its part of the first operand's rows g and g + 8; q
+//     is held in the same order.
+//   out  O^T[dim][8 heads] = V^T P^T: P^T comes from S^T by transposing 8 x 8 matrices of 16-bit numbers
+//     between lanes, so lane (g, t) has the keys kappa(2t), kappa(2t + 1) and those + 8; it reads their elements
+//     64 c + 8 g .. + 7, pairs two keys' by byte permutes, and the rows of the product are whatever elements
+//     its reads brought.
+// kappa(g) = g, with bit 2 flipped where g is odd: then the 8 lanes of a phase read from 8 different bank groups in
+// both places.
 // The 8-column tile of the instruction holds the heads: fewer than 8 waste matrix work, which is not
 // what bounds this kernel.  The exponentials are relative to a running value that is raised only where
 // a score exceeds it by more than 2^kLazy; p is rounded to the storage type for the matrix
@@ -24,6 +31,7 @@
 #pragma once
 
 #include "kb_block8.cuh"
+#include "kb_tcgen05.cuh"
 
 namespace kb {
 
@@ -34,10 +42,9 @@ constexpr float kRoom = 7.0f, kLazy = 8.0f;
 struct PagedParams {
   const void* q;
   uint64_t q_row, q_head;
-  const void *k, *v;
-  uint64_t k_page, k_row, k_head, v_page, v_row, v_head;
   uint64_t pages;
   uint32_t page_size, max_pages;
+  uint32_t box;                             // keys of a copy: 16, or the power of two that divides page_size
   const int* table;
   uint64_t table_row;
   const int* lengths;
@@ -49,14 +56,24 @@ struct PagedParams {
   float* lse;
   uint32_t q_heads;
   bool vec_out;
-  float* part;                              // [2 * grid][8 NT][DP] sums, then [2 * grid][8 NT][2] (r, sum of p)
-  float* part_rl;
-  unsigned int* arrived;                    // [grid], zero between calls
+  float* part;                              // [2 * CTAs][8 NT][DP] sums of p v
+  float* part_rl;                           // [2 * CTAs][8 NT][2]: r, sum of p
+  unsigned int* arrived;                    // [CTAs], zero between calls
   unsigned int* status;
 };
 
 constexpr int kPagedWarps = 8, kPagedThreads = 32 * kPagedWarps;
 constexpr uint32_t kStepKeys = 16 * kPagedWarps;   // keys of a unit
+constexpr uint32_t kPagedStages = 3;
+constexpr uint32_t kPagedWaves = 3;                // of CTAs, one per SM, at most
+template <int DP, int NT>
+struct PagedTile {
+  static constexpr uint32_t kHalf = DP / 64 * 2048;                      // 16 keys, or values
+  static constexpr uint32_t kRing = kPagedWarps * kPagedStages * 2 * kHalf;
+  static_assert(8 * NT * DP * 4 <= 2 * kHalf, "a warp's sums fit a tile");
+  static constexpr uint32_t smem(uint32_t pieces) { return 1024 + kRing + pieces * 8 * NT * 4; }   // and the join's factors
+};
+__host__ __device__ __forceinline__ uint32_t paged_kappa(uint32_t g) { return g ^ ((g & 1) << 2); }
 
 // A sequence's keys as the table can hold them, and units per group of heads: one at least, for the zeros of an
 // empty sequence
@@ -65,21 +82,15 @@ __host__ __device__ __forceinline__ uint32_t paged_length(int length, uint32_t m
   return length <= 0 ? 0u : (uint64_t)length > most ? (uint32_t)most : (uint32_t)length;
 }
 __host__ __device__ __forceinline__ uint32_t paged_units(uint32_t keys) { return keys ? (keys + kStepKeys - 1) / kStepKeys : 1u; }
-// Piece c of `pieces` of a row of n units starts here
-__host__ __device__ __forceinline__ unsigned long long piece_first(unsigned long long n, uint32_t c, uint32_t pieces) {
-  return n / pieces * c + (n % pieces) * c / pieces;
+// Piece c of `pieces` of a row of n >= pieces units starts here: the first n % pieces of them have one more
+__host__ __device__ __forceinline__ uint32_t piece_first(uint32_t n, uint32_t c, uint32_t pieces) {
+  const uint32_t more = n % pieces;
+  return n / pieces * c + (c < more ? c : more);
 }
 // The piece that unit u lies in
-__host__ __device__ __forceinline__ uint32_t piece_of(unsigned long long n, unsigned long long u, uint32_t pieces) {
-  uint32_t lo = 0, hi = pieces - 1;
-  while (lo < hi) {
-    const uint32_t mid = (lo + hi + 1) / 2;
-    if (piece_first(n, mid, pieces) <= u)
-      lo = mid;
-    else
-      hi = mid - 1;
-  }
-  return lo;
+__host__ __device__ __forceinline__ uint32_t piece_of(uint32_t n, uint32_t u, uint32_t pieces) {
+  const uint32_t size = n / pieces, more = n % pieces, bigger = more * (size + 1);
+  return u < bigger ? u / (size + 1) : more + (u - bigger) / size;
 }
 
 template <int DT>
@@ -103,99 +114,163 @@ __device__ __forceinline__ float exp2_fast(float x) {   // 2^x, 2 ulp; 0 for -in
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
 }
-__device__ __forceinline__ uint4 load_once(const void* p) {   // read through once: not kept in the first-level cache
-  uint4 v;
-  asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
-  return v;
-}
 // The reference of a row's exponentials as it enters an exponent: 0 while no score above -infinity was met
 __device__ __forceinline__ float known(float r) { return r == -INFINITY ? 0.0f : r; }
 
-// DP: 64 or 128, dim rounded up.  NT: tiles of 8 heads.  PAGE16: pages are multiples of 16 keys, so that the 16
-// keys of a warp's step lie on one page.
-template <int DT, int DP, int NT, bool PAGE16>
-__global__ void __launch_bounds__(kPagedThreads, NT == 1 ? 2 : 1) attention_paged_kernel(const PagedParams p) {
+// DP: 64 or 128, dim rounded up.  NT: tiles of 8 heads.
+template <int DT, int DP, int NT>
+__global__ void __launch_bounds__(kPagedThreads, 1)
+    attention_paged_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const PagedParams p) {
+  using T = PagedTile<DP, NT>;
   constexpr int kH = DP / 32, kC = DP / 64, kHeads = 8 * NT;
-  extern __shared__ float sums[];                 // [warps][heads][DP], and the join's weights
+  constexpr uint32_t kS = kPagedStages;
+  extern __shared__ unsigned char dyn[];
+  __shared__ uint64_t full[kPagedWarps][kS];
   __shared__ float warp_r[kPagedWarps][kHeads], warp_l[kPagedWarps][kHeads], item_r[kHeads], item_l[kHeads];
-  __shared__ unsigned long long scan[kPagedWarps];
-  __shared__ uint32_t found_seq, last_word;
-  __shared__ unsigned long long found_before;
+  __shared__ uint4 q_lanes[NT * kH * 32];
+  __shared__ const float4* sums_of[kPagedWarps];
+  __shared__ uint32_t scan[kPagedWarps], found_seq, found_before, last_word;
+  __shared__ unsigned int abort_word;
+  volatile unsigned int* abort_flag = &abort_word;
+  unsigned char* base = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(dyn) + 1023) & ~(uintptr_t)1023);
+  float* factors = reinterpret_cast<float*>(base + T::kRing);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-  const uint32_t per_seq = p.hkv * p.chunks;
-
-  // Units of all items, and the sequence that this piece starts in.
-  unsigned long long total = 0, u0 = 0, u1 = 0;
-  uint32_t pieces = 1;
-  for (int pass = 0; pass < 2; ++pass) {
-    unsigned long long before = 0;
-    bool found = false;
-    for (uint32_t base = 0; base < p.sequences && !found; base += kPagedThreads) {
-      const uint32_t s = base + threadIdx.x;
-      const uint32_t keys = s < p.sequences ? paged_length(p.lengths[s], p.max_pages, p.page_size) : 0;
-      const unsigned long long mine = s < p.sequences ? (unsigned long long)paged_units(keys) * per_seq : 0;
-      unsigned long long sum = mine;
-#pragma unroll
-      for (int o = 1; o < 32; o *= 2) {
-        const unsigned long long up = __shfl_up_sync(0xFFFFFFFFu, sum, o);
-        if (lane >= o) sum += up;
-      }
-      __syncthreads();
-      if (lane == 31) scan[warp] = sum;
-      __syncthreads();
-      unsigned long long all = 0, mine_before = before + sum - mine;
-#pragma unroll
-      for (int w = 0; w < kPagedWarps; ++w) {
-        if (w < warp) mine_before += scan[w];
-        all += scan[w];
-      }
-      if (pass == 1) {
-        const bool here = mine && u0 >= mine_before && u0 < mine_before + mine;
-        if (here) {
-          found_seq = s;
-          found_before = mine_before;
-        }
-        found = __syncthreads_or(here);
-      } else if (blockIdx.x == 0 && s < p.sequences && (p.lengths[s] < 0 || (uint64_t)p.lengths[s] > (uint64_t)p.max_pages * p.page_size)) {
-        set_status(p.status, (unsigned int)KB_ERR_INVALID_ARG);
-      }
-      before += all;
-    }
-    if (pass == 0) {
-      total = before;
-      pieces = (uint32_t)min((unsigned long long)gridDim.x, total);   // every piece has a unit
-      if (blockIdx.x >= pieces) return;
-      u0 = piece_first(total, blockIdx.x, pieces);
-      u1 = piece_first(total, blockIdx.x + 1, pieces);
-    }
+  if (threadIdx.x < kPagedWarps * kS) mbar_init(&full[threadIdx.x / kS][threadIdx.x % kS], 1);
+  if (threadIdx.x == 0) {
+    abort_word = 0u;
+    mbar_fence_init();
+    prefetch_map(&map_k);
+    prefetch_map(&map_v);
   }
-  __syncthreads();
-  uint32_t seq = found_seq;
-  unsigned long long seq_first = found_before;   // the first unit of the sequence's first item
+  const uint32_t item = blockIdx.x, per_seq = gridDim.x, hk = item / p.chunks, h0 = hk * p.group + item % p.chunks * kHeads;
+  const uint32_t heads = min((uint32_t)kHeads, (hk + 1) * p.group - h0);   // query heads h0 .. of this CTA
 
-  for (unsigned long long u = u0; u < u1;) {
-    const uint32_t keys = paged_length(p.lengths[seq], p.max_pages, p.page_size), units = paged_units(keys);
-    const uint32_t item = (uint32_t)((u - seq_first) / units), unit0 = (uint32_t)((u - seq_first) % units);
-    const uint32_t unit1 = (uint32_t)min((unsigned long long)units, unit0 + (u1 - u));
-    const unsigned long long item_first = u - unit0;
-    const uint32_t hk = item / p.chunks, h0 = hk * p.group + item % p.chunks * kHeads;   // first query head
-    const uint32_t heads = min((uint32_t)kHeads, (hk + 1) * p.group - h0);
+  // Units of all sequences, and the sequence that this piece starts in.  Up to a CTA's threads of them are read once.
+  uint32_t total = 0, pieces = 1, u0 = 0, u1 = 0, units = 0, before = 0;
+  auto scan_from = [&](uint32_t base) {   // this thread's sequence: its units, those before it; and of all up to here
+    const uint32_t s = base + threadIdx.x;
+    units = s < p.sequences ? paged_units(paged_length(p.lengths[s], p.max_pages, p.page_size)) : 0;
+    uint32_t sum = units;
+#pragma unroll
+    for (int o = 1; o < 32; o *= 2) {
+      const uint32_t up = __shfl_up_sync(0xFFFFFFFFu, sum, o);
+      if (lane >= o) sum += up;
+    }
+    __syncthreads();
+    if (lane == 31) scan[warp] = sum;
+    __syncthreads();
+    before = total + sum - units;
+#pragma unroll
+    for (int w = 0; w < kPagedWarps; ++w) {
+      if (w < warp) before += scan[w];
+      total += scan[w];
+    }
+  };
+  for (uint32_t base = 0; base < p.sequences; base += kPagedThreads) scan_from(base);
+  pieces = min(gridDim.y, total);   // every piece has a unit
+  if (blockIdx.y >= pieces) return;
+  u0 = piece_first(total, blockIdx.y, pieces);
+  u1 = piece_first(total, blockIdx.y + 1, pieces);
+  bool found = false;
+  const uint32_t all_units = total;
+  total = 0;
+  for (uint32_t base = 0; base < p.sequences && !found; base += kPagedThreads) {
+    if (p.sequences > kPagedThreads) scan_from(base);
+    const bool here = units && u0 >= before && u0 < before + units;
+    if (here) {
+      found_seq = base + threadIdx.x;
+      found_before = before;
+    }
+    found = __syncthreads_or(here);
+  }
+  if (!found) return;   // lengths that changed in between
+  total = all_units;
+  if (blockIdx.x == 0 && blockIdx.y == 0)
+    for (uint32_t s = threadIdx.x; s < p.sequences; s += kPagedThreads)
+      if (p.lengths[s] < 0 || (uint64_t)p.lengths[s] > (uint64_t)p.max_pages * p.page_size) set_status(p.status, (unsigned int)KB_ERR_INVALID_ARG);
+  uint32_t seq = found_seq, seq_first = found_before;   // the sequence and its first unit
 
-    // q as the second operand of the scores: heads h0 + 8 n + g
-    uint32_t qb[NT][kH][4];
-#pragma unroll
-    for (int n = 0; n < NT; ++n)
-#pragma unroll
-      for (int h = 0; h < kH; ++h) {
-        const uint32_t head = 8 * n + g, d = 32 * h + 8 * t;
-        uint4 w = make_uint4(0u, 0u, 0u, 0u);
-        if (head < heads && d < p.dim)
-          w = *reinterpret_cast<const uint4*>(static_cast<const unsigned short*>(p.q) + seq * p.q_row + (h0 + head) * p.q_head + d);
-        qb[n][h][0] = w.x;
-        qb[n][h][1] = w.y;
-        qb[n][h][2] = w.z;
-        qb[n][h][3] = w.w;
+  // ---- this warp's copies: the tiles of the piece's sequences one after the other, up to kS ahead of their use
+  unsigned char* ring = base + warp * kS * 2 * T::kHalf;
+  uint32_t p_seq = seq, p_first = seq_first, p_key = (u0 - seq_first) * kStepKeys + warp * 16, p_end = 0;
+  uint32_t p_stage = 0, issued = 0, used = 0, pages_at = 0;
+  int pages = -1;                                 // lane i: the page of the key (box = 16: of the step i on) pages_at + ...
+  bool p_known = false, bad = false;              // p_end and pages are p_seq's
+  unsigned long long there = 0;                   // 16 bits per tile on its way, the next one lowest: keys that are there
+  bool ok = true;                                 // no wait has run out
+  auto produce = [&]() {
+    if (!ok) return;
+    for (;;) {
+      if (!p_known) {
+        if (p_seq >= p.sequences || p_first >= u1) return;
+        const uint32_t keys = paged_length(p.lengths[p_seq], p.max_pages, p.page_size), n = paged_units(keys);
+        p_end = u1 - p_first >= n ? keys : (u1 - p_first) * kStepKeys;
+        p_known = true;
+        pages_at = p_key + 32 * kStepKeys;        // none yet
       }
+      if (p_key < p_end) break;
+      p_first += paged_units(paged_length(p.lengths[p_seq], p.max_pages, p.page_size));
+      ++p_seq;
+      p_key = warp * 16;
+      p_known = false;
+    }
+    // pages of the next 32 steps at once, or of the 16 keys of this one
+    const bool whole = p.box == 16;
+    if (!whole || p_key - pages_at >= 32 * kStepKeys) {
+      pages_at = p_key;
+      const uint32_t key = whole ? p_key + lane * kStepKeys : p_key + (lane & 15);
+      pages = -1;
+      if (key < p_end) {
+        const int page = p.table[p_seq * p.table_row + key / p.page_size];
+        if (page >= 0 && (uint64_t)page < p.pages)
+          pages = page;
+        else
+          bad = true;
+      }
+    }
+    const uint32_t left = p_end - p_key;
+    uint32_t mask;
+    if (whole)
+      mask = __shfl_sync(0xFFFFFFFFu, pages, (p_key - pages_at) / kStepKeys) >= 0 ? 0xFFFFu : 0u;
+    else
+      mask = __ballot_sync(0xFFFFFFFFu, pages >= 0) & 0xFFFFu;
+    if (left < 16) mask &= (1u << left) - 1;
+    there |= (unsigned long long)mask << (16 * (issued - used));
+    const uint32_t bar = smem_u32(&full[warp][p_stage]), to = smem_u32(ring + p_stage * 2 * T::kHalf);
+    uint32_t boxes = 0;
+    for (uint32_t i = 0; i < 16; i += p.box) boxes += (mask >> i) & 1u;
+    expect_tx_elect(bar, boxes * p.box * 128 * kC * 2);
+    for (uint32_t i = 0; i < 16; i += p.box) {
+      const int page = __shfl_sync(0xFFFFFFFFu, pages, whole ? (p_key - pages_at) / kStepKeys : i);
+      if (((mask >> i) & 1u) == 0) continue;
+      const int row = (int)((p_key + i) % p.page_size);
+#pragma unroll
+      for (int c = 0; c < kC; ++c) {
+        tma_load_4d(to + c * 2048 + i * 128, &map_k, c * 64, (int)hk, row, page, bar);
+        tma_load_4d(to + T::kHalf + c * 2048 + i * 128, &map_v, c * 64, (int)hk, row, page, bar);
+      }
+    }
+    ++issued;
+    p_stage = p_stage + 1 == kS ? 0 : p_stage + 1;
+    p_key += kStepKeys;
+  };
+  for (uint32_t i = 0; i < kS; ++i) produce();
+
+  uint32_t stage = 0, phase = 0;
+  const uint32_t key_of[2] = {paged_kappa(g), paged_kappa(g) + 8};                              // rows g and g + 8 of the scores
+  const uint32_t val_of[4] = {2u * t, (2u * t + 1) ^ 4u, 2u * t + 8, ((2u * t + 1) ^ 4u) + 8};   // kappa(2t), kappa(2t + 1), and + 8
+  for (uint32_t u = u0; u < u1 && seq < p.sequences; ++seq) {
+    const uint32_t keys = paged_length(p.lengths[seq], p.max_pages, p.page_size), seq_units = paged_units(keys);
+    const uint32_t unit0 = u - seq_first, unit1 = min(seq_units, u1 - seq_first);
+    const uint32_t key_end = unit1 == seq_units ? keys : unit1 * kStepKeys;
+    // q as the second operand of the scores, in the lanes' order: heads h0 + 8 n + g
+    for (uint32_t i = threadIdx.x; i < NT * kH * 32; i += kPagedThreads) {
+      const uint32_t head = i / (kH * 32) * 8 + (i & 31) / 4, d = i / 32 % kH * 32 + (i & 3) * 8;
+      uint4 w = make_uint4(0u, 0u, 0u, 0u);
+      if (head < heads && d < p.dim)
+        w = *reinterpret_cast<const uint4*>(static_cast<const unsigned short*>(p.q) + seq * p.q_row + (h0 + head) * p.q_head + d);
+      q_lanes[i] = w;
+    }
     float acc[NT][kC][4][4], r[NT][2], l[NT][2];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
@@ -204,94 +279,43 @@ __global__ void __launch_bounds__(kPagedThreads, NT == 1 ? 2 : 1) attention_page
 #pragma unroll
       for (int i = 0; i < kC * 16; ++i) acc[n][i / 16][i / 4 % 4][i % 4] = 0.0f;
     }
-
-    const int* table = p.table + seq * p.table_row;
-    const uint32_t key_end = min(keys, unit1 * kStepKeys);
-    const unsigned short* kh = static_cast<const unsigned short*>(p.k) + hk * p.k_head;
-    const unsigned short* vh = static_cast<const unsigned short*>(p.v) + hk * p.v_head;
-    bool bad = false;
-    // Page of key `key`, -1 where there is none or the table names one that is not there
-    auto page_of = [&](uint32_t key) -> int {
-      if (key >= key_end) return -1;
-      const int page = table[key / p.page_size];
-      if (page >= 0 && (uint64_t)page < p.pages) return page;
-      bad = true;
-      return -1;
-    };
-    uint4 kr[2][kH], vr[4][kC];
-    // The pages of a warp's next 32 steps (PAGE16: lane i has step i's) or of the next step's 16 keys (lane i has key i's)
-    uint32_t key0 = unit0 * kStepKeys + warp * 16;
-    int pages = -1;
-    uint32_t ahead = 0;                       // PAGE16: steps whose pages the lanes hold
-    uint32_t pages_at = key0;                 // the key that lane 0's page belongs to
-    auto fetch_pages = [&](uint32_t key) {
-      pages_at = key;
-      pages = PAGE16 ? page_of(key + lane * kStepKeys) : page_of(key + (lane & 15));
-      ahead = 32;
-    };
-    // Page and place on it of key key0 + i
-    auto row_of = [&](uint32_t key, int i, int& page, uint32_t& off) {
-      if constexpr (PAGE16) {
-        page = __shfl_sync(0xFFFFFFFFu, pages, (key - pages_at) / kStepKeys);
-        off = key % p.page_size + i;
-        if (key + i >= key_end) page = -1;
-      } else {
-        page = __shfl_sync(0xFFFFFFFFu, pages, i);
-        off = (key + i) % p.page_size;
+    __syncthreads();
+    unsigned char* scratch = nullptr;          // the tile that this warp used last
+    for (uint32_t key0 = unit0 * kStepKeys + warp * 16; key0 < key_end; key0 += kStepKeys) {
+      if (scratch) produce();                  // into the tile used before this one
+      ok = ok && mbar_wait_bounded(&full[warp][stage], phase, abort_flag, p.status);
+      __syncwarp();
+      const unsigned char* tile = ring + stage * 2 * T::kHalf;
+      scratch = ring + stage * 2 * T::kHalf;
+      const uint32_t mask = (uint32_t)there & 0xFFFFu;
+      there >>= 16;
+      ++used;
+      if (++stage == kS) {
+        stage = 0;
+        phase ^= 1u;
       }
-    };
-    auto load_k = [&](uint32_t key, bool (&there)[2]) {
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        int page;
-        uint32_t off;
-        row_of(key, g + 8 * i, page, off);
-        there[i] = page >= 0;
-        const unsigned short* at = kh + (uint64_t)(uint32_t)page * p.k_page + (uint64_t)off * p.k_row + 8 * t;
-#pragma unroll
-        for (int h = 0; h < kH; ++h)
-          kr[i][h] = there[i] && 32 * h + 8 * t < (int)p.dim ? load_once(at + 32 * h) : make_uint4(0u, 0u, 0u, 0u);
-      }
-    };
-    auto load_v = [&](uint32_t key) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        int page;
-        uint32_t off;
-        row_of(key, 2 * t + (i & 1) + 8 * (i >> 1), page, off);
-        const unsigned short* at = vh + (uint64_t)(uint32_t)page * p.v_page + (uint64_t)off * p.v_row + 8 * g;
-#pragma unroll
-        for (int c = 0; c < kC; ++c)
-          vr[i][c] = page >= 0 && 64 * c + 8 * g < (int)p.dim ? load_once(at + 64 * c) : make_uint4(0u, 0u, 0u, 0u);
-      }
-    };
-
-    bool there[2] = {false, false};
-    if (key0 < key_end) {
-      fetch_pages(key0);
-      load_k(key0, there);
-    }
-    for (; key0 < key_end; key0 += kStepKeys) {
-      load_v(key0);
+      if (!ok) continue;
+      auto read = [&](uint32_t at, uint32_t row, int c, uint32_t unit) {   // 16 bytes of a swizzled row
+        return *reinterpret_cast<const uint4*>(tile + at + c * 2048 + row * 128 + ((unit ^ (row & 7)) * 16));
+      };
       float s[NT][4];
 #pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.0f;
+      for (int n = 0; n < NT; ++n) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.0f;
 #pragma unroll
-        for (int h = 0; h < kH; ++h) {
-          mma_16816<DT>(s[n], kr[0][h].x, kr[1][h].x, kr[0][h].y, kr[1][h].y, qb[n][h][0], qb[n][h][1]);
-          mma_16816<DT>(s[n], kr[0][h].z, kr[1][h].z, kr[0][h].w, kr[1][h].w, qb[n][h][2], qb[n][h][3]);
+      for (int h = 0; h < kH; ++h) {
+        const uint4 k0 = read(0, key_of[0], h / 2, h % 2 * 4 + t), k1 = read(0, key_of[1], h / 2, h % 2 * 4 + t);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          const uint4 qv = q_lanes[(n * kH + h) * 32 + lane];
+          mma_16816<DT>(s[n], k0.x, k1.x, k0.y, k1.y, qv.x, qv.y);
+          mma_16816<DT>(s[n], k0.z, k1.z, k0.w, k1.w, qv.z, qv.w);
         }
       }
-      const bool seen0 = there[0], seen1 = there[1];
-      if (key0 + kStepKeys < key_end) {   // the next keys are on their way while these are worked on
-        if (!PAGE16 || (key0 + kStepKeys - pages_at) / kStepKeys >= ahead) fetch_pages(key0 + kStepKeys);
-        load_k(key0 + kStepKeys, there);
-      }
+      const bool seen0 = (mask >> key_of[0]) & 1u, seen1 = (mask >> key_of[1]) & 1u;
       uint32_t pb[NT][2];
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
-        float x[4];   // keys g, g, g + 8, g + 8; heads 2t, 2t + 1, 2t, 2t + 1
+        float x[4];   // keys of rows g, g, g + 8, g + 8; heads 2t, 2t + 1, 2t, 2t + 1
 #pragma unroll
         for (int i = 0; i < 4; ++i) x[i] = (i < 2 ? seen0 : seen1) ? s[n][i] * p.scale_log2 : -INFINITY;
         const float top0 = fmaxf(x[0], x[2]), top1 = fmaxf(x[1], x[3]);
@@ -321,21 +345,25 @@ __global__ void __launch_bounds__(kPagedThreads, NT == 1 ? 2 : 1) attention_page
       }
 #pragma unroll
       for (int c = 0; c < kC; ++c) {
-        const uint32_t* v0 = reinterpret_cast<const uint32_t*>(&vr[0][c]);
-        const uint32_t* v1 = reinterpret_cast<const uint32_t*>(&vr[1][c]);
-        const uint32_t* v2 = reinterpret_cast<const uint32_t*>(&vr[2][c]);
-        const uint32_t* v3 = reinterpret_cast<const uint32_t*>(&vr[3][c]);
+        uint4 v4[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          v4[i] = read(T::kHalf, val_of[i], c, g);
+          if (mask != 0xFFFFu && ((mask >> val_of[i]) & 1u) == 0) v4[i] = make_uint4(0u, 0u, 0u, 0u);   // 0 times NaN is not 0
+        }
+        const uint32_t w[4][4] = {{v4[0].x, v4[0].y, v4[0].z, v4[0].w}, {v4[1].x, v4[1].y, v4[1].z, v4[1].w},
+                                  {v4[2].x, v4[2].y, v4[2].z, v4[2].w}, {v4[3].x, v4[3].y, v4[3].z, v4[3].w}};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {   // rows g: element i of the lane's 8, rows g + 8: element 4 + i
           const uint32_t pick = i & 1 ? 0x7632u : 0x5410u;
-          const uint32_t a0 = __byte_perm(v0[i >> 1], v1[i >> 1], pick), a1 = __byte_perm(v0[2 + (i >> 1)], v1[2 + (i >> 1)], pick);
-          const uint32_t a2 = __byte_perm(v2[i >> 1], v3[i >> 1], pick), a3 = __byte_perm(v2[2 + (i >> 1)], v3[2 + (i >> 1)], pick);
+          const uint32_t a0 = __byte_perm(w[0][i >> 1], w[1][i >> 1], pick), a1 = __byte_perm(w[0][2 + (i >> 1)], w[1][2 + (i >> 1)], pick);
+          const uint32_t a2 = __byte_perm(w[2][i >> 1], w[3][i >> 1], pick), a3 = __byte_perm(w[2][2 + (i >> 1)], w[3][2 + (i >> 1)], pick);
 #pragma unroll
           for (int n = 0; n < NT; ++n) mma_16816<DT>(acc[n][c][i], a0, a1, a2, a3, pb[n][0], pb[n][1]);
         }
       }
+      __syncwarp();   // the tile is read
     }
-    if (bad) set_status(p.status, (unsigned int)KB_ERR_INVALID_ARG);
 
     // The warps' parts: one reference for all, sums of p over the lanes, sums of p v over the warps
 #pragma unroll
@@ -363,20 +391,25 @@ __global__ void __launch_bounds__(kPagedThreads, NT == 1 ? 2 : 1) attention_page
       item_l[threadIdx.x] = sum;
     }
     __syncthreads();
+    // sums of p v go to the tile that the warp used last; warps without a tile of this sequence have none
+    const uint32_t warps = min((uint32_t)kPagedWarps, (key_end - unit0 * kStepKeys + 15) / 16);
+    if (scratch) {
 #pragma unroll
-    for (int n = 0; n < NT; ++n)
+      for (int n = 0; n < NT; ++n)
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const uint32_t head = 8 * n + 2 * t + i;
-        const float f = r[n][i] == -INFINITY ? 0.0f : exp2_fast(r[n][i] - item_r[head]);
+        for (int i = 0; i < 2; ++i) {
+          const uint32_t head = 8 * n + 2 * t + i;
+          const float f = r[n][i] == -INFINITY ? 0.0f : exp2_fast(r[n][i] - item_r[head]);
 #pragma unroll
-        for (int c = 0; c < kC; ++c) {
-          float* to = sums + ((uint32_t)warp * kHeads + head) * DP + 64 * c + 8 * g;
-          *reinterpret_cast<float4*>(to) = make_float4(acc[n][c][0][i] * f, acc[n][c][1][i] * f, acc[n][c][2][i] * f, acc[n][c][3][i] * f);
-          *reinterpret_cast<float4*>(to + 4) =
-              make_float4(acc[n][c][0][2 + i] * f, acc[n][c][1][2 + i] * f, acc[n][c][2][2 + i] * f, acc[n][c][3][2 + i] * f);
+          for (int c = 0; c < kC; ++c) {
+            float* to = reinterpret_cast<float*>(scratch) + head * DP + 64 * c + 8 * g;
+            *reinterpret_cast<float4*>(to) = make_float4(acc[n][c][0][i] * f, acc[n][c][1][i] * f, acc[n][c][2][i] * f, acc[n][c][3][i] * f);
+            *reinterpret_cast<float4*>(to + 4) =
+                make_float4(acc[n][c][0][2 + i] * f, acc[n][c][1][2 + i] * f, acc[n][c][2][2 + i] * f, acc[n][c][3][2 + i] * f);
+          }
         }
-      }
+      if (lane == 0) sums_of[warp] = reinterpret_cast<const float4*>(scratch);
+    }
     __syncthreads();
 
     // Four elements of a head, of sum l and reference r, to the outputs
@@ -395,14 +428,15 @@ __global__ void __launch_bounds__(kPagedThreads, NT == 1 ? 2 : 1) attention_page
       }
       if (d == 0 && p.lse) p.lse[(uint64_t)seq * p.q_heads + h0 + head] = none ? -INFINITY : (top + log2f(sum)) * 0.69314718055994531f;
     };
-    const bool whole = unit0 == 0 && unit1 == units;
-    // this piece's place in the workspace: an item that began earlier is the piece's first, the other its last
-    float* mine = p.part + (uint64_t)(2 * blockIdx.x + (unit0 == 0)) * kHeads * DP;
+    const bool whole = unit0 == 0 && unit1 == seq_units;
+    // places in the workspace: a sequence that began in an earlier piece is its piece's first, another its last
+    auto place = [&](uint32_t piece, bool began) { return (uint64_t)2 * (piece * per_seq + item) + (began ? 1 : 0); };
+    const uint64_t here = place(blockIdx.y, unit0 == 0);
+    float* mine = p.part + here * kHeads * DP;
     for (uint32_t i = threadIdx.x; i < kHeads * DP / 4; i += kPagedThreads) {
       float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll
-      for (int w = 0; w < kPagedWarps; ++w) {
-        const float4 x = reinterpret_cast<const float4*>(sums)[w * (kHeads * DP / 4) + i];
+      for (uint32_t w = 0; w < warps; ++w) {
+        const float4 x = sums_of[w][i];
         o.x += x.x;
         o.y += x.y;
         o.z += x.z;
@@ -415,42 +449,47 @@ __global__ void __launch_bounds__(kPagedThreads, NT == 1 ? 2 : 1) attention_page
     }
     if (!whole) {
       if (threadIdx.x < kHeads)
-        __stcg(reinterpret_cast<float2*>(p.part_rl) + (uint64_t)(2 * blockIdx.x + (unit0 == 0)) * kHeads + threadIdx.x,
-               make_float2(item_r[threadIdx.x], item_l[threadIdx.x]));
-      const uint32_t c0 = piece_of(total, item_first, pieces), c1 = piece_of(total, item_first + units - 1, pieces);
+        __stcg(reinterpret_cast<float2*>(p.part_rl) + here * kHeads + threadIdx.x, make_float2(item_r[threadIdx.x], item_l[threadIdx.x]));
+      const uint32_t c0 = piece_of(total, seq_first, pieces), parts = piece_of(total, seq_first + seq_units - 1, pieces) - c0 + 1;
       __threadfence();
       __syncthreads();
       if (threadIdx.x == 0) {
-        const bool last = atomicAdd(p.arrived + c0, 1u) == c1 - c0;
-        if (last) p.arrived[c0] = 0u;   // as the next call expects it
+        unsigned int* count = p.arrived + c0 * per_seq + item;   // a sequence that goes on is the last of the piece it began in
+        const bool last = atomicAdd(count, 1u) == parts - 1;
+        if (last) *count = 0u;                                   // as the next call expects it
         last_word = last;
         __threadfence();
       }
       __syncthreads();
       if (last_word) {
-        const uint32_t parts = c1 - c0 + 1;
-        auto place = [&](uint32_t i) { return (uint64_t)(2 * (c0 + i) + (i == 0)); };
-        if (threadIdx.x < kHeads) {
-          const float2* rl = reinterpret_cast<const float2*>(p.part_rl) + threadIdx.x;
+        // a warp per head: the parts' common reference and their factors
+        for (uint32_t head = warp; head < kHeads; head += kPagedWarps) {
+          const float2* rl = reinterpret_cast<const float2*>(p.part_rl) + head;
           float top = -INFINITY, sum = 0.0f;
-          for (uint32_t i = 0; i < parts; ++i) top = fmaxf(top, __ldcg(rl + place(i) * kHeads).x);
-          for (uint32_t i = 0; i < parts; ++i) {
-            const float2 x = __ldcg(rl + place(i) * kHeads);
+          for (uint32_t i = lane; i < parts; i += 32) top = fmaxf(top, __ldcg(rl + place(c0 + i, i == 0) * kHeads).x);
+#pragma unroll
+          for (int o = 16; o > 0; o /= 2) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+          for (uint32_t i = lane; i < parts; i += 32) {
+            const float2 x = __ldcg(rl + place(c0 + i, i == 0) * kHeads);
             const float f = x.x == -INFINITY ? 0.0f : exp2_fast(x.x - top);
-            sums[i * kHeads + threadIdx.x] = f;
-            sum += x.y * f;
+            factors[i * kHeads + head] = f;
+            sum = fmaf(x.y, f, sum);
           }
-          item_r[threadIdx.x] = top;
-          item_l[threadIdx.x] = sum;
+#pragma unroll
+          for (int o = 16; o > 0; o /= 2) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+          if (lane == 0) {
+            item_r[head] = top;
+            item_l[head] = sum;
+          }
         }
         __syncthreads();
         for (uint32_t j = threadIdx.x; j < kHeads * DP / 4; j += kPagedThreads) {
           const uint32_t head = j / (DP / 4);
           float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll 4
+#pragma unroll 8
           for (uint32_t i = 0; i < parts; ++i) {
-            const float4 x = __ldcg(reinterpret_cast<const float4*>(p.part) + place(i) * (kHeads * DP / 4) + j);
-            const float f = sums[i * kHeads + head];
+            const float4 x = __ldcg(reinterpret_cast<const float4*>(p.part) + place(c0 + i, i == 0) * (kHeads * DP / 4) + j);
+            const float f = factors[i * kHeads + head];
             o.x = fmaf(x.x, f, o.x);
             o.y = fmaf(x.y, f, o.y);
             o.z = fmaf(x.z, f, o.z);
@@ -460,11 +499,18 @@ __global__ void __launch_bounds__(kPagedThreads, NT == 1 ? 2 : 1) attention_page
         }
       }
     }
-    __syncthreads();   // shared memory is used again
-    u += unit1 - unit0;
-    if (u - seq_first == (unsigned long long)units * per_seq && u < u1) {
-      seq_first = u;
-      ++seq;
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // the sums were read before copies come in their place
+    __syncthreads();                                               // shared memory is used again
+    if (scratch) produce();
+    u = seq_first + unit1;
+    seq_first += seq_units;
+  }
+  if (bad) set_status(p.status, (unsigned int)KB_ERR_INVALID_ARG);
+  if (!ok) {   // what is on its way lands before the CTA ends
+    for (uint32_t i = 0; i < kS; ++i) {
+      const unsigned long long t0 = global_ns();
+      while (issued > i && !mbar_try_wait(&full[warp][(issued - 1 - i) % kS], ((issued - 1 - i) / kS) & 1u))
+        if (global_ns() - t0 > 1000000000ull) break;
     }
   }
 }
