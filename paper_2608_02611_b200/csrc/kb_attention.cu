@@ -168,11 +168,12 @@ kb_status launch_paged(kb_ctx* ctx, const CUtensorMap& k, const CUtensorMap& v, 
 
 // ---- attention over prompts ----------------------------------------------------------------------
 
-// Tensor map of heads [tokens][heads][dim], boxes of 64 elements of dim and 128 tokens of a head in the 128-byte
+// Tensor map of heads [tokens][heads][dim], boxes of 64 elements of dim and `rows` tokens of a head in the 128-byte
 // swizzle; places outside the tensor read as zero.
-kb_status encode_heads(kb_ctx* ctx, CUtensorMap* map, const Heads& t, uint64_t tokens, uint32_t heads, uint32_t dim, kb_dtype dtype) {
+kb_status encode_heads(kb_ctx* ctx, CUtensorMap* map, const Heads& t, uint64_t tokens, uint32_t heads, uint32_t dim, kb_dtype dtype,
+                       uint32_t rows) {
   const cuuint64_t dims[3] = {dim, tokens, heads}, strides[2] = {t.row * 2, t.head * 2};
-  const cuuint32_t box[3] = {64, 128, 1}, step[3] = {1, 1, 1};
+  const cuuint32_t box[3] = {64, rows, 1}, step[3] = {1, 1, 1};
   const CUresult rc = reinterpret_cast<EncodeTiled>(ctx->encode_tiled)(
       map, dtype == KB_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(t.p), dims, strides,
       box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
@@ -358,9 +359,9 @@ extern "C" kb_status kb_attention(kb_ctx* ctx, const void* d_q, uint64_t q_row, 
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   KB_TRY(prepare_prompt(ctx));
   CUtensorMap map_q, map_k, map_v;
-  KB_TRY(encode_heads(ctx, &map_q, q, q_tokens, q_heads, dim, dtype));
-  KB_TRY(encode_heads(ctx, &map_k, k, std::max<uint64_t>(k_tokens, 1), kv_heads, dim, dtype));
-  KB_TRY(encode_heads(ctx, &map_v, v, std::max<uint64_t>(k_tokens, 1), kv_heads, dim, dtype));
+  KB_TRY(encode_heads(ctx, &map_q, q, q_tokens, q_heads, dim, dtype, 128));
+  KB_TRY(encode_heads(ctx, &map_k, k, std::max<uint64_t>(k_tokens, 1), kv_heads, dim, dtype, kPromptKeys));
+  KB_TRY(encode_heads(ctx, &map_v, v, std::max<uint64_t>(k_tokens, 1), kv_heads, dim, dtype, kPromptKeys));
   PromptParams p = {};
   p.q_offsets = d_q_offsets;
   p.k_offsets = d_k_offsets;
@@ -388,11 +389,12 @@ extern "C" kb_status kb_attention(kb_ctx* ctx, const void* d_q, uint64_t q_row, 
   p.o_head = out_head;
   p.lse = d_lse;
   p.status = ctx->d_status;
+  p.next = ctx->d_status + 40;
   // the lengths are the device's: room for every sequence's last, partial piece
   const uint64_t rows = p.pair ? 128 : 256, pieces = d_q_offsets ? q_tokens / rows + sequences : (q_tokens + rows - 1) / rows;
   const uint64_t grid = pieces * (p.pair ? q_heads / 2 : q_heads);
   if (grid > 0x7FFFFFFFull) return fail(ctx, KB_ERR_UNSUPPORTED, "%s: more than 2^31 - 1 tiles", where);
-  const unsigned int n = (unsigned int)grid;
+  const unsigned int n = (unsigned int)std::min<uint64_t>(grid, ctx->sm_count);
   if (dim <= 64)
     return dtype == KB_F16 ? launch_prompt<KB_F16, 64>(ctx, map_q, map_k, map_v, p, n, st) : launch_prompt<KB_BF16, 64>(ctx, map_q, map_k, map_v, p, n, st);
   return dtype == KB_F16 ? launch_prompt<KB_F16, 128>(ctx, map_q, map_k, map_v, p, n, st) : launch_prompt<KB_BF16, 128>(ctx, map_q, map_k, map_v, p, n, st);

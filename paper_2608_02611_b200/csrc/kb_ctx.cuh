@@ -46,7 +46,7 @@ struct kb_ctx {
   float steps_hist[2] = {0.0f, 0.0f};   // the same for the last call on each accumulator set
   // [0] status, [1..3] counters of the binary64 gate, [4] effective K of an indexed call,
   // [8..10] and [16..18] the two counter sets of the binary32 gate, [20..23] two 64-bit sums of
-  // fruitless second looks on their way to the host, [60] probe sink
+  // fruitless second looks on their way to the host, [40..41] items of kb_attention, [60] probe sink
   unsigned int* d_status = nullptr;
   uint32_t forced_grid = 0;
   unsigned char* small_ws = nullptr; // single-launch path: [tickets 4 KB | partial records 384 KB]

@@ -1,16 +1,17 @@
 // Attention over whole prompts (contract in include/kb_attention.h).
 //
-// A CTA takes two tiles of 128 queries against the keys and values that they share, 128 keys at a
+// A CTA takes two tiles of 128 queries against the keys and values that they share, 64 keys at a
 // time: two neighbouring heads of a group at the same 128 queries, or 256 queries of one head where groups
-// are odd.  Per tile and step the tensor cores make S = Q K^T (128 x 128, accumulated in tensor memory), a
+// are odd.  Per tile and step the tensor cores make S = Q K^T (128 x 64, accumulated in tensor memory), a
 // warpgroup with one thread per query turns S into P = 2^(S c - r) in registers and writes it back over S
 // in 16 bits, and the tensor cores add P V to the output, which stays in tensor memory to the end.
-// While one tile's warpgroup is at its exponentials the tensor cores work for the other tile.
+// S has two places per tile: the next step's scores are there when a warpgroup is done with this one's, and
+// no product waits for the one before it (one place for 128 keys: 3830 cycles for 128 keys of both tiles, of which the
+// warpgroups computed for 1720 and waited for the rest).
 //
 // The running reference r of a query (shared with the paged kernel: kRoom, kLazy) is raised only where a score
 // exceeds it by more than 2^kLazy, so the output in tensor memory is rescaled a few times per query and
-// not once per step.  Bound by the exponentials and the tensor cores together: a tile's step is 1024 cycles
-// of 128 x 128 x 128 products (two at dim 128) and 16384 exponentials, 1024 cycles at 16 a cycle.
+// not once per step.
 //
 // What a query does not see never enters its sums: scores behind a mask become -infinity before anything is
 // done with them, and values of keys behind a sequence's end are zeroed in shared memory before they
@@ -18,8 +19,11 @@
 // broken inputs: where a query's output is not finite although its sum is, the values it does not see are looked
 // at, and if one of them is not finite the query is computed again without them (repair).
 //
-// Roles: warp 0 copies, warp 1 issues matrix instructions, warps 2 and 3 idle; warps 4 to 7 and 8 to 11
-// are the tiles' warpgroups.  Every wait is bounded.
+// CTAs are persistent: one per SM takes items off a common count, those with the most keys first, and its copies and
+// score products run ahead into the next item while the last one's outputs are stored.
+//
+// Roles: warp 0 copies, warps 1 to 4 issue matrix instructions, warp 5 hands out the items, warp 6 zeroes values behind a
+// sequence's end, warps 8 to 11 and 12 to 15 are the tiles' warpgroups.  Every wait is bounded.
 #pragma once
 
 #include "kb_paged.cuh"
@@ -27,8 +31,10 @@
 
 namespace kb {
 
+
 struct PromptParams {
   const int *q_offsets, *k_offsets;   // NULL: one sequence of all tokens
+  unsigned int* next;                 // [0] items handed out beyond the first of each CTA, [1] CTAs that have ended; 0 between calls
   uint32_t sequences, q_tokens, k_tokens;
   uint32_t hq, group, dim;
   bool pair;                          // tiles are two heads (else: two pieces of 128 queries)
@@ -42,27 +48,34 @@ struct PromptParams {
   unsigned int* status;
 };
 
+constexpr uint32_t kPromptKeys = 64;   // keys of a step
 template <int DP>   // dim rounded up to 64 or 128
 struct PromptTile {
   static constexpr uint32_t kChunks = DP / 64;                  // of 64 elements = 128 bytes
-  static constexpr uint32_t kTileBytes = 128 * DP * 2;          // 128 rows of q, k or v
-  static constexpr uint32_t kStages = DP == 128 ? 4 : 8;        // of the ring of k and v tiles
-  static constexpr uint32_t kSmem = 1024 + (2 + kStages) * kTileBytes;
-  static constexpr uint32_t kTmemS = 0, kTmemO = 256, kTmemCols = 512;   // per tile: S 128 columns, O DP columns
-  static constexpr int kThreads = 384;
-  // 168 registers per thread at launch, shared out 56 / 224 / 224 to the three warpgroups
-  static constexpr int kRegsLaunch = 168, kRegsControl = 56, kRegsSoftmax = 224;
-  static_assert(128 * kRegsControl + 256 * kRegsSoftmax <= kThreads * kRegsLaunch, "register shares");
+  static constexpr uint32_t kTileBytes = 128 * DP * 2;          // 128 rows of q
+  static constexpr uint32_t kStepBytes = kPromptKeys * DP * 2;  // of k or v
+  static constexpr uint32_t kChunkBytes = kPromptKeys * 128;    // of which 64 elements
+  static constexpr uint32_t kStages = 256 / kPromptKeys;        // of the rings of k and of v tiles
+  static constexpr uint32_t kOutPitch = 80, kOutBytes = 32 * kOutPitch;   // a warp's way out: 64 bytes of 32 rows at a time
+  static constexpr uint32_t kSmem = 1024 + 2 * kTileBytes + 2 * kStages * kStepBytes + 8 * kOutBytes;
+  // tensor memory: per tile 128 columns for S, in places of kPromptKeys, and DP columns of O
+  static constexpr uint32_t kPlaces = 128 / kPromptKeys;
+  static constexpr uint32_t kTmemS = 0, kTmemO = 256, kTmemCols = 512;
+  static constexpr int kThreads = 512;
+  // 128 registers per thread at launch, shared out 56 to the first two warpgroups and 200 to the others
+  static constexpr int kRegsLaunch = 128, kRegsControl = 56, kRegsSoftmax = 200;
+  static_assert(256 * kRegsControl + 256 * kRegsSoftmax <= kThreads * kRegsLaunch, "register shares");
 };
+static_assert(PromptTile<128>::kSmem <= 227 * 1024 - 1024, "shared memory");
 
-// Tiles of 128 keys that the queries [row, row + rows) of a sequence see: causal ones see the keys up to
+// Steps of kPromptKeys keys that the queries [row, row + rows) of a sequence see: causal ones see the keys up to
 // their place plus nk - nq.
-__host__ __device__ __forceinline__ uint32_t prompt_tiles(uint32_t row, uint32_t rows, uint32_t nq, uint32_t nk, bool causal) {
+__host__ __device__ __forceinline__ uint32_t prompt_steps(uint32_t row, uint32_t rows, uint32_t nq, uint32_t nk, bool causal) {
   if (row >= nq || rows == 0) return 0;
   const uint32_t last = row + rows < nq ? row + rows - 1 : nq - 1;
   long long seen = nk;
   if (causal && (long long)last + nk - nq + 1 < seen) seen = (long long)last + nk - nq + 1;
-  return seen <= 0 ? 0u : (uint32_t)((seen + 127) / 128);
+  return seen <= 0 ? 0u : (uint32_t)((seen + kPromptKeys - 1) / kPromptKeys);
 }
 // Keys that query `row` sees
 __host__ __device__ __forceinline__ uint32_t prompt_seen(uint32_t row, uint32_t nq, uint32_t nk, bool causal) {
@@ -74,6 +87,11 @@ __host__ __device__ __forceinline__ uint32_t prompt_seen(uint32_t row, uint32_t 
 __device__ __forceinline__ float max_nan(float a, float b) {   // NaN if either is
   float r;
   asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ float max3_nan(float a, float b, float c) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
 }
 // x * c - r for two numbers as one packed instruction
@@ -89,30 +107,204 @@ __device__ __forceinline__ void add_pair(float& s0, float& s1, float x0, float x
       : "f"(x0), "f"(x1));
 }
 
-// A query's output once more from global memory, by one warp, over the keys that it sees alone.
+// A whole warp waits; false if the wait ran out.
+__device__ __noinline__ bool wait_long(uint64_t* bar, uint32_t parity, volatile unsigned int* abort_flag, unsigned int* status) {
+  return mbar_wait_bounded(bar, parity, abort_flag, status);
+}
+__device__ __forceinline__ bool wait_warp(uint64_t* bar, uint32_t parity, volatile unsigned int* abort_flag, unsigned int* status) {
+  if (__all_sync(0xFFFFFFFFu, mbar_try_wait(bar, parity))) return true;
+  return __all_sync(0xFFFFFFFFu, wait_long(bar, parity, abort_flag, status));
+}
+
+// An item: what a CTA's roles have to know of it
+struct PromptItem {
+  uint32_t q0, nq, k0, nk, row0, head0;   // the sequence, the item's first query and head
+  uint32_t n[2];                          // steps of either tile
+  uint32_t steps;                         // the larger of the two
+  uint32_t live;                          // 0: no more items
+};
+// A warp's 32 queries (from `first` on) of which some, those that `ask`, are not finite although their sums are.  If a
+// value that one of them does not see is not finite (0 times it is NaN), its output once more from global memory, over the
+// keys that it sees alone.
 template <int DT>
-__device__ __noinline__ void repair_row(const PromptParams& p, uint32_t q_at, uint32_t k0, uint32_t keys, uint32_t h, float r, float by, int lane) {
-  const uint32_t hk = h / p.group;
-  const uint64_t qa = q_at * p.q_row + h * p.q_head;
-  float o[4] = {0.0f, 0.0f, 0.0f, 0.0f};   // elements lane, 32 + lane, ...
-  for (uint32_t j0 = 0; j0 < keys; j0 += 32) {
-    float s = 0.0f;
-    if (j0 + lane < keys) {
-      const uint64_t ka = (uint64_t)(k0 + j0 + lane) * p.k_row + hk * p.k_head;
-      for (uint32_t d = 0; d < p.dim; ++d) s = fmaf(load_elem<DT>(p.q, qa + d), load_elem<DT>(p.k, ka + d), s);
-    }
-    const float e = exp2_fast(fmaf(s, p.scale_log2, -r));
-    for (uint32_t j = 0; j < 32 && j0 + j < keys; ++j) {
-      const float w = __shfl_sync(0xFFFFFFFFu, e, j);
-      const uint64_t va = (uint64_t)(k0 + j0 + j) * p.v_row + hk * p.v_head;
+__device__ __forceinline__ void repair_rows(const PromptParams& p, const PromptItem& x, uint32_t first, uint32_t last, uint32_t h, bool ask,
+                                         uint32_t seen, float r, float by, int lane) {
+  const uint32_t hk = h / p.group, least = __reduce_min_sync(0xFFFFFFFFu, ask ? seen : 0xFFFFFFFFu);
+  uint32_t last_bad = 0;   // 1 + the last key with a value that is not finite, of those some row does not see
+#pragma unroll 1
+  for (uint32_t k = least; k < last; ++k) {
+    bool bad = false;
+#pragma unroll 1
+    for (uint32_t d = lane; d < p.dim; d += 32)
+      bad |= !(fabsf(load_elem<DT>(p.v, (uint64_t)(x.k0 + k) * p.v_row + hk * p.v_head + d)) <= 3.402823466e38f);
+    if (__any_sync(0xFFFFFFFFu, bad)) last_bad = k + 1;
+  }
+  uint32_t todo = __ballot_sync(0xFFFFFFFFu, ask && seen < last_bad);
+  __syncwarp();            // what was stored of these rows comes before what is stored now
+  while (todo) {
+    const int src = __ffs(todo) - 1;
+    todo &= todo - 1;
+    const uint32_t keys = __shfl_sync(0xFFFFFFFFu, seen, src), token = x.q0 + first + src;
+    const float row_r = __shfl_sync(0xFFFFFFFFu, r, src), row_by = __shfl_sync(0xFFFFFFFFu, by, src);
+    const uint64_t qa = token * p.q_row + h * p.q_head;
+    float o[4] = {0.0f, 0.0f, 0.0f, 0.0f};   // elements lane, 32 + lane, ...
+#pragma unroll 1
+    for (uint32_t j0 = 0; j0 < keys; j0 += 32) {
+      float s = 0.0f;
+      if (j0 + lane < keys) {
+        const uint64_t ka = (uint64_t)(x.k0 + j0 + lane) * p.k_row + hk * p.k_head;
+#pragma unroll 1
+        for (uint32_t d = 0; d < p.dim; ++d) s = fmaf(load_elem<DT>(p.q, qa + d), load_elem<DT>(p.k, ka + d), s);
+      }
+      const float e = exp2_fast(fmaf(s, p.scale_log2, -row_r));
+#pragma unroll 1
+      for (uint32_t j = 0; j < 32 && j0 + j < keys; ++j) {
+        const float w = __shfl_sync(0xFFFFFFFFu, e, j);
+        const uint64_t va = (uint64_t)(x.k0 + j0 + j) * p.v_row + hk * p.v_head;
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (i * 32 + lane < (int)p.dim) o[i] = fmaf(w, load_elem<DT>(p.v, va + i * 32 + lane), o[i]);
+        for (int i = 0; i < 4; ++i)
+          if (i * 32 + lane < (int)p.dim) o[i] = fmaf(w, load_elem<DT>(p.v, va + i * 32 + lane), o[i]);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (i * 32 + lane < (int)p.dim) store_elem<DT>(p.out, token * p.o_row + h * p.o_head + i * 32 + lane, o[i] * row_by);
+  }
+}
+
+// Which item has number `it`: a warp's answer.  Up to 32 sequences: the items with the most keys come first, whatever
+// their sequence, so that no CTA begins a long one when the others are about to end.  Piece j of a sequence (128 or 256
+// queries) is on level base + j of the number of keys (causal), all pieces of it on level base (not causal); the
+// level of item `it` is the largest that has more than `it` items on it or above.  More sequences: one after the
+// other, the later pieces of each first.
+struct PromptSequences {
+  uint32_t shift;                 // pieces have 1 << shift queries
+  bool causal, held;              // held: all sequences, one per lane
+  uint32_t q0, nq, k0, nk;        // of sequence at + lane
+  uint32_t total, top;            // pieces of all; no level is above
+  uint32_t at, before;            // not held: where the search goes on, pieces before that
+  __device__ __forceinline__ uint32_t pieces() const { return (nq + (1u << shift) - 1) >> shift; }
+  __device__ __forceinline__ uint32_t base() const { return causal ? (nk > nq ? (nk - nq) >> shift : 0u) : nk >> shift; }
+  __device__ __forceinline__ uint32_t on_or_above(uint32_t level) const {
+    if (!causal) return base() >= level ? pieces() : 0u;
+    const uint32_t end = base() + pieces();
+    return end <= level ? 0u : min(pieces(), end - level);
+  }
+};
+__device__ __forceinline__ uint32_t warp_prefix(uint32_t v, int lane) {   // sum up to and with this lane
+#pragma unroll
+  for (int o = 1; o < 32; o *= 2) {
+    const uint32_t up = __shfl_up_sync(0xFFFFFFFFu, v, o);
+    if (lane >= o) v += up;
+  }
+  return v;
+}
+__device__ __forceinline__ void prompt_load(const PromptParams& p, PromptSequences& q, uint32_t s, bool& bad) {
+  q.q0 = q.nq = q.k0 = q.nk = 0;
+  if (s >= p.sequences) return;
+  if (!p.q_offsets) {
+    q.nq = p.q_tokens;
+    q.nk = p.k_tokens;
+    return;
+  }
+  const int a = p.q_offsets[s], b = p.q_offsets[s + 1], c = p.k_offsets[s], d = p.k_offsets[s + 1];
+  if (a < 0 || a > b || (uint32_t)b > p.q_tokens || c < 0 || c > d || (uint32_t)d > p.k_tokens) {
+    bad = true;
+    return;
+  }
+  q.q0 = a;
+  q.nq = b - a;
+  q.k0 = c;
+  q.nk = d - c;
+}
+__device__ __forceinline__ void prompt_begin(const PromptParams& p, PromptSequences& q, int lane, bool report) {
+  q.shift = p.pair ? 7 : 8;
+  q.causal = p.causal;
+  q.held = p.sequences <= 32;
+  q.total = q.at = q.before = 0;
+  bool bad = false;
+#pragma unroll 1
+  for (uint32_t s0 = 0; s0 < p.sequences; s0 += 32) {
+    prompt_load(p, q, s0 + lane, bad);
+    q.total += __reduce_add_sync(0xFFFFFFFFu, q.pieces());
+  }
+  q.top = __reduce_max_sync(0xFFFFFFFFu, q.base() + q.pieces());
+  if (!q.held) prompt_load(p, q, lane, bad);
+  if (bad && report) set_status(p.status, (unsigned int)KB_ERR_INVALID_ARG);
+}
+// The sequence and first query of item `it` < total
+__device__ __forceinline__ void prompt_find(const PromptParams& p, PromptSequences& q, uint32_t it, int lane, PromptItem& x) {
+  // items before those of this round, and lane's among them, of which it leaves out the last `over` pieces
+  uint32_t before = 0, mine, over = 0;
+  if (q.held) {
+    uint32_t lo = 0, hi = q.top;   // more than `it` items on or above lo, not so many on or above hi
+#pragma unroll 1
+    while (hi - lo > 1) {
+      const uint32_t mid = (lo + hi) / 2;
+      if (__reduce_add_sync(0xFFFFFFFFu, q.on_or_above(mid)) > it)
+        lo = mid;
+      else
+        hi = mid;
+    }
+    over = q.on_or_above(lo + 1);
+    before = __reduce_add_sync(0xFFFFFFFFu, over);
+    mine = q.on_or_above(lo) - over;
+  } else {
+#pragma unroll 1
+    for (;;) {
+      mine = q.pieces();
+      const uint32_t all = __reduce_add_sync(0xFFFFFFFFu, mine);
+      before = q.before;
+      if (it < before + all || q.at + 32 >= p.sequences) break;
+      q.before += all;
+      q.at += 32;
+      bool bad = false;
+      prompt_load(p, q, q.at + lane, bad);
     }
   }
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    if (i * 32 + lane < (int)p.dim) store_elem<DT>(p.out, q_at * p.o_row + h * p.o_head + i * 32 + lane, o[i] * by);
+  const uint32_t first = before + warp_prefix(mine, lane) - mine;
+  const int src = max(0, __ffs(__ballot_sync(0xFFFFFFFFu, it >= first && it < first + mine)) - 1);
+  x.row0 = __shfl_sync(0xFFFFFFFFu, q.pieces() - 1 - over - (it - first), src) << q.shift;
+  x.q0 = __shfl_sync(0xFFFFFFFFu, q.q0, src);
+  x.nq = __shfl_sync(0xFFFFFFFFu, q.nq, src);
+  x.k0 = __shfl_sync(0xFFFFFFFFu, q.k0, src);
+  x.nk = __shfl_sync(0xFFFFFFFFu, q.nk, src);
+}
+
+// A warp hands out the CTA's items.  A function of its own: inlined, it took 60 KB of the kernel's instructions, which
+// did not fit their cache any more.
+__device__ __noinline__ void hand_out_items(const PromptParams& p, PromptSequences q, uint32_t units, int lane, PromptItem* items, uint64_t* item_full,
+                                            uint64_t* item_empty, uint64_t* want, volatile unsigned int* abort_flag) {
+  const uint32_t total = q.total * units;
+  uint32_t number = blockIdx.x;
+#pragma unroll 1
+  for (uint32_t taken = 0;;) {
+    const uint32_t slot = taken & 1;
+    PromptItem x = {};
+    if (number < total) {
+      prompt_find(p, q, number / units, lane, x);
+      x.head0 = number % units * (p.pair ? 2 : 1);
+      x.n[0] = prompt_steps(x.row0, 128, x.nq, x.nk, p.causal);
+      x.n[1] = p.pair ? x.n[0] : prompt_steps(x.row0 + 128, 128, x.nq, x.nk, p.causal);
+      x.steps = max(x.n[0], x.n[1]);
+      x.live = 1;
+    }
+    if (!wait_warp(&item_empty[slot], ((taken >> 1) & 1u) ^ 1u, abort_flag, p.status)) break;
+    if (lane == 0) items[slot] = x;
+    __syncwarp();
+    mbar_arrive_if(&item_full[slot], lane == 0);
+    ++taken;
+    // towards the end the next one is taken when the last copy of this one is under way, not before: others may be free earlier
+    if (!x.live) break;
+    if (number + 2 * gridDim.x >= total && !wait_warp(want, (taken - 1) & 1u, abort_flag, p.status)) break;
+    if (lane == 0) number = gridDim.x + atomicAdd(p.next, 1u);
+    number = __shfl_sync(0xFFFFFFFFu, number, 0);
+  }
+  // the last CTA leaves the counts as the next call expects them
+  if (lane == 0 && atomicAdd(p.next + 1, 1u) == gridDim.x - 1) {
+    p.next[0] = 0u;
+    p.next[1] = 0u;
+  }
 }
 
 template <int DT, int DP>
@@ -120,348 +312,331 @@ __global__ void __launch_bounds__(PromptTile<DP>::kThreads, 1)
     attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                      const __grid_constant__ CUtensorMap map_v, const PromptParams p) {
   using T = PromptTile<DP>;
+  constexpr uint32_t kS = T::kStages, kP = T::kPlaces;
   extern __shared__ unsigned char dyn[];
-  __shared__ uint64_t q_full[2], full[T::kStages], empty[T::kStages], s_full[2], p_full[2], o_full[2], drained;
-  __shared__ uint32_t tmem_base, scan[12], found[5];
+  __shared__ uint64_t q_full[2], q_empty[2], k_full[kS], k_empty[kS], v_full[kS], v_empty[kS], v_tail[kS];
+  __shared__ uint64_t s_full[2][kP], p_full[2][kP], o_full[2][kP], item_full[2], item_empty[2], want, drained[5];
+  __shared__ PromptItem items[2];
+  __shared__ uint32_t tmem_base;
   __shared__ unsigned int abort_word;
   volatile unsigned int* abort_flag = &abort_word;
   unsigned char* base = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(dyn) + 1023) & ~(uintptr_t)1023);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-
-  // Which item: the queries [row, row + rows_per) of a sequence.  Later pieces of a sequence, which see more keys, come first.
-  const uint32_t units = p.pair ? p.hq / 2 : p.hq;
-  const uint32_t item = blockIdx.x / units, unit = blockIdx.x % units;
-  const uint32_t rows_per = p.pair ? 128 : 256;
-  if (threadIdx.x == 0) found[4] = 0;
-  uint32_t before = 0;
-  bool here = false;
-  for (uint32_t s0 = 0; s0 < p.sequences && !here; s0 += T::kThreads) {
-    const uint32_t s = s0 + threadIdx.x;
-    uint32_t qa = 0, nq = 0, ka = 0, nk = 0;
-    if (s < p.sequences) {
-      if (p.q_offsets) {
-        const int a = p.q_offsets[s], b = p.q_offsets[s + 1], c = p.k_offsets[s], d = p.k_offsets[s + 1];
-        if (a >= 0 && a <= b && (uint32_t)b <= p.q_tokens && c >= 0 && c <= d && (uint32_t)d <= p.k_tokens) {
-          qa = a;
-          nq = b - a;
-          ka = c;
-          nk = d - c;
-        } else if (blockIdx.x == 0) {
-          set_status(p.status, (unsigned int)KB_ERR_INVALID_ARG);
-        }
-      } else {
-        nq = p.q_tokens;
-        nk = p.k_tokens;
+  if (threadIdx.x == 0) {
+    prefetch_map(&map_q);
+    prefetch_map(&map_k);
+    prefetch_map(&map_v);
+    for (uint32_t i = 0; i < kS; ++i) {
+      mbar_init(&k_full[i], 1);
+      mbar_init(&k_empty[i], 2);
+      mbar_init(&v_full[i], 1);
+      mbar_init(&v_empty[i], 2);
+      mbar_init(&v_tail[i], 1);
+    }
+    for (int t = 0; t < 2; ++t) {
+      mbar_init(&q_full[t], 1);
+      mbar_init(&q_empty[t], 1);
+      mbar_init(&item_full[t], 1);
+      mbar_init(&item_empty[t], 14);   // warps 0 to 4, 6 and 8 to 15
+      for (uint32_t b = 0; b < kP; ++b) {
+        mbar_init(&s_full[t][b], 1);
+        mbar_init(&p_full[t][b], 4);
+        mbar_init(&o_full[t][b], 1);
       }
     }
-    const uint32_t mine = (nq + rows_per - 1) / rows_per;
-    uint32_t sum = mine;
-#pragma unroll
-    for (int o = 1; o < 32; o *= 2) {
-      const uint32_t up = __shfl_up_sync(0xFFFFFFFFu, sum, o);
-      if (lane >= o) sum += up;
-    }
-    __syncthreads();
-    if (lane == 31) scan[warp] = sum;
-    __syncthreads();
-    uint32_t all = 0, mine_before = before + sum - mine;
-#pragma unroll
-    for (int w = 0; w < T::kThreads / 32; ++w) {
-      if (w < warp) mine_before += scan[w];
-      all += scan[w];
-    }
-    const bool mine_here = item >= mine_before && item < mine_before + mine;
-    if (mine_here) {
-      found[0] = qa;
-      found[1] = nq;
-      found[2] = ka;
-      found[3] = nk;
-      found[4] = mine - (item - mine_before);   // 1 + the piece
-    }
-    here = __syncthreads_or(mine_here);
-    before += all;
-  }
-  __syncthreads();
-  if (found[4] == 0) return;   // fewer items than the host had to allow for
-  const uint32_t q0 = found[0], nq = found[1], k0 = found[2], nk = found[3], row0 = (found[4] - 1) * rows_per;
-  const uint32_t head0 = p.pair ? 2 * unit : unit;
-  // per tile: first query, number of key tiles
-  const uint32_t n0 = prompt_tiles(row0, 128, nq, nk, p.causal);
-  const uint32_t n1 = p.pair ? n0 : prompt_tiles(row0 + 128, 128, nq, nk, p.causal);
-  const uint32_t steps = max(n0, n1);
-
-  if (threadIdx.x == 0) {
-    for (uint32_t i = 0; i < T::kStages; ++i) {
-      mbar_init(&full[i], 1);
-      mbar_init(&empty[i], 1);
-    }
-    for (int i = 0; i < 2; ++i) {
-      mbar_init(&q_full[i], 1);
-      mbar_init(&s_full[i], 1);
-      mbar_init(&p_full[i], 4);
-      mbar_init(&o_full[i], 1);
-    }
-    mbar_init(&drained, 1);
+    mbar_init(&want, 1);
+    for (int i = 1; i < 5; ++i) mbar_init(&drained[i], 1);
     abort_word = 0u;
     mbar_fence_init();
   }
   if (warp == 1) tmem_alloc<1>(&tmem_base, T::kTmemCols);
+  const uint32_t units = p.pair ? p.hq / 2 : p.hq;
+  PromptSequences q;
+  if (warp == 5) prompt_begin(p, q, lane, blockIdx.x == 0);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = tmem_base;
-  unsigned char* ring = base + 2 * T::kTileBytes;
+  unsigned char *ring = base + 2 * T::kTileBytes, *ring_v = ring + kS * T::kStepBytes, *way_out = ring_v + kS * T::kStepBytes;
+  bool go = true;   // no wait has run out
+  auto wait = [&](uint64_t* bar, uint32_t parity) { return go = go && wait_warp(bar, parity & 1u, abort_flag, p.status); };
+  uint32_t taken = 0;
+  auto next_item = [&](PromptItem& x, auto how) {   // the next item, in order, for a role's warp
+    const uint32_t slot = taken & 1;
+    if (!how(&item_full[slot], taken >> 1)) return false;
+    x = items[slot];
+    __syncwarp();
+    mbar_arrive_if(&item_empty[slot], lane == 0);
+    ++taken;
+    return x.live != 0;
+  };
 
-  if (warp < 4) regs_shrink<T::kRegsControl>();
-  if (warp == 0) {
-    // the ring takes K0, V0, K1, V1, ...: the order in which the matrix instructions want them
-    const int hk = (int)(head0 / p.group);
-    uint32_t st = 0, phase = 0, issued = 0;
-    bool go = true;
-    if (steps) {
+  if (warp < 8) regs_shrink<T::kRegsControl>();
+  if (warp == 5) {
+    hand_out_items(p, q, units, lane, items, item_full, item_empty, &want, abort_flag);
+  } else if (warp == 0) {
+    uint32_t k_issued = 0, v_issued = 0, q_items[2] = {0, 0};
+    PromptItem x;
+#pragma unroll 1
+    while (next_item(x, wait)) {
+      const int hk = (int)(x.head0 / p.group);
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        if ((t ? n1 : n0) == 0) continue;
+        if (x.n[t] == 0 || !wait(&q_empty[t], q_items[t] + 1)) continue;
+        ++q_items[t];
         const uint32_t bar = smem_u32(&q_full[t]);
         expect_tx_elect(bar, T::kTileBytes);
+#pragma unroll
         for (uint32_t c = 0; c < T::kChunks; ++c)
-          tma_load_3d(smem_u32(base + t * T::kTileBytes) + c * 16384, &map_q, (int)(c * 64), (int)(q0 + row0 + (p.pair ? 0 : t * 128)),
-                      (int)(head0 + (p.pair ? t : 0)), bar);
+          tma_load_3d(smem_u32(base) + t * T::kTileBytes + c * 16384, &map_q, (int)(c * 64), (int)(x.q0 + x.row0 + (p.pair ? 0 : t * 128)),
+                      (int)(x.head0 + (p.pair ? t : 0)), bar);
       }
-    }
-    for (uint32_t i = 0; i < 2 * steps; ++i) {
-      go = __all_sync(0xFFFFFFFFu, mbar_wait_bounded(&empty[st], phase ^ 1u, abort_flag, p.status));
-      if (!go) break;
-      const uint32_t s = smem_u32(ring + st * T::kTileBytes), bar = smem_u32(&full[st]);
-      expect_tx_elect(bar, T::kTileBytes);
-      for (uint32_t c = 0; c < T::kChunks; ++c)
-        tma_load_3d(s + c * 16384, i & 1 ? &map_v : &map_k, (int)(c * 64), (int)(k0 + i / 2 * 128), hk, bar);
-      ++issued;
-      if (++st == T::kStages) {
-        st = 0;
-        phase ^= 1u;
+      auto copy = [&](const CUtensorMap* map, unsigned char* to, uint64_t* full, uint64_t* empty, uint32_t& issued, uint32_t step) {
+        const uint32_t st = issued % kS;
+        if (!wait(&empty[st], issued / kS + 1)) return;
+        const uint32_t s = smem_u32(to) + st * T::kStepBytes, bar = smem_u32(&full[st]);
+        expect_tx_elect(bar, T::kStepBytes);
+#pragma unroll
+        for (uint32_t c = 0; c < T::kChunks; ++c)
+          tma_load_3d(s + c * T::kChunkBytes, map, (int)(c * 64), (int)(x.k0 + step * kPromptKeys), hk, bar);
+        ++issued;
+      };
+      // values past the sequence's end have to be zeroed first: warp 6 hands that tile on
+      auto values = [&](uint32_t step) { copy(&map_v, ring_v, (step + 1) * kPromptKeys > x.nk ? v_tail : v_full, v_empty, v_issued, step); };
+      if (x.steps) copy(&map_k, ring, k_full, k_empty, k_issued, 0);
+#pragma unroll 1
+      for (uint32_t i = 0; i < x.steps && go; ++i) {
+        if (i + 1 < x.steps) copy(&map_k, ring, k_full, k_empty, k_issued, i + 1);
+        values(i);
       }
+      mbar_arrive_if(&want, lane == 0);
     }
     if (!go) {   // what is on its way lands before the CTA ends
-      drain_copies(full, T::kStages, issued);
-      for (int t = 0; t < 2; ++t)
-        if (t ? n1 : n0) drain_copies(&q_full[t], 1, 1);
+      drain_copies(k_full, kS, k_issued);
+      drain_copies(v_full, kS, v_issued);
+      for (int t = 0; t < 2; ++t) drain_copies(&q_full[t], 1, q_items[t]);
       __syncwarp();
     }
-  } else if (warp == 1 && steps) {
-    const uint32_t idesc_s = mma_idesc_f16(DT == KB_BF16, false, 128, 128), idesc_o = mma_idesc_f16(DT == KB_BF16, true, 128, DP);
-    uint32_t st = 0, phase = 0;
-    bool go = true;
-    auto wait = [&](uint64_t* bar, uint32_t parity) {
-      if (go) go = __all_sync(0xFFFFFFFFu, mbar_wait_bounded(bar, parity, abort_flag, p.status));
-      tc_fence_after();
-    };
-    auto scores = [&](int t, uint32_t stage) {
-      const uint32_t a = smem_u32(base + t * T::kTileBytes), b = smem_u32(ring + stage * T::kTileBytes);
-      for (uint32_t c = 0; c < T::kChunks; ++c)
-        mma_f16_block(tmem + T::kTmemS + t * 128, smem_desc_k128(a + c * 16384), smem_desc_k128(b + c * 16384), idesc_s, c > 0);
-      mma_commit(&s_full[t]);
-    };
-    auto next = [&]() {
-      if (++st == T::kStages) {
-        st = 0;
-        phase ^= 1u;
+  } else if (warp == 6) {
+    // values behind a sequence's end are another's, or anything: zeros
+    uint32_t v_used = 0, phases = 0;
+    PromptItem x;
+#pragma unroll 1
+    while (next_item(x, wait)) {
+      v_used += x.steps;
+      if (x.steps * kPromptKeys <= x.nk) continue;
+      const uint32_t st = (v_used - 1) % kS, gone = x.steps * kPromptKeys - x.nk, rest = kPromptKeys - gone;
+      if (!wait(&v_tail[st], phases >> st)) continue;
+      phases ^= 1u << st;
+#pragma unroll 1
+      for (uint32_t k = lane; k < gone * 8 * T::kChunks; k += 32) {
+        const uint32_t row = rest + (k >> 3) % gone, c = (k >> 3) / gone;
+        *reinterpret_cast<uint4*>(ring_v + st * T::kStepBytes + c * T::kChunkBytes + row * 128 + (k & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
       }
-    };
-    wait(&full[st], phase);
-    for (int t = 0; t < 2; ++t) {
-      if ((t ? n1 : n0) == 0) continue;
-      wait(&q_full[t], 0);
-      if (go) scores(t, st);
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      __syncwarp();
+      mbar_arrive_if(&v_full[st], lane == 0);
     }
-    if (go) mma_commit(&empty[st]);
-    next();
-    for (uint32_t j = 0; j < steps && go; ++j) {
-      const uint32_t vst = st;
-      wait(&full[vst], phase);
-      if (!go) break;
-      const uint32_t rest = nk - j * 128;
-      if (rest < 128) {   // values behind the sequence's end: another's, or anything
-        for (uint32_t i = lane; i < (128 - rest) * 8 * T::kChunks; i += 32) {
-          const uint32_t unit16 = i & 7, row = rest + (i >> 3) % (128 - rest), c = (i >> 3) / (128 - rest);
-          *reinterpret_cast<uint4*>(ring + vst * T::kTileBytes + c * 16384 + row * 128 + unit16 * 16) = make_uint4(0u, 0u, 0u, 0u);
-        }
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        __syncwarp();
-      }
-      next();
-      const uint32_t kst = st;
-      const bool more = j + 1 < steps;
-      if (more) wait(&full[kst], phase);
-      for (int t = 0; t < 2 && go; ++t) {
-        const uint32_t n = t ? n1 : n0;
-        if (j >= n) continue;
-        wait(&p_full[t], j & 1u);
-        if (!go) break;
-        const uint32_t v = smem_u32(ring + vst * T::kTileBytes);
+  } else if (warp >= 1 && warp < 5) {
+    // Four warps issue matrix instructions, so that what one spends on its waits hides under the others' products: warps 1
+    // and 2 a tile's scores, warps 3 and 4 a tile's outputs.
+    const int t = (warp - 1) & 1;
+    uint32_t used = 0, done = 0, q_items = 0;   // tiles of the ring; steps of this tile; its items
+    PromptItem x;
+    if (warp < 3) {
+      const uint32_t idesc = mma_idesc_f16(DT == KB_BF16, false, 128, kPromptKeys);
+      const uint32_t a = smem_u32(base) + t * T::kTileBytes;
+  #pragma unroll 1
+    while (next_item(x, wait)) {
+        const uint32_t n = t ? x.n[1] : x.n[0];
+        if (n) wait(&q_full[t], q_items++);
+#pragma unroll 1
+        for (uint32_t i = 0; i < x.steps && go; ++i, ++used) {
+          const uint32_t st = used % kS, b = smem_u32(ring) + st * T::kStepBytes;
+          wait(&k_full[st], used / kS);   // of steps past the tile's, too: both tiles release K
+          if (i < n && go) {
+            const uint32_t place = done % kP;
+            if (done >= kP && !wait(&o_full[t][place], done / kP - 1)) break;   // S goes where P of kP steps ago was
+            tc_fence_after();
 #pragma unroll
-        for (uint32_t c = 0; c < 2; ++c)   // 64 keys each
-          mma_f16_block_ts(tmem + T::kTmemO + t * DP, tmem + T::kTmemS + t * 128 + c * 32, smem_desc_n128(v + c * 8192, 16384), idesc_o, j > 0 || c > 0);
-        mma_commit(&o_full[t]);
-        if (j + 1 < n) {
-          // the next scores go where P is read from: that has to be over
-          wait(&o_full[t], j & 1u);
-          if (go) scores(t, kst);
+            for (uint32_t c = 0; c < T::kChunks; ++c)
+              mma_f16_block(tmem + T::kTmemS + t * 128 + place * kPromptKeys, smem_desc_k128(a + c * 16384), smem_desc_k128(b + c * T::kChunkBytes),
+                            idesc, c > 0);
+            mma_commit(&s_full[t][place]);
+            if (i + 1 == n) mma_commit(&q_empty[t]);
+            ++done;
+          }
+          if (go) mma_commit(&k_empty[st]);
         }
       }
-      if (!go) break;
-      mma_commit(&empty[vst]);
-      if (more) {
-        mma_commit(&empty[kst]);
-        next();
+    } else {
+      const uint32_t idesc = mma_idesc_f16(DT == KB_BF16, true, 128, DP);
+  #pragma unroll 1
+    while (next_item(x, wait)) {
+        const uint32_t n = t ? x.n[1] : x.n[0];
+#pragma unroll 1
+        for (uint32_t i = 0; i < x.steps && go; ++i, ++used) {
+          const uint32_t st = used % kS, v = smem_u32(ring_v) + st * T::kStepBytes;
+          wait(&v_full[st], used / kS);
+          if (i < n && go) {
+            const uint32_t place = done % kP;
+            if (!wait(&p_full[t][place], done / kP)) break;
+            tc_fence_after();
+#pragma unroll
+            for (uint32_t c = 0; c < kPromptKeys / 64; ++c)
+              mma_f16_block_ts(tmem + T::kTmemO + t * DP, tmem + T::kTmemS + t * 128 + place * kPromptKeys + c * 32,
+                               smem_desc_n128(v + c * 8192, T::kChunkBytes), idesc, i > 0 || c > 0);
+            mma_commit(&o_full[t][place]);
+            ++done;
+          }
+          if (go) mma_commit(&v_empty[st]);
+        }
       }
     }
     if (!go) {   // what has been issued ends before tensor memory is freed
-      mma_commit(&drained);
+      mma_commit(&drained[warp]);
       const unsigned long long t0 = global_ns();
-      while (!mbar_try_wait(&drained, 0))
+      while (!mbar_try_wait(&drained[warp], 0))
         if (global_ns() - t0 > 1000000000ull) break;
       __syncwarp();
     }
-  } else if (warp >= 4) {
+  } else if (warp >= 8) {
     regs_grow<T::kRegsSoftmax>();
-    const int t = (warp - 4) >> 2, quarter = warp & 3;
-    const uint32_t n = t ? n1 : n0, row = row0 + (p.pair ? 0 : t * 128) + quarter * 32 + lane, h = head0 + (p.pair ? t : 0);
+    const int t = (warp - 8) >> 2, quarter = warp & 3;
     const uint32_t at_s = tmem + T::kTmemS + t * 128 + ((uint32_t)(quarter * 32) << 16);
     const uint32_t at_o = tmem + T::kTmemO + t * DP + ((uint32_t)(quarter * 32) << 16);
-    const uint32_t seen = row < nq ? prompt_seen(row, nq, nk, p.causal) : 0;
-    const uint32_t seen_by_all = __reduce_min_sync(0xFFFFFFFFu, seen);
+    unsigned char* rows = way_out + (warp - 8) * T::kOutBytes;
     const float c = p.scale_log2;
-    float r = -INFINITY, l0 = 0.0f, l1 = 0.0f;
-    // after a wait has run out every later one returns at once: the loop runs to its end, because reads of
-    // tensor memory are collective
-    bool ok = true;
-    for (uint32_t j = 0; j < n; ++j) {
-      ok &= mbar_wait_bounded(&s_full[t], j & 1u, abort_flag, p.status);
-      __syncwarp();
-      tc_fence_after();
-      float s[4][32];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) tmem_ld32(at_s + i * 32, s[i]);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) tmem_wait_ld(s[i]);
-      if (j * 128 + 128 > seen_by_all) {
-        const int left = (int)seen - (int)(j * 128);   // keys of this tile that the query sees
-#pragma unroll
-        for (int i = 0; i < 128; ++i) s[i / 32][i % 32] = i < left ? s[i / 32][i % 32] : -INFINITY;
-      }
-      float m[4] = {s[0][0], s[0][1], s[0][2], s[0][3]};
-#pragma unroll
-      for (int i = 4; i < 128; ++i) m[i % 4] = max_nan(m[i % 4], s[i / 32][i % 32]);
-      const float top = max_nan(max_nan(m[0], m[1]), max_nan(m[2], m[3])) * c;   // scale > 0; NaN stays
-      if (__any_sync(0xFFFFFFFFu, top - kRoom > r + kLazy)) {
-        const float raised = fmaxf(r, top - kRoom), f = r == -INFINITY ? 0.0f : exp2_fast(r - raised);
-        r = raised;
-        l0 *= f;
-        l1 *= f;
-        if (j > 0) {
-          ok &= mbar_wait_bounded(&o_full[t], (j - 1) & 1u, abort_flag, p.status);
-          __syncwarp();
-          tc_fence_after();
+    // no call between reads of tensor memory and their use: everything is in registers there
+    auto wait_here = [&](uint64_t* bar, uint32_t parity) {
+      return go = __all_sync(0xFFFFFFFFu, mbar_wait_bounded(bar, parity & 1u, abort_flag, p.status));
+    };
+    uint32_t done = 0;
+    PromptItem x;
 #pragma unroll 1
-          for (int i = 0; i < DP; i += 32) {
-            float o[32];
-            tmem_ld32(at_o + i, o);
-            tmem_wait_ld(o);
+    while (next_item(x, wait_here)) {
+      const uint32_t n = t ? x.n[1] : x.n[0], nq = x.nq, nk = x.nk;
+      const uint32_t row = x.row0 + (p.pair ? 0 : t * 128) + quarter * 32 + lane, h = x.head0 + (p.pair ? t : 0);
+      const uint32_t seen = row < nq ? prompt_seen(row, nq, nk, p.causal) : 0;
+      const uint32_t seen_by_all = __reduce_min_sync(0xFFFFFFFFu, seen);
+      float r = -INFINITY, l0 = 0.0f, l1 = 0.0f;
+#pragma unroll 1
+      for (uint32_t i = 0; i < n; ++i, ++done) {
+        const uint32_t place = done % kP, at = at_s + place * kPromptKeys;
+        if (!wait_here(&s_full[t][place], done / kP)) break;
+        tc_fence_after();
+        float s[kPromptKeys];
 #pragma unroll
-            for (int k = 0; k < 32; ++k) o[k] *= f;
-            tmem_st32(at_o + i, reinterpret_cast<const uint32_t*>(o));
+        for (uint32_t k = 0; k < kPromptKeys; k += 64) {
+          tmem_ld32(at + k, s + k);
+          tmem_ld32(at + k + 32, s + k + 32);
+        }
+#pragma unroll
+        for (uint32_t k = 0; k < kPromptKeys; k += 64) tmem_wait_ld64(s + k);
+        if ((i + 1) * kPromptKeys > seen_by_all) {
+          const int left = (int)seen - (int)(i * kPromptKeys);   // keys of this step that the query sees
+#pragma unroll
+          for (int k = 0; k < (int)kPromptKeys; ++k) s[k] = k < left ? s[k] : -INFINITY;
+        }
+        float m[4] = {s[0], s[1], s[2], s[3]};
+#pragma unroll
+        for (uint32_t k = 4; k < kPromptKeys - 4; k += 8) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) m[e] = max3_nan(m[e], s[k + 2 * e], s[k + 2 * e + 1]);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) m[e] = max_nan(m[e], s[kPromptKeys - 4 + e]);
+        const float top = max_nan(max_nan(m[0], m[1]), max_nan(m[2], m[3])) * c;   // scale > 0; NaN stays
+        if (__any_sync(0xFFFFFFFFu, !(top - kRoom <= r + kLazy))) {   // raised, or NaN
+          float raised = max_nan(r, top - kRoom);
+          raised += raised == -INFINITY ? 0.0f : raised - raised;   // +infinity becomes NaN, which all its row becomes
+          const float f = r == -INFINITY ? 0.0f : exp2_fast(r - raised);
+          r = raised;
+          l0 *= f;
+          l1 *= f;
+          if (i > 0) {
+            if (!wait_here(&o_full[t][(done - 1) % kP], (done - 1) / kP)) break;
+            tc_fence_after();
+#pragma unroll 1
+            for (int d = 0; d < DP; d += 32) {
+              float o[32];
+              tmem_ld32(at_o + d, o);
+              tmem_wait_ld(o);
+#pragma unroll
+              for (int k = 0; k < 32; ++k) o[k] *= f;
+              tmem_st32(at_o + d, reinterpret_cast<const uint32_t*>(o));
+            }
           }
         }
-      }
-      const float minus_r = -known(r);
-      uint32_t w[64];
+        const float minus_r = -known(r);
+        uint32_t w[kPromptKeys / 2];
 #pragma unroll
-      for (int i = 0; i < 128; i += 2) {
-        float &x = s[i / 32][i % 32], &y = s[i / 32][i % 32 + 1];
-        scale_pair(x, y, c, minus_r);
-        x = exp2_fast(x);
-        y = exp2_fast(y);
-        add_pair(l0, l1, x, y);
-        w[i / 2] = pack2<DT>(x, y);
-      }
-      tmem_st32(at_s, w);
-      tmem_st32(at_s + 32, w + 32);
-      tmem_wait_st();
-      tc_fence_before();
-      __syncwarp();
-      mbar_arrive_if(&p_full[t], lane == 0);
-    }
-    const float l = l0 + l1;
-    const bool none = l == 0.0f;
-    const float by = 1.0f / l;
-    if (n) {
-      ok &= mbar_wait_bounded(&o_full[t], (n - 1) & 1u, abort_flag, p.status);
-      __syncwarp();
-      tc_fence_after();
-    }
-    if (__all_sync(0xFFFFFFFFu, ok)) {
-      const bool in = row < nq;
-      if (in && p.lse) p.lse[(uint64_t)(q0 + row) * p.hq + h] = none ? -INFINITY : (r + log2f(l)) * 0.69314718055994531f;
-      // rows go through shared memory (the tile's queries are not needed any more), so that a warp's stores cover whole rows
-      constexpr int kUnits = DP / 8;   // of 16 bytes
-      unsigned char* rows = base + t * T::kTileBytes + quarter * 32 * DP * 2;
-      bool odd = false;                // an element that is not finite
+        for (uint32_t k = 0; k < kPromptKeys; k += 2) {
+          float &a = s[k], &b = s[k + 1];
+          scale_pair(a, b, c, minus_r);
+          a = exp2_fast(a);
+          b = exp2_fast(b);
+          add_pair(l0, l1, a, b);
+          w[k / 2] = pack2<DT>(a, b);
+        }
 #pragma unroll
-      for (int i = 0; i < DP; i += 32) {
+        for (uint32_t k = 0; k < kPromptKeys / 2; k += 32) tmem_st32(at + k, w + k);
+        tmem_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        mbar_arrive_if(&p_full[t][place], lane == 0);
+      }
+      if (!go) break;
+      const float l = l0 + l1, by = 1.0f / l;
+      const bool none = l == 0.0f, in = row < nq;
+      if (n) {
+        if (!wait_here(&o_full[t][(done - 1) % kP], (done - 1) / kP)) break;
+        tc_fence_after();
+      }
+      if (in && p.lse) p.lse[(uint64_t)(x.q0 + row) * p.hq + h] = none ? -INFINITY : (r + log2f(l)) * 0.69314718055994531f;
+      // 64 bytes of 32 rows at a time through shared memory, so that a warp's stores cover whole sectors.  A loop of few
+      // instructions: it runs once per item, and unrolled it took longer to fetch than to execute.
+      const uint32_t first = row - lane, mask = none ? 0u : 0xFFFFFFFFu;
+      float most = 0.0f;               // largest magnitude, or NaN
+      unsigned short* to = static_cast<unsigned short*>(p.out) + (uint64_t)(x.q0 + first + (lane >> 2)) * p.o_row + h * p.o_head + (lane & 3) * 8;
+      const int rows_left = (int)(nq - first) - (lane >> 2);
+#pragma unroll 1
+      for (int d = 0; d < (int)p.dim && first < nq; d += 32, to += 32) {
         float o[32];
+        uint32_t w[16];
         if (n) {
-          tmem_ld32(at_o + i, o);
+          tmem_ld32(at_o + d, o);
           tmem_wait_ld(o);
         }
 #pragma unroll
-        for (int k = 0; k < 32; ++k) {
-          o[k] = none ? 0.0f : o[k] * by;
-          odd |= !(fabsf(o[k]) <= 3.402823466e38f);
+        for (int k = 0; k < 32; k += 2) {
+          const float a = o[k] * by, b = o[k + 1] * by;
+          most = max3_nan(most, fabsf(a), fabsf(b));
+          w[k / 2] = pack2<DT>(a, b) & mask;
         }
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          const float* v = o + 8 * u;
-          const int at = (i / 8 + u) ^ (lane & 7);
-          *reinterpret_cast<uint4*>(rows + lane * DP * 2 + at * 16) =
-              make_uint4(pack2<DT>(v[0], v[1]), pack2<DT>(v[2], v[3]), pack2<DT>(v[4], v[5]), pack2<DT>(v[6], v[7]));
-        }
-      }
-      __syncwarp();
-      const uint32_t first = row - lane;
-      for (int i = lane; i < 32 * kUnits; i += 32) {
-        const uint32_t rr = i / kUnits, u = i % kUnits;
-        if (first + rr >= nq || u * 8 >= p.dim) continue;
-        const unsigned char* from = rows + rr * DP * 2 + ((u ^ (rr & 7)) * 16);
-        unsigned short* to = static_cast<unsigned short*>(p.out) + (uint64_t)(q0 + first + rr) * p.o_row + h * p.o_head + u * 8;
-        if (p.vec_out) {
-          *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(from);
-        } else {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) to[e] = reinterpret_cast<const unsigned short*>(from)[e];
-        }
-      }
-      // rows that are not finite although their sums are: values that they do not see?
-      const bool ask = in && odd && l > 0.0f && l <= 3.402823466e38f && seen < min(nk, n * 128);
-      if (__any_sync(0xFFFFFFFFu, ask)) {
-        const uint32_t least = __reduce_min_sync(0xFFFFFFFFu, ask ? seen : 0xFFFFFFFFu);
-        uint32_t last_bad = 0;   // 1 + the last key with a value that is not finite, of those some row does not see
-        const uint32_t hk = h / p.group;
-        for (uint32_t k = least; k < min(nk, n * 128); ++k) {
-          bool bad = false;
-          for (uint32_t d = lane; d < p.dim; d += 32)
-            bad |= !(fabsf(load_elem<DT>(p.v, (uint64_t)(k0 + k) * p.v_row + hk * p.v_head + d)) <= 3.402823466e38f);
-          if (__any_sync(0xFFFFFFFFu, bad)) last_bad = k + 1;
-        }
-        uint32_t todo = __ballot_sync(0xFFFFFFFFu, ask && seen < last_bad);
+        for (int u = 0; u < 4; ++u)
+          *reinterpret_cast<uint4*>(rows + lane * T::kOutPitch + u * 16) = make_uint4(w[4 * u], w[4 * u + 1], w[4 * u + 2], w[4 * u + 3]);
         __syncwarp();
-        while (todo) {
-          const int src = __ffs(todo) - 1;
-          todo &= todo - 1;
-          repair_row<DT>(p, q0 + first + src, k0, __shfl_sync(0xFFFFFFFFu, seen, src), h, __shfl_sync(0xFFFFFFFFu, r, src),
-                         __shfl_sync(0xFFFFFFFFu, by, src), lane);
+        if (d + (lane & 3) * 8 < (int)p.dim) {
+          const unsigned char* from = rows + (lane >> 2) * T::kOutPitch + (lane & 3) * 16;
+          if (p.vec_out) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              if (8 * k < rows_left) *reinterpret_cast<uint4*>(to + 8 * k * p.o_row) = *reinterpret_cast<const uint4*>(from + 8 * k * T::kOutPitch);
+          } else {
+#pragma unroll 1
+            for (int k = 0; k < 32; ++k)
+              if (k / 8 * 8 < rows_left) to[k / 8 * 8 * p.o_row + k % 8] = reinterpret_cast<const unsigned short*>(from + k / 8 * 8 * T::kOutPitch)[k % 8];
+          }
         }
+        __syncwarp();
       }
+      const bool odd = !(most <= 3.402823466e38f);
+      // rows that are not finite although their sums are: values that they do not see?
+      const uint32_t last = min(nk, n * kPromptKeys);
+      const bool ask = in && odd && l > 0.0f && l <= 3.402823466e38f && seen < last;
+      if (__any_sync(0xFFFFFFFFu, ask)) repair_rows<DT>(p, x, first, last, h, ask, seen, r, by, lane);
     }
   }
   tc_fence_before();
