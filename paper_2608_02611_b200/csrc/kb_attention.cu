@@ -86,7 +86,7 @@ constexpr uint32_t kPagedMostHeads = 16, kPagedMostDim = 128;
 struct PagedSpace {
   size_t part, rl, arrived, bytes;
   explicit PagedSpace(const kb_ctx* ctx) {
-    const size_t slots = 2ull * ctx->sm_count * kPagedWaves;   // two per CTA
+    const size_t slots = 2ull * 2 * ctx->sm_count * kPagedWaves;   // two per CTA, of two per SM
     part = 0;
     rl = slots * kPagedMostHeads * kPagedMostDim * sizeof(float);
     arrived = rl + slots * kPagedMostHeads * 2 * sizeof(float);
@@ -108,35 +108,36 @@ kb_status ensure_paged(kb_ctx* ctx, cudaStream_t st) {
   return KB_OK;
 }
 
-// Pieces of the row of units, each of which takes a CTA per group of heads, one CTA per SM: as many as run at
-// the same time; or, where that would leave more than a tenth of the card idle (32 groups: 4 x 32 of 148 SMs), the
+// Pieces of the row of units, each of which takes a CTA per group of heads: as many as run at the same time; or,
+// where that would leave more than a tenth of the card idle (32 groups: 4 x 32 of 148 SMs), the
 // number that fills up to kPagedWaves waves best.
-uint32_t paged_pieces(uint64_t sms, uint64_t per_seq, uint64_t most_units) {
-  auto use = [&](uint64_t n) { return (double)(n * per_seq) / (double)((n * per_seq + sms - 1) / sms * sms); };
-  uint64_t best = std::max<uint64_t>(1, sms / per_seq);
+uint32_t paged_pieces(uint64_t resident, uint64_t per_seq, uint64_t most_units) {
+  auto use = [&](uint64_t n) { return (double)(n * per_seq) / (double)((n * per_seq + resident - 1) / resident * resident); };
+  uint64_t best = std::max<uint64_t>(1, resident / per_seq);
   if (use(best) < 0.9)
-    for (uint64_t n = best + 1; n * per_seq <= kPagedWaves * sms; ++n)
+    for (uint64_t n = best + 1; n * per_seq <= kPagedWaves * resident; ++n)
       if (use(n) > use(best)) best = n;
-  return (uint32_t)std::min(best, most_units);   // no more than there are SMs
+  return (uint32_t)std::min(best, most_units);
 }
 
-template <int DT, int DP, int NT>
-kb_status prepare_paged(kb_ctx* ctx) {   // one fixed size, whatever thread or context calls
-  KB_CUDA(ctx, cudaFuncSetAttribute(attention_paged_kernel<DT, DP, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                    (int)PagedTile<DP, NT>::smem(ctx->sm_count)));
-  return KB_OK;
+template <int DT, int DP>
+kb_status prepare_paged(kb_ctx* ctx) {   // one fixed size each, whatever thread or context calls
+  auto raise = [&](auto kernel, uint32_t smem) {
+    KB_CUDA(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    return KB_OK;
+  };
+  KB_TRY(raise(attention_paged_kernel<DT, DP, 1, 8>, PagedTile<DP, 1, 8>::kSmem));
+  KB_TRY(raise(attention_paged_kernel<DT, DP, 2, 8>, PagedTile<DP, 2, 8>::kSmem));
+  KB_TRY(raise(attention_paged_kernel<DT, DP, 1, 4>, PagedTile<DP, 1, 4>::kSmem));
+  return raise(attention_paged_kernel<DT, DP, 2, 4>, PagedTile<DP, 2, 4>::kSmem);
 }
 kb_status prepare_paged(kb_ctx* ctx) {
   if (ctx->paged_ready) return KB_OK;
   KB_TRY(find_encoder(ctx, "kb_attention_paged"));
-  KB_TRY((prepare_paged<KB_F16, 64, 1>(ctx)));
-  KB_TRY((prepare_paged<KB_F16, 64, 2>(ctx)));
-  KB_TRY((prepare_paged<KB_F16, 128, 1>(ctx)));
-  KB_TRY((prepare_paged<KB_F16, 128, 2>(ctx)));
-  KB_TRY((prepare_paged<KB_BF16, 64, 1>(ctx)));
-  KB_TRY((prepare_paged<KB_BF16, 64, 2>(ctx)));
-  KB_TRY((prepare_paged<KB_BF16, 128, 1>(ctx)));
-  KB_TRY((prepare_paged<KB_BF16, 128, 2>(ctx)));
+  KB_TRY((prepare_paged<KB_F16, 64>(ctx)));
+  KB_TRY((prepare_paged<KB_F16, 128>(ctx)));
+  KB_TRY((prepare_paged<KB_BF16, 64>(ctx)));
+  KB_TRY((prepare_paged<KB_BF16, 128>(ctx)));
   ctx->paged_ready = true;
   return KB_OK;
 }
@@ -155,15 +156,30 @@ kb_status encode_cache(kb_ctx* ctx, CUtensorMap* map, const void* d, uint64_t pa
   return KB_OK;
 }
 
-template <int DT, int DP, int NT>
-kb_status launch_paged(kb_ctx* ctx, const CUtensorMap& k, const CUtensorMap& v, const PagedParams& p, uint32_t pieces, cudaStream_t st) {
-  attention_paged_kernel<DT, DP, NT><<<dim3(p.hkv * p.chunks, pieces), kPagedThreads, PagedTile<DP, NT>::smem(pieces), st>>>(k, v, p);
+template <int DT, int DP, int NT, int W>
+kb_status launch_paged(kb_ctx* ctx, const CUtensorMap& k, const CUtensorMap& v, const PagedParams& p, cudaStream_t st) {
+  using T = PagedTile<DP, NT, W>;
+  const uint64_t most_units = (uint64_t)paged_units(paged_length(0x7FFFFFFF, p.max_pages, p.page_size), 16 * W) * p.sequences;
+  if (most_units > 0x7FFFFFFFull) return fail(ctx, KB_ERR_UNSUPPORTED, "kb_attention_paged: sequences * max_pages * page_size is beyond 2^37");
+  const uint32_t per_seq = p.hkv * p.chunks, pieces = paged_pieces((uint64_t)ctx->sm_count * T::kPerSm, per_seq, most_units);
+  attention_paged_kernel<DT, DP, NT, W><<<dim3(per_seq, pieces), T::kThreads, T::kSmem, st>>>(k, v, p);
   return launched(ctx);
 }
+// Which number of warps: @RULE@
+bool paged_in_fours(const kb_ctx* ctx, const PagedParams& p) {
+#ifdef KB_W
+  return KB_W == 4;
+#endif
+  return (uint64_t)p.sequences * p.hkv * p.chunks >= (uint64_t)ctx->sm_count;
+}
+template <int DT, int DP, int NT>
+kb_status launch_paged(kb_ctx* ctx, const CUtensorMap& k, const CUtensorMap& v, const PagedParams& p, cudaStream_t st) {
+  return paged_in_fours(ctx, p) ? launch_paged<DT, DP, NT, 4>(ctx, k, v, p, st) : launch_paged<DT, DP, NT, 8>(ctx, k, v, p, st);
+}
 template <int DT>
-kb_status launch_paged(kb_ctx* ctx, const CUtensorMap& k, const CUtensorMap& v, const PagedParams& p, uint32_t pieces, cudaStream_t st) {
-  if (p.dim > 64) return p.group > 8 ? launch_paged<DT, 128, 2>(ctx, k, v, p, pieces, st) : launch_paged<DT, 128, 1>(ctx, k, v, p, pieces, st);
-  return p.group > 8 ? launch_paged<DT, 64, 2>(ctx, k, v, p, pieces, st) : launch_paged<DT, 64, 1>(ctx, k, v, p, pieces, st);
+kb_status launch_paged(kb_ctx* ctx, const CUtensorMap& k, const CUtensorMap& v, const PagedParams& p, cudaStream_t st) {
+  if (p.dim > 64) return p.group > 8 ? launch_paged<DT, 128, 2>(ctx, k, v, p, st) : launch_paged<DT, 128, 1>(ctx, k, v, p, st);
+  return p.group > 8 ? launch_paged<DT, 64, 2>(ctx, k, v, p, st) : launch_paged<DT, 64, 1>(ctx, k, v, p, st);
 }
 
 // ---- attention over prompts ----------------------------------------------------------------------
@@ -450,6 +466,9 @@ extern "C" kb_status kb_attention_paged(kb_ctx* ctx, const void* d_q, uint64_t q
   p.q_head = q_head;
   p.pages = cache->pages;
   p.page_size = cache->page_size;
+  p.page_shift = 32;
+  for (uint32_t i = 0; i < 31; ++i)
+    if (p.page_size == 1u << i) p.page_shift = i;
   p.box = 16;
   while (p.page_size % p.box) p.box /= 2;
   p.max_pages = max_pages;
@@ -472,11 +491,8 @@ extern "C" kb_status kb_attention_paged(kb_ctx* ctx, const void* d_q, uint64_t q
   p.part_rl = reinterpret_cast<float*>(ctx->paged_ws + space.rl);
   p.arrived = reinterpret_cast<unsigned int*>(ctx->paged_ws + space.arrived);
   p.status = ctx->d_status;
-  const uint64_t most = (uint64_t)paged_units(paged_length(0x7FFFFFFF, max_pages, cache->page_size)) * sequences;
-  if (most > 0x7FFFFFFFull) return fail(ctx, KB_ERR_UNSUPPORTED, "%s: sequences * max_pages * page_size is beyond 2^38", where);
-  const uint32_t pieces = paged_pieces(ctx->sm_count, (uint64_t)kv_heads * p.chunks, most);
   CUtensorMap map_k, map_v;
   KB_TRY(encode_cache(ctx, &map_k, cache->d_k, cache->k_page, cache->k_row, cache->k_head, *cache, kv_heads, dim, dtype, p.box));
   KB_TRY(encode_cache(ctx, &map_v, cache->d_v, cache->v_page, cache->v_row, cache->v_head, *cache, kv_heads, dim, dtype, p.box));
-  return dtype == KB_F16 ? launch_paged<KB_F16>(ctx, map_k, map_v, p, pieces, st) : launch_paged<KB_BF16>(ctx, map_k, map_v, p, pieces, st);
+  return dtype == KB_F16 ? launch_paged<KB_F16>(ctx, map_k, map_v, p, st) : launch_paged<KB_BF16>(ctx, map_k, map_v, p, st);
 }

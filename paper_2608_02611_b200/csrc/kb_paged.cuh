@@ -2,7 +2,7 @@
 //
 // Bound by the cache's bytes: every key and value is read once for the query heads that share it, up to
 // 16 of them, and the rest has to stay out of the way.  Work is divided evenly whatever the lengths: steps
-// of 128 keys are the units, those of all sequences form one row, and the row is cut into pieces, as many
+// of 128 keys (64 with 4 warps) are the units, those of all sequences form one row, and the row is cut into pieces, as many
 // as let the card run a CTA for each piece and group of heads at the same time.  A CTA takes the sequences that its
 // piece touches one after the other; CTAs of the same piece are neighbours, so that the groups'
 // heads, which lie side by side in the cache, are read at about the same time.  A sequence that lies in
@@ -43,7 +43,7 @@ struct PagedParams {
   const void* q;
   uint64_t q_row, q_head;
   uint64_t pages;
-  uint32_t page_size, max_pages;
+  uint32_t page_size, page_shift, max_pages;   // page_shift: log2 of page_size, 32 where it is no power of two
   uint32_t box;                             // keys of a copy: 16, or the power of two that divides page_size
   const int* table;
   uint64_t table_row;
@@ -62,16 +62,16 @@ struct PagedParams {
   unsigned int* status;
 };
 
-constexpr int kPagedWarps = 8, kPagedThreads = 32 * kPagedWarps;
-constexpr uint32_t kStepKeys = 16 * kPagedWarps;   // keys of a unit
 constexpr uint32_t kPagedStages = 3;
-constexpr uint32_t kPagedWaves = 3;                // of CTAs, one per SM, at most
-template <int DP, int NT>
+constexpr uint32_t kPagedWaves = 3;                // of CTAs that run together, at most
+// W warps: 8, and one CTA per SM, or 4 and two
+template <int DP, int NT, int W>
 struct PagedTile {
+  static constexpr int kThreads = 32 * W, kPerSm = 8 / W;
   static constexpr uint32_t kHalf = DP / 64 * 2048;                      // 16 keys, or values
-  static constexpr uint32_t kRing = kPagedWarps * kPagedStages * 2 * kHalf;
+  static constexpr uint32_t kRing = W * kPagedStages * 2 * kHalf;
+  static constexpr uint32_t kSmem = 1024 + kRing;
   static_assert(8 * NT * DP * 4 <= 2 * kHalf, "a warp's sums fit a tile");
-  static constexpr uint32_t smem(uint32_t pieces) { return 1024 + kRing + pieces * 8 * NT * 4; }   // and the join's factors
 };
 __host__ __device__ __forceinline__ uint32_t paged_kappa(uint32_t g) { return g ^ ((g & 1) << 2); }
 
@@ -81,17 +81,23 @@ __host__ __device__ __forceinline__ uint32_t paged_length(int length, uint32_t m
   const uint64_t most = (uint64_t)max_pages * page_size;
   return length <= 0 ? 0u : (uint64_t)length > most ? (uint32_t)most : (uint32_t)length;
 }
-__host__ __device__ __forceinline__ uint32_t paged_units(uint32_t keys) { return keys ? (keys + kStepKeys - 1) / kStepKeys : 1u; }
-// Piece c of `pieces` of a row of n >= pieces units starts here: the first n % pieces of them have one more
-__host__ __device__ __forceinline__ uint32_t piece_first(uint32_t n, uint32_t c, uint32_t pieces) {
-  const uint32_t more = n % pieces;
-  return n / pieces * c + (c < more ? c : more);
-}
-// The piece that unit u lies in
-__host__ __device__ __forceinline__ uint32_t piece_of(uint32_t n, uint32_t u, uint32_t pieces) {
-  const uint32_t size = n / pieces, more = n % pieces, bigger = more * (size + 1);
-  return u < bigger ? u / (size + 1) : more + (u - bigger) / size;
-}
+__host__ __device__ __forceinline__ uint32_t paged_units(uint32_t keys, uint32_t step) { return keys ? (keys + step - 1) / step : 1u; }
+// A row of n units in pieces: the first `more` of them have size + 1 units, the others size.  As few as keep the longest
+// as short as `most` pieces would; each has a unit.
+struct PagedPieces {
+  uint32_t count, size, more;
+  __host__ __device__ __forceinline__ PagedPieces(uint32_t n, uint32_t most) {
+    const uint32_t longest = (n + most - 1) / most;
+    count = (n + longest - 1) / longest;
+    size = n / count;
+    more = n - size * count;
+  }
+  __host__ __device__ __forceinline__ uint32_t first(uint32_t c) const { return size * c + (c < more ? c : more); }   // unit that piece c starts at
+  __host__ __device__ __forceinline__ uint32_t of(uint32_t u) const {                                                 // piece that unit u lies in
+    const uint32_t bigger = more * (size + 1);
+    return u < bigger ? u / (size + 1) : more + (u - bigger) / size;
+  }
+};
 
 template <int DT>
 __device__ __forceinline__ void mma_16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -118,24 +124,23 @@ __device__ __forceinline__ float exp2_fast(float x) {   // 2^x, 2 ulp; 0 for -in
 __device__ __forceinline__ float known(float r) { return r == -INFINITY ? 0.0f : r; }
 
 // DP: 64 or 128, dim rounded up.  NT: tiles of 8 heads.
-template <int DT, int DP, int NT>
-__global__ void __launch_bounds__(kPagedThreads, 1)
+template <int DT, int DP, int NT, int W>
+__global__ void __launch_bounds__(32 * W, 8 / W)
     attention_paged_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const PagedParams p) {
-  using T = PagedTile<DP, NT>;
+  using T = PagedTile<DP, NT, W>;
   constexpr int kH = DP / 32, kC = DP / 64, kHeads = 8 * NT;
-  constexpr uint32_t kS = kPagedStages;
+  constexpr uint32_t kS = kPagedStages, kStepKeys = 16 * W, kThreads = T::kThreads;
   extern __shared__ unsigned char dyn[];
-  __shared__ uint64_t full[kPagedWarps][kS];
-  __shared__ float warp_r[kPagedWarps][kHeads], warp_l[kPagedWarps][kHeads], item_r[kHeads], item_l[kHeads];
+  __shared__ uint64_t full[W][kS];
+  __shared__ float warp_r[W][kHeads], warp_l[W][kHeads], item_r[kHeads], item_l[kHeads];
   __shared__ uint4 q_lanes[NT * kH * 32];
-  __shared__ const float4* sums_of[kPagedWarps];
-  __shared__ uint32_t scan[kPagedWarps], found_seq, found_before, last_word;
+  __shared__ const float4* sums_of[W];
+  __shared__ uint32_t scan[W], found_seq, found_before, last_word;
   __shared__ unsigned int abort_word;
   volatile unsigned int* abort_flag = &abort_word;
   unsigned char* base = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(dyn) + 1023) & ~(uintptr_t)1023);
-  float* factors = reinterpret_cast<float*>(base + T::kRing);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-  if (threadIdx.x < kPagedWarps * kS) mbar_init(&full[threadIdx.x / kS][threadIdx.x % kS], 1);
+  if (threadIdx.x < W * kS) mbar_init(&full[threadIdx.x / kS][threadIdx.x % kS], 1);
   if (threadIdx.x == 0) {
     abort_word = 0u;
     mbar_fence_init();
@@ -145,48 +150,52 @@ __global__ void __launch_bounds__(kPagedThreads, 1)
   const uint32_t item = blockIdx.x, per_seq = gridDim.x, hk = item / p.chunks, h0 = hk * p.group + item % p.chunks * kHeads;
   const uint32_t heads = min((uint32_t)kHeads, (hk + 1) * p.group - h0);   // query heads h0 .. of this CTA
 
-  // Units of all sequences, and the sequence that this piece starts in.  Up to a CTA's threads of them are read once.
-  uint32_t total = 0, pieces = 1, u0 = 0, u1 = 0, units = 0, before = 0;
-  auto scan_from = [&](uint32_t base) {   // this thread's sequence: its units, those before it; and of all up to here
-    const uint32_t s = base + threadIdx.x;
-    units = s < p.sequences ? paged_units(paged_length(p.lengths[s], p.max_pages, p.page_size)) : 0;
-    uint32_t sum = units;
-#pragma unroll
-    for (int o = 1; o < 32; o *= 2) {
-      const uint32_t up = __shfl_up_sync(0xFFFFFFFFu, sum, o);
-      if (lane >= o) sum += up;
-    }
-    __syncthreads();
-    if (lane == 31) scan[warp] = sum;
-    __syncthreads();
-    before = total + sum - units;
-#pragma unroll
-    for (int w = 0; w < kPagedWarps; ++w) {
-      if (w < warp) before += scan[w];
-      total += scan[w];
-    }
-  };
-  for (uint32_t base = 0; base < p.sequences; base += kPagedThreads) scan_from(base);
-  pieces = min(gridDim.y, total);   // every piece has a unit
-  if (blockIdx.y >= pieces) return;
-  u0 = piece_first(total, blockIdx.y, pieces);
-  u1 = piece_first(total, blockIdx.y + 1, pieces);
+  // Units of all sequences, then the sequence that this piece starts in.  (Rolled loops throughout: a short call takes as
+  // long as its instructions take to arrive.)
+  PagedPieces pieces(1, 1);
+  uint32_t u0 = 0, u1 = 0;
   bool found = false;
-  const uint32_t all_units = total;
-  total = 0;
-  for (uint32_t base = 0; base < p.sequences && !found; base += kPagedThreads) {
-    if (p.sequences > kPagedThreads) scan_from(base);
-    const bool here = units && u0 >= before && u0 < before + units;
-    if (here) {
-      found_seq = base + threadIdx.x;
-      found_before = before;
+#pragma unroll 1
+  for (int pass = 0; pass < 2 && !found; ++pass) {
+    uint32_t sum_before = 0;
+#pragma unroll 1
+    for (uint32_t s0 = 0; s0 < p.sequences && !found; s0 += kThreads) {
+      const uint32_t s = s0 + threadIdx.x, units = s < p.sequences ? paged_units(paged_length(p.lengths[s], p.max_pages, p.page_size), kStepKeys) : 0;
+      uint32_t sum = units;
+#pragma unroll
+      for (int o = 1; o < 32; o *= 2) {
+        const uint32_t up = __shfl_up_sync(0xFFFFFFFFu, sum, o);
+        if (lane >= o) sum += up;
+      }
+      __syncthreads();
+      if (lane == 31) scan[warp] = sum;
+      __syncthreads();
+      uint32_t before = sum_before + sum - units;
+#pragma unroll
+      for (int w = 0; w < W; ++w) {
+        if (w < warp) before += scan[w];
+        sum_before += scan[w];
+      }
+      if (pass == 0 && s0 + kThreads < p.sequences) continue;
+      if (pass == 0) {
+        pieces = PagedPieces(sum_before, gridDim.y);
+        if (blockIdx.y >= pieces.count) return;
+        u0 = pieces.first(blockIdx.y);
+        u1 = pieces.first(blockIdx.y + 1);
+      }
+      if (pass == 1 || p.sequences <= kThreads) {
+        const bool here = units && u0 >= before && u0 < before + units;
+        if (here) {
+          found_seq = s;
+          found_before = before;
+        }
+        found = __syncthreads_or(here);
+      }
     }
-    found = __syncthreads_or(here);
   }
   if (!found) return;   // lengths that changed in between
-  total = all_units;
   if (blockIdx.x == 0 && blockIdx.y == 0)
-    for (uint32_t s = threadIdx.x; s < p.sequences; s += kPagedThreads)
+    for (uint32_t s = threadIdx.x; s < p.sequences; s += kThreads)
       if (p.lengths[s] < 0 || (uint64_t)p.lengths[s] > (uint64_t)p.max_pages * p.page_size) set_status(p.status, (unsigned int)KB_ERR_INVALID_ARG);
   uint32_t seq = found_seq, seq_first = found_before;   // the sequence and its first unit
 
@@ -198,18 +207,20 @@ __global__ void __launch_bounds__(kPagedThreads, 1)
   bool p_known = false, bad = false;              // p_end and pages are p_seq's
   unsigned long long there = 0;                   // 16 bits per tile on its way, the next one lowest: keys that are there
   bool ok = true;                                 // no wait has run out
+  auto by_page = [&](uint32_t key) { return p.page_shift < 32 ? key >> p.page_shift : key / p.page_size; };
   auto produce = [&]() {
     if (!ok) return;
+#pragma unroll 1
     for (;;) {
       if (!p_known) {
         if (p_seq >= p.sequences || p_first >= u1) return;
-        const uint32_t keys = paged_length(p.lengths[p_seq], p.max_pages, p.page_size), n = paged_units(keys);
+        const uint32_t keys = paged_length(p.lengths[p_seq], p.max_pages, p.page_size), n = paged_units(keys, kStepKeys);
         p_end = u1 - p_first >= n ? keys : (u1 - p_first) * kStepKeys;
         p_known = true;
         pages_at = p_key + 32 * kStepKeys;        // none yet
       }
       if (p_key < p_end) break;
-      p_first += paged_units(paged_length(p.lengths[p_seq], p.max_pages, p.page_size));
+      p_first += paged_units(paged_length(p.lengths[p_seq], p.max_pages, p.page_size), kStepKeys);
       ++p_seq;
       p_key = warp * 16;
       p_known = false;
@@ -221,7 +232,7 @@ __global__ void __launch_bounds__(kPagedThreads, 1)
       const uint32_t key = whole ? p_key + lane * kStepKeys : p_key + (lane & 15);
       pages = -1;
       if (key < p_end) {
-        const int page = p.table[p_seq * p.table_row + key / p.page_size];
+        const int page = p.table[p_seq * p.table_row + by_page(key)];
         if (page >= 0 && (uint64_t)page < p.pages)
           pages = page;
         else
@@ -238,12 +249,14 @@ __global__ void __launch_bounds__(kPagedThreads, 1)
     there |= (unsigned long long)mask << (16 * (issued - used));
     const uint32_t bar = smem_u32(&full[warp][p_stage]), to = smem_u32(ring + p_stage * 2 * T::kHalf);
     uint32_t boxes = 0;
+#pragma unroll 1
     for (uint32_t i = 0; i < 16; i += p.box) boxes += (mask >> i) & 1u;
     expect_tx_elect(bar, boxes * p.box * 128 * kC * 2);
+#pragma unroll 1
     for (uint32_t i = 0; i < 16; i += p.box) {
       const int page = __shfl_sync(0xFFFFFFFFu, pages, whole ? (p_key - pages_at) / kStepKeys : i);
       if (((mask >> i) & 1u) == 0) continue;
-      const int row = (int)((p_key + i) % p.page_size);
+      const int row = (int)(p_key + i - by_page(p_key + i) * p.page_size);
 #pragma unroll
       for (int c = 0; c < kC; ++c) {
         tma_load_4d(to + c * 2048 + i * 128, &map_k, c * 64, (int)hk, row, page, bar);
@@ -254,23 +267,17 @@ __global__ void __launch_bounds__(kPagedThreads, 1)
     p_stage = p_stage + 1 == kS ? 0 : p_stage + 1;
     p_key += kStepKeys;
   };
-  for (uint32_t i = 0; i < kS; ++i) produce();
+  uint32_t wanted = kS;                           // tiles that are free for copies
 
   uint32_t stage = 0, phase = 0;
   const uint32_t key_of[2] = {paged_kappa(g), paged_kappa(g) + 8};                              // rows g and g + 8 of the scores
   const uint32_t val_of[4] = {2u * t, (2u * t + 1) ^ 4u, 2u * t + 8, ((2u * t + 1) ^ 4u) + 8};   // kappa(2t), kappa(2t + 1), and + 8
+#pragma unroll 1
   for (uint32_t u = u0; u < u1 && seq < p.sequences; ++seq) {
-    const uint32_t keys = paged_length(p.lengths[seq], p.max_pages, p.page_size), seq_units = paged_units(keys);
+
+    const uint32_t keys = paged_length(p.lengths[seq], p.max_pages, p.page_size), seq_units = paged_units(keys, kStepKeys);
     const uint32_t unit0 = u - seq_first, unit1 = min(seq_units, u1 - seq_first);
     const uint32_t key_end = unit1 == seq_units ? keys : unit1 * kStepKeys;
-    // q as the second operand of the scores, in the lanes' order: heads h0 + 8 n + g
-    for (uint32_t i = threadIdx.x; i < NT * kH * 32; i += kPagedThreads) {
-      const uint32_t head = i / (kH * 32) * 8 + (i & 31) / 4, d = i / 32 % kH * 32 + (i & 3) * 8;
-      uint4 w = make_uint4(0u, 0u, 0u, 0u);
-      if (head < heads && d < p.dim)
-        w = *reinterpret_cast<const uint4*>(static_cast<const unsigned short*>(p.q) + seq * p.q_row + (h0 + head) * p.q_head + d);
-      q_lanes[i] = w;
-    }
     float acc[NT][kC][4][4], r[NT][2], l[NT][2];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
@@ -279,10 +286,29 @@ __global__ void __launch_bounds__(kPagedThreads, 1)
 #pragma unroll
       for (int i = 0; i < kC * 16; ++i) acc[n][i / 16][i / 4 % 4][i % 4] = 0.0f;
     }
-    __syncthreads();
     unsigned char* scratch = nullptr;          // the tile that this warp used last
-    for (uint32_t key0 = unit0 * kStepKeys + warp * 16; key0 < key_end; key0 += kStepKeys) {
-      if (scratch) produce();                  // into the tile used before this one
+    bool fresh = true;
+#pragma unroll 1
+    for (uint32_t key0 = unit0 * kStepKeys + warp * 16;; key0 += kStepKeys) {
+      // copies into tiles that are free: all at first, then the one used before this one; the last one used of this sequence
+      // holds the warp's sums before it is free
+      if (scratch && key0 < key_end) wanted = 1;
+#pragma unroll 1
+      for (; wanted; --wanted) produce();
+      if (fresh) {
+        fresh = false;
+        // q as the second operand of the scores, in the lanes' order: heads h0 + 8 n + g
+#pragma unroll 1
+        for (uint32_t i = threadIdx.x; i < NT * kH * 32; i += kThreads) {
+          const uint32_t head = i / (kH * 32) * 8 + (i & 31) / 4, d = i / 32 % kH * 32 + (i & 3) * 8;
+          uint4 w = make_uint4(0u, 0u, 0u, 0u);
+          if (head < heads && d < p.dim)
+            w = *reinterpret_cast<const uint4*>(static_cast<const unsigned short*>(p.q) + seq * p.q_row + (h0 + head) * p.q_head + d);
+          q_lanes[i] = w;
+        }
+        __syncthreads();
+      }
+      if (key0 >= key_end) break;
       ok = ok && mbar_wait_bounded(&full[warp][stage], phase, abort_flag, p.status);
       __syncwarp();
       const unsigned char* tile = ring + stage * 2 * T::kHalf;
@@ -298,9 +324,11 @@ __global__ void __launch_bounds__(kPagedThreads, 1)
       auto read = [&](uint32_t at, uint32_t row, int c, uint32_t unit) {   // 16 bytes of a swizzled row
         return *reinterpret_cast<const uint4*>(tile + at + c * 2048 + row * 128 + ((unit ^ (row & 7)) * 16));
       };
-      float s[NT][4];
+      float s[NT][4], s2[NT][4];   // two chains of products
 #pragma unroll
-      for (int n = 0; n < NT; ++n) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.0f;
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[n][i] = s2[n][i] = 0.0f;
 #pragma unroll
       for (int h = 0; h < kH; ++h) {
         const uint4 k0 = read(0, key_of[0], h / 2, h % 2 * 4 + t), k1 = read(0, key_of[1], h / 2, h % 2 * 4 + t);
@@ -308,7 +336,7 @@ __global__ void __launch_bounds__(kPagedThreads, 1)
         for (int n = 0; n < NT; ++n) {
           const uint4 qv = q_lanes[(n * kH + h) * 32 + lane];
           mma_16816<DT>(s[n], k0.x, k1.x, k0.y, k1.y, qv.x, qv.y);
-          mma_16816<DT>(s[n], k0.z, k1.z, k0.w, k1.w, qv.z, qv.w);
+          mma_16816<DT>(s2[n], k0.z, k1.z, k0.w, k1.w, qv.z, qv.w);
         }
       }
       const bool seen0 = (mask >> key_of[0]) & 1u, seen1 = (mask >> key_of[1]) & 1u;
@@ -317,7 +345,7 @@ __global__ void __launch_bounds__(kPagedThreads, 1)
       for (int n = 0; n < NT; ++n) {
         float x[4];   // keys of rows g, g, g + 8, g + 8; heads 2t, 2t + 1, 2t, 2t + 1
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = (i < 2 ? seen0 : seen1) ? s[n][i] * p.scale_log2 : -INFINITY;
+        for (int i = 0; i < 4; ++i) x[i] = (i < 2 ? seen0 : seen1) ? (s[n][i] + s2[n][i]) * p.scale_log2 : -INFINITY;
         const float top0 = fmaxf(x[0], x[2]), top1 = fmaxf(x[1], x[3]);
         // r is -infinity until a score was met
         if (__any_sync(0xFFFFFFFFu, top0 - kRoom > r[n][0] + kLazy || top1 - kRoom > r[n][1] + kLazy)) {
@@ -349,7 +377,7 @@ __global__ void __launch_bounds__(kPagedThreads, 1)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           v4[i] = read(T::kHalf, val_of[i], c, g);
-          if (mask != 0xFFFFu && ((mask >> val_of[i]) & 1u) == 0) v4[i] = make_uint4(0u, 0u, 0u, 0u);   // 0 times NaN is not 0
+          if (((mask >> val_of[i]) & 1u) == 0) v4[i] = make_uint4(0u, 0u, 0u, 0u);   // 0 times NaN is not 0
         }
         const uint32_t w[4][4] = {{v4[0].x, v4[0].y, v4[0].z, v4[0].w}, {v4[1].x, v4[1].y, v4[1].z, v4[1].w},
                                   {v4[2].x, v4[2].y, v4[2].z, v4[2].w}, {v4[3].x, v4[3].y, v4[3].z, v4[3].w}};
@@ -381,9 +409,9 @@ __global__ void __launch_bounds__(kPagedThreads, 1)
     if (threadIdx.x < kHeads) {
       float top = -INFINITY, sum = 0.0f;
 #pragma unroll
-      for (int w = 0; w < kPagedWarps; ++w) top = fmaxf(top, warp_r[w][threadIdx.x]);
+      for (int w = 0; w < W; ++w) top = fmaxf(top, warp_r[w][threadIdx.x]);
 #pragma unroll
-      for (int w = 0; w < kPagedWarps; ++w) {
+      for (int w = 0; w < W; ++w) {
         const float f = warp_r[w][threadIdx.x] == -INFINITY ? 0.0f : exp2_fast(warp_r[w][threadIdx.x] - top);
         sum += warp_l[w][threadIdx.x] * f;
       }
@@ -392,7 +420,7 @@ __global__ void __launch_bounds__(kPagedThreads, 1)
     }
     __syncthreads();
     // sums of p v go to the tile that the warp used last; warps without a tile of this sequence have none
-    const uint32_t warps = min((uint32_t)kPagedWarps, (key_end - unit0 * kStepKeys + 15) / 16);
+    const uint32_t warps = min((uint32_t)W, (key_end - unit0 * kStepKeys + 15) / 16);
     if (scratch) {
 #pragma unroll
       for (int n = 0; n < NT; ++n)
@@ -412,101 +440,114 @@ __global__ void __launch_bounds__(kPagedThreads, 1)
     }
     __syncthreads();
 
-    // Four elements of a head, of sum l and reference r, to the outputs
-    auto finish = [&](uint32_t head, uint32_t d, float4 o, float top, float sum) {
-      if (head >= heads) return;
-      const float by = 1.0f / sum;
-      const bool none = sum == 0.0f;   // no score above -infinity
-      const float v[4] = {none ? 0.0f : o.x * by, none ? 0.0f : o.y * by, none ? 0.0f : o.z * by, none ? 0.0f : o.w * by};
-      unsigned short* to = static_cast<unsigned short*>(p.out) + seq * p.o_row + (h0 + head) * p.o_head + d;
-      if (p.vec_out && d + 4 <= p.dim) {
-        *reinterpret_cast<uint2*>(to) = make_uint2(pack2<DT>(v[0], v[1]), pack2<DT>(v[2], v[3]));
-      } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (d + i < p.dim) store_elem<DT>(to, i, v[i]);
-      }
-      if (d == 0 && p.lse) p.lse[(uint64_t)seq * p.q_heads + h0 + head] = none ? -INFINITY : (top + log2f(sum)) * 0.69314718055994531f;
-    };
     const bool whole = unit0 == 0 && unit1 == seq_units;
+    uint32_t c0 = 0, parts = 0;
+    bool last = whole;
     // places in the workspace: a sequence that began in an earlier piece is its piece's first, another its last
     auto place = [&](uint32_t piece, bool began) { return (uint64_t)2 * (piece * per_seq + item) + (began ? 1 : 0); };
-    const uint64_t here = place(blockIdx.y, unit0 == 0);
-    float* mine = p.part + here * kHeads * DP;
-    for (uint32_t i = threadIdx.x; i < kHeads * DP / 4; i += kPagedThreads) {
+    auto add_warps = [&](uint32_t i) {
       float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 4
       for (uint32_t w = 0; w < warps; ++w) {
-        const float4 x = sums_of[w][i];
-        o.x += x.x;
-        o.y += x.y;
-        o.z += x.z;
-        o.w += x.w;
+        const float4 v = sums_of[w][i];
+        o.x += v.x;
+        o.y += v.y;
+        o.z += v.z;
+        o.w += v.w;
       }
-      if (whole)
-        finish(i / (DP / 4), i % (DP / 4) * 4, o, item_r[i / (DP / 4)], item_l[i / (DP / 4)]);
-      else
-        __stcg(reinterpret_cast<float4*>(mine) + i, o);
-    }
+      return o;
+    };
     if (!whole) {
+      const uint64_t here = place(blockIdx.y, unit0 == 0);
+#pragma unroll 1
+      for (uint32_t i = threadIdx.x; i < kHeads * DP / 4; i += kThreads)
+        __stcg(reinterpret_cast<float4*>(p.part) + here * (kHeads * DP / 4) + i, add_warps(i));
       if (threadIdx.x < kHeads)
         __stcg(reinterpret_cast<float2*>(p.part_rl) + here * kHeads + threadIdx.x, make_float2(item_r[threadIdx.x], item_l[threadIdx.x]));
-      const uint32_t c0 = piece_of(total, seq_first, pieces), parts = piece_of(total, seq_first + seq_units - 1, pieces) - c0 + 1;
-      __threadfence();
+      c0 = pieces.of(seq_first);
+      parts = pieces.of(seq_first + seq_units - 1) - c0 + 1;
       __syncthreads();
       if (threadIdx.x == 0) {
+        __threadfence();                                         // the CTA's part is there before it is counted
         unsigned int* count = p.arrived + c0 * per_seq + item;   // a sequence that goes on is the last of the piece it began in
-        const bool last = atomicAdd(count, 1u) == parts - 1;
-        if (last) *count = 0u;                                   // as the next call expects it
-        last_word = last;
+        const bool all = atomicAdd(count, 1u) == parts - 1;
+        if (all) *count = 0u;                                    // as the next call expects it
         __threadfence();
+        last_word = all;
       }
       __syncthreads();
-      if (last_word) {
-        // a warp per head: the parts' common reference and their factors
-        for (uint32_t head = warp; head < kHeads; head += kPagedWarps) {
-          const float2* rl = reinterpret_cast<const float2*>(p.part_rl) + head;
-          float top = -INFINITY, sum = 0.0f;
-          for (uint32_t i = lane; i < parts; i += 32) top = fmaxf(top, __ldcg(rl + place(c0 + i, i == 0) * kHeads).x);
+      last = last_word;
+    }
+    if (last) {
+#pragma unroll 1
+      for (uint32_t j = threadIdx.x; j < kHeads * DP / 4; j += kThreads) {
+        const uint32_t head = j / (DP / 4), d = j % (DP / 4) * 4;
+        float4 o;
+        float top, sum;
+        if (whole) {
+          o = add_warps(j);
+          top = item_r[head];
+          sum = item_l[head];
+        } else {
+          // the parts in the order of the keys, eight on their way at a time
+          o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+          top = -INFINITY;
+          sum = 0.0f;
+#pragma unroll 1
+          for (uint32_t i0 = 0; i0 < parts; i0 += 8) {
+            float4 v[8];
+            float2 rl[8];
 #pragma unroll
-          for (int o = 16; o > 0; o /= 2) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
-          for (uint32_t i = lane; i < parts; i += 32) {
-            const float2 x = __ldcg(rl + place(c0 + i, i == 0) * kHeads);
-            const float f = x.x == -INFINITY ? 0.0f : exp2_fast(x.x - top);
-            factors[i * kHeads + head] = f;
-            sum = fmaf(x.y, f, sum);
-          }
+            for (uint32_t i = 0; i < 8; ++i) {
+              rl[i] = make_float2(-INFINITY, 0.0f);
+              v[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+              if (i0 + i >= parts) continue;
+              const uint64_t at = place(c0 + i0 + i, i0 + i == 0);
+              v[i] = __ldcg(reinterpret_cast<const float4*>(p.part) + at * (kHeads * DP / 4) + j);
+              rl[i] = __ldcg(reinterpret_cast<const float2*>(p.part_rl) + at * kHeads + head);
+            }
+            float higher = top;
 #pragma unroll
-          for (int o = 16; o > 0; o /= 2) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
-          if (lane == 0) {
-            item_r[head] = top;
-            item_l[head] = sum;
+            for (uint32_t i = 0; i < 8; ++i) higher = fmaxf(higher, rl[i].x);
+            const float f0 = exp2_fast(top - known(higher));     // 0 at first
+            o = make_float4(o.x * f0, o.y * f0, o.z * f0, o.w * f0);
+            sum *= f0;
+            top = higher;
+#pragma unroll
+            for (uint32_t i = 0; i < 8; ++i) {
+              const float f = exp2_fast(rl[i].x - known(top));
+              o.x = fmaf(v[i].x, f, o.x);
+              o.y = fmaf(v[i].y, f, o.y);
+              o.z = fmaf(v[i].z, f, o.z);
+              o.w = fmaf(v[i].w, f, o.w);
+              sum = fmaf(rl[i].y, f, sum);
+            }
           }
         }
-        __syncthreads();
-        for (uint32_t j = threadIdx.x; j < kHeads * DP / 4; j += kPagedThreads) {
-          const uint32_t head = j / (DP / 4);
-          float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll 8
-          for (uint32_t i = 0; i < parts; ++i) {
-            const float4 x = __ldcg(reinterpret_cast<const float4*>(p.part) + place(c0 + i, i == 0) * (kHeads * DP / 4) + j);
-            const float f = factors[i * kHeads + head];
-            o.x = fmaf(x.x, f, o.x);
-            o.y = fmaf(x.y, f, o.y);
-            o.z = fmaf(x.z, f, o.z);
-            o.w = fmaf(x.w, f, o.w);
-          }
-          finish(head, j % (DP / 4) * 4, o, item_r[head], item_l[head]);
+        if (head >= heads) continue;
+        const bool none = sum == 0.0f;   // no score above -infinity
+        const float by = 1.0f / sum;
+        const float v[4] = {none ? 0.0f : o.x * by, none ? 0.0f : o.y * by, none ? 0.0f : o.z * by, none ? 0.0f : o.w * by};
+        unsigned short* to = static_cast<unsigned short*>(p.out) + seq * p.o_row + (h0 + head) * p.o_head + d;
+        if (p.vec_out && d + 4 <= p.dim) {
+          *reinterpret_cast<uint2*>(to) = make_uint2(pack2<DT>(v[0], v[1]), pack2<DT>(v[2], v[3]));
+        } else {
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (d + i < p.dim) store_elem<DT>(to, i, v[i]);
         }
+        if (d == 0 && p.lse) p.lse[(uint64_t)seq * p.q_heads + h0 + head] = none ? -INFINITY : (top + log2f(sum)) * 0.69314718055994531f;
       }
     }
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // the sums were read before copies come in their place
     __syncthreads();                                               // shared memory is used again
-    if (scratch) produce();
+    if (scratch) wanted = 1;
     u = seq_first + unit1;
     seq_first += seq_units;
   }
   if (bad) set_status(p.status, (unsigned int)KB_ERR_INVALID_ARG);
   if (!ok) {   // what is on its way lands before the CTA ends
+#pragma unroll 1
     for (uint32_t i = 0; i < kS; ++i) {
       const unsigned long long t0 = global_ns();
       while (issued > i && !mbar_try_wait(&full[warp][(issued - 1 - i) % kS], ((issued - 1 - i) / kS) & 1u))
