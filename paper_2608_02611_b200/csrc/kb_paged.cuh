@@ -132,10 +132,10 @@ __global__ void __launch_bounds__(32 * W, 8 / W)
   constexpr uint32_t kS = kPagedStages, kStepKeys = 16 * W, kThreads = T::kThreads;
   extern __shared__ unsigned char dyn[];
   __shared__ uint64_t full[W][kS];
-  __shared__ float warp_r[W][kHeads], warp_l[W][kHeads], item_r[kHeads], item_l[kHeads];
-  __shared__ uint4 q_lanes[NT * kH * 32];
+  __shared__ float warp_r[W][kHeads], warp_l[W][kHeads];
+  __shared__ uint4 q_lanes[2][NT * kH * 32];   // of this sequence and of the next one
   __shared__ const float4* sums_of[W];
-  __shared__ uint32_t scan[W], found_seq, found_before, last_word;
+  __shared__ uint32_t scan[W], found_seq, found_before, join_word[2];
   __shared__ unsigned int abort_word;
   volatile unsigned int* abort_flag = &abort_word;
   unsigned char* base = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(dyn) + 1023) & ~(uintptr_t)1023);
@@ -268,6 +268,44 @@ __global__ void __launch_bounds__(32 * W, 8 / W)
     p_key += kStepKeys;
   };
   uint32_t wanted = kS;                           // tiles that are free for copies
+  // q as the second operand of the scores, in the lanes' order: heads h0 + 8 n + g
+  constexpr uint32_t kQ = NT * kH * 32, kQEach = (kQ + kThreads - 1) / kThreads;
+  uint4 q_next[kQEach];
+  auto load_q = [&](uint32_t of) {
+#pragma unroll
+    for (uint32_t e = 0; e < kQEach; ++e) {
+      const uint32_t i = e * kThreads + threadIdx.x, head = i / (kH * 32) * 8 + (i & 31) / 4, d = i / 32 % kH * 32 + (i & 3) * 8;
+      q_next[e] = make_uint4(0u, 0u, 0u, 0u);
+      if (i < kQ && head < heads && d < p.dim)
+        q_next[e] = *reinterpret_cast<const uint4*>(static_cast<const unsigned short*>(p.q) + of * p.q_row + (h0 + head) * p.q_head + d);
+    }
+  };
+  auto store_q = [&](uint32_t to) {
+#pragma unroll
+    for (uint32_t e = 0; e < kQEach; ++e)
+      if (e * kThreads + threadIdx.x < kQ) q_lanes[to][e * kThreads + threadIdx.x] = q_next[e];
+  };
+  uint32_t q_at = 0;
+  // Sequences that this piece has a part of, the one that began earlier and the one that goes on: first unit, units
+  uint32_t part_first[2] = {0, 0}, part_units[2] = {0, 0}, part_seq[2] = {0, 0};
+  // places in the workspace: a sequence that began in an earlier piece is its piece's first, another its last
+  auto place = [&](uint32_t piece, bool began) { return (uint64_t)2 * (piece * per_seq + item) + (began ? 1 : 0); };
+  // Four elements d .. of a head's output: o / sum, and its lse
+  auto finish = [&](uint32_t of, uint32_t head, uint32_t d, float4 o, float top, float sum) {
+    if (head >= heads) return;
+    const bool none = sum == 0.0f;   // no score above -infinity
+    const float by = 1.0f / sum;
+    const float v[4] = {none ? 0.0f : o.x * by, none ? 0.0f : o.y * by, none ? 0.0f : o.z * by, none ? 0.0f : o.w * by};
+    unsigned short* to = static_cast<unsigned short*>(p.out) + of * p.o_row + (h0 + head) * p.o_head + d;
+    if (p.vec_out && d + 4 <= p.dim) {
+      *reinterpret_cast<uint2*>(to) = make_uint2(pack2<DT>(v[0], v[1]), pack2<DT>(v[2], v[3]));
+    } else {
+#pragma unroll 1
+      for (int i = 0; i < 4; ++i)
+        if (d + i < p.dim) store_elem<DT>(to, i, i < 2 ? (i ? v[1] : v[0]) : (i == 2 ? v[2] : v[3]));
+    }
+    if (d == 0 && p.lse) p.lse[(uint64_t)of * p.q_heads + h0 + head] = none ? -INFINITY : (top + log2f(sum)) * 0.69314718055994531f;
+  };
 
   uint32_t stage = 0, phase = 0;
   const uint32_t key_of[2] = {paged_kappa(g), paged_kappa(g) + 8};                              // rows g and g + 8 of the scores
@@ -297,16 +335,12 @@ __global__ void __launch_bounds__(32 * W, 8 / W)
       for (; wanted; --wanted) produce();
       if (fresh) {
         fresh = false;
-        // q as the second operand of the scores, in the lanes' order: heads h0 + 8 n + g
-#pragma unroll 1
-        for (uint32_t i = threadIdx.x; i < NT * kH * 32; i += kThreads) {
-          const uint32_t head = i / (kH * 32) * 8 + (i & 31) / 4, d = i / 32 % kH * 32 + (i & 3) * 8;
-          uint4 w = make_uint4(0u, 0u, 0u, 0u);
-          if (head < heads && d < p.dim)
-            w = *reinterpret_cast<const uint4*>(static_cast<const unsigned short*>(p.q) + seq * p.q_row + (h0 + head) * p.q_head + d);
-          q_lanes[i] = w;
+        if (u == u0) {   // later sequences' were loaded while the one before was worked on
+          load_q(seq);
+          store_q(0);
+          __syncthreads();
         }
-        __syncthreads();
+        if (seq_first + seq_units < u1 && seq + 1 < p.sequences) load_q(seq + 1);
       }
       if (key0 >= key_end) break;
       ok = ok && mbar_wait_bounded(&full[warp][stage], phase, abort_flag, p.status);
@@ -334,7 +368,7 @@ __global__ void __launch_bounds__(32 * W, 8 / W)
         const uint4 k0 = read(0, key_of[0], h / 2, h % 2 * 4 + t), k1 = read(0, key_of[1], h / 2, h % 2 * 4 + t);
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-          const uint4 qv = q_lanes[(n * kH + h) * 32 + lane];
+          const uint4 qv = q_lanes[q_at][(n * kH + h) * 32 + lane];
           mma_16816<DT>(s[n], k0.x, k1.x, k0.y, k1.y, qv.x, qv.y);
           mma_16816<DT>(s2[n], k0.z, k1.z, k0.w, k1.w, qv.z, qv.w);
         }
@@ -393,157 +427,134 @@ __global__ void __launch_bounds__(32 * W, 8 / W)
       __syncwarp();   // the tile is read
     }
 
-    // The warps' parts: one reference for all, sums of p over the lanes, sums of p v over the warps
-#pragma unroll
-    for (int n = 0; n < NT; ++n)
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-#pragma unroll
-        for (int o = 4; o < 32; o *= 2) l[n][i] += __shfl_xor_sync(0xFFFFFFFFu, l[n][i], o);
-        if (g == 0) {
-          warp_r[warp][8 * n + 2 * t + i] = r[n][i];
-          warp_l[warp][8 * n + 2 * t + i] = l[n][i];
-        }
-      }
-    __syncthreads();
-    if (threadIdx.x < kHeads) {
-      float top = -INFINITY, sum = 0.0f;
-#pragma unroll
-      for (int w = 0; w < W; ++w) top = fmaxf(top, warp_r[w][threadIdx.x]);
-#pragma unroll
-      for (int w = 0; w < W; ++w) {
-        const float f = warp_r[w][threadIdx.x] == -INFINITY ? 0.0f : exp2_fast(warp_r[w][threadIdx.x] - top);
-        sum += warp_l[w][threadIdx.x] * f;
-      }
-      item_r[threadIdx.x] = top;
-      item_l[threadIdx.x] = sum;
-    }
-    __syncthreads();
-    // sums of p v go to the tile that the warp used last; warps without a tile of this sequence have none
+    // The warps' sums meet in shared memory, those of p v in the tile that the warp used last; warps without a tile of this
+    // sequence have none.
     const uint32_t warps = min((uint32_t)W, (key_end - unit0 * kStepKeys + 15) / 16);
+    const bool whole = unit0 == 0 && unit1 == seq_units;
     if (scratch) {
 #pragma unroll
       for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           const uint32_t head = 8 * n + 2 * t + i;
-          const float f = r[n][i] == -INFINITY ? 0.0f : exp2_fast(r[n][i] - item_r[head]);
+#pragma unroll
+          for (int o = 4; o < 32; o *= 2) l[n][i] += __shfl_xor_sync(0xFFFFFFFFu, l[n][i], o);
+          if (g == 0) {
+            warp_r[warp][head] = r[n][i];
+            warp_l[warp][head] = l[n][i];
+          }
 #pragma unroll
           for (int c = 0; c < kC; ++c) {
             float* to = reinterpret_cast<float*>(scratch) + head * DP + 64 * c + 8 * g;
-            *reinterpret_cast<float4*>(to) = make_float4(acc[n][c][0][i] * f, acc[n][c][1][i] * f, acc[n][c][2][i] * f, acc[n][c][3][i] * f);
-            *reinterpret_cast<float4*>(to + 4) =
-                make_float4(acc[n][c][0][2 + i] * f, acc[n][c][1][2 + i] * f, acc[n][c][2][2 + i] * f, acc[n][c][3][2 + i] * f);
+            *reinterpret_cast<float4*>(to) = make_float4(acc[n][c][0][i], acc[n][c][1][i], acc[n][c][2][i], acc[n][c][3][i]);
+            *reinterpret_cast<float4*>(to + 4) = make_float4(acc[n][c][0][2 + i], acc[n][c][1][2 + i], acc[n][c][2][2 + i], acc[n][c][3][2 + i]);
           }
         }
       if (lane == 0) sums_of[warp] = reinterpret_cast<const float4*>(scratch);
     }
+    store_q(q_at ^ 1u);
     __syncthreads();
-
-    const bool whole = unit0 == 0 && unit1 == seq_units;
-    uint32_t c0 = 0, parts = 0;
-    bool last = whole;
-    // places in the workspace: a sequence that began in an earlier piece is its piece's first, another its last
-    auto place = [&](uint32_t piece, bool began) { return (uint64_t)2 * (piece * per_seq + item) + (began ? 1 : 0); };
-    auto add_warps = [&](uint32_t i) {
+    const uint64_t here = place(blockIdx.y, unit0 == 0);
+#pragma unroll 1
+    for (uint32_t j = threadIdx.x; j < kHeads * DP / 4; j += kThreads) {
+      const uint32_t head = j / (DP / 4), d = j % (DP / 4) * 4;
+      float top = -INFINITY, sum = 0.0f;
       float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll 4
-      for (uint32_t w = 0; w < warps; ++w) {
-        const float4 v = sums_of[w][i];
-        o.x += v.x;
-        o.y += v.y;
-        o.z += v.z;
-        o.w += v.w;
+#pragma unroll
+      for (int w = 0; w < W; ++w) top = fmaxf(top, w < (int)warps ? warp_r[w][head] : -INFINITY);
+#pragma unroll
+      for (int w = 0; w < W; ++w) {
+        if (w >= (int)warps) break;
+        const float4 v = sums_of[w][j];
+        const float f = exp2_fast(warp_r[w][head] - known(top));
+        sum = fmaf(warp_l[w][head], f, sum);
+        o.x = fmaf(v.x, f, o.x);
+        o.y = fmaf(v.y, f, o.y);
+        o.z = fmaf(v.z, f, o.z);
+        o.w = fmaf(v.w, f, o.w);
       }
-      return o;
-    };
-    if (!whole) {
-      const uint64_t here = place(blockIdx.y, unit0 == 0);
-#pragma unroll 1
-      for (uint32_t i = threadIdx.x; i < kHeads * DP / 4; i += kThreads)
-        __stcg(reinterpret_cast<float4*>(p.part) + here * (kHeads * DP / 4) + i, add_warps(i));
-      if (threadIdx.x < kHeads)
-        __stcg(reinterpret_cast<float2*>(p.part_rl) + here * kHeads + threadIdx.x, make_float2(item_r[threadIdx.x], item_l[threadIdx.x]));
-      c0 = pieces.of(seq_first);
-      parts = pieces.of(seq_first + seq_units - 1) - c0 + 1;
-      __syncthreads();
-      if (threadIdx.x == 0) {
-        __threadfence();                                         // the CTA's part is there before it is counted
-        unsigned int* count = p.arrived + c0 * per_seq + item;   // a sequence that goes on is the last of the piece it began in
-        const bool all = atomicAdd(count, 1u) == parts - 1;
-        if (all) *count = 0u;                                    // as the next call expects it
-        __threadfence();
-        last_word = all;
+      if (whole) {
+        finish(seq, head, d, o, top, sum);
+      } else {
+        __stcg(reinterpret_cast<float4*>(p.part) + here * (kHeads * DP / 4) + j, o);
+        if (d == 0) __stcg(reinterpret_cast<float2*>(p.part_rl) + here * kHeads + head, make_float2(top, sum));
       }
-      __syncthreads();
-      last = last_word;
     }
-    if (last) {
-#pragma unroll 1
-      for (uint32_t j = threadIdx.x; j < kHeads * DP / 4; j += kThreads) {
-        const uint32_t head = j / (DP / 4), d = j % (DP / 4) * 4;
-        float4 o;
-        float top, sum;
-        if (whole) {
-          o = add_warps(j);
-          top = item_r[head];
-          sum = item_l[head];
-        } else {
-          // the parts in the order of the keys, eight on their way at a time
-          o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-          top = -INFINITY;
-          sum = 0.0f;
-#pragma unroll 1
-          for (uint32_t i0 = 0; i0 < parts; i0 += 8) {
-            float4 v[8];
-            float2 rl[8];
-#pragma unroll
-            for (uint32_t i = 0; i < 8; ++i) {
-              rl[i] = make_float2(-INFINITY, 0.0f);
-              v[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-              if (i0 + i >= parts) continue;
-              const uint64_t at = place(c0 + i0 + i, i0 + i == 0);
-              v[i] = __ldcg(reinterpret_cast<const float4*>(p.part) + at * (kHeads * DP / 4) + j);
-              rl[i] = __ldcg(reinterpret_cast<const float2*>(p.part_rl) + at * kHeads + head);
-            }
-            float higher = top;
-#pragma unroll
-            for (uint32_t i = 0; i < 8; ++i) higher = fmaxf(higher, rl[i].x);
-            const float f0 = exp2_fast(top - known(higher));     // 0 at first
-            o = make_float4(o.x * f0, o.y * f0, o.z * f0, o.w * f0);
-            sum *= f0;
-            top = higher;
-#pragma unroll
-            for (uint32_t i = 0; i < 8; ++i) {
-              const float f = exp2_fast(rl[i].x - known(top));
-              o.x = fmaf(v[i].x, f, o.x);
-              o.y = fmaf(v[i].y, f, o.y);
-              o.z = fmaf(v[i].z, f, o.z);
-              o.w = fmaf(v[i].w, f, o.w);
-              sum = fmaf(rl[i].y, f, sum);
-            }
-          }
-        }
-        if (head >= heads) continue;
-        const bool none = sum == 0.0f;   // no score above -infinity
-        const float by = 1.0f / sum;
-        const float v[4] = {none ? 0.0f : o.x * by, none ? 0.0f : o.y * by, none ? 0.0f : o.z * by, none ? 0.0f : o.w * by};
-        unsigned short* to = static_cast<unsigned short*>(p.out) + seq * p.o_row + (h0 + head) * p.o_head + d;
-        if (p.vec_out && d + 4 <= p.dim) {
-          *reinterpret_cast<uint2*>(to) = make_uint2(pack2<DT>(v[0], v[1]), pack2<DT>(v[2], v[3]));
-        } else {
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (d + i < p.dim) store_elem<DT>(to, i, v[i]);
-        }
-        if (d == 0 && p.lse) p.lse[(uint64_t)seq * p.q_heads + h0 + head] = none ? -INFINITY : (top + log2f(sum)) * 0.69314718055994531f;
-      }
+    if (!whole) {
+      const int which = unit0 == 0;
+      part_first[which] = seq_first;
+      part_units[which] = seq_units;
+      part_seq[which] = seq;
     }
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // the sums were read before copies come in their place
     __syncthreads();                                               // shared memory is used again
     if (scratch) wanted = 1;
+    q_at ^= 1u;
     u = seq_first + unit1;
     seq_first += seq_units;
+  }
+
+  // Parts are counted once all of the piece is done; the CTA that counts a sequence's last one adds them up.
+  uint32_t c0[2], parts[2];
+#pragma unroll
+  for (int which = 0; which < 2; ++which) {
+    c0[which] = part_units[which] ? pieces.of(part_first[which]) : 0;
+    parts[which] = part_units[which] ? pieces.of(part_first[which] + part_units[which] - 1) - c0[which] + 1 : 0;
+    if (threadIdx.x == 32 * which) {
+      join_word[which] = 0u;
+      if (parts[which]) {
+        __threadfence();                                                // the CTA's part is there before it is counted
+        unsigned int* count = p.arrived + c0[which] * per_seq + item;   // a sequence that goes on is the last of the piece it began in
+        const bool all = atomicAdd(count, 1u) == parts[which] - 1;
+        if (all) *count = 0u;                                           // as the next call expects it
+        __threadfence();
+        join_word[which] = all;
+      }
+    }
+  }
+  __syncthreads();
+#pragma unroll 1
+  for (int which = 0; which < 2; ++which) {
+    if (!join_word[which]) continue;
+    const uint32_t from = which ? c0[1] : c0[0], count = which ? parts[1] : parts[0], of = which ? part_seq[1] : part_seq[0];
+#pragma unroll 1
+    for (uint32_t j = threadIdx.x; j < kHeads * DP / 4; j += kThreads) {
+      const uint32_t head = j / (DP / 4);
+      // the parts in the order of the keys, eight on their way at a time
+      float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+      float top = -INFINITY, sum = 0.0f;
+#pragma unroll 1
+      for (uint32_t i0 = 0; i0 < count; i0 += 8) {
+        float4 v[8];
+        float2 rl[8];
+#pragma unroll
+        for (uint32_t i = 0; i < 8; ++i) {
+          rl[i] = make_float2(-INFINITY, 0.0f);
+          v[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+          if (i0 + i >= count) continue;
+          const uint64_t at = place(from + i0 + i, i0 + i == 0);
+          v[i] = __ldcg(reinterpret_cast<const float4*>(p.part) + at * (kHeads * DP / 4) + j);
+          rl[i] = __ldcg(reinterpret_cast<const float2*>(p.part_rl) + at * kHeads + head);
+        }
+        float higher = top;
+#pragma unroll
+        for (uint32_t i = 0; i < 8; ++i) higher = fmaxf(higher, rl[i].x);
+        const float f0 = exp2_fast(top - known(higher));     // 0 at first
+        o = make_float4(o.x * f0, o.y * f0, o.z * f0, o.w * f0);
+        sum *= f0;
+        top = higher;
+#pragma unroll
+        for (uint32_t i = 0; i < 8; ++i) {
+          const float f = exp2_fast(rl[i].x - known(top));
+          o.x = fmaf(v[i].x, f, o.x);
+          o.y = fmaf(v[i].y, f, o.y);
+          o.z = fmaf(v[i].z, f, o.z);
+          o.w = fmaf(v[i].w, f, o.w);
+          sum = fmaf(rl[i].y, f, sum);
+        }
+      }
+      finish(of, head, j % (DP / 4) * 4, o, top, sum);
+    }
   }
   if (bad) set_status(p.status, (unsigned int)KB_ERR_INVALID_ARG);
   if (!ok) {   // what is on its way lands before the CTA ends
