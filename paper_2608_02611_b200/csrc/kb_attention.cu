@@ -63,13 +63,15 @@ kb_status check_cache(kb_ctx* ctx, const char* where, const kb_paged_cache& c, i
 
 template <int DT, int L>
 kb_status launch_rope(kb_ctx* ctx, const RopeParams& p, bool vec, cudaStream_t st) {
-  // a token per CTA until they fill the card, then several, so that the weights and the start are paid for less often
-  const uint32_t per = p.tokens >= 16ull * ctx->sm_count ? kRopeTokens : 1;
-  const unsigned int grid = (unsigned int)((p.tokens + per - 1) / per);
+  // as many tokens per CTA as leave three CTAs for each SM; with fewer, the heads of a token are shared out as well
+  const uint64_t fill = 3ull * ctx->sm_count;
+  const uint32_t per = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(kRopeTokens, p.tokens / fill));
+  const uint64_t grid = (p.tokens + per - 1) / per;
+  const uint32_t heads = p.hq + 2 * p.hkv, turns = (heads * L + kRopeThreads - 1) / kRopeThreads;   // of a CTA's warps through a token
   if (vec)
-    qk_norm_rope_kernel<DT, L><<<grid, kRopeThreads, 0, st>>>(p, per);
+    qk_norm_rope_kernel<DT, L><<<dim3((unsigned int)grid, (unsigned int)std::min<uint64_t>(turns, (fill + grid - 1) / grid)), kRopeThreads, 0, st>>>(p, per);
   else
-    qk_norm_rope_plain_kernel<DT, L><<<grid, kRopeThreads, 0, st>>>(p, per);
+    qk_norm_rope_plain_kernel<DT, L><<<(unsigned int)grid, kRopeThreads, 0, st>>>(p, per);
   return launched(ctx);
 }
 template <int DT>

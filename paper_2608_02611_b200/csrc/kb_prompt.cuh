@@ -23,7 +23,8 @@
 // score products run ahead into the next item while the last one's outputs are stored.
 //
 // Roles: warp 0 copies, warps 1 to 4 issue matrix instructions, warp 5 hands out the items, warp 6 zeroes values behind a
-// sequence's end, warps 8 to 11 and 12 to 15 are the tiles' warpgroups.  Every wait is bounded.
+// sequence's end, warps 8 to 11 and 12 to 15 are the tiles' warpgroups, warps 16 to 19 divide and store the outputs of both
+// tiles (4000 cycles per item, in which the tiles' warpgroups begin the next one).  Every wait is bounded.
 #pragma once
 
 #include "kb_paged.cuh"
@@ -56,15 +57,15 @@ struct PromptTile {
   static constexpr uint32_t kStepBytes = kPromptKeys * DP * 2;  // of k or v
   static constexpr uint32_t kChunkBytes = kPromptKeys * 128;    // of which 64 elements
   static constexpr uint32_t kStages = 256 / kPromptKeys;        // of the rings of k and of v tiles
-  static constexpr uint32_t kOutPitch = 80, kOutBytes = 32 * kOutPitch;   // a warp's way out: 64 bytes of 32 rows at a time
-  static constexpr uint32_t kSmem = 1024 + 2 * kTileBytes + 2 * kStages * kStepBytes + 8 * kOutBytes;
+  static constexpr uint32_t kOutPitch = 144, kOutBytes = 32 * kOutPitch;   // a warp's way out: 128 bytes of 32 rows at a time
+  static constexpr uint32_t kSmem = 1024 + 2 * kTileBytes + 2 * kStages * kStepBytes + 4 * kOutBytes;
   // tensor memory: per tile 128 columns for S, in places of kPromptKeys, and DP columns of O
   static constexpr uint32_t kPlaces = 128 / kPromptKeys;
   static constexpr uint32_t kTmemS = 0, kTmemO = 256, kTmemCols = 512;
-  static constexpr int kThreads = 512;
-  // 128 registers per thread at launch, shared out 56 to the first two warpgroups and 200 to the others
-  static constexpr int kRegsLaunch = 128, kRegsControl = 56, kRegsSoftmax = 200;
-  static_assert(256 * kRegsControl + 256 * kRegsSoftmax <= kThreads * kRegsLaunch, "register shares");
+  static constexpr int kThreads = 640;
+  // 96 registers per thread at launch, shared out 48 to the first two warpgroups, 152 to the next two and 80 to the last
+  static constexpr int kRegsLaunch = 96, kRegsControl = 48, kRegsSoftmax = 152, kRegsOut = 80;
+  static_assert(256 * kRegsControl + 256 * kRegsSoftmax + 128 * kRegsOut <= kThreads * kRegsLaunch, "register shares");
 };
 static_assert(PromptTile<128>::kSmem <= 227 * 1024 - 1024, "shared memory");
 
@@ -316,6 +317,8 @@ __global__ void __launch_bounds__(PromptTile<DP>::kThreads, 1)
   extern __shared__ unsigned char dyn[];
   __shared__ uint64_t q_full[2], q_empty[2], k_full[kS], k_empty[kS], v_full[kS], v_empty[kS], v_tail[kS];
   __shared__ uint64_t s_full[2][kP], p_full[2][kP], o_full[2][kP], item_full[2], item_empty[2], want, drained[5];
+  __shared__ uint64_t sum_full[2], o_free[2];
+  __shared__ float2 row_sum[2][128];   // r and l of the tiles' queries
   __shared__ PromptItem items[2];
   __shared__ uint32_t tmem_base;
   __shared__ unsigned int abort_word;
@@ -337,7 +340,9 @@ __global__ void __launch_bounds__(PromptTile<DP>::kThreads, 1)
       mbar_init(&q_full[t], 1);
       mbar_init(&q_empty[t], 1);
       mbar_init(&item_full[t], 1);
-      mbar_init(&item_empty[t], 14);   // warps 0 to 4, 6 and 8 to 15
+      mbar_init(&item_empty[t], 18);   // warps 0 to 4, 6 and 8 to 19
+      mbar_init(&sum_full[t], 4);
+      mbar_init(&o_free[t], 4);
       for (uint32_t b = 0; b < kP; ++b) {
         mbar_init(&s_full[t][b], 1);
         mbar_init(&p_full[t][b], 4);
@@ -441,7 +446,7 @@ __global__ void __launch_bounds__(PromptTile<DP>::kThreads, 1)
     // Four warps issue matrix instructions, so that what one spends on its waits hides under the others' products: warps 1
     // and 2 a tile's scores, warps 3 and 4 a tile's outputs.
     const int t = (warp - 1) & 1;
-    uint32_t used = 0, done = 0, q_items = 0;   // tiles of the ring; steps of this tile; its items
+    uint32_t used = 0, done = 0, q_items = 0;   // tiles of the ring; steps of this tile; items (scores: those with steps of it)
     PromptItem x;
     if (warp < 3) {
       const uint32_t idesc = mma_idesc_f16(DT == KB_BF16, false, 128, kPromptKeys);
@@ -480,6 +485,7 @@ __global__ void __launch_bounds__(PromptTile<DP>::kThreads, 1)
           wait(&v_full[st], used / kS);
           if (i < n && go) {
             const uint32_t place = done % kP;
+            if (i == 0 && !wait(&o_free[t], q_items + 1)) break;   // the last item's outputs have been read
             if (!wait(&p_full[t][place], done / kP)) break;
             tc_fence_after();
 #pragma unroll
@@ -491,6 +497,7 @@ __global__ void __launch_bounds__(PromptTile<DP>::kThreads, 1)
           }
           if (go) mma_commit(&v_empty[st]);
         }
+        ++q_items;
       }
     }
     if (!go) {   // what has been issued ends before tensor memory is freed
@@ -500,23 +507,22 @@ __global__ void __launch_bounds__(PromptTile<DP>::kThreads, 1)
         if (global_ns() - t0 > 1000000000ull) break;
       __syncwarp();
     }
-  } else if (warp >= 8) {
+  } else if (warp >= 8 && warp < 16) {
     regs_grow<T::kRegsSoftmax>();
     const int t = (warp - 8) >> 2, quarter = warp & 3;
     const uint32_t at_s = tmem + T::kTmemS + t * 128 + ((uint32_t)(quarter * 32) << 16);
     const uint32_t at_o = tmem + T::kTmemO + t * DP + ((uint32_t)(quarter * 32) << 16);
-    unsigned char* rows = way_out + (warp - 8) * T::kOutBytes;
     const float c = p.scale_log2;
     // no call between reads of tensor memory and their use: everything is in registers there
     auto wait_here = [&](uint64_t* bar, uint32_t parity) {
       return go = __all_sync(0xFFFFFFFFu, mbar_wait_bounded(bar, parity & 1u, abort_flag, p.status));
     };
-    uint32_t done = 0;
+    uint32_t done = 0, items_done = 0;
     PromptItem x;
 #pragma unroll 1
     while (next_item(x, wait_here)) {
       const uint32_t n = t ? x.n[1] : x.n[0], nq = x.nq, nk = x.nk;
-      const uint32_t row = x.row0 + (p.pair ? 0 : t * 128) + quarter * 32 + lane, h = x.head0 + (p.pair ? t : 0);
+      const uint32_t row = x.row0 + (p.pair ? 0 : t * 128) + quarter * 32 + lane;
       const uint32_t seen = row < nq ? prompt_seen(row, nq, nk, p.causal) : 0;
       const uint32_t seen_by_all = __reduce_min_sync(0xFFFFFFFFu, seen);
       float r = -INFINITY, l0 = 0.0f, l1 = 0.0f;
@@ -586,57 +592,94 @@ __global__ void __launch_bounds__(PromptTile<DP>::kThreads, 1)
         __syncwarp();
         mbar_arrive_if(&p_full[t][place], lane == 0);
       }
-      if (!go) break;
-      const float l = l0 + l1, by = 1.0f / l;
-      const bool none = l == 0.0f, in = row < nq;
-      if (n) {
-        if (!wait_here(&o_full[t][(done - 1) % kP], (done - 1) / kP)) break;
-        tc_fence_after();
-      }
-      if (in && p.lse) p.lse[(uint64_t)(x.q0 + row) * p.hq + h] = none ? -INFINITY : (r + log2f(l)) * 0.69314718055994531f;
-      // 64 bytes of 32 rows at a time through shared memory, so that a warp's stores cover whole sectors.  A loop of few
-      // instructions: it runs once per item, and unrolled it took longer to fetch than to execute.
-      const uint32_t first = row - lane, mask = none ? 0u : 0xFFFFFFFFu;
-      float most = 0.0f;               // largest magnitude, or NaN
-      unsigned short* to = static_cast<unsigned short*>(p.out) + (uint64_t)(x.q0 + first + (lane >> 2)) * p.o_row + h * p.o_head + (lane & 3) * 8;
-      const int rows_left = (int)(nq - first) - (lane >> 2);
+      // the sums to the last warpgroup, which has taken the last item's by then
+      if (!go || !wait_here(&o_free[t], items_done + 1)) break;
+      ++items_done;
+      row_sum[t][quarter * 32 + lane] = make_float2(r, l0 + l1);
+      __syncwarp();
+      mbar_arrive_if(&sum_full[t], lane == 0);
+    }
+  } else if (warp >= 16) {
+    // outputs: a tile's sums of p v by its sums of p, while the other warpgroups are at the next item
+    regs_shrink<T::kRegsOut>();
+    const int quarter = warp & 3;
+    unsigned char* rows = way_out + quarter * T::kOutBytes;
+    auto wait_here = [&](uint64_t* bar, uint32_t parity) {
+      return go = __all_sync(0xFFFFFFFFu, mbar_wait_bounded(bar, parity & 1u, abort_flag, p.status));
+    };
+    uint32_t done[2] = {0, 0}, items_done = 0;
+    PromptItem x;
 #pragma unroll 1
-      for (int d = 0; d < (int)p.dim && first < nq; d += 32, to += 32) {
-        float o[32];
-        uint32_t w[16];
+    while (next_item(x, wait_here)) {
+#pragma unroll 1
+      for (int t = 0; t < 2; ++t) {
+        const uint32_t n = t ? x.n[1] : x.n[0], nq = x.nq, h = x.head0 + (p.pair ? t : 0);
+        const uint32_t first = x.row0 + (p.pair ? 0 : t * 128) + quarter * 32, row = first + lane;
+        const uint32_t steps = (t ? done[1] : done[0]) + n;
+        if (t)
+          done[1] = steps;
+        else
+          done[0] = steps;
+        if (!wait_here(&sum_full[t], items_done)) break;
+        const float2 rl = row_sum[t][quarter * 32 + lane];
+        const float r = rl.x, l = rl.y, by = 1.0f / l;
+        const bool none = l == 0.0f, in = row < nq;
         if (n) {
-          tmem_ld32(at_o + d, o);
-          tmem_wait_ld(o);
+          if (!wait_here(&o_full[t][(steps - 1) % kP], (steps - 1) / kP)) break;
+          tc_fence_after();
         }
-#pragma unroll
-        for (int k = 0; k < 32; k += 2) {
-          const float a = o[k] * by, b = o[k + 1] * by;
-          most = max3_nan(most, fabsf(a), fabsf(b));
-          w[k / 2] = pack2<DT>(a, b) & mask;
-        }
-#pragma unroll
-        for (int u = 0; u < 4; ++u)
-          *reinterpret_cast<uint4*>(rows + lane * T::kOutPitch + u * 16) = make_uint4(w[4 * u], w[4 * u + 1], w[4 * u + 2], w[4 * u + 3]);
-        __syncwarp();
-        if (d + (lane & 3) * 8 < (int)p.dim) {
-          const unsigned char* from = rows + (lane >> 2) * T::kOutPitch + (lane & 3) * 16;
-          if (p.vec_out) {
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-              if (8 * k < rows_left) *reinterpret_cast<uint4*>(to + 8 * k * p.o_row) = *reinterpret_cast<const uint4*>(from + 8 * k * T::kOutPitch);
-          } else {
+        // 128 bytes of 32 rows at a time through shared memory, so that a warp's stores cover whole lines
+        const uint32_t mask = none ? 0u : 0xFFFFFFFFu, at_o = tmem + T::kTmemO + t * DP + ((uint32_t)(quarter * 32) << 16);
+        float most = 0.0f;               // largest magnitude, or NaN
+        unsigned short* to = static_cast<unsigned short*>(p.out) + (uint64_t)(x.q0 + first + (lane >> 3)) * p.o_row + h * p.o_head + (lane & 7) * 8;
+        const int rows_left = (int)(nq - first) - (lane >> 3);
 #pragma unroll 1
-            for (int k = 0; k < 32; ++k)
-              if (k / 8 * 8 < rows_left) to[k / 8 * 8 * p.o_row + k % 8] = reinterpret_cast<const unsigned short*>(from + k / 8 * 8 * T::kOutPitch)[k % 8];
+        for (int d = 0; d < (int)p.dim && first < nq; d += 64, to += 64) {
+#pragma unroll
+          for (int e = 0; e < 64; e += 32) {
+            float o[32];
+            uint32_t w[16];
+            if (n) {
+              tmem_ld32(at_o + d + e, o);
+              tmem_wait_ld(o);
+            }
+#pragma unroll
+            for (int k = 0; k < 32; k += 2) {
+              const float a = o[k] * by, b = o[k + 1] * by;
+              most = max3_nan(most, fabsf(a), fabsf(b));
+              w[k / 2] = pack2<DT>(a, b) & mask;
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+              *reinterpret_cast<uint4*>(rows + lane * T::kOutPitch + e * 2 + u * 16) = make_uint4(w[4 * u], w[4 * u + 1], w[4 * u + 2], w[4 * u + 3]);
           }
+          __syncwarp();
+          if (d + (lane & 7) * 8 < (int)p.dim) {
+            const unsigned char* from = rows + (lane >> 3) * T::kOutPitch + (lane & 7) * 16;
+            if (p.vec_out) {
+#pragma unroll
+              for (int k = 0; k < 8; ++k)
+                if (4 * k < rows_left) *reinterpret_cast<uint4*>(to + 4 * k * p.o_row) = *reinterpret_cast<const uint4*>(from + 4 * k * T::kOutPitch);
+            } else {
+#pragma unroll 1
+              for (int k = 0; k < 64; ++k)
+                if (k / 8 * 4 < rows_left) to[k / 8 * 4 * p.o_row + k % 8] = reinterpret_cast<const unsigned short*>(from + k / 8 * 4 * T::kOutPitch)[k % 8];
+            }
+          }
+          __syncwarp();
         }
+        tc_fence_before();
         __syncwarp();
+        mbar_arrive_if(&o_free[t], lane == 0);
+        if (in && p.lse) p.lse[(uint64_t)(x.q0 + row) * p.hq + h] = none ? -INFINITY : (r + log2f(l)) * 0.69314718055994531f;
+        // rows that are not finite although their sums are: values that they do not see?
+        const bool odd = !(most <= 3.402823466e38f);
+        const uint32_t last = min(x.nk, n * kPromptKeys), seen = in ? prompt_seen(row, nq, x.nk, p.causal) : 0;
+        const bool ask = in && odd && l > 0.0f && l <= 3.402823466e38f && seen < last;
+        if (__any_sync(0xFFFFFFFFu, ask)) repair_rows<DT>(p, x, first, last, h, ask, seen, r, by, lane);
       }
-      const bool odd = !(most <= 3.402823466e38f);
-      // rows that are not finite although their sums are: values that they do not see?
-      const uint32_t last = min(nk, n * kPromptKeys);
-      const bool ask = in && odd && l > 0.0f && l <= 3.402823466e38f && seen < last;
-      if (__any_sync(0xFFFFFFFFu, ask)) repair_rows<DT>(p, x, first, last, h, ask, seen, r, by, lane);
+      if (!go) break;
+      ++items_done;
     }
   }
   tc_fence_before();

@@ -90,20 +90,32 @@ __device__ __forceinline__ float rope_weight(const RopeParams& p, const void* w,
 // Rows on vector boundaries with dim a multiple of 8 and pairs of which four make a vector.  L lanes hold a
 // row, two vectors of four elements each, so that the elements of a pair are in one lane: of halves, lane c
 // has 4 c .. + 3 and half + 4 c .. + 3, and the lanes after those have 8 of the elements that are not turned each;
-// of neighbours, 8 c .. + 7.  A warp works on 32 / L heads of one kind at a time, so that what differs between
-// q, k and v is the same for all its lanes, and has the next kRopeAhead pieces on their way meanwhile
-// (16384 tokens of 32 + 8 + 8 heads of 128, bf16, stored in a cache: one row at a time 176 us).
+// of neighbours, 8 c .. + 7.  A warp takes 32 / L heads of one kind through the CTA's tokens, four of whose loads are
+// under way before the first is used; what depends on the head (weights, addresses but for a step per token) is
+// done once for them.  16384 tokens of 32 + 8 + 8 heads of 128, bf16, stored in a cache: a row at a time 176 us;
+// heads in turn, which had to be told apart for every row (240 instructions for 512 bytes), 121 us; so 94.5 (4.6 TB/s;
+// issue slots 64% busy), in binary32 without a cache 119 (5.6 TB/s).
 __device__ __forceinline__ void vec_words(uint2 v, uint32_t* w) { w[0] = v.x, w[1] = v.y; }
 __device__ __forceinline__ void vec_words(uint4 v, uint32_t* w) { w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w; }
 __device__ __forceinline__ void words_vec(const uint32_t* w, uint2& v) { v = make_uint2(w[0], w[1]); }
 __device__ __forceinline__ void words_vec(const uint32_t* w, uint4& v) { v = make_uint4(w[0], w[1], w[2], w[3]); }
-template <int DT>
-struct RopePiece {
-  static constexpr int kWords = DT == KB_F32 ? 8 : 4, kAhead = DT == KB_F32 ? 2 : 4;
-};
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 r;
+  asm("{\n.reg .b64 a, b;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nmul.rn.f32x2 a, a, b;\nmov.b64 {%0, %1}, a;\n}"
+      : "=f"(r.x), "=f"(r.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return r;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 r;
+  asm("{\n.reg .b64 a, b, c;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nmov.b64 c, {%6, %7};\nfma.rn.f32x2 a, a, b, c;\nmov.b64 {%0, %1}, a;\n}"
+      : "=f"(r.x), "=f"(r.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return r;
+}
 template <int DT, int L>
-__global__ void __launch_bounds__(kRopeThreads, 3) qk_norm_rope_kernel(const RopeParams p, const uint32_t per_cta) {
-  constexpr int kWarps = kRopeThreads / 32, kBytes = DT == KB_F32 ? 4 : 2, kWords = RopePiece<DT>::kWords, kAhead = RopePiece<DT>::kAhead;
+__global__ void __launch_bounds__(kRopeThreads, 4) qk_norm_rope_kernel(const RopeParams p, const uint32_t per_cta) {
+  constexpr int kWarps = kRopeThreads / 32, kBytes = DT == KB_F32 ? 4 : 2, kWords = 2 * kBytes, kAhead = 4;
   constexpr uint32_t kHeads = 32 / L;        // heads of a piece
   using Vec = typename std::conditional<DT == KB_F32, uint4, uint2>::type;
   __shared__ __align__(16) RopeShared sh;
@@ -112,140 +124,130 @@ __global__ void __launch_bounds__(kRopeThreads, 3) qk_norm_rope_kernel(const Rop
   const uint32_t warp = threadIdx.x >> 5, c = threadIdx.x % L, sub = (threadIdx.x & 31) / L;
   // pieces of a token: queries', keys', values'
   const uint32_t nq = p.q_out ? (p.hq + kHeads - 1) / kHeads : 0, nkv = (p.hkv + kHeads - 1) / kHeads;
-  const uint32_t nk = p.k_out || p.k_cache ? nkv : 0, per_token = nq + nk + (p.k_cache ? nkv : 0);
+  const uint32_t nk = p.k_out || p.k_cache ? nkv : 0, pieces = nq + nk + (p.k_cache ? nkv : 0);
   // the lane's two vectors, and its pairs
-  const uint32_t turned = p.interleaved ? p.dim / 8 : p.half / 4;   // lanes with pairs (the rest have cosine 1)
-  const bool has = c * 8 < p.dim;
-  const uint32_t ea = p.interleaved ? 8 * c : c < turned ? 4 * c : 2 * p.half + 8 * (c - turned);
-  const uint32_t eb = p.interleaved || c >= turned ? ea + 4 : p.half + 4 * c;
-
-  struct Place {
-    uint32_t t, piece;
-  };
-  auto forward = [&](Place x) {
-    x.piece += kWarps;
-    while (x.piece >= per_token) {
-      x.piece -= per_token;
-      ++x.t;
-    }
-    return x;
-  };
-  auto load = [&](Place x, uint32_t* raw) {
-    const bool is_q = x.piece < nq, is_k = !is_q && x.piece < nq + nk;
-    const uint32_t head = (x.piece - (is_q ? 0 : is_k ? nq : nq + nk)) * kHeads + sub;
-    const void* src = is_q ? p.q : is_k ? p.k : p.v;
-    const uint64_t row = is_q ? p.q_row : is_k ? p.k_row : p.v_row, step = is_q ? p.q_head : is_k ? p.k_head : p.v_head;
-#pragma unroll
-    for (int i = 0; i < kWords; ++i) raw[i] = 0u;
-    if (x.t < ntok && has && head < (is_q ? p.hq : p.hkv)) {
-      const unsigned char* from = static_cast<const unsigned char*>(src) + ((t0 + x.t) * row + head * step) * kBytes;
-      const Vec a = *reinterpret_cast<const Vec*>(from + ea * kBytes), b = *reinterpret_cast<const Vec*>(from + eb * kBytes);
-      vec_words(a, raw);
-      vec_words(b, raw + kWords / 2);
-    }
-  };
-  Place ahead{0, warp};
-  while (ahead.piece >= per_token) {
-    ahead.piece -= per_token;
-    ++ahead.t;
-  }
-  Place now = ahead;
-  uint32_t next[kAhead][kWords];
-#pragma unroll
-  for (int u = 0; u < kAhead; ++u) {
-    load(ahead, next[u]);
-    ahead = forward(ahead);
-  }
-  rope_begin(p, sh, t0, ntok);
-  float wq[8], wk[8];
-#pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const uint32_t e = j < 4 ? ea + j : eb + j - 4;
-    wq[j] = rope_weight<DT>(p, p.q_weight, e);
-    wk[j] = rope_weight<DT>(p, p.k_weight, e);
-  }
+  const uint32_t turned = p.interleaved ? p.half * 2 : p.half;       // four times the lanes with pairs, or more
+  const bool has = c * 8 < p.dim, turns = (p.interleaved ? 8 * c : 4 * c) < turned;
+  const uint32_t ea = p.interleaved ? 8 * c : turns ? 4 * c : 2 * p.half + 8 * (c - p.half / 4);
+  const uint32_t eb = p.interleaved || !turns ? ea + 4 : p.half + 4 * c;
   const float per_dim = 1.0f / (float)p.dim;
-  __syncthreads();
+  bool begun = false;
 
-  while (now.t < ntok) {
-    uint32_t raw[kAhead][kWords];
+#pragma unroll 1
+  for (uint32_t piece = blockIdx.y * kWarps + warp; piece < pieces || !begun; piece += kWarps * gridDim.y) {
+    const bool is_q = piece < nq, is_v = piece >= nq + nk;
+    const uint32_t head = (piece - (is_q ? 0 : is_v ? nq + nk : nq)) * kHeads + sub;
+    const bool mine = piece < pieces && has && head < (is_q ? p.hq : p.hkv);
+    const uint64_t in_row = is_q ? p.q_row : is_v ? p.v_row : p.k_row;
+    const unsigned char* from = static_cast<const unsigned char*>(is_q ? p.q : is_v ? p.v : p.k) +
+                                (t0 * in_row + head * (is_q ? p.q_head : is_v ? p.v_head : p.k_head)) * kBytes;
+    unsigned char* to = static_cast<unsigned char*>(is_q ? p.q_out : is_v ? nullptr : p.k_out);
+    const uint64_t out_row = is_q ? p.qo_row : p.ko_row;
+    if (to) to += (t0 * out_row + head * (is_q ? p.qo_head : p.ko_head) + ea) * kBytes;
+    from += ea * kBytes;
+    const uint32_t other = (eb - ea) * kBytes;   // from the lane's one vector to the other
+    const uint64_t in_step = in_row * kBytes, out_step = out_row * kBytes;
+    unsigned char* cache = static_cast<unsigned char*>(is_q ? nullptr : is_v ? p.v_cache : p.k_cache);
+    if (cache) cache += (head * (is_v ? p.vc_head : p.kc_head) + ea) * kBytes;
+    const long long* slots = is_v ? sh.at_v : sh.at_k;
+    float2 w[4];
+    const void* weight = is_q ? p.q_weight : p.k_weight;
+#pragma unroll 1
+    for (uint32_t first = 0; first < ntok; first += kAhead) {
+      uint32_t raw[kAhead][kWords];
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
+      for (int u = 0; u < kAhead; ++u, from += in_step) {
+        Vec a = {}, b = {};
+        if (mine && first + u < ntok) {
+          a = *reinterpret_cast<const Vec*>(from);
+          b = *reinterpret_cast<const Vec*>(from + other);
+        }
+        vec_words(a, raw[u]);
+        vec_words(b, raw[u] + kWords / 2);
+      }
+      if (!begun) {   // the CTA's angles, while the first rows are on their way
+        begun = true;
+        rope_begin(p, sh, t0, ntok);
+        __syncthreads();
+        if (piece >= pieces) break;
+      }
+      if (first == 0 && !is_v) {
 #pragma unroll
-      for (int i = 0; i < kWords; ++i) raw[u][i] = next[u][i];
-      load(ahead, next[u]);
-      ahead = forward(ahead);
-    }
+        for (int j = 0; j < 4; ++j) {
+          const uint32_t e = j < 2 ? ea + 2 * j : eb + 2 * j - 4;
+          w[j] = make_float2(rope_weight<DT>(p, weight, e), rope_weight<DT>(p, weight, e + 1));
+        }
+      }
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u, now = forward(now)) {
-      if (now.t >= ntok) break;   // the same for the whole warp
-      const bool is_q = now.piece < nq, is_k = !is_q && now.piece < nq + nk;
-      const uint32_t head = (now.piece - (is_q ? 0 : is_k ? nq : nq + nk)) * kHeads + sub;
-      const uint64_t token = t0 + now.t;
-      auto put = [&](void* dst, uint64_t at) {
-        unsigned char* to = static_cast<unsigned char*>(dst) + at * kBytes;
+      for (int u = 0; u < kAhead; ++u) {
+        const uint32_t t = first + u;
+        if (t >= ntok) break;
+        if (!is_v) {
+          float v[8];
+          if constexpr (DT == KB_F32) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = __uint_as_float(raw[u][j]);
+          } else {
+            Elem<DT>::decode(make_uint4(raw[u][0], raw[u][1], raw[u][2], raw[u][3]), v);
+          }
+          float2 x[4] = {{v[0], v[1]}, {v[2], v[3]}, {v[4], v[5]}, {v[6], v[7]}};
+          if (p.norm) {
+            float2 sums = mul2(x[0], x[0]);
+#pragma unroll
+            for (int j = 1; j < 4; ++j) sums = fma2(x[j], x[j], sums);
+            float sum = sums.x + sums.y;
+#pragma unroll
+            for (int o = L / 2; o > 0; o /= 2) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+            const float by = rsqrtf(fmaf(sum, per_dim, p.eps));
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[j] = mul2(mul2(x[j], make_float2(by, by)), w[j]);
+          }
+          if (turns) {
+            const float4 co = *reinterpret_cast<const float4*>(&sh.cos_of[t][4 * c]), si = *reinterpret_cast<const float4*>(&sh.sin_of[t][4 * c]);
+            if (!p.interleaved) {
+              const float2 cs[2] = {{co.x, co.y}, {co.z, co.w}}, sn[2] = {{si.x, si.y}, {si.z, si.w}};
+#pragma unroll
+              for (int j = 0; j < 2; ++j) {
+                const float2 a = x[j], b = x[j + 2];
+                x[j] = fma2(a, cs[j], mul2(b, make_float2(-sn[j].x, -sn[j].y)));
+                x[j + 2] = fma2(b, cs[j], mul2(a, sn[j]));
+              }
+            } else {
+              const float cs[4] = {co.x, co.y, co.z, co.w}, sn[4] = {si.x, si.y, si.z, si.w};
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                if (4 * c + j >= p.half) continue;
+                x[j] = make_float2(fmaf(x[j].x, cs[j], -(x[j].y * sn[j])), fmaf(x[j].y, cs[j], x[j].x * sn[j]));
+              }
+            }
+          }
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            if constexpr (DT == KB_F32) {
+              raw[u][2 * j] = __float_as_uint(x[j].x);
+              raw[u][2 * j + 1] = __float_as_uint(x[j].y);
+            } else {
+              raw[u][j] = pack2<DT>(x[j].x, x[j].y);
+            }
+          }
+        }
+        if (!mine) continue;
         Vec a, b;
         words_vec(raw[u], a);
         words_vec(raw[u] + kWords / 2, b);
-        *reinterpret_cast<Vec*>(to + ea * kBytes) = a;
-        *reinterpret_cast<Vec*>(to + eb * kBytes) = b;
-      };
-      if (is_q || is_k) {
-        float v[8];
-        if constexpr (DT == KB_F32) {
-#pragma unroll
-          for (int j = 0; j < 8; ++j) v[j] = __uint_as_float(raw[u][j]);
-        } else {
-          Elem<DT>::decode(make_uint4(raw[u][0], raw[u][1], raw[u][2], raw[u][3]), v);
+        if (to) {
+          *reinterpret_cast<Vec*>(to) = a;
+          *reinterpret_cast<Vec*>(to + other) = b;
+          to += out_step;
         }
-        if (p.norm) {
-          float sum = 0.0f;
-          if (has) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) sum = fmaf(v[j], v[j], sum);
-          }
-#pragma unroll
-          for (int o = L / 2; o > 0; o /= 2) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
-          const float by = rsqrtf(fmaf(sum, per_dim, p.eps));
-#pragma unroll
-          for (int j = 0; j < 8; ++j) v[j] *= by * (is_q ? wq[j] : wk[j]);
-        }
-        if (c < turned) {
-          const float4 cs = *reinterpret_cast<const float4*>(&sh.cos_of[now.t][4 * c]), sn = *reinterpret_cast<const float4*>(&sh.sin_of[now.t][4 * c]);
-          const float co[4] = {cs.x, cs.y, cs.z, cs.w}, si[4] = {sn.x, sn.y, sn.z, sn.w};
-          if (!p.interleaved) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const float a = v[j], b = v[j + 4];
-              v[j] = fmaf(a, co[j], -(b * si[j]));
-              v[j + 4] = fmaf(b, co[j], a * si[j]);
-            }
-          } else {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const float a = v[2 * j], b = v[2 * j + 1];
-              if (4 * c + j >= p.half) continue;
-              v[2 * j] = fmaf(a, co[j], -(b * si[j]));
-              v[2 * j + 1] = fmaf(b, co[j], a * si[j]);
-            }
+        if (cache) {
+          const long long slot = slots[t];
+          if (slot >= 0) {
+            unsigned char* d = cache + slot * kBytes;
+            *reinterpret_cast<Vec*>(d) = a;
+            *reinterpret_cast<Vec*>(d + other) = b;
           }
         }
-        if constexpr (DT == KB_F32) {
-#pragma unroll
-          for (int j = 0; j < 8; ++j) raw[u][j] = __float_as_uint(v[j]);
-        } else {
-#pragma unroll
-          for (int j = 0; j < 4; ++j) raw[u][j] = pack2<DT>(v[2 * j], v[2 * j + 1]);
-        }
-      }
-      if (!has || head >= (is_q ? p.hq : p.hkv)) continue;
-      if (is_q) {
-        put(p.q_out, token * p.qo_row + head * p.qo_head);
-      } else if (is_k) {
-        if (p.k_out) put(p.k_out, token * p.ko_row + head * p.ko_head);
-        if (p.k_cache && sh.at_k[now.t] >= 0) put(p.k_cache, (uint64_t)sh.at_k[now.t] + head * p.kc_head);
-      } else if (sh.at_v[now.t] >= 0) {
-        put(p.v_cache, (uint64_t)sh.at_v[now.t] + head * p.vc_head);
       }
     }
   }
