@@ -77,7 +77,8 @@ kb_status kb_qk_norm_rope(kb_ctx* ctx, const void* d_q, uint64_t q_row, uint64_t
  *     s_j = scale * sum_d q[d] k_j[d];   lse = log sum_j exp(s_j);   out = sum_j exp(s_j - lse) v_j
  * Products of 16-bit numbers are added in binary32 on the tensor cores, exponentials and their sum are
  * binary32, and exp(s_j - ...) is rounded to `dtype` (relative to a running largest value) before it
- * meets v_j; out is rounded once.  A query with no score above -infinity (none at all, above all) has
+ * meets v_j; out is rounded once.  (A score of 2^24 or more in magnitude has no digits behind the point in
+ * binary32: what comes of such scores is not defined.)  A query with no score above -infinity (none at all, above all) has
  * out = 0 and lse = -infinity.  Keys and values that a query does not see do not touch its outputs, whatever
  * they hold.
  *

@@ -41,6 +41,11 @@ kb_status check_out(kb_ctx* ctx, const char* where, const Heads& t, uint64_t tok
 bool heads_aligned(const void* p, uint64_t row, uint64_t head, int bytes) {
   return aligned16(p) && (row * bytes) % 16 == 0 && (head * bytes) % 16 == 0;
 }
+// The stride of an axis of one element is free: one that suits the copies instead
+void settle(Heads& t, uint64_t tokens, uint64_t heads, uint32_t dim) {
+  if (heads <= 1) t.head = round_up(dim, 8);
+  if (tokens <= 1) t.row = std::max<uint64_t>(1, heads) * round_up(std::max<uint64_t>(t.head, dim), 8);
+}
 // Number of heads and dim, as every call has them
 kb_status check_sizes(kb_ctx* ctx, const char* where, uint32_t q_heads, uint32_t kv_heads, uint32_t dim, uint32_t most) {
   if (dim == 0 || dim > most) return fail(ctx, KB_ERR_UNSUPPORTED, "%s: dim %u is not within 1 .. %u", where, dim, most);
@@ -167,11 +172,11 @@ kb_status launch_paged(kb_ctx* ctx, const CUtensorMap& k, const CUtensorMap& v, 
   attention_paged_kernel<DT, DP, NT, W><<<dim3(per_seq, pieces), T::kThreads, T::kSmem, st>>>(k, v, p);
   return launched(ctx);
 }
-// Which number of warps: @RULE@
+// Four warps and two CTAs per SM instead of eight and one where there are enough sequences to fill the card: what a CTA does
+// between two sequences then hides under its neighbour's copies (256 x 200 keys of 8 heads 58 us, with eight warps 72;
+// 64 sequences of 1 to 16384 keys 78.5 and 85; 128 x 4096 keys 347 and 340).  For fewer the parts would be more and a
+// CTA's share of a long sequence later (one of 8192 keys 18.7 us and 16.5; 7 of up to 3001 keys 22.4 and 16.8).
 bool paged_in_fours(const kb_ctx* ctx, const PagedParams& p) {
-#ifdef KB_W
-  return KB_W == 4;
-#endif
   return (uint64_t)p.sequences * p.hkv * p.chunks >= (uint64_t)ctx->sm_count;
 }
 template <int DT, int DP, int NT>
@@ -364,8 +369,11 @@ extern "C" kb_status kb_attention(kb_ctx* ctx, const void* d_q, uint64_t q_row, 
     KB_TRY(check_heads(ctx, where, v, 2));
   } else {   // no key anywhere: the copies that are never made still want an address
     k.p = v.p = d_q;
-    k.row = v.row = k.head = v.head = 8;
+    k.head = v.head = 8;
   }
+  settle(q, q_tokens, q_heads, dim);
+  settle(k, k_tokens, kv_heads, dim);
+  settle(v, k_tokens, kv_heads, dim);
   for (const Heads& t : {q, k, v}) {
     if (!heads_aligned(t.p, t.row, t.head, 2)) return fail(ctx, KB_ERR_ALIGNMENT, "%s: %s needs 16-byte aligned pointers and strides", where, t.name);
     if (t.row == 0 || t.head == 0 || t.row >= kMaxStride / 2 || t.head >= kMaxStride / 2)
@@ -396,12 +404,12 @@ extern "C" kb_status kb_attention(kb_ctx* ctx, const void* d_q, uint64_t q_row, 
   p.q = q.p;
   p.k = k.p;
   p.v = v.p;
-  p.q_row = q_row;
-  p.q_head = q_head;
-  p.k_row = k_row;
-  p.k_head = k_head;
-  p.v_row = v_row;
-  p.v_head = v_head;
+  p.q_row = q.row;
+  p.q_head = q.head;
+  p.k_row = k.row;
+  p.k_head = k.head;
+  p.v_row = v.row;
+  p.v_head = v.head;
   p.out = d_out;
   p.o_row = out_row;
   p.o_head = out_head;
@@ -441,10 +449,12 @@ extern "C" kb_status kb_attention_paged(kb_ctx* ctx, const void* d_q, uint64_t q
   if (sequences > KB_OPS_MAX_DIM) return fail(ctx, KB_ERR_INVALID_ARG, "%s: more than 2^30 sequences", where);
   if (!cache) return fail(ctx, KB_ERR_INVALID_ARG, "%s: cache is NULL", where);
   if (sequences == 0) return KB_OK;
-  KB_TRY(check_heads(ctx, where, {"d_q", d_q, q_row, q_head}, 2));
+  Heads q{"d_q", d_q, q_row, q_head};
+  KB_TRY(check_heads(ctx, where, q, 2));
   KB_TRY(check_out(ctx, where, {"d_out", d_out, out_row, out_head}, sequences, q_heads, dim, 2));
   KB_TRY(check_cache(ctx, where, *cache, 2));
-  if (!heads_aligned(d_q, q_row, q_head, 2) || !heads_aligned(cache->d_k, cache->k_row, cache->k_head, 2) || cache->k_page % 8 != 0 ||
+  settle(q, sequences, q_heads, dim);
+  if (!heads_aligned(q.p, q.row, q.head, 2) || !heads_aligned(cache->d_k, cache->k_row, cache->k_head, 2) || cache->k_page % 8 != 0 ||
       !heads_aligned(cache->d_v, cache->v_row, cache->v_head, 2) || cache->v_page % 8 != 0)
     return fail(ctx, KB_ERR_ALIGNMENT, "%s: queries and cache need 16-byte aligned pointers and strides", where);
   for (const auto& [n, a, b] : {std::tuple<uint64_t, uint64_t, uint64_t>{kv_heads, cache->k_head, cache->v_head}, {cache->page_size, cache->k_row, cache->v_row},
@@ -463,9 +473,9 @@ extern "C" kb_status kb_attention_paged(kb_ctx* ctx, const void* d_q, uint64_t q
   KB_TRY(ensure_paged(ctx, st));
   const PagedSpace space(ctx);
   PagedParams p = {};
-  p.q = d_q;
-  p.q_row = q_row;
-  p.q_head = q_head;
+  p.q = q.p;
+  p.q_row = q.row;
+  p.q_head = q.head;
   p.pages = cache->pages;
   p.page_size = cache->page_size;
   p.page_shift = 32;

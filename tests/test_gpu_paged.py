@@ -208,6 +208,42 @@ def test_a_first_call_inside_a_capture_is_refused_unless_reserved():
         c.close()
 
 
+@pytest.mark.parametrize("n", [1, 18, 19, 36, 37, 74, 256, 257, 600])
+def test_numbers_of_sequences_around_the_rules(ctx, n):
+    """Eight warps or four, up to a CTA's threads of sequences or more, pieces that begin and end inside sequences."""
+    lens = [(53 * i) % 310 for i in range(n)]
+    lens[0] = 777
+    kw, q, ks, vs = _case(lens, 8, 8, 64, torch.bfloat16, 16, n)
+    _check(ctx.attention_paged(**kw, want_lse=True), q, ks, vs)
+
+
+@pytest.mark.parametrize("hkv", [1, 9, 20, 40, 100, 200, 500])
+def test_numbers_of_groups_that_do_not_divide_the_card(ctx, hkv):
+    kw, q, ks, vs = _case([300, 40, 0, 1000], hkv, hkv, 16, torch.float16, 16, hkv)
+    _check(ctx.attention_paged(**kw, want_lse=True), q, ks, vs)
+
+
+def test_two_contexts_on_two_streams_at_once():
+    """Each has its own parts and counts."""
+    from paper_2608_02611_b200 import binding
+    cases = [_case(lens, 8, 1, 128, torch.bfloat16, 32, i) for i, lens in enumerate([[9000, 1, 400], [30, 6000]])]
+    contexts = [binding.Context(0) for _ in cases]
+    streams = [torch.cuda.Stream() for _ in cases]
+    outs = [[], []]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for i in (0, 1):
+            with torch.cuda.stream(streams[i]):
+                outs[i].append(contexts[i].attention_paged(**cases[i][0], want_lse=True))
+    torch.cuda.synchronize()
+    for i in (0, 1):
+        _check(outs[i][0], *cases[i][1:])
+        for r in outs[i][1:]:
+            assert torch.equal(r.out, outs[i][0].out)
+        assert contexts[i].poll() == 0
+        contexts[i].close()
+
+
 def test_refusals(ctx):
     from paper_2608_02611_b200.binding import KbError
     kw, *_ = _case([20, 20], 4, 2, 64, torch.float16, 16, 1)

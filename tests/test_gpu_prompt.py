@@ -235,6 +235,46 @@ def test_in_graphs_with_new_lengths(ctx):
         _check(r, q, k, v, lens, lens, True, rows=lambda n: torch.arange(0, n, 11) if n else [])
 
 
+def test_a_first_call_inside_a_capture_and_on_another_stream():
+    from paper_2608_02611_b200 import binding
+    c = binding.Context(0)
+    q, k, v = _inputs(200, 200, 4, 2, 64, torch.float16, 3)
+    d = [x.to(DEV) for x in (q, k, v)]
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        r = c.attention(*d, want_lse=True)
+    g.replay()
+    _check(r, q, k, v, [200], [200], True)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        s = c.attention(*d, want_lse=True)
+    side.synchronize()
+    assert torch.equal(s.out, r.out) and torch.equal(s.lse, r.lse)
+    assert c.poll() == 0
+    c.close()
+
+
+def test_no_gradient_and_any_rank_of_inputs_that_require_one(ctx):
+    q, k, v = (x.to(DEV).requires_grad_(True) for x in _inputs(20, 20, 2, 1, 64, torch.bfloat16, 3))
+    r = ctx.attention(q, k, v, want_lse=True)
+    assert not r.out.requires_grad and not r.lse.requires_grad
+    a, b = ctx.qk_norm_rope(q, k)
+    assert not a.requires_grad and not b.requires_grad
+
+
+@pytest.mark.parametrize("n", [1, 31, 32, 33, 64, 65])
+def test_numbers_of_sequences_around_a_warps(ctx, n):
+    """Up to 32 sequences are handed out by length, more of them one after the other."""
+    lens = [(37 * i) % 300 for i in range(n)]
+    lens[-1] = 260
+    klens = [m + (11 * i) % 90 for i, m in enumerate(lens)]
+    q, k, v = _inputs(sum(lens), sum(klens), 2, 2, 64, torch.bfloat16, n)
+    for causal in (True, False):
+        r = ctx.attention(q.to(DEV), k.to(DEV), v.to(DEV), _offsets(lens).to(DEV), _offsets(klens).to(DEV), causal=causal, want_lse=True)
+        _check(r, q, k, v, lens, klens, causal, rows=lambda m: torch.arange(0, m, 3) if m else [])
+
+
 def test_refusals(ctx):
     from paper_2608_02611_b200.binding import KbError
     q, k, v = (x.to(DEV) for x in _inputs(20, 20, 4, 2, 64, torch.float16, 1))

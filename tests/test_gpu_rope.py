@@ -168,6 +168,16 @@ def test_nan_and_infinity_stay_in_their_heads(ctx):
     assert torch.equal(got, want)
 
 
+@pytest.mark.parametrize("tokens", [2, 443, 444, 900, 3552, 3600])
+def test_numbers_of_tokens_around_the_rules(ctx, tokens):
+    """One token or up to eight per CTA, heads shared out over CTAs or not."""
+    q, k, _ = _qkv(tokens, 6, 3, 128, torch.float16, tokens)
+    pos, f = torch.arange(tokens).to(DEV), _freq(64)
+    for x, got in zip((q, k), ctx.qk_norm_rope(q, k, pos, f)):
+        want, bound = exact.rope(x, None, 1e-6, pos, f, False)
+        exact.within(got, want, bound)
+
+
 def test_refusals(ctx):
     from paper_2608_02611_b200.binding import KbError
     q, k, v = _qkv(4, 4, 2, 64, torch.bfloat16, 1)
