@@ -74,10 +74,9 @@ kb_status launch_rope(kb_ctx* ctx, const RopeParams& p, bool vec, cudaStream_t s
   const uint64_t grid = (p.tokens + per - 1) / per;
   const uint32_t heads = p.hq + 2 * p.hkv, turns = (heads * L + kRopeThreads - 1) / kRopeThreads;   // of a CTA's warps through a token
   if (vec)
-    qk_norm_rope_kernel<DT, L><<<dim3((unsigned int)grid, (unsigned int)std::min<uint64_t>(turns, (fill + grid - 1) / grid)), kRopeThreads, 0, st>>>(p, per);
-  else
-    qk_norm_rope_plain_kernel<DT, L><<<(unsigned int)grid, kRopeThreads, 0, st>>>(p, per);
-  return launched(ctx);
+    return launch_dependent(ctx, qk_norm_rope_kernel<DT, L>, dim3((unsigned int)grid, (unsigned int)std::min<uint64_t>(turns, (fill + grid - 1) / grid)),
+                            kRopeThreads, 0, st, p, per);
+  return launch_dependent(ctx, qk_norm_rope_plain_kernel<DT, L>, dim3((unsigned int)grid), kRopeThreads, 0, st, p, per);
 }
 template <int DT>
 kb_status launch_rope(kb_ctx* ctx, const RopeParams& p, bool vec, cudaStream_t st) {
@@ -169,8 +168,7 @@ kb_status launch_paged(kb_ctx* ctx, const CUtensorMap& k, const CUtensorMap& v, 
   const uint64_t most_units = (uint64_t)paged_units(paged_length(0x7FFFFFFF, p.max_pages, p.page_size), 16 * W) * p.sequences;
   if (most_units > 0x7FFFFFFFull) return fail(ctx, KB_ERR_UNSUPPORTED, "kb_attention_paged: sequences * max_pages * page_size is beyond 2^37");
   const uint32_t per_seq = p.hkv * p.chunks, pieces = paged_pieces((uint64_t)ctx->sm_count * T::kPerSm, per_seq, most_units);
-  attention_paged_kernel<DT, DP, NT, W><<<dim3(per_seq, pieces), T::kThreads, T::kSmem, st>>>(k, v, p);
-  return launched(ctx);
+  return launch_dependent(ctx, attention_paged_kernel<DT, DP, NT, W>, dim3(per_seq, pieces), T::kThreads, T::kSmem, st, k, v, p);
 }
 // Four warps and two CTAs per SM instead of eight and one where there are enough sequences to fill the card: what a CTA does
 // between two sequences then hides under its neighbour's copies (256 x 200 keys of 8 heads 58 us, with eight warps 72;
@@ -230,8 +228,7 @@ kb_status prepare_prompt(kb_ctx* ctx) {
 template <int DT, int DP>
 kb_status launch_prompt(kb_ctx* ctx, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const PromptParams& p,
                         unsigned int grid, cudaStream_t st) {
-  attention_kernel<DT, DP><<<grid, PromptTile<DP>::kThreads, PromptTile<DP>::kSmem, st>>>(q, k, v, p);
-  return launched(ctx);
+  return launch_dependent(ctx, attention_kernel<DT, DP>, dim3(grid), PromptTile<DP>::kThreads, PromptTile<DP>::kSmem, st, q, k, v, p);
 }
 
 }  // namespace

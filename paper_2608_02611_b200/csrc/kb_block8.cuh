@@ -14,6 +14,13 @@
 
 namespace kb {
 
+// A kernel launched as a dependent of the one before it on its stream (launch_dependent) runs up to here while that one
+// ends, and reads and writes no global memory before; in turn it lets the next one begin.  The wait ends when
+// everything before this kernel is over and visible.
+__device__ __forceinline__ void after_the_kernel_before() {
+  asm volatile("griddepcontrol.launch_dependents;\ngriddepcontrol.wait;" ::: "memory");
+}
+
 constexpr uint32_t kGroup = 256;
 
 template <bool VEC>

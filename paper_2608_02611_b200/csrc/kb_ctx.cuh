@@ -248,6 +248,24 @@ inline kb_status launched(kb_ctx* ctx) {
   return KB_OK;
 }
 
+// Launches a kernel that begins with after_the_kernel_before(): its start overlaps the end of the kernel before it on
+// the stream, whatever that one is.
+template <class... Params, class... Args>
+kb_status launch_dependent(kb_ctx* ctx, void (*kernel)(Params...), dim3 grid, int threads, size_t smem, cudaStream_t st, const Args&... args) {
+  cudaLaunchConfig_t cfg = {};
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cfg.attrs = attr;
+  cfg.numAttrs = ctx->dependent_launch ? 1 : 0;
+  KB_CUDA(ctx, cudaLaunchKernelEx(&cfg, kernel, args...));
+  return launched(ctx);
+}
+
 // The driver's encoder of tensor maps, looked up at first use.
 using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,

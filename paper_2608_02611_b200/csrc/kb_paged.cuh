@@ -147,6 +147,7 @@ __global__ void __launch_bounds__(32 * W, 8 / W)
     prefetch_map(&map_k);
     prefetch_map(&map_v);
   }
+  after_the_kernel_before();
   const uint32_t item = blockIdx.x, per_seq = gridDim.x, hk = item / p.chunks, h0 = hk * p.group + item % p.chunks * kHeads;
   const uint32_t heads = min((uint32_t)kHeads, (hk + 1) * p.group - h0);   // query heads h0 .. of this CTA
 

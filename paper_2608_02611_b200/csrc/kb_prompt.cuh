@@ -73,16 +73,15 @@ static_assert(PromptTile<128>::kSmem <= 227 * 1024 - 1024, "shared memory");
 // their place plus nk - nq.
 __host__ __device__ __forceinline__ uint32_t prompt_steps(uint32_t row, uint32_t rows, uint32_t nq, uint32_t nk, bool causal) {
   if (row >= nq || rows == 0) return 0;
-  const uint32_t last = row + rows < nq ? row + rows - 1 : nq - 1;
-  long long seen = nk;
-  if (causal && (long long)last + nk - nq + 1 < seen) seen = (long long)last + nk - nq + 1;
-  return seen <= 0 ? 0u : (uint32_t)((seen + kPromptKeys - 1) / kPromptKeys);
+  const int last = (int)(row + rows < nq ? row + rows : nq);           // all of these are at most 2^30
+  const int seen = causal ? min(last + (int)nk - (int)nq, (int)nk) : (int)nk;
+  return seen <= 0 ? 0u : ((uint32_t)seen + kPromptKeys - 1) / kPromptKeys;
 }
 // Keys that query `row` sees
 __host__ __device__ __forceinline__ uint32_t prompt_seen(uint32_t row, uint32_t nq, uint32_t nk, bool causal) {
   if (!causal) return nk;
-  const long long seen = (long long)row + nk - nq + 1;
-  return seen <= 0 ? 0u : seen < nk ? (uint32_t)seen : nk;
+  const int seen = (int)(row + 1) + (int)nk - (int)nq;
+  return seen <= 0 ? 0u : min((uint32_t)seen, nk);
 }
 
 __device__ __forceinline__ float max_nan(float a, float b) {   // NaN if either is
@@ -277,14 +276,16 @@ __device__ __forceinline__ void prompt_find(const PromptParams& p, PromptSequenc
 __device__ __noinline__ void hand_out_items(const PromptParams& p, PromptSequences q, uint32_t units, int lane, PromptItem* items, uint64_t* item_full,
                                             uint64_t* item_empty, uint64_t* want, volatile unsigned int* abort_flag) {
   const uint32_t total = q.total * units;
+  const double per_unit = 1.0 / (double)units;
   uint32_t number = blockIdx.x;
 #pragma unroll 1
   for (uint32_t taken = 0;;) {
     const uint32_t slot = taken & 1;
     PromptItem x = {};
     if (number < total) {
-      prompt_find(p, q, number / units, lane, x);
-      x.head0 = number % units * (p.pair ? 2 : 1);
+      const uint32_t it = (uint32_t)(((double)number + 0.5) * per_unit);   // number / units
+      prompt_find(p, q, it, lane, x);
+      x.head0 = (number - it * units) * (p.pair ? 2 : 1);
       x.n[0] = prompt_steps(x.row0, 128, x.nq, x.nk, p.causal);
       x.n[1] = p.pair ? x.n[0] : prompt_steps(x.row0 + 128, 128, x.nq, x.nk, p.causal);
       x.steps = max(x.n[0], x.n[1]);
@@ -355,6 +356,7 @@ __global__ void __launch_bounds__(PromptTile<DP>::kThreads, 1)
     mbar_fence_init();
   }
   if (warp == 1) tmem_alloc<1>(&tmem_base, T::kTmemCols);
+  after_the_kernel_before();
   const uint32_t units = p.pair ? p.hq / 2 : p.hq;
   PromptSequences q;
   if (warp == 5) prompt_begin(p, q, lane, blockIdx.x == 0);

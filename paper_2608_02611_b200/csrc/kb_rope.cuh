@@ -132,6 +132,7 @@ __global__ void __launch_bounds__(kRopeThreads, 4) qk_norm_rope_kernel(const Rop
   const uint32_t eb = p.interleaved || !turns ? ea + 4 : p.half + 4 * c;
   const float per_dim = 1.0f / (float)p.dim;
   bool begun = false;
+  after_the_kernel_before();
 
 #pragma unroll 1
   for (uint32_t piece = blockIdx.y * kWarps + warp; piece < pieces || !begun; piece += kWarps * gridDim.y) {
@@ -262,6 +263,7 @@ __global__ void __launch_bounds__(kRopeThreads) qk_norm_rope_plain_kernel(const 
   const uint64_t t0 = (uint64_t)blockIdx.x * per_cta;
   const uint32_t ntok = (uint32_t)min((uint64_t)per_cta, p.tokens - t0), c = threadIdx.x % L, slot = threadIdx.x / L;
   float* row = swap + slot * (L * 8);
+  after_the_kernel_before();
   rope_begin(p, sh, t0, ntok);
   __syncthreads();
   const uint32_t first = p.q_out ? 0 : p.hq, rows = p.hq + (p.k_out || p.k_cache ? p.hkv : 0) + (p.k_cache ? p.hkv : 0);

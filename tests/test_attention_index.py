@@ -26,7 +26,7 @@ def test_index_functions_of_the_kernels(tmp_path):
 @pytest.mark.parametrize("header,have,want", [
     ("kb_paged.cuh", "return g ^ ((g & 1) << 2);", "return g ^ ((g & 1) << 1);"),
     ("kb_paged.cuh", "return u < bigger ? u / (size + 1) : more + (u - bigger) / size;", "return u / (size + 1);"),
-    ("kb_prompt.cuh", "const long long seen = (long long)row + nk - nq + 1;", "const long long seen = (long long)row + nk - nq;"),
+    ("kb_prompt.cuh", "const int seen = (int)(row + 1) + (int)nk - (int)nq;", "const int seen = (int)row + (int)nk - (int)nq;"),
     ("kb_rope.cuh", "const double part = t - floor(t);", "const double part = t - (double)(long long)t;"),
 ])
 def test_a_changed_index_is_noticed(tmp_path, header, have, want):
