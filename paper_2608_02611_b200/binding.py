@@ -647,9 +647,11 @@ def _native():
         if _kb_torch.built_for != native_marker():
             raise ImportError(f"_kb_torch.so was built for {_kb_torch.built_for}, this is {native_marker()}: build it again "
                               "(python -m paper_2608_02611_b200.build)")
-        _kb_torch.bind(KbError, *[ctypes.cast(getattr(L, name), ctypes.c_void_p).value for name in (
-            "kb_quantize_blocks", "kb_layernorm", "kb_layernorm_backward", "kb_matmul_blocks", "kb_last_error",
-            "kb_qk_norm_rope", "kb_attention", "kb_attention_paged")])
+        def addresses(*names):
+            return [ctypes.cast(getattr(L, name), ctypes.c_void_p).value for name in names]
+        _kb_torch.bind(KbError, *addresses("kb_quantize_blocks", "kb_layernorm", "kb_layernorm_backward", "kb_matmul_blocks",
+                                           "kb_last_error"))
+        _kb_torch.bind_attention(*addresses("kb_qk_norm_rope", "kb_attention", "kb_attention_paged"))
         _native_module = _kb_torch
     return _native_module
 

@@ -23,10 +23,12 @@ struct {
   decltype(&::kb_layernorm_backward) layernorm_backward;
   decltype(&::kb_matmul_blocks) matmul_blocks;
   decltype(&::kb_last_error) last_error;
+} g_lib;
+struct {
   decltype(&::kb_qk_norm_rope) qk_norm_rope;
   decltype(&::kb_attention) attention;
   decltype(&::kb_attention_paged) attention_paged;
-} g_lib;
+} g_attention;
 
 struct Refused {};             // a Python exception is set
 
@@ -459,7 +461,7 @@ PyObject* qk_norm_rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (qo.defined()) oq = heads_of(c, qo, "q_out");
     if (ko.defined()) ok = heads_of(c, ko, "k_out");
     c.run([&] {
-      return g_lib.qk_norm_rope(c.ctx, hq.p, hq.row, hq.head, (uint32_t)hq.heads, hk.p, hk.row, hk.head, (uint32_t)hk.heads,
+      return g_attention.qk_norm_rope(c.ctx, hq.p, hq.row, hq.head, (uint32_t)hq.heads, hk.p, hk.row, hk.head, (uint32_t)hk.heads,
                                 hq.tokens, (uint32_t)hq.dim, (kb_dtype)code_of(type), norm, wq, wk, (kb_dtype)code_of(params),
                                 (float)eps, positions, inv_freq, rotary, interleaved, oq.p, oq.row, oq.head, ok.p, ok.row,
                                 ok.head, hv.p, hv.row, hv.head, cached ? &cache : nullptr, slots, c.stream);
@@ -507,7 +509,7 @@ PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
     float* lp = want_lse ? lse.data_ptr<float>() : nullptr;
     const uint32_t count = count32(c, sequences, "sequences");
     c.run([&] {
-      return g_lib.attention(c.ctx, hq.p, hq.row, hq.head, (uint32_t)hq.heads, hq.tokens, hk.p, hk.row, hk.head, hv.p, hv.row,
+      return g_attention.attention(c.ctx, hq.p, hq.row, hq.head, (uint32_t)hq.heads, hq.tokens, hk.p, hk.row, hk.head, hv.p, hv.row,
                              hv.head, (uint32_t)hk.heads, hk.tokens, (uint32_t)hq.dim, (kb_dtype)code_of(type), qo, ko, count,
                              causal, (float)scale, ho.p, ho.row, ho.head, lp, c.stream);
     });
@@ -542,7 +544,7 @@ PyObject* attention_paged(PyObject*, PyObject* const* a, Py_ssize_t n) {
     kb_paged_cache held = cache;
     if (held.pages == 0) held.d_k = some(held.d_k), held.d_v = some(held.d_v);
     c.run([&] {
-      return g_lib.attention_paged(c.ctx, hq.p, hq.row, hq.head, (uint32_t)hq.heads, &held, (uint32_t)hkv, (uint32_t)hq.dim,
+      return g_attention.attention_paged(c.ctx, hq.p, hq.row, hq.head, (uint32_t)hq.heads, &held, (uint32_t)hkv, (uint32_t)hq.dim,
                                    (kb_dtype)code_of(type), tp, table_row, most, lens, sequences, (float)scale, ho.p, ho.row,
                                    ho.head, lp, c.stream);
     });
@@ -550,19 +552,30 @@ PyObject* attention_paged(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// Sets the entry points of `table` to the addresses a[0], a[1], ..
+template <typename Table>
+void set_entries(Table& table, PyObject* const* a) {
+  void* p[sizeof table / sizeof(void*)];
+  for (size_t i = 0; i < sizeof p / sizeof *p; ++i) {
+    p[i] = PyLong_AsVoidPtr(a[i]);
+    if (!p[i]) throw Refused{};
+  }
+  static_assert(sizeof p == sizeof table, "one address per entry point");
+  std::memcpy(&table, p, sizeof p);
+}
 // (error class, addresses of the entry points in the order of g_lib)
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  constexpr int kEntries = sizeof g_lib / sizeof(void*);
-  return guarded(n, 1 + kEntries, [&]() -> PyObject* {
-    void* p[kEntries];
-    for (int i = 0; i < kEntries; ++i) {
-      p[i] = PyLong_AsVoidPtr(a[1 + i]);
-      if (!p[i]) throw Refused{};
-    }
-    static_assert(sizeof p == sizeof g_lib, "one address per entry point");
-    std::memcpy(&g_lib, p, sizeof p);
+  return guarded(n, 1 + sizeof g_lib / sizeof(void*), [&]() -> PyObject* {
+    set_entries(g_lib, a + 1);
     Py_INCREF(a[0]);
     Py_XSETREF(g_error, a[0]);
+    Py_RETURN_NONE;
+  });
+}
+// (addresses of the entry points in the order of g_attention)
+PyObject* bind_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, sizeof g_attention / sizeof(void*), [&]() -> PyObject* {
+    set_entries(g_attention, a);
     Py_RETURN_NONE;
   });
 }
@@ -576,6 +589,7 @@ PyMethodDef methods[] = {KB_FAST(quantize_blocks),
                          KB_FAST(attention),
                          KB_FAST(attention_paged),
                          KB_FAST(bind),
+                         KB_FAST(bind_attention),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_kb_torch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
