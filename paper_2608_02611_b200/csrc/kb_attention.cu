@@ -72,7 +72,7 @@ kb_status launch_rope(kb_ctx* ctx, const RopeParams& p, bool vec, cudaStream_t s
   const uint64_t fill = 3ull * ctx->sm_count;
   const uint32_t per = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(kRopeTokens, p.tokens / fill));
   const uint64_t grid = (p.tokens + per - 1) / per;
-  const uint32_t heads = p.hq + 2 * p.hkv, turns = (heads * L + kRopeThreads - 1) / kRopeThreads;   // of a CTA's warps through a token
+  const uint64_t turns = ((p.hq + 2ull * p.hkv) * L + kRopeThreads - 1) / kRopeThreads;   // of a CTA's warps through a token
   if (vec)
     return launch_dependent(ctx, qk_norm_rope_kernel<DT, L>, dim3((unsigned int)grid, (unsigned int)std::min<uint64_t>(turns, (fill + grid - 1) / grid)),
                             kRopeThreads, 0, st, p, per);
@@ -147,15 +147,16 @@ kb_status prepare_paged(kb_ctx* ctx) {
   ctx->paged_ready = true;
   return KB_OK;
 }
-// Tensor map of a cache [pages][page size][heads][dim], boxes of 64 elements of a head and `box` keys of a page
+// Tensor map of a cache [pages][page size][heads][dim], as elements of a head, keys of a page, pieces of a head (of 64 elements, or
+// one of all), heads, pages; boxes of 64 elements, `box_rows` keys and all pieces.
 kb_status encode_cache(kb_ctx* ctx, CUtensorMap* map, const void* d, uint64_t page, uint64_t row, uint64_t head, const kb_paged_cache& c,
-                       uint32_t heads, uint32_t dim, kb_dtype dtype, uint32_t box_rows) {
+                       uint32_t heads, uint32_t dim, kb_dtype dtype, uint32_t box_rows, uint32_t pieces) {
   const uint64_t any = round_up(dim, 8);   // the stride of an axis of one element is free
-  const cuuint64_t dims[4] = {dim, heads, c.page_size, std::max<uint64_t>(c.pages, 1)};
-  const cuuint64_t strides[3] = {(heads > 1 ? head : any) * 2, (c.page_size > 1 ? row : any) * 2, (c.pages > 1 ? page : any) * 2};
-  const cuuint32_t box[4] = {64, 1, box_rows, 1}, step[4] = {1, 1, 1, 1};
+  const cuuint64_t dims[5] = {dim / pieces, c.page_size, pieces, heads, std::max<uint64_t>(c.pages, 1)};
+  const cuuint64_t strides[4] = {(c.page_size > 1 ? row : any) * 2, 128, (heads > 1 ? head : any) * 2, (c.pages > 1 ? page : any) * 2};
+  const cuuint32_t box[5] = {64, box_rows, pieces, 1, 1}, step[5] = {1, 1, 1, 1, 1};
   const CUresult rc = reinterpret_cast<EncodeTiled>(ctx->encode_tiled)(
-      map, dtype == KB_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(d), dims, strides,
+      map, dtype == KB_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, const_cast<void*>(d), dims, strides,
       box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
       CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   if (rc != CUDA_SUCCESS) return fail(ctx, KB_ERR_CUDA, "cuTensorMapEncodeTiled failed with %d for a cache", (int)rc);
@@ -480,6 +481,9 @@ extern "C" kb_status kb_attention_paged(kb_ctx* ctx, const void* d_q, uint64_t q
     if (p.page_size == 1u << i) p.page_shift = i;
   p.box = 16;
   while (p.page_size % p.box) p.box /= 2;
+  // one copy brings all of 16 keys where their pieces of 64 elements follow one another as the kernel wants them
+  const uint32_t whole = p.box == 16 && dim % 64 == 0 ? dim / 64 : 1;
+  p.copies = (dim + 63) / 64 / whole;
   p.max_pages = max_pages;
   p.table = d_table;
   p.table_row = table_row;
@@ -501,7 +505,7 @@ extern "C" kb_status kb_attention_paged(kb_ctx* ctx, const void* d_q, uint64_t q
   p.arrived = reinterpret_cast<unsigned int*>(ctx->paged_ws + space.arrived);
   p.status = ctx->d_status;
   CUtensorMap map_k, map_v;
-  KB_TRY(encode_cache(ctx, &map_k, cache->d_k, cache->k_page, cache->k_row, cache->k_head, *cache, kv_heads, dim, dtype, p.box));
-  KB_TRY(encode_cache(ctx, &map_v, cache->d_v, cache->v_page, cache->v_row, cache->v_head, *cache, kv_heads, dim, dtype, p.box));
+  KB_TRY(encode_cache(ctx, &map_k, cache->d_k, cache->k_page, cache->k_row, cache->k_head, *cache, kv_heads, dim, dtype, p.box, whole));
+  KB_TRY(encode_cache(ctx, &map_v, cache->d_v, cache->v_page, cache->v_row, cache->v_head, *cache, kv_heads, dim, dtype, p.box, whole));
   return dtype == KB_F16 ? launch_paged<KB_F16>(ctx, map_k, map_v, p, st) : launch_paged<KB_BF16>(ctx, map_k, map_v, p, st);
 }

@@ -10,7 +10,7 @@
 // last adds the parts up in the order of the keys.
 //
 // A warp takes 16 keys of a step at a time, which a ring of its own in shared memory gets by tensor-map copies
-// (boxes of 64 elements and up to 16 keys of a page in the 128-byte swizzle), kPagedStages tiles ahead and
+// (boxes of up to 16 keys of a page, 64 elements after another, in the 128-byte swizzle), kPagedStages tiles ahead and
 // on into the next sequence: 192 KB are on their way per SM at dim 128.  Straight from global memory into
 // registers, with 16 warps per SM, 128 x 4096 keys of 8 heads took 486 us.  From there they go into warp-wide
 // matrix instructions without any rearrangement, because the order of a contraction and of an operand's rows is
@@ -45,6 +45,7 @@ struct PagedParams {
   uint64_t pages;
   uint32_t page_size, page_shift, max_pages;   // page_shift: log2 of page_size, 32 where it is no power of two
   uint32_t box;                             // keys of a copy: 16, or the power of two that divides page_size
+  uint32_t copies;                          // of the keys' 64 elements each: 1 where a copy takes all of whole 64s
   const int* table;
   uint64_t table_row;
   const int* lengths;
@@ -258,10 +259,10 @@ __global__ void __launch_bounds__(32 * W, 8 / W)
       const int page = __shfl_sync(0xFFFFFFFFu, pages, whole ? (p_key - pages_at) / kStepKeys : i);
       if (((mask >> i) & 1u) == 0) continue;
       const int row = (int)(p_key + i - by_page(p_key + i) * p.page_size);
-#pragma unroll
-      for (int c = 0; c < kC; ++c) {
-        tma_load_4d(to + c * 2048 + i * 128, &map_k, c * 64, (int)hk, row, page, bar);
-        tma_load_4d(to + T::kHalf + c * 2048 + i * 128, &map_v, c * 64, (int)hk, row, page, bar);
+#pragma unroll 1
+      for (uint32_t c = 0; c < p.copies; ++c) {
+        tma_load_5d(to + c * 2048 + i * 128, &map_k, (int)(c * 64), row, 0, (int)hk, page, bar);
+        tma_load_5d(to + T::kHalf + c * 2048 + i * 128, &map_v, (int)(c * 64), row, 0, (int)hk, page, bar);
       }
     }
     ++issued;
@@ -507,8 +508,10 @@ __global__ void __launch_bounds__(32 * W, 8 / W)
         __threadfence();                                                // the CTA's part is there before it is counted
         unsigned int* count = p.arrived + c0[which] * per_seq + item;   // a sequence that goes on is the last of the piece it began in
         const bool all = atomicAdd(count, 1u) == parts[which] - 1;
-        if (all) *count = 0u;                                           // as the next call expects it
-        __threadfence();
+        if (all) {
+          *count = 0u;                                                  // as the next call expects it
+          __threadfence();
+        }
         join_word[which] = all;
       }
     }

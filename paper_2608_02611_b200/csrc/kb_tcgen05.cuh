@@ -240,12 +240,12 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst_smem, const CUtensorMap
       "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
       : "memory");
 }
-__device__ __forceinline__ void tma_load_4d(uint32_t dst_smem, const CUtensorMap* map, int x, int y, int z, int w, uint32_t bar) {
+__device__ __forceinline__ void tma_load_5d(uint32_t dst_smem, const CUtensorMap* map, int x, int y, int z, int w, int v, uint32_t bar) {
   asm volatile(
       "{\n.reg .pred one;\nelect.sync _|one, 0xFFFFFFFF;\n"
-      "@one cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes "
-      "[%0], [%1, {%2, %3, %4, %5}], [%6];\n}" ::"r"(dst_smem),
-      "l"(map), "r"(x), "r"(y), "r"(z), "r"(w), "r"(bar)
+      "@one cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes "
+      "[%0], [%1, {%2, %3, %4, %5, %6}], [%7];\n}" ::"r"(dst_smem),
+      "l"(map), "r"(x), "r"(y), "r"(z), "r"(w), "r"(v), "r"(bar)
       : "memory");
 }
 __device__ __forceinline__ void prefetch_map(const CUtensorMap* map) {

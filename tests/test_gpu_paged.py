@@ -74,9 +74,10 @@ def test_against_64_bits(ctx, dtype, dim, hq, hkv):
 
 @pytest.mark.parametrize("page", [1, 5, 8, 16, 24, 48, 100, 128, 1024])
 @pytest.mark.parametrize("heads_first", [False, True])
-def test_pages_of_any_size_and_order(ctx, page, heads_first):
+@pytest.mark.parametrize("dim", [64, 96, 128])
+def test_pages_of_any_size_and_order(ctx, page, heads_first, dim):
     lens = [1, page, page + 1, 2 * page - 1 or 1, 333, 1000]
-    kw, q, ks, vs = _case(lens, 8, 2, 64, torch.bfloat16, page, page, heads_first=heads_first)
+    kw, q, ks, vs = _case(lens, 8, 2, dim, torch.bfloat16, page, page, heads_first=heads_first)
     _check(ctx.attention_paged(**kw, want_lse=True), q, ks, vs)
 
 
