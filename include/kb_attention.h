@@ -57,7 +57,8 @@ typedef struct {
  *   d_q_out          DEVICE heads, or NULL.  May be d_q itself, with the same strides.
  *   d_k_out          the same for the keys.
  *   cache, d_slots   NULL, or where the turned keys and the values d_v go as well: DEVICE [tokens] slots;
- *                    a negative one stores nothing.  Slots that come twice hold one of the tokens.
+ *                    a negative one stores nothing.  Each slot comes once; in one that comes twice
+ *                    the elements are one token's or the other's, each by itself.
  *   d_v              DEVICE heads of the values; NULL without a cache.
  * At least one of d_q_out, d_k_out and cache is not NULL. */
 kb_status kb_qk_norm_rope(kb_ctx* ctx, const void* d_q, uint64_t q_row, uint64_t q_head, uint32_t q_heads,
@@ -84,10 +85,10 @@ kb_status kb_qk_norm_rope(kb_ctx* ctx, const void* d_q, uint64_t q_row, uint64_t
  *
  *   d_q              DEVICE heads of `dtype` (KB_F16 or KB_BF16), q_tokens of them.
  *   d_k, d_v         DEVICE heads, k_tokens of them.  Pointers of q, k and v 16-byte aligned, row and head
- *                    strides multiples of 8; dim a multiple of 8 up to 128.
+ *                    strides multiples of 8, not 0, less than 2^39; dim a multiple of 8 up to 128.
  *   d_q_offsets, d_k_offsets  DEVICE [sequences + 1], ascending, within 0 .. q_tokens (k_tokens); both
  *                    NULL for one sequence of all tokens.  Queries outside every sequence are not written.
- *   scale            finite and > 0.
+ *   scale            > 0, at most 2^127.
  *   d_out            DEVICE heads of `dtype`; does not overlap the inputs.
  *   d_lse            DEVICE binary32 [q_tokens][q_heads]; NULL: not written. */
 kb_status kb_attention(kb_ctx* ctx, const void* d_q, uint64_t q_row, uint64_t q_head, uint32_t q_heads,
@@ -103,10 +104,12 @@ kb_status kb_attention(kb_ctx* ctx, const void* d_q, uint64_t q_row, uint64_t q_
  * of sequence s is in slot table[s][j / page_size] * page_size + j % page_size of the cache.
  *
  *   d_q              DEVICE heads [sequences][q_heads][dim] of `dtype` (KB_F16 or KB_BF16).
- *   cache            pointers 16-byte aligned, strides multiples of 8; dim a multiple of 8 up to 128.
+ *   cache            pointers 16-byte aligned, strides multiples of 8, not 0, less than 2^39; dim a multiple
+ *                    of 8 up to 128.
  *   d_table          DEVICE [sequences][max_pages], row stride table_row; entries past a sequence's last
  *                    page are not looked at.
- *   d_lengths        DEVICE [sequences], 0 .. max_pages * page_size (the new token's own key included).
+ *   d_lengths        DEVICE [sequences], 0 .. max_pages * page_size (the new token's own key included);
+ *                    sequences * max_pages * page_size at most 2^36.
  *   d_out, d_lse     DEVICE heads [sequences][q_heads][dim]; binary32 [sequences][q_heads] or NULL.
  * Keys on a page outside the cache, or past max_pages, are left out.  Long sequences are divided over
  * the card; the parts meet in a workspace of the context whose size no call changes: the first call

@@ -15,6 +15,7 @@ using namespace kb;
 namespace {
 
 constexpr uint64_t kMaxStride = 1ull << 40;   // elements
+constexpr double kLog2e = 1.4426950408889634;
 
 // Heads of a batch, [tokens][heads][dim]: not null, element-aligned, strides that an address can hold.
 struct Heads {
@@ -167,7 +168,7 @@ template <int DT, int DP, int NT, int W>
 kb_status launch_paged(kb_ctx* ctx, const CUtensorMap& k, const CUtensorMap& v, const PagedParams& p, cudaStream_t st) {
   using T = PagedTile<DP, NT, W>;
   const uint64_t most_units = (uint64_t)paged_units(paged_length(0x7FFFFFFF, p.max_pages, p.page_size), 16 * W) * p.sequences;
-  if (most_units > 0x7FFFFFFFull) return fail(ctx, KB_ERR_UNSUPPORTED, "kb_attention_paged: sequences * max_pages * page_size is beyond 2^37");
+  if (most_units > 0x7FFFFFFFull) return fail(ctx, KB_ERR_UNSUPPORTED, "kb_attention_paged: sequences * max_pages * page_size is beyond 2^36");
   const uint32_t per_seq = p.hkv * p.chunks, pieces = paged_pieces((uint64_t)ctx->sm_count * T::kPerSm, per_seq, most_units);
   return launch_dependent(ctx, attention_paged_kernel<DT, DP, NT, W>, dim3(per_seq, pieces), T::kThreads, T::kSmem, st, k, v, p);
 }
@@ -353,7 +354,8 @@ extern "C" kb_status kb_attention(kb_ctx* ctx, const void* d_q, uint64_t q_row, 
   KB_TRY(check_sizes(ctx, where, q_heads, kv_heads, dim, KB_ATTENTION_MAX_DIM));
   if (dim % 8 != 0) return fail(ctx, KB_ERR_UNSUPPORTED, "%s: dim %u is not a multiple of 8", where, dim);
   if (causal != 0 && causal != 1) return fail(ctx, KB_ERR_INVALID_ARG, "%s: causal must be 0 or 1", where);
-  if (!(scale > 0.0f) || !std::isfinite(scale)) return fail(ctx, KB_ERR_INVALID_ARG, "%s: scale must be finite and > 0", where);
+  const float scale_log2 = (float)(scale * kLog2e);
+  if (!(scale > 0.0f) || !std::isfinite(scale_log2)) return fail(ctx, KB_ERR_INVALID_ARG, "%s: scale must be > 0 and at most 2^127", where);
   if (q_tokens > KB_OPS_MAX_DIM || k_tokens > KB_OPS_MAX_DIM || sequences > KB_OPS_MAX_DIM)
     return fail(ctx, KB_ERR_INVALID_ARG, "%s: tokens or sequences beyond 2^30", where);
   if ((d_q_offsets == nullptr) != (d_k_offsets == nullptr) || (!d_q_offsets && sequences != 1))
@@ -398,7 +400,7 @@ extern "C" kb_status kb_attention(kb_ctx* ctx, const void* d_q, uint64_t q_row, 
   p.pair = p.group % 2 == 0;
   p.causal = causal;
   p.vec_out = aligned16(d_out) && out_row % 8 == 0 && out_head % 8 == 0;
-  p.scale_log2 = (float)((double)scale * 1.4426950408889634);
+  p.scale_log2 = scale_log2;
   p.q = q.p;
   p.k = k.p;
   p.v = v.p;
@@ -443,7 +445,8 @@ extern "C" kb_status kb_attention_paged(kb_ctx* ctx, const void* d_q, uint64_t q
   if (dtype != KB_F16 && dtype != KB_BF16) return fail(ctx, KB_ERR_UNSUPPORTED, "%s: dtype %d is not fp16 or bf16", where, (int)dtype);
   KB_TRY(check_sizes(ctx, where, q_heads, kv_heads, dim, KB_ATTENTION_MAX_DIM));
   if (dim % 8 != 0) return fail(ctx, KB_ERR_UNSUPPORTED, "%s: dim %u is not a multiple of 8", where, dim);
-  if (!(scale > 0.0f) || !std::isfinite(scale)) return fail(ctx, KB_ERR_INVALID_ARG, "%s: scale must be finite and > 0", where);
+  const float scale_log2 = (float)(scale * kLog2e);
+  if (!(scale > 0.0f) || !std::isfinite(scale_log2)) return fail(ctx, KB_ERR_INVALID_ARG, "%s: scale must be > 0 and at most 2^127", where);
   if (sequences > KB_OPS_MAX_DIM) return fail(ctx, KB_ERR_INVALID_ARG, "%s: more than 2^30 sequences", where);
   if (!cache) return fail(ctx, KB_ERR_INVALID_ARG, "%s: cache is NULL", where);
   if (sequences == 0) return KB_OK;
@@ -493,7 +496,7 @@ extern "C" kb_status kb_attention_paged(kb_ctx* ctx, const void* d_q, uint64_t q
   p.group = q_heads / kv_heads;
   p.chunks = p.group > 8 ? (p.group + 15) / 16 : 1;
   p.dim = dim;
-  p.scale_log2 = (float)((double)scale * 1.4426950408889634);
+  p.scale_log2 = scale_log2;
   p.out = d_out;
   p.o_row = out_row;
   p.o_head = out_head;

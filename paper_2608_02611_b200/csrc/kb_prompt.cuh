@@ -32,7 +32,6 @@
 
 namespace kb {
 
-
 struct PromptParams {
   const int *q_offsets, *k_offsets;   // NULL: one sequence of all tokens
   unsigned int* next;                 // [0] items handed out beyond the first of each CTA, [1] CTAs that have ended; 0 between calls
@@ -355,6 +354,8 @@ __global__ void __launch_bounds__(PromptTile<DP>::kThreads, 1)
     abort_word = 0u;
     mbar_fence_init();
   }
+  // before the kernel before this one is over: no CTA with tensor memory of its own runs beside this one, whose
+  // registers leave no room
   if (warp == 1) tmem_alloc<1>(&tmem_base, T::kTmemCols);
   after_the_kernel_before();
   const uint32_t units = p.pair ? p.hq / 2 : p.hq;

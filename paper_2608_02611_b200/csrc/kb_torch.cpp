@@ -344,6 +344,7 @@ uint64_t stride_of(const Call& c, const at::Tensor& t, int64_t axis, int64_t dim
 Heads heads_of(const Call& c, const at::Tensor& t, const char* name) {
   if (t.dim() != 3) refuse(c.where, std::string(name) + " must be [tokens, heads, dim]");
   const int64_t dim = t.size(2);
+  if (t.size(1) > 0x7FFFFFFF || dim > 0x7FFFFFFF) refuse(c.where, std::string(name) + " has more than 2^31 - 1 heads, or elements of one");
   if (dim > 1 && t.numel() && t.stride(2) != 1) refuse(c.where, std::string("the elements of the heads of ") + name + " must be adjacent");
   Heads h{t.size(0), t.size(1), dim, 0, 0, t.data_ptr()};
   h.head = stride_of(c, t, 1, dim, name);

@@ -252,7 +252,7 @@ def test_refusals(ctx):
         dict(q=kw["q"].float()), dict(q=kw["q"].bfloat16()), dict(q=kw["q"][:, :3]), dict(q=kw["q"][:1]), dict(q=kw["q"].cpu()),
         dict(q=kw["q"][..., :60]), dict(k_cache=kw["k_cache"].bfloat16()), dict(k_cache=kw["k_cache"][:, :8]), dict(k_cache=kw["k_cache"][:, :, :1]),
         dict(table=kw["table"].long()), dict(table=kw["table"][:1]), dict(table=kw["table"][0]), dict(lengths=kw["lengths"].long()),
-        dict(lengths=kw["lengths"][:1]), dict(scale=0.0), dict(scale=-1.0), dict(scale=float("inf")), dict(scale=float("nan")),
+        dict(lengths=kw["lengths"][:1]), dict(scale=0.0), dict(scale=-1.0), dict(scale=float("inf")), dict(scale=3e38), dict(scale=float("nan")),
         dict(out=kw["q"].float()), dict(out=kw["q"][:, :2]), dict(out=kw["q"][:, :1].expand(2, 4, 64)),
         dict(q=torch.zeros(2 * 4 * 64 + 1, dtype=torch.float16, device=DEV)[1:].view(2, 4, 64)),          # not on 16 bytes
         dict(q=torch.zeros(2, 4, 136, dtype=torch.float16, device=DEV), k_cache=torch.zeros(2, 16, 2, 136, dtype=torch.float16, device=DEV),

@@ -285,7 +285,7 @@ def test_refusals(ctx):
         dict(q=q.float(), k=k.float(), v=v.float()), dict(q=q.bfloat16()), dict(q=q[:, :3]), dict(q=q.cpu()), dict(q=odd), dict(q=wide, k=wide, v=wide),
         dict(q=q[..., :60], k=k[..., :60], v=v[..., :60]), dict(v=v[:, :1]), dict(v=v[:10]), dict(k=k[:10], v=v[:10]), dict(k=k[..., :56]),
         dict(q_offsets=o.long()), dict(q_offsets=o[:0]), dict(q_offsets=None, k_offsets=o), dict(k_offsets=_offsets([10, 10]).to(DEV)),
-        dict(scale=0.0), dict(scale=float("nan")), dict(scale=-2.0), dict(out=q.float()), dict(out=q[:, :2]), dict(out=q[:1].expand(20, 4, 64)),
+        dict(scale=0.0), dict(scale=float("nan")), dict(scale=-2.0), dict(scale=3e38), dict(out=q.float()), dict(out=q[:, :2]), dict(out=q[:1].expand(20, 4, 64)),
         dict(k=k[:, :1].expand(20, 2, 64)), dict(q=q.transpose(0, 2)), dict(q=q[0]),
     ]
     for change in bad:

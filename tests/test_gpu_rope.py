@@ -129,6 +129,19 @@ def test_stores_in_a_paged_cache(ctx, dtype, heads_first):
     assert b is None and torch.equal(a, qo)
 
 
+def test_slots_that_come_twice_hold_elements_of_their_tokens(ctx):
+    """One after the other in the cache: slot 5 is everyone's, the others' neighbours stay as they were."""
+    tokens = 3000
+    q, k, v = _qkv(tokens, 2, 2, 64, torch.bfloat16, 3)
+    kc, vc = (torch.zeros(2, 16, 2, 64, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    _, ko = ctx.qk_norm_rope(q, k, v=v, k_cache=kc, v_cache=vc, slots=torch.full((tokens,), 5).to(DEV))
+    for cache, rows in ((kc, ko), (vc, v)):
+        assert bool((cache.view(32, 2, 64)[5] == rows).any(0).all())
+        cache[0, 5] = 0
+        assert not bool(cache.any())
+    assert ctx.poll() == 0
+
+
 def test_slots_that_are_not_there_store_nothing_and_show(ctx):
     q, k, v = _qkv(4, 2, 1, 64, torch.bfloat16, 1)
     kc, vc = torch.zeros(3, 16, 1, 64, dtype=torch.bfloat16, device=DEV), torch.zeros(3, 16, 1, 64, dtype=torch.bfloat16, device=DEV)
@@ -192,6 +205,7 @@ def test_refusals(ctx):
         dict(k_cache=cache, v_cache=cache, v=v, slots=slots.int()), dict(k_cache=cache, v_cache=cache.half(), v=v, slots=slots),
         dict(k_cache=cache[:, :, :1], v_cache=cache[:, :, :1], v=v, slots=slots), dict(want_q=False, want_k=False),
         dict(q=q.transpose(0, 2)), dict(out=(q.float(), None)), dict(out=(q[:, :1].expand(4, 4, 64), None)), dict(out=(torch.empty(4, 4, 65, device=DEV, dtype=torch.bfloat16), None)),
+        dict(q=q[:, :1].expand(4, 2 ** 32, 64)),
         dict(q=torch.zeros(4, 4, 257, device=DEV), k=torch.zeros(4, 2, 257, device=DEV), inv_freq=None),
     ]
     for change in bad:
