@@ -39,6 +39,7 @@ struct PromptParams {
   uint32_t hq, group, dim;
   bool pair;                          // tiles are two heads (else: two pieces of 128 queries)
   bool causal, vec_out;
+  uint32_t phase_keys;                // keys of a phase's sequences; 0: all sequences are one phase
   float scale_log2;
   const void *q, *k, *v;              // for repair
   uint64_t q_row, q_head, k_row, k_head, v_row, v_head;
@@ -171,15 +172,17 @@ __device__ __forceinline__ void repair_rows(const PromptParams& p, const PromptI
   }
 }
 
-// Which item has number `it`: a warp's answer.  Up to 32 sequences: the items with the most keys come first, whatever
-// their sequence, so that no CTA begins a long one when the others are about to end.  Piece j of a sequence (128 or 256
+// Which item has number `it`: a warp's answer.  Up to 32 sequences: the items with the most keys of a phase (mostly there is
+// one phase) come first, whatever their sequence, so that no CTA begins a long one when the others are about to end.  Piece j of a sequence (128 or 256
 // queries) is on level base + j of the number of keys (causal), all pieces of it on level base (not causal); the
 // level of item `it` is the largest that has more than `it` items on it or above.  More sequences: one after the
 // other, the later pieces of each first.
 struct PromptSequences {
   uint32_t shift;                 // pieces have 1 << shift queries
   bool causal, held;              // held: all sequences, one per lane
-  uint32_t q0, nq, k0, nk;        // of sequence at + lane
+  uint32_t q0, nq, k0, nk;        // of sequence at + lane; with phases of the lane-th longest
+  uint32_t phase, phase_first;    // of the sequence, and its first piece
+  uint32_t units;                 // heads or pairs of heads of a piece
   uint32_t total, top;            // pieces of all; no level is above
   uint32_t at, before;            // not held: where the search goes on, pieces before that
   __device__ __forceinline__ uint32_t pieces() const { return (nq + (1u << shift) - 1) >> shift; }
@@ -216,11 +219,38 @@ __device__ __forceinline__ void prompt_load(const PromptParams& p, PromptSequenc
   q.k0 = c;
   q.nk = d - c;
 }
+// Sequences in phases, the longest first, each of as many as have about p.phase_keys keys, so that the keys and values that
+// the card is at work on stay in the second-level cache (why and when: prompt_phase_keys).
+__device__ __forceinline__ void prompt_phases(const PromptParams& p, PromptSequences& q, int lane) {
+  const uint32_t key = q.pieces() ? q.base() + q.pieces() : 0u;
+  uint32_t rank = 0;
+#pragma unroll 1
+  for (int j = 0; j < 32; ++j) {
+    const uint32_t other = __shfl_sync(0xFFFFFFFFu, key, j);
+    rank += other > key || (other == key && j < lane) ? 1u : 0u;
+  }
+  PromptSequences sorted = q;
+#pragma unroll 1
+  for (int j = 0; j < 32; ++j) {
+    const bool here = __shfl_sync(0xFFFFFFFFu, rank, j) == (uint32_t)lane;
+    const uint32_t q0 = __shfl_sync(0xFFFFFFFFu, q.q0, j), nq = __shfl_sync(0xFFFFFFFFu, q.nq, j);
+    const uint32_t k0 = __shfl_sync(0xFFFFFFFFu, q.k0, j), nk = __shfl_sync(0xFFFFFFFFu, q.nk, j);
+    if (here) sorted.q0 = q0, sorted.nq = nq, sorted.k0 = k0, sorted.nk = nk;
+  }
+  q = sorted;
+  const uint32_t keys = warp_prefix(q.nk, lane) - q.nk, pieces = warp_prefix(q.pieces(), lane) - q.pieces();   // before this one
+  q.phase = keys / p.phase_keys;
+  const uint32_t before = __shfl_up_sync(0xFFFFFFFFu, q.phase, 1);
+  const uint32_t firsts = __ballot_sync(0xFFFFFFFFu, lane == 0 || before != q.phase);
+  const int first = 31 - __clz(firsts & (0xFFFFFFFFu >> (31 - lane)));   // lane of the phase's first sequence
+  q.phase_first = __shfl_sync(0xFFFFFFFFu, pieces, first);
+}
 __device__ __forceinline__ void prompt_begin(const PromptParams& p, PromptSequences& q, int lane, bool report) {
   q.shift = p.pair ? 7 : 8;
   q.causal = p.causal;
   q.held = p.sequences <= 32;
-  q.total = q.at = q.before = 0;
+  q.total = q.at = q.before = q.phase = q.phase_first = 0;
+  q.units = p.pair ? p.hq / 2 : p.hq;
   bool bad = false;
 #pragma unroll 1
   for (uint32_t s0 = 0; s0 < p.sequences; s0 += 32) {
@@ -228,11 +258,22 @@ __device__ __forceinline__ void prompt_begin(const PromptParams& p, PromptSequen
     q.total += __reduce_add_sync(0xFFFFFFFFu, q.pieces());
   }
   q.top = __reduce_max_sync(0xFFFFFFFFu, q.base() + q.pieces());
-  if (!q.held) prompt_load(p, q, lane, bad);
+  if (!q.held)
+    prompt_load(p, q, lane, bad);
+  else if (p.phase_keys)
+    prompt_phases(p, q, lane);
   if (bad && report) set_status(p.status, (unsigned int)KB_ERR_INVALID_ARG);
 }
-// The sequence and first query of item `it` < total
-__device__ __forceinline__ void prompt_find(const PromptParams& p, PromptSequences& q, uint32_t it, int lane, PromptItem& x) {
+// The sequence, first query and first head of item `number` < total * units
+__device__ __forceinline__ void prompt_find(const PromptParams& p, PromptSequences& q, uint32_t number, int lane, PromptItem& x) {
+  uint32_t it = number / q.units;   // among the pieces of all; below: among those of the phase
+  x.head0 = (number - it * q.units) * (p.pair ? 2 : 1);
+  bool in_phase = true;             // the lane's sequence is
+  if (q.held && p.phase_keys) {
+    const int src = 31 - __clz(__ballot_sync(0xFFFFFFFFu, q.phase_first <= it));   // the last sequence of a phase that has begun by then
+    in_phase = q.phase == __shfl_sync(0xFFFFFFFFu, q.phase, src);
+    it -= __shfl_sync(0xFFFFFFFFu, q.phase_first, src);
+  }
   // items before those of this round, and lane's among them, of which it leaves out the last `over` pieces
   uint32_t before = 0, mine, over = 0;
   if (q.held) {
@@ -240,14 +281,14 @@ __device__ __forceinline__ void prompt_find(const PromptParams& p, PromptSequenc
 #pragma unroll 1
     while (hi - lo > 1) {
       const uint32_t mid = (lo + hi) / 2;
-      if (__reduce_add_sync(0xFFFFFFFFu, q.on_or_above(mid)) > it)
+      if (__reduce_add_sync(0xFFFFFFFFu, in_phase ? q.on_or_above(mid) : 0u) > it)
         lo = mid;
       else
         hi = mid;
     }
-    over = q.on_or_above(lo + 1);
+    over = in_phase ? q.on_or_above(lo + 1) : 0u;
     before = __reduce_add_sync(0xFFFFFFFFu, over);
-    mine = q.on_or_above(lo) - over;
+    mine = in_phase ? q.on_or_above(lo) - over : 0u;
   } else {
 #pragma unroll 1
     for (;;) {
@@ -272,19 +313,16 @@ __device__ __forceinline__ void prompt_find(const PromptParams& p, PromptSequenc
 
 // A warp hands out the CTA's items.  A function of its own: inlined, it took 60 KB of the kernel's instructions, which
 // did not fit their cache any more.
-__device__ __noinline__ void hand_out_items(const PromptParams& p, PromptSequences q, uint32_t units, int lane, PromptItem* items, uint64_t* item_full,
+__device__ __noinline__ void hand_out_items(const PromptParams& p, PromptSequences q, int lane, PromptItem* items, uint64_t* item_full,
                                             uint64_t* item_empty, uint64_t* want, volatile unsigned int* abort_flag) {
-  const uint32_t total = q.total * units;
-  const double per_unit = 1.0 / (double)units;
+  const uint32_t total = q.total * q.units;
   uint32_t number = blockIdx.x;
 #pragma unroll 1
   for (uint32_t taken = 0;;) {
     const uint32_t slot = taken & 1;
     PromptItem x = {};
     if (number < total) {
-      const uint32_t it = (uint32_t)(((double)number + 0.5) * per_unit);   // number / units
-      prompt_find(p, q, it, lane, x);
-      x.head0 = (number - it * units) * (p.pair ? 2 : 1);
+      prompt_find(p, q, number, lane, x);
       x.n[0] = prompt_steps(x.row0, 128, x.nq, x.nk, p.causal);
       x.n[1] = p.pair ? x.n[0] : prompt_steps(x.row0 + 128, 128, x.nq, x.nk, p.causal);
       x.steps = max(x.n[0], x.n[1]);
@@ -358,7 +396,6 @@ __global__ void __launch_bounds__(PromptTile<DP>::kThreads, 1)
   // registers leave no room
   if (warp == 1) tmem_alloc<1>(&tmem_base, T::kTmemCols);
   after_the_kernel_before();
-  const uint32_t units = p.pair ? p.hq / 2 : p.hq;
   PromptSequences q;
   if (warp == 5) prompt_begin(p, q, lane, blockIdx.x == 0);
   tc_fence_before();
@@ -381,7 +418,7 @@ __global__ void __launch_bounds__(PromptTile<DP>::kThreads, 1)
 
   if (warp < 8) regs_shrink<T::kRegsControl>();
   if (warp == 5) {
-    hand_out_items(p, q, units, lane, items, item_full, item_empty, &want, abort_flag);
+    hand_out_items(p, q, lane, items, item_full, item_empty, &want, abort_flag);
   } else if (warp == 0) {
     uint32_t k_issued = 0, v_issued = 0, q_items[2] = {0, 0};
     PromptItem x;

@@ -117,6 +117,33 @@ def test_many_sequences(ctx):
     _check(r, q, k, v, lens, lens, True)
 
 
+@pytest.mark.parametrize("hq,hkv", [(32, 32), (32, 16)])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("lens", [
+    [300, 2100, 0, 1, 1500, 2100, 129, 4000, 64, 777],
+    [16, 5000, 8000],
+    [9000],
+    [340] * 29 + [0, 1, 300],
+])
+def test_more_keys_than_the_cache_holds(ctx, lens, causal, hq, hkv):
+    """Then sequences are worked on in phases, whose order no output shows: each is what a call of its own gives, and some
+    rows are compared with 64 bits."""
+    tokens = sum(lens)
+    assert 4 * tokens * hkv * 128 > 64 << 20
+    q, k, v = (t.to(DEV) for t in _inputs(tokens, tokens, hq, hkv, 128, torch.bfloat16, 5))
+    offsets = _offsets(lens).to(DEV)
+    out = torch.full_like(q, float("nan"))
+    r = ctx.attention(q, k, v, offsets, causal=causal, want_lse=True, out=out)
+    at = 0
+    for n in lens:
+        if n:
+            one = ctx.attention(q[at:at + n], k[at:at + n], v[at:at + n], causal=causal, want_lse=True)
+            assert torch.equal(one.out, out[at:at + n]) and torch.equal(one.lse, r.lse[at:at + n]), (at, n)
+        at += n
+    assert ctx.poll() == 0
+    _check(r, q.cpu(), k.cpu(), v.cpu(), lens, lens, causal, rows=lambda n: [0, n // 2, n - 1] if n else [])
+
+
 @pytest.mark.parametrize("order", ["rising", "falling", "steps"])
 def test_scores_that_rise_and_fall(ctx, order):
     """References that have to be raised tile after tile, by small and by huge amounts."""
