@@ -525,8 +525,11 @@ __global__ void __launch_bounds__(PromptTile<DP>::kThreads, 1)
           wait(&v_full[st], used / kS);
           if (i < n && go) {
             const uint32_t place = done % kP;
-            if (i == 0 && !wait(&o_free[t], q_items + 1)) break;   // the last item's outputs have been read
             if (!wait(&p_full[t][place], done / kP)) break;
+            // The last item's outputs have been read.  Items without steps of this tile skip this wait, so it stands behind the one
+            // for P: that comes from a warpgroup that has waited for the item before the last, and a phase more than one behind
+            // would pass for the next.
+            if (i == 0 && !wait(&o_free[t], q_items + 1)) break;
             tc_fence_after();
 #pragma unroll
             for (uint32_t c = 0; c < kPromptKeys / 64; ++c)

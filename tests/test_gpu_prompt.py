@@ -117,6 +117,25 @@ def test_many_sequences(ctx):
     _check(r, q, k, v, lens, lens, True)
 
 
+@pytest.mark.parametrize("dtype", HALVES)
+@pytest.mark.parametrize("group", [1, 2, 3])
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("lens", LENS + [[1], [900], [40] * 40])
+def test_heads_many_and_few_give_the_same_bits(ctx, lens, dim, group, dtype):
+    """Calls with few items take one tile at a time, others two heads or two pieces: no output shows which.  Values that
+    are not finite lie behind what some queries see."""
+    q, k, v = (t.to(DEV) for t in _inputs(sum(lens), sum(lens), group, 1, dim, dtype, 8))
+    v[-1, :, :3] = float("nan")
+    v[sum(lens) // 2, :, 5] = float("inf")
+    offsets, heads = _offsets(lens).to(DEV), 300 // group
+    many = [t.repeat(1, heads, 1) for t in (q, k, v)]
+    for causal in (True, False):
+        few, all_ = ctx.attention(q, k, v, offsets, causal=causal, want_lse=True), ctx.attention(*many, offsets, causal=causal, want_lse=True)
+        assert torch.equal(few.out.repeat(1, heads, 1).view(torch.int16), all_.out.view(torch.int16))
+        assert torch.equal(few.lse.repeat(1, heads).view(torch.int32), all_.lse.view(torch.int32))
+    assert ctx.poll() == 0
+
+
 @pytest.mark.parametrize("hq,hkv", [(32, 32), (32, 16)])
 @pytest.mark.parametrize("causal", [True, False])
 @pytest.mark.parametrize("lens", [
