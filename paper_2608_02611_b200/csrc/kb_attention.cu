@@ -427,8 +427,17 @@ extern "C" kb_status kb_attention(kb_ctx* ctx, const void* d_q, uint64_t q_row, 
   p.status = ctx->d_status;
   p.next = ctx->d_status + 40;
   // the lengths are the device's: room for every sequence's last, partial piece
-  const uint64_t rows = p.pair ? 128 : 256, pieces = d_q_offsets ? q_tokens / rows + sequences : (q_tokens + rows - 1) / rows;
-  const uint64_t grid = pieces * (p.pair ? q_heads / 2 : q_heads);
+  auto items = [&](uint64_t rows, uint64_t units) { return (d_q_offsets ? q_tokens / rows + sequences : (q_tokens + rows - 1) / rows) * units; };
+  uint64_t grid = p.pair ? items(128, q_heads / 2) : items(256, q_heads);
+  p.second = p.pair ? 0 : 128;
+  // Fewer items than SMs: one tile each, whose steps are shorter with nobody beside them (1 x 1000 tokens of 32 heads on 8 32.6 and
+  // 28.9 us, 128 behind 8192 cached ones 130 and 101, 4096 of 8 heads on 2 72 and 57); with more, two tiles keep the tensor
+  // cores busier (1500 tokens of 32 heads, 192 items: 42 and 57 us).
+  if (grid <= (uint64_t)ctx->sm_count) {
+    p.pair = false;
+    p.second = kPromptNoSecond;
+    grid = items(128, q_heads);
+  }
   if (grid > 0x7FFFFFFFull) return fail(ctx, KB_ERR_UNSUPPORTED, "%s: more than 2^31 - 1 tiles", where);
   const unsigned int n = (unsigned int)std::min<uint64_t>(grid, ctx->sm_count);
   if (dim <= 64)

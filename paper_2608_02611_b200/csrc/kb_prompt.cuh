@@ -2,7 +2,7 @@
 //
 // A CTA takes two tiles of 128 queries against the keys and values that they share, 64 keys at a
 // time: two neighbouring heads of a group at the same 128 queries, or 256 queries of one head where groups
-// are odd.  Per tile and step the tensor cores make S = Q K^T (128 x 64, accumulated in tensor memory), a
+// are odd (where there are fewer such items than SMs: one tile).  Per tile and step the tensor cores make S = Q K^T (128 x 64, accumulated in tensor memory), a
 // warpgroup with one thread per query turns S into P = 2^(S c - r) in registers and writes it back over S
 // in 16 bits, and the tensor cores add P V to the output, which stays in tensor memory to the end.
 // S has two places per tile: the next step's scores are there when a warpgroup is done with this one's, and
@@ -37,7 +37,8 @@ struct PromptParams {
   unsigned int* next;                 // [0] items handed out beyond the first of each CTA, [1] CTAs that have ended; 0 between calls
   uint32_t sequences, q_tokens, k_tokens;
   uint32_t hq, group, dim;
-  bool pair;                          // tiles are two heads (else: two pieces of 128 queries)
+  bool pair;                          // an item's tiles are two heads (else: of one head)
+  uint32_t second;                    // queries from an item's first tile to its second: 0, 128, or kPromptNoSecond
   bool causal, vec_out;
   uint32_t phase_keys;                // keys of a phase's sequences; 0: all sequences are one phase
   float scale_log2;
@@ -50,6 +51,7 @@ struct PromptParams {
 };
 
 constexpr uint32_t kPromptKeys = 64;   // keys of a step
+constexpr uint32_t kPromptNoSecond = 1u << 30;   // past the end of any sequence
 template <int DP>   // dim rounded up to 64 or 128
 struct PromptTile {
   static constexpr uint32_t kChunks = DP / 64;                  // of 64 elements = 128 bytes
@@ -246,7 +248,7 @@ __device__ __forceinline__ void prompt_phases(const PromptParams& p, PromptSeque
   q.phase_first = __shfl_sync(0xFFFFFFFFu, pieces, first);
 }
 __device__ __forceinline__ void prompt_begin(const PromptParams& p, PromptSequences& q, int lane, bool report) {
-  q.shift = p.pair ? 7 : 8;
+  q.shift = p.second == 128 ? 8 : 7;
   q.causal = p.causal;
   q.held = p.sequences <= 32;
   q.total = q.at = q.before = q.phase = q.phase_first = 0;
@@ -324,7 +326,7 @@ __device__ __noinline__ void hand_out_items(const PromptParams& p, PromptSequenc
     if (number < total) {
       prompt_find(p, q, number, lane, x);
       x.n[0] = prompt_steps(x.row0, 128, x.nq, x.nk, p.causal);
-      x.n[1] = p.pair ? x.n[0] : prompt_steps(x.row0 + 128, 128, x.nq, x.nk, p.causal);
+      x.n[1] = p.pair ? x.n[0] : prompt_steps(x.row0 + p.second, 128, x.nq, x.nk, p.causal);
       x.steps = max(x.n[0], x.n[1]);
       x.live = 1;
     }
@@ -433,7 +435,7 @@ __global__ void __launch_bounds__(PromptTile<DP>::kThreads, 1)
         expect_tx_elect(bar, T::kTileBytes);
 #pragma unroll
         for (uint32_t c = 0; c < T::kChunks; ++c)
-          tma_load_3d(smem_u32(base) + t * T::kTileBytes + c * 16384, &map_q, (int)(c * 64), (int)(x.q0 + x.row0 + (p.pair ? 0 : t * 128)),
+          tma_load_3d(smem_u32(base) + t * T::kTileBytes + c * 16384, &map_q, (int)(c * 64), (int)(x.q0 + x.row0 + t * p.second),
                       (int)(x.head0 + (p.pair ? t : 0)), bar);
       }
       auto copy = [&](const CUtensorMap* map, unsigned char* to, uint64_t* full, uint64_t* empty, uint32_t& issued, uint32_t step) {
@@ -565,7 +567,7 @@ __global__ void __launch_bounds__(PromptTile<DP>::kThreads, 1)
 #pragma unroll 1
     while (next_item(x, wait_here)) {
       const uint32_t n = t ? x.n[1] : x.n[0], nq = x.nq, nk = x.nk;
-      const uint32_t row = x.row0 + (p.pair ? 0 : t * 128) + quarter * 32 + lane;
+      const uint32_t row = x.row0 + t * p.second + quarter * 32 + lane;
       const uint32_t seen = row < nq ? prompt_seen(row, nq, nk, p.causal) : 0;
       const uint32_t seen_by_all = __reduce_min_sync(0xFFFFFFFFu, seen);
       float r = -INFINITY, l0 = 0.0f, l1 = 0.0f;
@@ -657,7 +659,7 @@ __global__ void __launch_bounds__(PromptTile<DP>::kThreads, 1)
 #pragma unroll 1
       for (int t = 0; t < 2; ++t) {
         const uint32_t n = t ? x.n[1] : x.n[0], nq = x.nq, h = x.head0 + (p.pair ? t : 0);
-        const uint32_t first = x.row0 + (p.pair ? 0 : t * 128) + quarter * 32, row = first + lane;
+        const uint32_t first = x.row0 + t * p.second + quarter * 32, row = first + lane;
         const uint32_t steps = (t ? done[1] : done[0]) + n;
         if (t)
           done[1] = steps;
