@@ -301,6 +301,32 @@ def test_a_first_call_inside_a_capture_and_on_another_stream():
     c.close()
 
 
+def test_two_contexts_on_two_streams_at_once():
+    """Each has its count of items; calls of one take turns on the card with the other's, products of another kernel with
+    tensor memory among them."""
+    from paper_2608_02611_b200 import binding
+    lens = [900, 3, 400, 0, 257]
+    q, k, v = (t.to(DEV) for t in _inputs(sum(lens), sum(lens), 40, 8, 128, torch.bfloat16, 9))
+    offsets = _offsets(lens).to(DEV)
+    both = [(binding.Context(0), torch.cuda.Stream()) for _ in range(2)]
+    want = both[0][0].attention(q, k, v, offsets, want_lse=True)
+    x, s = both[0][0].quantize_blocks(q.reshape(sum(lens), -1))
+    w, ws = both[0][0].quantize_blocks(torch.randn(512, x.shape[1], device=DEV), tiles=True)
+    product = both[0][0].matmul_blocks(x, s, w, ws)
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(40):
+        for ctx, stream in both:
+            with torch.cuda.stream(stream):
+                got.append((ctx.attention(q, k, v, offsets, want_lse=True), ctx.matmul_blocks(x, s, w, ws)))
+    torch.cuda.synchronize()
+    for r, p in got:
+        assert torch.equal(r.out, want.out) and torch.equal(r.lse, want.lse) and torch.equal(p, product)
+    for ctx, _ in both:
+        assert ctx.poll() == 0
+        ctx.close()
+
+
 def test_no_gradient_and_any_rank_of_inputs_that_require_one(ctx):
     q, k, v = (x.to(DEV).requires_grad_(True) for x in _inputs(20, 20, 2, 1, 64, torch.bfloat16, 3))
     r = ctx.attention(q, k, v, want_lse=True)
