@@ -23,9 +23,9 @@
 // score products run ahead into the next item while the last one's outputs are stored.
 //
 // Bound by the tensor cores and the exponentials together: a step's 4 products of both tiles and its 16384 exponentials take
-// 1024 cycles each, and the two warpgroups, which feed one with the other's results, keep either busy about half of the time (44
-// to 50% in the counters).  16384 tokens of 32 heads on 8, causal: 1950 us (1120 TFLOP/s) in bursts, 2020 under the
-// power cap; 8192 tokens without a mask 915 us (1200 TFLOP/s).
+// 1024 cycles each, and the two warpgroups, which feed one with the other's results, keep either busy 65% of the time
+// in long prompts and 47% in short ones, where items begin and end.  16384 tokens of 32 heads on 8, causal: 1743 us alone at the full
+// clock (1260 TFLOP/s), 2020 in a long run under the power cap, at 1.5 GHz; 8192 tokens without a mask 915 us (1200 TFLOP/s).
 //
 // Roles: warp 0 copies, warps 1 to 4 issue matrix instructions, warp 5 hands out the items, warp 6 zeroes values behind a
 // sequence's end, warps 8 to 11 and 12 to 15 are the tiles' warpgroups, warps 16 to 19 divide and store the outputs of both
