@@ -81,7 +81,7 @@ kb_status kb_qk_norm_rope(kb_ctx* ctx, const void* d_q, uint64_t q_row, uint64_t
  * meets v_j; out is rounded once.  (A score of 2^24 or more in magnitude has no digits behind the point in
  * binary32: what comes of such scores is not defined.)  A query with no score above -infinity (none at all, above all) has
  * out = 0 and lse = -infinity.  Keys and values that a query does not see do not touch its outputs, whatever
- * they hold.
+ * they hold; a value that is not finite makes that element of the queries that see it infinite or NaN.
  *
  *   d_q              DEVICE heads of `dtype` (KB_F16 or KB_BF16), q_tokens of them.
  *   d_k, d_v         DEVICE heads, k_tokens of them.  Pointers of q, k and v 16-byte aligned, row and head

@@ -411,13 +411,7 @@ extern "C" kb_status kb_attention(kb_ctx* ctx, const void* d_q, uint64_t q_row, 
   p.vec_out = aligned16(d_out) && out_row % 8 == 0 && out_head % 8 == 0;
   p.phase_keys = prompt_phase_keys(k_tokens, kv_heads, dim);
   p.scale_log2 = scale_log2;
-  p.q = q.p;
-  p.k = k.p;
   p.v = v.p;
-  p.q_row = q.row;
-  p.q_head = q.head;
-  p.k_row = k.row;
-  p.k_head = k.head;
   p.v_row = v.row;
   p.v_head = v.head;
   p.out = d_out;

@@ -15,9 +15,12 @@
 //
 // What a query does not see never enters its sums: scores behind a mask become -infinity before anything is
 // done with them, and values of keys behind a sequence's end are zeroed in shared memory before they
-// are multiplied (0 times NaN is not 0).  Values of a causal tile's later keys are ordinary numbers in all but
-// broken inputs: where a query's output is not finite although its sum is, the values it does not see are looked
-// at, and if one of them is not finite the query is computed again without them (repair).
+// are multiplied (0 times NaN is not 0).  So are the values that are not finite of an item's last steps, whose keys only some of
+// its queries see (two or three steps of an item, five at most): two warps look at them while the step's scores are
+// worked on, and the queries that see such values get them back as their outputs are stored (add_taken_out).  The cost is the
+// same however long the text is: of 8 x 2048 tokens 384 us, without the look 379; 16384 tokens of 8 heads with a NaN near
+// the end 0.50 ms, without it 0.48.  Looking only where an output is not finite would be free, but the rows would have to be computed
+// again over all their keys (0.83 s for that NaN), or the item a second time, for which each CTA would wait at its end (77 tokens: 8.9 us, so 7.9).
 //
 // CTAs are persistent: one per SM takes items off a common count, those with the most keys first, and its copies and
 // score products run ahead into the next item while the last one's outputs are stored.
@@ -27,9 +30,10 @@
 // in long prompts and 47% in short ones, where items begin and end.  16384 tokens of 32 heads on 8, causal: 1743 us alone at the full
 // clock (1260 TFLOP/s), 2020 in a long run under the power cap, at 1.5 GHz; 8192 tokens without a mask 915 us (1200 TFLOP/s).
 //
-// Roles: warp 0 copies, warps 1 to 4 issue matrix instructions, warp 5 hands out the items, warp 6 zeroes values behind a
-// sequence's end, warps 8 to 11 and 12 to 15 are the tiles' warpgroups, warps 16 to 19 divide and store the outputs of both
-// tiles (4000 cycles per item, in which the tiles' warpgroups begin the next one).  Every wait is bounded.
+// Roles: warp 0 copies, warps 1 to 4 issue matrix instructions, warp 5 hands out the items, warps 6 and 7 look at
+// values, warps 8 to 11 and 12 to 15 are the tiles' warpgroups, warps 16 to 19 divide and store the outputs of both tiles (4000
+// cycles per item, in which the tiles' warpgroups begin the next one).  Every wait is bounded.  The warps' instructions share
+// one cache: the look and the outputs' loop are the shorter for it (8 x 2048 tokens: 388 us with the outputs' 64 columns unrolled, so 384).
 #pragma once
 
 #include "kb_paged.cuh"
@@ -47,8 +51,8 @@ struct PromptParams {
   bool causal, vec_out;
   uint32_t phase_keys;                // keys of a phase's sequences; 0: all sequences are one phase
   float scale_log2;
-  const void *q, *k, *v;              // for repair
-  uint64_t q_row, q_head, k_row, k_head, v_row, v_head;
+  const void* v;                      // for the values that were taken out
+  uint64_t v_row, v_head;
   void* out;
   uint64_t o_row, o_head;
   float* lse;
@@ -128,54 +132,76 @@ struct PromptItem {
   uint32_t q0, nq, k0, nk, row0, head0;   // the sequence, the item's first query and head
   uint32_t n[2];                          // steps of either tile
   uint32_t steps;                         // the larger of the two
+  uint32_t look;                          // from this step on: keys that some query does not see, or behind the sequence's end
   uint32_t live;                          // 0: no more items
 };
-// A warp's 32 queries (from `first` on) of which some, those that `ask`, are not finite although their sums are.  If a
-// value that one of them does not see is not finite (0 times it is NaN), its output once more from global memory, over the
-// keys that it sees alone.
+// True if one of the 16-bit numbers of n vectors of 16 bytes (a multiple of 256) is not finite (a warp's work): 0 times it is NaN.
 template <int DT>
-__device__ __forceinline__ void repair_rows(const PromptParams& p, const PromptItem& x, uint32_t first, uint32_t last, uint32_t h, bool ask,
-                                         uint32_t seen, float r, float by, int lane) {
-  const uint32_t hk = h / p.group, least = __reduce_min_sync(0xFFFFFFFFu, ask ? seen : 0xFFFFFFFFu);
-  uint32_t last_bad = 0;   // 1 + the last key with a value that is not finite, of those some row does not see
+__device__ __forceinline__ bool some_not_finite(const unsigned char* at, uint32_t n, int lane) {
+  uint32_t sum[4] = {0u, 0u, 0u, 0u};
+  auto add = [&](uint32_t& to, uint32_t w) {
+    if constexpr (DT == KB_BF16)
+      asm("fma.rn.bf16x2 %0, %1, %2, %0;" : "+r"(to) : "r"(w), "r"(0u));
+    else
+      asm("fma.rn.f16x2 %0, %1, %2, %0;" : "+r"(to) : "r"(w), "r"(0u));
+  };
 #pragma unroll 1
-  for (uint32_t k = least; k < last; ++k) {
-    bool bad = false;
-#pragma unroll 1
-    for (uint32_t d = lane; d < p.dim; d += 32)
-      bad |= !(fabsf(load_elem<DT>(p.v, (uint64_t)(x.k0 + k) * p.v_row + hk * p.v_head + d)) <= 3.402823466e38f);
-    if (__any_sync(0xFFFFFFFFu, bad)) last_bad = k + 1;
-  }
-  uint32_t todo = __ballot_sync(0xFFFFFFFFu, ask && seen < last_bad);
-  __syncwarp();            // what was stored of these rows comes before what is stored now
-  while (todo) {
-    const int src = __ffs(todo) - 1;
-    todo &= todo - 1;
-    const uint32_t keys = __shfl_sync(0xFFFFFFFFu, seen, src), token = x.q0 + first + src;
-    const float row_r = __shfl_sync(0xFFFFFFFFu, r, src), row_by = __shfl_sync(0xFFFFFFFFu, by, src);
-    const uint64_t qa = token * p.q_row + h * p.q_head;
-    float o[4] = {0.0f, 0.0f, 0.0f, 0.0f};   // elements lane, 32 + lane, ...
-#pragma unroll 1
-    for (uint32_t j0 = 0; j0 < keys; j0 += 32) {
-      float s = 0.0f;
-      if (j0 + lane < keys) {
-        const uint64_t ka = (uint64_t)(x.k0 + j0 + lane) * p.k_row + hk * p.k_head;
-#pragma unroll 1
-        for (uint32_t d = 0; d < p.dim; ++d) s = fmaf(load_elem<DT>(p.q, qa + d), load_elem<DT>(p.k, ka + d), s);
-      }
-      const float e = exp2_fast(fmaf(s, p.scale_log2, -row_r));
-#pragma unroll 1
-      for (uint32_t j = 0; j < 32 && j0 + j < keys; ++j) {
-        const float w = __shfl_sync(0xFFFFFFFFu, e, j);
-        const uint64_t va = (uint64_t)(x.k0 + j0 + j) * p.v_row + hk * p.v_head;
+  for (const unsigned char *v = at + lane * 16, *end = at + n * 16; v < end; v += 8 * 512)
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (i * 32 + lane < (int)p.dim) o[i] = fmaf(w, load_elem<DT>(p.v, va + i * 32 + lane), o[i]);
+    for (uint32_t i = 0; i < 8; ++i) {
+      const uint4 w = *reinterpret_cast<const uint4*>(v + i * 512);
+      add(sum[0], w.x);
+      add(sum[1], w.y);
+      add(sum[2], w.z);
+      add(sum[3], w.w);
+    }
+  return __any_sync(0xFFFFFFFFu, ((sum[0] | sum[1] | sum[2] | sum[3]) & 0x7FFF7FFFu) != 0);   // else zeros of either sign
+}
+// Sets those numbers to zero
+template <int DT>
+__device__ __noinline__ void take_out(unsigned char* at, uint32_t n, int lane) {
+  constexpr uint32_t kInfinity = DT == KB_BF16 ? 0x7F80u : 0x7C00u;
+#pragma unroll 1
+  for (uint32_t i = lane; i < n * 8; i += 32) {
+    unsigned short* e = reinterpret_cast<unsigned short*>(at) + i;
+    if ((*e & kInfinity) == kInfinity) *e = 0;
+  }
+}
+// What the outputs' warps have to know of an item's values
+struct PromptLooked {
+  uint32_t nq, nk, k0, key;   // the sequence; the first key that was looked at
+  uint32_t taken_out[2];      // not 0: the even (odd) places of the ring had values that are not finite
+};
+// 64 columns (from `col` on) of the outputs of a warp's 32 queries (from `first` on; a lane's sum is l) in shared memory: adds
+// the values that are not finite and that the products left out, those of the looked-at keys that a query sees.
+// With one of them the output is infinite or NaN, whatever the probabilities.  Each key is the last that one query sees.
+template <int DT>
+__device__ __forceinline__ void add_taken_out(const PromptParams& p, const PromptLooked& x, uint32_t first, float l, uint32_t h, uint32_t col,
+                                              unsigned char* rows, uint32_t pitch, int lane) {
+  constexpr uint32_t kAtOnce = 4;
+  const uint32_t c = col + 2 * lane, last = prompt_seen(min(first + 31, x.nq - 1), x.nq, x.nk, true);
+  const uint32_t some = __ballot_sync(0xFFFFFFFFu, l != 0.0f);   // nothing is added to the zeros of a query without a sum
+  const unsigned short* v = static_cast<const unsigned short*>(p.v) + (uint64_t)x.k0 * p.v_row + h / p.group * p.v_head + c;
+  float sum[2] = {0.0f, 0.0f};
+#pragma unroll 1
+  for (uint32_t key = x.key; key < last; key += kAtOnce) {
+    uint32_t w[kAtOnce];
+#pragma unroll
+    for (uint32_t u = 0; u < kAtOnce; ++u) w[u] = key + u < last && c < p.dim ? *reinterpret_cast<const uint32_t*>(v + (key + u) * p.v_row) : 0u;
+#pragma unroll
+    for (uint32_t u = 0; u < kAtOnce; ++u) {
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const float one = load_elem<DT>(&w[u], e);
+        if (!(fabsf(one) <= 3.402823466e38f)) sum[e] += one;
+      }
+      const uint32_t row = key + u + x.nq - x.nk - first;   // of the query that sees all up to this key
+      if (row < 32 && (some >> row & 1u) && key + u < last) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+          if (!(sum[e] == 0.0f)) store_elem<DT>(rows + row * pitch, 2 * lane + e, load_elem<DT>(rows + row * pitch, 2 * lane + e) + sum[e]);
       }
     }
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (i * 32 + lane < (int)p.dim) store_elem<DT>(p.out, token * p.o_row + h * p.o_head + i * 32 + lane, o[i] * row_by);
   }
 }
 
@@ -333,6 +359,7 @@ __device__ __noinline__ void hand_out_items(const PromptParams& p, PromptSequenc
       x.n[0] = prompt_steps(x.row0, 128, x.nq, x.nk, p.causal);
       x.n[1] = p.pair ? x.n[0] : prompt_steps(x.row0 + p.second, 128, x.nq, x.nk, p.causal);
       x.steps = max(x.n[0], x.n[1]);
+      x.look = prompt_seen(x.row0, x.nq, x.nk, p.causal) / kPromptKeys;
       x.live = 1;
     }
     if (!wait_warp(&item_empty[slot], ((taken >> 1) & 1u) ^ 1u, abort_flag, p.status)) break;
@@ -362,7 +389,8 @@ __global__ void __launch_bounds__(PromptTile<DP>::kThreads, 1)
   extern __shared__ unsigned char dyn[];
   __shared__ uint64_t q_full[2], q_empty[2], k_full[kS], k_empty[kS], v_full[kS], v_empty[kS], v_tail[kS];
   __shared__ uint64_t s_full[2][kP], p_full[2][kP], o_full[2][kP], item_full[2], item_empty[2], want, drained[5];
-  __shared__ uint64_t sum_full[2], o_free[2];
+  __shared__ uint64_t sum_full[2], o_free[2], looked[4];
+  __shared__ PromptLooked values_of[4];   // by the item's number; looked: it is there
   __shared__ float2 row_sum[2][128];   // r and l of the tiles' queries
   __shared__ PromptItem items[2];
   __shared__ uint32_t tmem_base;
@@ -385,7 +413,7 @@ __global__ void __launch_bounds__(PromptTile<DP>::kThreads, 1)
       mbar_init(&q_full[t], 1);
       mbar_init(&q_empty[t], 1);
       mbar_init(&item_full[t], 1);
-      mbar_init(&item_empty[t], 18);   // warps 0 to 4, 6 and 8 to 19
+      mbar_init(&item_empty[t], 19);   // all warps but the one that hands them out
       mbar_init(&sum_full[t], 4);
       mbar_init(&o_free[t], 4);
       for (uint32_t b = 0; b < kP; ++b) {
@@ -395,6 +423,7 @@ __global__ void __launch_bounds__(PromptTile<DP>::kThreads, 1)
       }
     }
     mbar_init(&want, 1);
+    for (int i = 0; i < 4; ++i) mbar_init(&looked[i], 2);
     for (int i = 1; i < 5; ++i) mbar_init(&drained[i], 1);
     abort_word = 0u;
     mbar_fence_init();
@@ -453,8 +482,8 @@ __global__ void __launch_bounds__(PromptTile<DP>::kThreads, 1)
           tma_load_3d(s + c * T::kChunkBytes, map, (int)(c * 64), (int)(x.k0 + step * kPromptKeys), hk, bar);
         ++issued;
       };
-      // values past the sequence's end have to be zeroed first: warp 6 hands that tile on
-      auto values = [&](uint32_t step) { copy(&map_v, ring_v, (step + 1) * kPromptKeys > x.nk ? v_tail : v_full, v_empty, v_issued, step); };
+      // values that some query does not see have to be looked at first: warps 6 and 7 hand those tiles on
+      auto values = [&](uint32_t step) { copy(&map_v, ring_v, step >= x.look ? v_tail : v_full, v_empty, v_issued, step); };
       if (x.steps) copy(&map_k, ring, k_full, k_empty, k_issued, 0);
 #pragma unroll 1
       for (uint32_t i = 0; i < x.steps && go; ++i) {
@@ -469,25 +498,46 @@ __global__ void __launch_bounds__(PromptTile<DP>::kThreads, 1)
       for (int t = 0; t < 2; ++t) drain_copies(&q_full[t], 1, q_items[t]);
       __syncwarp();
     }
-  } else if (warp == 6) {
-    // values behind a sequence's end are another's, or anything: zeros
+  } else if (warp == 6 || warp == 7) {
+    // Values behind a sequence's end are another's, or anything: zeros.  Those of keys that only some queries see must be finite
+    // where they meet the others' zeros.  Each of the two warps has every other place of the ring, which is every other step, and
+    // always the same ones: a wait that passes over a phase which is not complete would not wait.
+    // (values_of: an item is here once the last warpgroup has taken the item before the last, so what is overwritten was read.)
     uint32_t v_used = 0, phases = 0;
     PromptItem x;
 #pragma unroll 1
     while (next_item(x, wait)) {
-      v_used += x.steps;
-      if (x.steps * kPromptKeys <= x.nk) continue;
-      const uint32_t st = (v_used - 1) % kS, gone = x.steps * kPromptKeys - x.nk, rest = kPromptKeys - gone;
-      if (!wait(&v_tail[st], phases >> st)) continue;
-      phases ^= 1u << st;
+      uint32_t odd = 0;
 #pragma unroll 1
-      for (uint32_t k = lane; k < gone * 8 * T::kChunks; k += 32) {
-        const uint32_t row = rest + (k >> 3) % gone, c = (k >> 3) / gone;
-        *reinterpret_cast<uint4*>(ring_v + st * T::kStepBytes + c * T::kChunkBytes + row * 128 + (k & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+      for (uint32_t i = x.look; i < x.steps; ++i) {
+        const uint32_t st = (v_used + i) % kS, rows = min(kPromptKeys, x.nk - i * kPromptKeys);
+        if (((st ^ warp) & 1) != 0) continue;
+        if (!wait(&v_tail[st], phases >> st)) break;
+        phases ^= 1u << st;
+        unsigned char* tile = ring_v + st * T::kStepBytes;
+        if (rows < kPromptKeys) {
+#pragma unroll 1
+          for (uint32_t k = rows * 8 + lane; k < kPromptKeys * 8; k += 32)
+#pragma unroll
+            for (uint32_t c = 0; c < T::kChunks; ++c) *reinterpret_cast<uint4*>(tile + c * T::kChunkBytes + k * 16) = make_uint4(0u, 0u, 0u, 0u);
+          __syncwarp();
+        }
+        if (p.causal && some_not_finite<DT>(tile, T::kStepBytes / 16, lane)) {
+          take_out<DT>(tile, T::kStepBytes / 16, lane);
+          odd = 1;
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        mbar_arrive_if(&v_full[st], lane == 0);
       }
-      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      v_used += x.steps;
+      PromptLooked& to = values_of[(taken - 1) & 3];
+      if (lane == 0) {
+        if (warp == 6) to.nq = x.nq, to.nk = x.nk, to.k0 = x.k0, to.key = x.look * kPromptKeys;
+        to.taken_out[warp & 1] = odd;
+      }
       __syncwarp();
-      mbar_arrive_if(&v_full[st], lane == 0);
+      if (go) mbar_arrive_if(&looked[(taken - 1) & 3], lane == 0);
     }
   } else if (warp >= 1 && warp < 5) {
     // Four warps issue matrix instructions, so that what one spends on its waits hides under the others' products: warps 1
@@ -661,6 +711,8 @@ __global__ void __launch_bounds__(PromptTile<DP>::kThreads, 1)
     PromptItem x;
 #pragma unroll 1
     while (next_item(x, wait_here)) {
+      if (!wait_here(&looked[items_done & 3], items_done >> 2)) break;
+      const PromptLooked& looked_at = values_of[items_done & 3];
 #pragma unroll 1
       for (int t = 0; t < 2; ++t) {
         const uint32_t n = t ? x.n[1] : x.n[0], nq = x.nq, h = x.head0 + (p.pair ? t : 0);
@@ -680,12 +732,11 @@ __global__ void __launch_bounds__(PromptTile<DP>::kThreads, 1)
         }
         // 128 bytes of 32 rows at a time through shared memory, so that a warp's stores cover whole lines
         const uint32_t mask = none ? 0u : 0xFFFFFFFFu, at_o = tmem + T::kTmemO + t * DP + ((uint32_t)(quarter * 32) << 16);
-        float most = 0.0f;               // largest magnitude, or NaN
         unsigned short* to = static_cast<unsigned short*>(p.out) + (uint64_t)(x.q0 + first + (lane >> 3)) * p.o_row + h * p.o_head + (lane & 7) * 8;
         const int rows_left = (int)(nq - first) - (lane >> 3);
 #pragma unroll 1
         for (int d = 0; d < (int)p.dim && first < nq; d += 64, to += 64) {
-#pragma unroll
+#pragma unroll 1
           for (int e = 0; e < 64; e += 32) {
             float o[32];
             uint32_t w[16];
@@ -696,7 +747,6 @@ __global__ void __launch_bounds__(PromptTile<DP>::kThreads, 1)
 #pragma unroll
             for (int k = 0; k < 32; k += 2) {
               const float a = o[k] * by, b = o[k + 1] * by;
-              most = max3_nan(most, fabsf(a), fabsf(b));
               w[k / 2] = pack2<DT>(a, b) & mask;
             }
 #pragma unroll
@@ -704,6 +754,10 @@ __global__ void __launch_bounds__(PromptTile<DP>::kThreads, 1)
               *reinterpret_cast<uint4*>(rows + lane * T::kOutPitch + e * 2 + u * 16) = make_uint4(w[4 * u], w[4 * u + 1], w[4 * u + 2], w[4 * u + 3]);
           }
           __syncwarp();
+          if (looked_at.taken_out[0] | looked_at.taken_out[1]) {
+            add_taken_out<DT>(p, looked_at, first, l, h, d, rows, T::kOutPitch, lane);
+            __syncwarp();
+          }
           if (d + (lane & 7) * 8 < (int)p.dim) {
             const unsigned char* from = rows + (lane >> 3) * T::kOutPitch + (lane & 7) * 16;
             if (p.vec_out) {
@@ -722,11 +776,6 @@ __global__ void __launch_bounds__(PromptTile<DP>::kThreads, 1)
         __syncwarp();
         mbar_arrive_if(&o_free[t], lane == 0);
         if (in && p.lse) p.lse[(uint64_t)(x.q0 + row) * p.hq + h] = none ? -INFINITY : (r + log2f(l)) * 0.69314718055994531f;
-        // rows that are not finite although their sums are: values that they do not see?
-        const bool odd = !(most <= 3.402823466e38f);
-        const uint32_t last = min(x.nk, n * kPromptKeys), seen = in ? prompt_seen(row, nq, x.nk, p.causal) : 0;
-        const bool ask = in && odd && l > 0.0f && l <= 3.402823466e38f && seen < last;
-        if (__any_sync(0xFFFFFFFFu, ask)) repair_rows<DT>(p, x, first, last, h, ask, seen, r, by, lane);
       }
       if (!go) break;
       ++items_done;
