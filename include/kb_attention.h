@@ -45,13 +45,14 @@ typedef struct {
  *     x = x / sqrt(sum(x^2) / dim + eps) * weight                         (norm = 1; left out with norm = 0)
  *     a' = a cos(w) - b sin(w),  b' = b cos(w) + a sin(w)      w = position[t] * inv_freq[i]
  * for the pairs (a, b) = (x[i], x[i + r/2]), or (x[2i], x[2i + 1]) with interleaved = 1, i < r/2 and
- * r = rotary_dim; the elements from r on are not turned.  The angle is reduced exactly to a
- * part of a turn before it is rounded, so that far positions lose nothing.
+ * r = rotary_dim; the elements from r on are not turned.  The angle is reduced to a part of a turn
+ * before it is rounded: beside that rounding it is off by at most 2^-63 turns times the position (and 2^-74 inv_freq
+ * turns times the position), which is nothing up to positions of 2^36 on either side of 0.
  *
  *   d_q, d_k         DEVICE heads of `dtype` (KB_F32, KB_F16 or KB_BF16); dim 1 .. 256.
  *   norm, eps        eps is finite and > 0 with norm = 1 and not looked at with norm = 0.
  *   d_q_weight, d_k_weight  DEVICE [dim] of `param_dtype` (`dtype` or KB_F32); NULL: 1.
- *   d_positions      DEVICE [tokens], any 64-bit number.
+ *   d_positions      DEVICE [tokens], any 64-bit number (how near far ones come: above).
  *   d_inv_freq       DEVICE [r/2] binary64, radians per position, finite; NULL with r = 0.
  *   rotary_dim       even, 0 .. dim.
  *   d_q_out          DEVICE heads, or NULL.  May be d_q itself, with the same strides.

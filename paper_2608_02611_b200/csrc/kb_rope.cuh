@@ -6,9 +6,12 @@
 // nothing leaves the registers.  The angles are the same for all heads of a token: a CTA works on
 // whole tokens and first puts their cosines and sines into shared memory, one per thread.
 //
-// An angle is position * inv_freq radians, and only its fraction of a turn matters.  inv_freq / (2 pi) is
-// taken to a 64-bit fixed-point fraction; its product with the position, modulo 2^64, is exact, so
-// the error is the fraction's own (2^-53 of it) times the position, whatever the position.  The quarter of the turn
+// An angle is position * inv_freq radians, and only its fraction of a turn matters.  inv_freq / (2 pi) is rounded to
+// binary64, whose fraction of a turn is taken in units of 2^-64; its product with the position, modulo 2^64, is exact.  What the
+// rounding left, at most 2^-53 of the quotient, is taken in binary32, and so is its product with the position.  So
+// the angle is off by 2^-64 of a turn (and 2^-75 of inv_freq) times the position beside what binary32 rounds: by nothing up to 2^36.
+// (The rounding left in binary64, and the digits behind the 64th, would do for any position, but cost 16384 tokens
+// 2.3 us of 93.7 and 1001 tokens 0.6 of 8.3, for registers and their spills.)  The quarter of the turn
 // goes off as an integer and at most an eighth of a turn on either side is left for sincospi.
 #pragma once
 
@@ -43,14 +46,30 @@ constexpr uint32_t kRopeThreads = 256;
 constexpr uint32_t kRopeTokens = 8;       // tokens per CTA, at most
 constexpr uint32_t kRopeMaxHalf = 128;
 
-// cos and sin of the angle position * freq radians
-__host__ __device__ __forceinline__ uint64_t rope_turn(double freq) {   // part of a turn per position, in units of 2^-64
-  const double t = freq * 0.15915494309189533577;   // 1 / (2 pi)
+// freq / (2 pi), rounded: the product by itself, not part of a fused operation
+__host__ __device__ __forceinline__ double rope_quotient(double freq) {
+#ifdef __CUDA_ARCH__
+  return __dmul_rn(freq, 0.15915494309189535);
+#else
+  return freq * 0.15915494309189535;
+#endif
+}
+// The part of a turn per position, in units of 2^-64
+__host__ __device__ __forceinline__ uint64_t rope_turn(double freq) {
+  const double t = rope_quotient(freq);
   const double part = t - floor(t);
   return part < 1.0 ? (uint64_t)(part * 18446744073709551616.0) : 0ull;
 }
+// What the quotient's rounding left, in turns; 1 / (2 pi) in two parts
+__host__ __device__ __forceinline__ float rope_rest(double freq) {
+  return fmaf((float)freq, -9.8393383e-18f, (float)fma(freq, 0.15915494309189535, -rope_quotient(freq)));
+}
+// cos and sin of the angle position * freq radians
 __device__ __forceinline__ float2 rope_cos_sin(long long position, double freq) {
-  const uint64_t turn = (uint64_t)position * rope_turn(freq);
+  if (freq < 0.0) position = (long long)(0ull - (uint64_t)position);   // a fraction a little below 1 would be rounded
+  freq = fabs(freq);
+  const float more = (float)position * rope_rest(freq);
+  const uint64_t turn = (uint64_t)position * rope_turn(freq) + (uint64_t)__float2ll_rn((more - rintf(more)) * 18446744073709551616.0f);
   const uint32_t quarter = (uint32_t)((turn + (1ull << 61)) >> 62);              // 0..3, 4 wraps to 0
   const long long rest = (long long)(turn - ((uint64_t)(quarter & 3u) << 62));   // within an eighth of a turn
   float s, c;
