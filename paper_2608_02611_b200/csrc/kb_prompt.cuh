@@ -676,15 +676,20 @@ __global__ void __launch_bounds__(PromptTile<DP>::kThreads, 1)
         }
         const float minus_r = -known(r);
         uint32_t w[kPromptKeys / 2];
+        float step0, step1;   // this step's sum: a long row's would round each of its numbers to its own, much larger steps
 #pragma unroll
         for (uint32_t k = 0; k < kPromptKeys; k += 2) {
           float &a = s[k], &b = s[k + 1];
           scale_pair(a, b, c, minus_r);
           a = exp2_fast(a);
           b = exp2_fast(b);
-          add_pair(l0, l1, a, b);
+          if (k == 0)
+            step0 = a, step1 = b;
+          else
+            add_pair(step0, step1, a, b);
           w[k / 2] = pack2<DT>(a, b);
         }
+        add_pair(l0, l1, step0, step1);
 #pragma unroll
         for (uint32_t k = 0; k < kPromptKeys / 2; k += 32) tmem_st32(at + k, w + k);
         tmem_wait_st();
