@@ -89,6 +89,7 @@ kb_status kb_qk_norm_rope(kb_ctx* ctx, const void* d_q, uint64_t q_row, uint64_t
  *                    strides multiples of 8, not 0, less than 2^39; dim a multiple of 8 up to 128.
  *   d_q_offsets, d_k_offsets  DEVICE [sequences + 1], ascending, within 0 .. q_tokens (k_tokens); both
  *                    NULL for one sequence of all tokens.  Queries outside every sequence are not written.
+ *   sequences        at most 2^24, of at most 2^24 keys each.
  *   scale            > 0, at most 2^127.
  *   d_out            DEVICE heads of `dtype`; does not overlap the inputs.
  *   d_lse            DEVICE binary32 [q_tokens][q_heads]; NULL: not written. */

@@ -365,8 +365,9 @@ extern "C" kb_status kb_attention(kb_ctx* ctx, const void* d_q, uint64_t q_row, 
   if (causal != 0 && causal != 1) return fail(ctx, KB_ERR_INVALID_ARG, "%s: causal must be 0 or 1", where);
   const float scale_log2 = (float)(scale * kLog2e);
   if (!(scale > 0.0f) || !std::isfinite(scale_log2)) return fail(ctx, KB_ERR_INVALID_ARG, "%s: scale must be > 0 and at most 2^127", where);
-  if (q_tokens > KB_OPS_MAX_DIM || k_tokens > KB_OPS_MAX_DIM || sequences > KB_OPS_MAX_DIM)
-    return fail(ctx, KB_ERR_INVALID_ARG, "%s: tokens or sequences beyond 2^30", where);
+  if (q_tokens > KB_OPS_MAX_DIM || k_tokens > KB_OPS_MAX_DIM || sequences > kPromptMostSequences)
+    return fail(ctx, KB_ERR_INVALID_ARG, "%s: tokens beyond 2^30, or sequences beyond 2^24", where);
+  if (!d_k_offsets && k_tokens > kPromptMostKeys) return fail(ctx, KB_ERR_INVALID_ARG, "%s: a sequence of more than 2^24 keys", where);
   if ((d_q_offsets == nullptr) != (d_k_offsets == nullptr) || (!d_q_offsets && sequences != 1))
     return fail(ctx, KB_ERR_INVALID_ARG, "%s: offsets of queries and keys come together, and without them there is one sequence", where);
   if (q_tokens == 0 || sequences == 0) return KB_OK;

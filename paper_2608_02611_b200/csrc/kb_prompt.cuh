@@ -61,6 +61,10 @@ struct PromptParams {
 
 constexpr uint32_t kPromptKeys = 64;   // keys of a step
 constexpr uint32_t kPromptNoSecond = 1u << 30;   // past the end of any sequence
+// Keys of a sequence, and sequences, at most.  The last warpgroup waits for an item as long as its keys take (16 ns each with two
+// tiles at the clock under the power cap: 0.3 s), the others for the next item as long as empty sequences take to be passed over (32
+// in half a microsecond), and every wait is given up after 2 s.  It also keeps a number of keys and one of queries, added, within an int.
+constexpr uint32_t kPromptMostKeys = 1u << 24, kPromptMostSequences = 1u << 24;
 template <int DP>   // dim rounded up to 64 or 128
 struct PromptTile {
   static constexpr uint32_t kChunks = DP / 64;                  // of 64 elements = 128 bytes
@@ -84,7 +88,7 @@ static_assert(PromptTile<128>::kSmem <= 227 * 1024 - 1024, "shared memory");
 // their place plus nk - nq.
 __host__ __device__ __forceinline__ uint32_t prompt_steps(uint32_t row, uint32_t rows, uint32_t nq, uint32_t nk, bool causal) {
   if (row >= nq || rows == 0) return 0;
-  const int last = (int)(row + rows < nq ? row + rows : nq);           // all of these are at most 2^30
+  const int last = (int)(row + rows < nq ? row + rows : nq);           // nq at most 2^30, nk kPromptMostKeys
   const int seen = causal ? min(last + (int)nk - (int)nq, (int)nk) : (int)nk;
   return seen <= 0 ? 0u : ((uint32_t)seen + kPromptKeys - 1) / kPromptKeys;
 }
@@ -243,7 +247,7 @@ __device__ __forceinline__ void prompt_load(const PromptParams& p, PromptSequenc
     return;
   }
   const int a = p.q_offsets[s], b = p.q_offsets[s + 1], c = p.k_offsets[s], d = p.k_offsets[s + 1];
-  if (a < 0 || a > b || (uint32_t)b > p.q_tokens || c < 0 || c > d || (uint32_t)d > p.k_tokens) {
+  if (a < 0 || a > b || (uint32_t)b > p.q_tokens || c < 0 || c > d || (uint32_t)d > p.k_tokens || (uint32_t)(d - c) > kPromptMostKeys) {
     bad = true;
     return;
   }
