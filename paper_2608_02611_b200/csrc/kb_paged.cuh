@@ -141,10 +141,12 @@ __global__ void __launch_bounds__(32 * W, 8 / W)
   volatile unsigned int* abort_flag = &abort_word;
   unsigned char* base = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(dyn) + 1023) & ~(uintptr_t)1023);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-  if (threadIdx.x < W * kS) mbar_init(&full[threadIdx.x / kS][threadIdx.x % kS], 1);
+  if (threadIdx.x < W * kS) {
+    mbar_init(&full[threadIdx.x / kS][threadIdx.x % kS], 1);
+    mbar_fence_init();   // each thread's own barrier, for the copies
+  }
   if (threadIdx.x == 0) {
     abort_word = 0u;
-    mbar_fence_init();
     prefetch_map(&map_k);
     prefetch_map(&map_v);
   }
