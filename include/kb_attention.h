@@ -59,7 +59,8 @@ typedef struct {
  *   d_k_out          the same for the keys.
  *   cache, d_slots   NULL, or where the turned keys and the values d_v go as well: DEVICE [tokens] slots;
  *                    a negative one stores nothing.  Each slot comes once; in one that comes twice
- *                    the elements are one token's or the other's, each by itself.
+ *                    the elements are one token's or the other's, each by itself.  Slots and heads of the
+ *                    cache do not overlap (strides that let them are refused).
  *   d_v              DEVICE heads of the values; NULL without a cache.
  * At least one of d_q_out, d_k_out and cache is not NULL. */
 kb_status kb_qk_norm_rope(kb_ctx* ctx, const void* d_q, uint64_t q_row, uint64_t q_head, uint32_t q_heads,

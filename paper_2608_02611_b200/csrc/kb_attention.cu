@@ -30,12 +30,26 @@ kb_status check_heads(kb_ctx* ctx, const char* where, const Heads& t, int bytes)
     return fail(ctx, KB_ERR_INVALID_ARG, "%s: a stride of %s is beyond 2^40 elements", where, t.name);
   return KB_OK;
 }
+// No two rows of dim elements are one where axes of these lengths and strides lie within each other, in whatever order
+struct Axis {
+  uint64_t n, stride;
+};
+template <size_t N>
+bool rows_apart(Axis (&axes)[N], uint64_t dim) {
+  std::sort(axes, axes + N, [](const Axis& a, const Axis& b) { return a.stride < b.stride; });
+  unsigned __int128 extent = dim;
+  for (const Axis& a : axes) {
+    if (a.n <= 1) continue;
+    if (a.stride < extent) return false;
+    extent += (unsigned __int128)(a.n - 1) * a.stride;
+  }
+  return true;
+}
 // The same for an output, no two elements of which may be one
 kb_status check_out(kb_ctx* ctx, const char* where, const Heads& t, uint64_t tokens, uint64_t heads, uint64_t dim, int bytes) {
   KB_TRY(check_heads(ctx, where, t, bytes));
-  const bool by_row = (tokens <= 1 || t.row >= (heads - 1) * t.head + dim) && (heads <= 1 || t.head >= dim);
-  const bool by_head = (heads <= 1 || t.head >= (tokens - 1) * t.row + dim) && (tokens <= 1 || t.row >= dim);
-  if (!by_row && !by_head) return fail(ctx, KB_ERR_INVALID_ARG, "%s: the strides of %s let its rows overlap", where, t.name);
+  Axis axes[2] = {{tokens, t.row}, {heads, t.head}};
+  if (!rows_apart(axes, dim)) return fail(ctx, KB_ERR_INVALID_ARG, "%s: the strides of %s let its rows overlap", where, t.name);
   return KB_OK;
 }
 // Rows start on 16-byte boundaries
@@ -288,6 +302,9 @@ extern "C" kb_status kb_qk_norm_rope(kb_ctx* ctx, const void* d_q, uint64_t q_ro
   if (cache) {
     KB_TRY(check_heads(ctx, where, {"d_v", d_v, v_row, v_head}, e));
     KB_TRY(check_cache(ctx, where, *cache, e));
+    Axis k_axes[3] = {{cache->pages, cache->k_page}, {cache->page_size, cache->k_row}, {kv_heads, cache->k_head}};
+    Axis v_axes[3] = {{cache->pages, cache->v_page}, {cache->page_size, cache->v_row}, {kv_heads, cache->v_head}};
+    if (!rows_apart(k_axes, dim) || !rows_apart(v_axes, dim)) return fail(ctx, KB_ERR_INVALID_ARG, "%s: the strides of the cache let its slots overlap", where);
     if (!d_slots) return fail(ctx, KB_ERR_INVALID_ARG, "%s: a cache without d_slots", where);
     if (!aligned_to(d_slots, 8)) return fail(ctx, KB_ERR_ALIGNMENT, "%s: d_slots is not aligned to its element type", where);
   }
