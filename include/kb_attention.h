@@ -3,10 +3,11 @@
  * of queries and keys with the position rotation, attention over whole prompts, attention of one new
  * token over a paged cache.
  *
- * Attention is one of the workloads whose kernels the paper searches (SDPAttn, Appendix "Benchmark
- * Descriptions and Shapes") and what the gate's third workload is modelled on; like the calls of
- * kb_ops.h these make reference outputs and a baseline kernel for such candidates.  The conventions of
- * kb.h and kb_ops.h hold.  They are a serving path's forms: no call here has a gradient.  In addition:
+ * The gate's third workload is modelled on an attention output of 32 heads of 128; these calls make such outputs
+ * and a baseline kernel to compare candidates' times with.  (Attention is also one of the workloads whose kernels the
+ * paper searches, SDPAttn in Appendix "Benchmark Descriptions and Shapes", with heads of 1024: those are beyond
+ * KB_ATTENTION_MAX_DIM and are refused.)  The conventions of kb.h and kb_ops.h hold.  They are a serving
+ * path's forms: no call here has a gradient.  In addition:
  *   - Heads of a packed batch are [tokens][heads][dim]: the elements of dim are adjacent, and the
  *     strides between tokens (..._row) and heads (..._head) are free, in elements.  Slices of one
  *     projection [tokens][(q_heads + 2 kv_heads) dim] are such tensors.
@@ -80,8 +81,9 @@ kb_status kb_qk_norm_rope(kb_ctx* ctx, const void* d_q, uint64_t q_row, uint64_t
  *     s_j = scale * sum_d q[d] k_j[d];   lse = log sum_j exp(s_j);   out = sum_j exp(s_j - lse) v_j
  * Products of 16-bit numbers are added in binary32 on the tensor cores, exponentials and their sum are
  * binary32, and exp(s_j - ...) is rounded to `dtype` (relative to a running largest value) before it
- * meets v_j; out is rounded once.  (A score of 2^24 or more in magnitude has no digits behind the point in
- * binary32: what comes of such scores is not defined.)  A query with no score above -infinity (none at all, above all) has
+ * meets v_j; out is rounded once.  (The largest exponential of a query is between 2^7 and 2^15 there, so that bfloat16
+ * values of 2^112 and more, over the number of keys, can make a sum infinite.  A score of 2^24 or more in magnitude has no
+ * digits behind the point in binary32: what comes of such scores is not defined.)  A query with no score above -infinity (none at all, above all) has
  * out = 0 and lse = -infinity.  Keys and values that a query does not see do not touch its outputs, whatever
  * they hold; a value that is not finite makes that element of the queries that see it infinite or NaN.
  *

@@ -4,7 +4,7 @@
  * product of two such operands.
  *
  * The paper searches kernels for operators of models (Appendix "Benchmark Descriptions and Shapes":
- * RMSNorm, LinearReLUDiv, attention and others; of those only attention is here, in kb_attention.h).  The calls of kb.h compare and
+ * RMSNorm, LinearReLUDiv, attention and others; of those only attention is here, in kb_attention.h, with heads of up to 128).  The calls of kb.h compare and
  * rank candidates; these calls make, in the gate's own storage types, the operands and a baseline kernel
  * for candidates of a linear layer in 8 bits.  They compute what they are asked for and nothing else:
  * gradients come from the backward calls, not from a framework's bookkeeping.

@@ -736,7 +736,7 @@ def qk_norm_rope(self, q: torch.Tensor, k: torch.Tensor, positions: Optional[tor
     """kb_qk_norm_rope -> (q, k): each head of ``q`` [tokens, q heads, dim] and ``k`` [tokens, kv heads, dim] divided by
     its root mean square (unless ``norm`` is false) and turned by its token's position.
 
-    ``positions`` int64 [tokens]; ``inv_freq`` float64 [pairs], radians per position, turns the first 2 * pairs elements:
+    ``positions`` int64 [tokens] (angles lose nothing up to 2**36); ``inv_freq`` float64 [pairs], radians per position, turns the first 2 * pairs elements:
     halves against each other, or neighbours with ``interleaved``; None turns nothing.  With ``k_cache`` and ``v_cache``
     [pages, page size, kv heads, dim] the turned keys and ``v`` also go to ``slots`` (int64 [tokens]: page * page size +
     place on it; negative: not stored).  ``want_q``/``want_k`` false: that output is None and is not computed, or only
@@ -756,7 +756,7 @@ def attention(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_offsets
     (``q_offsets`` unless given; one sequence of all tokens without either); its last query sees all of its
     keys and each earlier one a key less, unless ``causal`` is false.  ``scale`` is 1 / sqrt(dim) unless given.
     lse: float32 [tokens, q heads].  Queries that see nothing give zeros and -infinity; rows of the outputs
-    outside every sequence are not written.
+    outside every sequence are not written.  ``out`` does not overlap the inputs; a sequence has at most 2**24 keys.
     """
     return AttentionResult(*(_native_module or _native()).attention(self._h, self.device.index, q, k, v, q_offsets, k_offsets, causal,
                                                                     scale, want_lse, out))

@@ -187,9 +187,10 @@ kb_status launch_paged(kb_ctx* ctx, const CUtensorMap& k, const CUtensorMap& v, 
   return launch_dependent(ctx, attention_paged_kernel<DT, DP, NT, W>, dim3(per_seq, pieces), T::kThreads, T::kSmem, st, k, v, p);
 }
 // Four warps and two CTAs per SM instead of eight and one where there are enough sequences to fill the card: what a CTA does
-// between two sequences then hides under its neighbour's copies (256 x 200 keys of 8 heads 58 us, with eight warps 72;
-// 64 sequences of 1 to 16384 keys 78.5 and 85; 128 x 4096 keys 347 and 340).  For fewer the parts would be more and a
-// CTA's share of a long sequence later (one of 8192 keys 18.7 us and 16.5; 7 of up to 3001 keys 22.4 and 16.8).
+// between two sequences then hides under its neighbour's copies (of 8 heads: 256 x 200 keys 55 us, with eight warps 72; 128 x 200 31 and
+// 38.5; 32 x 200 9.4 and 11.3; 64 sequences of 1 to 16384 keys 78.5 and 85).  For fewer the parts would be more and a
+// CTA's share of a long sequence later (one of 8192 keys 18.7 us and 16.5; 7 of up to 3001 keys 22.4 and 16.8; 16 x 200 9.9 and 7.5, 18 x 1000
+// 16.5 and 14.6).  Not everything past the border gains: 20 x 200 13.7 us and 12.3, 128 x 1000 93 and 88, 128 x 4096 337 and 331.
 bool paged_in_fours(const kb_ctx* ctx, const PagedParams& p) {
   return (uint64_t)p.sequences * p.hkv * p.chunks >= (uint64_t)ctx->sm_count;
 }
@@ -244,8 +245,8 @@ kb_status prepare_prompt(kb_ctx* ctx) {
 // Keys of a phase (prompt_phases).  Items in the order of their lengths alone, whatever their sequence, keep the card even to the
 // end, but go through all keys and values once per length: past the second-level cache (126 MB, whose halves both hold
 // what both halves of the card read) those come from memory each time.  8 x 2048 tokens of 32 heads read 1309 MB then, in phases
-// of 32 MB 455 MB (416 and 381 us; 8 x 4096 of 32 heads on 8: 1252 and 1175).  Up to 64 MB they stay there as it is, and phases
-// only make the end less even (13 sequences with 43 MB: 258 and 263 us).
+// of 32 MB 455 MB (327 us and 317; 8 x 4096 of 32 heads on 8: 1043 and 985; 8 x 2048 on 16, 134 MB: 312 to 318 and 319 to 353, 16 x 1024 of 32 heads 245
+// and 243).  Up to 64 MB they stay there as it is (13 sequences with 43 MB: 272 us, in phases 259 to 268).  By the tensors' sizes, like the tiles.
 uint32_t prompt_phase_keys(uint64_t keys, uint64_t kv_heads, uint64_t dim) {
   const uint64_t bytes = 2 * 2 * kv_heads * dim;   // of a key and its value
   return keys * bytes <= (64u << 20) ? 0u : (uint32_t)std::max<uint64_t>(1, (32u << 20) / bytes);
@@ -442,9 +443,9 @@ extern "C" kb_status kb_attention(kb_ctx* ctx, const void* d_q, uint64_t q_row, 
   auto items = [&](uint64_t rows, uint64_t units) { return (d_q_offsets ? q_tokens / rows + sequences : (q_tokens + rows - 1) / rows) * units; };
   uint64_t grid = p.pair ? items(128, q_heads / 2) : items(256, q_heads);
   p.second = p.pair ? 0 : 128;
-  // Fewer items than SMs: one tile each, whose steps are shorter with nobody beside them (1 x 1000 tokens of 32 heads on 8 32.6 and
-  // 28.9 us, 128 behind 8192 cached ones 130 and 101, 4096 of 8 heads on 2 72 and 57); with more, two tiles keep the tensor
-  // cores busier (1500 tokens of 32 heads, 192 items: 42 and 57 us).
+  // Fewer items than SMs: one tile each, whose steps are shorter with nobody beside them (1000 tokens of 32 heads on 8 25 us, in
+  // twos 30; 1152, 144 items, 28 and 30; 128 behind 8192 cached ones 97 and 131; 4096 of 8 heads on 2 54 and 72); with more, two tiles keep the
+  // tensor cores busier (1280 tokens, 160 items: 32 us, one by one 45; 1500 40 and 51).  By the tensors' sizes, of which lengths on the device may use less.
   if (grid <= (uint64_t)ctx->sm_count) {
     p.pair = false;
     p.second = kPromptNoSecond;

@@ -26,8 +26,8 @@
 // both places.
 // The 8-column tile of the instruction holds the heads: fewer than 8 waste matrix work, which is not
 // what bounds this kernel.  The exponentials are relative to a running value that is raised only where
-// a score exceeds it by more than 2^kLazy; p is rounded to the storage type for the matrix
-// instruction, the sum of the rounded p is kept in binary32.
+// a score, in powers of two, is more than kLazy above the largest there was when it was last raised; p is rounded to the
+// storage type for the matrix instruction, the sum is of p before that, in binary32.
 #pragma once
 
 #include "kb_block8.cuh"

@@ -9,9 +9,9 @@
 // no product waits for the one before it (one place for 128 keys: 3830 cycles for 128 keys of both tiles, of which the
 // warpgroups computed for 1720 and waited for the rest).
 //
-// The running reference r of a query (shared with the paged kernel: kRoom, kLazy) is raised only where a score
-// exceeds it by more than 2^kLazy, so the output in tensor memory is rescaled a few times per query and
-// not once per step.
+// The running reference r of a query (shared with the paged kernel: kRoom, kLazy) is raised only where a score, in powers of
+// two, is more than kLazy above the largest there was when it was last raised (kRoom + kLazy above r), so the output in
+// tensor memory is rescaled a few times per query and not once per step.
 //
 // What a query does not see never enters its sums: scores behind a mask become -infinity before anything is
 // done with them, and values of keys behind a sequence's end are zeroed in shared memory before they
@@ -26,9 +26,9 @@
 // score products run ahead into the next item while the last one's outputs are stored.
 //
 // Bound by the tensor cores and the exponentials together: a step's 4 products of both tiles and its 16384 exponentials take
-// 1024 cycles each, and the two warpgroups, which feed one with the other's results, keep either busy 65% of the time
-// in long prompts and 47% in short ones, where items begin and end.  16384 tokens of 32 heads on 8, causal: 1743 us alone at the full
-// clock (1260 TFLOP/s), 2020 in a long run under the power cap, at 1.5 GHz; 8192 tokens without a mask 915 us (1200 TFLOP/s).
+// 1024 cycles each, and the two warpgroups, which feed one with the other's results, keep either busy 63% of the time
+// in long prompts and 45% in short ones, where items begin and end.  16384 tokens of 32 heads on 8, causal: 1787 us alone at the full
+// clock (1230 TFLOP/s), 2040 in a long run under the power cap, at 1.5 GHz; 8192 tokens without a mask 900 us (1220 TFLOP/s).
 //
 // Roles: warp 0 copies, warps 1 to 4 issue matrix instructions, warp 5 hands out the items, warps 6 and 7 look at
 // values, warps 8 to 11 and 12 to 15 are the tiles' warpgroups, warps 16 to 19 divide and store the outputs of both tiles (4000
@@ -59,7 +59,7 @@ struct PromptParams {
   unsigned int* status;
 };
 
-constexpr uint32_t kPromptKeys = 64;   // keys of a step
+constexpr uint32_t kPromptKeys = 64;   // keys of a step: two reads of tensor memory, one block of a product's contraction
 constexpr uint32_t kPromptNoSecond = 1u << 30;   // past the end of any sequence
 // Keys of a sequence, and sequences, at most.  The last warpgroup waits for an item as long as its keys take (16 ns each with two
 // tiles at the clock under the power cap: 0.3 s), the others for the next item as long as empty sequences take to be passed over (32
@@ -210,7 +210,9 @@ __device__ __forceinline__ void add_taken_out(const PromptParams& p, const Promp
 }
 
 // Which item has number `it`: a warp's answer.  Up to 32 sequences: the items with the most keys of a phase (mostly there is
-// one phase) come first, whatever their sequence, so that no CTA begins a long one when the others are about to end.  Piece j of a sequence (128 or 256
+// one phase) come first, whatever their sequence, so that no CTA begins a long one when the others are about to end (8192 tokens of
+// 32 heads on 8 in 8, 16 and 32 equal prompts 102, 79 and 66 us, one after the other 114, 91 and 74; of ragged lengths 165, 109 and 97, 195, 124
+// and 114).  Piece j of a sequence (128 or 256
 // queries) is on level base + j of the number of keys (causal), all pieces of it on level base (not causal); the
 // level of item `it` is the largest that has more than `it` items on it or above.  More sequences: one after the
 // other, the later pieces of each first.
@@ -552,8 +554,8 @@ __global__ void __launch_bounds__(PromptTile<DP>::kThreads, 1)
     if (warp < 3) {
       const uint32_t idesc = mma_idesc_f16(DT == KB_BF16, false, 128, kPromptKeys);
       const uint32_t a = smem_u32(base) + t * T::kTileBytes;
-  #pragma unroll 1
-    while (next_item(x, wait)) {
+#pragma unroll 1
+      while (next_item(x, wait)) {
         const uint32_t n = t ? x.n[1] : x.n[0];
         if (n) wait(&q_full[t], q_items++);
 #pragma unroll 1
@@ -577,8 +579,8 @@ __global__ void __launch_bounds__(PromptTile<DP>::kThreads, 1)
       }
     } else {
       const uint32_t idesc = mma_idesc_f16(DT == KB_BF16, true, 128, DP);
-  #pragma unroll 1
-    while (next_item(x, wait)) {
+#pragma unroll 1
+      while (next_item(x, wait)) {
         const uint32_t n = t ? x.n[1] : x.n[0];
 #pragma unroll 1
         for (uint32_t i = 0; i < x.steps && go; ++i, ++used) {
@@ -592,10 +594,8 @@ __global__ void __launch_bounds__(PromptTile<DP>::kThreads, 1)
             // would pass for the next.
             if (i == 0 && !wait(&o_free[t], q_items + 1)) break;
             tc_fence_after();
-#pragma unroll
-            for (uint32_t c = 0; c < kPromptKeys / 64; ++c)
-              mma_f16_block_ts(tmem + T::kTmemO + t * DP, tmem + T::kTmemS + t * 128 + place * kPromptKeys + c * 32,
-                               smem_desc_n128(v + c * 8192, T::kChunkBytes), idesc, i > 0 || c > 0);
+            mma_f16_block_ts(tmem + T::kTmemO + t * DP, tmem + T::kTmemS + t * 128 + place * kPromptKeys, smem_desc_n128(v, T::kChunkBytes),
+                             idesc, i > 0);
             mma_commit(&o_full[t][place]);
             ++done;
           }
@@ -636,13 +636,9 @@ __global__ void __launch_bounds__(PromptTile<DP>::kThreads, 1)
         if (!wait_here(&s_full[t][place], done / kP)) break;
         tc_fence_after();
         float s[kPromptKeys];
-#pragma unroll
-        for (uint32_t k = 0; k < kPromptKeys; k += 64) {
-          tmem_ld32(at + k, s + k);
-          tmem_ld32(at + k + 32, s + k + 32);
-        }
-#pragma unroll
-        for (uint32_t k = 0; k < kPromptKeys; k += 64) tmem_wait_ld64(s + k);
+        tmem_ld32(at, s);
+        tmem_ld32(at + 32, s + 32);
+        tmem_wait_ld64(s);
         if ((i + 1) * kPromptKeys > seen_by_all) {
           const int left = (int)seen - (int)(i * kPromptKeys);   // keys of this step that the query sees
 #pragma unroll
@@ -680,7 +676,9 @@ __global__ void __launch_bounds__(PromptTile<DP>::kThreads, 1)
         }
         const float minus_r = -known(r);
         uint32_t w[kPromptKeys / 2];
-        float step0, step1;   // this step's sum: a long row's would round each of its numbers to its own, much larger steps
+        // This step's sum: a long row's would round each of its numbers to its own, much larger steps (lse of 131072 keys alike off by
+        // 6e-4).  It costs 16384 tokens of dim 128 2040 us, without it 1992, and 4 x 4096 of dim 64 433 us and 419.
+        float step0, step1;
 #pragma unroll
         for (uint32_t k = 0; k < kPromptKeys; k += 2) {
           float &a = s[k], &b = s[k + 1];
@@ -694,8 +692,7 @@ __global__ void __launch_bounds__(PromptTile<DP>::kThreads, 1)
           w[k / 2] = pack2<DT>(a, b);
         }
         add_pair(l0, l1, step0, step1);
-#pragma unroll
-        for (uint32_t k = 0; k < kPromptKeys / 2; k += 32) tmem_st32(at + k, w + k);
+        tmem_st32(at, w);
         tmem_wait_st();
         tc_fence_before();
         __syncwarp();

@@ -112,8 +112,9 @@ __device__ __forceinline__ float rope_weight(const RopeParams& p, const void* w,
 // of neighbours, 8 c .. + 7.  A warp takes 32 / L heads of one kind through the CTA's tokens, four of whose loads are
 // under way before the first is used; what depends on the head (weights, addresses but for a step per token) is
 // done once for them.  16384 tokens of 32 + 8 + 8 heads of 128, bf16, stored in a cache: a row at a time 176 us;
-// heads in turn, which had to be told apart for every row (240 instructions for 512 bytes), 121 us; so 94.5 (4.6 TB/s;
-// issue slots 64% busy), in binary32 without a cache 119 (5.6 TB/s).
+// heads in turn, which had to be told apart for every row (240 instructions for 512 bytes), 121 us; so 94 (4.6 TB/s; issue
+// slots 70% busy, with 43% of the warps, of 64 registers), in binary32 without a cache 115 (5.8 TB/s; there some 100 bytes of the
+// registers spill).
 __device__ __forceinline__ void vec_words(uint2 v, uint32_t* w) { w[0] = v.x, w[1] = v.y; }
 __device__ __forceinline__ void vec_words(uint4 v, uint32_t* w) { w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w; }
 __device__ __forceinline__ void words_vec(const uint32_t* w, uint2& v) { v = make_uint2(w[0], w[1]); }
